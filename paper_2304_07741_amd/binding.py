@@ -28,6 +28,19 @@ TEMPLATE_EXPORTS = ["canvas_template_parse", "canvas_template_query", "canvas_te
 CANVAS_MAX_VARS = 8
 # include/canvas_block.h
 BLOCK_EXPORTS = ["canvas_block_compile", "canvas_block_query", "canvas_block_forward", "canvas_block_backward", "canvas_block_destroy"]
+# include/canvas_norm.h
+NORM_EXPORTS = ["canvas_norm_compile", "canvas_norm_query", "canvas_norm_forward", "canvas_norm_backward", "canvas_norm_destroy"]
+CANVAS_NORM_POST, CANVAS_NORM_PRE = 1, 2
+CANVAS_NORM_MAX_CHANNELS = 16384
+CANVAS_GATE_NONE, CANVAS_GATE_SIGMOID, CANVAS_GATE_SILU = 0, 1, 2
+# include/canvas_logprob.h
+LOGPROB_EXPORTS = ["canvas_logprob_compile", "canvas_logprob_query", "canvas_logprob_forward", "canvas_logprob_backward", "canvas_logprob_destroy"]
+CANVAS_LOGPROB_MAX_TOP = 64
+# include/canvas_ortho.h
+ORTHO_EXPORTS = ["canvas_ortho_compile", "canvas_ortho_query", "canvas_ortho_step", "canvas_ortho_destroy"]
+CANVAS_ORTHO_NESTEROV = 1
+CANVAS_ORTHO_MAX_SIDE = 16384
+CANVAS_ORTHO_MAX_STEPS = 16
 
 
 class CanvasOptions(ctypes.Structure):
@@ -53,6 +66,21 @@ class CanvasBlockInfo(ctypes.Structure):
     _fields_ = [("instances", ctypes.c_int32), ("expand", ctypes.c_int32), ("template_channels", ctypes.c_int64),
                 ("n_weights", ctypes.c_int32), ("reserved0", ctypes.c_int32), ("workspace_bytes", ctypes.c_uint64),
                 ("plan", CanvasDagInfo)]
+
+
+class CanvasNormInfo(ctypes.Structure):
+    _fields_ = [("n_launches_fwd", ctypes.c_int32), ("n_launches_bwd", ctypes.c_int32), ("workspace_bytes", ctypes.c_uint64),
+                ("min_bytes_fwd", ctypes.c_double), ("min_bytes_bwd", ctypes.c_double)]
+
+
+class CanvasLogprobInfo(ctypes.Structure):
+    _fields_ = [("n_launches_fwd", ctypes.c_int32), ("n_launches_bwd", ctypes.c_int32), ("workspace_bytes", ctypes.c_uint64),
+                ("min_bytes_fwd", ctypes.c_double), ("min_bytes_bwd", ctypes.c_double)]
+
+
+class CanvasOrthoInfo(ctypes.Structure):
+    _fields_ = [("n_launches", ctypes.c_int32), ("reserved0", ctypes.c_int32), ("workspace_bytes", ctypes.c_uint64),
+                ("flops", ctypes.c_double), ("min_bytes", ctypes.c_double)]
 
 
 class CanvasTarget(ctypes.Structure):
@@ -122,6 +150,26 @@ def load():
         lib.canvas_block_backward.argtypes = [vp, vp, ctypes.POINTER(vp), vp, vp, ctypes.POINTER(vp), vp, sz, vp]
         lib.canvas_block_destroy.argtypes = [vp]
         lib.canvas_block_destroy.restype = None
+        i64, f32, u32, i32 = ctypes.c_int64, ctypes.c_float, ctypes.c_uint32, ctypes.c_int32
+        opt = ctypes.POINTER(CanvasOptions)
+        lib.canvas_norm_compile.argtypes = [ctypes.POINTER(i64), ctypes.c_int, u32, ctypes.c_int, f32, opt, ctypes.POINTER(vp)]
+        lib.canvas_norm_query.argtypes = [vp, ctypes.POINTER(CanvasNormInfo)]
+        lib.canvas_norm_forward.argtypes = [vp] * 10 + [sz, vp]
+        lib.canvas_norm_backward.argtypes = [vp] * 16 + [sz, vp]
+        lib.canvas_norm_destroy.argtypes = [vp]
+        lib.canvas_norm_destroy.restype = None
+        lib.canvas_logprob_compile.argtypes = [i64, i64, ctypes.c_int, i32, opt, ctypes.POINTER(vp)]
+        lib.canvas_logprob_query.argtypes = [vp, ctypes.POINTER(CanvasLogprobInfo)]
+        lib.canvas_logprob_forward.argtypes = [vp, vp, i64, f32, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.canvas_logprob_backward.argtypes = [vp, vp, i64, f32, vp, i64, vp, vp, vp, vp, i64, vp, sz, vp]
+        lib.canvas_logprob_destroy.argtypes = [vp]
+        lib.canvas_logprob_destroy.restype = None
+        lib.canvas_ortho_compile.argtypes = [ctypes.POINTER(i64), ctypes.c_int, i32, u32, ctypes.POINTER(vp)]
+        lib.canvas_ortho_query.argtypes = [vp, ctypes.POINTER(CanvasOrthoInfo)]
+        f64 = ctypes.c_double
+        lib.canvas_ortho_step.argtypes = [vp, vp, vp, vp, f64, vp, vp, f64, f64, vp, vp, vp, sz, vp]
+        lib.canvas_ortho_destroy.argtypes = [vp]
+        lib.canvas_ortho_destroy.restype = None
         _lib = lib
     return _lib
 
@@ -235,6 +283,103 @@ def canvas_block_backward(handle, x, weights, dy, dx, dweights, workspace):
 
 def canvas_block_destroy(handle):
     load().canvas_block_destroy(handle)
+
+
+# ---------------------------------------------------------------- norms around blocks (include/canvas_norm.h)
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _bytes(t):
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def canvas_norm_compile(shape, dtype, parts, gate=CANVAS_GATE_NONE, eps=1e-6, flags=0):
+    """shape: N, C, H, W.  parts: CANVAS_NORM_POST | CANVAS_NORM_PRE."""
+    shp = (ctypes.c_int64 * 4)(*[int(v) for v in shape])
+    opt = CanvasOptions(flags=flags)
+    h = ctypes.c_void_p()
+    _check(load().canvas_norm_compile(shp, int(dtype), int(parts), int(gate), float(eps), ctypes.byref(opt), ctypes.byref(h)))
+    return h
+
+
+def canvas_norm_query(handle):
+    info = CanvasNormInfo()
+    _check(load().canvas_norm_query(handle, ctypes.byref(info)))
+    return info
+
+
+def canvas_norm_forward(handle, x, z, gate, w_post, scale, w_pre, x_out, u, workspace):
+    """Tensors that the plan's parts do not have are None."""
+    _check(load().canvas_norm_forward(handle, _ptr(x), _ptr(z), _ptr(gate), _ptr(w_post), _ptr(scale), _ptr(w_pre), _ptr(x_out), _ptr(u),
+                                      _ptr(workspace), _bytes(workspace), _stream()))
+
+
+def canvas_norm_backward(handle, x, z, gate, w_post, scale, w_pre, dx_out, du, dx, dz, dgate, dw_post, dscale, dw_pre, workspace):
+    _check(load().canvas_norm_backward(handle, _ptr(x), _ptr(z), _ptr(gate), _ptr(w_post), _ptr(scale), _ptr(w_pre), _ptr(dx_out), _ptr(du),
+                                       _ptr(dx), _ptr(dz), _ptr(dgate), _ptr(dw_post), _ptr(dscale), _ptr(dw_pre), _ptr(workspace),
+                                       _bytes(workspace), _stream()))
+
+
+def canvas_norm_destroy(handle):
+    load().canvas_norm_destroy(handle)
+
+
+# ---------------------------------------------------------------- token log probabilities (include/canvas_logprob.h)
+
+def canvas_logprob_compile(rows, classes, dtype, top_k=0, flags=0):
+    opt = CanvasOptions(flags=flags)
+    h = ctypes.c_void_p()
+    _check(load().canvas_logprob_compile(int(rows), int(classes), int(dtype), int(top_k), ctypes.byref(opt), ctypes.byref(h)))
+    return h
+
+
+def canvas_logprob_query(handle):
+    info = CanvasLogprobInfo()
+    _check(load().canvas_logprob_query(handle, ctypes.byref(info)))
+    return info
+
+
+def canvas_logprob_forward(handle, logits, pitch, inv_temperature, mask, mask_pitch, tokens, logprob, entropy, top_logprob, top_index, workspace):
+    _check(load().canvas_logprob_forward(handle, _ptr(logits), int(pitch), float(inv_temperature), _ptr(mask), int(mask_pitch), _ptr(tokens),
+                                         _ptr(logprob), _ptr(entropy), _ptr(top_logprob), _ptr(top_index), _ptr(workspace), _bytes(workspace),
+                                         _stream()))
+
+
+def canvas_logprob_backward(handle, logits, pitch, inv_temperature, mask, mask_pitch, tokens, dlogprob, dentropy, dlogits, dpitch, workspace):
+    _check(load().canvas_logprob_backward(handle, _ptr(logits), int(pitch), float(inv_temperature), _ptr(mask), int(mask_pitch), _ptr(tokens),
+                                          _ptr(dlogprob), _ptr(dentropy), _ptr(dlogits), int(dpitch), _ptr(workspace), _bytes(workspace), _stream()))
+
+
+def canvas_logprob_destroy(handle):
+    load().canvas_logprob_destroy(handle)
+
+
+# ---------------------------------------------------------------- orthogonalised updates (include/canvas_ortho.h)
+
+def canvas_ortho_compile(shape, dtype, steps=5, flags=0):
+    """shape: G, R, K, as weight_shape of canvas_dag_query."""
+    shp = (ctypes.c_int64 * 3)(*[int(v) for v in shape])
+    h = ctypes.c_void_p()
+    _check(load().canvas_ortho_compile(shp, int(dtype), int(steps), int(flags), ctypes.byref(h)))
+    return h
+
+
+def canvas_ortho_query(handle):
+    info = CanvasOrthoInfo()
+    _check(load().canvas_ortho_query(handle, ctypes.byref(info)))
+    return info
+
+
+def canvas_ortho_step(handle, grad, momentum, momentum_out, mu, master, master_out, lr, decay, weights, update, workspace):
+    """momentum / momentum_out, master / master_out and weights, or update, may be None."""
+    _check(load().canvas_ortho_step(handle, _ptr(grad), _ptr(momentum), _ptr(momentum_out), float(mu), _ptr(master), _ptr(master_out), float(lr),
+                                    float(decay), _ptr(weights), _ptr(update), _ptr(workspace), _bytes(workspace), _stream()))
+
+
+def canvas_ortho_destroy(handle):
+    load().canvas_ortho_destroy(handle)
 
 
 # ---------------------------------------------------------------- templates (include/canvas_template.h), host only

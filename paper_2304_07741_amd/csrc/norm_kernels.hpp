@@ -1,0 +1,44 @@
+// Launches of the residual norm (include/canvas_norm.h).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace canvas {
+namespace norm {
+
+struct Shape {
+    int64_t N = 0, P = 0;  // images, pixels of one
+    int C = 0;
+    bool bf16 = false, post = false, pre = false;
+    int gate = 0;  // canvas_gate
+    float eps = 0.f;
+};
+
+// Plan of one shape: how many partial sums of the weights' gradients the backward kernel leaves.
+struct Plan {
+    int partials = 0;
+};
+Plan plan_of(const Shape& s);
+
+struct Fwd {
+    const void *x, *z, *g;
+    const float *w_post, *scale, *w_pre;
+    void *x_out, *u;
+    float *r2, *r1;  // one per pixel, null for an inference plan
+};
+struct Bwd {
+    const void *x, *z, *g;
+    const float *w_post, *scale, *w_pre;
+    const void *dx_out, *du;
+    void *dx, *dz, *dg;
+    float *dw_post, *dscale, *dw_pre;
+    const float *r2, *r1;
+    float* partial;  // [partials][2][C]: sums of D act zh, of du xh
+};
+
+void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream);
+void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream);
+
+}  // namespace norm
+}  // namespace canvas

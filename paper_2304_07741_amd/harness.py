@@ -133,6 +133,199 @@ class BlockRunner:
                 "dw": [dw[j * nw:(j + 1) * nw] for j in range(self.m)]}
 
 
+def _check_tensor(name, t, shape, dtype, device):
+    """The library takes addresses: what a runner hands on has to be what its plan was compiled for."""
+    if t is None or tuple(t.shape) != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        got = "None" if t is None else f"{tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}"
+        raise ValueError(f"{name}: a contiguous {shape} tensor of {dtype} on {device} is needed, got {got}")
+
+
+class _PlanRunner:
+    """One compiled plan, its workspace and the buffers it writes; close() releases the plan."""
+
+    handle = None
+
+    def _open(self, dtype, device):
+        if not torch.cuda.is_available():
+            raise RuntimeError("no GPU: the library has no CPU path")
+        self.device = torch.device(device)
+        self.tdtype = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+        self.cdtype = B.CANVAS_BF16 if dtype == "bf16" else B.CANVAS_F32
+
+    def _workspace(self, n):
+        return torch.empty(max(16, int(n)), dtype=torch.uint8, device=self.device)
+
+    def _empty(self, shape, dtype=None):
+        return torch.empty(shape, dtype=dtype or self.tdtype, device=self.device)
+
+    def close(self):
+        if self.handle is not None:
+            self._destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class NormRunner(_PlanRunner):
+    """The norms between two blocks (include/canvas_norm.h): x' = x + scale act(gate) norm(z) w_post, u = norm(x') w_pre.
+
+    forward() and backward() take the caller's tensors and return the runner's own buffers, which the next call overwrites.
+    Between the two the caller leaves x as it is.
+    """
+
+    _destroy = staticmethod(B.canvas_norm_destroy)
+
+    def __init__(self, shape, dtype, parts, gate=B.CANVAS_GATE_NONE, eps=1e-6, flags=0, device="cuda:0"):
+        self._open(dtype, device)
+        self.shape = tuple(int(v) for v in shape)
+        self.handle = B.canvas_norm_compile(self.shape, self.cdtype, parts, gate, eps, flags)
+        self.info = B.canvas_norm_query(self.handle)
+        self.post, self.pre, self.gate = bool(parts & B.CANVAS_NORM_POST), bool(parts & B.CANVAS_NORM_PRE), gate != B.CANVAS_GATE_NONE
+        self.ws = self._workspace(self.info.workspace_bytes)
+        self.x = None
+        self.out = {}
+        if self.post:
+            self.out["x_out"] = self._empty(self.shape)
+        if self.pre:
+            self.out["u"] = self._empty(self.shape)
+        self.grads = {}
+        if not flags & B.CANVAS_OPT_INFERENCE:
+            c = self.shape[1:2]
+            if self.pre:
+                self.grads |= {"dx": self._empty(self.shape), "dw_pre": self._empty(c, torch.float32)}
+            if self.post:
+                self.grads |= {"dz": self._empty(self.shape), "dw_post": self._empty(c, torch.float32), "dscale": self._empty(c, torch.float32)}
+            if self.gate:
+                self.grads["dgate"] = self._empty(self.shape)
+
+    def _check(self, maps, weights):
+        for name, t in maps.items():
+            _check_tensor(name, t, self.shape, self.tdtype, self.device)
+        for name, t in weights.items():
+            _check_tensor(name, t, self.shape[1:2], torch.float32, self.device)
+
+    def _of_the_block(self, z, gate, w_post, scale, w_pre):
+        maps, weights = {}, {}
+        if self.post:
+            maps["z"] = z
+            weights |= {"w_post": w_post, "scale": scale}
+        if self.gate:
+            maps["gate"] = gate
+        if self.pre:
+            weights["w_pre"] = w_pre
+        self._check(maps, weights)
+
+    def forward(self, x, z=None, gate=None, w_post=None, scale=None, w_pre=None):
+        self._of_the_block(z, gate, w_post, scale, w_pre)
+        self._check({"x": x}, {})
+        B.canvas_norm_forward(self.handle, x, z, gate, w_post, scale, w_pre, self.out.get("x_out"), self.out.get("u"), self.ws)
+        self.x = x
+        return self.out
+
+    def backward(self, x_out, z=None, gate=None, w_post=None, scale=None, w_pre=None, dx_out=None, du=None):
+        """Of the runner's last forward(), whose x it has kept.  x_out: what that call returned under that name (x itself in a
+        plan without POST); it says which pass is meant, the kernel computes its values again in fp32."""
+        if self.x is None or x_out is not (self.out["x_out"] if self.post else self.x):
+            raise ValueError("x_out: not the result of this runner's last forward()")
+        self._of_the_block(z, gate, w_post, scale, w_pre)
+        self._check({"du": du} if self.pre else {}, {})
+        if dx_out is not None or not self.pre:
+            self._check({"dx_out": dx_out}, {})
+        g = self.grads
+        B.canvas_norm_backward(self.handle, self.x, z, gate, w_post, scale, w_pre, dx_out, du, g.get("dx"), g.get("dz"), g.get("dgate"),
+                               g.get("dw_post"), g.get("dscale"), g.get("dw_pre"), self.ws)
+        return g
+
+
+class LogprobRunner(_PlanRunner):
+    """Log probabilities of tokens with entropy and top alternatives (include/canvas_logprob.h), and their gradient.
+
+    logits: [rows, classes] with any row pitch; mask: [rows, classes] or [classes] bytes, zero where a class is not allowed.
+    """
+
+    _destroy = staticmethod(B.canvas_logprob_destroy)
+
+    def __init__(self, rows, classes, dtype, top_k=0, flags=0, device="cuda:0"):
+        self._open(dtype, device)
+        self.rows, self.classes, self.top = int(rows), int(classes), int(top_k)
+        self.handle = B.canvas_logprob_compile(rows, classes, self.cdtype, top_k, flags)
+        self.info = B.canvas_logprob_query(self.handle)
+        self.ws = self._workspace(self.info.workspace_bytes)
+        self.out = {"logprob": self._empty(self.rows, torch.float32), "entropy": self._empty(self.rows, torch.float32)}
+        if self.top:
+            self.out |= {"top_logprob": self._empty((self.rows, self.top), torch.float32), "top_index": self._empty((self.rows, self.top), torch.int32)}
+        self.grads = {} if flags & B.CANVAS_OPT_INFERENCE else {"dlogits": self._empty((self.rows, self.classes))}
+
+    def _arguments(self, logits, tokens, mask):
+        """(pitch, mask pitch) of tensors that were checked."""
+        if tuple(logits.shape) != (self.rows, self.classes) or logits.dtype != self.tdtype or logits.device != self.device or logits.stride(1) != 1:
+            raise ValueError(f"logits: a {(self.rows, self.classes)} tensor of {self.tdtype} on {self.device} with dense rows is needed")
+        _check_tensor("tokens", tokens, (self.rows,), torch.int64, self.device)
+        pitch = logits.stride(0) if self.rows > 1 else self.classes
+        if mask is None:
+            return pitch, 0
+        if mask.dtype not in (torch.uint8, torch.bool) or mask.device != self.device or mask.stride(-1) != 1 \
+                or tuple(mask.shape) not in ((self.classes,), (self.rows, self.classes)):
+            raise ValueError(f"mask: bytes or truth values of {(self.rows, self.classes)} or {(self.classes,)} on {self.device} are needed")
+        return pitch, mask.stride(0) if mask.dim() == 2 and self.rows > 1 else 0
+
+    def forward(self, logits, tokens, mask=None, inv_temperature=1.0):
+        pitch, mask_pitch = self._arguments(logits, tokens, mask)
+        o = self.out
+        B.canvas_logprob_forward(self.handle, logits, pitch, inv_temperature, mask, mask_pitch, tokens, o["logprob"], o["entropy"],
+                                 o.get("top_logprob"), o.get("top_index"), self.ws)
+        return o
+
+    def backward(self, logits, tokens, dlogprob=None, dentropy=None, mask=None, inv_temperature=1.0):
+        pitch, mask_pitch = self._arguments(logits, tokens, mask)
+        for name, t in (("dlogprob", dlogprob), ("dentropy", dentropy)):
+            if t is not None:
+                _check_tensor(name, t, (self.rows,), torch.float32, self.device)
+        B.canvas_logprob_backward(self.handle, logits, pitch, inv_temperature, mask, mask_pitch, tokens, dlogprob, dentropy,
+                                  self.grads["dlogits"], self.classes, self.ws)
+        return self.grads
+
+
+class OrthoRunner(_PlanRunner):
+    """Orthogonalised update of an FC weight (include/canvas_ortho.h): shape [G, R, K] as the DAG's weight_shape."""
+
+    _destroy = staticmethod(B.canvas_ortho_destroy)
+
+    def __init__(self, shape, dtype, steps=5, flags=0, device="cuda:0"):
+        self._open(dtype, device)
+        self.shape = tuple(int(v) for v in shape)
+        self.handle = B.canvas_ortho_compile(self.shape, self.cdtype, steps, flags)
+        self.info = B.canvas_ortho_query(self.handle)
+        self.ws = self._workspace(self.info.workspace_bytes)
+        self.out = {"update": self._empty(self.shape)}
+
+    def _buffer(self, name, dtype=None):
+        if name not in self.out:
+            self.out[name] = self._empty(self.shape, dtype)
+        return self.out[name]
+
+    def step(self, grad, momentum=None, master=None, mu=0.95, lr=0.0, decay=0.0):
+        """Returns update, and momentum and master / weights where they were given: buffers of the runner, the arguments stay as
+        they are."""
+        for name, t in (("grad", grad), ("momentum", momentum), ("master", master)):
+            if t is not None or name == "grad":
+                _check_tensor(name, t, self.shape, torch.float32, self.device)
+        names = ["update"]
+        m = w = p = None
+        if momentum is not None:
+            m = self._buffer("momentum", torch.float32)
+            names.append("momentum")
+        if master is not None:
+            w, p = self._buffer("master", torch.float32), self._buffer("weights")
+            names += ["master", "weights"]
+        B.canvas_ortho_step(self.handle, grad, momentum, m, mu, master, w, lr, decay, p, self.out["update"], self.ws)
+        return {k: self.out[k] for k in names}
+
+
 def run_case(case, flags=0, dy=None):
     """Upload a workload (see workloads.py), run forward + backward, return (results, runner)."""
     from . import workloads as wl

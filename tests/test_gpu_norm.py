@@ -1,0 +1,167 @@
+"""The norms between two blocks against their definition in 64 bits."""
+import pytest
+import torch
+
+import operators_ref as ref
+from helpers import TOL, assert_close
+from paper_2304_07741_amd import binding as B
+from paper_2304_07741_amd import harness
+
+pytestmark = pytest.mark.gpu
+
+BOTH = B.CANVAS_NORM_POST | B.CANVAS_NORM_PRE
+# parts, gate
+PLANS = [(BOTH, B.CANVAS_GATE_SILU), (BOTH, B.CANVAS_GATE_NONE), (B.CANVAS_NORM_PRE, B.CANVAS_GATE_NONE), (B.CANVAS_NORM_POST, B.CANVAS_GATE_SIGMOID)]
+# one pixel and one channel; rows of tokens, short, odd and longer than a workgroup; planes from two pixels on: odd, of whole
+# vectors, longer than a tile; few and many channels
+SHAPES = [(1, 1, 1, 1), (3, 1, 2, 5), (1, 7, 1, 1), (5, 64, 1, 1), (37, 1000, 1, 1), (3, 4099, 1, 1), (2, 16384, 1, 1), (700, 48, 1, 1),
+          (2, 33, 1, 2), (3, 8, 3, 1), (70, 24, 2, 2), (5, 64, 7, 7), (2, 257, 9, 13), (3, 96, 16, 16), (1, 16, 1, 4099), (2, 520, 14, 14), (1, 2100, 5, 8),
+          (9, 40, 28, 28), (1, 5000, 3, 3)]
+EPS = 1e-3
+
+
+def _case(shape, dtype, parts, gate, seed, scale_x=1.0):
+    n, c, h, w = shape
+    gen = torch.Generator().manual_seed(seed)
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    maps = {k: (torch.randn(n, c, h, w, generator=gen) * s).to(dt) for k, s in (("x", scale_x), ("z", 0.7), ("g", 2.0), ("dy", 1.0), ("du", 1.0))}
+    weights = {"w_post": torch.randn(c, generator=gen), "scale": torch.randn(c, generator=gen) * 0.5, "w_pre": torch.randn(c, generator=gen)}
+    post, pre = bool(parts & B.CANVAS_NORM_POST), bool(parts & B.CANVAS_NORM_PRE)
+    if not post:
+        maps.pop("z"), weights.pop("w_post"), weights.pop("scale")
+    if not gate:
+        maps.pop("g")
+    if not pre:
+        weights.pop("w_pre"), maps.pop("du")
+    return maps, weights
+
+
+def _reference(shape, maps, weights, gate, with_dy):
+    n, c, h, w = shape
+    m = {k: v.double().reshape(n, c, h * w) for k, v in maps.items()}
+    wt = {k: v.double() for k, v in weights.items()}
+    y, u = ref.norm_forward(m["x"], m.get("z"), m.get("g"), wt.get("w_post"), wt.get("scale"), wt.get("w_pre"), gate, EPS)
+    out = {"x_out": y, "u": u}
+    out |= ref.norm_backward(y, m.get("z"), m.get("g"), wt.get("w_post"), wt.get("scale"), wt.get("w_pre"), gate, EPS, m["dy"] if with_dy else None, m.get("du"))
+    return {k: v.numpy() for k, v in out.items() if v is not None}
+
+
+def _run(shape, dtype, parts, gate, maps, weights, with_dy=True, device="cuda:0"):
+    r = harness.NormRunner(shape, dtype, parts, gate=gate, eps=EPS)
+    d = {k: v.to(device) for k, v in {**maps, **weights}.items()}
+    for t in [*r.out.values(), *r.grads.values()]:
+        t.fill_(float("nan"))
+    r.ws.fill_(0xFF)
+    block = (d.get("z"), d.get("g"), d.get("w_post"), d.get("scale"), d.get("w_pre"))
+    out = r.forward(d["x"], *block)
+    got = {**out, **r.backward(out.get("x_out", d["x"]), *block, dx_out=d["dy"] if with_dy else None, du=d.get("du"))}
+    torch.cuda.synchronize()
+    res = {k: v.double().cpu().numpy() for k, v in got.items()}
+    r.close()
+    return res
+
+
+@pytest.mark.parametrize("parts,gate", PLANS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_forward_and_backward(shape, dtype, parts, gate):
+    maps, weights = _case(shape, dtype, parts, gate, seed=sum(shape))
+    want = _reference(shape, maps, weights, gate, True)
+    got = _run(shape, dtype, parts, gate, maps, weights)
+    n, c, h, w = shape
+    for k, g in got.items():
+        # the weights' gradients are fp32 sums of the operands as they were loaded; bf16 plans read x' rounded, which each of
+        # the terms carries once: 2^-9 of a term, so the bound of the maps holds for their sum
+        floor = 1e-2 if k in ("dz", "dw_post", "dscale", "dgate", "dx", "dw_pre") and c == 1 else 1e-30
+        assert_close(g.reshape(want[k].shape), want[k], TOL[dtype], f"{shape} {dtype} {k}", floor=floor)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_no_gradient_on_the_stream_is_a_gradient_of_zeros(dtype):
+    shape = (3, 48, 5, 7)
+    maps, weights = _case(shape, dtype, BOTH, B.CANVAS_GATE_SILU, 11)
+    want = _reference(shape, maps, weights, B.CANVAS_GATE_SILU, False)
+    got = _run(shape, dtype, BOTH, B.CANVAS_GATE_SILU, maps, weights, with_dy=False)
+    for k, g in got.items():
+        assert_close(g.reshape(want[k].shape), want[k], TOL[dtype], k)
+
+
+def test_pixels_of_zeros_and_of_large_values():
+    """A pixel whose channels are all zero is divided by the root of eps; squares of 1e18 stay in range."""
+    shape = (2, 64, 6, 6)
+    for scale in (0.0, 1e-18, 1e15):
+        maps, weights = _case(shape, "f32", BOTH, B.CANVAS_GATE_NONE, 5)
+        maps["x"] = maps["x"] * scale
+        maps["z"][0, :, 2, 3] = 0
+        maps["x"][0, :, 2, 3] = 0
+        want = _reference(shape, maps, weights, B.CANVAS_GATE_NONE, True)
+        got = _run(shape, "f32", BOTH, B.CANVAS_GATE_NONE, maps, weights)
+        for k in ("x_out", "u", "dx", "dz", "dw_pre"):
+            assert_close(got[k].reshape(want[k].shape), want[k], TOL["f32"], f"{scale} {k}")
+
+
+def test_a_pixel_with_nan_keeps_it_to_itself():
+    shape = (2, 40, 7, 7)
+    maps, weights = _case(shape, "bf16", BOTH, B.CANVAS_GATE_SIGMOID, 9)
+    clean = _run(shape, "bf16", BOTH, B.CANVAS_GATE_SIGMOID, maps, weights)
+    maps["z"][1, 3, 4, 5] = float("nan")
+    got = _run(shape, "bf16", BOTH, B.CANVAS_GATE_SIGMOID, maps, weights)
+    for k in ("x_out", "u", "dx", "dz", "dgate"):
+        t = torch.from_numpy(got[k]).clone()
+        assert torch.isnan(t[1, :, 4, 5]).any(), k
+        t[1, :, 4, 5] = torch.from_numpy(clean[k])[1, :, 4, 5]
+        assert torch.equal(t, torch.from_numpy(clean[k])), k
+
+
+@pytest.mark.parametrize("shape", [(64, 64, 20, 20), (300, 512, 1, 1)])
+def test_two_runs_and_two_streams_give_the_same_bits(shape):
+    maps, weights = _case(shape, "bf16", BOTH, B.CANVAS_GATE_SILU, 2)
+    first = _run(shape, "bf16", BOTH, B.CANVAS_GATE_SILU, maps, weights)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        again = _run(shape, "bf16", BOTH, B.CANVAS_GATE_SILU, maps, weights)
+    for k in first:
+        assert (first[k] == again[k]).all(), k
+
+
+def test_inference_plan():
+    shape = (4, 96, 7, 7)
+    maps, weights = _case(shape, "bf16", BOTH, B.CANVAS_GATE_SILU, 4)
+    want = _reference(shape, maps, weights, B.CANVAS_GATE_SILU, True)
+    r = harness.NormRunner(shape, "bf16", BOTH, gate=B.CANVAS_GATE_SILU, eps=EPS, flags=B.CANVAS_OPT_INFERENCE)
+    assert r.info.workspace_bytes == 0 and r.info.n_launches_bwd == 0
+    d = {k: v.cuda() for k, v in {**maps, **weights}.items()}
+    out = r.forward(d["x"], d["z"], d["g"], d["w_post"], d["scale"], d["w_pre"])
+    for k, g in out.items():
+        assert_close(g.double().cpu().numpy().reshape(want[k].shape), want[k], TOL["bf16"], k)
+    with pytest.raises(B.CanvasError) as e:
+        r.backward(out["x_out"], d["z"], d["g"], d["w_post"], d["scale"], d["w_pre"], dx_out=d["dy"], du=d["du"])
+    assert e.value.status == -6
+    r.close()
+
+
+def test_gradient_against_differences_of_the_kernel():
+    """(L(x + h d) - L(x - h d)) / 2h of the forward kernel.  Truncation ~ h^2 = 1e-4 of the value, the fp32 rounding of the
+    outputs 1e-7 sqrt(n) / h ~ 1e-3 of a loss gradient of norm sqrt(n): 5e-3 bounds both."""
+    shape, h = (2, 32, 4, 4), 1e-2
+    maps, weights = _case(shape, "f32", BOTH, B.CANVAS_GATE_SILU, 21)
+    got = _run(shape, "f32", BOTH, B.CANVAS_GATE_SILU, maps, weights)
+    gen = torch.Generator().manual_seed(1)
+
+    def loss(m, w):
+        r = harness.NormRunner(shape, "f32", BOTH, gate=B.CANVAS_GATE_SILU, eps=EPS)
+        d = {k: v.cuda() for k, v in {**m, **w}.items()}
+        out = {k: v.double().cpu() for k, v in r.forward(d["x"], d["z"], d["g"], d["w_post"], d["scale"], d["w_pre"]).items()}
+        r.close()
+        return float((out["x_out"] * m["dy"].double()).sum() + (out["u"] * m["du"].double()).sum())
+
+    for name, grad in (("x", "dx"), ("z", "dz"), ("g", "dgate"), ("w_post", "dw_post"), ("scale", "dscale"), ("w_pre", "dw_pre")):
+        src = maps if name in maps else weights
+        g = torch.from_numpy(got[grad])
+        d = torch.randn(src[name].shape, generator=gen) * 0.1 + (g / g.norm()).float()
+        d /= d.norm()
+        up = {k: (v + h * d if k == name else v) for k, v in src.items()}
+        down = {k: (v - h * d if k == name else v) for k, v in src.items()}
+        pair = [loss(m, weights) if src is maps else loss(maps, m) for m in (up, down)]
+        want, have = (pair[0] - pair[1]) / (2 * h), float((g * d.double()).sum())
+        assert abs(want - have) <= 5e-3 * abs(have) + 5e-3, (name, want, have)

@@ -1,0 +1,118 @@
+"""Orthogonalised updates against the definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import operators_ref as ref
+from paper_2304_07741_amd import binding as B
+from paper_2304_07741_amd import harness
+
+pytestmark = pytest.mark.gpu
+
+# one element; one row, one column; grouped FCs; odd sides; sides around 16, 32, 64 and 128; tall ones; many small matrices
+SHAPES = [(1, 1, 1), (3, 1, 7), (2, 9, 1), (8, 8, 72), (1, 16, 16), (5, 17, 33), (1, 72, 8), (2, 64, 576), (1, 63, 65), (1, 64, 640), (3, 65, 130), (1, 130, 300),
+          (1, 129, 129), (1, 300, 130), (70, 40, 10), (1, 256, 2304), (1, 33, 5000), (2, 200, 1031), (1, 640, 200), (1, 520, 776), (1, 1100, 1300)]
+
+# Each operand of a product carries 22 bits and sums are fp32: 2^-22 of the largest singular value.  Five steps raise what a
+# weak direction holds by at most 3.4445^5 = 485 while the strongest stays near one, so an error grows to 485 * 2^-22 = 1.2e-4.
+TOL_F32 = 1.2e-4
+TOL_BF16 = TOL_F32 + 2.0 ** -8
+
+
+def _inputs(shape, seed, kind="noise"):
+    gen = torch.Generator().manual_seed(seed)
+    g, r, k = shape
+    grad = torch.randn(g, r, k, generator=gen)
+    if kind == "low":
+        rank = max(1, min(r, k) // 8)
+        grad = torch.randn(g, r, rank, generator=gen) @ torch.randn(g, rank, k, generator=gen) + 0.05 * grad
+    return grad, torch.randn(g, r, k, generator=gen), torch.randn(g, r, k, generator=gen)
+
+
+def _err(got, want):
+    got, want = got.double().cpu(), want.double()
+    assert torch.isfinite(got).all()
+    return max(float((got - want).norm() / want.norm().clamp(min=1e-30)), float((got - want).abs().max() / want.abs().max().clamp(min=1e-30)))
+
+
+def _step(shape, dtype, grad, momentum=None, master=None, mu=0.9, lr=0.02, decay=0.1, steps=5, flags=0):
+    r = harness.OrthoRunner(shape, dtype, steps=steps, flags=flags)
+    r.ws.fill_(0xFF)
+    r.out["update"].fill_(float("nan"))
+    d = [None if t is None else t.cuda() for t in (grad, momentum, master)]
+    out = {k: v.cpu() for k, v in r.step(*d, mu=mu, lr=lr, decay=decay).items()}
+    r.close()
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["noise", "low"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_step(shape, kind, dtype):
+    grad, momentum, master = _inputs(shape, sum(shape), kind)
+    momentum = momentum * 0.1
+    tol = TOL_F32 if dtype == "f32" else TOL_BF16
+    nesterov = sum(shape) % 2 == 0
+    want = ref.ortho_step(grad.double(), momentum.double(), 0.9, nesterov, 5, master.double(), 0.02, 0.1)
+    got = _step(shape, dtype, grad, momentum, master, flags=B.CANVAS_ORTHO_NESTEROV if nesterov else 0)
+    assert _err(got["update"], want["update"]) <= tol
+    assert _err(got["momentum"], want["momentum"]) <= 1e-6
+    assert _err(got["master"], want["master"]) <= 0.02 * TOL_F32 + 1e-6
+    assert torch.equal(got["weights"], got["master"].to(got["weights"].dtype))
+
+
+@pytest.mark.parametrize("steps", [0, 1, 2, 8])
+@pytest.mark.parametrize("shape", [(2, 24, 40), (1, 150, 70), (1, 260, 300)])
+def test_number_of_steps(shape, steps):
+    grad, _, _ = _inputs(shape, 3)
+    want = ref.ortho_step(grad.double(), None, 0, False, steps)
+    got = _step(shape, "f32", grad, steps=steps)
+    assert set(got) == {"update"} and _err(got["update"], want["update"]) <= TOL_F32 * max(1, steps / 5)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-7, 1e25])
+@pytest.mark.parametrize("shape", [(2, 24, 40), (1, 200, 300)])
+def test_gradients_of_any_size(shape, scale):
+    grad, _, _ = _inputs(shape, 4)
+    grad = grad * scale
+    want = ref.ortho_step(grad.double(), None, 0, False, 5)
+    got = _step(shape, "f32", grad)["update"].double()
+    # (1e-30: the division by |v| + 1e-7 leaves 1e-22 and less, which the fp16 pairs do not hold: zeros to that accuracy)
+    assert torch.isfinite(got).all() and float((got - want["update"]).norm()) <= TOL_F32 * max(1.0, float(want["update"].norm()))
+
+
+@pytest.mark.parametrize("shape", [(4, 24, 40), (4, 130, 200)])
+def test_zeros_and_nan_stay_in_their_matrix(shape):
+    grad, _, _ = _inputs(shape, 5)
+    clean = _step(shape, "f32", grad)["update"]
+    grad[1] = 0
+    grad[2, 3, 5] = math.nan
+    got = _step(shape, "f32", grad)["update"]
+    assert (got[1] == 0).all() and torch.isnan(got[2]).any()
+    assert torch.equal(got[0], clean[0]) and torch.equal(got[3], clean[3])
+    grad[2, 3, 5] = math.inf
+    got = _step(shape, "f32", grad)["update"]
+    assert torch.isnan(got[2]).any() and torch.equal(got[0], clean[0]) and torch.equal(got[3], clean[3])
+
+
+@pytest.mark.parametrize("shape", [(3, 40, 56), (1, 256, 300)])
+def test_in_place_and_on_another_stream(shape):
+    """momentum_out = momentum and master_out = master give the bits of separate tensors; so does a second stream."""
+    grad, momentum, master = _inputs(shape, 6)
+    a = _step(shape, "bf16", grad, momentum, master)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        r = harness.OrthoRunner(shape, "bf16")
+        g, m, w = grad.cuda(), momentum.cuda(), master.cuda()
+        u, p = r.out["update"], torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+        B.canvas_ortho_step(r.handle, g, m, m, 0.9, w, w, 0.02, 0.1, p, u, r.ws)
+        side.synchronize()
+    for k, t in (("update", u), ("momentum", m), ("master", w), ("weights", p)):
+        assert torch.equal(a[k], t.cpu()), k
+    # without an update tensor
+    m, w = momentum.cuda(), master.cuda()
+    B.canvas_ortho_step(r.handle, g, m, m, 0.9, w, w, 0.02, 0.1, None, None, r.ws)
+    torch.cuda.synchronize()
+    assert torch.equal(a["master"], w.cpu())
+    r.close()
