@@ -32,7 +32,7 @@ int canvas_ortho_compile(const int64_t shape[3], canvas_dtype dt, int32_t steps,
         for (int i = 0; i < 3; i++)
             if (shape[i] < 1) return set_last_error(CANVAS_BAD_ARG, "every size must be at least 1");
         const int64_t most = INT32_MAX, G = shape[0], R = shape[1], K = shape[2];
-        if (G > most || R > most || K > most || R * K > most || G > most / (R * K)) return set_last_error(CANVAS_UNSUPPORTED, "G * R * K must be below 2^31");
+        if (G > most || R > most || K > most || R * K > most / 2 || G > most / (R * K)) return set_last_error(CANVAS_UNSUPPORTED, "R * K must be below 2^30, G * R * K below 2^31");
         if (std::min(R, K) > CANVAS_ORTHO_MAX_SIDE || G > 65535) return set_last_error(CANVAS_UNSUPPORTED, "matrices too large or too many");
         auto h = std::make_unique<canvas_ortho>();
         canvas::ortho::Shape& s = h->s;

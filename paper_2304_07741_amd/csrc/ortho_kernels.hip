@@ -1,20 +1,57 @@
-// Newton-Schulz products in fp32, one thread per element of a result.
+// Newton-Schulz products of the orthogonalised update.
+//
+// A matrix of fp32 values v is held as two fp16 planes: hi = fp16(2^12 v), lo = fp16(2^12 v - hi).  |X| <= 1.3 and |b A + c A A + a I| <= 4
+// in every step (spectral norms bound the elements), so hi stays below 2^14, and lo keeps 11 more bits of every element above
+// 2^-15 of the largest possible one.  A product of two such matrices is hi hi + hi lo + lo hi on the matrix units with fp32
+// sums; lo lo is below 2^-22 of a term.
+//
+// Per step, with both X [m][n] and its transpose at hand so that every operand is read along the index that is summed over:
+//   A = X X^T   (tiles on and below the diagonal, written on both sides of it)
+//   B = a I + b A + c A A^T  (the same)
+//   X = B X     (from the rows of B and of X^T; both X and X^T are written, or, in the last step, the outputs)
 #include "ortho_kernels.hpp"
 
 #include "device_util.hpp"
 #include "launch.hpp"
+#include "tile_util.hpp"
 
 namespace canvas {
 namespace ortho {
 namespace {
 
-constexpr int kThreads = 256, kTile = 16;
+constexpr int kThreads = 256;
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr double kEps = 1e-7;
+constexpr float kScale = 4096.f;  // 2^12
+constexpr int kDepth = 32;        // of one step of a product; leading dimensions are multiples of it, zeros behind the columns
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+using tile::u32x4;
+
+// One matrix per group as two planes of rows; lo is `plane` elements behind hi, the next group's `step` behind this one's.
+struct Pair {
+    _Float16* hi;
+    int64_t plane, step;
+    int ld;
+};
+
+__device__ __forceinline__ uint32_t pack_pair(float v) {  // v scaled: hi in the low half, lo in the high one
+    const _Float16 h = (_Float16)v, l = (_Float16)(v - (float)h);
+    return (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
+}
+__device__ __forceinline__ float of_half(uint32_t u) { return (float)__builtin_bit_cast(_Float16, (uint16_t)u); }
 
 __device__ __forceinline__ float direction(const Shape& s, const Args& a, int64_t i, float m_new) {
     if (!a.momentum) return a.grad[i];
     return s.nesterov ? (float)(a.grad[i] + a.mu * m_new) : m_new;  // (mu in 64 bits: gradient and momentum may cancel)
+}
+
+// 16 bytes per lane from `from` + voff + soff to LDS, lane after lane behind `to` (the same for the whole wave).
+__device__ __forceinline__ tile::rsrc_t whole_memory(const void* from) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(from), 0, 0xffffffffu, 0x00020000); }
+__device__ __forceinline__ void load_to_lds(tile::rsrc_t from, unsigned char* to, uint32_t voff, int soff) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, voff, soff, 0, 0);
 }
 
 __global__ __launch_bounds__(kThreads) void k_mix(Shape s, Args a, double* sums) {
@@ -40,48 +77,56 @@ __global__ __launch_bounds__(kThreads) void k_mix(Shape s, Args a, double* sums)
     if (threadIdx.x == 0) sums[blockIdx.y * gridDim.x + blockIdx.x] = buf[0];
 }
 
-__global__ __launch_bounds__(kThreads) void k_start(Shape s, Args a, const double* sums, int parts, float* x) {
+// 1 / (|v| + 1e-7) of this workgroup's matrix.
+__device__ double inverse_norm(const double* sums, int parts, double* buf) {
     double t = 0;
-    for (int k = 0; k < parts; k++) t += sums[blockIdx.y * parts + k];
-    const double inv = 1.0 / (sqrt(t) + kEps);
-    const int64_t len = s.R * s.K, k = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (k >= len) return;
-    const int64_t i = blockIdx.y * len + k;
-    const int64_t row = k / s.K, col = k - row * s.K;
-    x[blockIdx.y * len + (s.tall ? col * s.n + row : k)] = (float)(direction(s, a, i, a.momentum ? a.momentum_out[i] : 0.f) * inv);
-}
-
-// c[i][j] = p sum_k a[i][k] b(k, j) + q d[i][j],  b(k, j) = b[j][k] with NT, else b[k][j]
-template <bool NT>
-__global__ __launch_bounds__(kTile* kTile) void k_product(const float* a, const float* b, const float* d, float* c, int64_t rows, int64_t cols, int64_t depth,
-                                                          float p, float q, int64_t step_a, int64_t step_b, int64_t step_c) {
-    __shared__ float ta[kTile][kTile + 1], tb[kTile][kTile + 1];
-    a += blockIdx.z * step_a;
-    b += blockIdx.z * step_b;
-    c += blockIdx.z * step_c;
-    const int64_t i0 = (int64_t)blockIdx.y * kTile, j0 = (int64_t)blockIdx.x * kTile;
-    const int ty = threadIdx.x / kTile, tx = threadIdx.x % kTile;
-    float t = 0.f;
-    for (int64_t k0 = 0; k0 < depth; k0 += kTile) {
-        ta[ty][tx] = i0 + ty < rows && k0 + tx < depth ? a[(i0 + ty) * depth + k0 + tx] : 0.f;
-        if (NT)
-            tb[tx][ty] = j0 + ty < cols && k0 + tx < depth ? b[(j0 + ty) * depth + k0 + tx] : 0.f;
-        else
-            tb[ty][tx] = k0 + ty < depth && j0 + tx < cols ? b[(k0 + ty) * cols + j0 + tx] : 0.f;
-        __syncthreads();
-        for (int k = 0; k < kTile; k++) t += ta[ty][k] * tb[k][tx];
+    for (int k = threadIdx.x; k < parts; k += kThreads) t += sums[k];
+    buf[threadIdx.x] = t;
+    __syncthreads();
+    for (int o = kThreads / 2; o; o >>= 1) {
+        if ((int)threadIdx.x < o) buf[threadIdx.x] += buf[threadIdx.x + o];
         __syncthreads();
     }
-    const int64_t i = i0 + ty, j = j0 + tx;
-    if (i < rows && j < cols) c[i * cols + j] = p * t + (q != 0.f ? q * d[blockIdx.z * step_c + i * cols + j] : 0.f);
+    return 1.0 / (sqrt(buf[0]) + kEps);
 }
 
-__global__ __launch_bounds__(kThreads) void k_finish(Shape s, Args a, const float* x) {
-    const int64_t len = s.R * s.K, k = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (k >= len) return;
-    const int64_t i = blockIdx.y * len + k;
-    const int64_t row = k / s.K, col = k - row * s.K;
-    const float o = x[blockIdx.y * len + (s.tall ? col * s.n + row : k)];
+// X and X^T of the normalised direction, 64 x 64 elements per workgroup through LDS; zeros behind the columns.
+__global__ __launch_bounds__(kThreads) void k_start(Shape s, Args a, const double* sums, int parts, Pair x, Pair xt) {
+    __shared__ double buf[kThreads];
+    __shared__ uint32_t img[64][65];
+    const double inv = inverse_norm(sums + (int64_t)blockIdx.y * parts, parts, buf);
+    const unsigned wide = (unsigned)((s.K + 63) / 64), by = blockIdx.x / wide;
+    const int64_t len = s.R * s.K, r0 = (int64_t)by * 64, c0 = (int64_t)(blockIdx.x - by * wide) * 64;
+    const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
+    // orig: the planes laid out as the gradient is; turned: its transpose
+    const Pair orig = s.tall ? xt : x, turned = s.tall ? x : xt;
+    for (int r = ty; r < 64; r += 4) {
+        const int64_t row = r0 + r, col = c0 + tx;
+        uint32_t p = 0;
+        if (row < s.R && col < s.K) {
+            const int64_t i = blockIdx.y * len + row * s.K + col;
+            p = pack_pair((float)(direction(s, a, i, a.momentum ? a.momentum_out[i] : 0.f) * inv) * kScale);
+        }
+        img[r][tx] = p;
+        if (row < s.R && col < orig.ld) {
+            _Float16* at = orig.hi + blockIdx.y * orig.step + row * orig.ld + col;
+            *reinterpret_cast<uint16_t*>(at) = (uint16_t)p;
+            *reinterpret_cast<uint16_t*>(at + orig.plane) = (uint16_t)(p >> 16);
+        }
+    }
+    __syncthreads();
+    for (int r = ty; r < 64; r += 4) {
+        const int64_t row = c0 + r, col = r0 + tx;  // of the transpose
+        if (row < s.K && col < turned.ld) {
+            const uint32_t p = img[tx][r];
+            _Float16* at = turned.hi + blockIdx.y * turned.step + row * turned.ld + col;
+            *reinterpret_cast<uint16_t*>(at) = (uint16_t)p;
+            *reinterpret_cast<uint16_t*>(at + turned.plane) = (uint16_t)(p >> 16);
+        }
+    }
+}
+
+__device__ __forceinline__ void finish_one(const Shape& s, const Args& a, int64_t i, float o) {
     if (a.update) {
         if (s.bf16)
             static_cast<uint16_t*>(a.update)[i] = f32_to_bf16(o);
@@ -100,8 +145,223 @@ __global__ __launch_bounds__(kThreads) void k_finish(Shape s, Args a, const floa
     }
 }
 
+// Plans without products: the normalised direction itself.
+__global__ __launch_bounds__(kThreads) void k_normalised(Shape s, Args a, const double* sums, int parts) {
+    __shared__ double buf[kThreads];
+    const double inv = inverse_norm(sums + (int64_t)blockIdx.y * parts, parts, buf);
+    const int64_t len = s.R * s.K, k = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (k >= len) return;
+    const int64_t i = blockIdx.y * len + k;
+    finish_one(s, a, i, (float)(direction(s, a, i, a.momentum ? a.momentum_out[i] : 0.f) * inv));
+}
+
+enum Kind { kGram, kSquare, kUpdate, kLast };
+
+// C[i][j] = sum_k P[i][k] Q[j][k], rows of P x rows of Q, over `depth` (a multiple of kDepth, zeros at its end).
+struct Product {
+    Pair p, q;
+    int rows, cols, depth;
+    Pair out;   // kGram, kSquare: C, both sides; kUpdate: X
+    Pair turn;  // kUpdate: X^T
+    int tiles_i, tiles_j, tiles;
+};
+
+// BM x BN results per workgroup of 2 x 2 waves.  Both planes of both operands are loaded straight into LDS, 32 summands at a time, into
+// the buffer that the previous step has left, while the products of the present one run.  Rows of 64 bytes lie four to a line
+// of all banks; a 16-byte piece c of row r lies at place c ^ (r / 4) % 4, so that the pieces that eight rows read together
+// fall on different banks.
+template <int BM, int BN, Kind KIND>
+__global__ __launch_bounds__(kThreads) void k_product(Shape s, Args args, Product g) {
+    constexpr int TM = BM / 64, TN = BN / 64;
+    constexpr int kOpA = BM * 64, kOpB = BN * 64;            // bytes of one plane of a step
+    constexpr int kStage = 2 * (kOpA + kOpB);
+    constexpr int kLds = 2 * kStage > BM * BN * 4 ? 2 * kStage : BM * BN * 4;
+    __shared__ __align__(16) unsigned char lds[kLds];
+
+    const unsigned seq = tile::xcd_sequence();
+    const int grp = seq / g.tiles, t = seq - grp * g.tiles;
+    int bi, bj;
+    if (KIND == kGram || KIND == kSquare) {
+        bi = (int)((__fsqrt_rn(8.f * t + 1.f) - 1.f) * 0.5f);
+        while (bi * (bi + 1) / 2 > t) bi--;
+        while ((bi + 1) * (bi + 2) / 2 <= t) bi++;
+        bj = t - bi * (bi + 1) / 2;
+    } else {
+        bj = t / g.tiles_i;
+        bi = t - bj * g.tiles_i;
+    }
+    const int i0 = bi * BM, j0 = bj * BN;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wi = (wave >> 1) * (BM / 2), wj = (wave & 1) * (BN / 2);
+
+    // 16-byte pieces of this thread in a plane of a step; rows past the end are the last one again
+    auto piece = [&](int q, int first, int rows, int ld) {
+        const int at = tid + q * kThreads, r = at >> 2, c = (at & 3) ^ ((r >> 2) & 3);
+        const int row = first + r < rows ? r : rows - 1 - first;
+        return (uint32_t)row * (uint32_t)ld * 2u + (uint32_t)c * 16u;
+    };
+    uint32_t va[BM / 64], vb[BN / 64];
+#pragma unroll
+    for (int q = 0; q < BM / 64; q++) va[q] = piece(q, i0, g.rows, g.p.ld);
+#pragma unroll
+    for (int q = 0; q < BN / 64; q++) vb[q] = piece(q, j0, g.cols, g.q.ld);
+    const _Float16* pa = g.p.hi + grp * g.p.step + (int64_t)i0 * g.p.ld;
+    const _Float16* pb = g.q.hi + grp * g.q.step + (int64_t)j0 * g.q.ld;
+    const tile::rsrc_t ra[2] = {whole_memory(pa), whole_memory(pa + g.p.plane)};
+    const tile::rsrc_t rb[2] = {whole_memory(pb), whole_memory(pb + g.q.plane)};
+    auto load = [&](int step) {
+        unsigned char* to = lds + (step & 1) * kStage + wave * 1024;
+        const int k = step * (kDepth * 2);
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+#pragma unroll
+            for (int q = 0; q < BM / 64; q++)
+                load_to_lds(ra[h], to + h * kOpA + q * 4096, va[q], k);
+#pragma unroll
+            for (int q = 0; q < BN / 64; q++)
+                load_to_lds(rb[h], to + 2 * kOpA + h * kOpB + q * 4096, vb[q], k);
+        }
+    };
+
+    f32x16 acc[TM][TN] = {};
+    const int steps = g.depth / kDepth;
+    load(0);
+    for (int step = 0; step < steps; step++) {
+        __syncthreads();  // this step's operands are there, and everybody has read the last one's
+        const unsigned char* at = lds + (step & 1) * kStage;
+        half8 a[2][TM][2], b[2][TN][2];
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const int c = k * 2 + (lane >> 5);
+#pragma unroll
+            for (int x = 0; x < TM; x++) {
+                const int r = wi + x * 32 + (lane & 31);
+#pragma unroll
+                for (int h = 0; h < 2; h++) a[k][x][h] = *reinterpret_cast<const half8*>(at + h * kOpA + r * 64 + ((c ^ ((r >> 2) & 3)) << 4));
+            }
+#pragma unroll
+            for (int y = 0; y < TN; y++) {
+                const int r = wj + y * 32 + (lane & 31);
+#pragma unroll
+                for (int h = 0; h < 2; h++) b[k][y][h] = *reinterpret_cast<const half8*>(at + 2 * kOpA + h * kOpB + r * 64 + ((c ^ ((r >> 2) & 3)) << 4));
+            }
+        }
+        if (step + 1 < steps) load(step + 1);
+#pragma unroll
+        for (int k = 0; k < 2; k++)
+#pragma unroll
+            for (int x = 0; x < TM; x++)
+#pragma unroll
+                for (int y = 0; y < TN; y++) {
+                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[k][x][1], b[k][y][0], acc[x][y], 0, 0, 0);
+                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[k][x][0], b[k][y][1], acc[x][y], 0, 0, 0);
+                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[k][x][0], b[k][y][0], acc[x][y], 0, 0, 0);
+                }
+    }
+    __syncthreads();
+
+    // The results as an image in LDS, first as fp32, then, read row by row, as pairs in the same places, which the transpose is
+    // written from.  Columns are exchanged in pieces of 16 by bits of the row, so that eight rows of a column and both halves of
+    // a wave fall on different banks.
+    uint32_t* img = reinterpret_cast<uint32_t*>(lds);
+    auto place = [&](int r, int c) { return r * BN + (c ^ (((((r >> 3) & 3) << 4) ^ (((r >> 2) & 1) << 5)) & (BN - 1))); };
+#pragma unroll
+    for (int x = 0; x < TM; x++)
+#pragma unroll
+        for (int y = 0; y < TN; y++)
+#pragma unroll
+            for (int k = 0; k < 16; k++) {
+                const int r = wi + x * 32 + (k >> 2) * 8 + (lane >> 5) * 4 + (k & 3), c = wj + y * 32 + (lane & 31);
+                img[place(r, c)] = __float_as_uint(acc[x][y][k]);
+            }
+    __syncthreads();
+    constexpr int kChunks = BN / 8;
+    for (int e = tid; e < BM * kChunks; e += kThreads) {
+        const int r = e / kChunks, c = (e - r * kChunks) * 8, i = i0 + r, j = j0 + c;
+        uint32_t* from = img + place(r, c);
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++) v[k] = __uint_as_float(from[k]);
+        if (KIND == kLast) {
+            if (i >= g.rows) continue;
+            const int64_t at = (int64_t)grp * s.R * s.K + (int64_t)i * s.K + j;
+#pragma unroll
+            for (int k = 0; k < 8; k++)
+                if (j + k < g.cols) finish_one(s, args, at + k, v[k] * (1.f / (kScale * kScale)));
+            continue;
+        }
+        const bool in = i < g.rows && j < g.out.ld;
+        _Float16* to = g.out.hi + grp * g.out.step + (int64_t)i * g.out.ld + j;
+        u32x4 ah = {}, al = {};
+        if (KIND == kSquare && in) {
+            const _Float16* pa2 = g.p.hi + grp * g.p.step + (int64_t)i * g.p.ld + j;
+            ah = *reinterpret_cast<const u32x4*>(pa2);
+            al = *reinterpret_cast<const u32x4*>(pa2 + g.p.plane);
+        }
+        uint32_t p[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+            float w = v[k] * (1.f / kScale);
+            if (KIND == kSquare) {
+                const uint32_t hw = ah[k >> 1] >> ((k & 1) * 16), lw = al[k >> 1] >> ((k & 1) * 16);
+                w = kC * w + (kB * (of_half(hw & 0xffffu) + of_half(lw & 0xffffu)) + (i == j + k ? kA * kScale : 0.f));
+            }
+            p[k] = i < g.rows && j + k < g.cols ? pack_pair(w) : 0u;
+            from[k] = p[k];
+        }
+        if (in) {
+            u32x4 hi, lo;
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                hi[k] = __builtin_amdgcn_perm(p[2 * k + 1], p[2 * k], 0x05040100u);
+                lo[k] = __builtin_amdgcn_perm(p[2 * k + 1], p[2 * k], 0x07060302u);
+            }
+            *reinterpret_cast<u32x4*>(to) = hi;
+            *reinterpret_cast<u32x4*>(to + g.out.plane) = lo;
+        }
+    }
+    if (KIND == kLast || (KIND != kUpdate && bi == bj)) return;
+    __syncthreads();
+    const Pair turn = KIND == kUpdate ? g.turn : g.out;
+    for (int e = tid; e < BN * (BM / 8); e += kThreads) {
+        // four pieces of eight rows side by side, then the columns
+        const int piece4 = e & 3, rest = e >> 2, c = rest % BN, r = (rest / BN) * 32 + piece4 * 8, i = i0 + r, j = j0 + c;
+        if (j >= g.cols || i >= turn.ld) continue;
+        uint32_t p[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++) p[k] = img[place(r + k, c)];
+        u32x4 hi, lo;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            hi[k] = __builtin_amdgcn_perm(p[2 * k + 1], p[2 * k], 0x05040100u);
+            lo[k] = __builtin_amdgcn_perm(p[2 * k + 1], p[2 * k], 0x07060302u);
+        }
+        _Float16* to = turn.hi + grp * turn.step + (int64_t)j * turn.ld + i;
+        *reinterpret_cast<u32x4*>(to) = hi;
+        *reinterpret_cast<u32x4*>(to + turn.plane) = lo;
+    }
+}
+
 uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
 unsigned blocks(int64_t n, int64_t per) { return (unsigned)((n + per - 1) / per); }
+int padded(int64_t n) { return (int)((n + kDepth - 1) / kDepth * kDepth); }
+
+template <int B, Kind KIND>
+void launch(const Shape& s, const Args& a, Product g, hipStream_t stream) {
+    g.tiles_i = (g.rows + B - 1) / B;
+    g.tiles_j = (g.cols + B - 1) / B;
+    g.tiles = KIND == kGram || KIND == kSquare ? g.tiles_i * (g.tiles_i + 1) / 2 : g.tiles_i * g.tiles_j;
+    CANVAS_LAUNCH((k_product<B, B, KIND>), dim3((unsigned)(g.tiles * s.G)), dim3(kThreads), 0, stream, s, a, g);
+}
+template <Kind KIND>
+void product(const Shape& s, const Args& a, const Product& g, hipStream_t stream) {
+    const int64_t ti = (g.rows + 127) / 128, tj = (g.cols + 127) / 128;
+    const int64_t tiles = s.G * (KIND == kGram || KIND == kSquare ? ti * (ti + 1) / 2 : ti * tj);
+    if (tiles >= 128)
+        launch<128, KIND>(s, a, g, stream);
+    else
+        launch<64, KIND>(s, a, g, stream);
+}
 
 }  // namespace
 
@@ -109,8 +369,10 @@ Plan plan_of(const Shape& s) {
     Plan p;
     p.parts = (int)((s.R * s.K + 16 * kThreads - 1) / (16 * kThreads));
     if (p.parts > 256) p.parts = 256;
-    p.launches = 3 + 3 * s.steps;
-    p.workspace_bytes = up256(8ull * s.G * p.parts) + 2 * up256(4ull * s.G * s.m * s.n) + 2 * up256(4ull * s.G * s.m * s.m);
+    p.launches = s.steps ? 2 + 3 * s.steps : 2;
+    p.workspace_bytes = up256(8ull * s.G * p.parts);
+    if (s.steps)
+        p.workspace_bytes += 2 * up256(4ull * s.G * s.m * padded(s.n)) + 2 * up256(4ull * s.G * s.n * padded(s.m)) + 2 * up256(4ull * s.G * s.m * padded(s.m));
     return p;
 }
 
@@ -121,24 +383,35 @@ void step(const Shape& s, const Plan& p, const Args& a, hipStream_t stream) {
         at += up256(bytes);
         return r;
     };
+    auto pair = [&](int64_t rows, int64_t cols) {
+        Pair q;
+        q.ld = padded(cols);
+        q.plane = rows * q.ld;
+        q.step = 2 * q.plane;
+        q.hi = (_Float16*)take(4ull * s.G * q.plane);
+        return q;
+    };
     double* sums = (double*)take(8ull * s.G * p.parts);
-    float* x = (float*)take(4ull * s.G * s.m * s.n);
-    float* x2 = (float*)take(4ull * s.G * s.m * s.n);
-    float* q = (float*)take(4ull * s.G * s.m * s.m);
-    float* b = (float*)take(4ull * s.G * s.m * s.m);
-    const unsigned G = (unsigned)s.G, all = blocks(s.R * s.K, kThreads);
+    const unsigned G = (unsigned)s.G;
     CANVAS_LAUNCH(k_mix, dim3(p.parts, G), dim3(kThreads), 0, stream, s, a, sums);
-    CANVAS_LAUNCH(k_start, dim3(all, G), dim3(kThreads), 0, stream, s, a, sums, p.parts, x);
-    const dim3 tt(kTile * kTile), gq(blocks(s.m, kTile), blocks(s.m, kTile), G), gx(blocks(s.n, kTile), blocks(s.m, kTile), G);
-    for (int k = 0; k < s.steps; k++) {
-        CANVAS_LAUNCH(k_product<true>, gq, tt, 0, stream, x, x, (const float*)nullptr, q, s.m, s.m, s.n, 1.f, 0.f, s.m * s.n, s.m * s.n, s.m * s.m);
-        CANVAS_LAUNCH(k_product<true>, gq, tt, 0, stream, q, q, q, b, s.m, s.m, s.m, kC, kB, s.m * s.m, s.m * s.m, s.m * s.m);
-        CANVAS_LAUNCH(k_product<false>, gx, tt, 0, stream, b, x, x, x2, s.m, s.n, s.m, 1.f, kA, s.m * s.m, s.m * s.n, s.m * s.n);
-        float* t = x;
-        x = x2;
-        x2 = t;
+    if (!s.steps) {
+        CANVAS_LAUNCH(k_normalised, dim3(blocks(s.R * s.K, kThreads), G), dim3(kThreads), 0, stream, s, a, sums, p.parts);
+        return;
     }
-    CANVAS_LAUNCH(k_finish, dim3(all, G), dim3(kThreads), 0, stream, s, a, x);
+    Pair x[2] = {pair(s.m, s.n), pair(s.m, s.n)}, xt[2] = {pair(s.n, s.m), pair(s.n, s.m)}, q = pair(s.m, s.m), b = pair(s.m, s.m);
+    CANVAS_LAUNCH(k_start, dim3(blocks(s.K, 64) * blocks(s.R, 64), G), dim3(kThreads), 0, stream, s, a, sums, p.parts, x[0], xt[0]);
+    const int m = (int)s.m, n = (int)s.n;
+    for (int k = 0; k < s.steps; k++) {
+        const Pair &from = x[k & 1], &from_t = xt[k & 1], &to = x[~k & 1], &to_t = xt[~k & 1];
+        product<kGram>(s, a, Product{from, from, m, m, from.ld, q, q, 0, 0, 0}, stream);
+        product<kSquare>(s, a, Product{q, q, m, m, q.ld, b, b, 0, 0, 0}, stream);
+        if (k + 1 < s.steps)
+            product<kUpdate>(s, a, Product{b, from_t, m, n, b.ld, to, to_t, 0, 0, 0}, stream);
+        else if (s.tall)
+            product<kLast>(s, a, Product{from_t, b, n, m, b.ld, to, to_t, 0, 0, 0}, stream);
+        else
+            product<kLast>(s, a, Product{b, from_t, m, n, b.ld, to, to_t, 0, 0, 0}, stream);
+    }
 }
 
 }  // namespace ortho
