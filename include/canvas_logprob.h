@@ -33,6 +33,7 @@ extern "C" {
 #endif
 
 #define CANVAS_LOGPROB_MAX_TOP 64
+#define CANVAS_LOGPROB_MAX_CLASSES (1 << 22)
 
 typedef struct canvas_logprob canvas_logprob;
 
@@ -42,8 +43,8 @@ typedef struct canvas_logprob_info {
     double min_bytes_fwd, min_bytes_bwd;    /* logits read once, or read and written once; without a mask */
 } canvas_logprob_info;
 
-/* Host only.  rows >= 1, classes >= 1 (both < 2^31), dt: type of logits and dlogits, 0 <= top_k <= CANVAS_LOGPROB_MAX_TOP.
- * opt: flags 0 or CANVAS_OPT_INFERENCE (no backward).  Errors: BAD_ARG, UNSUPPORTED. */
+/* Host only.  1 <= rows < 2^31, 1 <= classes <= CANVAS_LOGPROB_MAX_CLASSES, dt: type of logits and dlogits,
+ * 0 <= top_k <= CANVAS_LOGPROB_MAX_TOP.  opt: flags 0 or CANVAS_OPT_INFERENCE (no backward).  Errors: BAD_ARG, UNSUPPORTED (too many rows or classes). */
 int canvas_logprob_compile(int64_t rows, int64_t classes, canvas_dtype dt, int32_t top_k, const canvas_options* opt,
                            canvas_logprob** out);
 

@@ -46,7 +46,7 @@ int canvas_logprob_compile(int64_t rows, int64_t classes, canvas_dtype dt, int32
         uint32_t flags = 0;
         if (int rc = check_options(opt, CANVAS_OPT_INFERENCE, flags)) return rc;
         if (rows < 1 || classes < 1) return set_last_error(CANVAS_BAD_ARG, "rows and classes must be at least 1");
-        if (rows > INT32_MAX || classes > INT32_MAX) return set_last_error(CANVAS_UNSUPPORTED, "rows and classes must be below 2^31");
+        if (rows > INT32_MAX || classes > CANVAS_LOGPROB_MAX_CLASSES) return set_last_error(CANVAS_UNSUPPORTED, "too many rows or classes");
         if (top_k < 0 || top_k > CANVAS_LOGPROB_MAX_TOP) return set_last_error(CANVAS_BAD_ARG, "top_k out of range");
         auto h = std::make_unique<canvas_logprob>();
         h->s.rows = rows;

@@ -1,143 +1,524 @@
-// Log probabilities of given tokens: a workgroup of 256 threads per row, which reads the row once for its largest logit, once
-// for the sums and once for every alternative.
+// Log probabilities of given tokens.
+//
+// Forward: a row, or a segment of a long one, is read once, 16 bytes per load.  Every thread keeps the largest logit m that it
+// has met, S = sum exp(z - z_m) and sum exp(z - z_m) (z - z_m), rescaled whenever m grows, so every exponential is
+// taken once; the threads' are joined in a fixed order.  Segments leave theirs, and their best keys, to a second launch.
+//
+// Alternatives: classes are ordered by whole numbers of 64 bits (order_of the logit, then the complement of the index), all
+// different.  Every thread finds its best class on the way; the k-th best of the threads' best is a lower bound for the k-th
+// best of all, and only the k threads whose best reaches it can hold classes that do: at most k times a thread's classes, few
+// in general.  Those threads read theirs again; what reaches the bound is collected in LDS and ranked by counting.
+//
+// Backward: element by element from the row's (m, log S, entropy).
 #include "logprob_kernels.hpp"
+
+#include <algorithm>
 
 #include "device_util.hpp"
 #include "launch.hpp"
+#include "tile_util.hpp"
 
 namespace canvas {
 namespace logprob {
 namespace {
 
-constexpr int kThreads = 256;
+using tile::u32x4;
+constexpr float kInf = __builtin_inff(), kLowest = -3.402823466e38f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kJoin = 256;  // threads per row of the launch that joins segments
 
-__device__ __forceinline__ float ld(const float* p, int64_t i) { return p[i]; }
-__device__ __forceinline__ float ld(const uint16_t* p, int64_t i) { return bf16_to_f32(p[i]); }
-__device__ __forceinline__ void st(float* p, int64_t i, float v) { p[i] = v; }
-__device__ __forceinline__ void st(uint16_t* p, int64_t i, float v) { p[i] = f32_to_bf16(v); }
+template <class T>
+struct Type;
+template <>
+struct Type<float> {
+    static constexpr int kVec = 4;
+    static __device__ __forceinline__ float at(const u32x4& v, int e) { return __uint_as_float(v[e]); }
+    static __device__ __forceinline__ void hide(u32x4& v, int e) { v[e] = 0xff800000u; }
+    static __device__ __forceinline__ float one(const float* p) { return *p; }
+    static __device__ __forceinline__ void put(float* p, float v) { *p = v; }
+};
+template <>
+struct Type<uint16_t> {
+    static constexpr int kVec = 8;
+    static __device__ __forceinline__ float at(const u32x4& v, int e) { return (e & 1) ? tile::hi_f32(v[e >> 1]) : tile::lo_f32(v[e >> 1]); }
+    static __device__ __forceinline__ void hide(u32x4& v, int e) { v[e >> 1] = (e & 1) ? (v[e >> 1] & 0xffffu) | 0xff800000u : (v[e >> 1] & 0xffff0000u) | 0xff80u; }
+    static __device__ __forceinline__ float one(const uint16_t* p) { return bf16_to_f32(*p); }
+    static __device__ __forceinline__ void put(uint16_t* p, float v) { *p = f32_to_bf16(v); }
+};
 
-// Order of the alternatives as whole numbers: NaN first, then larger logits (zeros of both signs are equal), then lower
-// indices.  0 is no alternative.
-constexpr uint32_t kNan = 0xffc00000u;
-__device__ __forceinline__ uint64_t key_of(float v, uint32_t index) {
-    const uint32_t u = __float_as_uint(v + 0.f);
-    const uint32_t o = v != v ? kNan : (u & 0x80000000u) ? ~u : u | 0x80000000u;
-    return (uint64_t)o << 32 | (uint32_t)~index;
+// kVec logits, or their bytes of the mask, from index i on, some of them behind `end` (-inf, and 0): one by one, in few registers.
+template <class T>
+__device__ __forceinline__ u32x4 last_logits(const T* z, int i, int end) {
+    constexpr int V = Type<T>::kVec;
+    u32x4 v{};
+#pragma unroll 1
+    for (int e = 0; e < V; e++) {
+        const uint32_t x = __float_as_uint(i + e < end ? Type<T>::one(z + i + e) : -kInf);
+        if (V == 4) {
+            v = u32x4{v[1], v[2], v[3], x};
+        } else {
+            v = u32x4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16 | (x & 0xffff0000u)};
+        }
+    }
+    return v;
 }
-__device__ __forceinline__ float value_of(uint64_t key) {
-    const uint32_t o = (uint32_t)(key >> 32);
+template <int V>
+__device__ __forceinline__ uint64_t mask_bytes(const uint8_t* mask, int i, int end) {
+    uint64_t w = 0;
+    if (i + V <= end) {
+        __builtin_memcpy(&w, mask + i, V);
+    } else {
+#pragma unroll 1
+        for (int e = V - 1; e >= 0; e--) w = w << 8 | (i + e < end ? mask[i + e] : 0);
+    }
+    return w;
+}
+__device__ __forceinline__ bool allowed(uint64_t w, int e) { return ((e < 4 ? (uint32_t)w : (uint32_t)(w >> 32)) >> ((e & 3) * 8)) & 0xffu; }
+
+// Vector number `at` of `end` logits; -inf behind them and where the mask hides them.
+template <class T>
+__device__ __forceinline__ u32x4 load_vector(const T* z, int at, int end, const uint8_t* mask) {
+    using Y = Type<T>;
+    constexpr int V = Y::kVec;
+    const int i = at * V;
+    u32x4 v;
+    if (i + V <= end)
+        __builtin_memcpy(&v, z + i, 16);
+    else if (i < end)
+        v = last_logits(z, i, end);
+    else
+        v = V == 4 ? u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u} : u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u};
+    if (mask && i < end) {
+        const uint64_t w = mask_bytes<V>(mask, i, end);
+#pragma unroll
+        for (int e = 0; e < V; e++)
+            if (!allowed(w, e)) Y::hide(v, e);
+    }
+    return v;
+}
+
+// The order of logits as whole numbers: NaN above all, zeros of both signs equal.  -inf is kNone, below every other.
+constexpr uint32_t kNan = 0xffc00000u, kNone = 0x007fffffu;
+__device__ __forceinline__ uint32_t order_of(float v) {
+    const uint32_t u = __float_as_uint(v + 0.f);
+    return v != v ? kNan : (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t o) {
     return o == kNan ? __uint_as_float(0x7fc00000u) : __uint_as_float((o & 0x80000000u) ? o & 0x7fffffffu : ~o);
 }
+__device__ __forceinline__ uint64_t key_of(uint32_t o, uint32_t index) { return o <= kNone ? 0 : (uint64_t)o << 32 | (uint32_t)~index; }
 
-template <class V, class F>
-__device__ V over_row(V v, V* buf, F join) {
+struct Largest {
+    static __device__ __forceinline__ float of(float a, float b) { return fmaxf(a, b); }
+};
+struct Total {
+    static __device__ __forceinline__ float of(float a, float b) { return a + b; }
+};
+template <class J, int LANES = 64>
+__device__ __forceinline__ float over_wave(float v) {  // of LANES lanes side by side
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) v = J::of(v, __shfl_xor(v, o));
+    return v;
+}
+// Over the THREADS threads of a row: a wave, or a workgroup through `buf` (one float per wave; a barrier before it is used
+// again is the caller's).
+template <int THREADS, class J>
+__device__ __forceinline__ float over_row(float v, float* buf) {
+    v = over_wave<J>(v);
+    if (THREADS == 64) return v;
+    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
     __syncthreads();
-    buf[threadIdx.x] = v;
-    __syncthreads();
-    for (int o = kThreads / 2; o; o >>= 1) {
-        if ((int)threadIdx.x < o) buf[threadIdx.x] = join(buf[threadIdx.x], buf[threadIdx.x + o]);
-        __syncthreads();
-    }
-    return buf[0];
+    return over_wave<J, THREADS / 64>(buf[threadIdx.x & (THREADS / 64 - 1)]);
 }
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_fwd(Shape s, Fwd a) {
-    __shared__ uint64_t ibuf[kThreads];
-    __shared__ float fbuf[kThreads];
-    const int64_t row = blockIdx.x;
-    const T* z = static_cast<const T*>(a.logits) + row * a.pitch;
-    const uint8_t* mask = a.mask ? a.mask + row * a.mask_pitch : nullptr;
-    const float inf = __builtin_inff();
-    auto at = [&](int64_t i) { return mask && !mask[i] ? -inf : ld(z, i); };
-    float m = -inf;
-    for (int64_t i = threadIdx.x; i < s.classes; i += kThreads) m = fmaxf(m, at(i));  // (fmaxf drops NaN: the sums below have it)
-    m = over_row(m, fbuf, [](float x, float y) { return fmaxf(x, y); });
-    const float most = m == -inf ? 0.f : m;
-    float sum = 0.f, along = 0.f;
-    for (int64_t i = threadIdx.x; i < s.classes; i += kThreads) {
-        const float v = at(i);
-        const float d = (v - most) * a.it, e = v == -inf ? 0.f : expf(d);
-        sum += e;
-        if (e != 0.f) along += e * d;
-    }
-    auto add = [](float x, float y) { return x + y; };
-    sum = over_row(sum, fbuf, add);
-    along = over_row(along, fbuf, add);
-    const bool empty = sum == 0.f;
-    const float log_sum = empty ? -inf : logf(sum), entropy = empty ? 0.f : log_sum - along / sum;
-    if (threadIdx.x == 0) {
-        if (a.ws) reinterpret_cast<Row*>(a.ws)[row] = Row{most, log_sum, entropy, 0.f};
-        if (a.entropy) a.entropy[row] = entropy;
-        if (a.tokens) {
-            const int64_t t = a.tokens[row];
-            float lp = 0.f;
-            if (t >= 0 && t < s.classes) {
-                const float v = at(t);
-                lp = empty || (v == -inf && !(sum != sum)) ? -inf : (v - most) * a.it - log_sum;
+// The k largest of the keys that the THREADS threads of the workgroup hold, in descending order to `put(rank, key)`, 0 past
+// the last one.  best: this thread's largest key; each(f): calls f for its keys.  lds: THREADS keys, then k times the keys of
+// a thread.
+template <int THREADS, class EACH, class PUT>
+__device__ void select_keys(int k, uint64_t best, uint64_t* lds, EACH each, PUT put) {
+    __shared__ uint64_t s_bound;
+    __shared__ uint32_t s_count;
+    uint64_t* list = lds + THREADS;
+    lds[threadIdx.x] = best;
+    if (threadIdx.x == 0) s_count = 0;
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        constexpr int kEach = THREADS / 64;
+        uint64_t b[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; e++) b[e] = lds[e * 64 + threadIdx.x];
+        auto count = [&](auto pred) {
+            int n = 0;
+#pragma unroll
+            for (int e = 0; e < kEach; e++) n += __popcll(__ballot(pred(b[e])));
+            return n;
+        };
+        uint64_t bound = 1;  // (of k threads or fewer that hold anything: everything)
+        if (count([](uint64_t v) { return v != 0; }) > k) {
+            uint32_t t = 0;
+            int n = THREADS;
+            for (int bit = 31; bit >= 0 && n != k; bit--) {
+                const uint32_t c = t | 1u << bit;
+                const int m = count([=](uint64_t v) { return (uint32_t)(v >> 32) >= c; });
+                if (m >= k) {
+                    t = c;
+                    n = m;
+                }
             }
-            a.logprob[row] = lp;
+            uint32_t low = 0;
+            if (n > k) {  // equal logits among the threads' best: the lower indices
+                const int r = k - count([=](uint64_t v) { return (uint32_t)(v >> 32) > t; });
+                n = THREADS;
+                for (int bit = 31; bit >= 0 && n != r; bit--) {
+                    const uint32_t c = low | 1u << bit;
+                    const int m = count([=](uint64_t v) { return (uint32_t)(v >> 32) == t && (uint32_t)v >= c; });
+                    if (m >= r) {
+                        low = c;
+                        n = m;
+                    }
+                }
+            }
+            bound = (uint64_t)t << 32 | low;
         }
+        if (threadIdx.x == 0) s_bound = bound;
     }
-    uint64_t last = ~(uint64_t)0;
-    for (int k = 0; k < s.top; k++) {
-        uint64_t best = 0;
-        for (int64_t i = threadIdx.x; i < s.classes; i += kThreads) {
-            const float v = at(i);
-            if (v == -inf) continue;
-            const uint64_t key = key_of(v, (uint32_t)i);
-            if (key < last && key > best) best = key;
+    __syncthreads();
+    const uint64_t bound = s_bound;
+    if (best >= bound)
+        each([&](uint64_t key) {
+            if (key >= bound) list[atomicAdd(&s_count, 1u)] = key;  // (the ranks below do not depend on the places)
+        });
+    __syncthreads();
+    const int n = (int)s_count;
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+        const uint64_t key = list[i];
+        int rank = 0;
+        for (int j = 0; j < n; j++) rank += list[j] > key;
+        if (rank < k) put(rank, key);
+    }
+    for (int i = n + threadIdx.x; i < k; i += THREADS) put(i, (uint64_t)0);
+}
+
+// What a segment leaves for the join.
+struct alignas(16) Part {
+    float m, sum, along, unused;
+};
+
+__device__ __forceinline__ void write_row(const Fwd& a, int64_t row, const Row& r) {
+    if (a.ws) reinterpret_cast<Row*>(a.ws)[row] = r;
+    if (a.entropy) a.entropy[row] = r.entropy;
+}
+// The largest logit so far (the lowest finite value before any), S and sum relative to it, the latter in units of log 2.
+struct Running {
+    float m = kLowest, sum = 0.f, along = 0.f;
+    // Relative to a larger m.  (-300: below it the factor is zero, and the product must not be 0 * inf)
+    __device__ __forceinline__ void raise(float to, float scale) {
+        const float d = (m - to) * scale, f = __builtin_amdgcn_exp2f(d);
+        along = f * (along + sum * fmaxf(d, -300.f));
+        sum *= f;
+        m = to;
+    }
+    __device__ __forceinline__ void add(float v, float scale) {
+        const float d = (v - m) * scale, x = __builtin_amdgcn_exp2f(d);
+        sum += x;
+        along += x * fmaxf(d, -300.f);
+    }
+};
+
+__device__ __forceinline__ Row row_of(const Running& r) {
+    const bool empty = r.sum == 0.f;
+    return Row{r.m, empty ? -kInf : logf(r.sum), empty ? 0.f : logf(r.sum) - r.along / r.sum, 0.f};
+}
+template <class T>
+__device__ __forceinline__ void write_token(const Shape& s, const Fwd& a, int64_t row, const Row& r) {
+    if (!a.tokens) return;
+    const int64_t t = a.tokens[row];
+    float lp = 0.f;
+    if (t >= 0 && t < s.classes) {
+        const bool hidden = a.mask && !a.mask[row * a.mask_pitch + t];
+        const float v = hidden ? -kInf : Type<T>::one(static_cast<const T*>(a.logits) + row * a.pitch + t);
+        lp = r.log_sum == -kInf ? -kInf : (v - r.most) * a.it - r.log_sum;
+    }
+    a.logprob[row] = lp;
+}
+__device__ __forceinline__ void write_top(const Shape& s, const Fwd& a, int64_t row, const Row& r, int rank, uint64_t key) {
+    a.top_index[row * s.top + rank] = key ? (int32_t)~(uint32_t)key : -1;
+    a.top_logprob[row * s.top + rank] = key ? (value_of((uint32_t)(key >> 32)) - r.most) * a.it - r.log_sum : -kInf;
+}
+
+// One segment of `length` classes per workgroup of THREADS threads, or, with a wave per segment, four of them; kSweep vectors of a
+// thread in flight.
+constexpr int kSweep = 4;
+template <class T, int THREADS, bool TOP>
+__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_fwd(Shape s, Plan p, Fwd a) {
+    using Y = Type<T>;
+    constexpr int V = Y::kVec;
+    extern __shared__ uint64_t lds[];
+    __shared__ float buf[3][16];
+    const int tid = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
+    const int64_t tasks = s.rows * p.segments, per = THREADS == 64 ? 4 : 1;
+    const float scale = a.it * kLog2e;
+    for (int64_t first = (int64_t)blockIdx.x * per; first < tasks; first += (int64_t)gridDim.x * per) {
+        const int64_t task = first + (THREADS == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
+        if (THREADS == 64 && task >= tasks) break;  // (a wave of its own: no barriers on this path)
+        const int64_t row = p.segments == 1 ? task : task / p.segments;
+        const int64_t begin = (task - row * p.segments) * p.length;
+        const int end = (int)(p.length < s.classes - begin ? p.length : s.classes - begin);
+        const T* z = static_cast<const T*>(a.logits) + row * a.pitch + begin;
+        const uint8_t* mask = a.mask ? a.mask + row * a.mask_pitch + begin : nullptr;
+        const int vectors = (end + V - 1) / V;
+
+        Running r;
+        float best_value = -kInf;  // this thread's largest logit, and the first vector that has it
+        int best_at = tid;
+        for (int at = 0; at < vectors; at += kSweep * THREADS) {
+            u32x4 v[kSweep];
+            if ((at + kSweep * THREADS) * V <= end && !mask) {
+#pragma unroll
+                for (int q = 0; q < kSweep; q++) __builtin_memcpy(&v[q], z + (at + q * THREADS + tid) * V, 16);
+            } else {
+#pragma unroll
+                for (int q = 0; q < kSweep; q++) v[q] = load_vector(z, at + q * THREADS + tid, end, mask);
+            }
+            float m = r.m;
+#pragma unroll
+            for (int q = 0; q < kSweep; q++) {
+                float w = Y::at(v[q], 0);
+#pragma unroll
+                for (int e = 1; e < V; e++) w = fmaxf(w, Y::at(v[q], e));  // (drops NaN: the sums have it)
+                if (TOP && w > best_value) {
+                    best_value = w;
+                    best_at = at + q * THREADS + tid;
+                }
+                m = fmaxf(m, w);
+            }
+            r.raise(m, scale);
+#pragma unroll
+            for (int q = 0; q < kSweep; q++) {
+                tile::pin(v[q]);  // (unpacked again, not kept)
+#pragma unroll
+                for (int e = 0; e < V; e++) r.add(Y::at(v[q], e), scale);
+            }
         }
-        best = over_row(best, ibuf, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
-        if (threadIdx.x == 0) {
-            a.top_index[row * s.top + k] = best ? (int32_t)~(uint32_t)best : -1;
-            a.top_logprob[row * s.top + k] = best ? (value_of(best) - most) * a.it - log_sum : -inf;
+        const float own = r.sum;
+        r.raise(over_row<THREADS, Largest>(r.m, buf[0]), scale);
+        r.sum = over_row<THREADS, Total>(r.sum, buf[1]);
+        r.along = over_row<THREADS, Total>(r.along, buf[2]) * kLn2;
+        const Row whole = row_of(r);
+        if (tid == 0) {
+            if (p.segments == 1) {
+                write_row(a, row, whole);
+                write_token<T>(s, a, row, whole);
+            } else {
+                reinterpret_cast<Part*>(a.ws + p.parts_at)[task] = Part{r.m, r.sum, r.along, 0.f};
+            }
         }
-        last = best;
+        if (TOP) {
+            // f(key) for the classes of this thread
+            auto each = [&](auto f) {
+#pragma unroll 1
+                for (int at = tid; at < vectors; at += THREADS) {
+                    const u32x4 v = load_vector(z, at, end, mask);
+#pragma unroll
+                    for (int e = 0; e < V; e++) f(key_of(order_of(Y::at(v, e)), (uint32_t)begin + at * V + e));
+                }
+            };
+            uint64_t best = 0;
+            if (own != own) {  // NaN or an infinity among them
+                each([&](uint64_t key) { best = key > best ? key : best; });
+            } else if (own > 0.f) {
+                const u32x4 v = load_vector(z, best_at, end, mask);
+                int e = V - 1;
+#pragma unroll
+                for (int k = V - 2; k >= 0; k--)
+                    if (Y::at(v, k) == best_value) e = k;
+                best = key_of(order_of(best_value), (uint32_t)begin + best_at * V + e);
+            }
+            uint64_t* keys = reinterpret_cast<uint64_t*>(a.ws + p.keys_at) + task * s.top;
+            select_keys<THREADS>(s.top, best, lds, each, [&](int rank, uint64_t key) {
+                if (p.segments == 1)
+                    write_top(s, a, row, whole, rank, key);
+                else
+                    keys[rank] = key;
+            });
+        }
+        if (THREADS > 64) __syncthreads();  // (the buffers above are free again)
     }
 }
 
+// Joins the segments of a row: at most kMaxSegments of them.
+constexpr int kListKeys = 6144;  // places of the list of candidates
+constexpr int kMaxSegments = 64, kJoinKeys = kMaxSegments * 64 / kJoin;
 template <class T>
-__global__ __launch_bounds__(kThreads) void k_bwd(Shape s, Bwd a) {
-    const int64_t row = blockIdx.x;
-    const T* z = static_cast<const T*>(a.logits) + row * a.pitch;
-    T* dz = static_cast<T*>(a.dlogits) + row * a.dpitch;
-    const uint8_t* mask = a.mask ? a.mask + row * a.mask_pitch : nullptr;
-    const Row r = reinterpret_cast<const Row*>(a.ws)[row];
-    const float inf = __builtin_inff();
-    const int64_t t = a.tokens ? a.tokens[row] : -1;
-    const bool given = t >= 0 && t < s.classes, empty = r.log_sum == -inf;
-    const float g = given && a.dlogprob ? a.dlogprob[row] : 0.f, h = a.dentropy ? a.dentropy[row] : 0.f;
-    for (int64_t i = threadIdx.x; i < s.classes; i += kThreads) {
-        const bool hidden = empty || (mask && !mask[i]);
-        const float v = hidden ? -inf : ld(z, i);
-        const float lp = (v - r.most) * a.it - r.log_sum, p = v == -inf && r.log_sum == r.log_sum ? 0.f : expf(lp);
-        float d = -g * p - (p == 0.f ? 0.f : h * p * (lp + r.entropy));
-        if (i == t) d += g;
-        st(dz, i, hidden ? 0.f : d * a.it);
+__global__ __launch_bounds__(kJoin) void k_join(Shape s, Plan p, Fwd a) {
+    extern __shared__ uint64_t lds[];
+    for (int64_t row = blockIdx.x; row < s.rows; row += gridDim.x) {
+        const Part* parts = reinterpret_cast<const Part*>(a.ws + p.parts_at) + row * p.segments;
+        const int lane = threadIdx.x & 63;
+        const Part mine = lane < p.segments ? parts[lane] : Part{kLowest, 0.f, 0.f, 0.f};
+        Running whole{mine.m, mine.sum, mine.along * kLog2e};
+        whole.raise(over_wave<Largest>(mine.m), a.it * kLog2e);
+        whole.sum = over_wave<Total>(whole.sum);
+        whole.along = over_wave<Total>(whole.along) * kLn2;
+        const Row r = row_of(whole);
+        if (threadIdx.x == 0) {
+            write_row(a, row, r);
+            write_token<T>(s, a, row, r);
+        }
+        if (s.top > 0) {
+            const uint64_t* from = reinterpret_cast<const uint64_t*>(a.ws + p.keys_at) + row * p.segments * s.top;
+            const int n = p.segments * s.top;
+            uint64_t key[kJoinKeys], best = 0;
+#pragma unroll
+            for (int e = 0; e < kJoinKeys; e++) {
+                const int i = e * kJoin + threadIdx.x;
+                key[e] = i < n ? from[i] : 0;
+                best = key[e] > best ? key[e] : best;
+            }
+            select_keys<kJoin>(
+                s.top, best, lds,
+                [&](auto f) {
+#pragma unroll
+                    for (int e = 0; e < kJoinKeys; e++) f(key[e]);
+                },
+                [&](int rank, uint64_t k) { write_top(s, a, row, r, rank, k); });
+            __syncthreads();
+        }
     }
+}
+
+// A wave takes kBwdVecs vectors of 64 x 16 bytes of a row.
+constexpr int kBwdVecs = 4;
+template <class T>
+__global__ __launch_bounds__(256) void k_bwd(Shape s, Bwd a, int pieces) {
+    using Y = Type<T>;
+    constexpr int V = Y::kVec;
+    const int lane = threadIdx.x & 63;
+    const int64_t tasks = s.rows * pieces;
+    for (int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); task < tasks; task += (int64_t)gridDim.x * 4) {
+        const int64_t row = pieces == 1 ? task : task / pieces, begin = (task - row * pieces) * (64 * V * kBwdVecs);
+        constexpr int kPiece = 64 * V * kBwdVecs;
+        const int end = (int)(s.classes - begin < kPiece ? s.classes - begin : kPiece);
+        const T* z = static_cast<const T*>(a.logits) + row * a.pitch + begin;
+        T* dz = static_cast<T*>(a.dlogits) + row * a.dpitch + begin;
+        const uint8_t* mask = a.mask ? a.mask + row * a.mask_pitch + begin : nullptr;
+        u32x4 v[kBwdVecs];
+#pragma unroll
+        for (int q = 0; q < kBwdVecs; q++) v[q] = load_vector<T>(z, q * 64 + lane, end, nullptr);
+        const Row r = reinterpret_cast<const Row*>(a.ws)[row];
+        const int64_t t = a.tokens ? a.tokens[row] : -1;
+        const bool given = t >= 0 && t < s.classes, empty = r.log_sum == -kInf;
+        const float g = given && a.dlogprob ? a.dlogprob[row] * a.it : 0.f, h = a.dentropy ? a.dentropy[row] * a.it : 0.f;
+#pragma unroll
+        for (int q = 0; q < kBwdVecs; q++) {
+            const int i = (q * 64 + lane) * V;
+            if (i >= end) break;
+            float d[V];
+#pragma unroll
+            for (int e = 0; e < V; e++) {
+                const float lp = (Y::at(v[q], e) - r.most) * a.it - r.log_sum;
+                const float p = __builtin_amdgcn_exp2f(lp * kLog2e);
+                d[e] = -p * (g + h * (fmaxf(lp, -300.f) + r.entropy));
+                if (begin + i + e == t) d[e] += g;
+                if (empty) d[e] = 0.f;
+            }
+            if (mask) {
+                const uint64_t w = mask_bytes<V>(mask, i, end);
+#pragma unroll
+                for (int e = 0; e < V; e++)
+                    if (!allowed(w, e)) d[e] = 0.f;
+            }
+            if (i + V <= end) {
+                u32x4 w;
+                if (V == 4) {
+#pragma unroll
+                    for (int e = 0; e < 4; e++) w[e] = __float_as_uint(d[e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; e++) w[e] = tile::pack_bf16(d[2 * e & (V - 1)], d[(2 * e + 1) & (V - 1)]);
+                }
+                __builtin_memcpy(dz + i, &w, 16);
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; e++)
+                    if (i + e < end) Y::put(dz + i + e, d[e]);
+            }
+        }
+    }
+}
+
+constexpr int64_t kMostBlocks = 1 << 24;
+unsigned grid_of(int64_t n) { return (unsigned)(n < kMostBlocks ? n : kMostBlocks); }
+uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
+int64_t classes_per_thread(int64_t length, int threads, int vec) { return (length + (int64_t)threads * vec - 1) / ((int64_t)threads * vec) * vec; }
+
+template <class T, int THREADS, bool TOP>
+void fwd(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
+    const int64_t tasks = s.rows * p.segments;
+    const size_t lds = TOP ? 8ull * (THREADS + s.top * classes_per_thread(p.length, THREADS, Type<T>::kVec)) : 0;
+    CANVAS_LAUNCH((k_fwd<T, THREADS, TOP>), dim3(grid_of(THREADS == 64 ? (tasks + 3) / 4 : tasks)), dim3(THREADS == 64 ? 256 : THREADS), lds, stream, s, p, a);
+}
+template <class T>
+void forward_of(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
+    if (p.threads == 64)
+        fwd<T, 64, false>(s, p, a, stream);
+    else if (p.threads == 256)
+        s.top ? fwd<T, 256, true>(s, p, a, stream) : fwd<T, 256, false>(s, p, a, stream);
+    else
+        s.top ? fwd<T, 1024, true>(s, p, a, stream) : fwd<T, 1024, false>(s, p, a, stream);
+    if (p.segments > 1) {
+        const size_t lds = s.top ? 8ull * (kJoin + s.top * kJoinKeys) : 0;
+        CANVAS_LAUNCH(k_join<T>, dim3(grid_of(s.rows)), dim3(kJoin), lds, stream, s, p, a);
+    }
+}
+template <class T>
+void backward_of(const Shape& s, const Bwd& a, hipStream_t stream) {
+    const int piece = 64 * Type<T>::kVec * kBwdVecs;
+    const int pieces = (int)((s.classes + piece - 1) / piece);
+    CANVAS_LAUNCH(k_bwd<T>, dim3(grid_of((s.rows * pieces + 3) / 4)), dim3(256), 0, stream, s, a, pieces);
 }
 
 }  // namespace
 
 Plan plan_of(const Shape& s) {
     Plan p;
-    p.workspace_bytes = (uint64_t)s.rows * sizeof(Row);
+    const int vec = s.bf16 ? 8 : 4;
+    // With alternatives a segment is as long as the list in LDS allows: k times a thread's classes, 48 KB.
+    const int64_t most = s.top ? (int64_t)1024 * (kListKeys / s.top / vec * vec) : s.classes;
+    int64_t n = (s.classes + most - 1) / most;
+    // A few rows leave most compute units idle: segments of 2048 classes or more until there are about as many as those.
+    if (s.rows * n < 256) {
+        const int64_t want = 256 / s.rows, some = s.classes / 2048;
+        n = std::max(n, std::min(want, some));
+    }
+    n = std::min<int64_t>(n, kMaxSegments);
+    p.length = ((s.classes + n - 1) / n + vec - 1) / vec * vec;
+    p.segments = (int)((s.classes + p.length - 1) / p.length);
+    p.threads = !s.top && p.length <= 64 * vec * kSweep ? 64 : p.length <= (int64_t)256 * vec * 2 * kSweep ? 256 : 1024;
+    if (s.top && s.top * classes_per_thread(p.length, p.threads, vec) > kListKeys) p.threads = 1024;
+    const uint64_t tasks = (uint64_t)s.rows * p.segments;
+    p.workspace_bytes = up256((uint64_t)s.rows * sizeof(Row));
+    if (p.segments > 1) {
+        p.parts_at = p.workspace_bytes;
+        p.keys_at = p.parts_at + up256(tasks * sizeof(Part));
+        p.workspace_bytes = p.keys_at + up256(tasks * s.top * 8);
+        p.launches_fwd = 2;
+    }
     return p;
 }
 
-void forward(const Shape& s, const Plan&, const Fwd& a, hipStream_t stream) {
+void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
     if (s.bf16)
-        CANVAS_LAUNCH(k_fwd<uint16_t>, dim3((unsigned)s.rows), dim3(kThreads), 0, stream, s, a);
+        forward_of<uint16_t>(s, p, a, stream);
     else
-        CANVAS_LAUNCH(k_fwd<float>, dim3((unsigned)s.rows), dim3(kThreads), 0, stream, s, a);
+        forward_of<float>(s, p, a, stream);
 }
 
 void backward(const Shape& s, const Plan&, const Bwd& a, hipStream_t stream) {
     if (s.bf16)
-        CANVAS_LAUNCH(k_bwd<uint16_t>, dim3((unsigned)s.rows), dim3(kThreads), 0, stream, s, a);
+        backward_of<uint16_t>(s, a, stream);
     else
-        CANVAS_LAUNCH(k_bwd<float>, dim3((unsigned)s.rows), dim3(kThreads), 0, stream, s, a);
+        backward_of<float>(s, a, stream);
 }
 
 }  // namespace logprob

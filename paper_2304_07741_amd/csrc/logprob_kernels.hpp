@@ -13,14 +13,18 @@ struct Shape {
     int top = 0;
 };
 
-// What backward needs of a row: its largest logit (0 where that is -inf), log sum_i exp(z_i - z_max) (-inf for a row
+// What backward needs of a row: its largest logit (the lowest finite value if there is none), log sum_i exp(z_i - z_max) (-inf for a row
 // with nothing left) and the entropy.
 struct alignas(16) Row {
     float most, log_sum, entropy, unused;
 };
 
+// Rows are read in `segments` pieces of `length` classes by `threads` threads.
 struct Plan {
-    uint64_t workspace_bytes = 0;
+    uint64_t workspace_bytes = 0;  // the rows' results first, then those of segments
+    uint64_t parts_at = 0, keys_at = 0;
+    int64_t length = 0;
+    int segments = 1, threads = 0;
     int launches_fwd = 1;
 };
 Plan plan_of(const Shape& s);
