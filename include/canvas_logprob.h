@@ -33,7 +33,7 @@ extern "C" {
 #endif
 
 #define CANVAS_LOGPROB_MAX_TOP 64
-#define CANVAS_LOGPROB_MAX_CLASSES (1 << 22)
+#define CANVAS_LOGPROB_MAX_CLASSES (1 << 20)
 
 typedef struct canvas_logprob canvas_logprob;
 

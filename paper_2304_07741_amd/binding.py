@@ -36,7 +36,7 @@ CANVAS_GATE_NONE, CANVAS_GATE_SIGMOID, CANVAS_GATE_SILU = 0, 1, 2
 # include/canvas_logprob.h
 LOGPROB_EXPORTS = ["canvas_logprob_compile", "canvas_logprob_query", "canvas_logprob_forward", "canvas_logprob_backward", "canvas_logprob_destroy"]
 CANVAS_LOGPROB_MAX_TOP = 64
-CANVAS_LOGPROB_MAX_CLASSES = 1 << 22
+CANVAS_LOGPROB_MAX_CLASSES = 1 << 20
 # include/canvas_ortho.h
 ORTHO_EXPORTS = ["canvas_ortho_compile", "canvas_ortho_query", "canvas_ortho_step", "canvas_ortho_destroy"]
 CANVAS_ORTHO_NESTEROV = 1

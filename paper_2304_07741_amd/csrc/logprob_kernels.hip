@@ -7,13 +7,15 @@
 // Alternatives: classes are ordered by whole numbers of 64 bits (order_of the logit, then the complement of the index), all
 // different.  Every thread finds its best class on the way; the k-th best of the threads' best is a lower bound for the k-th
 // best of all, and only the k threads whose best reaches it can hold classes that do: at most k times a thread's classes, few
-// in general.  Those threads read theirs again; what reaches the bound is collected in LDS and ranked by counting.
+// in general.  Theirs are read again, spread over the workgroup; what reaches the bound is collected in LDS and ranked by
+// counting.
 //
 // Backward: element by element from the row's (m, log S, entropy).
 #include "logprob_kernels.hpp"
 
 #include <algorithm>
 
+#include "../../include/canvas_logprob.h"
 #include "device_util.hpp"
 #include "launch.hpp"
 #include "tile_util.hpp"
@@ -25,13 +27,16 @@ namespace {
 using tile::u32x4;
 constexpr float kInf = __builtin_inff(), kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kMostClassesLog = 20;
+constexpr uint32_t kMostClasses = 1u << kMostClassesLog;
+static_assert(kMostClasses == CANVAS_LOGPROB_MAX_CLASSES && CANVAS_LOGPROB_MAX_TOP <= 64, "limits of the kernels");
 constexpr int kJoin = 256;  // threads per row of the launch that joins segments
 
 template <class T>
 struct Type;
 template <>
 struct Type<float> {
-    static constexpr int kVec = 4;
+    static constexpr int kVec = 4, kLow = 0;
     static __device__ __forceinline__ float at(const u32x4& v, int e) { return __uint_as_float(v[e]); }
     static __device__ __forceinline__ void hide(u32x4& v, int e) { v[e] = 0xff800000u; }
     static __device__ __forceinline__ float one(const float* p) { return *p; }
@@ -39,7 +44,7 @@ struct Type<float> {
 };
 template <>
 struct Type<uint16_t> {
-    static constexpr int kVec = 8;
+    static constexpr int kVec = 8, kLow = 16;  // (16 bits tell bf16 numbers apart)
     static __device__ __forceinline__ float at(const u32x4& v, int e) { return (e & 1) ? tile::hi_f32(v[e >> 1]) : tile::lo_f32(v[e >> 1]); }
     static __device__ __forceinline__ void hide(u32x4& v, int e) { v[e >> 1] = (e & 1) ? (v[e >> 1] & 0xffffu) | 0xff800000u : (v[e >> 1] & 0xffff0000u) | 0xff80u; }
     static __device__ __forceinline__ float one(const uint16_t* p) { return bf16_to_f32(*p); }
@@ -131,69 +136,94 @@ __device__ __forceinline__ float over_row(float v, float* buf) {
     return over_wave<J, THREADS / 64>(buf[threadIdx.x & (THREADS / 64 - 1)]);
 }
 
+constexpr int kTogether = 8;  // keys compared at a time: the list has as many places more
 // The k largest of the keys that the THREADS threads of the workgroup hold, in descending order to `put(rank, key)`, 0 past
-// the last one.  best: this thread's largest key; each(f): calls f for its keys.  lds: THREADS keys, then k times the keys of
-// a thread.
-template <int THREADS, class EACH, class PUT>
-__device__ void select_keys(int k, uint64_t best, uint64_t* lds, EACH each, PUT put) {
+// the last one.  best: this thread's largest key; pieces: into how many its keys fall; piece(thread, number, f): calls f
+// for each key of one; LOW: bits of the order that may differ.  lds: THREADS keys, then k times the keys of a thread and
+// kTogether.
+template <int THREADS, int LOW, class PIECE, class PUT>
+__device__ void select_keys(int k, uint64_t best, int pieces, uint64_t* lds, PIECE piece, PUT put) {
     __shared__ uint64_t s_bound;
-    __shared__ uint32_t s_count;
+    __shared__ uint32_t s_count, s_holders, s_holder[64];  // (at most k threads reach the bound)
     uint64_t* list = lds + THREADS;
     lds[threadIdx.x] = best;
-    if (threadIdx.x == 0) s_count = 0;
+    if (threadIdx.x == 0) s_count = s_holders = 0;
     __syncthreads();
     if (threadIdx.x < 64) {
         constexpr int kEach = THREADS / 64;
-        uint64_t b[kEach];
+        uint32_t o[kEach], low[kEach];
 #pragma unroll
-        for (int e = 0; e < kEach; e++) b[e] = lds[e * 64 + threadIdx.x];
+        for (int e = 0; e < kEach; e++) {
+            const uint64_t b = lds[e * 64 + threadIdx.x];
+            o[e] = (uint32_t)(b >> 32);
+            low[e] = (uint32_t)b;
+        }
         auto count = [&](auto pred) {
             int n = 0;
 #pragma unroll
-            for (int e = 0; e < kEach; e++) n += __popcll(__ballot(pred(b[e])));
+            for (int e = 0; e < kEach; e++) n += __popcll(__ballot(pred(o[e], low[e])));
             return n;
         };
         uint64_t bound = 1;  // (of k threads or fewer that hold anything: everything)
-        if (count([](uint64_t v) { return v != 0; }) > k) {
+        if (count([](uint32_t x, uint32_t) { return x != 0; }) > k) {
+            // the largest t that k threads or more reach, bit by bit; then, of those that equal it, the lower indices
             uint32_t t = 0;
             int n = THREADS;
-            for (int bit = 31; bit >= 0 && n != k; bit--) {
+            for (int bit = 31; bit >= LOW && n != k; bit--) {
                 const uint32_t c = t | 1u << bit;
-                const int m = count([=](uint64_t v) { return (uint32_t)(v >> 32) >= c; });
+                const int m = count([=](uint32_t x, uint32_t) { return x >= c; });
                 if (m >= k) {
                     t = c;
                     n = m;
                 }
             }
-            uint32_t low = 0;
-            if (n > k) {  // equal logits among the threads' best: the lower indices
-                const int r = k - count([=](uint64_t v) { return (uint32_t)(v >> 32) > t; });
+            uint32_t l = 0;
+            if (n > k) {
+                const int r = k - count([=](uint32_t x, uint32_t) { return x >> LOW > t >> LOW; });
                 n = THREADS;
-                for (int bit = 31; bit >= 0 && n != r; bit--) {
-                    const uint32_t c = low | 1u << bit;
-                    const int m = count([=](uint64_t v) { return (uint32_t)(v >> 32) == t && (uint32_t)v >= c; });
+                l = ~(kMostClasses - 1u);
+                for (int bit = kMostClassesLog - 1; bit >= 0 && n != r; bit--) {
+                    const uint32_t c = l | 1u << bit;
+                    const int m = count([=](uint32_t x, uint32_t y) { return x >> LOW == t >> LOW && y >= c; });
                     if (m >= r) {
-                        low = c;
+                        l = c;
                         n = m;
                     }
                 }
+                // (the bits below LOW are all the same in keys of one order: take them from the keys themselves)
+#pragma unroll
+                for (int e = 0; e < kEach; e++) {
+                    const uint64_t who = __ballot(o[e] >> LOW == t >> LOW);
+                    if (who) t = __builtin_amdgcn_readlane(o[e], __builtin_ctzll(who));
+                }
             }
-            bound = (uint64_t)t << 32 | low;
+            bound = (uint64_t)t << 32 | l;
         }
         if (threadIdx.x == 0) s_bound = bound;
     }
     __syncthreads();
     const uint64_t bound = s_bound;
-    if (best >= bound)
-        each([&](uint64_t key) {
-            if (key >= bound) list[atomicAdd(&s_count, 1u)] = key;  // (the ranks below do not depend on the places)
+    // (the places in both lists do not matter: the ranks do not depend on them)
+    if (best >= bound) s_holder[atomicAdd(&s_holders, 1u)] = threadIdx.x;
+    __syncthreads();
+    const int items = (int)s_holders * pieces;
+    for (int i = threadIdx.x; i < items; i += THREADS) {
+        const int h = i / pieces;
+        piece((int)s_holder[h], i - h * pieces, [&](uint64_t key) {
+            if (key >= bound) list[atomicAdd(&s_count, 1u)] = key;
         });
+    }
     __syncthreads();
     const int n = (int)s_count;
+    if (threadIdx.x < kTogether) list[n + threadIdx.x] = 0;
+    __syncthreads();
     for (int i = threadIdx.x; i < n; i += THREADS) {
         const uint64_t key = list[i];
         int rank = 0;
-        for (int j = 0; j < n; j++) rank += list[j] > key;
+        for (int j = 0; j < n; j += kTogether) {
+#pragma unroll
+            for (int e = 0; e < kTogether; e++) rank += list[j + e] > key;
+        }
         if (rank < k) put(rank, key);
     }
     for (int i = n + threadIdx.x; i < k; i += THREADS) put(i, (uint64_t)0);
@@ -271,8 +301,8 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_fwd(Shape s, 
         Running r;
         float best_value = -kInf;  // this thread's largest logit, and the first vector that has it
         int best_at = tid;
+        u32x4 v[kSweep];
         for (int at = 0; at < vectors; at += kSweep * THREADS) {
-            u32x4 v[kSweep];
             if ((at + kSweep * THREADS) * V <= end && !mask) {
 #pragma unroll
                 for (int q = 0; q < kSweep; q++) __builtin_memcpy(&v[q], z + (at + q * THREADS + tid) * V, 16);
@@ -314,28 +344,35 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_fwd(Shape s, 
             }
         }
         if (TOP) {
-            // f(key) for the classes of this thread
-            auto each = [&](auto f) {
-#pragma unroll 1
-                for (int at = tid; at < vectors; at += THREADS) {
-                    const u32x4 v = load_vector(z, at, end, mask);
+            // f(key) for the classes of a thread's vector
+            auto piece = [&](int thread, int number, auto f) {
+                const int at = number * THREADS + thread;
+                const u32x4 w = load_vector(z, at, end, mask);
 #pragma unroll
-                    for (int e = 0; e < V; e++) f(key_of(order_of(Y::at(v, e)), (uint32_t)begin + at * V + e));
-                }
+                for (int e = 0; e < V; e++) f(key_of(order_of(Y::at(w, e)), (uint32_t)begin + at * V + e));
             };
+            const int pieces = (vectors + THREADS - 1) / THREADS;
             uint64_t best = 0;
             if (own != own) {  // NaN or an infinity among them
-                each([&](uint64_t key) { best = key > best ? key : best; });
+#pragma unroll 1
+                for (int q = 0; q < pieces; q++) piece(tid, q, [&](uint64_t key) { best = key > best ? key : best; });
             } else if (own > 0.f) {
-                const u32x4 v = load_vector(z, best_at, end, mask);
+                u32x4 w = v[0];
+                if (pieces <= kSweep) {  // (a short segment is still in the registers)
+#pragma unroll
+                    for (int q = 1; q < kSweep; q++)
+                        if (best_at == q * THREADS + tid) w = v[q];
+                } else {
+                    w = load_vector(z, best_at, end, mask);
+                }
                 int e = V - 1;
 #pragma unroll
                 for (int k = V - 2; k >= 0; k--)
-                    if (Y::at(v, k) == best_value) e = k;
+                    if (Y::at(w, k) == best_value) e = k;
                 best = key_of(order_of(best_value), (uint32_t)begin + best_at * V + e);
             }
             uint64_t* keys = reinterpret_cast<uint64_t*>(a.ws + p.keys_at) + task * s.top;
-            select_keys<THREADS>(s.top, best, lds, each, [&](int rank, uint64_t key) {
+            select_keys<THREADS, Y::kLow>(s.top, best, pieces, lds, piece, [&](int rank, uint64_t key) {
                 if (p.segments == 1)
                     write_top(s, a, row, whole, rank, key);
                 else
@@ -346,7 +383,7 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_fwd(Shape s, 
     }
 }
 
-// Joins the segments of a row: at most kMaxSegments of them.
+// Joins the segments of a row: at most kMaxSegments of them (with the most alternatives 43 hold the most classes).
 constexpr int kListKeys = 6144;  // places of the list of candidates
 constexpr int kMaxSegments = 64, kJoinKeys = kMaxSegments * 64 / kJoin;
 template <class T>
@@ -367,19 +404,18 @@ __global__ __launch_bounds__(kJoin) void k_join(Shape s, Plan p, Fwd a) {
         }
         if (s.top > 0) {
             const uint64_t* from = reinterpret_cast<const uint64_t*>(a.ws + p.keys_at) + row * p.segments * s.top;
-            const int n = p.segments * s.top;
-            uint64_t key[kJoinKeys], best = 0;
-#pragma unroll
-            for (int e = 0; e < kJoinKeys; e++) {
-                const int i = e * kJoin + threadIdx.x;
-                key[e] = i < n ? from[i] : 0;
-                best = key[e] > best ? key[e] : best;
+            const int n = p.segments * s.top, pieces = (n + kJoin - 1) / kJoin;
+            uint64_t best = 0;
+            for (int q = 0; q < pieces; q++) {
+                const int i = q * kJoin + threadIdx.x;
+                const uint64_t key = i < n ? from[i] : 0;
+                best = key > best ? key : best;
             }
-            select_keys<kJoin>(
-                s.top, best, lds,
-                [&](auto f) {
-#pragma unroll
-                    for (int e = 0; e < kJoinKeys; e++) f(key[e]);
+            select_keys<kJoin, Type<T>::kLow>(
+                s.top, best, pieces, lds,
+                [&](int thread, int number, auto f) {
+                    const int i = number * kJoin + thread;
+                    f(i < n ? from[i] : 0);
                 },
                 [&](int rank, uint64_t k) { write_top(s, a, row, r, rank, k); });
             __syncthreads();
@@ -455,19 +491,17 @@ int64_t classes_per_thread(int64_t length, int threads, int vec) { return (lengt
 template <class T, int THREADS, bool TOP>
 void fwd(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
     const int64_t tasks = s.rows * p.segments;
-    const size_t lds = TOP ? 8ull * (THREADS + s.top * classes_per_thread(p.length, THREADS, Type<T>::kVec)) : 0;
+    const size_t lds = TOP ? 8ull * (THREADS + kTogether + s.top * classes_per_thread(p.length, THREADS, Type<T>::kVec)) : 0;
     CANVAS_LAUNCH((k_fwd<T, THREADS, TOP>), dim3(grid_of(THREADS == 64 ? (tasks + 3) / 4 : tasks)), dim3(THREADS == 64 ? 256 : THREADS), lds, stream, s, p, a);
 }
 template <class T>
 void forward_of(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
     if (p.threads == 64)
         fwd<T, 64, false>(s, p, a, stream);
-    else if (p.threads == 256)
-        s.top ? fwd<T, 256, true>(s, p, a, stream) : fwd<T, 256, false>(s, p, a, stream);
     else
-        s.top ? fwd<T, 1024, true>(s, p, a, stream) : fwd<T, 1024, false>(s, p, a, stream);
+        s.top ? fwd<T, 256, true>(s, p, a, stream) : fwd<T, 256, false>(s, p, a, stream);
     if (p.segments > 1) {
-        const size_t lds = s.top ? 8ull * (kJoin + s.top * kJoinKeys) : 0;
+        const size_t lds = s.top ? 8ull * (kJoin + kTogether + s.top * kJoinKeys) : 0;
         CANVAS_LAUNCH(k_join<T>, dim3(grid_of(s.rows)), dim3(kJoin), lds, stream, s, p, a);
     }
 }
@@ -484,7 +518,7 @@ Plan plan_of(const Shape& s) {
     Plan p;
     const int vec = s.bf16 ? 8 : 4;
     // With alternatives a segment is as long as the list in LDS allows: k times a thread's classes, 48 KB.
-    const int64_t most = s.top ? (int64_t)1024 * (kListKeys / s.top / vec * vec) : s.classes;
+    const int64_t most = s.top ? (int64_t)256 * (kListKeys / s.top / vec * vec) : s.classes;
     int64_t n = (s.classes + most - 1) / most;
     // A few rows leave most compute units idle: segments of 2048 classes or more until there are about as many as those.
     if (s.rows * n < 256) {
@@ -494,8 +528,7 @@ Plan plan_of(const Shape& s) {
     n = std::min<int64_t>(n, kMaxSegments);
     p.length = ((s.classes + n - 1) / n + vec - 1) / vec * vec;
     p.segments = (int)((s.classes + p.length - 1) / p.length);
-    p.threads = !s.top && p.length <= 64 * vec * kSweep ? 64 : p.length <= (int64_t)256 * vec * 2 * kSweep ? 256 : 1024;
-    if (s.top && s.top * classes_per_thread(p.length, p.threads, vec) > kListKeys) p.threads = 1024;
+    p.threads = !s.top && p.length <= 64 * vec * kSweep ? 64 : 256;
     const uint64_t tasks = (uint64_t)s.rows * p.segments;
     p.workspace_bytes = up256((uint64_t)s.rows * sizeof(Row));
     if (p.segments > 1) {
