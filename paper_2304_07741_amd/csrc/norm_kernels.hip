@@ -1,202 +1,821 @@
-// Residual norm, forward and backward: a workgroup takes 64 pixels, its four waves the channels in turn.  Every pass over the
-// channels reads memory again.
+// Residual norm, forward and backward.  Both are bound by memory: five maps move forward, eight backward, and everything in
+// between stays in registers.
+//
+// Maps (planes of two pixels or more): a thread takes 16 bytes of pixels of `KC` channels, lanes side by side GX such pieces, the
+// other lanes and waves the channels in turn; sums over the channels go through lane exchanges and LDS.  The last piece of a
+// plane ends with it and may overlap the one before it: the pixels in common are computed twice, alike, and counted once in
+// the sums of the weights' gradients.  Where a plane is shorter than 16 bytes a thread takes two pixels.
+// Channels that no workgroup can hold (KC = 0) are read again for each of the passes, from the caches for the most part.
+//
+// Rows (planes of one pixel): TPR threads per row, KV times 16 bytes each.
+//
+// Workgroups of the backward kernels walk over tiles and keep the weights' gradients of their channels in registers (KC = 0: in
+// LDS); one partial sum per workgroup is left, which a second launch adds in a fixed order.
 #include "norm_kernels.hpp"
+
+#include <algorithm>
+#include <atomic>
 
 #include "device_util.hpp"
 #include "launch.hpp"
+#include "tile_util.hpp"
 
 namespace canvas {
 namespace norm {
 namespace {
 
-constexpr int kPix = 64, kSlots = 4;
+constexpr int kPost = 1, kPre = 2;
+constexpr float kLog2e = 1.4426950408889634f;
 
-template <class T>
-__device__ __forceinline__ float ld(const void* p, int64_t i);
-template <>
-__device__ __forceinline__ float ld<float>(const void* p, int64_t i) {
-    return static_cast<const float*>(p)[i];
-}
-template <>
-__device__ __forceinline__ float ld<uint16_t>(const void* p, int64_t i) {
-    return bf16_to_f32(static_cast<const uint16_t*>(p)[i]);
-}
-__device__ __forceinline__ void st(float* p, int64_t i, float v) { p[i] = v; }
-__device__ __forceinline__ void st(uint16_t* p, int64_t i, float v) { p[i] = f32_to_bf16(v); }
-
-__device__ __forceinline__ void gate_of(int kind, float g, float& a, float& da) {
-    if (kind == 0) {
-        a = 1.f;
-        da = 0.f;
-        return;
+// N elements of a map as they are in memory.
+template <class T, int N>
+struct Vec {
+    static constexpr int kWords = N * (int)sizeof(T) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ float at(int e) const {
+        if (sizeof(T) == 4) return __uint_as_float(w[e]);
+        return (e & 1) ? tile::hi_f32(w[e >> 1]) : tile::lo_f32(w[e >> 1]);
     }
-    const float s = 1.f / (1.f + expf(-g));
-    a = kind == 1 ? s : g * s;
-    da = kind == 1 ? s * (1.f - s) : s * (1.f + g * (1.f - s));
-}
-
-// Sum over the slots of one pixel.
-__device__ __forceinline__ float over_slots(float v, float (*buf)[kPix]) {
-    __syncthreads();
-    buf[threadIdx.y][threadIdx.x] = v;
-    __syncthreads();
-    float s = 0.f;
-    for (int k = 0; k < kSlots; k++) s += buf[k][threadIdx.x];
-    return s;
-}
-
-template <class T>
-__global__ __launch_bounds__(kPix* kSlots) void k_fwd(Shape s, Fwd a) {
-    __shared__ float buf[kSlots][kPix];
-    const int64_t total = s.N * s.P, q = (int64_t)blockIdx.x * kPix + threadIdx.x;
-    const bool in = q < total;
-    const int64_t n = in ? q / s.P : 0, base = n * s.C * s.P + (in ? q - n * s.P : 0);
-    float r2 = 0.f, r1 = 0.f;
-    if (s.post) {
-        float t = 0.f;
-        if (in)
-            for (int c = threadIdx.y; c < s.C; c += kSlots) {
-                const float z = ld<T>(a.z, base + c * s.P);
-                t += z * z;
-            }
-        r2 = 1.f / sqrtf(over_slots(t, buf) / s.C + s.eps);
+    // What is computed from it behind this point is computed anew: kept results of an earlier pass take more registers than there are.
+    __device__ __forceinline__ void renew() {
+#pragma unroll
+        for (int k = 0; k < kWords; k++) asm volatile("" : "+v"(w[k]));
     }
-    if (in && s.post && a.r2 && threadIdx.y == 0) a.r2[q] = r2;
-    auto joined = [&](int c) {
-        const int64_t i = base + c * s.P;
-        float y = ld<T>(a.x, i);
-        if (s.post) {
-            float g, dg;
-            gate_of(s.gate, s.gate ? ld<T>(a.g, i) : 0.f, g, dg);
-            y += a.scale[c] * g * (ld<T>(a.z, i) * r2 * a.w_post[c]);
+    __device__ __forceinline__ void load(const void* p, int64_t i) { __builtin_memcpy(w, static_cast<const T*>(p) + i, sizeof w); }
+};
+template <class T, int N>
+__device__ __forceinline__ void store(void* p, int64_t i, const float (&v)[N]) {
+    uint32_t w[Vec<T, N>::kWords];
+    if (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < N; e++) w[e % Vec<T, N>::kWords] = __float_as_uint(v[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N / 2; e++) w[e] = tile::pack_bf16(v[2 * e], v[2 * e + 1]);
+    }
+    __builtin_memcpy(static_cast<T*>(p) + i, w, sizeof w);
+}
+
+// act(g) and act'(g)
+struct Act {
+    float a = 1.f, da = 0.f;
+};
+__device__ __forceinline__ Act act_of(int kind, float g) {
+    Act r;
+    const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-g * kLog2e));
+    const float rest = s * (1.f - s);
+    r.a = kind == 1 ? s : g * s;
+    r.da = kind == 1 ? rest : s + g * rest;
+    return r;
+}
+
+// One element of backward from the values in memory and the sums over its pixel.
+struct Element {
+    Act act;
+    float zh = 0.f, xh, du;
+    template <int PARTS>
+    __device__ __forceinline__ void set(int gate, float x, float z, float g, float du_, float sw, float r2, float r1) {
+        if (PARTS & kPost) {
+            if (gate) act = act_of(gate, g);
+            zh = z * r2;
+            x += sw * act.a * zh;
         }
+        xh = x * r1;
+        du = du_;
+    }
+    template <int PARTS>
+    __device__ __forceinline__ float whole(float dy, float w1, float r1, float t1) const {  // D
+        return PARTS & kPre ? dy + r1 * (du * w1 - xh * t1) : dy;
+    }
+};
+
+// ---------------------------------------------------------------- maps
+
+// Where a thread is: piece number `q` of all (n, first pixel), `skip` pixels in common with the piece before it.
+struct Where {
+    bool in;
+    int64_t pixel, base;  // of N * P; of the first channel
+    int skip;
+};
+template <int VEC>
+__device__ __forceinline__ Where where_of(const Shape& s, int pieces, int64_t total, int64_t q) {
+    Where w;
+    w.in = q < total;
+    if (!w.in) q = total - 1;
+    const int64_t n = (uint64_t)q < 0x80000000ull ? (int64_t)((uint32_t)q / (uint32_t)pieces) : q / pieces;
+    const int g = (int)(q - n * pieces);
+    int p = g * VEC;
+    w.skip = 0;
+    if (p + VEC > s.P) {
+        w.skip = (int)(p + VEC - s.P);
+        p = (int)(s.P - VEC);
+    }
+    w.pixel = n * s.P + p;
+    w.base = n * s.C * s.P + p;
+    return w;
+}
+
+// Sums of v over the channel slots of each pixel: lanes gx, gx + GX, ... of all waves.  buf: a row of GX * VEC floats per wave.
+template <int VEC>
+__device__ __forceinline__ void over_channels(float (&v)[VEC], int gx, int GX, float* buf) {
+    for (int o = 32; o >= GX; o >>= 1) {
+#pragma unroll
+        for (int e = 0; e < VEC; e++) v[e] += __shfl_xor(v[e], o);
+    }
+    const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, row = GX * VEC;
+    __syncthreads();
+    if ((int)(threadIdx.x & 63) < GX) {
+#pragma unroll
+        for (int e = 0; e < VEC; e++) buf[wave * row + gx * VEC + e] = v[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < VEC; e++) v[e] = 0.f;
+    for (int w = 0; w < waves; w++) {
+#pragma unroll
+        for (int e = 0; e < VEC; e++) v[e] += buf[w * row + gx * VEC + e];
+    }
+}
+
+template <class T, int VEC, int KC, int PARTS>
+__global__ __launch_bounds__(512) void k_maps_fwd(Shape s, Fwd a, int log_gx, int pieces, int64_t total) {
+    extern __shared__ float lds[];
+    const int GX = 1 << log_gx, gx = threadIdx.x & (GX - 1), cy = threadIdx.x >> log_gx, CY = blockDim.x >> log_gx;
+    const Where at = where_of<VEC>(s, pieces, total, (int64_t)blockIdx.x * GX + gx);
+    const float inv = 1.f / s.C;
+    const bool gated = (PARTS & kPost) && s.gate;
+    constexpr int K = KC ? KC : 1;
+    Vec<T, VEC> x[K], z[K], g[K];
+    auto load_z = [&](int k, int c) { z[k].load(a.z, at.base + c * s.P); };
+    auto load_x = [&](int k, int c) {
+        x[k].load(a.x, at.base + c * s.P);
+        if (gated) g[k].load(a.g, at.base + c * s.P);
+    };
+    // f(k, c) for this thread's channels
+    auto each = [&](auto f) {
+        if constexpr (KC > 0) {
+#pragma unroll
+            for (int k = 0; k < KC; k++) {
+                const int c = cy + k * CY;
+                if (c < s.C) f(k, c);
+            }
+        } else {
+            for (int c = cy; c < s.C; c += CY) f(0, c);
+        }
+    };
+    if (KC) each([&](int k, int c) {
+            if (PARTS & kPost) load_z(k, c);
+            load_x(k, c);
+        });
+    float r2[VEC], t[VEC];
+    if (PARTS & kPost) {
+#pragma unroll
+        for (int e = 0; e < VEC; e++) r2[e] = 0.f;
+        each([&](int k, int c) {
+            if (!KC) load_z(k, c);
+#pragma unroll
+            for (int e = 0; e < VEC; e++) r2[e] += z[k].at(e) * z[k].at(e);
+        });
+        over_channels<VEC>(r2, gx, GX, lds);
+#pragma unroll
+        for (int e = 0; e < VEC; e++) {
+            r2[e] = rsqrtf(r2[e] * inv + s.eps);
+            if (a.r2 && cy == 0 && at.in) a.r2[at.pixel + e] = r2[e];
+        }
+    }
+    auto joined = [&](int k, int e, float sw) {
+        float y = x[k].at(e);
+        if (PARTS & kPost) y += sw * (gated ? act_of(s.gate, g[k].at(e)).a : 1.f) * (z[k].at(e) * r2[e]);
         return y;
     };
-    float t = 0.f;
-    if (in)
-        for (int c = threadIdx.y; c < s.C; c += kSlots) {
-            const float y = joined(c);
-            t += y * y;
-            if (s.post) st((T*)a.x_out, base + c * s.P, y);
+#pragma unroll
+    for (int e = 0; e < VEC; e++) t[e] = 0.f;
+    float y[K][VEC];
+    each([&](int k, int c) {
+        if (!KC) {
+            if (PARTS & kPost) load_z(k, c);
+            load_x(k, c);
         }
-    if (!s.pre) return;
-    r1 = 1.f / sqrtf(over_slots(t, buf) / s.C + s.eps);
-    if (!in) return;
-    if (a.r1 && threadIdx.y == 0) a.r1[q] = r1;
-    for (int c = threadIdx.y; c < s.C; c += kSlots) st((T*)a.u, base + c * s.P, joined(c) * r1 * a.w_pre[c]);
+        const float sw = PARTS & kPost ? a.scale[c] * a.w_post[c] : 0.f;
+#pragma unroll
+        for (int e = 0; e < VEC; e++) {
+            y[k][e] = joined(k, e, sw);
+            t[e] += y[k][e] * y[k][e];
+        }
+        if ((PARTS & kPost) && at.in) store<T, VEC>(a.x_out, at.base + c * s.P, y[k]);
+    });
+    if (!(PARTS & kPre)) return;
+    over_channels<VEC>(t, gx, GX, lds);
+#pragma unroll
+    for (int e = 0; e < VEC; e++) {
+        t[e] = rsqrtf(t[e] * inv + s.eps);
+        if (a.r1 && cy == 0 && at.in) a.r1[at.pixel + e] = t[e];
+    }
+    each([&](int k, int c) {
+        if (!KC) {
+            if (PARTS & kPost) load_z(k, c);
+            load_x(k, c);
+            const float sw = PARTS & kPost ? a.scale[c] * a.w_post[c] : 0.f;
+#pragma unroll
+            for (int e = 0; e < VEC; e++) y[k][e] = joined(k, e, sw);
+        }
+        const float w = a.w_pre[c];
+#pragma unroll
+        for (int e = 0; e < VEC; e++) y[k][e] *= t[e] * w;
+        if (at.in) store<T, VEC>(a.u, at.base + c * s.P, y[k]);
+    });
 }
 
+template <class T, int VEC, int KC, int PARTS>
+__global__ __launch_bounds__(512) void k_maps_bwd(Shape s, Bwd a, int log_gx, int pieces, int64_t total) {
+    extern __shared__ float lds[];
+    const int GX = 1 << log_gx, gx = threadIdx.x & (GX - 1), cy = threadIdx.x >> log_gx, CY = blockDim.x >> log_gx;
+    const float inv = 1.f / s.C;
+    const bool gated = (PARTS & kPost) && s.gate;
+    constexpr int K = KC ? KC : 1;
+    float* sums = lds + (blockDim.x >> 6) * GX * VEC;  // KC = 0: [2][C]
+    float kp[K], kx[K], sw[K], w1[K];
+    auto each = [&](auto f) {
+        if constexpr (KC > 0) {
+#pragma unroll
+            for (int k = 0; k < KC; k++) {
+                const int c = cy + k * CY;
+                if (c < s.C) f(k, c);
+            }
+        } else {
+            for (int c = cy; c < s.C; c += CY) f(0, c);
+        }
+    };
+    auto weights = [&](int k, int c) {
+        sw[k] = PARTS & kPost ? a.scale[c] * a.w_post[c] : 0.f;
+        w1[k] = PARTS & kPre ? a.w_pre[c] : 0.f;
+    };
+#pragma unroll
+    for (int k = 0; k < K; k++) kp[k] = kx[k] = sw[k] = w1[k] = 0.f;
+    if (KC) {
+        each(weights);
+    } else {
+        for (int i = threadIdx.x; i < 2 * s.C; i += blockDim.x) sums[i] = 0.f;
+        __syncthreads();
+    }
+    const int64_t tiles = (total + GX - 1) >> log_gx;
+    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const Where at = where_of<VEC>(s, pieces, total, (tile << log_gx) + gx);
+        Vec<T, VEC> x[K], z[K], g[K], dy[K], du[K];
+        auto load = [&](int k, int c, bool arriving) {
+            const int64_t i = at.base + c * s.P;
+            if (PARTS & kPre) {
+                x[k].load(a.x, i);
+                du[k].load(a.du, i);
+            }
+            if (PARTS & kPost) z[k].load(a.z, i);
+            if (gated) g[k].load(a.g, i);
+            if (arriving && a.dx_out) dy[k].load(a.dx_out, i);
+        };
+        auto renew = [&](int k) {
+            if (PARTS & kPre) {
+                x[k].renew();
+                du[k].renew();
+            }
+            if (PARTS & kPost) z[k].renew();
+            if (gated) g[k].renew();
+        };
+        if (KC) each([&](int k, int c) { load(k, c, true); });
+        float r2[VEC], r1[VEC], t1[VEC], t2[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; e++) {
+            r2[e] = PARTS & kPost ? a.r2[at.pixel + e] : 0.f;
+            r1[e] = PARTS & kPre ? a.r1[at.pixel + e] : 0.f;
+            t1[e] = t2[e] = 0.f;
+        }
+        auto element = [&](int k, int e) {
+            Element v;
+            v.set<PARTS>(s.gate, PARTS & kPre ? x[k].at(e) : 0.f, PARTS & kPost ? z[k].at(e) : 0.f, gated ? g[k].at(e) : 0.f,
+                         PARTS & kPre ? du[k].at(e) : 0.f, sw[k], r2[e], r1[e]);
+            return v;
+        };
+        if (PARTS & kPre) {
+            each([&](int k, int c) {
+                if (!KC) {
+                    weights(k, c);
+                    load(k, c, false);
+                }
+#pragma unroll
+                for (int e = 0; e < VEC; e++) {
+                    const Element v = element(k, e);
+                    t1[e] += v.du * w1[k] * v.xh;
+                }
+            });
+            over_channels<VEC>(t1, gx, GX, lds);
+#pragma unroll
+            for (int e = 0; e < VEC; e++) t1[e] *= inv;
+        }
+        float d[K][VEC];
+        each([&](int k, int c) {
+            if (!KC) {
+                weights(k, c);
+                load(k, c, true);
+            } else {
+                renew(k);
+            }
+            float sp = 0.f, sx = 0.f;
+#pragma unroll
+            for (int e = 0; e < VEC; e++) {
+                const Element v = element(k, e);
+                d[k][e] = v.whole<PARTS>(a.dx_out ? dy[k].at(e) : 0.f, w1[k], r1[e], t1[e]);
+                const float p = d[k][e] * v.act.a * v.zh;
+                t2[e] += p * sw[k];
+                if (e >= at.skip) {
+                    sp += p;
+                    sx += v.du * v.xh;
+                }
+            }
+            if (!at.in) sp = sx = 0.f;
+            if (KC) {
+                kp[k] += sp;
+                kx[k] += sx;
+            } else {
+                for (int o = GX >> 1; o; o >>= 1) {
+                    sp += __shfl_xor(sp, o);
+                    sx += __shfl_xor(sx, o);
+                }
+                if (gx == 0) {
+                    sums[c] += sp;
+                    sums[s.C + c] += sx;
+                }
+            }
+            if ((PARTS & kPre) && at.in) store<T, VEC>(a.dx, at.base + c * s.P, d[k]);
+        });
+        if (PARTS & kPost) {
+            over_channels<VEC>(t2, gx, GX, lds);
+#pragma unroll
+            for (int e = 0; e < VEC; e++) t2[e] *= inv;
+            each([&](int k, int c) {
+                if (!KC) {
+                    weights(k, c);
+                    load(k, c, true);
+                } else {
+                    renew(k);
+                }
+                float dz[VEC], dg[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; e++) {
+                    const Element v = element(k, e);
+                    const float D = KC ? d[k][e] : v.whole<PARTS>(a.dx_out ? dy[k].at(e) : 0.f, w1[k], r1[e], t1[e]);
+                    dz[e] = r2[e] * (D * v.act.a * sw[k] - v.zh * t2[e]);
+                    dg[e] = D * v.act.da * sw[k] * v.zh;
+                }
+                if (at.in) {
+                    store<T, VEC>(a.dz, at.base + c * s.P, dz);
+                    if (gated) store<T, VEC>(a.dg, at.base + c * s.P, dg);
+                }
+            });
+        }
+    }
+    float* out = a.partial + (int64_t)blockIdx.x * 2 * s.C;
+    if (KC) {
+        each([&](int k, int c) {
+            for (int o = GX >> 1; o; o >>= 1) {
+                kp[k] += __shfl_xor(kp[k], o);
+                kx[k] += __shfl_xor(kx[k], o);
+            }
+            if (gx == 0) {
+                out[c] = kp[k];
+                out[s.C + c] = kx[k];
+            }
+        });
+    } else {
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * s.C; i += blockDim.x) out[i] = sums[i];
+    }
+}
+
+// ---------------------------------------------------------------- rows
+
+// Over the TPR threads of a row; buf: a float per wave of the workgroup.
+template <int TPR>
+__device__ __forceinline__ float over_row(float v, float* buf) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    if (TPR == 64) return v;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < TPR / 64; w++) v += buf[w];
+    return v;
+}
+
+// N elements from i on, those behind the row's end as zeros.
+template <class T, int N>
+__device__ __forceinline__ void load_row(Vec<T, N>& v, const void* p, int64_t row, int c, int C) {
+    if (c + N <= C) {
+        v.load(p, row + c);
+        return;
+    }
+#pragma unroll
+    for (int w = 0; w < Vec<T, N>::kWords; w++) v.w[w] = 0;
+#pragma unroll
+    for (int e = 0; e < N; e++)
+        if (c + e < C) {
+            if (sizeof(T) == 4)
+                v.w[e % Vec<T, N>::kWords] = static_cast<const uint32_t*>(p)[row + c + e];
+            else
+                v.w[e >> 1] |= (uint32_t) static_cast<const uint16_t*>(p)[row + c + e] << ((e & 1) * 16);
+        }
+}
+template <class T, int N>
+__device__ __forceinline__ void store_row(void* p, int64_t row, int c, int C, const float (&v)[N]) {
+    if (c + N <= C) {
+        store<T, N>(p, row + c, v);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < N; e++)
+        if (c + e < C) {
+            if (sizeof(T) == 4)
+                static_cast<float*>(p)[row + c + e] = v[e];
+            else
+                static_cast<uint16_t*>(p)[row + c + e] = f32_to_bf16(v[e]);
+        }
+}
+template <int N>
+__device__ __forceinline__ void load_weights(float (&w)[N], const float* p, int c, int C) {
+    if (c + N <= C) {
+        __builtin_memcpy(w, p + c, sizeof w);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < N; e++) w[e] = c + e < C ? p[c + e] : 0.f;
+}
+
+template <int N>
+__device__ __forceinline__ void store_floats(float* p, int c, int C, const float (&v)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; e++)
+        if (c + e < C) p[c + e] = v[e];
+}
+
+template <class T, int TPR, int KV, int PARTS>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_fwd(Shape s, Fwd a) {
+    constexpr int V = 16 / sizeof(T), kRows = TPR < 256 ? 256 / TPR : 1;
+    __shared__ float buf[16];
+    const int t = threadIdx.x % TPR;
+    const int64_t n = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
+    if (n >= s.N) return;  // (with several rows per workgroup a row is a wave: no barriers)
+    const int64_t row = n * s.C;
+    const bool gated = (PARTS & kPost) && s.gate;
+    const float inv = 1.f / s.C;
+    Vec<T, V> x[KV], z[KV], g[KV];
+#pragma unroll
+    for (int k = 0; k < KV; k++) {
+        const int c = (k * TPR + t) * V;
+        load_row<T, V>(x[k], a.x, row, c, s.C);
+        if (PARTS & kPost) load_row<T, V>(z[k], a.z, row, c, s.C);
+        if (gated) load_row<T, V>(g[k], a.g, row, c, s.C);
+    }
+    float r2 = 0.f;
+    if (PARTS & kPost) {
+#pragma unroll
+        for (int k = 0; k < KV; k++)
+#pragma unroll
+            for (int e = 0; e < V; e++) r2 += z[k].at(e) * z[k].at(e);
+        r2 = rsqrtf(over_row<TPR>(r2, buf) * inv + s.eps);
+        if (a.r2 && t == 0) a.r2[n] = r2;
+    }
+    // x' before its rounding, computed again behind the sum of its squares
+    auto joined = [&](int k, float (&y)[V]) {
+        const int c = (k * TPR + t) * V;
+        float sw[V], w[V];
+        x[k].renew();
+        if (PARTS & kPost) {
+            z[k].renew();
+            if (gated) g[k].renew();
+            load_weights<V>(w, a.w_post, c, s.C);
+            load_weights<V>(sw, a.scale, c, s.C);
+        }
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            y[e] = x[k].at(e);
+            if (PARTS & kPost) y[e] += sw[e] * w[e] * (gated ? act_of(s.gate, g[k].at(e)).a : 1.f) * (z[k].at(e) * r2);
+        }
+    };
+    float y[V], r1 = 0.f;
+#pragma unroll
+    for (int k = 0; k < KV; k++) {
+        joined(k, y);
+#pragma unroll
+        for (int e = 0; e < V; e++) r1 += y[e] * y[e];
+        if (PARTS & kPost) store_row<T, V>(a.x_out, row, (k * TPR + t) * V, s.C, y);
+    }
+    if (!(PARTS & kPre)) return;
+    r1 = rsqrtf(over_row<TPR>(r1, buf) * inv + s.eps);
+    if (a.r1 && t == 0) a.r1[n] = r1;
+#pragma unroll
+    for (int k = 0; k < KV; k++) {
+        const int c = (k * TPR + t) * V;
+        float w1[V];
+        load_weights<V>(w1, a.w_pre, c, s.C);
+        if (KV > 1) joined(k, y);
+#pragma unroll
+        for (int e = 0; e < V; e++) y[e] *= r1 * w1[e];
+        store_row<T, V>(a.u, row, c, s.C, y);
+    }
+}
+
+// Rows of 1024 threads have no registers for the sums and the weights of their channels: sums in LDS, weights read again; the
+// longest have none for the values either, which are read again for each pass.
+template <class T, int TPR, int KV, int PARTS>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_bwd(Shape s, Bwd a) {
+    constexpr int V = 16 / sizeof(T), kRows = TPR < 256 ? 256 / TPR : 1;
+    constexpr bool kLong = TPR == 1024;
+    constexpr bool kAgain = kLong && KV > 1;
+    constexpr int KS = kLong ? 1 : KV, KX = kAgain ? 1 : KV;
+    extern __shared__ float lds[];
+    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    const bool gated = (PARTS & kPost) && s.gate;
+    const float inv = 1.f / s.C;
+    float sw[KS][V], w1[KS][V], kp[KS][V], kx[KS][V];
+    float* sums = lds + 16;  // kLong: [2][KV * V][TPR]
+    auto weights = [&](int k, int c) {
+        if (PARTS & kPost) {
+            float w[V];
+            load_weights<V>(w, a.w_post, c, s.C);
+            load_weights<V>(sw[k], a.scale, c, s.C);
+#pragma unroll
+            for (int e = 0; e < V; e++) sw[k][e] *= w[e];
+        }
+        if (PARTS & kPre) load_weights<V>(w1[k], a.w_pre, c, s.C);
+    };
+#pragma unroll
+    for (int k = 0; k < KV; k++) {
+        if (!kLong) weights(k, (k * TPR + t) * V);
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            if (kLong)
+                sums[(k * V + e) * TPR + t] = sums[((KV + k) * V + e) * TPR + t] = 0.f;
+            else
+                kp[k % KS][e] = kx[k % KS][e] = 0.f;
+        }
+    }
+    for (int64_t n = (int64_t)blockIdx.x * kRows + sub; n < s.N; n += (int64_t)gridDim.x * kRows) {
+        const int64_t row = n * s.C;
+        Vec<T, V> x[KX], z[KX], g[KX], dy[KX], du[KX];
+        auto load = [&](int k, int c) {
+            if (PARTS & kPre) {
+                load_row<T, V>(x[k], a.x, row, c, s.C);
+                load_row<T, V>(du[k], a.du, row, c, s.C);
+            }
+            if (PARTS & kPost) load_row<T, V>(z[k], a.z, row, c, s.C);
+            if (gated) load_row<T, V>(g[k], a.g, row, c, s.C);
+            if (a.dx_out) load_row<T, V>(dy[k], a.dx_out, row, c, s.C);
+        };
+        if (!kAgain) {
+#pragma unroll
+            for (int k = 0; k < KV; k++) load(k % KX, (k * TPR + t) * V);
+        }
+        const float r2 = PARTS & kPost ? a.r2[n] : 0.f, r1 = PARTS & kPre ? a.r1[n] : 0.f;
+        float t1 = 0.f, t2 = 0.f;
+        auto element = [&](int k, int e) {
+            Element v;
+            v.set<PARTS>(s.gate, PARTS & kPre ? x[k % KX].at(e) : 0.f, PARTS & kPost ? z[k % KX].at(e) : 0.f, gated ? g[k % KX].at(e) : 0.f,
+                         PARTS & kPre ? du[k % KX].at(e) : 0.f, PARTS & kPost ? sw[k % KS][e] : 0.f, r2, r1);
+            return v;
+        };
+        auto renew = [&](int k) {
+            if (kAgain) load(0, (k * TPR + t) * V);
+            if (PARTS & kPre) {
+                x[k % KX].renew();
+                du[k % KX].renew();
+            }
+            if (PARTS & kPost) z[k % KX].renew();
+            if (gated) g[k % KX].renew();
+            if (kLong) weights(0, (k * TPR + t) * V);
+        };
+        auto whole = [&](int k, int e, const Element& v) { return v.whole<PARTS>(a.dx_out ? dy[k % KX].at(e) : 0.f, PARTS & kPre ? w1[k % KS][e] : 0.f, r1, t1); };
+        if (PARTS & kPre) {
+#pragma unroll(kAgain ? 1 : KV)
+            for (int k = 0; k < KV; k++) {
+                if (kLong) renew(k);
+#pragma unroll
+                for (int e = 0; e < V; e++) {
+                    const Element v = element(k, e);
+                    t1 += v.du * w1[k % KS][e] * v.xh;
+                }
+            }
+            t1 = over_row<TPR>(t1, lds) * inv;
+        }
+        float d[KX][V];
+#pragma unroll(kAgain ? 1 : KV)
+        for (int k = 0; k < KV; k++) {
+            renew(k);
+#pragma unroll
+            for (int e = 0; e < V; e++) {
+                const Element v = element(k, e);
+                d[k % KX][e] = whole(k, e, v);
+                if (PARTS & kPost) {
+                    const float p = d[k % KX][e] * v.act.a * v.zh;
+                    t2 += p * sw[k % KS][e];
+                    if (kLong)
+                        sums[(k * V + e) * TPR + t] += p;
+                    else
+                        kp[k % KS][e] += p;
+                }
+                if (PARTS & kPre) {
+                    if (kLong)
+                        sums[((KV + k) * V + e) * TPR + t] += v.du * v.xh;
+                    else
+                        kx[k % KS][e] += v.du * v.xh;
+                }
+            }
+            if (PARTS & kPre) store_row<T, V>(a.dx, row, (k * TPR + t) * V, s.C, d[k % KX]);
+        }
+        if (PARTS & kPost) {
+            t2 = over_row<TPR>(t2, lds) * inv;
+#pragma unroll(kAgain ? 1 : KV)
+            for (int k = 0; k < KV; k++) {
+                renew(k);
+                float dz[V], dg[V];
+#pragma unroll
+                for (int e = 0; e < V; e++) {
+                    const Element v = element(k, e);
+                    const float D = kAgain ? whole(k, e, v) : d[k % KX][e];
+                    dz[e] = r2 * (D * v.act.a * sw[k % KS][e] - v.zh * t2);
+                    dg[e] = D * v.act.da * sw[k % KS][e] * v.zh;
+                }
+                store_row<T, V>(a.dz, row, (k * TPR + t) * V, s.C, dz);
+                if (gated) store_row<T, V>(a.dg, row, (k * TPR + t) * V, s.C, dg);
+            }
+        }
+    }
+    // the rows of a workgroup in order, then its partial sums
+    float* out = a.partial + (int64_t)blockIdx.x * 2 * s.C;
+    if (kRows == 1) {
+#pragma unroll
+        for (int k = 0; k < KV; k++) {
+            const int c = (k * TPR + t) * V;
+            if (kLong) {
+#pragma unroll
+                for (int e = 0; e < V; e++) {
+                    kp[0][e] = sums[(k * V + e) * TPR + t];
+                    kx[0][e] = sums[((KV + k) * V + e) * TPR + t];
+                }
+            }
+            store_floats<V>(out, c, s.C, kp[k % KS]);
+            store_floats<V>(out + s.C, c, s.C, kx[k % KS]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int k = 0; k < KV; k++) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < V; e++) lds[threadIdx.x * V + e] = h ? kx[k % KS][e] : kp[k % KS][e];
+            __syncthreads();
+            for (int i = threadIdx.x; i < TPR * V; i += 256) {
+                float v = 0.f;
+#pragma unroll
+                for (int r = 0; r < kRows; r++) v += lds[r * TPR * V + i];
+                const int c = k * TPR * V + i;
+                if (c < s.C) out[h * s.C + c] = v;
+            }
+        }
+}
+
+// ---------------------------------------------------------------- sums of the weights' gradients
+
+constexpr int kSumSlices = 16;
+__global__ __launch_bounds__(64 * kSumSlices) void k_sums(Shape s, Bwd a, int partials) {
+    __shared__ float buf[kSumSlices][64];
+    const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6, i = blockIdx.x * 64 + lane, n = 2 * s.C;
+    float v = 0.f;
+    if (i < n)
+#pragma unroll 8
+        for (int p = slice; p < partials; p += kSumSlices) v += a.partial[(int64_t)p * n + i];
+    buf[slice][lane] = v;
+    __syncthreads();
+    if (slice || i >= n) return;
+    v = 0.f;
+#pragma unroll
+    for (int k = 0; k < kSumSlices; k++) v += buf[k][lane];
+    if (i >= s.C) {
+        if (s.pre) a.dw_pre[i - s.C] = v;
+    } else if (s.post) {
+        a.dw_post[i] = a.scale[i] * v;
+        a.dscale[i] = a.w_post[i] * v;
+    }
+}
+
+// ---------------------------------------------------------------- launches
+
+template <class T, int VEC, int KC, int PARTS>
+void maps(const Shape& s, const Plan& p, const Fwd* f, const Bwd* b, hipStream_t stream) {
+    const int64_t tiles = (p.total + (1 << p.log_gx) - 1) >> p.log_gx;
+    const int lds = p.threads / 64 * (1 << p.log_gx) * VEC * 4;
+    if (f) {
+        CANVAS_LAUNCH((k_maps_fwd<T, VEC, KC, PARTS>), dim3((unsigned)tiles), dim3(p.threads), lds, stream, s, *f, p.log_gx, p.pieces, p.total);
+    } else {
+        const int all = lds + (KC ? 0 : 8 * s.C);
+        if (all > 65536) {
+            static std::atomic<uint64_t> asked{0};
+            allow_lds(asked, reinterpret_cast<const void*>(&k_maps_bwd<T, VEC, KC, PARTS>), all);
+        }
+        CANVAS_LAUNCH((k_maps_bwd<T, VEC, KC, PARTS>), dim3(p.partials), dim3(p.threads), all, stream, s, *b, p.log_gx, p.pieces, p.total);
+    }
+}
+template <class T, int TPR, int KV, int PARTS>
+void rows(const Shape& s, const Plan& p, const Fwd* f, const Bwd* b, hipStream_t stream) {
+    constexpr int kBlock = TPR < 256 ? 256 : TPR, kRows = kBlock / TPR;
+    if (f)
+        CANVAS_LAUNCH((k_rows_fwd<T, TPR, KV, PARTS>), dim3((unsigned)((s.N + kRows - 1) / kRows)), dim3(kBlock), 0, stream, s, *f);
+    else {
+        const int lds = kRows > 1 ? 256 * 64 / (int)sizeof(T) : 64 + (TPR == 1024 ? TPR * KV * 128 / (int)sizeof(T) : 0);
+        if (lds > 65536) {
+            static std::atomic<uint64_t> asked{0};
+            allow_lds(asked, reinterpret_cast<const void*>(&k_rows_bwd<T, TPR, KV, PARTS>), lds);
+        }
+        CANVAS_LAUNCH((k_rows_bwd<T, TPR, KV, PARTS>), dim3(p.partials), dim3(kBlock), lds, stream, s, *b);
+    }
+}
+template <class T, int PARTS>
+void run(const Shape& s, const Plan& p, const Fwd* f, const Bwd* b, hipStream_t stream) {
+    constexpr int V = 16 / sizeof(T);
+    if (p.tpr) {
+        switch (p.tpr * 8 + p.kv) {
+        case 64 * 8 + 1: return rows<T, 64, 1, PARTS>(s, p, f, b, stream);
+        case 64 * 8 + 2: return rows<T, 64, 2, PARTS>(s, p, f, b, stream);
+        case 256 * 8 + 1: return rows<T, 256, 1, PARTS>(s, p, f, b, stream);
+        case 256 * 8 + 2: return rows<T, 256, 2, PARTS>(s, p, f, b, stream);
+        case 1024 * 8 + 1: return rows<T, 1024, 1, PARTS>(s, p, f, b, stream);
+        default: return rows<T, 1024, 16 / V, PARTS>(s, p, f, b, stream);
+        }
+    }
+    if (p.vec == 2) return maps<T, 2, 0, PARTS>(s, p, f, b, stream);
+    switch (p.kc) {
+    case 1: return maps<T, V, 1, PARTS>(s, p, f, b, stream);
+    case 2: return maps<T, V, 2, PARTS>(s, p, f, b, stream);
+    case 4: return maps<T, V, 4, PARTS>(s, p, f, b, stream);
+    default: return maps<T, V, 0, PARTS>(s, p, f, b, stream);
+    }
+}
 template <class T>
-__global__ __launch_bounds__(kPix* kSlots) void k_bwd(Shape s, Bwd a) {
-    __shared__ float buf[kSlots][kPix];
-    const int64_t total = s.N * s.P, q = (int64_t)blockIdx.x * kPix + threadIdx.x;
-    const bool in = q < total;
-    const int64_t n = in ? q / s.P : 0, base = n * s.C * s.P + (in ? q - n * s.P : 0);
-    const float r2 = in && s.post ? a.r2[q] : 0.f, r1 = in && s.pre ? a.r1[q] : 0.f;
-    auto unit = [&](int c) {  // xh
-        const int64_t i = base + c * s.P;
-        float y = ld<T>(a.x, i);
-        if (s.post) {
-            float g, dg;
-            gate_of(s.gate, s.gate ? ld<T>(a.g, i) : 0.f, g, dg);
-            y += a.scale[c] * g * (ld<T>(a.z, i) * r2 * a.w_post[c]);
-        }
-        return y * r1;
-    };
-    float t1 = 0.f;
-    if (s.pre) {
-        float t = 0.f;
-        if (in)
-            for (int c = threadIdx.y; c < s.C; c += kSlots) t += ld<T>(a.du, base + c * s.P) * a.w_pre[c] * unit(c);
-        t1 = over_slots(t, buf) / s.C;
-    }
-    auto whole = [&](int c, float& du_xh) {  // D
-        const int64_t i = base + c * s.P;
-        float d = a.dx_out ? ld<T>(a.dx_out, i) : 0.f;
-        du_xh = 0.f;
-        if (s.pre) {
-            const float du = ld<T>(a.du, i), xh = unit(c);
-            du_xh = du * xh;
-            d += r1 * (du * a.w_pre[c] - xh * t1);
-        }
-        return d;
-    };
-    float t2 = 0.f;
-    if (s.post) {
-        float t = 0.f;
-        if (in)
-            for (int c = threadIdx.y; c < s.C; c += kSlots) {
-                const int64_t i = base + c * s.P;
-                float g, dg, un;
-                gate_of(s.gate, s.gate ? ld<T>(a.g, i) : 0.f, g, dg);
-                t += whole(c, un) * g * (a.scale[c] * a.w_post[c]) * (ld<T>(a.z, i) * r2);
-            }
-        t2 = over_slots(t, buf) / s.C;
-    }
-    for (int c = threadIdx.y; c < s.C; c += kSlots) {
-        const int64_t i = base + c * s.P;
-        float kp = 0.f, kx = 0.f;
-        if (in) {
-            const float d = whole(c, kx);
-            if (s.pre) st((T*)a.dx, i, d);
-            if (s.post) {
-                float g, dg;
-                gate_of(s.gate, s.gate ? ld<T>(a.g, i) : 0.f, g, dg);
-                const float zh = ld<T>(a.z, i) * r2, sw = a.scale[c] * a.w_post[c];
-                kp = d * g * zh;
-                st((T*)a.dz, i, r2 * (d * g * sw - zh * t2));
-                if (s.gate) st((T*)a.dg, i, d * dg * sw * zh);
-            }
-        }
-        for (int o = 32; o; o >>= 1) {
-            kp += __shfl_xor(kp, o);
-            kx += __shfl_xor(kx, o);
-        }
-        if (threadIdx.x == 0) {
-            a.partial[((int64_t)blockIdx.x * 2) * s.C + c] = kp;
-            a.partial[((int64_t)blockIdx.x * 2 + 1) * s.C + c] = kx;
-        }
-    }
-}
-
-__global__ __launch_bounds__(256) void k_sums(Shape s, Bwd a, int partials) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= s.C) return;
-    float kp = 0.f, kx = 0.f;
-    for (int b = 0; b < partials; b++) {
-        kp += a.partial[((int64_t)b * 2) * s.C + c];
-        kx += a.partial[((int64_t)b * 2 + 1) * s.C + c];
-    }
-    if (s.post) {
-        a.dw_post[c] = a.scale[c] * kp;
-        a.dscale[c] = a.w_post[c] * kp;
-    }
-    if (s.pre) a.dw_pre[c] = kx;
+void run_parts(const Shape& s, const Plan& p, const Fwd* f, const Bwd* b, hipStream_t stream) {
+    if (s.post && s.pre)
+        run<T, kPost | kPre>(s, p, f, b, stream);
+    else if (s.post)
+        run<T, kPost>(s, p, f, b, stream);
+    else
+        run<T, kPre>(s, p, f, b, stream);
 }
 
 }  // namespace
 
 Plan plan_of(const Shape& s) {
     Plan p;
-    p.partials = (int)((s.N * s.P + kPix - 1) / kPix);
+    const int v = s.bf16 ? 8 : 4;
+    if (s.P == 1) {
+        const int sizes[][2] = {{64, 1}, {64, 2}, {256, 1}, {256, 2}, {1024, 1}, {1024, 16 / v}};
+        for (const auto& z : sizes) {
+            p.tpr = z[0];
+            p.kv = z[1];
+            if (z[0] * z[1] * v >= s.C) break;
+        }
+        const int64_t per = p.tpr < 256 ? 256 / p.tpr : 1;
+        p.partials = (int)std::min<int64_t>((s.N + per - 1) / per, 512);
+        return p;
+    }
+    p.vec = s.P >= v ? v : 2;
+    p.pieces = (int)((s.P + p.vec - 1) / p.vec);
+    p.total = s.N * p.pieces;
+    // Pieces side by side: as many as make a workgroup's share of a plane's row whole cache lines, fewer where that leaves
+    // compute units idle or a workgroup without room for all channels.
+    const bool held = p.vec == v && s.C <= 1024;
+    p.log_gx = held ? 4 : 3;
+    while (p.log_gx > 1 && ((p.total >> p.log_gx) < 256 || (held && s.C > 4 * (512 >> p.log_gx)))) p.log_gx--;
+    p.threads = held && s.C <= 4 * (256 >> p.log_gx) ? 256 : 512;
+    const int slots = p.threads >> p.log_gx, need = (s.C + slots - 1) / slots;
+    p.kc = !held ? 0 : need > 2 ? 4 : need;
+    const int64_t tiles = (p.total + (1 << p.log_gx) - 1) >> p.log_gx;
+    p.partials = (int)std::min<int64_t>(tiles, p.kc ? 512 : 256);
     return p;
 }
 
 void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
-    const dim3 block(kPix, kSlots);
     if (s.bf16)
-        CANVAS_LAUNCH(k_fwd<uint16_t>, dim3(p.partials), block, 0, stream, s, a);
+        run_parts<uint16_t>(s, p, &a, nullptr, stream);
     else
-        CANVAS_LAUNCH(k_fwd<float>, dim3(p.partials), block, 0, stream, s, a);
+        run_parts<float>(s, p, &a, nullptr, stream);
 }
 
 void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
-    const dim3 block(kPix, kSlots);
     if (s.bf16)
-        CANVAS_LAUNCH(k_bwd<uint16_t>, dim3(p.partials), block, 0, stream, s, a);
+        run_parts<uint16_t>(s, p, nullptr, &a, stream);
     else
-        CANVAS_LAUNCH(k_bwd<float>, dim3(p.partials), block, 0, stream, s, a);
-    CANVAS_LAUNCH(k_sums, dim3((s.C + 255) / 256), dim3(256), 0, stream, s, a, p.partials);
+        run_parts<float>(s, p, nullptr, &a, stream);
+    CANVAS_LAUNCH(k_sums, dim3((2 * s.C + 63) / 64), dim3(64 * kSumSlices), 0, stream, s, a, p.partials);
 }
 
 }  // namespace norm

@@ -15,9 +15,12 @@ struct Shape {
     float eps = 0.f;
 };
 
-// Plan of one shape: how many partial sums of the weights' gradients the backward kernel leaves.
+// Which kernels a shape takes.
 struct Plan {
-    int partials = 0;
+    int tpr = 0, kv = 0;                                   // rows: threads per row, 16-byte accesses of a thread (0: maps)
+    int vec = 0, log_gx = 0, threads = 0, kc = 0, pieces = 0;  // maps: pixels of a thread, pieces side by side, channels held
+    int64_t total = 0;                                     // pieces of all planes
+    int partials = 0;                                      // workgroups of the backward kernel
 };
 Plan plan_of(const Shape& s);
 
