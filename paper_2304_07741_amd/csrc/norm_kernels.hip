@@ -19,6 +19,7 @@
 #include "device_util.hpp"
 #include "launch.hpp"
 #include "tile_util.hpp"
+#include "wave_util.hpp"
 
 namespace canvas {
 namespace norm {
@@ -69,26 +70,6 @@ __device__ __forceinline__ Act act_of(int kind, float g) {
     return r;
 }
 
-// One element of backward from the values in memory and the sums over its pixel.
-struct Element {
-    Act act;
-    float zh = 0.f, xh, du;
-    template <int PARTS>
-    __device__ __forceinline__ void set(int gate, float x, float z, float g, float du_, float sw, float r2, float r1) {
-        if (PARTS & kPost) {
-            if (gate) act = act_of(gate, g);
-            zh = z * r2;
-            x += sw * act.a * zh;
-        }
-        xh = x * r1;
-        du = du_;
-    }
-    template <int PARTS>
-    __device__ __forceinline__ float whole(float dy, float w1, float r1, float t1) const {  // D
-        return PARTS & kPre ? dy + r1 * (du * w1 - xh * t1) : dy;
-    }
-};
-
 // ---------------------------------------------------------------- maps
 
 // Where a thread is: piece number `q` of all (n, first pixel), `skip` pixels in common with the piece before it.
@@ -118,9 +99,19 @@ __device__ __forceinline__ Where where_of(const Shape& s, int pieces, int64_t to
 // Sums of v over the channel slots of each pixel: lanes gx, gx + GX, ... of all waves.  buf: a row of GX * VEC floats per wave.
 template <int VEC>
 __device__ __forceinline__ void over_channels(float (&v)[VEC], int gx, int GX, float* buf) {
-    for (int o = 32; o >= GX; o >>= 1) {
 #pragma unroll
-        for (int e = 0; e < VEC; e++) v[e] += __shfl_xor(v[e], o);
+    for (int e = 0; e < VEC; e++) v[e] = wave::over<16, wave::Sum>(v[e]);
+    if (GX <= 8) {
+#pragma unroll
+        for (int e = 0; e < VEC; e++) v[e] = wave::step<8, wave::Sum>(v[e]);
+    }
+    if (GX <= 4) {
+#pragma unroll
+        for (int e = 0; e < VEC; e++) v[e] = wave::step<4, wave::Sum>(v[e]);
+    }
+    if (GX <= 2) {
+#pragma unroll
+        for (int e = 0; e < VEC; e++) v[e] = wave::step<2, wave::Sum>(v[e]);
     }
     const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, row = GX * VEC;
     __syncthreads();
@@ -141,7 +132,7 @@ template <class T, int VEC, int KC, int PARTS>
 __global__ __launch_bounds__(512) void k_maps_fwd(Shape s, Fwd a, int log_gx, int pieces, int64_t total) {
     extern __shared__ float lds[];
     const int GX = 1 << log_gx, gx = threadIdx.x & (GX - 1), cy = threadIdx.x >> log_gx, CY = blockDim.x >> log_gx;
-    const Where at = where_of<VEC>(s, pieces, total, (int64_t)blockIdx.x * GX + gx);
+    const Where at = where_of<VEC>(s, pieces, total, (int64_t)tile::xcd_sequence() * GX + gx);
     const float inv = 1.f / s.C;
     const bool gated = (PARTS & kPost) && s.gate;
     constexpr int K = KC ? KC : 1;
@@ -259,8 +250,9 @@ __global__ __launch_bounds__(512) void k_maps_bwd(Shape s, Bwd a, int log_gx, in
         __syncthreads();
     }
     const int64_t tiles = (total + GX - 1) >> log_gx;
-    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const Where at = where_of<VEC>(s, pieces, total, (tile << log_gx) + gx);
+    const bool overlap = (int64_t)pieces * VEC > s.P;
+    for (int64_t place = tile::xcd_sequence(); place < tiles; place += gridDim.x) {
+        const Where at = where_of<VEC>(s, pieces, total, (place << log_gx) + gx);
         Vec<T, VEC> x[K], z[K], g[K], dy[K], du[K];
         auto load = [&](int k, int c, bool arriving) {
             const int64_t i = at.base + c * s.P;
@@ -288,11 +280,18 @@ __global__ __launch_bounds__(512) void k_maps_bwd(Shape s, Bwd a, int log_gx, in
             r1[e] = PARTS & kPre ? a.r1[at.pixel + e] : 0.f;
             t1[e] = t2[e] = 0.f;
         }
-        auto element = [&](int k, int e) {
-            Element v;
-            v.set<PARTS>(s.gate, PARTS & kPre ? x[k].at(e) : 0.f, PARTS & kPost ? z[k].at(e) : 0.f, gated ? g[k].at(e) : 0.f,
-                         PARTS & kPre ? du[k].at(e) : 0.f, sw[k], r2[e], r1[e]);
-            return v;
+        // m = act zh, kept from the first pass for the second where there is room
+        constexpr bool kKeep = KC == 1 || KC == 2;
+        constexpr int KM = kKeep ? K : 1;
+        float m[KM][VEC], d[K][VEC];
+        auto branch = [&](int k) {
+#pragma unroll
+            for (int e = 0; e < VEC; e++) m[k % KM][e] = PARTS & kPost ? (gated ? act_of(s.gate, g[k].at(e)).a : 1.f) * (z[k].at(e) * r2[e]) : 0.f;
+        };
+        auto unit = [&](int k, int e) { return (PARTS & kPost ? x[k].at(e) + sw[k] * m[k % KM][e] : x[k].at(e)) * r1[e]; };  // xh
+        auto whole = [&](int k, int e, float xh) {                                                                       // D
+            const float dy_e = a.dx_out ? dy[k].at(e) : 0.f;
+            return PARTS & kPre ? dy_e + r1[e] * (du[k].at(e) * w1[k] - xh * t1[e]) : dy_e;
         };
         if (PARTS & kPre) {
             each([&](int k, int c) {
@@ -300,17 +299,14 @@ __global__ __launch_bounds__(512) void k_maps_bwd(Shape s, Bwd a, int log_gx, in
                     weights(k, c);
                     load(k, c, false);
                 }
+                branch(k);
 #pragma unroll
-                for (int e = 0; e < VEC; e++) {
-                    const Element v = element(k, e);
-                    t1[e] += v.du * w1[k] * v.xh;
-                }
+                for (int e = 0; e < VEC; e++) t1[e] += du[k].at(e) * w1[k] * unit(k, e);
             });
             over_channels<VEC>(t1, gx, GX, lds);
 #pragma unroll
             for (int e = 0; e < VEC; e++) t1[e] *= inv;
         }
-        float d[K][VEC];
         each([&](int k, int c) {
             if (!KC) {
                 weights(k, c);
@@ -318,17 +314,17 @@ __global__ __launch_bounds__(512) void k_maps_bwd(Shape s, Bwd a, int log_gx, in
             } else {
                 renew(k);
             }
+            if (!kKeep || !(PARTS & kPre)) branch(k);
             float sp = 0.f, sx = 0.f;
 #pragma unroll
             for (int e = 0; e < VEC; e++) {
-                const Element v = element(k, e);
-                d[k][e] = v.whole<PARTS>(a.dx_out ? dy[k].at(e) : 0.f, w1[k], r1[e], t1[e]);
-                const float p = d[k][e] * v.act.a * v.zh;
+                const float xh = PARTS & kPre ? unit(k, e) : 0.f;
+                d[k][e] = whole(k, e, xh);
+                float p = PARTS & kPost ? d[k][e] * m[k % KM][e] : 0.f, q = PARTS & kPre ? du[k].at(e) * xh : 0.f;
                 t2[e] += p * sw[k];
-                if (e >= at.skip) {
-                    sp += p;
-                    sx += v.du * v.xh;
-                }
+                if (overlap && e < at.skip) p = q = 0.f;
+                sp += p;
+                sx += q;
             }
             if (!at.in) sp = sx = 0.f;
             if (KC) {
@@ -354,16 +350,18 @@ __global__ __launch_bounds__(512) void k_maps_bwd(Shape s, Bwd a, int log_gx, in
                 if (!KC) {
                     weights(k, c);
                     load(k, c, true);
+                    branch(k);
                 } else {
                     renew(k);
                 }
                 float dz[VEC], dg[VEC];
 #pragma unroll
                 for (int e = 0; e < VEC; e++) {
-                    const Element v = element(k, e);
-                    const float D = KC ? d[k][e] : v.whole<PARTS>(a.dx_out ? dy[k].at(e) : 0.f, w1[k], r1[e], t1[e]);
-                    dz[e] = r2[e] * (D * v.act.a * sw[k] - v.zh * t2[e]);
-                    dg[e] = D * v.act.da * sw[k] * v.zh;
+                    Act act;
+                    if (gated) act = act_of(s.gate, g[k].at(e));
+                    const float D = (KC ? d[k][e] : whole(k, e, PARTS & kPre ? unit(k, e) : 0.f)) * sw[k], zh = z[k].at(e) * r2[e];
+                    dz[e] = r2[e] * (D * act.a - zh * t2[e]);
+                    dg[e] = D * act.da * zh;
                 }
                 if (at.in) {
                     store<T, VEC>(a.dz, at.base + c * s.P, dz);
@@ -395,8 +393,13 @@ __global__ __launch_bounds__(512) void k_maps_bwd(Shape s, Bwd a, int log_gx, in
 // Over the TPR threads of a row; buf: a float per wave of the workgroup.
 template <int TPR>
 __device__ __forceinline__ float over_row(float v, float* buf) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    if (TPR == 16) {  // (rotations of a row of 16 lanes)
+        v = wave::step<8, wave::Sum>(v);
+        v = wave::step<4, wave::Sum>(v);
+        v = wave::step<2, wave::Sum>(v);
+        return wave::step<1, wave::Sum>(v);
+    }
+    v = wave::over<1, wave::Sum>(v);
     if (TPR == 64) return v;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
@@ -463,7 +466,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_fwd(Shape s, Fwd
     __shared__ float buf[16];
     const int t = threadIdx.x % TPR;
     const int64_t n = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
-    if (n >= s.N) return;  // (with several rows per workgroup a row is a wave: no barriers)
+    if (n >= s.N) return;  // (with several rows per workgroup a row is within a wave: no barriers)
     const int64_t row = n * s.C;
     const bool gated = (PARTS & kPost) && s.gate;
     const float inv = 1.f / s.C;
@@ -577,12 +580,6 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_bwd(Shape s, Bwd
         }
         const float r2 = PARTS & kPost ? a.r2[n] : 0.f, r1 = PARTS & kPre ? a.r1[n] : 0.f;
         float t1 = 0.f, t2 = 0.f;
-        auto element = [&](int k, int e) {
-            Element v;
-            v.set<PARTS>(s.gate, PARTS & kPre ? x[k % KX].at(e) : 0.f, PARTS & kPost ? z[k % KX].at(e) : 0.f, gated ? g[k % KX].at(e) : 0.f,
-                         PARTS & kPre ? du[k % KX].at(e) : 0.f, PARTS & kPost ? sw[k % KS][e] : 0.f, r2, r1);
-            return v;
-        };
         auto renew = [&](int k) {
             if (kAgain) load(0, (k * TPR + t) * V);
             if (PARTS & kPre) {
@@ -593,29 +590,38 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_bwd(Shape s, Bwd
             if (gated) g[k % KX].renew();
             if (kLong) weights(0, (k * TPR + t) * V);
         };
-        auto whole = [&](int k, int e, const Element& v) { return v.whole<PARTS>(a.dx_out ? dy[k % KX].at(e) : 0.f, PARTS & kPre ? w1[k % KS][e] : 0.f, r1, t1); };
+        // m = act zh, kept from the first pass for the second
+        float m[KX][V], d[KX][V];
+        auto branch = [&](int k) {
+#pragma unroll
+            for (int e = 0; e < V; e++)
+                m[k % KX][e] = PARTS & kPost ? (gated ? act_of(s.gate, g[k % KX].at(e)).a : 1.f) * (z[k % KX].at(e) * r2) : 0.f;
+        };
+        auto unit = [&](int k, int e) { return (PARTS & kPost ? x[k % KX].at(e) + sw[k % KS][e] * m[k % KX][e] : x[k % KX].at(e)) * r1; };  // xh
+        auto whole = [&](int k, int e, float xh) {                                                                                     // D
+            const float dy_e = a.dx_out ? dy[k % KX].at(e) : 0.f;
+            return PARTS & kPre ? dy_e + r1 * (du[k % KX].at(e) * w1[k % KS][e] - xh * t1) : dy_e;
+        };
         if (PARTS & kPre) {
 #pragma unroll(kAgain ? 1 : KV)
             for (int k = 0; k < KV; k++) {
                 if (kLong) renew(k);
+                branch(k);
 #pragma unroll
-                for (int e = 0; e < V; e++) {
-                    const Element v = element(k, e);
-                    t1 += v.du * w1[k % KS][e] * v.xh;
-                }
+                for (int e = 0; e < V; e++) t1 += du[k % KX].at(e) * w1[k % KS][e] * unit(k, e);
             }
             t1 = over_row<TPR>(t1, lds) * inv;
         }
-        float d[KX][V];
 #pragma unroll(kAgain ? 1 : KV)
         for (int k = 0; k < KV; k++) {
             renew(k);
+            if (kAgain || !(PARTS & kPre)) branch(k);
 #pragma unroll
             for (int e = 0; e < V; e++) {
-                const Element v = element(k, e);
-                d[k % KX][e] = whole(k, e, v);
+                const float xh = PARTS & kPre ? unit(k, e) : 0.f;
+                d[k % KX][e] = whole(k, e, xh);
                 if (PARTS & kPost) {
-                    const float p = d[k % KX][e] * v.act.a * v.zh;
+                    const float p = d[k % KX][e] * m[k % KX][e];
                     t2 += p * sw[k % KS][e];
                     if (kLong)
                         sums[(k * V + e) * TPR + t] += p;
@@ -623,10 +629,11 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_bwd(Shape s, Bwd
                         kp[k % KS][e] += p;
                 }
                 if (PARTS & kPre) {
+                    const float q = du[k % KX].at(e) * xh;
                     if (kLong)
-                        sums[((KV + k) * V + e) * TPR + t] += v.du * v.xh;
+                        sums[((KV + k) * V + e) * TPR + t] += q;
                     else
-                        kx[k % KS][e] += v.du * v.xh;
+                        kx[k % KS][e] += q;
                 }
             }
             if (PARTS & kPre) store_row<T, V>(a.dx, row, (k * TPR + t) * V, s.C, d[k % KX]);
@@ -636,13 +643,15 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_bwd(Shape s, Bwd
 #pragma unroll(kAgain ? 1 : KV)
             for (int k = 0; k < KV; k++) {
                 renew(k);
+                if (kAgain) branch(k);
                 float dz[V], dg[V];
 #pragma unroll
                 for (int e = 0; e < V; e++) {
-                    const Element v = element(k, e);
-                    const float D = kAgain ? whole(k, e, v) : d[k % KX][e];
-                    dz[e] = r2 * (D * v.act.a * sw[k % KS][e] - v.zh * t2);
-                    dg[e] = D * v.act.da * sw[k % KS][e] * v.zh;
+                    Act act;
+                    if (gated) act = act_of(s.gate, g[k % KX].at(e));
+                    const float D = (kAgain ? whole(k, e, PARTS & kPre ? unit(k, e) : 0.f) : d[k % KX][e]) * sw[k % KS][e], zh = z[k % KX].at(e) * r2;
+                    dz[e] = r2 * (D * act.a - zh * t2);
+                    dg[e] = D * act.da * zh;
                 }
                 store_row<T, V>(a.dz, row, (k * TPR + t) * V, s.C, dz);
                 if (gated) store_row<T, V>(a.dg, row, (k * TPR + t) * V, s.C, dg);
@@ -745,6 +754,7 @@ void run(const Shape& s, const Plan& p, const Fwd* f, const Bwd* b, hipStream_t 
     constexpr int V = 16 / sizeof(T);
     if (p.tpr) {
         switch (p.tpr * 8 + p.kv) {
+        case 16 * 8 + 1: return rows<T, 16, 1, PARTS>(s, p, f, b, stream);
         case 64 * 8 + 1: return rows<T, 64, 1, PARTS>(s, p, f, b, stream);
         case 64 * 8 + 2: return rows<T, 64, 2, PARTS>(s, p, f, b, stream);
         case 256 * 8 + 1: return rows<T, 256, 1, PARTS>(s, p, f, b, stream);
@@ -777,14 +787,14 @@ Plan plan_of(const Shape& s) {
     Plan p;
     const int v = s.bf16 ? 8 : 4;
     if (s.P == 1) {
-        const int sizes[][2] = {{64, 1}, {64, 2}, {256, 1}, {256, 2}, {1024, 1}, {1024, 16 / v}};
+        const int sizes[][2] = {{16, 1}, {64, 1}, {64, 2}, {256, 1}, {256, 2}, {1024, 1}, {1024, 16 / v}};
         for (const auto& z : sizes) {
             p.tpr = z[0];
             p.kv = z[1];
             if (z[0] * z[1] * v >= s.C) break;
         }
         const int64_t per = p.tpr < 256 ? 256 / p.tpr : 1;
-        p.partials = (int)std::min<int64_t>((s.N + per - 1) / per, 512);
+        p.partials = (int)std::min<int64_t>((s.N + per - 1) / per, p.tpr == 1024 ? 256 : 512);
         return p;
     }
     p.vec = s.P >= v ? v : 2;
