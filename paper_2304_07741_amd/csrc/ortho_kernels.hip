@@ -11,6 +11,8 @@
 //   X = B X     (from the rows of B and of X^T; both X and X^T are written, or, in the last step, the outputs)
 #include "ortho_kernels.hpp"
 
+#include <algorithm>
+
 #include "device_util.hpp"
 #include "launch.hpp"
 #include "tile_util.hpp"
@@ -54,12 +56,13 @@ __device__ __forceinline__ void load_to_lds(tile::rsrc_t from, unsigned char* to
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, voff, soff, 0, 0);
 }
 
+// Momentum and the sum of squares of the direction, one part of a matrix per workgroup.
 __global__ __launch_bounds__(kThreads) void k_mix(Shape s, Args a, double* sums) {
     __shared__ double buf[kThreads];
-    const int64_t len = s.R * s.K, base = blockIdx.y * len;
+    const int64_t len = s.R * s.K, base = blockIdx.y * len, stride = (int64_t)gridDim.x * kThreads;
+    const int64_t first = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     double t = 0;
-    for (int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x; k < len; k += (int64_t)gridDim.x * kThreads) {
-        const int64_t i = base + k;
+    auto one = [&](int64_t i) {
         float m = 0.f;
         if (a.momentum) {
             m = (float)(a.mu * a.momentum[i] + a.grad[i]);
@@ -67,6 +70,27 @@ __global__ __launch_bounds__(kThreads) void k_mix(Shape s, Args a, double* sums)
         }
         const double v = direction(s, a, i, m);
         t += v * v;
+    };
+    if ((len & 3) == 0) {  // every matrix begins at 16 bytes
+        for (int64_t k = first; k < len / 4; k += stride) {
+            const int64_t i = base + 4 * k;
+            const f32x4 g = *reinterpret_cast<const f32x4*>(a.grad + i);
+            f32x4 v = g;
+            if (a.momentum) {
+                const f32x4 old = *reinterpret_cast<const f32x4*>(a.momentum + i);
+                f32x4 m;
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    m[e] = (float)(a.mu * old[e] + g[e]);
+                    v[e] = s.nesterov ? (float)(g[e] + a.mu * m[e]) : m[e];
+                }
+                *reinterpret_cast<f32x4*>(a.momentum_out + i) = m;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; e++) t += (double)v[e] * v[e];
+        }
+    } else {
+        for (int64_t k = first; k < len; k += stride) one(base + k);
     }
     buf[threadIdx.x] = t;
     __syncthreads();
@@ -164,24 +188,22 @@ struct Product {
     Pair out;   // kGram, kSquare: C, both sides; kUpdate: X
     Pair turn;  // kUpdate: X^T
     int tiles_i, tiles_j, tiles;
+    // The sum over k cut into `splits` parts, a workgroup each, where there are few tiles.  Parts are left in memory for a launch
+    // that adds them in their order.  (One launch in which the last workgroup at a tile adds them needs a fence over all XCDs
+    // per workgroup, which writes back its L2: 89 us against 10 for the Gram matrix of 512 x 2048.)
+    int splits;
+    f32x4* parts;
 };
 
-// BM x BN results per workgroup of 2 x 2 waves.  Both planes of both operands are loaded straight into LDS, 32 summands at a time, into
-// the buffer that the previous step has left, while the products of the present one run.  Rows of 64 bytes lie four to a line
-// of all banks; a 16-byte piece c of row r lies at place c ^ (r / 4) % 4, so that the pieces that eight rows read together
-// fall on different banks.
+struct Tile {
+    int grp, i0, j0;
+    bool diagonal;
+};
 template <int BM, int BN, Kind KIND>
-__global__ __launch_bounds__(kThreads) void k_product(Shape s, Args args, Product g) {
-    constexpr int TM = BM / 64, TN = BN / 64;
-    constexpr int kOpA = BM * 64, kOpB = BN * 64;            // bytes of one plane of a step
-    constexpr int kStage = 2 * (kOpA + kOpB);
-    constexpr int kLds = 2 * kStage > BM * BN * 4 ? 2 * kStage : BM * BN * 4;
-    __shared__ __align__(16) unsigned char lds[kLds];
-
-    const unsigned seq = tile::xcd_sequence();
-    const int grp = seq / g.tiles, t = seq - grp * g.tiles;
+__device__ __forceinline__ Tile tile_of(const Product& g, int task) {
+    const int grp = task / g.tiles, t = task - grp * g.tiles;
     int bi, bj;
-    if (KIND == kGram || KIND == kSquare) {
+    if (KIND == kGram || KIND == kSquare) {  // row by row of the triangle
         bi = (int)((__fsqrt_rn(8.f * t + 1.f) - 1.f) * 0.5f);
         while (bi * (bi + 1) / 2 > t) bi--;
         while ((bi + 1) * (bi + 2) / 2 <= t) bi++;
@@ -190,76 +212,15 @@ __global__ __launch_bounds__(kThreads) void k_product(Shape s, Args args, Produc
         bj = t / g.tiles_i;
         bi = t - bj * g.tiles_i;
     }
-    const int i0 = bi * BM, j0 = bj * BN;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wi = (wave >> 1) * (BM / 2), wj = (wave & 1) * (BN / 2);
+    return Tile{grp, bi * BM, bj * BN, bi == bj};
+}
 
-    // 16-byte pieces of this thread in a plane of a step; rows past the end are the last one again
-    auto piece = [&](int q, int first, int rows, int ld) {
-        const int at = tid + q * kThreads, r = at >> 2, c = (at & 3) ^ ((r >> 2) & 3);
-        const int row = first + r < rows ? r : rows - 1 - first;
-        return (uint32_t)row * (uint32_t)ld * 2u + (uint32_t)c * 16u;
-    };
-    uint32_t va[BM / 64], vb[BN / 64];
-#pragma unroll
-    for (int q = 0; q < BM / 64; q++) va[q] = piece(q, i0, g.rows, g.p.ld);
-#pragma unroll
-    for (int q = 0; q < BN / 64; q++) vb[q] = piece(q, j0, g.cols, g.q.ld);
-    const _Float16* pa = g.p.hi + grp * g.p.step + (int64_t)i0 * g.p.ld;
-    const _Float16* pb = g.q.hi + grp * g.q.step + (int64_t)j0 * g.q.ld;
-    const tile::rsrc_t ra[2] = {whole_memory(pa), whole_memory(pa + g.p.plane)};
-    const tile::rsrc_t rb[2] = {whole_memory(pb), whole_memory(pb + g.q.plane)};
-    auto load = [&](int step) {
-        unsigned char* to = lds + (step & 1) * kStage + wave * 1024;
-        const int k = step * (kDepth * 2);
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-#pragma unroll
-            for (int q = 0; q < BM / 64; q++)
-                load_to_lds(ra[h], to + h * kOpA + q * 4096, va[q], k);
-#pragma unroll
-            for (int q = 0; q < BN / 64; q++)
-                load_to_lds(rb[h], to + 2 * kOpA + h * kOpB + q * 4096, vb[q], k);
-        }
-    };
-
-    f32x16 acc[TM][TN] = {};
-    const int steps = g.depth / kDepth;
-    load(0);
-    for (int step = 0; step < steps; step++) {
-        __syncthreads();  // this step's operands are there, and everybody has read the last one's
-        const unsigned char* at = lds + (step & 1) * kStage;
-        half8 a[2][TM][2], b[2][TN][2];
-#pragma unroll
-        for (int k = 0; k < 2; k++) {
-            const int c = k * 2 + (lane >> 5);
-#pragma unroll
-            for (int x = 0; x < TM; x++) {
-                const int r = wi + x * 32 + (lane & 31);
-#pragma unroll
-                for (int h = 0; h < 2; h++) a[k][x][h] = *reinterpret_cast<const half8*>(at + h * kOpA + r * 64 + ((c ^ ((r >> 2) & 3)) << 4));
-            }
-#pragma unroll
-            for (int y = 0; y < TN; y++) {
-                const int r = wj + y * 32 + (lane & 31);
-#pragma unroll
-                for (int h = 0; h < 2; h++) b[k][y][h] = *reinterpret_cast<const half8*>(at + 2 * kOpA + h * kOpB + r * 64 + ((c ^ ((r >> 2) & 3)) << 4));
-            }
-        }
-        if (step + 1 < steps) load(step + 1);
-#pragma unroll
-        for (int k = 0; k < 2; k++)
-#pragma unroll
-            for (int x = 0; x < TM; x++)
-#pragma unroll
-                for (int y = 0; y < TN; y++) {
-                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[k][x][1], b[k][y][0], acc[x][y], 0, 0, 0);
-                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[k][x][0], b[k][y][1], acc[x][y], 0, 0, 0);
-                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[k][x][0], b[k][y][0], acc[x][y], 0, 0, 0);
-                }
-    }
-    __syncthreads();
-
+// The results of a tile, as the matrix units leave them in the registers of its workgroup, to where they belong.
+template <int BM, int BN, Kind KIND>
+__device__ __forceinline__ void finish(const Shape& s, const Args& args, const Product& g, const Tile& at, const f32x16 (&acc)[BM / 64][BN / 64], unsigned char* lds) {
+    constexpr int TM = BM / 64, TN = BN / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wi = (wave >> 1) * (BM / 2), wj = (wave & 1) * (BN / 2);
+    const int grp = at.grp, i0 = at.i0, j0 = at.j0;
     // The results as an image in LDS, first as fp32, then, read row by row, as pairs in the same places, which the transpose is
     // written from.  Columns are exchanged in pieces of 16 by bits of the row, so that eight rows of a column and both halves of
     // a wave fall on different banks.
@@ -284,10 +245,10 @@ __global__ __launch_bounds__(kThreads) void k_product(Shape s, Args args, Produc
         for (int k = 0; k < 8; k++) v[k] = __uint_as_float(from[k]);
         if (KIND == kLast) {
             if (i >= g.rows) continue;
-            const int64_t at = (int64_t)grp * s.R * s.K + (int64_t)i * s.K + j;
+            const int64_t first = (int64_t)grp * s.R * s.K + (int64_t)i * s.K + j;
 #pragma unroll
             for (int k = 0; k < 8; k++)
-                if (j + k < g.cols) finish_one(s, args, at + k, v[k] * (1.f / (kScale * kScale)));
+                if (j + k < g.cols) finish_one(s, args, first + k, v[k] * (1.f / (kScale * kScale)));
             continue;
         }
         const bool in = i < g.rows && j < g.out.ld;
@@ -320,7 +281,7 @@ __global__ __launch_bounds__(kThreads) void k_product(Shape s, Args args, Produc
             *reinterpret_cast<u32x4*>(to + g.out.plane) = lo;
         }
     }
-    if (KIND == kLast || (KIND != kUpdate && bi == bj)) return;
+    if (KIND == kLast || (KIND != kUpdate && at.diagonal)) return;
     __syncthreads();
     const Pair turn = KIND == kUpdate ? g.turn : g.out;
     for (int e = tid; e < BN * (BM / 8); e += kThreads) {
@@ -342,25 +303,175 @@ __global__ __launch_bounds__(kThreads) void k_product(Shape s, Args args, Produc
     }
 }
 
+
+// BM x BN results per workgroup of 2 x 2 waves.  Both planes of both operands are loaded straight into LDS, SUB times 32 summands
+// at a time, into the buffer that the previous step has left, while the products of the present one run.  Rows of 64 bytes
+// lie four to a line of all banks; a 16-byte piece c of row r lies at place c ^ (r / 4) % 4, so that the pieces that eight rows
+// read together fall on different banks.
+template <int BM, int BN, int SUB, Kind KIND>
+__global__ __launch_bounds__(kThreads) void k_product(Shape s, Args args, Product g) {
+    constexpr int TM = BM / 64, TN = BN / 64;
+    constexpr int kOpA = BM * 64, kOpB = BN * 64;            // bytes of one plane of 32 summands
+    constexpr int kPart = 2 * (kOpA + kOpB), kStage = SUB * kPart;
+    constexpr int kLds = 2 * kStage > BM * BN * 4 ? 2 * kStage : BM * BN * 4;
+    __shared__ __align__(16) unsigned char lds[kLds];
+
+    const unsigned seq = tile::xcd_sequence();
+    const int task = seq / g.splits, split = seq - task * g.splits;
+    const Tile at_tile = tile_of<BM, BN, KIND>(g, task);
+    const int grp = at_tile.grp, i0 = at_tile.i0, j0 = at_tile.j0;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wi = (wave >> 1) * (BM / 2), wj = (wave & 1) * (BN / 2);
+
+    // 16-byte pieces of this thread in a plane of a step; rows past the end are the last one again
+    auto piece = [&](int q, int first, int rows, int ld) {
+        const int at = tid + q * kThreads, r = at >> 2, c = (at & 3) ^ ((r >> 2) & 3);
+        const int row = first + r < rows ? r : rows - 1 - first;
+        return (uint32_t)row * (uint32_t)ld * 2u + (uint32_t)c * 16u;
+    };
+    uint32_t va[BM / 64], vb[BN / 64];
+#pragma unroll
+    for (int q = 0; q < BM / 64; q++) va[q] = piece(q, i0, g.rows, g.p.ld);
+#pragma unroll
+    for (int q = 0; q < BN / 64; q++) vb[q] = piece(q, j0, g.cols, g.q.ld);
+    const _Float16* pa = g.p.hi + grp * g.p.step + (int64_t)i0 * g.p.ld;
+    const _Float16* pb = g.q.hi + grp * g.q.step + (int64_t)j0 * g.q.ld;
+    const tile::rsrc_t ra[2] = {whole_memory(pa), whole_memory(pa + g.p.plane)};
+    const tile::rsrc_t rb[2] = {whole_memory(pb), whole_memory(pb + g.q.plane)};
+    const int all = g.depth / kDepth, begin = (int)((int64_t)all * split / g.splits), end = (int)((int64_t)all * (split + 1) / g.splits);
+    auto load = [&](int first, int buffer) {
+#pragma unroll
+        for (int u = 0; u < SUB; u++) {
+            if (u && first + u >= end) break;
+            unsigned char* to = lds + buffer * kStage + u * kPart + wave * 1024;
+            const int k = (first + u) * (kDepth * 2);
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+#pragma unroll
+                for (int q = 0; q < BM / 64; q++) load_to_lds(ra[h], to + h * kOpA + q * 4096, va[q], k);
+#pragma unroll
+                for (int q = 0; q < BN / 64; q++) load_to_lds(rb[h], to + 2 * kOpA + h * kOpB + q * 4096, vb[q], k);
+            }
+        }
+    };
+
+    f32x16 acc[TM][TN] = {};
+    load(begin, 0);
+    for (int step = begin, buffer = 0; step < end; step += SUB, buffer ^= 1) {
+        __syncthreads();  // this step's operands are there, and everybody has read the last one's
+        half8 a[SUB][2][TM][2], b[SUB][2][TN][2];
+#pragma unroll
+        for (int u = 0; u < SUB; u++) {
+            const unsigned char* at = lds + buffer * kStage + u * kPart;
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                const int c = k * 2 + (lane >> 5);
+#pragma unroll
+                for (int x = 0; x < TM; x++) {
+                    const int r = wi + x * 32 + (lane & 31);
+#pragma unroll
+                    for (int h = 0; h < 2; h++) a[u][k][x][h] = *reinterpret_cast<const half8*>(at + h * kOpA + r * 64 + ((c ^ ((r >> 2) & 3)) << 4));
+                }
+#pragma unroll
+                for (int y = 0; y < TN; y++) {
+                    const int r = wj + y * 32 + (lane & 31);
+#pragma unroll
+                    for (int h = 0; h < 2; h++) b[u][k][y][h] = *reinterpret_cast<const half8*>(at + 2 * kOpA + h * kOpB + r * 64 + ((c ^ ((r >> 2) & 3)) << 4));
+                }
+            }
+        }
+        if (step + SUB < end) load(step + SUB, buffer ^ 1);
+#pragma unroll
+        for (int u = 0; u < SUB; u++) {
+            if (u && step + u >= end) break;
+#pragma unroll
+            for (int k = 0; k < 2; k++)
+#pragma unroll
+                for (int x = 0; x < TM; x++)
+#pragma unroll
+                    for (int y = 0; y < TN; y++) {
+                        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[u][k][x][1], b[u][k][y][0], acc[x][y], 0, 0, 0);
+                        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[u][k][x][0], b[u][k][y][1], acc[x][y], 0, 0, 0);
+                        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[u][k][x][0], b[u][k][y][0], acc[x][y], 0, 0, 0);
+                    }
+        }
+    }
+    __syncthreads();
+
+    if (g.splits == 1) {
+        finish<BM, BN, KIND>(s, args, g, at_tile, acc, lds);
+        return;
+    }
+    f32x4* mine = g.parts + ((int64_t)task * g.splits + split) * (BM * BN / 4) + tid;
+#pragma unroll
+    for (int x = 0; x < TM; x++)
+#pragma unroll
+        for (int y = 0; y < TN; y++)
+#pragma unroll
+            for (int q = 0; q < 4; q++)
+                mine[((x * TN + y) * 4 + q) * kThreads] = f32x4{acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
+}
+
+// Adds the parts of a tile and finishes it.
+template <int BM, int BN, Kind KIND>
+__global__ __launch_bounds__(kThreads) void k_add(Shape s, Args args, Product g) {
+    constexpr int TM = BM / 64, TN = BN / 64, kEach = BM * BN / 4;
+    __shared__ __align__(16) unsigned char lds[BM * BN * 4];
+    const f32x4* from = g.parts + (int64_t)blockIdx.x * g.splits * kEach + threadIdx.x;
+    f32x16 acc[TM][TN] = {};
+    for (int part = 0; part < g.splits; part++, from += kEach)
+#pragma unroll
+        for (int x = 0; x < TM; x++)
+#pragma unroll
+            for (int y = 0; y < TN; y++)
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    const f32x4 v = from[((x * TN + y) * 4 + q) * kThreads];
+#pragma unroll
+                    for (int e = 0; e < 4; e++) acc[x][y][4 * q + e] += v[e];
+                }
+    finish<BM, BN, KIND>(s, args, g, tile_of<BM, BN, KIND>(g, blockIdx.x), acc, lds);
+}
+
 uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
 unsigned blocks(int64_t n, int64_t per) { return (unsigned)((n + per - 1) / per); }
 int padded(int64_t n) { return (int)((n + kDepth - 1) / kDepth * kDepth); }
 
-template <int B, Kind KIND>
-void launch(const Shape& s, const Args& a, Product g, hipStream_t stream) {
-    g.tiles_i = (g.rows + B - 1) / B;
-    g.tiles_j = (g.cols + B - 1) / B;
-    g.tiles = KIND == kGram || KIND == kSquare ? g.tiles_i * (g.tiles_i + 1) / 2 : g.tiles_i * g.tiles_j;
-    CANVAS_LAUNCH((k_product<B, B, KIND>), dim3((unsigned)(g.tiles * s.G)), dim3(kThreads), 0, stream, s, a, g);
+// How a product is cut: sides of the tiles, parts of the sum.
+struct Cut {
+    int side, tiles_i, tiles_j, tiles, splits;
+};
+Cut cut_of(bool symmetric, int64_t rows, int64_t cols, int64_t depth, int64_t G) {
+    Cut c;
+    auto tiles = [&](int side) {
+        c.side = side;
+        c.tiles_i = (int)((rows + side - 1) / side);
+        c.tiles_j = (int)((cols + side - 1) / side);
+        c.tiles = symmetric ? c.tiles_i * (c.tiles_i + 1) / 2 : c.tiles_i * c.tiles_j;
+        return c.tiles * G;
+    };
+    if (tiles(128) < 128) tiles(64);
+    const int64_t steps = depth / kDepth, slots = 512 / (c.tiles * G), room = steps / 8;
+    c.splits = (int)std::max<int64_t>(1, std::min(slots, room));
+    return c;
+}
+
+template <int B, int SUB, Kind KIND>
+void launch(const Shape& s, const Args& a, const Product& g, hipStream_t stream) {
+    CANVAS_LAUNCH((k_product<B, B, SUB, KIND>), dim3((unsigned)(g.tiles * g.splits * s.G)), dim3(kThreads), 0, stream, s, a, g);
+    if (g.splits > 1) CANVAS_LAUNCH((k_add<B, B, KIND>), dim3((unsigned)(g.tiles * s.G)), dim3(kThreads), 0, stream, s, a, g);
 }
 template <Kind KIND>
-void product(const Shape& s, const Args& a, const Product& g, hipStream_t stream) {
-    const int64_t ti = (g.rows + 127) / 128, tj = (g.cols + 127) / 128;
-    const int64_t tiles = s.G * (KIND == kGram || KIND == kSquare ? ti * (ti + 1) / 2 : ti * tj);
-    if (tiles >= 128)
-        launch<128, KIND>(s, a, g, stream);
+void product(const Shape& s, const Args& a, Product g, hipStream_t stream) {
+    const Cut c = cut_of(KIND == kGram || KIND == kSquare, g.rows, g.cols, g.depth, s.G);
+    g.tiles_i = c.tiles_i;
+    g.tiles_j = c.tiles_j;
+    g.tiles = c.tiles;
+    g.splits = c.splits;
+    if (c.side == 128)
+        launch<128, 1, KIND>(s, a, g, stream);
     else
-        launch<64, KIND>(s, a, g, stream);
+        launch<64, 2, KIND>(s, a, g, stream);
 }
 
 }  // namespace
@@ -368,11 +479,16 @@ void product(const Shape& s, const Args& a, const Product& g, hipStream_t stream
 Plan plan_of(const Shape& s) {
     Plan p;
     p.parts = (int)((s.R * s.K + 16 * kThreads - 1) / (16 * kThreads));
-    if (p.parts > 256) p.parts = 256;
-    p.launches = s.steps ? 2 + 3 * s.steps : 2;
+    if (p.parts > 1024) p.parts = 1024;
+    p.launches = 2;
     p.workspace_bytes = up256(8ull * s.G * p.parts);
-    if (s.steps)
-        p.workspace_bytes += 2 * up256(4ull * s.G * s.m * padded(s.n)) + 2 * up256(4ull * s.G * s.n * padded(s.m)) + 2 * up256(4ull * s.G * s.m * padded(s.m));
+    if (!s.steps) return p;
+    const Cut gram = cut_of(true, s.m, s.m, padded(s.n), s.G), square = cut_of(true, s.m, s.m, padded(s.m), s.G);
+    const Cut update = cut_of(false, s.m, s.n, padded(s.m), s.G), last = s.tall ? cut_of(false, s.n, s.m, padded(s.m), s.G) : update;
+    for (const Cut& c : {gram, square, update, last})
+        if (c.splits > 1) p.part_bytes = std::max<uint64_t>(p.part_bytes, 4ull * c.side * c.side * c.tiles * c.splits * s.G);
+    p.launches += s.steps * (1 + (gram.splits > 1) + 1 + (square.splits > 1)) + (s.steps - 1) * (1 + (update.splits > 1)) + 1 + (last.splits > 1);
+    p.workspace_bytes += 2 * up256(4ull * s.G * s.m * padded(s.n)) + 2 * up256(4ull * s.G * s.n * padded(s.m)) + 2 * up256(4ull * s.G * s.m * padded(s.m)) + up256(p.part_bytes);
     return p;
 }
 
@@ -392,6 +508,7 @@ void step(const Shape& s, const Plan& p, const Args& a, hipStream_t stream) {
         return q;
     };
     double* sums = (double*)take(8ull * s.G * p.parts);
+    f32x4* parts = (f32x4*)take(p.part_bytes);
     const unsigned G = (unsigned)s.G;
     CANVAS_LAUNCH(k_mix, dim3(p.parts, G), dim3(kThreads), 0, stream, s, a, sums);
     if (!s.steps) {
@@ -403,14 +520,14 @@ void step(const Shape& s, const Plan& p, const Args& a, hipStream_t stream) {
     const int m = (int)s.m, n = (int)s.n;
     for (int k = 0; k < s.steps; k++) {
         const Pair &from = x[k & 1], &from_t = xt[k & 1], &to = x[~k & 1], &to_t = xt[~k & 1];
-        product<kGram>(s, a, Product{from, from, m, m, from.ld, q, q, 0, 0, 0}, stream);
-        product<kSquare>(s, a, Product{q, q, m, m, q.ld, b, b, 0, 0, 0}, stream);
+        product<kGram>(s, a, Product{from, from, m, m, from.ld, q, q, 0, 0, 0, 0, parts}, stream);
+        product<kSquare>(s, a, Product{q, q, m, m, q.ld, b, b, 0, 0, 0, 0, parts}, stream);
         if (k + 1 < s.steps)
-            product<kUpdate>(s, a, Product{b, from_t, m, n, b.ld, to, to_t, 0, 0, 0}, stream);
+            product<kUpdate>(s, a, Product{b, from_t, m, n, b.ld, to, to_t, 0, 0, 0, 0, parts}, stream);
         else if (s.tall)
-            product<kLast>(s, a, Product{from_t, b, n, m, b.ld, to, to_t, 0, 0, 0}, stream);
+            product<kLast>(s, a, Product{from_t, b, n, m, b.ld, to, to_t, 0, 0, 0, 0, parts}, stream);
         else
-            product<kLast>(s, a, Product{b, from_t, m, n, b.ld, to, to_t, 0, 0, 0}, stream);
+            product<kLast>(s, a, Product{b, from_t, m, n, b.ld, to, to_t, 0, 0, 0, 0, parts}, stream);
     }
 }
 

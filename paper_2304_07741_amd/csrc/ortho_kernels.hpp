@@ -18,7 +18,8 @@ struct Shape {
 struct Plan {
     uint64_t workspace_bytes = 0;
     int launches = 0;
-    int parts = 0;  // workgroups per matrix that square and sum
+    int parts = 0;            // workgroups per matrix that square and sum
+    uint64_t part_bytes = 0;  // of sums that are cut into parts
 };
 Plan plan_of(const Shape& s);
 
