@@ -12,9 +12,12 @@
 #include "ortho_kernels.hpp"
 
 #include <algorithm>
+#include <atomic>
 
 #include "device_util.hpp"
 #include "launch.hpp"
+#include "ortho_device.hpp"
+#include "ortho_small_kernels.hpp"
 #include "tile_util.hpp"
 
 namespace canvas {
@@ -22,8 +25,6 @@ namespace ortho {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
-constexpr double kEps = 1e-7;
 constexpr float kScale = 4096.f;  // 2^12
 constexpr int kDepth = 32;        // of one step of a product; leading dimensions are multiples of it, zeros behind the columns
 
@@ -44,11 +45,6 @@ __device__ __forceinline__ uint32_t pack_pair(float v) {  // v scaled: hi in the
     return (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
 }
 __device__ __forceinline__ float of_half(uint32_t u) { return (float)__builtin_bit_cast(_Float16, (uint16_t)u); }
-
-__device__ __forceinline__ float direction(const Shape& s, const Args& a, int64_t i, float m_new) {
-    if (!a.momentum) return a.grad[i];
-    return s.nesterov ? (float)(a.grad[i] + a.mu * m_new) : m_new;  // (mu in 64 bits: gradient and momentum may cancel)
-}
 
 // 16 bytes per lane from `from` + voff + soff to LDS, lane after lane behind `to` (the same for the whole wave).
 __device__ __forceinline__ tile::rsrc_t whole_memory(const void* from) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(from), 0, 0xffffffffu, 0x00020000); }
@@ -102,77 +98,80 @@ __global__ __launch_bounds__(kThreads) void k_mix(Shape s, Args a, double* sums)
 }
 
 // 1 / (|v| + 1e-7) of this workgroup's matrix.
-__device__ double inverse_norm(const double* sums, int parts, double* buf) {
+__device__ double inverse_norm(const double* sums, int parts) {
+    __shared__ double buf[kThreads / 64];
     double t = 0;
     for (int k = threadIdx.x; k < parts; k += kThreads) t += sums[k];
-    buf[threadIdx.x] = t;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
+    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = t;
     __syncthreads();
-    for (int o = kThreads / 2; o; o >>= 1) {
-        if ((int)threadIdx.x < o) buf[threadIdx.x] += buf[threadIdx.x + o];
-        __syncthreads();
-    }
-    return 1.0 / (sqrt(buf[0]) + kEps);
+    t = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; w++) t += buf[w];
+    return 1.0 / (sqrt(t) + kEps);
 }
 
 // X and X^T of the normalised direction, 64 x 64 elements per workgroup through LDS; zeros behind the columns.
 __global__ __launch_bounds__(kThreads) void k_start(Shape s, Args a, const double* sums, int parts, Pair x, Pair xt) {
-    __shared__ double buf[kThreads];
     __shared__ uint32_t img[64][65];
-    const double inv = inverse_norm(sums + (int64_t)blockIdx.y * parts, parts, buf);
     const unsigned wide = (unsigned)((s.K + 63) / 64), by = blockIdx.x / wide;
     const int64_t len = s.R * s.K, r0 = (int64_t)by * 64, c0 = (int64_t)(blockIdx.x - by * wide) * 64;
-    const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
+    const int c = (threadIdx.x & 15) * 4, r = threadIdx.x >> 4;
+    const bool whole = (s.K & 3) == 0;  // four elements side by side are aligned and in one row
+    const float* m = a.momentum ? a.momentum_out : nullptr;
+    f32x4 v[4];
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const int64_t row = r0 + r + 16 * k, col = c0 + c, i = blockIdx.y * len + row * s.K + col;
+        v[k] = f32x4{};
+        if (row >= s.R || col >= s.K) continue;
+        if (whole) {
+            const f32x4 g = !m || s.nesterov ? *reinterpret_cast<const f32x4*>(a.grad + i) : f32x4{}, w = m ? *reinterpret_cast<const f32x4*>(m + i) : f32x4{};
+#pragma unroll
+            for (int e = 0; e < 4; e++) v[k][e] = !m ? g[e] : s.nesterov ? (float)(g[e] + a.mu * w[e]) : w[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (col + e < s.K) v[k][e] = direction(s, a, i + e, m ? m[i + e] : 0.f);
+        }
+    }
+    const double inv = inverse_norm(sums + (int64_t)blockIdx.y * parts, parts);
+    // four pairs side by side
+    auto put = [&](const Pair& to, int64_t row, int64_t col, const uint32_t (&p)[4]) {
+        _Float16* at = to.hi + blockIdx.y * to.step + row * to.ld + col;
+        const uint32_t hi[2] = {__builtin_amdgcn_perm(p[1], p[0], 0x05040100u), __builtin_amdgcn_perm(p[3], p[2], 0x05040100u)};
+        const uint32_t lo[2] = {__builtin_amdgcn_perm(p[1], p[0], 0x07060302u), __builtin_amdgcn_perm(p[3], p[2], 0x07060302u)};
+        __builtin_memcpy(at, hi, 8);
+        __builtin_memcpy(at + to.plane, lo, 8);
+    };
     // orig: the planes laid out as the gradient is; turned: its transpose
     const Pair orig = s.tall ? xt : x, turned = s.tall ? x : xt;
-    for (int r = ty; r < 64; r += 4) {
-        const int64_t row = r0 + r, col = c0 + tx;
-        uint32_t p = 0;
-        if (row < s.R && col < s.K) {
-            const int64_t i = blockIdx.y * len + row * s.K + col;
-            p = pack_pair((float)(direction(s, a, i, a.momentum ? a.momentum_out[i] : 0.f) * inv) * kScale);
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const int64_t row = r0 + r + 16 * k, col = c0 + c;
+        uint32_t p[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            p[e] = pack_pair((float)(v[k][e] * inv) * kScale);
+            img[r + 16 * k][c + e] = p[e];
         }
-        img[r][tx] = p;
-        if (row < s.R && col < orig.ld) {
-            _Float16* at = orig.hi + blockIdx.y * orig.step + row * orig.ld + col;
-            *reinterpret_cast<uint16_t*>(at) = (uint16_t)p;
-            *reinterpret_cast<uint16_t*>(at + orig.plane) = (uint16_t)(p >> 16);
-        }
+        if (row < s.R && col < orig.ld) put(orig, row, col, p);
     }
     __syncthreads();
-    for (int r = ty; r < 64; r += 4) {
-        const int64_t row = c0 + r, col = r0 + tx;  // of the transpose
-        if (row < s.K && col < turned.ld) {
-            const uint32_t p = img[tx][r];
-            _Float16* at = turned.hi + blockIdx.y * turned.step + row * turned.ld + col;
-            *reinterpret_cast<uint16_t*>(at) = (uint16_t)p;
-            *reinterpret_cast<uint16_t*>(at + turned.plane) = (uint16_t)(p >> 16);
-        }
-    }
-}
-
-__device__ __forceinline__ void finish_one(const Shape& s, const Args& a, int64_t i, float o) {
-    if (a.update) {
-        if (s.bf16)
-            static_cast<uint16_t*>(a.update)[i] = f32_to_bf16(o);
-        else
-            static_cast<float*>(a.update)[i] = o;
-    }
-    if (a.master) {
-        const float w = (float)((1.0 - a.lr * a.decay) * a.master[i] - a.lr * o);
-        a.master_out[i] = w;
-        if (a.weights) {
-            if (s.bf16)
-                static_cast<uint16_t*>(a.weights)[i] = f32_to_bf16(w);
-            else
-                static_cast<float*>(a.weights)[i] = w;
-        }
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const int64_t row = c0 + r + 16 * k, col = r0 + c;  // of the transpose
+        uint32_t p[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) p[e] = img[c + e][r + 16 * k];
+        if (row < s.K && col < turned.ld) put(turned, row, col, p);
     }
 }
 
 // Plans without products: the normalised direction itself.
 __global__ __launch_bounds__(kThreads) void k_normalised(Shape s, Args a, const double* sums, int parts) {
-    __shared__ double buf[kThreads];
-    const double inv = inverse_norm(sums + (int64_t)blockIdx.y * parts, parts, buf);
+    const double inv = inverse_norm(sums + (int64_t)blockIdx.y * parts, parts);
     const int64_t len = s.R * s.K, k = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (k >= len) return;
     const int64_t i = blockIdx.y * len + k;
@@ -199,6 +198,20 @@ struct Tile {
     int grp, i0, j0;
     bool diagonal;
 };
+// A way of cutting products: tiles of BM x BN by WI x WJ waves, SUB times kDepth summands at a time.
+template <int BM_, int BN_, int WI_, int WJ_, int SUB_>
+struct Form {
+    static constexpr int BM = BM_, BN = BN_, WI = WI_, WJ = WJ_, SUB = SUB_;
+    static constexpr int kThreads = 64 * WI * WJ, TM = BM / WI / 32, TN = BN / WJ / 32;
+    static constexpr int kOpA = BM * 64, kOpB = BN * 64;  // bytes of one plane of kDepth summands
+    static constexpr int kPart = 2 * (kOpA + kOpB), kStage = SUB * kPart;
+    static constexpr int kRows = BM * BN * 4 > 2 * kStage ? 2 * kStage / (BN * 4) : BM;  // of results that LDS takes at once
+    static constexpr int kLds = 2 * kStage > kRows * BN * 4 ? 2 * kStage : kRows * BN * 4;
+};
+using Large = Form<256, 256, 2, 4, 1>;
+using Middle = Form<128, 128, 2, 2, 1>;
+using Small = Form<64, 64, 2, 2, 2>;
+
 template <int BM, int BN, Kind KIND>
 __device__ __forceinline__ Tile tile_of(const Product& g, int task) {
     const int grp = task / g.tiles, t = task - grp * g.tiles;
@@ -216,16 +229,20 @@ __device__ __forceinline__ Tile tile_of(const Product& g, int task) {
 }
 
 // The results of a tile, as the matrix units leave them in the registers of its workgroup, to where they belong.
-template <int BM, int BN, Kind KIND>
-__device__ __forceinline__ void finish(const Shape& s, const Args& args, const Product& g, const Tile& at, const f32x16 (&acc)[BM / 64][BN / 64], unsigned char* lds) {
-    constexpr int TM = BM / 64, TN = BN / 64;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wi = (wave >> 1) * (BM / 2), wj = (wave & 1) * (BN / 2);
-    const int grp = at.grp, i0 = at.i0, j0 = at.j0;
+template <class F, Kind KIND>
+__device__ __forceinline__ void finish(const Shape& s, const Args& args, const Product& g, const Tile& at, const f32x16 (&acc)[F::TM][F::TN], unsigned char* lds) {
+    constexpr int BN = F::BN, BM = F::kRows, TM = F::TM, TN = F::TN;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wj = wave % F::WJ * (TN * 32);
+    const int grp = at.grp, j0 = at.j0;
+    for (int half = 0; half < F::BM / F::kRows; half++) {
+    const int i0 = at.i0 + half * F::kRows, wi = wave / F::WJ * (TM * 32) - half * F::kRows;
+    if (half) __syncthreads();
     // The results as an image in LDS, first as fp32, then, read row by row, as pairs in the same places, which the transpose is
     // written from.  Columns are exchanged in pieces of 16 by bits of the row, so that eight rows of a column and both halves of
     // a wave fall on different banks.
     uint32_t* img = reinterpret_cast<uint32_t*>(lds);
     auto place = [&](int r, int c) { return r * BN + (c ^ (((((r >> 3) & 3) << 4) ^ (((r >> 2) & 1) << 5)) & (BN - 1))); };
+    if (wi >= 0 && wi < F::kRows)
 #pragma unroll
     for (int x = 0; x < TM; x++)
 #pragma unroll
@@ -237,7 +254,7 @@ __device__ __forceinline__ void finish(const Shape& s, const Args& args, const P
             }
     __syncthreads();
     constexpr int kChunks = BN / 8;
-    for (int e = tid; e < BM * kChunks; e += kThreads) {
+    for (int e = tid; e < BM * kChunks; e += F::kThreads) {
         const int r = e / kChunks, c = (e - r * kChunks) * 8, i = i0 + r, j = j0 + c;
         uint32_t* from = img + place(r, c);
         float v[8];
@@ -281,10 +298,10 @@ __device__ __forceinline__ void finish(const Shape& s, const Args& args, const P
             *reinterpret_cast<u32x4*>(to + g.out.plane) = lo;
         }
     }
-    if (KIND == kLast || (KIND != kUpdate && at.diagonal)) return;
+    if (KIND == kLast || (KIND != kUpdate && at.diagonal)) continue;
     __syncthreads();
     const Pair turn = KIND == kUpdate ? g.turn : g.out;
-    for (int e = tid; e < BN * (BM / 8); e += kThreads) {
+    for (int e = tid; e < BN * (BM / 8); e += F::kThreads) {
         // four pieces of eight rows side by side, then the columns
         const int piece4 = e & 3, rest = e >> 2, c = rest % BN, r = (rest / BN) * 32 + piece4 * 8, i = i0 + r, j = j0 + c;
         if (j >= g.cols || i >= turn.ld) continue;
@@ -301,27 +318,26 @@ __device__ __forceinline__ void finish(const Shape& s, const Args& args, const P
         *reinterpret_cast<u32x4*>(to) = hi;
         *reinterpret_cast<u32x4*>(to + turn.plane) = lo;
     }
+    }
 }
 
-
-// BM x BN results per workgroup of 2 x 2 waves.  Both planes of both operands are loaded straight into LDS, SUB times 32 summands
-// at a time, into the buffer that the previous step has left, while the products of the present one run.  Rows of 64 bytes
-// lie four to a line of all banks; a 16-byte piece c of row r lies at place c ^ (r / 4) % 4, so that the pieces that eight rows
-// read together fall on different banks.
-template <int BM, int BN, int SUB, Kind KIND>
-__global__ __launch_bounds__(kThreads) void k_product(Shape s, Args args, Product g) {
-    constexpr int TM = BM / 64, TN = BN / 64;
-    constexpr int kOpA = BM * 64, kOpB = BN * 64;            // bytes of one plane of 32 summands
-    constexpr int kPart = 2 * (kOpA + kOpB), kStage = SUB * kPart;
-    constexpr int kLds = 2 * kStage > BM * BN * 4 ? 2 * kStage : BM * BN * 4;
-    __shared__ __align__(16) unsigned char lds[kLds];
+// One tile of results, or one part of its sum, per workgroup.  Both planes of both operands are loaded straight into LDS, SUB
+// times 32 summands at a time, into the buffer that the previous step has left, while the products of the present one run.  Rows of
+// 64 bytes lie four to a line of all banks; a 16-byte piece c of row r lies at place c ^ (r / 4) % 4, so that the pieces that
+// eight rows read together fall on different banks.
+template <class F, Kind KIND>
+__global__ __launch_bounds__(F::kThreads) void k_product(Shape s, Args args, Product g) {
+    constexpr int BM = F::BM, BN = F::BN, SUB = F::SUB, TM = F::TM, TN = F::TN, kThreads = F::kThreads;
+    constexpr int kOpA = F::kOpA, kOpB = F::kOpB, kPart = F::kPart, kStage = F::kStage;
+    constexpr int kTimesA = BM * 4 / kThreads, kTimesB = BN * 4 / kThreads;  // 16-byte pieces of a thread in a plane
+    extern __shared__ __align__(16) unsigned char lds[];
 
     const unsigned seq = tile::xcd_sequence();
     const int task = seq / g.splits, split = seq - task * g.splits;
     const Tile at_tile = tile_of<BM, BN, KIND>(g, task);
     const int grp = at_tile.grp, i0 = at_tile.i0, j0 = at_tile.j0;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wi = (wave >> 1) * (BM / 2), wj = (wave & 1) * (BN / 2);
+    const int wi = wave / F::WJ * (TM * 32), wj = wave % F::WJ * (TN * 32);
 
     // 16-byte pieces of this thread in a plane of a step; rows past the end are the last one again
     auto piece = [&](int q, int first, int rows, int ld) {
@@ -329,11 +345,11 @@ __global__ __launch_bounds__(kThreads) void k_product(Shape s, Args args, Produc
         const int row = first + r < rows ? r : rows - 1 - first;
         return (uint32_t)row * (uint32_t)ld * 2u + (uint32_t)c * 16u;
     };
-    uint32_t va[BM / 64], vb[BN / 64];
+    uint32_t va[kTimesA], vb[kTimesB];
 #pragma unroll
-    for (int q = 0; q < BM / 64; q++) va[q] = piece(q, i0, g.rows, g.p.ld);
+    for (int q = 0; q < kTimesA; q++) va[q] = piece(q, i0, g.rows, g.p.ld);
 #pragma unroll
-    for (int q = 0; q < BN / 64; q++) vb[q] = piece(q, j0, g.cols, g.q.ld);
+    for (int q = 0; q < kTimesB; q++) vb[q] = piece(q, j0, g.cols, g.q.ld);
     const _Float16* pa = g.p.hi + grp * g.p.step + (int64_t)i0 * g.p.ld;
     const _Float16* pb = g.q.hi + grp * g.q.step + (int64_t)j0 * g.q.ld;
     const tile::rsrc_t ra[2] = {whole_memory(pa), whole_memory(pa + g.p.plane)};
@@ -348,9 +364,9 @@ __global__ __launch_bounds__(kThreads) void k_product(Shape s, Args args, Produc
 #pragma unroll
             for (int h = 0; h < 2; h++) {
 #pragma unroll
-                for (int q = 0; q < BM / 64; q++) load_to_lds(ra[h], to + h * kOpA + q * 4096, va[q], k);
+                for (int q = 0; q < kTimesA; q++) load_to_lds(ra[h], to + h * kOpA + q * (kThreads * 16), va[q], k);
 #pragma unroll
-                for (int q = 0; q < BN / 64; q++) load_to_lds(rb[h], to + 2 * kOpA + h * kOpB + q * 4096, vb[q], k);
+                for (int q = 0; q < kTimesB; q++) load_to_lds(rb[h], to + 2 * kOpA + h * kOpB + q * (kThreads * 16), vb[q], k);
             }
         }
     };
@@ -399,7 +415,7 @@ __global__ __launch_bounds__(kThreads) void k_product(Shape s, Args args, Produc
     __syncthreads();
 
     if (g.splits == 1) {
-        finish<BM, BN, KIND>(s, args, g, at_tile, acc, lds);
+        finish<F, KIND>(s, args, g, at_tile, acc, lds);
         return;
     }
     f32x4* mine = g.parts + ((int64_t)task * g.splits + split) * (BM * BN / 4) + tid;
@@ -413,12 +429,13 @@ __global__ __launch_bounds__(kThreads) void k_product(Shape s, Args args, Produc
 }
 
 // Adds the parts of a tile and finishes it.
-template <int BM, int BN, Kind KIND>
-__global__ __launch_bounds__(kThreads) void k_add(Shape s, Args args, Product g) {
-    constexpr int TM = BM / 64, TN = BN / 64, kEach = BM * BN / 4;
-    __shared__ __align__(16) unsigned char lds[BM * BN * 4];
+template <class F, Kind KIND>
+__global__ __launch_bounds__(F::kThreads) void k_add(Shape s, Args args, Product g) {
+    constexpr int TM = F::TM, TN = F::TN, kEach = F::BM * F::BN / 4, kThreads = F::kThreads;
+    extern __shared__ __align__(16) unsigned char lds[];
     const f32x4* from = g.parts + (int64_t)blockIdx.x * g.splits * kEach + threadIdx.x;
     f32x16 acc[TM][TN] = {};
+#pragma unroll 4
     for (int part = 0; part < g.splits; part++, from += kEach)
 #pragma unroll
         for (int x = 0; x < TM; x++)
@@ -430,7 +447,7 @@ __global__ __launch_bounds__(kThreads) void k_add(Shape s, Args args, Product g)
 #pragma unroll
                     for (int e = 0; e < 4; e++) acc[x][y][4 * q + e] += v[e];
                 }
-    finish<BM, BN, KIND>(s, args, g, tile_of<BM, BN, KIND>(g, blockIdx.x), acc, lds);
+    finish<F, KIND>(s, args, g, tile_of<F::BM, F::BN, KIND>(g, blockIdx.x), acc, lds);
 }
 
 uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
@@ -450,16 +467,23 @@ Cut cut_of(bool symmetric, int64_t rows, int64_t cols, int64_t depth, int64_t G)
         c.tiles = symmetric ? c.tiles_i * (c.tiles_i + 1) / 2 : c.tiles_i * c.tiles_j;
         return c.tiles * G;
     };
-    if (tiles(128) < 128) tiles(64);
+    // (a tile that mostly hangs over the edges is work for nothing)
+    auto full = [&](double share) { return (double)rows * cols >= share * c.side * c.side * c.tiles_i * c.tiles_j; };
+    if (!(tiles(256) >= 200 && full(0.75)) && !(tiles(128) >= 128 && full(0.6))) tiles(64);
     const int64_t steps = depth / kDepth, slots = 512 / (c.tiles * G), room = steps / 8;
-    c.splits = (int)std::max<int64_t>(1, std::min(slots, room));
+    c.splits = c.side == 256 ? 1 : (int)std::max<int64_t>(1, std::min(slots, room));
     return c;
 }
 
-template <int B, int SUB, Kind KIND>
+template <class F, Kind KIND>
 void launch(const Shape& s, const Args& a, const Product& g, hipStream_t stream) {
-    CANVAS_LAUNCH((k_product<B, B, SUB, KIND>), dim3((unsigned)(g.tiles * g.splits * s.G)), dim3(kThreads), 0, stream, s, a, g);
-    if (g.splits > 1) CANVAS_LAUNCH((k_add<B, B, KIND>), dim3((unsigned)(g.tiles * s.G)), dim3(kThreads), 0, stream, s, a, g);
+    if (F::kLds > 65536) {
+        static std::atomic<uint64_t> asked{0}, asked_add{0};
+        allow_lds(asked, reinterpret_cast<const void*>(&k_product<F, KIND>), F::kLds);
+        if (g.splits > 1) allow_lds(asked_add, reinterpret_cast<const void*>(&k_add<F, KIND>), F::kLds);
+    }
+    CANVAS_LAUNCH((k_product<F, KIND>), dim3((unsigned)(g.tiles * g.splits * s.G)), dim3(F::kThreads), F::kLds, stream, s, a, g);
+    if (g.splits > 1) CANVAS_LAUNCH((k_add<F, KIND>), dim3((unsigned)(g.tiles * s.G)), dim3(F::kThreads), F::kRows * F::BN * 4, stream, s, a, g);
 }
 template <Kind KIND>
 void product(const Shape& s, const Args& a, Product g, hipStream_t stream) {
@@ -468,16 +492,23 @@ void product(const Shape& s, const Args& a, Product g, hipStream_t stream) {
     g.tiles_j = c.tiles_j;
     g.tiles = c.tiles;
     g.splits = c.splits;
-    if (c.side == 128)
-        launch<128, 1, KIND>(s, a, g, stream);
+    if (c.side == 256)
+        launch<Large, KIND>(s, a, g, stream);
+    else if (c.side == 128)
+        launch<Middle, KIND>(s, a, g, stream);
     else
-        launch<64, 2, KIND>(s, a, g, stream);
+        launch<Small, KIND>(s, a, g, stream);
 }
 
 }  // namespace
 
 Plan plan_of(const Shape& s) {
     Plan p;
+    if (small_plan(s).fits) {
+        p.small = true;
+        p.launches = 1;
+        return p;
+    }
     p.parts = (int)((s.R * s.K + 16 * kThreads - 1) / (16 * kThreads));
     if (p.parts > 1024) p.parts = 1024;
     p.launches = 2;
@@ -493,6 +524,7 @@ Plan plan_of(const Shape& s) {
 }
 
 void step(const Shape& s, const Plan& p, const Args& a, hipStream_t stream) {
+    if (p.small) return step_small(s, a, stream);
     char* at = a.ws;
     auto take = [&](uint64_t bytes) {
         char* r = at;

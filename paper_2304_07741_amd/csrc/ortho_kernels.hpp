@@ -18,6 +18,7 @@ struct Shape {
 struct Plan {
     uint64_t workspace_bytes = 0;
     int launches = 0;
+    bool small = false;       // one launch of ortho_small_kernels.hip, without a workspace
     int parts = 0;            // workgroups per matrix that square and sum
     uint64_t part_bytes = 0;  // of sums that are cut into parts
 };
