@@ -52,6 +52,13 @@ __device__ __forceinline__ void load_to_lds(tile::rsrc_t from, unsigned char* to
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, voff, soff, 0, 0);
 }
 
+// A barrier behind which everybody's loads to LDS have arrived.  (A barrier alone waits for them only where the compiler sees a read
+// behind it that may concern them.)
+__device__ __forceinline__ void loads_arrived() {
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    __syncthreads();
+}
+
 // Momentum and the sum of squares of the direction, one part of a matrix per workgroup.
 __global__ __launch_bounds__(kThreads) void k_mix(Shape s, Args a, double* sums) {
     __shared__ double buf[kThreads];
@@ -198,19 +205,22 @@ struct Tile {
     int grp, i0, j0;
     bool diagonal;
 };
-// A way of cutting products: tiles of BM x BN by WI x WJ waves, SUB times kDepth summands at a time.
-template <int BM_, int BN_, int WI_, int WJ_, int SUB_>
+// A way of cutting products: tiles of BM x BN by WI x WJ waves, SUB times kDepth summands at a time in BUFFERS buffers; with sums
+// in parts or not.
+template <int BM_, int BN_, int WI_, int WJ_, int SUB_, int BUFFERS_, bool SPLITS_>
 struct Form {
-    static constexpr int BM = BM_, BN = BN_, WI = WI_, WJ = WJ_, SUB = SUB_;
+    static constexpr int BM = BM_, BN = BN_, WI = WI_, WJ = WJ_, SUB = SUB_, kBuffers = BUFFERS_;
+    static constexpr bool kSplits = SPLITS_;
     static constexpr int kThreads = 64 * WI * WJ, TM = BM / WI / 32, TN = BN / WJ / 32;
     static constexpr int kOpA = BM * 64, kOpB = BN * 64;  // bytes of one plane of kDepth summands
     static constexpr int kPart = 2 * (kOpA + kOpB), kStage = SUB * kPart;
-    static constexpr int kRows = BM * BN * 4 > 2 * kStage ? 2 * kStage / (BN * 4) : BM;  // of results that LDS takes at once
-    static constexpr int kLds = 2 * kStage > kRows * BN * 4 ? 2 * kStage : kRows * BN * 4;
+    static constexpr int kRows = BM * BN * 4 > kStage ? kStage / (BN * 4) : BM;  // of results that one buffer takes at once
 };
-using Large = Form<256, 256, 2, 4, 1>;
-using Middle = Form<128, 128, 2, 2, 1>;
-using Small = Form<64, 64, 2, 2, 2>;
+using Large = Form<256, 256, 2, 4, 1, 2, false>;
+using Middle = Form<128, 128, 2, 2, 1, 2, true>;
+using Small = Form<64, 64, 2, 2, 2, 2, true>;
+// Few workgroups with little to add up each: all of it is asked for at once.
+using Short = Form<64, 64, 2, 2, 8, 1, true>;
 
 template <int BM, int BN, Kind KIND>
 __device__ __forceinline__ Tile tile_of(const Product& g, int task) {
@@ -228,53 +238,61 @@ __device__ __forceinline__ Tile tile_of(const Product& g, int task) {
     return Tile{grp, bi * BM, bj * BN, bi == bj};
 }
 
-// The results of a tile, as the matrix units leave them in the registers of its workgroup, to where they belong.
-template <class F, Kind KIND>
-__device__ __forceinline__ void finish(const Shape& s, const Args& args, const Product& g, const Tile& at, const f32x16 (&acc)[F::TM][F::TN], unsigned char* lds) {
-    constexpr int BN = F::BN, BM = F::kRows, TM = F::TM, TN = F::TN;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wj = wave % F::WJ * (TN * 32);
-    const int grp = at.grp, j0 = at.j0;
-    for (int half = 0; half < F::BM / F::kRows; half++) {
-    const int i0 = at.i0 + half * F::kRows, wi = wave / F::WJ * (TM * 32) - half * F::kRows;
-    if (half) __syncthreads();
-    // The results as an image in LDS, first as fp32, then, read row by row, as pairs in the same places, which the transpose is
-    // written from.  Columns are exchanged in pieces of 16 by bits of the row, so that eight rows of a column and both halves of
-    // a wave fall on different banks.
-    uint32_t* img = reinterpret_cast<uint32_t*>(lds);
-    auto place = [&](int r, int c) { return r * BN + (c ^ (((((r >> 3) & 3) << 4) ^ (((r >> 2) & 1) << 5)) & (BN - 1))); };
-    if (wi >= 0 && wi < F::kRows)
+// Where element (r, c) of an image of rows of BN results is.  Columns are exchanged in pieces of 16 by bits of the row, so that
+// eight rows of a column, and the rows that the halves of a wave write at once, fall on different banks.
+template <int BN>
+__device__ __forceinline__ int place(int r, int c) {
+    return r * BN + (c ^ (((((r >> 3) & 3) << 4) ^ (((r >> 2) & 1) << 5)) & (BN - 1)));
+}
+// A block of 32 x 32 results, as the matrix units leave it, to its place.
+template <int BN>
+__device__ __forceinline__ void to_image(uint32_t* img, const f32x16& acc, int r0, int c0) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int x = 0; x < TM; x++)
+    for (int k = 0; k < 16; k++) img[place<BN>(r0 + (k >> 2) * 8 + (lane >> 5) * 4 + (k & 3), c0 + (lane & 31))] = __float_as_uint(acc[k]);
+}
+
+// Eight results side by side to two pieces of 16 bytes.
+__device__ __forceinline__ void put_pairs(_Float16* to, int64_t plane, const uint32_t (&p)[8]) {
+    u32x4 hi, lo;
 #pragma unroll
-        for (int y = 0; y < TN; y++)
-#pragma unroll
-            for (int k = 0; k < 16; k++) {
-                const int r = wi + x * 32 + (k >> 2) * 8 + (lane >> 5) * 4 + (k & 3), c = wj + y * 32 + (lane & 31);
-                img[place(r, c)] = __float_as_uint(acc[x][y][k]);
-            }
-    __syncthreads();
+    for (int k = 0; k < 4; k++) {
+        hi[k] = __builtin_amdgcn_perm(p[2 * k + 1], p[2 * k], 0x05040100u);
+        lo[k] = __builtin_amdgcn_perm(p[2 * k + 1], p[2 * k], 0x07060302u);
+    }
+    *reinterpret_cast<u32x4*>(to) = hi;
+    *reinterpret_cast<u32x4*>(to + plane) = lo;
+}
+
+// An image of BM x BN results, complete in LDS, to where it belongs: first as fp32, row by row; pairs are left in the same places,
+// which the transpose is written from.
+template <int BM, int BN, int THREADS, Kind KIND>
+__device__ __forceinline__ void emit(const Shape& s, const Args& args, const Product& g, int grp, int i0, int j0, bool diagonal, uint32_t* img) {
     constexpr int kChunks = BN / 8;
-    for (int e = tid; e < BM * kChunks; e += F::kThreads) {
+#pragma unroll 2
+    for (int e = threadIdx.x; e < BM * kChunks; e += THREADS) {
         const int r = e / kChunks, c = (e - r * kChunks) * 8, i = i0 + r, j = j0 + c;
-        uint32_t* from = img + place(r, c);
+        uint32_t* from = img + place<BN>(r, c);
         float v[8];
 #pragma unroll
         for (int k = 0; k < 8; k++) v[k] = __uint_as_float(from[k]);
         if (KIND == kLast) {
-            if (i >= g.rows) continue;
-            const int64_t first = (int64_t)grp * s.R * s.K + (int64_t)i * s.K + j;
+            if (i >= g.rows || j >= g.cols) continue;
 #pragma unroll
-            for (int k = 0; k < 8; k++)
-                if (j + k < g.cols) finish_one(s, args, first + k, v[k] * (1.f / (kScale * kScale)));
+            for (int k = 0; k < 8; k++) v[k] *= 1.f / (kScale * kScale);
+            const int64_t first = (int64_t)grp * s.R * s.K + (int64_t)i * s.K + j;
+            if ((s.K & 7) == 0)
+                finish_eight(s, args, first, v);
+            else
+                for (int k = 0; k < 8 && j + k < g.cols; k++) finish_one(s, args, first + k, v[k]);
             continue;
         }
         const bool in = i < g.rows && j < g.out.ld;
-        _Float16* to = g.out.hi + grp * g.out.step + (int64_t)i * g.out.ld + j;
         u32x4 ah = {}, al = {};
         if (KIND == kSquare && in) {
-            const _Float16* pa2 = g.p.hi + grp * g.p.step + (int64_t)i * g.p.ld + j;
-            ah = *reinterpret_cast<const u32x4*>(pa2);
-            al = *reinterpret_cast<const u32x4*>(pa2 + g.p.plane);
+            const _Float16* a = g.p.hi + grp * g.p.step + (int64_t)i * g.p.ld + j;
+            ah = *reinterpret_cast<const u32x4*>(a);
+            al = *reinterpret_cast<const u32x4*>(a + g.p.plane);
         }
         uint32_t p[8];
 #pragma unroll
@@ -287,42 +305,25 @@ __device__ __forceinline__ void finish(const Shape& s, const Args& args, const P
             p[k] = i < g.rows && j + k < g.cols ? pack_pair(w) : 0u;
             from[k] = p[k];
         }
-        if (in) {
-            u32x4 hi, lo;
-#pragma unroll
-            for (int k = 0; k < 4; k++) {
-                hi[k] = __builtin_amdgcn_perm(p[2 * k + 1], p[2 * k], 0x05040100u);
-                lo[k] = __builtin_amdgcn_perm(p[2 * k + 1], p[2 * k], 0x07060302u);
-            }
-            *reinterpret_cast<u32x4*>(to) = hi;
-            *reinterpret_cast<u32x4*>(to + g.out.plane) = lo;
-        }
+        if (in) put_pairs(g.out.hi + grp * g.out.step + (int64_t)i * g.out.ld + j, g.out.plane, p);
     }
-    if (KIND == kLast || (KIND != kUpdate && at.diagonal)) continue;
+    if (KIND == kLast || (KIND != kUpdate && diagonal)) return;
     __syncthreads();
     const Pair turn = KIND == kUpdate ? g.turn : g.out;
-    for (int e = tid; e < BN * (BM / 8); e += F::kThreads) {
+#pragma unroll 2
+    for (int e = threadIdx.x; e < BN * (BM / 8); e += THREADS) {
         // four pieces of eight rows side by side, then the columns
         const int piece4 = e & 3, rest = e >> 2, c = rest % BN, r = (rest / BN) * 32 + piece4 * 8, i = i0 + r, j = j0 + c;
         if (j >= g.cols || i >= turn.ld) continue;
         uint32_t p[8];
 #pragma unroll
-        for (int k = 0; k < 8; k++) p[k] = img[place(r + k, c)];
-        u32x4 hi, lo;
-#pragma unroll
-        for (int k = 0; k < 4; k++) {
-            hi[k] = __builtin_amdgcn_perm(p[2 * k + 1], p[2 * k], 0x05040100u);
-            lo[k] = __builtin_amdgcn_perm(p[2 * k + 1], p[2 * k], 0x07060302u);
-        }
-        _Float16* to = turn.hi + grp * turn.step + (int64_t)j * turn.ld + i;
-        *reinterpret_cast<u32x4*>(to) = hi;
-        *reinterpret_cast<u32x4*>(to + turn.plane) = lo;
-    }
+        for (int k = 0; k < 8; k++) p[k] = img[place<BN>(r + k, c)];
+        put_pairs(turn.hi + grp * turn.step + (int64_t)j * turn.ld + i, turn.plane, p);
     }
 }
 
 // One tile of results, or one part of its sum, per workgroup.  Both planes of both operands are loaded straight into LDS, SUB
-// times 32 summands at a time, into the buffer that the previous step has left, while the products of the present one run.  Rows of
+// times 32 summands at a time, a whole stage ahead of their use.  Rows of
 // 64 bytes lie four to a line of all banks; a 16-byte piece c of row r lies at place c ^ (r / 4) % 4, so that the pieces that
 // eight rows read together fall on different banks.
 template <class F, Kind KIND>
@@ -330,7 +331,8 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Shape s, Args args, Pro
     constexpr int BM = F::BM, BN = F::BN, SUB = F::SUB, TM = F::TM, TN = F::TN, kThreads = F::kThreads;
     constexpr int kOpA = F::kOpA, kOpB = F::kOpB, kPart = F::kPart, kStage = F::kStage;
     constexpr int kTimesA = BM * 4 / kThreads, kTimesB = BN * 4 / kThreads;  // 16-byte pieces of a thread in a plane
-    extern __shared__ __align__(16) unsigned char lds[];
+    // (two arrays, not one: the compiler has to see that loads into the one do not concern reads of the other)
+    __shared__ __align__(16) unsigned char first_buffer[kStage], second_buffer[F::kBuffers == 2 ? kStage : 16];
 
     const unsigned seq = tile::xcd_sequence();
     const int task = seq / g.splits, split = seq - task * g.splits;
@@ -355,11 +357,11 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Shape s, Args args, Pro
     const tile::rsrc_t ra[2] = {whole_memory(pa), whole_memory(pa + g.p.plane)};
     const tile::rsrc_t rb[2] = {whole_memory(pb), whole_memory(pb + g.q.plane)};
     const int all = g.depth / kDepth, begin = (int)((int64_t)all * split / g.splits), end = (int)((int64_t)all * (split + 1) / g.splits);
-    auto load = [&](int first, int buffer) {
+    auto load = [&](int first, unsigned char* buffer) {
 #pragma unroll
         for (int u = 0; u < SUB; u++) {
-            if (u && first + u >= end) break;
-            unsigned char* to = lds + buffer * kStage + u * kPart + wave * 1024;
+            if (first + u >= end) break;
+            unsigned char* to = buffer + u * kPart + wave * 1024;
             const int k = (first + u) * (kDepth * 2);
 #pragma unroll
             for (int h = 0; h < 2; h++) {
@@ -372,50 +374,95 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Shape s, Args args, Pro
     };
 
     f32x16 acc[TM][TN] = {};
-    load(begin, 0);
-    for (int step = begin, buffer = 0; step < end; step += SUB, buffer ^= 1) {
-        __syncthreads();  // this step's operands are there, and everybody has read the last one's
-        half8 a[SUB][2][TM][2], b[SUB][2][TN][2];
+    // the operands of 16 summands: half of those of one part of a stage
+    struct Operands {
+        half8 a[TM][2], b[TN][2];
+    };
+    auto read = [&](const unsigned char* buffer, int unit, Operands& o) {
+        const unsigned char* at = buffer + (unit >> 1) * kPart;
+        const int c = (unit & 1) * 2 + (lane >> 5);
 #pragma unroll
-        for (int u = 0; u < SUB; u++) {
-            const unsigned char* at = lds + buffer * kStage + u * kPart;
+        for (int x = 0; x < TM; x++) {
+            const int r = wi + x * 32 + (lane & 31);
 #pragma unroll
-            for (int k = 0; k < 2; k++) {
-                const int c = k * 2 + (lane >> 5);
+            for (int h = 0; h < 2; h++) o.a[x][h] = *reinterpret_cast<const half8*>(at + h * kOpA + r * 64 + ((c ^ ((r >> 2) & 3)) << 4));
+        }
 #pragma unroll
-                for (int x = 0; x < TM; x++) {
-                    const int r = wi + x * 32 + (lane & 31);
+        for (int y = 0; y < TN; y++) {
+            const int r = wj + y * 32 + (lane & 31);
 #pragma unroll
-                    for (int h = 0; h < 2; h++) a[u][k][x][h] = *reinterpret_cast<const half8*>(at + h * kOpA + r * 64 + ((c ^ ((r >> 2) & 3)) << 4));
-                }
+            for (int h = 0; h < 2; h++) o.b[y][h] = *reinterpret_cast<const half8*>(at + 2 * kOpA + h * kOpB + r * 64 + ((c ^ ((r >> 2) & 3)) << 4));
+        }
+    };
+    auto multiply = [&](const Operands& o) {
 #pragma unroll
-                for (int y = 0; y < TN; y++) {
-                    const int r = wj + y * 32 + (lane & 31);
+        for (int x = 0; x < TM; x++)
 #pragma unroll
-                    for (int h = 0; h < 2; h++) b[u][k][y][h] = *reinterpret_cast<const half8*>(at + 2 * kOpA + h * kOpB + r * 64 + ((c ^ ((r >> 2) & 3)) << 4));
-                }
+            for (int y = 0; y < TN; y++) {
+                acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.a[x][1], o.b[y][0], acc[x][y], 0, 0, 0);
+                acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.a[x][0], o.b[y][1], acc[x][y], 0, 0, 0);
+                acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.a[x][0], o.b[y][0], acc[x][y], 0, 0, 0);
             }
+    };
+    constexpr int kUnits = 2 * SUB;
+    Operands o[2];
+    if (F::kBuffers == 1) {
+        for (int step = begin; step < end; step += SUB) {
+            load(step, first_buffer);
+            loads_arrived();
+#pragma unroll
+            for (int unit = 0; unit < kUnits; unit++) {
+                if (step + unit / 2 >= end) break;
+                read(first_buffer, unit, o[0]);
+                multiply(o[0]);
+            }
+            __syncthreads();
         }
-        if (step + SUB < end) load(step + SUB, buffer ^ 1);
+    } else {
+        // One stage, `now` its buffer: each unit's products run while the next one's operands are read; before the last unit
+        // everybody has read this buffer and the next stage has arrived, so the one behind that is asked for.
+        auto stage = [&](int step, unsigned char* now, unsigned char* next) {
 #pragma unroll
-        for (int u = 0; u < SUB; u++) {
-            if (u && step + u >= end) break;
-#pragma unroll
-            for (int k = 0; k < 2; k++)
-#pragma unroll
-                for (int x = 0; x < TM; x++)
-#pragma unroll
-                    for (int y = 0; y < TN; y++) {
-                        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[u][k][x][1], b[u][k][y][0], acc[x][y], 0, 0, 0);
-                        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[u][k][x][0], b[u][k][y][1], acc[x][y], 0, 0, 0);
-                        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[u][k][x][0], b[u][k][y][0], acc[x][y], 0, 0, 0);
-                    }
+            for (int unit = 0; unit < kUnits; unit++) {
+                if (unit + 1 < kUnits) {
+                    read(now, unit + 1, o[(unit + 1) & 1]);
+                } else {
+                    loads_arrived();
+                    load(step + 2 * SUB, now);
+                    read(next, 0, o[0]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (step + unit / 2 < end) multiply(o[unit & 1]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        load(begin, first_buffer);
+        load(begin + SUB, second_buffer);
+        loads_arrived();
+        read(first_buffer, 0, o[0]);
+        for (int step = begin; step < end; step += 2 * SUB) {
+            stage(step, first_buffer, second_buffer);
+            if (step + SUB >= end) break;
+            stage(step + SUB, second_buffer, first_buffer);
         }
+        loads_arrived();
     }
-    __syncthreads();
 
     if (g.splits == 1) {
-        finish<F, KIND>(s, args, g, at_tile, acc, lds);
+        uint32_t* img = reinterpret_cast<uint32_t*>(first_buffer);
+#pragma unroll 1
+        for (int r0 = 0; r0 < BM; r0 += F::kRows) {
+            if (r0) __syncthreads();
+#pragma unroll
+            for (int x = 0; x < TM; x++) {
+                const int r = wi + x * 32 - r0;
+                if (r < 0 || r >= F::kRows) continue;
+#pragma unroll
+                for (int y = 0; y < TN; y++) to_image<BN>(img, acc[x][y], r, wj + y * 32);
+            }
+            __syncthreads();
+            emit<F::kRows, BN, kThreads, KIND>(s, args, g, grp, i0 + r0, j0, at_tile.diagonal, img);
+        }
         return;
     }
     f32x4* mine = g.parts + ((int64_t)task * g.splits + split) * (BM * BN / 4) + tid;
@@ -428,26 +475,31 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Shape s, Args args, Pro
                 mine[((x * TN + y) * 4 + q) * kThreads] = f32x4{acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
 }
 
-// Adds the parts of a tile and finishes it.
+// Adds the parts of 32 x 32 results, each of four waves every fourth part, and finishes them.
 template <class F, Kind KIND>
-__global__ __launch_bounds__(F::kThreads) void k_add(Shape s, Args args, Product g) {
-    constexpr int TM = F::TM, TN = F::TN, kEach = F::BM * F::BN / 4, kThreads = F::kThreads;
-    extern __shared__ __align__(16) unsigned char lds[];
-    const f32x4* from = g.parts + (int64_t)blockIdx.x * g.splits * kEach + threadIdx.x;
-    f32x16 acc[TM][TN] = {};
+__global__ __launch_bounds__(256) void k_add(Shape s, Args args, Product g) {
+    constexpr int kBlocks = F::BM / 32 * (F::BN / 32), kEach = F::BM * F::BN / 4;
+    __shared__ f32x4 sums[4][4][64];
+    __shared__ uint32_t img[32 * 32];
+    const int task = blockIdx.x / kBlocks, block = blockIdx.x - task * kBlocks, bi = block / (F::BN / 32), bj = block - bi * (F::BN / 32);
+    const Tile at = tile_of<F::BM, F::BN, KIND>(g, task);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // the block in the registers of the product's workgroup
+    const int owner = bi / F::TM * F::WJ + bj / F::TN, x = bi % F::TM, y = bj % F::TN;
+    const f32x4* from = g.parts + (int64_t)task * g.splits * kEach + (x * F::TN + y) * 4 * F::kThreads + owner * 64 + lane;
+    f32x4 acc[4] = {};
 #pragma unroll 4
-    for (int part = 0; part < g.splits; part++, from += kEach)
+    for (int part = wave; part < g.splits; part += 4)
 #pragma unroll
-        for (int x = 0; x < TM; x++)
+        for (int q = 0; q < 4; q++) acc[q] += from[(int64_t)part * kEach + q * F::kThreads];
 #pragma unroll
-            for (int y = 0; y < TN; y++)
+    for (int q = 0; q < 4; q++) sums[wave][q][lane] = acc[q];
+    __syncthreads();
+    const f32x4 v = sums[0][wave][lane] + sums[1][wave][lane] + sums[2][wave][lane] + sums[3][wave][lane];
 #pragma unroll
-                for (int q = 0; q < 4; q++) {
-                    const f32x4 v = from[((x * TN + y) * 4 + q) * kThreads];
-#pragma unroll
-                    for (int e = 0; e < 4; e++) acc[x][y][4 * q + e] += v[e];
-                }
-    finish<F, KIND>(s, args, g, tile_of<F::BM, F::BN, KIND>(g, blockIdx.x), acc, lds);
+    for (int e = 0; e < 4; e++) img[place<32>(wave * 8 + (lane >> 5) * 4 + e, lane & 31)] = __float_as_uint(v[e]);
+    __syncthreads();
+    emit<32, 32, 256, KIND>(s, args, g, at.grp, at.i0 + bi * 32, at.j0 + bj * 32, at.diagonal, img);
 }
 
 uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
@@ -457,6 +509,7 @@ int padded(int64_t n) { return (int)((n + kDepth - 1) / kDepth * kDepth); }
 // How a product is cut: sides of the tiles, parts of the sum.
 struct Cut {
     int side, tiles_i, tiles_j, tiles, splits;
+    bool brief;  // sides of 64: a workgroup on each compute unit at most, each with few steps
 };
 Cut cut_of(bool symmetric, int64_t rows, int64_t cols, int64_t depth, int64_t G) {
     Cut c;
@@ -470,20 +523,20 @@ Cut cut_of(bool symmetric, int64_t rows, int64_t cols, int64_t depth, int64_t G)
     // (a tile that mostly hangs over the edges is work for nothing)
     auto full = [&](double share) { return (double)rows * cols >= share * c.side * c.side * c.tiles_i * c.tiles_j; };
     if (!(tiles(256) >= 200 && full(0.75)) && !(tiles(128) >= 128 && full(0.6))) tiles(64);
-    const int64_t steps = depth / kDepth, slots = 512 / (c.tiles * G), room = steps / 8;
+    // Parts of a sum cost a launch and their way through memory (4 to 12 us): only where they leave 8 (16) steps or more to each,
+    // and not where there is a tile for most compute units already.
+    const int64_t steps = depth / kDepth, slots = c.tiles * G >= 160 ? 1 : 512 / (c.tiles * G), room = steps / (c.side == 64 ? 8 : 16);
     c.splits = c.side == 256 ? 1 : (int)std::max<int64_t>(1, std::min(slots, room));
+    c.brief = c.side == 64 && c.tiles * G * c.splits <= 256 && (steps + c.splits - 1) / c.splits <= Short::SUB;
     return c;
 }
 
 template <class F, Kind KIND>
 void launch(const Shape& s, const Args& a, const Product& g, hipStream_t stream) {
-    if (F::kLds > 65536) {
-        static std::atomic<uint64_t> asked{0}, asked_add{0};
-        allow_lds(asked, reinterpret_cast<const void*>(&k_product<F, KIND>), F::kLds);
-        if (g.splits > 1) allow_lds(asked_add, reinterpret_cast<const void*>(&k_add<F, KIND>), F::kLds);
+    CANVAS_LAUNCH((k_product<F, KIND>), dim3((unsigned)(g.tiles * g.splits * s.G)), dim3(F::kThreads), 0, stream, s, a, g);
+    if constexpr (F::kSplits) {
+        if (g.splits > 1) CANVAS_LAUNCH((k_add<F, KIND>), dim3((unsigned)(g.tiles * s.G) * (F::BM / 32 * (F::BN / 32))), dim3(256), 0, stream, s, a, g);
     }
-    CANVAS_LAUNCH((k_product<F, KIND>), dim3((unsigned)(g.tiles * g.splits * s.G)), dim3(F::kThreads), F::kLds, stream, s, a, g);
-    if (g.splits > 1) CANVAS_LAUNCH((k_add<F, KIND>), dim3((unsigned)(g.tiles * s.G)), dim3(F::kThreads), F::kRows * F::BN * 4, stream, s, a, g);
 }
 template <Kind KIND>
 void product(const Shape& s, const Args& a, Product g, hipStream_t stream) {
@@ -496,6 +549,8 @@ void product(const Shape& s, const Args& a, Product g, hipStream_t stream) {
         launch<Large, KIND>(s, a, g, stream);
     else if (c.side == 128)
         launch<Middle, KIND>(s, a, g, stream);
+    else if (c.brief)
+        launch<Short, KIND>(s, a, g, stream);
     else
         launch<Small, KIND>(s, a, g, stream);
 }
