@@ -272,10 +272,11 @@ __device__ __forceinline__ void emit(const Shape& s, const Args& args, const Pro
 #pragma unroll 2
     for (int e = threadIdx.x; e < BM * kChunks; e += THREADS) {
         const int r = e / kChunks, c = (e - r * kChunks) * 8, i = i0 + r, j = j0 + c;
-        uint32_t* from = img + place<BN>(r, c);
+        u32x4* from = reinterpret_cast<u32x4*>(img + place<BN>(r, c));  // (pieces of 16 columns stay together)
+        const u32x4 raw[2] = {from[0], from[1]};
         float v[8];
 #pragma unroll
-        for (int k = 0; k < 8; k++) v[k] = __uint_as_float(from[k]);
+        for (int k = 0; k < 8; k++) v[k] = __uint_as_float(raw[k >> 2][k & 3]);
         if (KIND == kLast) {
             if (i >= g.rows || j >= g.cols) continue;
 #pragma unroll
@@ -303,8 +304,9 @@ __device__ __forceinline__ void emit(const Shape& s, const Args& args, const Pro
                 w = kC * w + (kB * (of_half(hw & 0xffffu) + of_half(lw & 0xffffu)) + (i == j + k ? kA * kScale : 0.f));
             }
             p[k] = i < g.rows && j + k < g.cols ? pack_pair(w) : 0u;
-            from[k] = p[k];
         }
+        from[0] = u32x4{p[0], p[1], p[2], p[3]};
+        from[1] = u32x4{p[4], p[5], p[6], p[7]};
         if (in) put_pairs(g.out.hi + grp * g.out.step + (int64_t)i * g.out.ld + j, g.out.plane, p);
     }
     if (KIND == kLast || (KIND != kUpdate && diagonal)) return;
@@ -373,7 +375,9 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Shape s, Args args, Pro
         }
     };
 
-    f32x16 acc[TM][TN] = {};
+    // (products that add to one block of results wait for each other: with one block per wave the three pairings go apart)
+    constexpr int kChains = TM * TN == 1 ? 3 : 1;
+    f32x16 acc[TM][TN] = {}, apart[kChains - 1 ? kChains - 1 : 1] = {};
     // the operands of 16 summands: half of those of one part of a stage
     struct Operands {
         half8 a[TM][2], b[TN][2];
@@ -399,8 +403,9 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Shape s, Args args, Pro
         for (int x = 0; x < TM; x++)
 #pragma unroll
             for (int y = 0; y < TN; y++) {
-                acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.a[x][1], o.b[y][0], acc[x][y], 0, 0, 0);
-                acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.a[x][0], o.b[y][1], acc[x][y], 0, 0, 0);
+                f32x16 &first = kChains == 3 ? apart[0] : acc[x][y], &second = kChains == 3 ? apart[kChains / 2] : acc[x][y];
+                first = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.a[x][1], o.b[y][0], first, 0, 0, 0);
+                second = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.a[x][0], o.b[y][1], second, 0, 0, 0);
                 acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.a[x][0], o.b[y][0], acc[x][y], 0, 0, 0);
             }
     };
@@ -410,11 +415,13 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Shape s, Args args, Pro
         for (int step = begin; step < end; step += SUB) {
             load(step, first_buffer);
             loads_arrived();
+            read(first_buffer, 0, o[0]);
 #pragma unroll
             for (int unit = 0; unit < kUnits; unit++) {
-                if (step + unit / 2 >= end) break;
-                read(first_buffer, unit, o[0]);
-                multiply(o[0]);
+                if (unit + 1 < kUnits) read(first_buffer, unit + 1, o[(unit + 1) & 1]);  // (of no use behind the end, but in the buffer)
+                __builtin_amdgcn_sched_barrier(0);
+                if (step + unit / 2 < end) multiply(o[unit & 1]);
+                __builtin_amdgcn_sched_barrier(0);
             }
             __syncthreads();
         }
@@ -447,6 +454,7 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Shape s, Args args, Pro
         }
         loads_arrived();
     }
+    if (kChains == 3) acc[0][0] += apart[0] + apart[kChains / 2];
 
     if (g.splits == 1) {
         uint32_t* img = reinterpret_cast<uint32_t*>(first_buffer);
@@ -480,7 +488,7 @@ template <class F, Kind KIND>
 __global__ __launch_bounds__(256) void k_add(Shape s, Args args, Product g) {
     constexpr int kBlocks = F::BM / 32 * (F::BN / 32), kEach = F::BM * F::BN / 4;
     __shared__ f32x4 sums[4][4][64];
-    __shared__ uint32_t img[32 * 32];
+    __shared__ __align__(16) uint32_t img[32 * 32];
     const int task = blockIdx.x / kBlocks, block = blockIdx.x - task * kBlocks, bi = block / (F::BN / 32), bj = block - bi * (F::BN / 32);
     const Tile at = tile_of<F::BM, F::BN, KIND>(g, task);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
