@@ -210,10 +210,18 @@ def _ptrs(tensors):
     return arr
 
 
-def _stream():
-    import torch
+_torch = None
 
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+def _stream():
+    """torch's current stream of the current device, as an address."""
+    global _torch
+    if _torch is None:
+        import torch
+
+        torch.cuda.current_stream()      # (initialises the device)
+        _torch = torch
+    return _torch._C._cuda_getCurrentRawStream(_torch._C._cuda_getDevice())
 
 
 def canvas_dag_forward(handle, x, weights, y, workspace):

@@ -19,6 +19,7 @@
 #include "device_util.hpp"
 #include "launch.hpp"
 #include "tile_util.hpp"
+#include "wave_util.hpp"
 
 namespace canvas {
 namespace logprob {
@@ -113,36 +114,41 @@ __device__ __forceinline__ float value_of(uint32_t o) {
 }
 __device__ __forceinline__ uint64_t key_of(uint32_t o, uint32_t index) { return o <= kNone ? 0 : (uint64_t)o << 32 | (uint32_t)~index; }
 
-struct Largest {
-    static __device__ __forceinline__ float of(float a, float b) { return fmaxf(a, b); }
-};
-struct Total {
-    static __device__ __forceinline__ float of(float a, float b) { return a + b; }
-};
-template <class J, int LANES = 64>
-__device__ __forceinline__ float over_wave(float v) {  // of LANES lanes side by side
-#pragma unroll
-    for (int o = LANES / 2; o; o >>= 1) v = J::of(v, __shfl_xor(v, o));
-    return v;
-}
-// Over the THREADS threads of a row: a wave, or a workgroup through `buf` (one float per wave; a barrier before it is used
-// again is the caller's).
-template <int THREADS, class J>
-__device__ __forceinline__ float over_row(float v, float* buf) {
-    v = over_wave<J>(v);
+// Over the THREADS threads of a row: a wave, or a workgroup through `buf` (a place per wave; a barrier before it is used again is
+// the caller's).
+template <int THREADS>
+__device__ __forceinline__ float largest_of_row(float v, float* buf) {
+    v = wave::over<1, wave::Max>(v);
     if (THREADS == 64) return v;
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
     __syncthreads();
-    return over_wave<J, THREADS / 64>(buf[threadIdx.x & (THREADS / 64 - 1)]);
+    v = buf[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; w++) v = fmaxf(v, buf[w]);
+    return v;
+}
+template <int THREADS>
+__device__ __forceinline__ void sums_of_row(float& a, float& b, float2* buf) {
+    a = wave::over<1, wave::Sum>(a);
+    b = wave::over<1, wave::Sum>(b);
+    if (THREADS == 64) return;
+    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = make_float2(a, b);
+    __syncthreads();
+    a = b = 0.f;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; w++) {
+        a += buf[w].x;
+        b += buf[w].y;
+    }
 }
 
 constexpr int kTogether = 8;  // keys compared at a time: the list has as many places more
-// The k largest of the keys that the THREADS threads of the workgroup hold, in descending order to `put(rank, key)`, 0 past
-// the last one.  best: this thread's largest key; pieces: into how many its keys fall; piece(thread, number, f): calls f
-// for each key of one; LOW: bits of the order that may differ.  lds: THREADS keys, then k times the keys of a thread and
-// kTogether.
-template <int THREADS, int LOW, class PIECE, class PUT>
-__device__ void select_keys(int k, uint64_t best, int pieces, uint64_t* lds, PIECE piece, PUT put) {
+// The k largest of the keys that the THREADS threads of the workgroup hold, in descending order to `put(rank, key)`, 0 past the
+// last one.  best: this thread's largest key; LOW: bits of the order that are the same in all keys of one order.  own(f) calls f
+// for each of the thread's keys if they are at hand (pieces = 0); else they fall into `pieces`, and piece(thread, number, f)
+// calls f for each key of one.  lds: THREADS keys, then k times the keys of a thread and kTogether.
+template <int THREADS, int LOW, class OWN, class PIECE, class PUT>
+__device__ void select_keys(int k, uint64_t best, int pieces, uint64_t* lds, OWN own, PIECE piece, PUT put) {
     __shared__ uint64_t s_bound;
     __shared__ uint32_t s_count, s_holders, s_holder[64];  // (at most k threads reach the bound)
     uint64_t* list = lds + THREADS;
@@ -204,14 +210,19 @@ __device__ void select_keys(int k, uint64_t best, int pieces, uint64_t* lds, PIE
     __syncthreads();
     const uint64_t bound = s_bound;
     // (the places in both lists do not matter: the ranks do not depend on them)
-    if (best >= bound) s_holder[atomicAdd(&s_holders, 1u)] = threadIdx.x;
-    __syncthreads();
-    const int items = (int)s_holders * pieces;
-    for (int i = threadIdx.x; i < items; i += THREADS) {
-        const int h = i / pieces;
-        piece((int)s_holder[h], i - h * pieces, [&](uint64_t key) {
-            if (key >= bound) list[atomicAdd(&s_count, 1u)] = key;
-        });
+    auto candidate = [&](uint64_t key) {
+        if (key >= bound) list[atomicAdd(&s_count, 1u)] = key;
+    };
+    if (pieces == 0) {
+        if (best >= bound) own(candidate);
+    } else {
+        if (best >= bound) s_holder[atomicAdd(&s_holders, 1u)] = threadIdx.x;
+        __syncthreads();
+        const int items = (int)s_holders * pieces;
+        for (int i = threadIdx.x; i < items; i += THREADS) {
+            const int h = i / pieces;
+            piece((int)s_holder[h], i - h * pieces, candidate);
+        }
     }
     __syncthreads();
     const int n = (int)s_count;
@@ -284,7 +295,8 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_fwd(Shape s, 
     using Y = Type<T>;
     constexpr int V = Y::kVec;
     extern __shared__ uint64_t lds[];
-    __shared__ float buf[3][16];
+    __shared__ float most[4];
+    __shared__ float2 sums[4];
     const int tid = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
     const int64_t tasks = s.rows * p.segments, per = THREADS == 64 ? 4 : 1;
     const float scale = a.it * kLog2e;
@@ -331,9 +343,9 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_fwd(Shape s, 
             }
         }
         const float own = r.sum;
-        r.raise(over_row<THREADS, Largest>(r.m, buf[0]), scale);
-        r.sum = over_row<THREADS, Total>(r.sum, buf[1]);
-        r.along = over_row<THREADS, Total>(r.along, buf[2]) * kLn2;
+        r.raise(largest_of_row<THREADS>(r.m, most), scale);
+        sums_of_row<THREADS>(r.sum, r.along, sums);
+        r.along *= kLn2;
         const Row whole = row_of(r);
         if (tid == 0) {
             if (p.segments == 1) {
@@ -372,7 +384,11 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_fwd(Shape s, 
                 best = key_of(order_of(best_value), (uint32_t)begin + best_at * V + e);
             }
             uint64_t* keys = reinterpret_cast<uint64_t*>(a.ws + p.keys_at) + task * s.top;
-            select_keys<THREADS, Y::kLow>(s.top, best, pieces, lds, piece, [&](int rank, uint64_t key) {
+            auto own_keys = [&](auto f) {
+#pragma unroll
+                for (int e = 0; e < V; e++) f(key_of(order_of(Y::at(v[0], e)), (uint32_t)begin + tid * V + e));
+            };
+            select_keys<THREADS, Y::kLow>(s.top, best, pieces == 1 ? 0 : pieces, lds, own_keys, piece, [&](int rank, uint64_t key) {
                 if (p.segments == 1)
                     write_top(s, a, row, whole, rank, key);
                 else
@@ -394,9 +410,9 @@ __global__ __launch_bounds__(kJoin) void k_join(Shape s, Plan p, Fwd a) {
         const int lane = threadIdx.x & 63;
         const Part mine = lane < p.segments ? parts[lane] : Part{kLowest, 0.f, 0.f, 0.f};
         Running whole{mine.m, mine.sum, mine.along * kLog2e};
-        whole.raise(over_wave<Largest>(mine.m), a.it * kLog2e);
-        whole.sum = over_wave<Total>(whole.sum);
-        whole.along = over_wave<Total>(whole.along) * kLn2;
+        whole.raise(wave::over<1, wave::Max>(mine.m), a.it * kLog2e);
+        whole.sum = wave::over<1, wave::Sum>(whole.sum);
+        whole.along = wave::over<1, wave::Sum>(whole.along) * kLn2;
         const Row r = row_of(whole);
         if (threadIdx.x == 0) {
             write_row(a, row, r);
@@ -404,19 +420,22 @@ __global__ __launch_bounds__(kJoin) void k_join(Shape s, Plan p, Fwd a) {
         }
         if (s.top > 0) {
             const uint64_t* from = reinterpret_cast<const uint64_t*>(a.ws + p.keys_at) + row * p.segments * s.top;
-            const int n = p.segments * s.top, pieces = (n + kJoin - 1) / kJoin;
-            uint64_t best = 0;
-            for (int q = 0; q < pieces; q++) {
+            const int n = p.segments * s.top;
+            uint64_t key[kJoinKeys], best = 0;
+#pragma unroll
+            for (int q = 0; q < kJoinKeys; q++) {
                 const int i = q * kJoin + threadIdx.x;
-                const uint64_t key = i < n ? from[i] : 0;
-                best = key > best ? key : best;
+                key[q] = i < n ? from[i] : 0;
             }
+#pragma unroll
+            for (int q = 0; q < kJoinKeys; q++) best = key[q] > best ? key[q] : best;
             select_keys<kJoin, Type<T>::kLow>(
-                s.top, best, pieces, lds,
-                [&](int thread, int number, auto f) {
-                    const int i = number * kJoin + thread;
-                    f(i < n ? from[i] : 0);
+                s.top, best, 0, lds,
+                [&](auto f) {
+#pragma unroll
+                    for (int q = 0; q < kJoinKeys; q++) f(key[q]);
                 },
+                [](int, int, auto) {},
                 [&](int rank, uint64_t k) { write_top(s, a, row, r, rank, k); });
             __syncthreads();
         }

@@ -530,7 +530,7 @@ Cut cut_of(bool symmetric, int64_t rows, int64_t cols, int64_t depth, int64_t G)
     };
     // (a tile that mostly hangs over the edges is work for nothing)
     auto full = [&](double share) { return (double)rows * cols >= share * c.side * c.side * c.tiles_i * c.tiles_j; };
-    if (!(tiles(256) >= 200 && full(0.75)) && !(tiles(128) >= 128 && full(0.6))) tiles(64);
+    if (!(tiles(256) >= 200 && full(0.75)) && !(tiles(128) >= (symmetric ? 128 : 192) && full(0.6))) tiles(64);
     // Parts of a sum cost a launch and their way through memory (4 to 12 us): only where they leave 8 (16) steps or more to each,
     // and not where there is a tile for most compute units already.
     const int64_t steps = depth / kDepth, slots = c.tiles * G >= 160 ? 1 : 512 / (c.tiles * G), room = steps / (c.side == 64 ? 8 : 16);
@@ -570,6 +570,7 @@ Plan plan_of(const Shape& s) {
     if (small_plan(s).fits) {
         p.small = true;
         p.launches = 1;
+        p.workspace_bytes = 256;  // (unused: callers of every plan pass one)
         return p;
     }
     p.parts = (int)((s.R * s.K + 16 * kThreads - 1) / (16 * kThreads));

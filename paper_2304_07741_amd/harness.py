@@ -135,7 +135,7 @@ class BlockRunner:
 
 def _check_tensor(name, t, shape, dtype, device):
     """The library takes addresses: what a runner hands on has to be what its plan was compiled for."""
-    if t is None or tuple(t.shape) != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+    if t is None or t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
         got = "None" if t is None else f"{tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}"
         raise ValueError(f"{name}: a contiguous {shape} tensor of {dtype} on {device} is needed, got {got}")
 
@@ -202,26 +202,23 @@ class NormRunner(_PlanRunner):
             if self.gate:
                 self.grads["dgate"] = self._empty(self.shape)
 
-    def _check(self, maps, weights):
-        for name, t in maps.items():
-            _check_tensor(name, t, self.shape, self.tdtype, self.device)
-        for name, t in weights.items():
-            _check_tensor(name, t, self.shape[1:2], torch.float32, self.device)
+    def _map(self, name, t):
+        _check_tensor(name, t, self.shape, self.tdtype, self.device)
 
     def _of_the_block(self, z, gate, w_post, scale, w_pre):
-        maps, weights = {}, {}
+        c = self.shape[1:2]
         if self.post:
-            maps["z"] = z
-            weights |= {"w_post": w_post, "scale": scale}
+            self._map("z", z)
+            _check_tensor("w_post", w_post, c, torch.float32, self.device)
+            _check_tensor("scale", scale, c, torch.float32, self.device)
         if self.gate:
-            maps["gate"] = gate
+            self._map("gate", gate)
         if self.pre:
-            weights["w_pre"] = w_pre
-        self._check(maps, weights)
+            _check_tensor("w_pre", w_pre, c, torch.float32, self.device)
 
     def forward(self, x, z=None, gate=None, w_post=None, scale=None, w_pre=None):
         self._of_the_block(z, gate, w_post, scale, w_pre)
-        self._check({"x": x}, {})
+        self._map("x", x)
         B.canvas_norm_forward(self.handle, x, z, gate, w_post, scale, w_pre, self.out.get("x_out"), self.out.get("u"), self.ws)
         self.x = x
         return self.out
@@ -232,9 +229,10 @@ class NormRunner(_PlanRunner):
         if self.x is None or x_out is not (self.out["x_out"] if self.post else self.x):
             raise ValueError("x_out: not the result of this runner's last forward()")
         self._of_the_block(z, gate, w_post, scale, w_pre)
-        self._check({"du": du} if self.pre else {}, {})
+        if self.pre:
+            self._map("du", du)
         if dx_out is not None or not self.pre:
-            self._check({"dx_out": dx_out}, {})
+            self._map("dx_out", dx_out)
         g = self.grads
         B.canvas_norm_backward(self.handle, self.x, z, gate, w_post, scale, w_pre, dx_out, du, g.get("dx"), g.get("dz"), g.get("dgate"),
                                g.get("dw_post"), g.get("dscale"), g.get("dw_pre"), self.ws)
@@ -262,7 +260,7 @@ class LogprobRunner(_PlanRunner):
 
     def _arguments(self, logits, tokens, mask):
         """(pitch, mask pitch) of tensors that were checked."""
-        if tuple(logits.shape) != (self.rows, self.classes) or logits.dtype != self.tdtype or logits.device != self.device or logits.stride(1) != 1:
+        if logits.shape != (self.rows, self.classes) or logits.dtype is not self.tdtype or logits.device != self.device or logits.stride(1) != 1:
             raise ValueError(f"logits: a {(self.rows, self.classes)} tensor of {self.tdtype} on {self.device} with dense rows is needed")
         _check_tensor("tokens", tokens, (self.rows,), torch.int64, self.device)
         pitch = logits.stride(0) if self.rows > 1 else self.classes
