@@ -510,14 +510,70 @@ __global__ __launch_bounds__(256) void k_add(Shape s, Args args, Product g) {
     emit<32, 32, 256, KIND>(s, args, g, at.grp, at.i0 + bi * 32, at.j0 + bj * 32, at.diagonal, img);
 }
 
+// Symmetric products of few rows: 32 x 32 results per workgroup, the sum over k shared out among its eight waves, which load their
+// operands straight into registers, kAhead steps at a time, and add up through LDS.  A lane takes 32 bytes of a row per step (which
+// k's a lane holds does not matter as long as both operands agree).
+constexpr int kSlimWaves = 8, kAhead = 4;
+template <Kind KIND>
+__global__ __launch_bounds__(64 * kSlimWaves) void k_slim(Shape s, Args args, Product g) {
+    __shared__ f32x4 sums[kSlimWaves][4][64];
+    __shared__ __align__(16) uint32_t img[32 * 32];
+    const Tile at = tile_of<32, 32, KIND>(g, (int)tile::xcd_sequence());
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int ri = at.i0 + (lane & 31), rj = at.j0 + (lane & 31), k0 = (lane >> 5) * 16;
+    const _Float16* pi = g.p.hi + at.grp * g.p.step + (int64_t)(ri < g.rows ? ri : g.rows - 1) * g.p.ld + k0;
+    const _Float16* pj = g.q.hi + at.grp * g.q.step + (int64_t)(rj < g.cols ? rj : g.cols - 1) * g.q.ld + k0;
+    const int all = g.depth / kDepth, begin = all * wave / kSlimWaves, end = all * (wave + 1) / kSlimWaves;
+    f32x16 acc[3] = {};
+    for (int step = begin; step < end; step += kAhead) {
+        half8 a[kAhead][2][2], b[kAhead][2][2];
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            if (step + u >= end) break;
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                const int64_t o = (int64_t)(step + u) * kDepth + k * 8;
+                a[u][k][0] = *reinterpret_cast<const half8*>(pi + o);
+                a[u][k][1] = *reinterpret_cast<const half8*>(pi + o + g.p.plane);
+                b[u][k][0] = *reinterpret_cast<const half8*>(pj + o);
+                b[u][k][1] = *reinterpret_cast<const half8*>(pj + o + g.q.plane);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            if (step + u >= end) break;
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[u][k][1], b[u][k][0], acc[0], 0, 0, 0);
+                acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[u][k][0], b[u][k][1], acc[1], 0, 0, 0);
+                acc[2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[u][k][0], b[u][k][0], acc[2], 0, 0, 0);
+            }
+        }
+    }
+    acc[2] += acc[0] + acc[1];
+#pragma unroll
+    for (int q = 0; q < 4; q++) sums[wave][q][lane] = f32x4{acc[2][4 * q], acc[2][4 * q + 1], acc[2][4 * q + 2], acc[2][4 * q + 3]};
+    __syncthreads();
+    if (wave < 4) {
+        f32x4 v = sums[0][wave][lane];
+#pragma unroll
+        for (int w = 1; w < kSlimWaves; w++) v += sums[w][wave][lane];
+#pragma unroll
+        for (int e = 0; e < 4; e++) img[place<32>(wave * 8 + (lane >> 5) * 4 + e, lane & 31)] = __float_as_uint(v[e]);
+    }
+    __syncthreads();
+    emit<32, 32, 64 * kSlimWaves, KIND>(s, args, g, at.grp, at.i0, at.j0, at.diagonal, img);
+}
+
 uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
 unsigned blocks(int64_t n, int64_t per) { return (unsigned)((n + per - 1) / per); }
 int padded(int64_t n) { return (int)((n + kDepth - 1) / kDepth * kDepth); }
 
 // How a product is cut: sides of the tiles, parts of the sum.
 struct Cut {
-    int side, tiles_i, tiles_j, tiles, splits;
-    bool brief;  // sides of 64: a workgroup on each compute unit at most, each with few steps
+    int side, tiles_i, tiles_j, tiles, splits = 1;
+    bool slim = false;   // sides of 32
+    bool brief = false;  // sides of 64: a workgroup on each compute unit at most, each with few steps
 };
 Cut cut_of(bool symmetric, int64_t rows, int64_t cols, int64_t depth, int64_t G) {
     Cut c;
@@ -531,9 +587,17 @@ Cut cut_of(bool symmetric, int64_t rows, int64_t cols, int64_t depth, int64_t G)
     // (a tile that mostly hangs over the edges is work for nothing)
     auto full = [&](double share) { return (double)rows * cols >= share * c.side * c.side * c.tiles_i * c.tiles_j; };
     if (!(tiles(256) >= 200 && full(0.75)) && !(tiles(128) >= (symmetric ? 128 : 192) && full(0.6))) tiles(64);
+    const int64_t steps = depth / kDepth;
+    // Sides of 32 spread a short sum over more compute units (512 x 512 x 512: 7 us against 10 in parts of 64 x 64), but each reads
+    // so much more per result that a long one takes longer (256 x 256 x 2304: 19 us against 11).
+    if (symmetric && c.side == 64 && steps <= 24) {
+        c.slim = tiles(32) <= 256;
+        if (c.slim) return c;
+        tiles(64);
+    }
     // Parts of a sum cost a launch and their way through memory (4 to 12 us): only where they leave 8 (16) steps or more to each,
     // and not where there is a tile for most compute units already.
-    const int64_t steps = depth / kDepth, slots = c.tiles * G >= 160 ? 1 : 512 / (c.tiles * G), room = steps / (c.side == 64 ? 8 : 16);
+    const int64_t slots = c.tiles * G >= 160 ? 1 : 512 / (c.tiles * G), room = steps / (c.side == 64 ? 8 : 16);
     c.splits = c.side == 256 ? 1 : (int)std::max<int64_t>(1, std::min(slots, room));
     c.brief = c.side == 64 && c.tiles * G * c.splits <= 256 && (steps + c.splits - 1) / c.splits <= Short::SUB;
     return c;
@@ -553,6 +617,12 @@ void product(const Shape& s, const Args& a, Product g, hipStream_t stream) {
     g.tiles_j = c.tiles_j;
     g.tiles = c.tiles;
     g.splits = c.splits;
+    if constexpr (KIND == kGram || KIND == kSquare) {
+        if (c.slim) {
+            CANVAS_LAUNCH(k_slim<KIND>, dim3((unsigned)(g.tiles * s.G)), dim3(64 * kSlimWaves), 0, stream, s, a, g);
+            return;
+        }
+    }
     if (c.side == 256)
         launch<Large, KIND>(s, a, g, stream);
     else if (c.side == 128)
