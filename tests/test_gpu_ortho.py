@@ -116,3 +116,12 @@ def test_in_place_and_on_another_stream(shape):
     torch.cuda.synchronize()
     assert torch.equal(a["master"], w.cpu())
     r.close()
+
+
+@pytest.mark.parametrize("shape", [(4, 1100, 3300), (4, 3300, 1100), (4, 1024, 1500), (300, 100, 90)], ids=lambda s: "x".join(map(str, s)))
+def test_many_tiles(shape):
+    """Tiles of every size, with and without sums in parts; the definition in 64 bits is computed on the GPU."""
+    grad, _, _ = _inputs(shape, 8, "low")
+    d = grad.double().cuda()
+    want = torch.stack([ref.newton_schulz(m, 5) for m in d]).cpu()
+    assert _err(_step(shape, "f32", grad)["update"], want) <= TOL_F32
