@@ -702,7 +702,7 @@ __global__ __launch_bounds__(64 * kSumSlices) void k_sums(Shape s, Bwd a, int pa
     const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6, i = blockIdx.x * 64 + lane, n = 2 * s.C;
     float v = 0.f;
     if (i < n)
-#pragma unroll 8
+#pragma unroll 16
         for (int p = slice; p < partials; p += kSumSlices) v += a.partial[(int64_t)p * n + i];
     buf[slice][lane] = v;
     __syncthreads();
@@ -800,16 +800,18 @@ Plan plan_of(const Shape& s) {
     p.vec = s.P >= v ? v : 2;
     p.pieces = (int)((s.P + p.vec - 1) / p.vec);
     p.total = s.N * p.pieces;
-    // Pieces side by side: as many as make a workgroup's share of a plane's row whole cache lines, fewer where that leaves
-    // compute units idle or a workgroup without room for all channels.
+    // Pieces side by side: as many as make a workgroup's share of a plane's row a cache line, fewer where that leaves compute units
+    // idle or a workgroup without room for all channels.
     const bool held = p.vec == v && s.C <= 1024;
-    p.log_gx = held ? 4 : 3;
+    p.log_gx = 3;
     while (p.log_gx > 1 && ((p.total >> p.log_gx) < 256 || (held && s.C > 4 * (512 >> p.log_gx)))) p.log_gx--;
     p.threads = held && s.C <= 4 * (256 >> p.log_gx) ? 256 : 512;
     const int slots = p.threads >> p.log_gx, need = (s.C + slots - 1) / slots;
     p.kc = !held ? 0 : need > 2 ? 4 : need;
     const int64_t tiles = (p.total + (1 << p.log_gx) - 1) >> p.log_gx;
-    p.partials = (int)std::min<int64_t>(tiles, p.kc ? 512 : 256);
+    // (workgroups that the registers of the held ones leave room for: 64 x 64 x 56 x 56 bf16 takes 50 us with three on a compute
+    // unit, 56 with two; fp32 97 and 90)
+    p.partials = (int)std::min<int64_t>(tiles, !p.kc ? 256 : s.bf16 && p.kc <= 2 && p.threads == 256 ? 768 : 512);
     return p;
 }
 
