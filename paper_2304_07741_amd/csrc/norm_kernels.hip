@@ -696,14 +696,22 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_bwd(Shape s, Bwd
 
 // ---------------------------------------------------------------- sums of the weights' gradients
 
-constexpr int kSumSlices = 16;
+constexpr int kSumSlices = 16, kTogether = 16;
 __global__ __launch_bounds__(64 * kSumSlices) void k_sums(Shape s, Bwd a, int partials) {
     __shared__ float buf[kSumSlices][64];
     const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6, i = blockIdx.x * 64 + lane, n = 2 * s.C;
     float v = 0.f;
     if (i < n)
-#pragma unroll 16
-        for (int p = slice; p < partials; p += kSumSlices) v += a.partial[(int64_t)p * n + i];
+        for (int first = slice; first < partials; first += kSumSlices * kTogether) {
+            float w[kTogether];  // (all asked for before the first is added)
+#pragma unroll
+            for (int u = 0; u < kTogether; u++) {
+                const int p = first + u * kSumSlices;
+                w[u] = p < partials ? a.partial[(int64_t)p * n + i] : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < kTogether; u++) v += w[u];
+        }
     buf[slice][lane] = v;
     __syncthreads();
     if (slice || i >= n) return;
