@@ -85,11 +85,11 @@ __device__ __forceinline__ Where where_of(const Shape& s, int pieces, int64_t to
     if (!w.in) q = total - 1;
     const int64_t n = (uint64_t)q < 0x80000000ull ? (int64_t)((uint32_t)q / (uint32_t)pieces) : q / pieces;
     const int g = (int)(q - n * pieces);
-    int p = g * VEC;
+    int64_t p = (int64_t)g * VEC;
     w.skip = 0;
     if (p + VEC > s.P) {
         w.skip = (int)(p + VEC - s.P);
-        p = (int)(s.P - VEC);
+        p = s.P - VEC;
     }
     w.pixel = n * s.P + p;
     w.base = n * s.C * s.P + p;

@@ -205,22 +205,18 @@ struct Tile {
     int grp, i0, j0;
     bool diagonal;
 };
-// A way of cutting products: tiles of BM x BN by WI x WJ waves, SUB times kDepth summands at a time in BUFFERS buffers; with sums
-// in parts or not.
-template <int BM_, int BN_, int WI_, int WJ_, int SUB_, int BUFFERS_, bool SPLITS_>
+// A way of cutting products: tiles of BM x BN by WI x WJ waves, SUB times kDepth summands at a time.
+template <int BM_, int BN_, int WI_, int WJ_, int SUB_>
 struct Form {
-    static constexpr int BM = BM_, BN = BN_, WI = WI_, WJ = WJ_, SUB = SUB_, kBuffers = BUFFERS_;
-    static constexpr bool kSplits = SPLITS_;
+    static constexpr int BM = BM_, BN = BN_, WI = WI_, WJ = WJ_, SUB = SUB_;
     static constexpr int kThreads = 64 * WI * WJ, TM = BM / WI / 32, TN = BN / WJ / 32;
     static constexpr int kOpA = BM * 64, kOpB = BN * 64;  // bytes of one plane of kDepth summands
     static constexpr int kPart = 2 * (kOpA + kOpB), kStage = SUB * kPart;
     static constexpr int kRows = BM * BN * 4 > kStage ? kStage / (BN * 4) : BM;  // of results that one buffer takes at once
 };
-using Large = Form<256, 256, 2, 4, 1, 2, false>;
-using Middle = Form<128, 128, 2, 2, 1, 2, true>;
-using Small = Form<64, 64, 2, 2, 2, 2, true>;
-// Few workgroups with little to add up each: all of it is asked for at once.
-using Short = Form<64, 64, 2, 2, 8, 1, true>;
+using Large = Form<256, 256, 2, 4, 1>;
+using Middle = Form<128, 128, 2, 2, 1>;
+using Small = Form<64, 64, 2, 2, 2>;
 
 template <int BM, int BN, Kind KIND>
 __device__ __forceinline__ Tile tile_of(const Product& g, int task) {
@@ -334,7 +330,7 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Shape s, Args args, Pro
     constexpr int kOpA = F::kOpA, kOpB = F::kOpB, kPart = F::kPart, kStage = F::kStage;
     constexpr int kTimesA = BM * 4 / kThreads, kTimesB = BN * 4 / kThreads;  // 16-byte pieces of a thread in a plane
     // (two arrays, not one: the compiler has to see that loads into the one do not concern reads of the other)
-    __shared__ __align__(16) unsigned char first_buffer[kStage], second_buffer[F::kBuffers == 2 ? kStage : 16];
+    __shared__ __align__(16) unsigned char first_buffer[kStage], second_buffer[kStage];
 
     const unsigned seq = tile::xcd_sequence();
     const int task = seq / g.splits, split = seq - task * g.splits;
@@ -411,52 +407,36 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Shape s, Args args, Pro
     };
     constexpr int kUnits = 2 * SUB;
     Operands o[2];
-    if (F::kBuffers == 1) {
-        for (int step = begin; step < end; step += SUB) {
-            load(step, first_buffer);
-            loads_arrived();
-            read(first_buffer, 0, o[0]);
+    // One stage, `now` its buffer: each unit's products run while the next one's operands are read; before the last unit
+    // everybody has read this buffer and the next stage has arrived, so the one behind that is asked for.
+    auto stage = [&](int step, unsigned char* now, unsigned char* next) {
 #pragma unroll
-            for (int unit = 0; unit < kUnits; unit++) {
-                if (unit + 1 < kUnits) read(first_buffer, unit + 1, o[(unit + 1) & 1]);  // (of no use behind the end, but in the buffer)
-                __builtin_amdgcn_sched_barrier(0);
-                if (step + unit / 2 < end) multiply(o[unit & 1]);
-                __builtin_amdgcn_sched_barrier(0);
+        for (int unit = 0; unit < kUnits; unit++) {
+            if (unit + 1 < kUnits) {
+                read(now, unit + 1, o[(unit + 1) & 1]);
+            } else {
+                loads_arrived();
+                load(step + 2 * SUB, now);
+                read(next, 0, o[0]);
             }
-            __syncthreads();
+            __builtin_amdgcn_sched_barrier(0);
+            if (step + unit / 2 < end) multiply(o[unit & 1]);
+            __builtin_amdgcn_sched_barrier(0);
         }
-    } else {
-        // One stage, `now` its buffer: each unit's products run while the next one's operands are read; before the last unit
-        // everybody has read this buffer and the next stage has arrived, so the one behind that is asked for.
-        auto stage = [&](int step, unsigned char* now, unsigned char* next) {
-#pragma unroll
-            for (int unit = 0; unit < kUnits; unit++) {
-                if (unit + 1 < kUnits) {
-                    read(now, unit + 1, o[(unit + 1) & 1]);
-                } else {
-                    loads_arrived();
-                    load(step + 2 * SUB, now);
-                    read(next, 0, o[0]);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-                if (step + unit / 2 < end) multiply(o[unit & 1]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        };
-        load(begin, first_buffer);
-        load(begin + SUB, second_buffer);
-        loads_arrived();
-        read(first_buffer, 0, o[0]);
-        for (int step = begin; step < end; step += 2 * SUB) {
-            stage(step, first_buffer, second_buffer);
-            if (step + SUB >= end) break;
-            stage(step + SUB, second_buffer, first_buffer);
-        }
-        loads_arrived();
+    };
+    load(begin, first_buffer);
+    load(begin + SUB, second_buffer);
+    loads_arrived();
+    read(first_buffer, 0, o[0]);
+    for (int step = begin; step < end; step += 2 * SUB) {
+        stage(step, first_buffer, second_buffer);
+        if (step + SUB >= end) break;
+        stage(step + SUB, second_buffer, first_buffer);
     }
+    loads_arrived();
     if (kChains == 3) acc[0][0] += apart[0] + apart[kChains / 2];
 
-    if (g.splits == 1) {
+    if (!(KIND == kGram || KIND == kSquare) || g.splits == 1) {
         uint32_t* img = reinterpret_cast<uint32_t*>(first_buffer);
 #pragma unroll 1
         for (int r0 = 0; r0 < BM; r0 += F::kRows) {
@@ -569,12 +549,17 @@ uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
 unsigned blocks(int64_t n, int64_t per) { return (unsigned)((n + per - 1) / per); }
 int padded(int64_t n) { return (int)((n + kDepth - 1) / kDepth * kDepth); }
 
-// How a product is cut: sides of the tiles, parts of the sum.
+// How a product is cut.
 struct Cut {
-    int side, tiles_i, tiles_j, tiles, splits = 1;
-    bool slim = false;   // sides of 32
-    bool brief = false;  // sides of 64: a workgroup on each compute unit at most, each with few steps
+    int side = 0, tiles_i = 0, tiles_j = 0, tiles = 0;  // of the tiles; 32: k_slim
+    int splits = 1;                                     // parts of the sum
 };
+// Measured with every other way forced, us of one product; "128 in 3" is a side and the parts of the sum:
+//   rows x summands, symmetric:   512 x 512         32: 7, 64 in 4: 10            256 x 2304    64 in 12: 10, 32: 19, 128 in 8: 14
+//                                 512 x 4608        64 in 8: 16, 128 in 8: 21     1024 x 4096   128 in 6: 36, 64 in 2: 39
+//                                 1536 x 6144       128 in 3: 69, 64 in 1: 100    2048 x 8192   256 in 7: 118, 128 in 3: 133
+//   rows x columns x summands:    512 x 4608 x 512  64: 20, 128: 21, 256: 43      1024 x 4096 x 1024   128: 40, 64: 45, 256: 73
+//                                 1536 x 6144 x 1536   256: 105, 128: 120         2048 x 8192 x 2048   256: 187, 128: 230
 Cut cut_of(bool symmetric, int64_t rows, int64_t cols, int64_t depth, int64_t G) {
     Cut c;
     auto tiles = [&](int side) {
@@ -586,39 +571,46 @@ Cut cut_of(bool symmetric, int64_t rows, int64_t cols, int64_t depth, int64_t G)
     };
     // (a tile that mostly hangs over the edges is work for nothing)
     auto full = [&](double share) { return (double)rows * cols >= share * c.side * c.side * c.tiles_i * c.tiles_j; };
-    if (!(tiles(256) >= 200 && full(0.75)) && !(tiles(128) >= (symmetric ? 128 : 192) && full(0.6))) tiles(64);
     const int64_t steps = depth / kDepth;
-    // Sides of 32 spread a short sum over more compute units (512 x 512 x 512: 7 us against 10 in parts of 64 x 64), but each reads
-    // so much more per result that a long one takes longer (256 x 256 x 2304: 19 us against 11).
-    if (symmetric && c.side == 64 && steps <= 24) {
-        c.slim = tiles(32) <= 256;
-        if (c.slim) return c;
-        tiles(64);
+    if (!symmetric) {
+        // the larger side as soon as it gives more than half of the compute units a tile
+        if (!(tiles(256) >= 140 && full(0.75)) && !(tiles(128) >= 192 && full(0.6))) tiles(64);
+        return c;
     }
-    // Parts of a sum cost a launch and their way through memory (4 to 12 us): only where they leave 8 (16) steps or more to each,
-    // and not where there is a tile for most compute units already.
-    const int64_t slots = c.tiles * G >= 160 ? 1 : 512 / (c.tiles * G), room = steps / (c.side == 64 ? 8 : 16);
-    c.splits = c.side == 256 ? 1 : (int)std::max<int64_t>(1, std::min(slots, room));
-    c.brief = c.side == 64 && c.tiles * G * c.splits <= 256 && (steps + c.splits - 1) / c.splits <= Short::SUB;
+    if (steps <= 24 && tiles(32) <= 256) return c;  // short sums: as many compute units as there are blocks of 32
+    int64_t t = tiles(256);
+    if (full(0.75) && (t >= 200 || (t >= 25 && steps >= 192))) {
+        c.splits = t >= 128 ? 1 : (int)(256 / t);
+        return c;
+    }
+    // Parts of a sum cost a launch and their way through memory (4 us and more): as many as give every compute unit one.
+    t = tiles(128);
+    if (full(0.6) && t * steps >= 3500) {
+        c.splits = (int)std::max<int64_t>(1, std::min(t > 128 ? 512 / t : 256 / t, steps / 16));
+        return c;
+    }
+    t = tiles(64);
+    c.splits = (int)std::max<int64_t>(1, std::min<int64_t>(280 / t, steps / 6));
     return c;
 }
 
 template <class F, Kind KIND>
 void launch(const Shape& s, const Args& a, const Product& g, hipStream_t stream) {
     CANVAS_LAUNCH((k_product<F, KIND>), dim3((unsigned)(g.tiles * g.splits * s.G)), dim3(F::kThreads), 0, stream, s, a, g);
-    if constexpr (F::kSplits) {
+    if constexpr (KIND == kGram || KIND == kSquare) {
         if (g.splits > 1) CANVAS_LAUNCH((k_add<F, KIND>), dim3((unsigned)(g.tiles * s.G) * (F::BM / 32 * (F::BN / 32))), dim3(256), 0, stream, s, a, g);
     }
 }
 template <Kind KIND>
 void product(const Shape& s, const Args& a, Product g, hipStream_t stream) {
-    const Cut c = cut_of(KIND == kGram || KIND == kSquare, g.rows, g.cols, g.depth, s.G);
+    constexpr bool kSymmetric = KIND == kGram || KIND == kSquare;
+    const Cut c = cut_of(kSymmetric, g.rows, g.cols, g.depth, s.G);
     g.tiles_i = c.tiles_i;
     g.tiles_j = c.tiles_j;
     g.tiles = c.tiles;
     g.splits = c.splits;
-    if constexpr (KIND == kGram || KIND == kSquare) {
-        if (c.slim) {
+    if constexpr (kSymmetric) {
+        if (c.side == 32) {
             CANVAS_LAUNCH(k_slim<KIND>, dim3((unsigned)(g.tiles * s.G)), dim3(64 * kSlimWaves), 0, stream, s, a, g);
             return;
         }
@@ -627,8 +619,6 @@ void product(const Shape& s, const Args& a, Product g, hipStream_t stream) {
         launch<Large, KIND>(s, a, g, stream);
     else if (c.side == 128)
         launch<Middle, KIND>(s, a, g, stream);
-    else if (c.brief)
-        launch<Short, KIND>(s, a, g, stream);
     else
         launch<Small, KIND>(s, a, g, stream);
 }
@@ -649,10 +639,9 @@ Plan plan_of(const Shape& s) {
     p.workspace_bytes = up256(8ull * s.G * p.parts);
     if (!s.steps) return p;
     const Cut gram = cut_of(true, s.m, s.m, padded(s.n), s.G), square = cut_of(true, s.m, s.m, padded(s.m), s.G);
-    const Cut update = cut_of(false, s.m, s.n, padded(s.m), s.G), last = s.tall ? cut_of(false, s.n, s.m, padded(s.m), s.G) : update;
-    for (const Cut& c : {gram, square, update, last})
+    for (const Cut& c : {gram, square})
         if (c.splits > 1) p.part_bytes = std::max<uint64_t>(p.part_bytes, 4ull * c.side * c.side * c.tiles * c.splits * s.G);
-    p.launches += s.steps * (1 + (gram.splits > 1) + 1 + (square.splits > 1)) + (s.steps - 1) * (1 + (update.splits > 1)) + 1 + (last.splits > 1);
+    p.launches += s.steps * (3 + (gram.splits > 1) + (square.splits > 1));
     p.workspace_bytes += 2 * up256(4ull * s.G * s.m * padded(s.n)) + 2 * up256(4ull * s.G * s.n * padded(s.m)) + 2 * up256(4ull * s.G * s.m * padded(s.m)) + up256(p.part_bytes);
     return p;
 }
