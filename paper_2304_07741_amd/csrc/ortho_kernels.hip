@@ -554,12 +554,12 @@ struct Cut {
     int side = 0, tiles_i = 0, tiles_j = 0, tiles = 0;  // of the tiles; 32: k_slim
     int splits = 1;                                     // parts of the sum
 };
-// Measured with every other way forced, us of one product; "128 in 3" is a side and the parts of the sum:
-//   rows x summands, symmetric:   512 x 512         32: 7, 64 in 4: 10            256 x 2304    64 in 12: 10, 32: 19, 128 in 8: 14
-//                                 512 x 4608        64 in 8: 16, 128 in 8: 21     1024 x 4096   128 in 6: 36, 64 in 2: 39
-//                                 1536 x 6144       128 in 3: 69, 64 in 1: 100    2048 x 8192   256 in 7: 118, 128 in 3: 133
-//   rows x columns x summands:    512 x 4608 x 512  64: 20, 128: 21, 256: 43      1024 x 4096 x 1024   128: 40, 64: 45, 256: 73
-//                                 1536 x 6144 x 1536   256: 105, 128: 120         2048 x 8192 x 2048   256: 187, 128: 230
+// Measured with the ways forced, us of one product; "128 in 3" is a side and the parts of the sum:
+//   rows x summands, symmetric:   512 x 512      32: 7, 64 in 4: 10          256 x 2304    64 in 12: 9, 128 in 8: 13, 32: 19
+//                                 512 x 4608     64 in 7: 17, 128 in 8: 21   1024 x 4096   128 in 7: 28, 64 in 2: 31
+//                                 1536 x 6144    128 in 3: 69, 64: 100       2048 x 8192   256 in 7: 118, 128 in 3: 133
+//   rows x columns x summands:    512 x 4608 x 512     64: 20, 128: 21, 256: 43   1024 x 4096 x 1024   128: 38, 64: 42, 256: 71
+//                                 1536 x 6144 x 1536   256: 115, 128: 130         2048 x 8192 x 2048   256: 190, 128: 233
 Cut cut_of(bool symmetric, int64_t rows, int64_t cols, int64_t depth, int64_t G) {
     Cut c;
     auto tiles = [&](int side) {

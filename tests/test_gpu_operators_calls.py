@@ -1,0 +1,136 @@
+"""How the operators around a block are called: recorded into graphs, on several streams at once, with tensors that do not fit."""
+import pytest
+import torch
+
+from paper_2304_07741_amd import binding as B
+from paper_2304_07741_amd import harness
+
+pytestmark = pytest.mark.gpu
+
+BOTH = B.CANVAS_NORM_POST | B.CANVAS_NORM_PRE
+
+
+def _norm_case(shape, dtype):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    x, z, g, dy, du = (torch.randn(*shape, generator=gen, device="cuda").to(dt) for _ in range(5))
+    w = [torch.randn(shape[1], generator=gen, device="cuda") for _ in range(3)]
+    r = harness.NormRunner(shape, dtype, BOTH, gate=B.CANVAS_GATE_SILU)
+
+    def run():
+        out = r.forward(x, z, g, *w)
+        return {**out, **r.backward(out["x_out"], z, g, *w, dx_out=dy, du=du)}
+
+    return r, [x, z, g, dy, du], run
+
+
+def _logprob_case(rows, classes, dtype, top):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(4)
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    logits = (torch.randn(rows, classes, generator=gen, device="cuda") * 3).to(dt)
+    tokens = torch.randint(0, classes, (rows,), generator=gen, device="cuda")
+    d = torch.randn(rows, generator=gen, device="cuda")
+    r = harness.LogprobRunner(rows, classes, dtype, top_k=top)
+
+    def run():
+        return {**r.forward(logits, tokens), **r.backward(logits, tokens, d, d)}
+
+    return r, [logits], run
+
+
+def _ortho_case(shape, dtype):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(5)
+    grad, momentum, master = (torch.randn(*shape, generator=gen, device="cuda") for _ in range(3))
+    r = harness.OrthoRunner(shape, dtype)
+    return r, [grad], lambda: r.step(grad, momentum, master, mu=0.9, lr=0.02)
+
+
+CASES = [lambda: _norm_case((4, 96, 14, 14), "bf16"), lambda: _norm_case((300, 200, 1, 1), "f32"), lambda: _norm_case((2, 9000, 1, 1), "bf16"),
+         lambda: _norm_case((2, 1500, 3, 5), "bf16"), lambda: _logprob_case(3, 70000, "bf16", 7), lambda: _logprob_case(200, 500, "f32", 0),
+         lambda: _ortho_case((3, 24, 40), "f32"), lambda: _ortho_case((1, 200, 700), "bf16"), lambda: _ortho_case((2, 520, 300), "f32")]
+NAMES = ["norm_map", "norm_rows", "norm_long_rows", "norm_many_channels", "logprob_split", "logprob_rows", "ortho_small", "ortho_parts", "ortho_tall"]
+
+
+@pytest.mark.parametrize("case", CASES, ids=NAMES)
+def test_recorded_into_a_graph(case):
+    """Every replay gives what the eager call gives on the inputs of that moment, other work on the GPU in between."""
+    r, inputs, run = case()
+    run()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        run()                                     # (as the capture will run)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run()
+    for k in range(4):
+        for t in inputs:
+            t.copy_(torch.roll(t, 1, -1))
+        want = {k: v.clone() for k, v in run().items()}
+        for t in out.values():
+            t.fill_(-1)
+        r.ws.fill_(0xFF)
+        torch.randn(1 << 20, device="cuda").sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        for name, v in want.items():
+            assert torch.equal(v, out[name]), (k, name)
+    r.close()
+
+
+def test_two_plans_on_two_streams():
+    """Calls that overlap on the GPU, a workspace each, give what they give alone."""
+    cases = [_ortho_case((1, 300, 900), "f32"), _ortho_case((1, 300, 900), "f32")]
+    alone = [{k: v.clone() for k, v in run().items()} for _, _, run in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(5):
+        for (_, _, run), s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                out = run()
+    torch.cuda.synchronize()
+    for (r, _, _), want in zip(cases, alone):
+        for k, v in want.items():
+            assert torch.equal(v, r.out[k]), k
+        r.close()
+
+
+def test_runners_refuse_tensors_that_do_not_fit():
+    shape = (2, 16, 4, 4)
+    r = harness.NormRunner(shape, "bf16", BOTH, gate=B.CANVAS_GATE_SIGMOID)
+    m = torch.zeros(shape, dtype=torch.bfloat16, device="cuda")
+    w = torch.zeros(16, device="cuda")
+    good = dict(x=m, z=m, gate=m, w_post=w, scale=w, w_pre=w)
+    out = r.forward(**good)
+    for name, bad in [("x", m.float()), ("x", m[:1]), ("z", m.transpose(2, 3)), ("gate", None), ("w_post", w.bfloat16()), ("scale", w[:8]), ("w_pre", w.cpu()),
+                      ("x", m.to(memory_format=torch.channels_last)[:, :, :, ::1].transpose(1, 2))]:
+        with pytest.raises(ValueError):
+            r.forward(**{**good, name: bad})
+    block = dict(z=m, gate=m, w_post=w, scale=w, w_pre=w)
+    with pytest.raises(ValueError):
+        r.backward(m, **block, du=m)              # not what forward() returned
+    with pytest.raises(ValueError):
+        r.backward(out["x_out"], **block, du=None)
+    r.close()
+    lp = harness.LogprobRunner(3, 10, "f32")
+    logits, tokens = torch.zeros(3, 10, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
+    lp.forward(logits, tokens)
+    for args in [(logits.bfloat16(), tokens), (logits[:, :9], tokens), (logits.T.contiguous().T, tokens), (logits, tokens.int()), (logits, tokens[:2])]:
+        with pytest.raises(ValueError):
+            lp.forward(*args)
+    for mask in (torch.ones(3, 9, dtype=torch.bool, device="cuda"), torch.ones(3, 10, device="cuda"), torch.ones(10, 3, dtype=torch.bool, device="cuda").T):
+        with pytest.raises(ValueError):
+            lp.forward(logits, tokens, mask=mask)
+    with pytest.raises(ValueError):
+        lp.backward(logits, tokens, torch.zeros(3, dtype=torch.float64, device="cuda"))
+    lp.close()
+    o = harness.OrthoRunner((1, 8, 12), "f32")
+    grad = torch.zeros(1, 8, 12, device="cuda")
+    for args in [(grad.double(),), (grad[0],), (grad.transpose(1, 2),), (grad, grad.bfloat16()), (grad, None, grad.cpu())]:
+        with pytest.raises(ValueError):
+            o.step(*args)
+    o.close()
