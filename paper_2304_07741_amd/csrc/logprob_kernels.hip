@@ -386,9 +386,13 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_fwd(Shape s, 
             uint64_t* keys = reinterpret_cast<uint64_t*>(a.ws + p.keys_at) + task * s.top;
             auto own_keys = [&](auto f) {
 #pragma unroll
-                for (int e = 0; e < V; e++) f(key_of(order_of(Y::at(v[0], e)), (uint32_t)begin + tid * V + e));
+                for (int q = 0; q < kSweep; q++) {
+                    if (q * THREADS >= vectors) break;
+#pragma unroll
+                    for (int e = 0; e < V; e++) f(key_of(order_of(Y::at(v[q], e)), (uint32_t)begin + (q * THREADS + tid) * V + e));
+                }
             };
-            select_keys<THREADS, Y::kLow>(s.top, best, pieces == 1 ? 0 : pieces, lds, own_keys, piece, [&](int rank, uint64_t key) {
+            select_keys<THREADS, Y::kLow>(s.top, best, pieces <= kSweep ? 0 : pieces, lds, own_keys, piece, [&](int rank, uint64_t key) {
                 if (p.segments == 1)
                     write_top(s, a, row, whole, rank, key);
                 else
@@ -539,8 +543,9 @@ Plan plan_of(const Shape& s) {
     // With alternatives a segment is as long as the list in LDS allows: k times a thread's classes, 48 KB.
     const int64_t most = s.top ? (int64_t)256 * (kListKeys / s.top / vec * vec) : s.classes;
     int64_t n = (s.classes + most - 1) / most;
-    // A few rows leave most compute units idle: segments of 2048 classes or more until there are about as many as those.
-    if (s.rows * n < 256) {
+    // A few rows leave most compute units idle: segments of 2048 classes or more until there are about as many as those.  (131072
+    // classes in 64 segments and their join take 15.5 us, in 16 of them 17; 8000 take 11 in three and 6 in one.)
+    if (s.rows * n < 256 && s.classes > 12288) {
         const int64_t want = 256 / s.rows, some = s.classes / 2048;
         n = std::max(n, std::min(want, some));
     }
