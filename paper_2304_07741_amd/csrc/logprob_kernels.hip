@@ -543,9 +543,10 @@ Plan plan_of(const Shape& s) {
     // With alternatives a segment is as long as the list in LDS allows: k times a thread's classes, 48 KB.
     const int64_t most = s.top ? (int64_t)256 * (kListKeys / s.top / vec * vec) : s.classes;
     int64_t n = (s.classes + most - 1) / most;
-    // A few rows leave most compute units idle: segments of 2048 classes or more until there are about as many as those.  (131072
-    // classes in 64 segments and their join take 15.5 us, in 16 of them 17; 8000 take 11 in three and 6 in one.)
-    if (s.rows * n < 256 && s.classes > 12288) {
+    // A few rows leave most compute units idle: segments of 2048 classes or more until there are about as many as those.  (Four rows
+    // of 131072 classes in 64 segments and their join take 15.5 us, in 16 of them 17; of 49152 classes 14 against 10 unsplit,
+    // and with a mask 13 against 17.)
+    if (s.rows * n < 256 && s.classes > 40960) {
         const int64_t want = 256 / s.rows, some = s.classes / 2048;
         n = std::max(n, std::min(want, some));
     }
