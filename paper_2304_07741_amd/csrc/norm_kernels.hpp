@@ -42,6 +42,9 @@ struct Bwd {
 
 void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream);
 void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream);
+// Everything but the sums over the partials.
+void maps_backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream);
+void rows_backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream);
 
 }  // namespace norm
 }  // namespace canvas
