@@ -102,6 +102,10 @@ __device__ __forceinline__ void over_channels(float (&v)[VEC], int gx, int GX, f
 #pragma unroll
         for (int e = 0; e < VEC; e++) v[e] = wave::step<2, wave::Sum>(v[e]);
     }
+    if (GX <= 1) {
+#pragma unroll
+        for (int e = 0; e < VEC; e++) v[e] = wave::step<1, wave::Sum>(v[e]);
+    }
     const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, row = GX * VEC;
     __syncthreads();
     if ((int)(threadIdx.x & 63) < GX) {
@@ -127,6 +131,7 @@ __device__ __forceinline__ void each_channel(int cy, int CY, int C, F f) {
             if (c < C) f(k, c);
         }
     } else {
+#pragma unroll 4
         for (int c = cy; c < C; c += CY) f(0, c);
     }
 }

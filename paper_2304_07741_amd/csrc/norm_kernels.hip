@@ -273,10 +273,13 @@ Plan plan_of(const Shape& s) {
     p.pieces = (int)((s.P + p.vec - 1) / p.vec);
     p.total = s.N * p.pieces;
     // Pieces side by side: as many as make a workgroup's share of a plane's row a cache line, fewer where that leaves compute units
-    // idle or a workgroup without room for all channels.
-    const bool held = p.vec == v && s.C <= 1024;
+    // idle or a workgroup without room for all channels (32 x 2048 x 7 x 7, one piece and all channels held: forward 17, backward
+    // 30 us; two pieces and channels read again: 35 and 75).  One piece alone, where two fill half of the compute units, loses
+    // if the channels are held (16 x 256 x 14 x 14 backward 13 us, with two 12) and gains if not (64 x 4096 x 7 x 7: 71 + 157 us,
+    // with two 87 + 168).
+    const bool held = p.vec == v && s.C <= 2048;
     p.log_gx = 3;
-    while (p.log_gx > 1 && ((p.total >> p.log_gx) < 256 || (held && s.C > 4 * (512 >> p.log_gx)))) p.log_gx--;
+    while (p.log_gx > 0 && ((p.total >> p.log_gx) < (p.log_gx > 1 || !held ? 256 : 128) || (held && s.C > 4 * (512 >> p.log_gx)))) p.log_gx--;
     p.threads = held && s.C <= 4 * (256 >> p.log_gx) ? 256 : 512;
     const int slots = p.threads >> p.log_gx, need = (s.C + slots - 1) / slots;
     p.kc = !held ? 0 : need > 2 ? 4 : need;

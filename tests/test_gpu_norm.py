@@ -165,3 +165,15 @@ def test_gradient_against_differences_of_the_kernel():
         pair = [loss(m, weights) if src is maps else loss(maps, m) for m in (up, down)]
         want, have = (pair[0] - pair[1]) / (2 * h), float((g * d.double()).sum())
         assert abs(want - have) <= 5e-3 * abs(have) + 5e-3, (name, want, have)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 1025, 3, 3), (2, 1500, 7, 7), (40, 2047, 3, 5), (70, 1030, 2, 13), (1, 2049, 7, 7), (33, 256, 7, 7)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_one_piece_of_a_plane_at_a_time(shape, dtype):
+    """Many channels or few pixels: a workgroup holds all channels of one piece, or reads them again; with more pieces than workgroups."""
+    for parts, gate in PLANS[:1] + PLANS[2:3]:
+        maps, weights = _case(shape, dtype, parts, gate, seed=sum(shape))
+        want = _reference(shape, maps, weights, gate, True)
+        for k, g in _run(shape, dtype, parts, gate, maps, weights).items():
+            assert_close(g.reshape(want[k].shape), want[k], TOL[dtype], f"{shape} {dtype} {k}")
