@@ -10,7 +10,8 @@
  *
  * The products run on the matrix units with fp32 sums.  Each operand is a pair of fp16 numbers that together hold 22 bits of
  * it, and a product adds the three pairings that matter, which is as exact as products in fp32 (|X| <= 1.3 throughout, so a
- * fixed scale keeps both numbers in range).  The sum of squares is kept in 64 bits: gradients of any size that fp32 holds are
+ * fixed scale keeps both numbers in range).  Where the longer side is several times the shorter one, two steps are joined, which
+ * changes the order of the products and not what they are: both polynomials of A are multiplied before X is.  The sum of squares is kept in 64 bits: gradients of any size that fp32 holds are
  * in range.  A matrix of zeros gives zeros; infinities and NaN make their own matrix NaN and no other.
  *
  * Pointers: device pointers, owned by the caller, 16-byte aligned, contiguous [G, R, K].  All functions return a
@@ -36,7 +37,7 @@ typedef struct canvas_ortho_info {
     int32_t n_launches;       /* kernels enqueued per call */
     int32_t reserved0;
     uint64_t workspace_bytes;
-    double flops;             /* of the products, each symmetric one on one side of its diagonal only */
+    double flops;             /* of the products as they are written above, each symmetric one on one side of its diagonal only */
     double min_bytes;         /* gradient read, update written; momentum read and written; without master weights */
 } canvas_ortho_info;
 

@@ -9,6 +9,10 @@
 //   A = X X^T   (tiles on and below the diagonal, written on both sides of it)
 //   B = a I + b A + c A A^T  (the same)
 //   X = B X     (from the rows of B and of X^T; both X and X^T are written, or, in the last step, the outputs)
+// Where the longer side is much longer, two steps at a time: with B0 and B1 polynomials of A, all these matrices commute, so
+// A1 = B0 A B0 is the second step's A, and X = (B1 B0) X.  Three short symmetric products take the place of two long ones, one of
+// them symmetric.  Rounding leaves the same error as step by step (what is wrong with B moves X by as much of X, also where X is
+// weak); three steps at a time would leave two to three times that.
 #include "ortho_kernels.hpp"
 
 #include <algorithm>
@@ -546,6 +550,10 @@ __global__ __launch_bounds__(64 * kSlimWaves) void k_slim(Shape s, Args args, Pr
 }
 
 uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
+// Whether two steps are taken at a time.  Measured, us of five steps one by one and so:
+//   2048 x 8192   1766, 1437    1536 x 6144   999, 822    1024 x 4096   411, 377    512 x 4608   225, 200    256 x 2304   128, 122
+//   2048 x 4096   1143, 1063    1536 x 3000   651, 603    1024 x 2048   297, 308    512 x 2048   160, 160    256 x 512    104, 108
+bool by_twos(const Shape& s) { return s.n >= (s.m > 1024 ? 2 : 4) * s.m; }
 unsigned blocks(int64_t n, int64_t per) { return (unsigned)((n + per - 1) / per); }
 int padded(int64_t n) { return (int)((n + kDepth - 1) / kDepth * kDepth); }
 
@@ -641,8 +649,9 @@ Plan plan_of(const Shape& s) {
     const Cut gram = cut_of(true, s.m, s.m, padded(s.n), s.G), square = cut_of(true, s.m, s.m, padded(s.m), s.G);
     for (const Cut& c : {gram, square})
         if (c.splits > 1) p.part_bytes = std::max<uint64_t>(p.part_bytes, 4ull * c.side * c.side * c.tiles * c.splits * s.G);
-    p.launches += s.steps * (3 + (gram.splits > 1) + (square.splits > 1));
-    p.workspace_bytes += 2 * up256(4ull * s.G * s.m * padded(s.n)) + 2 * up256(4ull * s.G * s.n * padded(s.m)) + 2 * up256(4ull * s.G * s.m * padded(s.m)) + up256(p.part_bytes);
+    const int twos = by_twos(s) ? s.steps / 2 : 0, ones = s.steps - twos;
+    p.launches += ones * (2 + (gram.splits > 1)) + (ones + 4 * twos) * (1 + (square.splits > 1));
+    p.workspace_bytes += 2 * up256(4ull * s.G * s.m * padded(s.n)) + 2 * up256(4ull * s.G * s.n * padded(s.m)) + 3 * up256(4ull * s.G * s.m * padded(s.m)) + up256(p.part_bytes);
     return p;
 }
 
@@ -670,19 +679,31 @@ void step(const Shape& s, const Plan& p, const Args& a, hipStream_t stream) {
         CANVAS_LAUNCH(k_normalised, dim3(blocks(s.R * s.K, kThreads), G), dim3(kThreads), 0, stream, s, a, sums, p.parts);
         return;
     }
-    Pair x[2] = {pair(s.m, s.n), pair(s.m, s.n)}, xt[2] = {pair(s.n, s.m), pair(s.n, s.m)}, q = pair(s.m, s.m), b = pair(s.m, s.m);
+    Pair x[2] = {pair(s.m, s.n), pair(s.m, s.n)}, xt[2] = {pair(s.n, s.m), pair(s.n, s.m)}, q = pair(s.m, s.m), b = pair(s.m, s.m), t = pair(s.m, s.m);
     CANVAS_LAUNCH(k_start, dim3(blocks(s.K, 64) * blocks(s.R, 64), G), dim3(kThreads), 0, stream, s, a, sums, p.parts, x[0], xt[0]);
     const int m = (int)s.m, n = (int)s.n;
-    for (int k = 0; k < s.steps; k++) {
-        const Pair &from = x[k & 1], &from_t = xt[k & 1], &to = x[~k & 1], &to_t = xt[~k & 1];
+    // C = P Q of symmetric matrices that commute
+    auto both = [&](const Pair& p, const Pair& q, const Pair& c) { product<kGram>(s, a, Product{p, q, m, m, p.ld, c, c, 0, 0, 0, 0, parts}, stream); };
+    auto polynomial = [&](const Pair& q, const Pair& b) { product<kSquare>(s, a, Product{q, q, m, m, q.ld, b, b, 0, 0, 0, 0, parts}, stream); };
+    for (int k = 0, at = 0; k < s.steps; k++, at ^= 1) {
+        const Pair &from = x[at], &from_t = xt[at], &to = x[at ^ 1], &to_t = xt[at ^ 1];
         product<kGram>(s, a, Product{from, from, m, m, from.ld, q, q, 0, 0, 0, 0, parts}, stream);
-        product<kSquare>(s, a, Product{q, q, m, m, q.ld, b, b, 0, 0, 0, 0, parts}, stream);
+        polynomial(q, b);
+        Pair left = b;
+        if (by_twos(s) && k + 1 < s.steps) {
+            both(b, q, t);
+            both(t, b, q);  // the second step's A
+            polynomial(q, t);
+            both(t, b, q);
+            left = q;
+            k++;
+        }
         if (k + 1 < s.steps)
-            product<kUpdate>(s, a, Product{b, from_t, m, n, b.ld, to, to_t, 0, 0, 0, 0, parts}, stream);
+            product<kUpdate>(s, a, Product{left, from_t, m, n, left.ld, to, to_t, 0, 0, 0, 0, parts}, stream);
         else if (s.tall)
-            product<kLast>(s, a, Product{from_t, b, n, m, b.ld, to, to_t, 0, 0, 0, 0, parts}, stream);
+            product<kLast>(s, a, Product{from_t, left, n, m, left.ld, to, to_t, 0, 0, 0, 0, parts}, stream);
         else
-            product<kLast>(s, a, Product{b, from_t, m, n, b.ld, to, to_t, 0, 0, 0, 0, parts}, stream);
+            product<kLast>(s, a, Product{left, from_t, m, n, left.ld, to, to_t, 0, 0, 0, 0, parts}, stream);
     }
 }
 

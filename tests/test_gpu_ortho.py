@@ -125,3 +125,13 @@ def test_many_tiles(shape):
     d = grad.double().cuda()
     want = torch.stack([ref.newton_schulz(m, 5) for m in d]).cpu()
     assert _err(_step(shape, "f32", grad)["update"], want) <= TOL_F32
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 5])
+@pytest.mark.parametrize("shape", [(1, 100, 450), (2, 500, 90), (3, 65, 1031)], ids=lambda s: "x".join(map(str, s)))
+def test_two_steps_at_a_time(shape, steps):
+    """One side several times the other: pairs of steps are joined, and an odd one is left at the end."""
+    for kind in ("noise", "low"):
+        grad, _, _ = _inputs(shape, 9 + steps, kind)
+        want = ref.ortho_step(grad.double(), None, 0, False, steps)
+        assert _err(_step(shape, "f32", grad, steps=steps)["update"], want["update"]) <= TOL_F32
