@@ -80,6 +80,12 @@ __device__ __forceinline__ uint64_t mask_bytes(const uint8_t* mask, int i, int e
     return w;
 }
 __device__ __forceinline__ bool allowed(uint64_t w, int e) { return ((e < 4 ? (uint32_t)w : (uint32_t)(w >> 32)) >> ((e & 3) * 8)) & 0xffu; }
+template <class T>
+__device__ __forceinline__ void hide_masked(u32x4& v, uint64_t w) {
+#pragma unroll
+    for (int e = 0; e < Type<T>::kVec; e++)
+        if (!allowed(w, e)) Type<T>::hide(v, e);
+}
 
 // Vector number `at` of `end` logits; -inf behind them and where the mask hides them.
 template <class T>
@@ -95,10 +101,7 @@ __device__ __forceinline__ u32x4 load_vector(const T* z, int at, int end, const 
     else
         v = V == 4 ? u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u} : u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u};
     if (mask && i < end) {
-        const uint64_t w = mask_bytes<V>(mask, i, end);
-#pragma unroll
-        for (int e = 0; e < V; e++)
-            if (!allowed(w, e)) Y::hide(v, e);
+        hide_masked<T>(v, mask_bytes<V>(mask, i, end));
     }
     return v;
 }
@@ -315,9 +318,16 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_fwd(Shape s, 
         int best_at = tid;
         u32x4 v[kSweep];
         for (int at = 0; at < vectors; at += kSweep * THREADS) {
-            if ((at + kSweep * THREADS) * V <= end && !mask) {
+            if ((at + kSweep * THREADS) * V <= end) {
 #pragma unroll
                 for (int q = 0; q < kSweep; q++) __builtin_memcpy(&v[q], z + (at + q * THREADS + tid) * V, 16);
+                if (mask) {
+                    uint64_t w[kSweep] = {};
+#pragma unroll
+                    for (int q = 0; q < kSweep; q++) __builtin_memcpy(&w[q], mask + (at + q * THREADS + tid) * V, V);
+#pragma unroll
+                    for (int q = 0; q < kSweep; q++) hide_masked<T>(v[q], w[q]);
+                }
             } else {
 #pragma unroll
                 for (int q = 0; q < kSweep; q++) v[q] = load_vector(z, at + q * THREADS + tid, end, mask);
