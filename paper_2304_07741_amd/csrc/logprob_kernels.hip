@@ -290,22 +290,23 @@ __device__ __forceinline__ void write_top(const Shape& s, const Fwd& a, int64_t 
     a.top_logprob[row * s.top + rank] = key ? (value_of((uint32_t)(key >> 32)) - r.most) * a.it - r.log_sum : -kInf;
 }
 
-// One segment of `length` classes per workgroup of THREADS threads, or, with a wave per segment, four of them; kSweep vectors of a
-// thread in flight.
+// One segment of `length` classes per workgroup of THREADS threads, or, with a wave per segment and nothing to select, four of them;
+// kSweep vectors of a thread in flight.
 constexpr int kSweep = 4;
+constexpr int segments_of(int threads, bool top) { return threads == 64 && !top ? 4 : 1; }
 template <class T, int THREADS, bool TOP>
-__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_fwd(Shape s, Plan p, Fwd a) {
+__global__ __launch_bounds__(THREADS * segments_of(THREADS, TOP)) void k_fwd(Shape s, Plan p, Fwd a) {
     using Y = Type<T>;
     constexpr int V = Y::kVec;
     extern __shared__ uint64_t lds[];
     __shared__ float most[4];
     __shared__ float2 sums[4];
     const int tid = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
-    const int64_t tasks = s.rows * p.segments, per = THREADS == 64 ? 4 : 1;
+    const int64_t tasks = s.rows * p.segments, per = segments_of(THREADS, TOP);
     const float scale = a.it * kLog2e;
     for (int64_t first = (int64_t)blockIdx.x * per; first < tasks; first += (int64_t)gridDim.x * per) {
-        const int64_t task = first + (THREADS == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
-        if (THREADS == 64 && task >= tasks) break;  // (a wave of its own: no barriers on this path)
+        const int64_t task = first + (per > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
+        if (per > 1 && task >= tasks) break;  // (a wave of its own: no barriers on this path)
         const int64_t row = p.segments == 1 ? task : task / p.segments;
         const int64_t begin = (task - row * p.segments) * p.length;
         const int end = (int)(p.length < s.classes - begin ? p.length : s.classes - begin);
@@ -409,7 +410,7 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_fwd(Shape s, 
                     keys[rank] = key;
             });
         }
-        if (THREADS > 64) __syncthreads();  // (the buffers above are free again)
+        if (TOP || THREADS > 64) __syncthreads();  // (the buffers above are free again)
     }
 }
 
@@ -525,12 +526,13 @@ template <class T, int THREADS, bool TOP>
 void fwd(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
     const int64_t tasks = s.rows * p.segments;
     const size_t lds = TOP ? 8ull * (THREADS + kTogether + s.top * classes_per_thread(p.length, THREADS, Type<T>::kVec)) : 0;
-    CANVAS_LAUNCH((k_fwd<T, THREADS, TOP>), dim3(grid_of(THREADS == 64 ? (tasks + 3) / 4 : tasks)), dim3(THREADS == 64 ? 256 : THREADS), lds, stream, s, p, a);
+    constexpr int per = segments_of(THREADS, TOP);
+    CANVAS_LAUNCH((k_fwd<T, THREADS, TOP>), dim3(grid_of((tasks + per - 1) / per)), dim3(THREADS * per), lds, stream, s, p, a);
 }
 template <class T>
 void forward_of(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
     if (p.threads == 64)
-        fwd<T, 64, false>(s, p, a, stream);
+        s.top ? fwd<T, 64, true>(s, p, a, stream) : fwd<T, 64, false>(s, p, a, stream);
     else
         s.top ? fwd<T, 256, true>(s, p, a, stream) : fwd<T, 256, false>(s, p, a, stream);
     if (p.segments > 1) {
@@ -563,7 +565,10 @@ Plan plan_of(const Shape& s) {
     n = std::min<int64_t>(n, kMaxSegments);
     p.length = ((s.classes + n - 1) / n + vec - 1) / vec * vec;
     p.segments = (int)((s.classes + p.length - 1) / p.length);
-    p.threads = !s.top && p.length <= 64 * vec * kSweep ? 64 : 256;
+    // A wave holds a short row.  It selects alternatives as long as half of its threads bound them (4000 x 1000 in bf16, with five 11 us,
+    // with 256 threads 26; with 32 12 and 30; 64, in fp32, 499 and 25), and segments have the compute units to themselves (four
+    // rows of 131072, masked: 16.3 and 15.6 us).
+    p.threads = p.length <= 64 * vec * kSweep && (!s.top || (s.top <= 32 && p.segments == 1)) ? 64 : 256;
     const uint64_t tasks = (uint64_t)s.rows * p.segments;
     p.workspace_bytes = up256((uint64_t)s.rows * sizeof(Row));
     if (p.segments > 1) {

@@ -239,3 +239,25 @@ def test_offsets_beyond_32_bits():
     grad = ref.logprob_backward(vals.double(), 1.0, None, tokens, dlp.double(), None)
     _same(logits.cpu(), grad, 2.0 ** -8, 1e-3, "dlogits")
     r.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [1, 5, 31, 32, 33])
+@pytest.mark.parametrize("classes", [3, 31, 64, 700, 1024, 1025, 2048, 2049])
+def test_alternatives_of_short_rows(classes, top, dtype):
+    """Rows that a wave or a workgroup holds: ties, orders, infinities and NaN, with and without a mask."""
+    top = min(top, classes)
+    wide, tokens, mask, _, dlp, dent = _case(12, classes, 1, dtype, True, classes + top, 1.0)
+    wide[0] = 0.25
+    wide[1] = torch.arange(classes + 1).flip(0).to(wide.dtype)
+    wide[2] = torch.arange(classes + 1).to(wide.dtype)
+    wide[3] = (torch.arange(classes + 1) % 7).to(wide.dtype)
+    wide[5, ::3] = -math.inf
+    wide[6] = -math.inf
+    wide[7, classes // 2] = math.nan
+    wide[8, -2] = math.inf
+    for m in (None, mask):
+        want = ref.logprob_forward(wide[:, :classes].double(), 1.0, m, tokens, top)
+        got = _run(wide, classes, dtype, tokens, m, 1.0, dlp, dent, top)
+        grad = ref.logprob_backward(wide[:, :classes].double(), 1.0, m, tokens, dlp.double(), dent.double())
+        _check(got, want, grad, dtype, dlp, dent, classes, 1.0)
