@@ -212,8 +212,9 @@ __global__ __launch_bounds__(64 * kSumSlices) void k_sums(Shape s, Bwd a, int pa
 
 template <class T, int VEC, int KC, int PARTS>
 void maps(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
-    const int64_t tiles = (p.total + (1 << p.log_gx) - 1) >> p.log_gx;
-    CANVAS_LAUNCH((k_maps_fwd<T, VEC, KC, PARTS>), dim3((unsigned)tiles), dim3(p.threads), p.threads / 64 * (1 << p.log_gx) * VEC * 4, stream, s, a, p.log_gx,
+    const Tiling& t = p.fwd;
+    const int64_t tiles = (p.total + (1 << t.log_gx) - 1) >> t.log_gx;
+    CANVAS_LAUNCH((k_maps_fwd<T, VEC, KC, PARTS>), dim3((unsigned)tiles), dim3(t.threads), t.threads / 64 * (1 << t.log_gx) * VEC * 4, stream, s, a, t.log_gx,
                   p.pieces, p.total);
 }
 template <class T, int TPR, int KV, int PARTS>
@@ -236,7 +237,7 @@ void run(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
         }
     }
     if (p.vec == 2) return maps<T, 2, 0, PARTS>(s, p, a, stream);
-    switch (p.kc) {
+    switch (p.fwd.kc) {
     case 1: return maps<T, V, 1, PARTS>(s, p, a, stream);
     case 2: return maps<T, V, 2, PARTS>(s, p, a, stream);
     case 4: return maps<T, V, 4, PARTS>(s, p, a, stream);
@@ -272,21 +273,31 @@ Plan plan_of(const Shape& s) {
     p.vec = s.P >= v ? v : 2;
     p.pieces = (int)((s.P + p.vec - 1) / p.vec);
     p.total = s.N * p.pieces;
+    const bool held = p.vec == v && s.C <= 2048;
     // Pieces side by side: as many as make a workgroup's share of a plane's row a cache line, fewer where that leaves compute units
     // idle or a workgroup without room for all channels (32 x 2048 x 7 x 7, one piece and all channels held: forward 17, backward
     // 30 us; two pieces and channels read again: 35 and 75).  One piece alone, where two fill half of the compute units, loses
     // if the channels are held (16 x 256 x 14 x 14 backward 13 us, with two 12) and gains if not (64 x 4096 x 7 x 7: 71 + 157 us,
-    // with two 87 + 168).
-    const bool held = p.vec == v && s.C <= 2048;
-    p.log_gx = 3;
-    while (p.log_gx > 0 && ((p.total >> p.log_gx) < (p.log_gx > 1 || !held ? 256 : 128) || (held && s.C > 4 * (512 >> p.log_gx)))) p.log_gx--;
-    p.threads = held && s.C <= 4 * (256 >> p.log_gx) ? 256 : 512;
-    const int slots = p.threads >> p.log_gx, need = (s.C + slots - 1) / slots;
-    p.kc = !held ? 0 : need > 2 ? 4 : need;
-    const int64_t tiles = (p.total + (1 << p.log_gx) - 1) >> p.log_gx;
+    // with two 87 + 168).  Down to four pieces, rather fewer of them than more than `rather` channels of a thread.
+    auto tiling = [&](int rather) {
+        Tiling t;
+        t.log_gx = 3;
+        while (t.log_gx > 0 && ((p.total >> t.log_gx) < (t.log_gx > 1 || !held ? 256 : 128) || (held && s.C > 4 * (512 >> t.log_gx)))) t.log_gx--;
+        while (held && t.log_gx > 2 && s.C > rather * (256 >> t.log_gx)) t.log_gx--;
+        t.threads = held && s.C <= 4 * (256 >> t.log_gx) ? 256 : 512;
+        const int slots = t.threads >> t.log_gx, need = (s.C + slots - 1) / slots;
+        t.kc = !held ? 0 : need > 2 ? 4 : need;
+        return t;
+    };
+    // Forward: 256 threads are better than 512 (64 x 256 x 28 x 28 bf16 28 us, 32; 64 x 160 x 28 x 28 21, 25), eight pieces better than
+    // four with half the channels (64 x 72 x 56 x 56 31 us, 35).  Backward: two channels leave registers for three waves per SIMD
+    // (64 x 128 x 28 x 28 bf16 31 us, 38; 64 x 256 x 28 x 28 56, 74; 128 x 256 x 14 x 14 fp32 48, 57).
+    p.fwd = tiling(4);
+    p.bwd = tiling(2);
+    const int64_t tiles = (p.total + (1 << p.bwd.log_gx) - 1) >> p.bwd.log_gx;
     // (workgroups that the registers of the held ones leave room for: 64 x 64 x 56 x 56 bf16 takes 47 us with three on a compute
     // unit, 51 with two; fp32 95 and 87)
-    p.partials = (int)std::min<int64_t>(tiles, !p.kc ? 256 : s.bf16 && p.kc <= 2 && p.threads == 256 ? 768 : 512);
+    p.partials = (int)std::min<int64_t>(tiles, !held ? 256 : s.bf16 && p.bwd.kc <= 2 && p.bwd.threads == 256 ? 768 : 512);
     return p;
 }
 

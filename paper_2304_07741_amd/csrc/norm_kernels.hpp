@@ -15,12 +15,17 @@ struct Shape {
     float eps = 0.f;
 };
 
+// How maps are cut: pieces side by side in a workgroup, its threads, channels that a thread holds.
+struct Tiling {
+    int log_gx = 0, threads = 0, kc = 0;
+};
 // Which kernels a shape takes.
 struct Plan {
-    int tpr = 0, kv = 0;                                   // rows: threads per row, 16-byte accesses of a thread (0: maps)
-    int vec = 0, log_gx = 0, threads = 0, kc = 0, pieces = 0;  // maps: pixels of a thread, pieces side by side, channels held
-    int64_t total = 0;                                     // pieces of all planes
-    int partials = 0;                                      // workgroups of the backward kernel
+    int tpr = 0, kv = 0;      // rows: threads per row, 16-byte accesses of a thread (0: maps)
+    int vec = 0, pieces = 0;  // maps: pixels of a thread, pieces of a plane
+    int64_t total = 0;        // of all planes
+    Tiling fwd, bwd;
+    int partials = 0;         // workgroups of the backward kernel
 };
 Plan plan_of(const Shape& s);
 

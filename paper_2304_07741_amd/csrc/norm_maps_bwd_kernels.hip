@@ -7,8 +7,8 @@
 // Bound by memory: eight maps move (five read, three written).  Some 50 operations per element are left beside them, which take
 // about as long where 8 pixels of bf16 lie in 16 bytes, so what only depends on the pixel is multiplied per pixel, and the gate's
 // kind is a constant of the kernel.  With the sums over the partials: 64 x 64 x 56 x 56 in 46 us bf16 (4.4 TB/s) and 87 us fp32
-// (4.7 TB/s), 128 x 256 x 14 x 14 in 40 us (2.6 TB/s), 128 x 512 x 7 x 7 in 25 us (2.1 TB/s): four channels per thread leave two
-// waves per SIMD, and the short planes' pieces overlap (56 pixels read for 49).
+// (4.7 TB/s), 64 x 256 x 28 x 28 in 56 us (3.7 TB/s), 128 x 256 x 14 x 14 in 39 us (2.6 TB/s), 128 x 512 x 7 x 7 in 24 us (2.1 TB/s): four
+// channels per thread leave two waves per SIMD, and the short planes' pieces overlap (56 pixels read for 49).
 #include <atomic>
 
 #include "launch.hpp"
@@ -176,18 +176,19 @@ __global__ __launch_bounds__(512, KC == 2 ? 3 : 1) void k_maps_bwd(Shape s, Bwd 
 
 template <class T, int VEC, int KC, int PARTS, int GATE>
 void maps(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
-    const int lds = p.threads / 64 * (1 << p.log_gx) * VEC * 4 + (KC ? 0 : 8 * s.C);
+    const Tiling& t = p.bwd;
+    const int lds = t.threads / 64 * (1 << t.log_gx) * VEC * 4 + (KC ? 0 : 8 * s.C);
     if (lds > 65536) {
         static std::atomic<uint64_t> asked{0};
         allow_lds(asked, reinterpret_cast<const void*>(&k_maps_bwd<T, VEC, KC, PARTS, GATE>), lds);
     }
-    CANVAS_LAUNCH((k_maps_bwd<T, VEC, KC, PARTS, GATE>), dim3(p.partials), dim3(p.threads), lds, stream, s, a, p.log_gx, p.pieces, p.total);
+    CANVAS_LAUNCH((k_maps_bwd<T, VEC, KC, PARTS, GATE>), dim3(p.partials), dim3(t.threads), lds, stream, s, a, t.log_gx, p.pieces, p.total);
 }
 template <class T, int PARTS, int GATE>
 void run(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
     constexpr int V = 16 / sizeof(T);
     if (p.vec == 2) return maps<T, 2, 0, PARTS, GATE>(s, p, a, stream);
-    switch (p.kc) {
+    switch (p.bwd.kc) {
     case 1: return maps<T, V, 1, PARTS, GATE>(s, p, a, stream);
     case 2: return maps<T, V, 2, PARTS, GATE>(s, p, a, stream);
     case 4: return maps<T, V, 4, PARTS, GATE>(s, p, a, stream);
