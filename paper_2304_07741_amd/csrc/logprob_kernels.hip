@@ -6,7 +6,7 @@
 //
 // Alternatives: classes are ordered by whole numbers of 64 bits (order_of the logit, then the complement of the index), all
 // different.  Every thread finds its best class on the way; the k-th best of the threads' best is a lower bound for the k-th
-// best of all, and only the k threads whose best reaches it can hold classes that do: at most k times a thread's classes, few
+// best of all, and only the threads whose best reaches it, k or few more, can hold classes that do: at most as many times a thread's classes, few
 // in general.  Theirs are read again, spread over the workgroup; what reaches the bound is collected in LDS and ranked by
 // counting.
 //
@@ -146,14 +146,15 @@ __device__ __forceinline__ void sums_of_row(float& a, float& b, float2* buf) {
 }
 
 constexpr int kTogether = 8;  // keys compared at a time: the list has as many places more
+constexpr int kSpare = 8;     // threads more than k that may reach the bound: the search for it ends the earlier, and seldom has to tell ties apart
 // The k largest of the keys that the THREADS threads of the workgroup hold, in descending order to `put(rank, key)`, 0 past the
 // last one.  best: this thread's largest key; LOW: bits of the order that are the same in all keys of one order.  own(f) calls f
 // for each of the thread's keys if they are at hand (pieces = 0); else they fall into `pieces`, and piece(thread, number, f)
-// calls f for each key of one.  lds: THREADS keys, then k times the keys of a thread and kTogether.
+// calls f for each key of one.  lds: THREADS keys, then k + kSpare times the keys of a thread and kTogether.
 template <int THREADS, int LOW, class OWN, class PIECE, class PUT>
 __device__ void select_keys(int k, uint64_t best, int pieces, uint64_t* lds, OWN own, PIECE piece, PUT put) {
     __shared__ uint64_t s_bound;
-    __shared__ uint32_t s_count, s_holders, s_holder[64];  // (at most k threads reach the bound)
+    __shared__ uint32_t s_count, s_holders, s_holder[64 + kSpare];  // (at most k + kSpare threads reach the bound)
     uint64_t* list = lds + THREADS;
     lds[threadIdx.x] = best;
     if (threadIdx.x == 0) s_count = s_holders = 0;
@@ -173,12 +174,14 @@ __device__ void select_keys(int k, uint64_t best, int pieces, uint64_t* lds, OWN
             for (int e = 0; e < kEach; e++) n += __popcll(__ballot(pred(o[e], low[e])));
             return n;
         };
-        uint64_t bound = 1;  // (of k threads or fewer that hold anything: everything)
-        if (count([](uint32_t x, uint32_t) { return x != 0; }) > k) {
-            // the largest t that k threads or more reach, bit by bit; then, of those that equal it, the lower indices
+        // (each one more is read again, or, in a wave, ranked by the few)
+        const int spare = pieces || THREADS == 64 ? 2 : kSpare;
+        uint64_t bound = 1;  // (of so few threads that hold anything: everything)
+        if (count([](uint32_t x, uint32_t) { return x != 0; }) > k + spare) {
+            // a t that k threads or few more reach, bit by bit; where too many equal it, the lower indices among those
             uint32_t t = 0;
             int n = THREADS;
-            for (int bit = 31; bit >= LOW && n != k; bit--) {
+            for (int bit = 31; bit >= LOW && n > k + spare; bit--) {
                 const uint32_t c = t | 1u << bit;
                 const int m = count([=](uint32_t x, uint32_t) { return x >= c; });
                 if (m >= k) {
@@ -187,11 +190,11 @@ __device__ void select_keys(int k, uint64_t best, int pieces, uint64_t* lds, OWN
                 }
             }
             uint32_t l = 0;
-            if (n > k) {
+            if (n > k + spare) {
                 const int r = k - count([=](uint32_t x, uint32_t) { return x >> LOW > t >> LOW; });
                 n = THREADS;
                 l = ~(kMostClasses - 1u);
-                for (int bit = kMostClassesLog - 1; bit >= 0 && n != r; bit--) {
+                for (int bit = kMostClassesLog - 1; bit >= 0 && n > r + spare; bit--) {
                     const uint32_t c = l | 1u << bit;
                     const int m = count([=](uint32_t x, uint32_t y) { return x >> LOW == t >> LOW && y >= c; });
                     if (m >= r) {
@@ -414,7 +417,7 @@ __global__ __launch_bounds__(THREADS * segments_of(THREADS, TOP)) void k_fwd(Sha
     }
 }
 
-// Joins the segments of a row: at most kMaxSegments of them (with the most alternatives 43 hold the most classes).
+// Joins the segments of a row: at most kMaxSegments of them (with the most alternatives 52 hold the most classes).
 constexpr int kListKeys = 6144;  // places of the list of candidates
 constexpr int kMaxSegments = 64, kJoinKeys = kMaxSegments * 64 / kJoin;
 template <class T>
@@ -525,7 +528,7 @@ int64_t classes_per_thread(int64_t length, int threads, int vec) { return (lengt
 template <class T, int THREADS, bool TOP>
 void fwd(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
     const int64_t tasks = s.rows * p.segments;
-    const size_t lds = TOP ? 8ull * (THREADS + kTogether + s.top * classes_per_thread(p.length, THREADS, Type<T>::kVec)) : 0;
+    const size_t lds = TOP ? 8ull * (THREADS + kTogether + (s.top + kSpare) * classes_per_thread(p.length, THREADS, Type<T>::kVec)) : 0;
     constexpr int per = segments_of(THREADS, TOP);
     CANVAS_LAUNCH((k_fwd<T, THREADS, TOP>), dim3(grid_of((tasks + per - 1) / per)), dim3(THREADS * per), lds, stream, s, p, a);
 }
@@ -536,7 +539,7 @@ void forward_of(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream)
     else
         s.top ? fwd<T, 256, true>(s, p, a, stream) : fwd<T, 256, false>(s, p, a, stream);
     if (p.segments > 1) {
-        const size_t lds = s.top ? 8ull * (kJoin + kTogether + s.top * kJoinKeys) : 0;
+        const size_t lds = s.top ? 8ull * (kJoin + kTogether + (s.top + kSpare) * kJoinKeys) : 0;
         CANVAS_LAUNCH(k_join<T>, dim3(grid_of(s.rows)), dim3(kJoin), lds, stream, s, p, a);
     }
 }
@@ -552,8 +555,8 @@ void backward_of(const Shape& s, const Bwd& a, hipStream_t stream) {
 Plan plan_of(const Shape& s) {
     Plan p;
     const int vec = s.bf16 ? 8 : 4;
-    // With alternatives a segment is as long as the list in LDS allows: k times a thread's classes, 48 KB.
-    const int64_t most = s.top ? (int64_t)256 * (kListKeys / s.top / vec * vec) : s.classes;
+    // With alternatives a segment is as long as the list in LDS allows: k + kSpare times a thread's classes, 48 KB.
+    const int64_t most = s.top ? (int64_t)256 * (kListKeys / (s.top + kSpare) / vec * vec) : s.classes;
     int64_t n = (s.classes + most - 1) / most;
     // A few rows leave most compute units idle: segments of 2048 classes or more until there are about as many as those.  (Four rows
     // of 131072 classes in 64 segments and their join take 15.5 us, in 16 of them 17; of 49152 classes 14 against 10 unsplit,
