@@ -6,11 +6,15 @@
 //
 // Alternatives: classes are ordered by whole numbers of 64 bits (order_of the logit, then the complement of the index), all
 // different.  Every thread finds its best class on the way; the k-th best of the threads' best is a lower bound for the k-th
-// best of all, and only the threads whose best reaches it, k or few more, can hold classes that do: at most as many times a thread's classes, few
-// in general.  Theirs are read again, spread over the workgroup; what reaches the bound is collected in LDS and ranked by
-// counting.
+// best of all, and only the threads whose best reaches it, k or few more, can hold classes that do: at most as many times a
+// thread's classes, few in general.  Theirs are read again, spread over the workgroup; what reaches the bound is collected in
+// LDS and ranked by counting.
 //
 // Backward: element by element from the row's (m, log S, entropy).
+//
+// Both are bound by memory on many rows: 4096 x 32768 in bf16 forward 44 us (6.0 TB/s, some of it from the last-level cache),
+// backward 111 us (4.8 TB/s).  With alternatives the search at a row's end is not hidden by other rows' loads: 1500 x 50021
+// with five of them takes 43 us, without 32.  Few rows are bound by latency: 256 x 1000 4 us per launch.
 #include "logprob_kernels.hpp"
 
 #include <algorithm>
@@ -559,8 +563,8 @@ Plan plan_of(const Shape& s) {
     const int64_t most = s.top ? (int64_t)256 * (kListKeys / (s.top + kSpare) / vec * vec) : s.classes;
     int64_t n = (s.classes + most - 1) / most;
     // A few rows leave most compute units idle: segments of 2048 classes or more until there are about as many as those.  (Four rows
-    // of 131072 classes in 64 segments and their join take 15.5 us, in 16 of them 17; of 49152 classes 14 against 10 unsplit,
-    // and with a mask 13 against 17.)
+    // of 131072 classes with 20 alternatives in 64 segments and their join take 12.8 us, in 16 of them 15.8, unsplit 17.9; of 40960
+    // classes 12.3, with a mask 12.9, unsplit 10.9 and 14.3.)
     if (s.rows * n < 256 && s.classes > 40960) {
         const int64_t want = 256 / s.rows, some = s.classes / 2048;
         n = std::max(n, std::min(want, some));

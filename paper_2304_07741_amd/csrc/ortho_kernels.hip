@@ -1,8 +1,8 @@
 // Newton-Schulz products of the orthogonalised update.
 //
-// A matrix of fp32 values v is held as two fp16 planes: hi = fp16(2^12 v), lo = fp16(2^12 v - hi).  |X| <= 1.3 and |b A + c A A + a I| <= 4
-// in every step (spectral norms bound the elements), so hi stays below 2^14, and lo keeps 11 more bits of every element above
-// 2^-15 of the largest possible one.  A product of two such matrices is hi hi + hi lo + lo hi on the matrix units with fp32
+// A matrix of fp32 values v is held as two fp16 planes: hi = fp16(2^12 v), lo = fp16(2^12 v - hi).  |X| <= 1.3 and |b A + c A A + a I| <= 3.45
+// in every step and the product of two of the latter below 12 (spectral norms bound the elements), so hi stays in fp16's range, and lo
+// keeps 11 more bits of every element above 2^-15 of the largest possible one.  A product of two such matrices is hi hi + hi lo + lo hi on the matrix units with fp32
 // sums; lo lo is below 2^-22 of a term.
 //
 // Per step, with both X [m][n] and its transpose at hand so that every operand is read along the index that is summed over:
@@ -13,6 +13,10 @@
 // A1 = B0 A B0 is the second step's A, and X = (B1 B0) X.  Three short symmetric products take the place of two long ones, one of
 // them symmetric.  Rounding leaves the same error as step by step (what is wrong with B moves X by as much of X, also where X is
 // weak); three steps at a time would leave two to three times that.
+//
+// Large matrices are bound by the matrix units, small ones by the launches that wait for each other.  2048 x 8192: the long products
+// take 190 us each (1080 TFLOP/s of fp16 products; a plain 8192 x 8192 x 8192 one of the library reaches 1145), Gram matrices 104 + 14 for the sums of their
+// parts, short products 37 + 10 (730 TFLOP/s), momentum and splitting 86; five steps 1437 us.  256 x 2304: 22 launches of 4-8 us, 119-122 us.
 #include "ortho_kernels.hpp"
 
 #include <algorithm>
@@ -189,7 +193,7 @@ __global__ __launch_bounds__(kThreads) void k_normalised(Shape s, Args a, const 
     finish_one(s, a, i, (float)(direction(s, a, i, a.momentum ? a.momentum_out[i] : 0.f) * inv));
 }
 
-enum Kind { kGram, kSquare, kUpdate, kLast };
+enum Kind { kGram, kSquare, kUpdate, kLast };  // kGram: all symmetric products that nothing is added to
 
 // C[i][j] = sum_k P[i][k] Q[j][k], rows of P x rows of Q, over `depth` (a multiple of kDepth, zeros at its end).
 struct Product {

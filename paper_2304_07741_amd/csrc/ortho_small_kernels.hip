@@ -3,6 +3,9 @@
 //
 // Rows of X are padded to a multiple of 16 floats plus 4 and those of A and B likewise, so that both the reads of 16 rows (16 bytes
 // each, operands that are summed along the rows) and those of 4 x 16 elements of a column block fall on different banks.
+//
+// Bound by latency: three dependent products per step, each of reads from LDS, a few matrix instructions and a barrier.  Eight of
+// 8 x 72, five steps: 13 us, of which the launch is 4 (17 launches of the kernels for large matrices: 68 us).
 #include "ortho_small_kernels.hpp"
 
 #include <atomic>
