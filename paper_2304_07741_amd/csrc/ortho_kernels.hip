@@ -557,7 +557,8 @@ uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
 // Whether two steps are taken at a time.  Measured, us of five steps one by one and so:
 //   2048 x 8192   1766, 1437    1536 x 6144   999, 822    1024 x 4096   411, 377    512 x 4608   225, 200    256 x 2304   128, 122
 //   2048 x 4096   1143, 1063    1536 x 3000   651, 603    1024 x 2048   297, 308    512 x 2048   160, 160    256 x 512    104, 108
-bool by_twos(const Shape& s) { return s.n >= (s.m > 1024 ? 2 : 4) * s.m; }
+//   two of 512 x 2048   206, 211    two of 420 x 4741   320, 262    eight of 256 x 2304   237, 203
+bool by_twos(const Shape& s) { return s.n >= (s.m > 1024 ? 2 : s.m > 512 ? 4 : 5) * s.m; }
 unsigned blocks(int64_t n, int64_t per) { return (unsigned)((n + per - 1) / per); }
 int padded(int64_t n) { return (int)((n + kDepth - 1) / kDepth * kDepth); }
 
