@@ -298,8 +298,9 @@ Plan plan_of(const Shape& s) {
     p.bwd = tiling(2);
     const int64_t tiles = (p.total + (1 << p.bwd.log_gx) - 1) >> p.bwd.log_gx;
     // (workgroups that the registers of the held ones leave room for: 64 x 64 x 56 x 56 bf16 takes 47 us with three on a compute
-    // unit, 51 with two; fp32 95 and 87)
-    p.partials = (int)std::min<int64_t>(tiles, !held ? 256 : s.bf16 && p.bwd.kc <= 2 && p.bwd.threads == 256 ? 768 : 512);
+    // unit, 51 with two; fp32 95 and 87.  Channels that are read again: two on a compute unit push each other's out of the cache,
+    // 64 x 4096 x 7 x 7 fp32 450 us, with one 372; two pixels at a time 1000 x 2048 x 2 x 3 127 and 154)
+    p.partials = (int)std::min<int64_t>(tiles, !held && p.vec > 2 ? 256 : s.bf16 && held && p.bwd.kc <= 2 && p.bwd.threads == 256 ? 768 : 512);
     return p;
 }
 
