@@ -91,6 +91,11 @@ __device__ __forceinline__ void hide_masked(u32x4& v, uint64_t w) {
         if (!allowed(w, e)) Type<T>::hide(v, e);
 }
 
+template <int V>
+__device__ __forceinline__ u32x4 nothing() {
+    return V == 4 ? u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u} : u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u};
+}
+
 // Vector number `at` of `end` logits; -inf behind them and where the mask hides them.
 template <class T>
 __device__ __forceinline__ u32x4 load_vector(const T* z, int at, int end, const uint8_t* mask) {
@@ -103,7 +108,7 @@ __device__ __forceinline__ u32x4 load_vector(const T* z, int at, int end, const 
     else if (i < end)
         v = last_logits(z, i, end);
     else
-        v = V == 4 ? u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u} : u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u};
+        v = nothing<V>();
     if (mask && i < end) {
         hide_masked<T>(v, mask_bytes<V>(mask, i, end));
     }
@@ -337,8 +342,29 @@ __global__ __launch_bounds__(THREADS * segments_of(THREADS, TOP)) void k_fwd(Sha
                     for (int q = 0; q < kSweep; q++) hide_masked<T>(v[q], w[q]);
                 }
             } else {
+                uint64_t w[kSweep];
 #pragma unroll
-                for (int q = 0; q < kSweep; q++) v[q] = load_vector(z, at + q * THREADS + tid, end, mask);
+                for (int q = 0; q < kSweep; q++) {
+                    const int i = (at + q * THREADS + tid) * V;
+                    v[q] = nothing<V>();
+                    w[q] = 0;
+                    if (i + V <= end) {
+                        __builtin_memcpy(&v[q], z + i, 16);
+                        if (mask) __builtin_memcpy(&w[q], mask + i, V);
+                    }
+                }
+                if (mask) {
+#pragma unroll
+                    for (int q = 0; q < kSweep; q++) hide_masked<T>(v[q], w[q]);
+                }
+                // the one vector that the row ends in
+                const int mine = end / V - at - tid;
+                if (end % V && mine >= 0 && mine < kSweep * THREADS && mine % THREADS == 0) {
+                    const u32x4 ending = load_vector(z, end / V, end, mask);
+#pragma unroll
+                    for (int q = 0; q < kSweep; q++)
+                        if (mine == q * THREADS) v[q] = ending;
+                }
             }
             float m = r.m;
 #pragma unroll
