@@ -598,10 +598,13 @@ Plan plan_of(const Shape& s) {
     n = std::min<int64_t>(n, kMaxSegments);
     p.length = ((s.classes + n - 1) / n + vec - 1) / vec * vec;
     p.segments = (int)((s.classes + p.length - 1) / p.length);
-    // A wave holds a short row.  It selects alternatives as long as half of its threads bound them (4000 x 1000 in bf16, with five 11 us,
-    // with 256 threads 26; with 32 12 and 30; 64, in fp32, 499 and 25), and segments have the compute units to themselves (four
-    // rows of 131072, masked: 16.3 and 15.6 us).
-    p.threads = p.length <= 64 * vec * kSweep && (!s.top || (s.top <= 32 && p.segments == 1)) ? 64 : 256;
+    // A wave takes a short row in one turn of its loads, in two if there are few alternatives, and twice as many where there are waves for
+    // all compute units (bf16, five alternatives: 4000 x 1000 11 us, with 256 threads 26; 4000 x 3000 13 and 25; 4000 x 5003 18 and
+    // 30, but 256 x 5003 with a mask 12.5 and 10.3; with 20 of them 256 x 3000 9.1 and 8.2).  It selects alternatives as long as half of its
+    // threads bound them (4000 x 1000 with 32 12 and 30 us, with 64, in fp32, 499 and 25; 4000 x 8192 with 32 92 and 32), and
+    // segments have the compute units to themselves (four rows of 131072, masked: 16.3 and 15.6 us).
+    const int64_t turns = (s.rows >= 2048 ? 2 : 1) * (s.top <= 8 ? 2 : 1);
+    p.threads = p.length <= turns * 64 * vec * kSweep && (!s.top || (s.top <= 32 && p.segments == 1)) ? 64 : 256;
     const uint64_t tasks = (uint64_t)s.rows * p.segments;
     p.workspace_bytes = up256((uint64_t)s.rows * sizeof(Row));
     if (p.segments > 1) {

@@ -261,3 +261,19 @@ def test_alternatives_of_short_rows(classes, top, dtype):
         got = _run(wide, classes, dtype, tokens, m, 1.0, dlp, dent, top)
         grad = ref.logprob_backward(wide[:, :classes].double(), 1.0, m, tokens, dlp.double(), dent.double())
         _check(got, want, grad, dtype, dlp, dent, classes, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("rows,classes,top", [(7, 3001, 20), (7, 4096, 32), (7, 4097, 32), (2050, 5003, 8), (2050, 4100, 0), (2050, 8193, 3)])
+def test_rows_that_a_wave_takes_in_turns(rows, classes, top, masked, dtype):
+    """All rows run; the definition is computed for the first and the last ones."""
+    wide, tokens, mask, _, dlp, dent = _case(rows, classes, 1, dtype, masked, classes + top, 1.0)
+    wide[0] = 0.25
+    wide[1] = torch.arange(classes + 1).to(wide.dtype)
+    some = sorted({*range(min(rows, 12)), *range(max(0, rows - 4), rows)})
+    logits, part = wide[some, :classes].double(), None if mask is None else mask[some]
+    want = ref.logprob_forward(logits, 1.0, part, tokens[some], top)
+    grad = ref.logprob_backward(logits, 1.0, part, tokens[some], dlp[some].double(), dent[some].double())
+    got = _run(wide, classes, dtype, tokens, mask, 1.0, dlp, dent, top)
+    _check({k: v[some] for k, v in got.items()}, want, grad, dtype, dlp, dent, classes, 1.0)
