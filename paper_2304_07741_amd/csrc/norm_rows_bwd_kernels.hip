@@ -1,7 +1,8 @@
 // Residual norm, backward on rows of tokens (planes of one pixel): the passes of norm_maps_bwd_kernels.hip with one pixel per row,
 // TPR threads per row and KV times 16 bytes each.  Workgroups walk over rows and keep the sums of their channels.
-// Bound by memory.  With the sums over the partials: 4096 x 2048 in fp32 50 us (5.3 TB/s), 8192 x 512 in bf16 21 us (3.3 TB/s),
-// 512 x 16384 in bf16 72 us (1.9 TB/s), whose values are read up to three times.
+// Bound by memory.  With the sums over the partials: 4096 x 2048 in fp32 50 us (5.3 TB/s), 8192 x 512 in bf16 20 us (3.4 TB/s), 2048 x 4096
+// in bf16 36 us (3.7 TB/s; by 256 threads of 32 bytes 39), 4096 x 8192 in bf16 120 us (4.5 TB/s), 512 x 16384 in bf16 73 us (1.8
+// TB/s), whose values are read up to three times.
 #include <atomic>
 
 #include "launch.hpp"
@@ -11,14 +12,13 @@ namespace canvas {
 namespace norm {
 namespace {
 
-// Rows of 1024 threads have no registers for the sums and the weights of their channels: sums in LDS, weights read again; the
-// longest have none for the values either, which are read again for each pass.
+// Rows that 1024 threads of 16 bytes do not hold leave no registers for the values, the weights and the sums of their channels: values and
+// weights are read again for each pass, the sums are in LDS.
 template <class T, int TPR, int KV, int PARTS, int GATE>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_bwd(Shape s, Bwd a) {
     constexpr int V = 16 / sizeof(T), kRows = TPR < 256 ? 256 / TPR : 1;
-    constexpr bool kLong = TPR == 1024;
-    constexpr bool kAgain = kLong && KV > 1;
-    constexpr int KS = kLong ? 1 : KV, KX = kAgain ? 1 : KV;
+    constexpr bool kLong = TPR == 1024 && KV > 1;
+    constexpr int KS = kLong ? 1 : KV, KX = kLong ? 1 : KV;
     extern __shared__ float lds[];
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
     constexpr bool kIsPost = PARTS & kPost, kIsPre = PARTS & kPre;
@@ -58,14 +58,14 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_bwd(Shape s, Bwd
             if (GATE) load_row<T, V>(g[k], a.g, row, c, s.C);
             if (a.dx_out) load_row<T, V>(dy[k], a.dx_out, row, c, s.C);
         };
-        if (!kAgain) {
+        if (!kLong) {
 #pragma unroll
             for (int k = 0; k < KV; k++) load(k % KX, (k * TPR + t) * V);
         }
         const float r2 = kIsPost ? a.r2[n] : 0.f, r1 = kIsPre ? a.r1[n] : 0.f;
         float t1 = 0.f, t2 = 0.f;
         auto renew = [&](int k) {
-            if (kAgain) load(0, (k * TPR + t) * V);
+            if (kLong) load(0, (k * TPR + t) * V);
             if (kIsPre) {
                 x[k % KX].renew();
                 du[k % KX].renew();
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_bwd(Shape s, Bwd
             return kIsPre ? dy_e - y * t1 + du[k % KX].at(e) * w1[k % KS][e] * r1 : dy_e;
         };
         if (kIsPre) {
-#pragma unroll(kAgain ? 1 : KV)
+#pragma unroll(kLong ? 1 : KV)
             for (int k = 0; k < KV; k++) {
                 if (kLong) renew(k);
                 branch(k);
@@ -95,10 +95,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_bwd(Shape s, Bwd
             }
             t1 = over_row<TPR>(t1, lds) * inv * r1 * r1 * r1;
         }
-#pragma unroll(kAgain ? 1 : KV)
+#pragma unroll(kLong ? 1 : KV)
         for (int k = 0; k < KV; k++) {
             renew(k);
-            if (kAgain || !kIsPre) branch(k);
+            if (kLong || !kIsPre) branch(k);
 #pragma unroll
             for (int e = 0; e < V; e++) {
                 const float y = kIsPre ? joined(k, e) : 0.f;
@@ -123,16 +123,16 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_bwd(Shape s, Bwd
         }
         if (kIsPost) {
             t2 = over_row<TPR>(t2, lds) * inv * r2 * r2;
-#pragma unroll(kAgain ? 1 : KV)
+#pragma unroll(kLong ? 1 : KV)
             for (int k = 0; k < KV; k++) {
                 renew(k);
-                if (kAgain) branch(k);
+                if (kLong) branch(k);
                 float dz[V], dg[V];
 #pragma unroll
                 for (int e = 0; e < V; e++) {
                     float av;
                     const float slope = act_slope<GATE>(GATE ? g[k % KX].at(e) : 0.f, av);
-                    const float D = kAgain ? whole(k, e, kIsPre ? joined(k, e) : 0.f) : d[k % KX][e], E = D * (sw[k % KS][e] * r2), zv = z[k % KX].at(e);
+                    const float D = kLong ? whole(k, e, kIsPre ? joined(k, e) : 0.f) : d[k % KX][e], E = D * (sw[k % KS][e] * r2), zv = z[k % KX].at(e);
                     dz[e] = E * av - zv * t2;
                     dg[e] = E * zv * slope;
                 }
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_bwd(Shape s, Bwd
 template <class T, int TPR, int KV, int PARTS, int GATE>
 void rows(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
     constexpr int kBlock = TPR < 256 ? 256 : TPR, kRows = kBlock / TPR;
-    constexpr int lds = kRows > 1 ? 256 * 64 / (int)sizeof(T) : 64 + (TPR == 1024 ? TPR * KV * 128 / (int)sizeof(T) : 0);
+    constexpr int lds = kRows > 1 ? 256 * 64 / (int)sizeof(T) : 64 + (TPR == 1024 && KV > 1 ? TPR * KV * 128 / (int)sizeof(T) : 0);
     if (lds > 65536) {
         static std::atomic<uint64_t> asked{0};
         allow_lds(asked, reinterpret_cast<const void*>(&k_rows_bwd<T, TPR, KV, PARTS, GATE>), lds);
@@ -195,7 +195,7 @@ void run(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
     case 64 * 8 + 1: return rows<T, 64, 1, PARTS, GATE>(s, p, a, stream);
     case 64 * 8 + 2: return rows<T, 64, 2, PARTS, GATE>(s, p, a, stream);
     case 256 * 8 + 1: return rows<T, 256, 1, PARTS, GATE>(s, p, a, stream);
-    case 256 * 8 + 2: return rows<T, 256, 2, PARTS, GATE>(s, p, a, stream);
+    case 512 * 8 + 1: return rows<T, 512, 1, PARTS, GATE>(s, p, a, stream);
     case 1024 * 8 + 1: return rows<T, 1024, 1, PARTS, GATE>(s, p, a, stream);
     default: return rows<T, 1024, 16 / V, PARTS, GATE>(s, p, a, stream);
     }
