@@ -13,7 +13,7 @@
 // Backward: element by element from the row's (m, log S, entropy).
 //
 // Both are bound by memory on many rows: 4096 x 32768 in bf16 forward 44 us (6.0 TB/s, some of it from the last-level cache),
-// backward 111 us (4.8 TB/s).  With alternatives the search at a row's end is not hidden by other rows' loads: 1500 x 50021
+// backward 108 us (5.0 TB/s).  With alternatives the search at a row's end is not hidden by other rows' loads: 1500 x 50021
 // with five of them takes 43 us, without 32.  Few rows are bound by latency: 256 x 1000 4 us per launch.
 #include "logprob_kernels.hpp"
 
@@ -113,6 +113,35 @@ __device__ __forceinline__ u32x4 load_vector(const T* z, int at, int end, const 
         hide_masked<T>(v, mask_bytes<V>(mask, i, end));
     }
     return v;
+}
+
+// Vectors at, at + STRIDE, ... of `end` logits, -inf behind them, and their bytes of the mask.  All of the whole ones are asked for before
+// any is looked at; the one that the row ends in comes one by one.
+template <class T, int N, int STRIDE>
+__device__ __forceinline__ void load_turn(u32x4 (&v)[N], uint64_t (&w)[N], const T* z, const uint8_t* mask, int at, int end) {
+    constexpr int V = Type<T>::kVec;
+#pragma unroll
+    for (int q = 0; q < N; q++) {
+        const int i = (at + q * STRIDE) * V;
+        v[q] = nothing<V>();
+        w[q] = 0;
+        if (i + V <= end) {
+            __builtin_memcpy(&v[q], z + i, 16);
+            if (mask) __builtin_memcpy(&w[q], mask + i, V);
+        }
+    }
+    const int mine = end / V - at;
+    if (end % V && mine >= 0 && mine < N * STRIDE && mine % STRIDE == 0) {
+        const int i = end / V * V;
+        const u32x4 ending = last_logits(z, i, end);
+        const uint64_t bytes = mask ? mask_bytes<V>(mask, i, end) : 0;
+#pragma unroll
+        for (int q = 0; q < N; q++)
+            if (mine == q * STRIDE) {
+                v[q] = ending;
+                w[q] = bytes;
+            }
+    }
 }
 
 // The order of logits as whole numbers: NaN above all, zeros of both signs equal.  -inf is kNone, below every other.
@@ -343,27 +372,10 @@ __global__ __launch_bounds__(THREADS * segments_of(THREADS, TOP)) void k_fwd(Sha
                 }
             } else {
                 uint64_t w[kSweep];
-#pragma unroll
-                for (int q = 0; q < kSweep; q++) {
-                    const int i = (at + q * THREADS + tid) * V;
-                    v[q] = nothing<V>();
-                    w[q] = 0;
-                    if (i + V <= end) {
-                        __builtin_memcpy(&v[q], z + i, 16);
-                        if (mask) __builtin_memcpy(&w[q], mask + i, V);
-                    }
-                }
+                load_turn<T, kSweep, THREADS>(v, w, z, mask, at + tid, end);
                 if (mask) {
 #pragma unroll
                     for (int q = 0; q < kSweep; q++) hide_masked<T>(v[q], w[q]);
-                }
-                // the one vector that the row ends in
-                const int mine = end / V - at - tid;
-                if (end % V && mine >= 0 && mine < kSweep * THREADS && mine % THREADS == 0) {
-                    const u32x4 ending = load_vector(z, end / V, end, mask);
-#pragma unroll
-                    for (int q = 0; q < kSweep; q++)
-                        if (mine == q * THREADS) v[q] = ending;
                 }
             }
             float m = r.m;
@@ -508,6 +520,14 @@ __global__ __launch_bounds__(256) void k_bwd(Shape s, Bwd a, int pieces) {
         u32x4 v[kBwdVecs];
 #pragma unroll
         for (int q = 0; q < kBwdVecs; q++) v[q] = load_vector<T>(z, q * 64 + lane, end, nullptr);
+        uint64_t allow[kBwdVecs];
+        if (mask) {
+#pragma unroll
+            for (int q = 0; q < kBwdVecs; q++) {
+                const int i = (q * 64 + lane) * V;
+                allow[q] = i < end ? mask_bytes<V>(mask, i, end) : 0;
+            }
+        }
         const Row r = reinterpret_cast<const Row*>(a.ws)[row];
         const int64_t t = a.tokens ? a.tokens[row] : -1;
         const bool given = t >= 0 && t < s.classes, empty = r.log_sum == -kInf;
@@ -526,10 +546,9 @@ __global__ __launch_bounds__(256) void k_bwd(Shape s, Bwd a, int pieces) {
                 if (empty) d[e] = 0.f;
             }
             if (mask) {
-                const uint64_t w = mask_bytes<V>(mask, i, end);
 #pragma unroll
                 for (int e = 0; e < V; e++)
-                    if (!allowed(w, e)) d[e] = 0.f;
+                    if (!allowed(allow[q], e)) d[e] = 0.f;
             }
             if (i + V <= end) {
                 u32x4 w;
