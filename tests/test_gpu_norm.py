@@ -177,3 +177,25 @@ def test_one_piece_of_a_plane_at_a_time(shape, dtype):
         want = _reference(shape, maps, weights, gate, True)
         for k, g in _run(shape, dtype, parts, gate, maps, weights).items():
             assert_close(g.reshape(want[k].shape), want[k], TOL[dtype], f"{shape} {dtype} {k}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(64, 64, 16, 16), (64, 72, 19, 21), (64, 128, 19, 21), (64, 200, 16, 17), (48, 300, 21, 20)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_maps_that_fill_the_chip(shape, dtype):
+    """Eight and four pieces of a plane side by side, forward and backward cut alike and differently, several tiles per workgroup."""
+    for parts, gate in PLANS[:1] + PLANS[3:]:
+        maps, weights = _case(shape, dtype, parts, gate, seed=sum(shape))
+        want = _reference(shape, maps, weights, gate, True)
+        for k, g in _run(shape, dtype, parts, gate, maps, weights).items():
+            assert_close(g.reshape(want[k].shape), want[k], TOL[dtype], f"{shape} {dtype} {k}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1100, 512, 1, 1), (1030, 2500, 1, 1), (520, 5120, 1, 1), (300, 8200, 1, 1)], ids=lambda s: "x".join(map(str, s)))
+def test_rows_that_fill_the_chip(shape, dtype):
+    """More rows than workgroups, by 64 to 1024 threads each."""
+    maps, weights = _case(shape, dtype, BOTH, B.CANVAS_GATE_SILU, seed=sum(shape))
+    want = _reference(shape, maps, weights, B.CANVAS_GATE_SILU, True)
+    for k, g in _run(shape, dtype, BOTH, B.CANVAS_GATE_SILU, maps, weights).items():
+        assert_close(g.reshape(want[k].shape), want[k], TOL[dtype], f"{shape} {dtype} {k}")
