@@ -199,3 +199,14 @@ def test_rows_that_fill_the_chip(shape, dtype):
     want = _reference(shape, maps, weights, B.CANVAS_GATE_SILU, True)
     for k, g in _run(shape, dtype, BOTH, B.CANVAS_GATE_SILU, maps, weights).items():
         assert_close(g.reshape(want[k].shape), want[k], TOL[dtype], f"{shape} {dtype} {k}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(300, 24, 1, 3), (700, 24, 2, 3), (2000, 17, 2, 3), (1, 8, 56, 56), (5, 8, 56, 56), (9, 8, 56, 56), (2, 72, 56, 56),
+                                   (5, 72, 56, 56), (1, 160, 56, 56), (1, 300, 56, 56), (1, 600, 56, 56), (260, 2049, 3, 3), (520, 2049, 3, 3), (1030, 2049, 3, 3)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_every_way_of_cutting_maps(shape, dtype):
+    maps, weights = _case(shape, dtype, BOTH, B.CANVAS_GATE_SIGMOID, seed=sum(shape))
+    want = _reference(shape, maps, weights, B.CANVAS_GATE_SIGMOID, True)
+    for k, g in _run(shape, dtype, BOTH, B.CANVAS_GATE_SIGMOID, maps, weights).items():
+        assert_close(g.reshape(want[k].shape), want[k], TOL[dtype], f"{shape} {dtype} {k}")
