@@ -135,3 +135,12 @@ def test_two_steps_at_a_time(shape, steps):
         grad, _, _ = _inputs(shape, 9 + steps, kind)
         want = ref.ortho_step(grad.double(), None, 0, False, steps)
         assert _err(_step(shape, "f32", grad, steps=steps)["update"], want["update"]) <= TOL_F32
+
+
+@pytest.mark.parametrize("shape", [(1, 1700, 6200), (14, 1250, 1300), (2, 1600, 3300), (6, 700, 720)], ids=lambda s: "x".join(map(str, s)))
+def test_large_tiles(shape):
+    """Symmetric products by tiles of 256 and 128, whole and in parts; the definition in 64 bits is computed on the GPU."""
+    grad, _, _ = _inputs(shape, 9, "low")
+    d = grad.double().cuda()
+    want = torch.stack([ref.newton_schulz(m, 5) for m in d]).cpu()
+    assert _err(_step(shape, "f32", grad)["update"], want) <= TOL_F32
