@@ -20,6 +20,8 @@
  * Sums are kept in fp32 relative to the row's largest logit.  Deterministic: no floating-point atomics.
  *
  * Pointers: device pointers, owned by the caller; logits and dlogits are aligned to their element, the others to 16 bytes.
+ * What a call writes must not share bytes with anything else that it reads or writes (BAD_ARG), dlogits in the place of logits
+ * aside; rows of the one between the rows of the other do not.
  * All functions return a canvas_status (0 = OK); canvas_last_error() has the message; nothing is launched after an error was
  * found.  A handle keeps no state of its calls: it may be used on several streams with a workspace each.
  */

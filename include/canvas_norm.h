@@ -24,7 +24,7 @@
  *
  * Pointers: device pointers, owned by the caller, 16-byte aligned, contiguous NCHW in the plan's element type; w_post,
  * scale, w_pre and their gradients are fp32 tensors of C elements.  What a call writes must not share bytes with anything
- * else that it reads or writes.  Tensors that the plan's parts do not have are ignored and may be NULL.  All functions
+ * else that it reads or writes (BAD_ARG).  Tensors that the plan's parts do not have are ignored and may be NULL.  All functions
  * return a canvas_status (0 = OK), canvas_last_error() has the message; nothing is launched after an error was found.
  * A handle keeps no state of its calls: it may be used on several streams with a workspace each.
  */

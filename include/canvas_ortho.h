@@ -50,7 +50,8 @@ int canvas_ortho_query(const canvas_ortho* ortho, canvas_ortho_info* info);
 
 /* grad fp32.  momentum and momentum_out: fp32, read and written, both or neither (then v = g); they may be the same tensor.
  * master and master_out: fp32, both or neither; they may be the same tensor.  weights: needs master; may be NULL.
- * update: may be NULL when master is given.  mu in [0, 1); lr and decay finite.  Nothing else may share bytes. */
+ * update: may be NULL when master is given.  mu in [0, 1); lr and decay finite.  Nothing else that is written
+ * may share bytes with anything (BAD_ARG). */
 int canvas_ortho_step(canvas_ortho* ortho, const float* grad, const float* momentum, float* momentum_out, double mu,
                       const float* master, float* master_out, double lr, double decay, void* weights, void* update,
                       void* workspace, size_t workspace_bytes, void* stream);

@@ -4,6 +4,7 @@
 
 #include <cstdint>
 #include <exception>
+#include <initializer_list>
 #include <string>
 
 #include "../../include/canvas_dag.h"
@@ -35,6 +36,40 @@ inline int check_options(const canvas_options* opt, uint32_t known, uint32_t& fl
 inline int check_workspace(const void* ws, size_t have, uint64_t want) {
     if (have < want) return set_last_error(CANVAS_WORKSPACE_TOO_SMALL, "workspace smaller than workspace_bytes");
     return want ? need(ws, "workspace") : CANVAS_OK;
+}
+
+// A tensor of a call: rows of `bytes` bytes, `pitch` bytes from one to the next.  Null: not part of the call.
+struct Region {
+    const char* name;
+    const void* p;
+    uint64_t bytes, rows = 1, pitch = 0;
+};
+inline bool share_bytes(const Region& a, const Region& b) {
+    if (!a.p || !b.p) return false;
+    if (a.rows < b.rows) return share_bytes(b, a);
+    // (unsigned: an address and 2^63 bytes behind it are below 2^64)
+    const uint64_t a0 = (uint64_t)(uintptr_t)a.p, b0 = (uint64_t)(uintptr_t)b.p;
+    if (a0 >= b0 + (b.rows - 1) * b.pitch + b.bytes || b0 >= a0 + (a.rows - 1) * a.pitch + a.bytes) return false;
+    if (a.rows == 1) return true;
+    // each row of b against the first of a's rows that ends behind its beginning
+    for (uint64_t r = 0; r < b.rows; r++) {
+        const uint64_t from = b0 + r * b.pitch, i = a0 + a.bytes > from ? 0 : (from - a0 - a.bytes) / a.pitch + 1;
+        if (i < a.rows && a0 + i * a.pitch < from + b.bytes) return true;
+    }
+    return false;
+}
+// CANVAS_OK, or BAD_ARG if what a call writes shares bytes with anything else that it writes or reads.
+inline int check_apart(std::initializer_list<Region> written, std::initializer_list<Region> read) {
+    auto clash = [](const Region& a, const Region& b) {
+        return set_last_error(CANVAS_BAD_ARG, std::string(a.name) + " is written and shares bytes with " + b.name);
+    };
+    for (const Region* a = written.begin(); a != written.end(); a++) {
+        for (const Region* b = a + 1; b != written.end(); b++)
+            if (share_bytes(*a, *b)) return clash(*a, *b);
+        for (const Region& b : read)
+            if (share_bytes(*a, b)) return clash(*a, b);
+    }
+    return CANVAS_OK;
 }
 
 inline int launched() {

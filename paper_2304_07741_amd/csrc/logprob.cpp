@@ -27,6 +27,14 @@ int check_rows(const canvas_logprob* h, const void* p, int64_t pitch, const char
     return CANVAS_OK;
 }
 
+Region rows_of(const canvas_logprob* h, const char* name, const void* p, int64_t pitch) {
+    const uint64_t e = h->s.bf16 ? 2 : 4;
+    return Region{name, p, e * h->s.classes, (uint64_t)h->s.rows, e * pitch};
+}
+Region mask_of(const canvas_logprob* h, const uint8_t* mask, int64_t mask_pitch) {
+    return Region{"mask", mask, (uint64_t)h->s.classes, mask_pitch ? (uint64_t)h->s.rows : 1, (uint64_t)mask_pitch};
+}
+
 int check_call(const canvas_logprob* h, const void* logits, int64_t pitch, float it, const uint8_t* mask, int64_t mask_pitch) {
     if (int rc = check_rows(h, logits, pitch, "logits")) return rc;
     if (!(it > 0.f) || !std::isfinite(it)) return set_last_error(CANVAS_BAD_ARG, "inv_temperature must be finite and positive");
@@ -84,6 +92,14 @@ int canvas_logprob_forward(canvas_logprob* lp, const void* logits, int64_t pitch
         if (entropy && (rc = need(entropy, "entropy"))) return rc;
         if (lp->s.top > 0 && ((rc = need(top_logprob, "top_logprob")) || (rc = need(top_index, "top_index")))) return rc;
         if ((rc = check_workspace(workspace, workspace_bytes, lp->plan.workspace_bytes))) return rc;
+        const uint64_t n = lp->s.rows, top = lp->s.top;
+        rc = check_apart({{"logprob", logprob, 4 * n},
+                          {"entropy", entropy, 4 * n},
+                          {"top_logprob", top ? top_logprob : nullptr, 4 * n * top},
+                          {"top_index", top ? top_index : nullptr, 4 * n * top},
+                          {"workspace", workspace, lp->plan.workspace_bytes}},
+                         {rows_of(lp, "logits", logits, pitch), mask_of(lp, mask, mask_pitch), {"tokens", tokens, 8 * n}});
+        if (rc) return rc;
         const canvas::logprob::Fwd a{logits, pitch, inv_temperature, mask, mask_pitch, tokens, logprob, entropy, top_logprob, top_index,
                                      static_cast<char*>(workspace)};
         (void)hipGetLastError();
@@ -105,6 +121,15 @@ int canvas_logprob_backward(canvas_logprob* lp, const void* logits, int64_t pitc
         if (dlogprob && (rc = need(dlogprob, "dlogprob"))) return rc;
         if (dentropy && (rc = need(dentropy, "dentropy"))) return rc;
         if ((rc = check_workspace(workspace, workspace_bytes, lp->plan.workspace_bytes))) return rc;
+        const uint64_t n = lp->s.rows;
+        rc = check_apart({rows_of(lp, "dlogits", dlogits, dpitch)},
+                         {rows_of(lp, "logits", dlogits == logits ? nullptr : logits, pitch),
+                          mask_of(lp, mask, mask_pitch),
+                          {"tokens", tokens, 8 * n},
+                          {"dlogprob", dlogprob, 4 * n},
+                          {"dentropy", dentropy, 4 * n},
+                          {"workspace", workspace, lp->plan.workspace_bytes}});
+        if (rc) return rc;
         const canvas::logprob::Bwd a{logits, pitch, inv_temperature, mask, mask_pitch, tokens, dlogprob, dentropy, dlogits, dpitch,
                                      static_cast<const char*>(workspace)};
         (void)hipGetLastError();

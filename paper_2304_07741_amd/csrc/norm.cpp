@@ -20,6 +20,7 @@ using canvas::set_last_error;
 using namespace canvas::abi;
 
 uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
+uint64_t map_bytes(const canvas::norm::Shape& s) { return (s.bf16 ? 2ull : 4ull) * s.N * s.C * s.P; }
 
 int check_weights(const canvas_norm* h, const void* z, const void* gate, const float* w_post, const float* scale, const float* w_pre) {
     int rc = CANVAS_OK;
@@ -94,6 +95,16 @@ int canvas_norm_forward(canvas_norm* norm, const void* x, const void* z, const v
         if (norm->s.post && (rc = need(x_out, "x_out"))) return rc;
         if (norm->s.pre && (rc = need(u, "u"))) return rc;
         if ((rc = check_workspace(workspace, workspace_bytes, norm->info.workspace_bytes))) return rc;
+        const canvas::norm::Shape& s = norm->s;
+        const uint64_t map = map_bytes(s), vec = 4ull * s.C;
+        rc = check_apart({{"x_out", s.post ? x_out : nullptr, map}, {"u", s.pre ? u : nullptr, map}, {"workspace", norm->inference ? nullptr : workspace, norm->info.workspace_bytes}},
+                         {{"x", x, map},
+                          {"z", s.post ? z : nullptr, map},
+                          {"gate", s.gate ? gate : nullptr, map},
+                          {"w_post", s.post ? w_post : nullptr, vec},
+                          {"scale", s.post ? scale : nullptr, vec},
+                          {"w_pre", s.pre ? w_pre : nullptr, vec}});
+        if (rc) return rc;
         char* ws = static_cast<char*>(workspace);
         canvas::norm::Fwd a{x, z, gate, w_post, scale, w_pre, x_out, u, nullptr, nullptr};
         if (!norm->inference) {
@@ -120,6 +131,23 @@ int canvas_norm_backward(canvas_norm* norm, const void* x, const void* z, const 
         if (s.pre && ((rc = need(x, "x")) || (rc = need(du, "du")) || (rc = need(dx, "dx")) || (rc = need(dw_pre, "dw_pre")))) return rc;
         if ((dx_out || !s.pre) && (rc = need(dx_out, "dx_out"))) return rc;
         if ((rc = check_workspace(workspace, workspace_bytes, norm->info.workspace_bytes))) return rc;
+        const uint64_t map = map_bytes(s), vec = 4ull * s.C;
+        rc = check_apart({{"dx", s.pre ? dx : nullptr, map},
+                          {"dz", s.post ? dz : nullptr, map},
+                          {"dgate", s.gate ? dgate : nullptr, map},
+                          {"dw_post", s.post ? dw_post : nullptr, vec},
+                          {"dscale", s.post ? dscale : nullptr, vec},
+                          {"dw_pre", s.pre ? dw_pre : nullptr, vec},
+                          {"workspace", workspace, norm->info.workspace_bytes}},
+                         {{"x", s.pre ? x : nullptr, map},
+                          {"z", s.post ? z : nullptr, map},
+                          {"gate", s.gate ? gate : nullptr, map},
+                          {"w_post", s.post ? w_post : nullptr, vec},
+                          {"scale", s.post ? scale : nullptr, vec},
+                          {"w_pre", s.pre ? w_pre : nullptr, vec},
+                          {"dx_out", dx_out, map},
+                          {"du", s.pre ? du : nullptr, map}});
+        if (rc) return rc;
         char* ws = static_cast<char*>(workspace);
         const canvas::norm::Bwd a{x, z, gate, w_post, scale, w_pre, dx_out, du, dx, dz, dgate, dw_post, dscale, dw_pre, reinterpret_cast<float*>(ws),
                                   reinterpret_cast<float*>(ws + norm->r1_at), reinterpret_cast<float*>(ws + norm->partial_at)};

@@ -77,6 +77,15 @@ int canvas_ortho_step(canvas_ortho* ortho, const float* grad, const float* momen
         if (weights && (rc = need(weights, "weights"))) return rc;
         if ((update || !master) && (rc = need(update, "update"))) return rc;
         if ((rc = check_workspace(workspace, workspace_bytes, ortho->plan.workspace_bytes))) return rc;
+        const canvas::ortho::Shape& s = ortho->s;
+        const uint64_t n = (uint64_t)(s.G * s.R * s.K), e = s.bf16 ? 2 : 4;
+        rc = check_apart({{"momentum_out", momentum_out, 4 * n},
+                          {"master_out", master_out, 4 * n},
+                          {"weights", weights, e * n},
+                          {"update", update, e * n},
+                          {"workspace", workspace, ortho->plan.workspace_bytes}},
+                         {{"grad", grad, 4 * n}, {"momentum", momentum == momentum_out ? nullptr : momentum, 4 * n}, {"master", master == master_out ? nullptr : master, 4 * n}});
+        if (rc) return rc;
         const canvas::ortho::Args a{grad, momentum, momentum_out, mu, master, master_out, lr, decay, weights, update, static_cast<char*>(workspace)};
         (void)hipGetLastError();
         canvas::ortho::step(ortho->s, ortho->plan, a, (hipStream_t)stream);

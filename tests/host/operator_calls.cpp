@@ -1,0 +1,234 @@
+// Calls of the operators around a block with the runtime's launch functions in this program's place: nothing reaches a GPU, addresses
+// are numbers.  First argument: what is looked at; prints "<what> cases <n> wrong <m>".
+//
+//   overlap   calls whose tensors share bytes where a call writes are refused before anything is launched, others are not
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <cstdio>
+#include <cstring>
+#include <map>
+#include <string>
+#include <vector>
+
+#include "../../include/canvas_logprob.h"
+#include "../../include/canvas_norm.h"
+#include "../../include/canvas_ortho.h"
+
+struct Launch {
+    const void* kernel;
+    dim3 grid, block;
+    size_t lds;
+};
+static std::vector<Launch> g_launches;
+static std::map<const void*, int> g_allowed;  // LDS that was asked for, by kernel
+
+extern "C" hipError_t hipLaunchKernel(const void* kernel, dim3 grid, dim3 block, void**, size_t lds, hipStream_t) {
+    g_launches.push_back(Launch{kernel, grid, block, lds});
+    return hipSuccess;
+}
+static Launch g_configuration;  // of the launch that is being made
+extern "C" hipError_t __hipPushCallConfiguration(dim3 grid, dim3 block, size_t lds, hipStream_t) {
+    g_configuration = Launch{nullptr, grid, block, lds};
+    return hipSuccess;
+}
+extern "C" hipError_t __hipPopCallConfiguration(dim3* grid, dim3* block, size_t* lds, hipStream_t* stream) {
+    *grid = g_configuration.grid;
+    *block = g_configuration.block;
+    *lds = g_configuration.lds;
+    *stream = nullptr;
+    return hipSuccess;
+}
+extern "C" hipError_t hipFuncSetAttribute(const void* kernel, hipFuncAttribute attr, int value) {
+    if (attr == hipFuncAttributeMaxDynamicSharedMemorySize) g_allowed[kernel] = value;
+    return hipSuccess;
+}
+extern "C" hipError_t hipGetDevice(int* d) {
+    *d = 0;
+    return hipSuccess;
+}
+extern "C" hipError_t hipGetLastError() { return hipSuccess; }
+
+static long g_cases = 0, g_wrong = 0;
+static void expect(bool ok, const std::string& what) {
+    g_cases++;
+    if (!ok && g_wrong++ < 20) printf("wrong: %s (%s)\n", what.c_str(), canvas_last_error());
+}
+
+// ---------------------------------------------------------------- overlap
+
+struct Tensor {
+    const char* name;
+    uint64_t bytes;
+    bool written;
+    uint64_t at = 0;
+    void* p() const { return reinterpret_cast<void*>(at); }
+};
+template <class CALL>
+static int call(CALL f, const std::vector<Tensor>& t, bool& launched) {
+    g_launches.clear();
+    const int rc = f(t);
+    launched = !g_launches.empty();
+    return rc;
+}
+// Every tensor apart, then each pair of which one is written: at one place, the one's end on the other's beginning, and side by side.
+template <class CALL, class MAY>
+static void pairs(const std::string& what, std::vector<Tensor> t, CALL f, MAY may) {
+    uint64_t at = 1ull << 32;
+    for (Tensor& x : t) {
+        x.at = at;
+        at += (x.bytes + 4095) / 4096 * 4096 + (1 << 20);
+    }
+    bool launched;
+    expect(call(f, t, launched) == CANVAS_OK && launched, what + ": all apart");
+    for (size_t i = 0; i < t.size(); i++)
+        for (size_t j = 0; j < t.size(); j++) {
+            if (i == j || !t[i].written) continue;
+            const std::string pair = what + ": " + t[i].name + " and " + t[j].name;
+            std::vector<Tensor> v = t;
+            const uint64_t room = at;  // behind all others
+            const uint64_t last_i = (t[i].bytes - 1) / 16 * 16, last_j = (t[j].bytes - 1) / 16 * 16;
+            v[i].at = v[j].at = room;
+            const bool fine = may(t[i].name, t[j].name);
+            expect((call(f, v, launched) == (fine ? CANVAS_OK : CANVAS_BAD_ARG)) && launched == fine, pair + " at one place");
+            if (last_i || last_j) {
+                v[i].at = room;
+                v[j].at = room + last_i;
+                if (last_i) expect(call(f, v, launched) == CANVAS_BAD_ARG && !launched, pair + ", the second on the first's end");
+                v[i].at = room + last_j;
+                v[j].at = room;
+                if (last_j) expect(call(f, v, launched) == CANVAS_BAD_ARG && !launched, pair + ", the first on the second's end");
+            }
+            v[i].at = room;
+            v[j].at = room + (t[i].bytes + 15) / 16 * 16;
+            expect(call(f, v, launched) == CANVAS_OK && launched, pair + " side by side");
+        }
+}
+
+static void norm_overlap() {
+    for (int64_t P : {1, 6, 49})
+        for (uint32_t parts = 1; parts <= 3; parts++)
+            for (int gate = 0; gate <= ((parts & 1) ? 2 : 0); gate++) {
+                const int64_t shape[4] = {3, 40, P, 1};
+                const uint64_t map = 2ull * 3 * 40 * P, vec = 160;
+                const bool post = parts & CANVAS_NORM_POST, pre = parts & CANVAS_NORM_PRE;
+                canvas_norm* h = nullptr;
+                if (canvas_norm_compile(shape, CANVAS_BF16, parts, (canvas_gate)gate, 1e-6f, nullptr, &h)) return expect(false, "norm compile");
+                canvas_norm_info info;
+                canvas_norm_query(h, &info);
+                const std::string what = "norm parts " + std::to_string(parts) + " pixels " + std::to_string(P) + " gate " + std::to_string(gate);
+                std::vector<Tensor> f{{"x", map, false}, {"workspace", info.workspace_bytes, true}};
+                if (post) f.insert(f.end(), {{"z", map, false}, {"w_post", vec, false}, {"scale", vec, false}, {"x_out", map, true}});
+                if (gate) f.push_back({"gate", map, false});
+                if (pre) f.insert(f.end(), {{"w_pre", vec, false}, {"u", map, true}});
+                auto get = [](const std::vector<Tensor>& t, const char* name) -> void* {
+                    for (const Tensor& x : t)
+                        if (!strcmp(x.name, name)) return x.p();
+                    return nullptr;
+                };
+                auto none = [](const char*, const char*) { return false; };
+                auto fl = [&](const std::vector<Tensor>& t, const char* n) { return static_cast<float*>(get(t, n)); };
+                pairs(what, f,
+                      [&](const std::vector<Tensor>& t) {
+                          return canvas_norm_forward(h, get(t, "x"), get(t, "z"), get(t, "gate"), fl(t, "w_post"), fl(t, "scale"), fl(t, "w_pre"), get(t, "x_out"),
+                                                     get(t, "u"), get(t, "workspace"), info.workspace_bytes, nullptr);
+                      },
+                      none);
+                std::vector<Tensor> b{{"dx_out", map, false}, {"workspace", info.workspace_bytes, true}};
+                if (post) b.insert(b.end(), {{"z", map, false}, {"w_post", vec, false}, {"scale", vec, false}, {"dz", map, true}, {"dw_post", vec, true}, {"dscale", vec, true}});
+                if (gate) b.insert(b.end(), {{"gate", map, false}, {"dgate", map, true}});
+                if (pre) b.insert(b.end(), {{"x", map, false}, {"w_pre", vec, false}, {"du", map, false}, {"dx", map, true}, {"dw_pre", vec, true}});
+                pairs(what + " backward", b,
+                      [&](const std::vector<Tensor>& t) {
+                          return canvas_norm_backward(h, get(t, "x"), get(t, "z"), get(t, "gate"), fl(t, "w_post"), fl(t, "scale"), fl(t, "w_pre"), get(t, "dx_out"),
+                                                      get(t, "du"), get(t, "dx"), get(t, "dz"), get(t, "dgate"), fl(t, "dw_post"), fl(t, "dscale"), fl(t, "dw_pre"),
+                                                      get(t, "workspace"), info.workspace_bytes, nullptr);
+                      },
+                      none);
+                canvas_norm_destroy(h);
+            }
+}
+
+static void logprob_overlap() {
+    const int64_t rows = 9, classes = 100;
+    for (int64_t pitch : {100, 137}) {
+        canvas_logprob* h = nullptr;
+        if (canvas_logprob_compile(rows, classes, CANVAS_F32, 3, nullptr, &h)) return expect(false, "logprob compile");
+        canvas_logprob_info info;
+        canvas_logprob_query(h, &info);
+        const uint64_t map = 4ull * ((rows - 1) * pitch + classes);
+        const std::string what = "logprob pitch " + std::to_string(pitch);
+        std::vector<Tensor> f{{"logits", map, false}, {"mask", (uint64_t)((rows - 1) * 128 + classes), false}, {"tokens", 8 * rows, false}, {"logprob", 4 * rows, true},
+                              {"entropy", 4 * rows, true}, {"top_logprob", 12 * rows, true}, {"top_index", 12 * rows, true}, {"workspace", info.workspace_bytes, true}};
+        if (pitch == classes)  // (with gaps between the rows a small tensor finds room in them)
+            pairs(what, f,
+                  [&](const std::vector<Tensor>& t) {
+                      return canvas_logprob_forward(h, t[0].p(), pitch, 1.f, (uint8_t*)t[1].p(), 128, (int64_t*)t[2].p(), (float*)t[3].p(), (float*)t[4].p(), (float*)t[5].p(),
+                                                    (int32_t*)t[6].p(), t[7].p(), info.workspace_bytes, nullptr);
+                  },
+                  [](const char*, const char*) { return false; });
+        std::vector<Tensor> b{{"logits", map, false}, {"dlogits", map, true}, {"tokens", 8 * rows, false}, {"dlogprob", 4 * rows, false}, {"dentropy", 4 * rows, false}, {"workspace", info.workspace_bytes, false}};
+        auto backward = [&](uint64_t logits, int64_t pitch, uint64_t dlogits, int64_t dpitch) {
+            g_launches.clear();
+            const int rc = canvas_logprob_backward(h, (void*)logits, pitch, 1.f, nullptr, 0, (int64_t*)(1ull << 20), (float*)(1ull << 21), (float*)(1ull << 22), (void*)dlogits, dpitch,
+                                                   (void*)(1ull << 23), info.workspace_bytes, nullptr);
+            return rc == CANVAS_OK ? g_launches.empty() ? -100 : 0 : g_launches.empty() ? rc : -101;
+        };
+        if (pitch == classes)
+            pairs(what + " backward", b,
+                  [&](const std::vector<Tensor>& t) {
+                      return canvas_logprob_backward(h, t[0].p(), pitch, 1.f, nullptr, 0, (int64_t*)t[2].p(), (float*)t[3].p(), (float*)t[4].p(), t[1].p(), pitch, t[5].p(),
+                                                     info.workspace_bytes, nullptr);
+                  },
+                  [](const char* a, const char* b) { return !strcmp(a, "dlogits") && !strcmp(b, "logits"); });
+        // rows between each other's rows, by brute force over the bytes
+        const uint64_t at = 1ull << 32;
+        for (int64_t dpitch : {100, 137, 200, 250})
+            for (int64_t lp : {100, 137, 200, 250})
+                for (int64_t off = -1200; off <= 1200; off += 7) {
+                    bool meet = false;
+                    for (int64_t i = 0; i < rows; i++)
+                        for (int64_t j = 0; j < rows; j++) {
+                            const int64_t d = off + j * dpitch - i * lp;
+                            meet |= d < classes && d > -classes;
+                        }
+                    const bool same = off == 0 && dpitch == lp;
+                    const int want = same || !meet ? 0 : CANVAS_BAD_ARG;
+                    expect(backward(at, lp, at + 4 * off, dpitch) == want, "logprob pitches " + std::to_string(lp) + " and " + std::to_string(dpitch) + " offset " + std::to_string(off));
+                }
+        canvas_logprob_destroy(h);
+    }
+}
+
+static void ortho_overlap() {
+    for (int64_t R : {8, 200}) {
+        const int64_t shape[3] = {2, R, 80};
+        const uint64_t f32 = 4ull * 2 * R * 80, bf16 = f32 / 2;
+        canvas_ortho* h = nullptr;
+        if (canvas_ortho_compile(shape, CANVAS_BF16, 5, 0, &h)) return expect(false, "ortho compile");
+        canvas_ortho_info info;
+        canvas_ortho_query(h, &info);
+        std::vector<Tensor> t{{"grad", f32, false}, {"momentum", f32, false}, {"momentum_out", f32, true}, {"master", f32, false}, {"master_out", f32, true},
+                              {"weights", bf16, true}, {"update", bf16, true}, {"workspace", info.workspace_bytes, true}};
+        pairs("ortho rows " + std::to_string(R), t,
+              [&](const std::vector<Tensor>& t) {
+                  return canvas_ortho_step(h, (float*)t[0].p(), (float*)t[1].p(), (float*)t[2].p(), 0.9, (float*)t[3].p(), (float*)t[4].p(), 0.1, 0.0, t[5].p(), t[6].p(),
+                                           t[7].p(), info.workspace_bytes, nullptr);
+              },
+              [](const char* a, const char* b) {
+                  return (!strcmp(a, "momentum_out") && !strcmp(b, "momentum")) || (!strcmp(a, "master_out") && !strcmp(b, "master"));
+              });
+        canvas_ortho_destroy(h);
+    }
+}
+
+int main(int argc, char** argv) {
+    const std::string what = argc > 1 ? argv[1] : "";
+    if (what == "overlap") {
+        norm_overlap();
+        logprob_overlap();
+        ortho_overlap();
+    }
+    printf("%s cases %ld wrong %ld\n", what.c_str(), g_cases, g_wrong);
+    return g_cases && !g_wrong ? 0 : 1;
+}

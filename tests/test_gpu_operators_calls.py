@@ -134,3 +134,46 @@ def test_runners_refuse_tensors_that_do_not_fit():
         with pytest.raises(ValueError):
             o.step(*args)
     o.close()
+
+
+@pytest.mark.parametrize("shape", [(3, 24, 7, 7), (2, 2100, 3, 3), (40, 64, 1, 1)], ids=lambda s: "x".join(map(str, s)))
+def test_a_runners_own_output_is_no_input(shape):
+    """x' on top of x is refused, and nothing is written."""
+    r, (x, z, g, _, _), _ = _norm_case(shape, "bf16")
+    w = [torch.ones(shape[1], device="cuda") for _ in range(3)]
+    out = r.forward(x, z, g, *w)
+    before = {k: v.clone() for k, v in out.items()}
+    with pytest.raises(B.CanvasError) as e:
+        r.forward(out["x_out"], z, g, *w)
+    assert e.value.status == -4 and "share" in str(e.value)
+    torch.cuda.synchronize()
+    for k, v in before.items():
+        assert torch.equal(v, r.out[k]), k
+    r.close()
+
+
+def test_nothing_is_read_that_a_call_writes():
+    o = harness.OrthoRunner((2, 40, 80), "f32")
+    grad, momentum = torch.randn(2, 40, 80, device="cuda"), torch.randn(2, 40, 80, device="cuda")
+    with pytest.raises(B.CanvasError):
+        B.canvas_ortho_step(o.handle, grad, momentum, grad, 0.9, None, None, 0.0, 0.0, None, o.out["update"], o.ws)
+    with pytest.raises(B.CanvasError):
+        o.step(o.out["update"])
+    o.close()
+    lp = harness.LogprobRunner(4, 100, "f32")
+    wide = torch.randn(5, 100, device="cuda")
+    tokens, d = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.ones(4, device="cuda")
+    lp.forward(wide[:4], tokens)
+    with pytest.raises(B.CanvasError):
+        B.canvas_logprob_backward(lp.handle, wide[:4], 100, 1.0, None, 0, tokens, d, None, wide[1:], 100, lp.ws)
+    lp.close()
+    # gradients in the gaps between the logits' rows
+    lp = harness.LogprobRunner(5, 50, "f32")
+    tokens, d = torch.zeros(5, dtype=torch.int64, device="cuda"), torch.ones(5, device="cuda")
+    logits = wide[:, :50]
+    lp.forward(logits, tokens)
+    want = lp.backward(logits, tokens, d)["dlogits"]
+    before = logits.clone()
+    B.canvas_logprob_backward(lp.handle, logits, 100, 1.0, None, 0, tokens, d, None, wide[:, 50:], 100, lp.ws)
+    assert torch.equal(wide[:, 50:], want) and torch.equal(logits, before)
+    lp.close()
