@@ -10,7 +10,7 @@
 
 namespace canvas {
 
-// More than 64 KB of dynamic LDS must be asked for, once per kernel and device.  `asked`: the kernel's own, a bit per device (beyond the 64th: asked for
+// More than 64 KB of dynamic LDS must be asked for, once per kernel and device: `bytes` is the most that any launch of the kernel takes.  `asked`: the kernel's own, a bit per device (beyond the 64th: asked for
 // with every launch).  A refusal is the error that the caller finds behind its launches (hipGetLastError), and the next launch asks again.
 inline void allow_lds(std::atomic<uint64_t>& asked, const void* kernel, int bytes) {
     int dev = -1;

@@ -11,6 +11,7 @@
 // channels per thread leave two waves per SIMD, and the short planes' pieces overlap (56 pixels read for 49).
 #include <atomic>
 
+#include "../../include/canvas_norm.h"
 #include "launch.hpp"
 #include "norm_device.hpp"
 
@@ -177,10 +178,11 @@ __global__ __launch_bounds__(512, KC == 2 ? 3 : 1) void k_maps_bwd(Shape s, Bwd 
 template <class T, int VEC, int KC, int PARTS, int GATE>
 void maps(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
     const Tiling& t = p.bwd;
+    constexpr int kMost = 512 / 64 * 8 * VEC * 4 + 8 * CANVAS_NORM_MAX_CHANNELS;  // eight pieces side by side, all channels' sums
     const int lds = t.threads / 64 * (1 << t.log_gx) * VEC * 4 + (KC ? 0 : 8 * s.C);
     if (lds > 65536) {
         static std::atomic<uint64_t> asked{0};
-        allow_lds(asked, reinterpret_cast<const void*>(&k_maps_bwd<T, VEC, KC, PARTS, GATE>), lds);
+        allow_lds(asked, reinterpret_cast<const void*>(&k_maps_bwd<T, VEC, KC, PARTS, GATE>), kMost);
     }
     CANVAS_LAUNCH((k_maps_bwd<T, VEC, KC, PARTS, GATE>), dim3(p.partials), dim3(t.threads), lds, stream, s, a, t.log_gx, p.pieces, p.total);
 }

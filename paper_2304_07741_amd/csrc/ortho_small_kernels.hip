@@ -138,7 +138,7 @@ void step_small(const Shape& s, const Args& a, hipStream_t stream) {
     const int lds = small_plan(s).lds;
     if (lds > 65536) {
         static std::atomic<uint64_t> asked{0};
-        allow_lds(asked, reinterpret_cast<const void*>(&k_small), lds);
+        allow_lds(asked, reinterpret_cast<const void*>(&k_small), kMostSmallLds);
     }
     CANVAS_LAUNCH(k_small, dim3((unsigned)s.G), dim3(kThreads), lds, stream, s, a);
 }

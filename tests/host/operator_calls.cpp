@@ -2,6 +2,7 @@
 // are numbers.  First argument: what is looked at; prints "<what> cases <n> wrong <m>".
 //
 //   overlap   calls whose tensors share bytes where a call writes are refused before anything is launched, others are not
+//   lds       every launch with more than 64 KB of LDS has asked for as much, whatever shapes came before it
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -53,6 +54,55 @@ static long g_cases = 0, g_wrong = 0;
 static void expect(bool ok, const std::string& what) {
     g_cases++;
     if (!ok && g_wrong++ < 20) printf("wrong: %s (%s)\n", what.c_str(), canvas_last_error());
+}
+
+// ---------------------------------------------------------------- calls with tensors far apart
+
+static void* place(int k) { return reinterpret_cast<void*>((uint64_t)(k + 1) << 44); }
+static uint8_t* const kSpace = static_cast<uint8_t*>(place(40));
+static int norm_forward_and_backward(int64_t n, int64_t c, int64_t p, canvas_dtype dt, uint32_t parts, int gate) {
+    const int64_t shape[4] = {n, c, p, 1};
+    canvas_norm* h = nullptr;
+    if (int rc = canvas_norm_compile(shape, dt, parts, (canvas_gate)gate, 1e-6f, nullptr, &h)) return rc;
+    canvas_norm_info info;
+    canvas_norm_query(h, &info);
+    auto f = [](int k) { return static_cast<float*>(place(k)); };
+    g_launches.clear();
+    int rc = canvas_norm_forward(h, place(0), place(1), place(2), f(3), f(4), f(5), place(6), place(7), kSpace, info.workspace_bytes, nullptr);
+    if (!rc) rc = canvas_norm_backward(h, place(0), place(1), place(2), f(3), f(4), f(5), place(8), place(9), place(10), place(11), place(12), f(13), f(14), f(15), kSpace, info.workspace_bytes, nullptr);
+    canvas_norm_destroy(h);
+    return rc;
+}
+static int ortho_step(int64_t g, int64_t r, int64_t k, canvas_dtype dt, int steps) {
+    const int64_t shape[3] = {g, r, k};
+    canvas_ortho* h = nullptr;
+    if (int rc = canvas_ortho_compile(shape, dt, steps, CANVAS_ORTHO_NESTEROV, &h)) return rc;
+    canvas_ortho_info info;
+    canvas_ortho_query(h, &info);
+    auto f = [](int k) { return static_cast<float*>(place(k)); };
+    g_launches.clear();
+    const int rc = canvas_ortho_step(h, f(0), f(1), f(2), 0.9, f(3), f(4), 0.1, 0.0, place(5), place(6), kSpace, info.workspace_bytes, nullptr);
+    canvas_ortho_destroy(h);
+    return rc;
+}
+
+// ---------------------------------------------------------------- lds
+
+static void lds() {
+    auto look = [](int rc, const std::string& what) {
+        bool ok = rc == CANVAS_OK && !g_launches.empty();
+        for (const Launch& l : g_launches) ok &= l.lds <= 65536 || (g_allowed.count(l.kernel) && (int64_t)l.lds <= g_allowed[l.kernel] && l.lds <= 163840);
+        expect(ok, what);
+    };
+    for (canvas_dtype dt : {CANVAS_F32, CANVAS_BF16})
+        for (uint32_t parts = 1; parts <= 3; parts++)
+            for (int gate = 0; gate <= ((parts & 1) ? 2 : 0); gate++)
+                for (int64_t p : {1, 2, 9, 64})
+                    for (int64_t c : {8200, 9000, 16384, 8300, 12000})
+                        look(norm_forward_and_backward(3, c, p, dt, parts, gate), "norm " + std::to_string(c) + " channels, " + std::to_string(p) + " pixels");
+    const int64_t small[][2] = {{63, 65}, {64, 100}, {64, 256}, {48, 480}, {16, 1400}, {63, 65}};
+    for (canvas_dtype dt : {CANVAS_F32, CANVAS_BF16})
+        for (const auto& s : small) look(ortho_step(2, s[0], s[1], dt, 5), "ortho " + std::to_string(s[0]) + " x " + std::to_string(s[1]));
 }
 
 // ---------------------------------------------------------------- overlap
@@ -229,6 +279,7 @@ int main(int argc, char** argv) {
         logprob_overlap();
         ortho_overlap();
     }
+    if (what == "lds") lds();
     printf("%s cases %ld wrong %ld\n", what.c_str(), g_cases, g_wrong);
     return g_cases && !g_wrong ? 0 : 1;
 }

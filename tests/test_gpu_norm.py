@@ -210,3 +210,13 @@ def test_every_way_of_cutting_maps(shape, dtype):
     want = _reference(shape, maps, weights, B.CANVAS_GATE_SIGMOID, True)
     for k, g in _run(shape, dtype, BOTH, B.CANVAS_GATE_SIGMOID, maps, weights).items():
         assert_close(g.reshape(want[k].shape), want[k], TOL[dtype], f"{shape} {dtype} {k}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_more_and_more_channels_in_one_process(dtype):
+    """Sums of 8200 channels take 64 KB of LDS and more, of 16384 twice as much: the later plan is not held to what the first one took."""
+    for shape in [(1, 8200, 3, 3), (2, 16384, 3, 3), (3, 12000, 1, 2), (2, 16384, 2, 1)]:
+        maps, weights = _case(shape, dtype, BOTH, B.CANVAS_GATE_SILU, seed=sum(shape))
+        want = _reference(shape, maps, weights, B.CANVAS_GATE_SILU, True)
+        for k, g in _run(shape, dtype, BOTH, B.CANVAS_GATE_SILU, maps, weights).items():
+            assert_close(g.reshape(want[k].shape), want[k], TOL[dtype], f"{shape} {dtype} {k}")

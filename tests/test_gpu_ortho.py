@@ -144,3 +144,12 @@ def test_large_tiles(shape):
     d = grad.double().cuda()
     want = torch.stack([ref.newton_schulz(m, 5) for m in d]).cpu()
     assert _err(_step(shape, "f32", grad)["update"], want) <= TOL_F32
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_larger_and_larger_small_matrices_in_one_process(dtype):
+    """63 x 65 takes 73 KB of LDS, 64 x 256 118: the later plan is not held to what the first one took."""
+    for shape in [(2, 63, 65), (1, 64, 256), (2, 48, 480), (1, 480, 48)]:
+        grad, _, _ = _inputs(shape, 10)
+        want = ref.ortho_step(grad.double(), None, 0, False, 5)
+        assert _err(_step(shape, dtype, grad)["update"], want["update"]) <= (TOL_F32 if dtype == "f32" else TOL_BF16)

@@ -33,3 +33,7 @@ def _look(program, what):
 
 def test_tensors_that_share_bytes_are_refused(program):
     assert _look(program, "overlap") > 5000
+
+
+def test_lds_is_asked_for_whatever_shapes_came_before(program):
+    assert _look(program, "lds") > 200
