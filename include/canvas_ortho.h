@@ -41,7 +41,8 @@ typedef struct canvas_ortho_info {
     double min_bytes;         /* gradient read, update written; momentum read and written; without master weights */
 } canvas_ortho_info;
 
-/* Host only.  shape: G, R, K, all >= 1, min(R, K) <= CANVAS_ORTHO_MAX_SIDE, R * K < 2^30, G * R * K < 2^31.  dt: type of update and weights.
+/* Host only.  shape: G, R, K, all >= 1, min(R, K) <= CANVAS_ORTHO_MAX_SIDE, R * K < 2^30, G * R * K < 2^31, and fewer
+ * than 2^24 blocks of 64 x 64 in all.  dt: type of update and weights.
  * steps: 0 .. CANVAS_ORTHO_MAX_STEPS (0: the normalised matrix itself).  flags: 0 or CANVAS_ORTHO_NESTEROV.
  * Errors: BAD_ARG, UNSUPPORTED. */
 int canvas_ortho_compile(const int64_t shape[3], canvas_dtype dt, int32_t steps, uint32_t flags, canvas_ortho** out);

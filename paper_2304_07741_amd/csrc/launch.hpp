@@ -20,6 +20,13 @@ inline void allow_lds(std::atomic<uint64_t>& asked, const void* kernel, int byte
     if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess) asked.fetch_or(bit, std::memory_order_relaxed);
 }
 
+// A launch has fewer than 2^32 threads along x: at most so many workgroups of `threads`, or rows of them.
+inline int64_t most_workgroups(int threads) { return (((int64_t)1 << 32) - 1) / threads; }
+inline dim3 rows_of_workgroups(int64_t workgroups, int threads) {
+    const int64_t most = most_workgroups(threads), rows = (workgroups + most - 1) / most;
+    return dim3((unsigned)((workgroups + rows - 1) / rows), (unsigned)rows);
+}
+
 struct TimingEvents {
     hipEvent_t start = nullptr, stop = nullptr;
 };

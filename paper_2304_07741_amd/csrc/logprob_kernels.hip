@@ -569,8 +569,8 @@ __global__ __launch_bounds__(256) void k_bwd(Shape s, Bwd a, int pieces) {
     }
 }
 
-constexpr int64_t kMostBlocks = 1 << 24;
-unsigned grid_of(int64_t n) { return (unsigned)(n < kMostBlocks ? n : kMostBlocks); }
+// (the kernels walk over what more workgroups than a launch can have would take)
+unsigned grid_of(int64_t n, int threads) { return (unsigned)std::min(n, most_workgroups(threads)); }
 uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
 int64_t classes_per_thread(int64_t length, int threads, int vec) { return (length + (int64_t)threads * vec - 1) / ((int64_t)threads * vec) * vec; }
 
@@ -579,7 +579,7 @@ void fwd(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
     const int64_t tasks = s.rows * p.segments;
     const size_t lds = TOP ? 8ull * (THREADS + kTogether + (s.top + kSpare) * classes_per_thread(p.length, THREADS, Type<T>::kVec)) : 0;
     constexpr int per = segments_of(THREADS, TOP);
-    CANVAS_LAUNCH((k_fwd<T, THREADS, TOP>), dim3(grid_of((tasks + per - 1) / per)), dim3(THREADS * per), lds, stream, s, p, a);
+    CANVAS_LAUNCH((k_fwd<T, THREADS, TOP>), dim3(grid_of((tasks + per - 1) / per, THREADS * per)), dim3(THREADS * per), lds, stream, s, p, a);
 }
 template <class T>
 void forward_of(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
@@ -589,14 +589,14 @@ void forward_of(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream)
         s.top ? fwd<T, 256, true>(s, p, a, stream) : fwd<T, 256, false>(s, p, a, stream);
     if (p.segments > 1) {
         const size_t lds = s.top ? 8ull * (kJoin + kTogether + (s.top + kSpare) * kJoinKeys) : 0;
-        CANVAS_LAUNCH(k_join<T>, dim3(grid_of(s.rows)), dim3(kJoin), lds, stream, s, p, a);
+        CANVAS_LAUNCH(k_join<T>, dim3(grid_of(s.rows, kJoin)), dim3(kJoin), lds, stream, s, p, a);
     }
 }
 template <class T>
 void backward_of(const Shape& s, const Bwd& a, hipStream_t stream) {
     const int piece = 64 * Type<T>::kVec * kBwdVecs;
     const int pieces = (int)((s.classes + piece - 1) / piece);
-    CANVAS_LAUNCH(k_bwd<T>, dim3(grid_of((s.rows * pieces + 3) / 4)), dim3(256), 0, stream, s, a, pieces);
+    CANVAS_LAUNCH(k_bwd<T>, dim3(grid_of((s.rows * pieces + 3) / 4, 256)), dim3(256), 0, stream, s, a, pieces);
 }
 
 }  // namespace

@@ -116,7 +116,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_fwd(Shape s, Fwd
     constexpr int V = 16 / sizeof(T), kRows = TPR < 256 ? 256 / TPR : 1;
     __shared__ float buf[16];
     const int t = threadIdx.x % TPR;
-    const int64_t n = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
+    const int64_t n = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kRows + threadIdx.x / TPR;
     if (n >= s.N) return;  // (with several rows per workgroup a row is within a wave: no barriers)
     const int64_t row = n * s.C;
     const bool gated = (PARTS & kPost) && s.gate, silu = s.gate == 2;
@@ -216,13 +216,14 @@ template <class T, int VEC, int KC, int PARTS>
 void maps(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
     const Tiling& t = p.fwd;
     const int64_t tiles = (p.total + (1 << t.log_gx) - 1) >> t.log_gx;
-    CANVAS_LAUNCH((k_maps_fwd<T, VEC, KC, PARTS>), dim3((unsigned)tiles), dim3(t.threads), t.threads / 64 * (1 << t.log_gx) * VEC * 4, stream, s, a, t.log_gx,
+    // (a last row of workgroups that is not full has pieces behind the last one: they write nothing)
+    CANVAS_LAUNCH((k_maps_fwd<T, VEC, KC, PARTS>), rows_of_workgroups(tiles, t.threads), dim3(t.threads), t.threads / 64 * (1 << t.log_gx) * VEC * 4, stream, s, a, t.log_gx,
                   p.pieces, p.total);
 }
 template <class T, int TPR, int KV, int PARTS>
 void rows(const Shape& s, const Fwd& a, hipStream_t stream) {
     constexpr int kBlock = TPR < 256 ? 256 : TPR, kRows = kBlock / TPR;
-    CANVAS_LAUNCH((k_rows_fwd<T, TPR, KV, PARTS>), dim3((unsigned)((s.N + kRows - 1) / kRows)), dim3(kBlock), 0, stream, s, a);
+    CANVAS_LAUNCH((k_rows_fwd<T, TPR, KV, PARTS>), rows_of_workgroups((s.N + kRows - 1) / kRows, kBlock), dim3(kBlock), 0, stream, s, a);
 }
 template <class T, int PARTS>
 void run(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {

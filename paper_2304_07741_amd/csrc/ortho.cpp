@@ -6,6 +6,7 @@
 #include <memory>
 
 #include "abi.hpp"
+#include "launch.hpp"
 #include "ortho_kernels.hpp"
 
 struct canvas_ortho {
@@ -46,6 +47,8 @@ int canvas_ortho_compile(const int64_t shape[3], canvas_dtype dt, int32_t steps,
         s.nesterov = (flags & CANVAS_ORTHO_NESTEROV) != 0;
         s.steps = steps;
         h->plan = canvas::ortho::plan_of(s);
+        // (thin matrices with 2^30 elements and more in all, whose padded transposes would take 256 GB)
+        if (h->plan.workgroups > canvas::most_workgroups(256)) return set_last_error(CANVAS_UNSUPPORTED, "matrices too large or too many for one launch");
         canvas_ortho_info& I = h->info;
         I.n_launches = h->plan.launches;
         I.workspace_bytes = h->plan.workspace_bytes;

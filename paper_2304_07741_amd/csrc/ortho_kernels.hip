@@ -651,6 +651,11 @@ Plan plan_of(const Shape& s) {
     p.launches = 2;
     p.workspace_bytes = up256(8ull * s.G * p.parts);
     if (!s.steps) return p;
+    // (256 x 256 results take 512 threads, less 256; symmetric products have few tiles where there are many matrices)
+    auto longest = [&](const Cut& c) { p.workgroups = std::max(p.workgroups, (int64_t)c.tiles * s.G * (c.side == 256 ? 2 : 1)); };
+    p.workgroups = (int64_t)blocks(s.K, 64) * blocks(s.R, 64);
+    longest(cut_of(false, s.m, s.n, padded(s.m), s.G));
+    if (s.tall) longest(cut_of(false, s.n, s.m, padded(s.m), s.G));
     const Cut gram = cut_of(true, s.m, s.m, padded(s.n), s.G), square = cut_of(true, s.m, s.m, padded(s.m), s.G);
     for (const Cut& c : {gram, square})
         if (c.splits > 1) p.part_bytes = std::max<uint64_t>(p.part_bytes, 4ull * c.side * c.side * c.tiles * c.splits * s.G);

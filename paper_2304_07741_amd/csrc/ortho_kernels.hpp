@@ -21,6 +21,7 @@ struct Plan {
     bool small = false;       // one launch of ortho_small_kernels.hip, without a workspace
     int parts = 0;            // workgroups per matrix that square and sum
     uint64_t part_bytes = 0;  // of sums that are cut into parts
+    int64_t workgroups = 0;   // of the longest launch, of 256 threads each
 };
 Plan plan_of(const Shape& s);
 

@@ -3,8 +3,10 @@
 //
 //   overlap   calls whose tensors share bytes where a call writes are refused before anything is launched, others are not
 //   lds       every launch with more than 64 KB of LDS has asked for as much, whatever shapes came before it
+//   threads   no launch has 2^32 threads or more along a dimension, over all shapes that the headers accept
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <cstdio>
 #include <cstring>
@@ -84,6 +86,55 @@ static int ortho_step(int64_t g, int64_t r, int64_t k, canvas_dtype dt, int step
     const int rc = canvas_ortho_step(h, f(0), f(1), f(2), 0.9, f(3), f(4), 0.1, 0.0, place(5), place(6), kSpace, info.workspace_bytes, nullptr);
     canvas_ortho_destroy(h);
     return rc;
+}
+
+static int logprob_forward_and_backward(int64_t rows, int64_t classes, canvas_dtype dt, int top) {
+    canvas_logprob* h = nullptr;
+    if (int rc = canvas_logprob_compile(rows, classes, dt, top, nullptr, &h)) return rc;
+    canvas_logprob_info info;
+    canvas_logprob_query(h, &info);
+    auto f = [](int k) { return static_cast<float*>(place(k)); };
+    g_launches.clear();
+    int rc = canvas_logprob_forward(h, place(0), classes, 1.f, nullptr, 0, (int64_t*)place(1), f(2), f(3), f(4), (int32_t*)place(5), kSpace, info.workspace_bytes, nullptr);
+    if (!rc) rc = canvas_logprob_backward(h, place(0), classes, 1.f, nullptr, 0, (int64_t*)place(1), f(6), f(7), place(8), classes, kSpace, info.workspace_bytes, nullptr);
+    canvas_logprob_destroy(h);
+    return rc;
+}
+
+// ---------------------------------------------------------------- threads
+
+static void threads() {
+    constexpr uint64_t kMost = (uint64_t)1 << 32;
+    auto look = [](int rc, bool may_refuse, const std::string& what) {
+        if (may_refuse && rc == CANVAS_UNSUPPORTED) return expect(g_launches.empty(), what + " refused");
+        bool ok = rc == CANVAS_OK && !g_launches.empty();
+        for (const Launch& l : g_launches)
+            ok &= (uint64_t)l.grid.x * l.block.x < kMost && (uint64_t)l.grid.y * l.block.y < 65536 && l.grid.z == 1 && l.block.x <= 1024 && l.grid.x > 0 && l.grid.y > 0;
+        expect(ok, what);
+    };
+    const int64_t pixels[] = {1, 1 << 20, (1 << 24) + 1, (1 << 26) - 1, (1 << 26) + 3, (1 << 27) + 1, (1 << 28) - 16, (1 << 28) + 1, (1 << 30) + 5, 0x7fffffff};
+    for (canvas_dtype dt : {CANVAS_F32, CANVAS_BF16})
+        for (int64_t p : {1, 2, 3, 8, 49})
+            for (int64_t np : pixels)
+                for (int64_t c : {1, 16, 64, 129, 512, 1024})
+                    for (uint32_t parts = 1; parts <= 3; parts++)
+                        look(norm_forward_and_backward(std::max<int64_t>(1, np / p), c, p, dt, parts, 0), false,
+                             "norm " + std::to_string(np / p) + " x " + std::to_string(c) + " x " + std::to_string(p));
+    for (canvas_dtype dt : {CANVAS_F32, CANVAS_BF16})
+        for (int64_t rows : pixels)
+            for (int64_t classes : {1, 10, 2000, 9000})
+                for (int top : {0, 5, 64}) {
+                    if (rows * classes > (int64_t)1 << 41) continue;
+                    look(logprob_forward_and_backward(rows, classes, dt, top), false, "logprob " + std::to_string(rows) + " x " + std::to_string(classes) + " top " + std::to_string(top));
+                }
+    for (int64_t g : {1, 7, 1000, 65535})
+        for (int64_t m : {1, 2, 33, 64, 65, 300, 4000, 16384})
+            for (int64_t n : pixels)
+                for (int tall = 0; tall < 2; tall++)
+                    for (int steps : {0, 1, 5}) {
+                        g_launches.clear();
+                        look(ortho_step(g, tall ? n : m, tall ? m : n, CANVAS_BF16, steps), true, "ortho " + std::to_string(g) + " of " + std::to_string(m) + " x " + std::to_string(n));
+                    }
 }
 
 // ---------------------------------------------------------------- lds
@@ -280,6 +331,7 @@ int main(int argc, char** argv) {
         ortho_overlap();
     }
     if (what == "lds") lds();
+    if (what == "threads") threads();
     printf("%s cases %ld wrong %ld\n", what.c_str(), g_cases, g_wrong);
     return g_cases && !g_wrong ? 0 : 1;
 }

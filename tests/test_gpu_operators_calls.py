@@ -177,3 +177,55 @@ def test_nothing_is_read_that_a_call_writes():
     B.canvas_logprob_backward(lp.handle, logits, 100, 1.0, None, 0, tokens, d, None, wide[:, 50:], 100, lp.ws)
     assert torch.equal(wide[:, 50:], want) and torch.equal(logits, before)
     lp.close()
+
+
+def _periodic(out, small, rows, what):
+    """Row i of `out` is row i % n of `small`, bit by bit."""
+    n = small.shape[0]
+    assert torch.equal(out[: rows // n * n].view(rows // n, *small.shape), small.expand(rows // n, *small.shape)), what
+    assert torch.equal(out[rows // n * n :], small[: rows % n]), what
+
+
+@pytest.mark.parametrize("rows,classes,top", [((1 << 26) + 5, 2, 0), ((1 << 24) + 3, 3, 33)])
+def test_more_rows_than_a_launch_has_workgroups(rows, classes, top):
+    """Log probabilities: 2^32 threads and more would be needed at once; every row has the bits of a plan of 14 rows."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(6)
+    logits, tokens = torch.randn(14, classes, generator=gen, device="cuda").bfloat16(), torch.arange(14, device="cuda") % classes
+    d = torch.randn(14, generator=gen, device="cuda")
+    small = harness.LogprobRunner(14, classes, "bf16", top_k=top)
+    want = {**small.forward(logits, tokens), **small.backward(logits, tokens, d, d)}
+    which = torch.arange(rows, device="cuda") % 14
+    r = harness.LogprobRunner(rows, classes, "bf16", top_k=top)
+    for t in [*r.out.values(), *r.grads.values()]:
+        t.fill_(-7)
+    many = (logits[which], tokens[which])
+    dd = d[which]
+    got = {**r.forward(*many), **r.backward(*many, dd, dd)}
+    for k, v in want.items():
+        _periodic(got[k], v, rows, k)
+    small.close()
+    r.close()
+
+
+@pytest.mark.parametrize("n,pixels", [((1 << 26) + 3, 2), ((1 << 28) + 5, 1)])
+def test_more_pixels_than_a_launch_has_workgroups(n, pixels):
+    """Norms of one channel: x' and u of every image have the bits of a plan of seven images."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(7)
+    x, z = (torch.randn(7, 1, pixels, 1, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    w = [torch.full((1,), v, device="cuda") for v in (0.5, 2.0, 0.7)]
+    small = harness.NormRunner((7, 1, pixels, 1), "bf16", BOTH, eps=0.1)
+    out = small.forward(x, z, None, *w)
+    want = {**out, **{k: v for k, v in small.backward(out["x_out"], z, None, *w, dx_out=x, du=z).items() if k in ("dx", "dz")}}
+    which = torch.arange(n, device="cuda") % 7
+    r = harness.NormRunner((n, 1, pixels, 1), "bf16", BOTH, eps=0.1)
+    for t in [*r.out.values(), *r.grads.values()]:
+        t.fill_(-7)
+    many = [t[which] for t in (x, z)]
+    out = r.forward(*many[:2], None, *w)
+    got = {**out, **r.backward(out["x_out"], many[1], None, *w, dx_out=many[0], du=many[1])}
+    for k, v in want.items():
+        _periodic(got[k], v, n, k)
+    small.close()
+    r.close()

@@ -37,3 +37,7 @@ def test_tensors_that_share_bytes_are_refused(program):
 
 def test_lds_is_asked_for_whatever_shapes_came_before(program):
     assert _look(program, "lds") > 200
+
+
+def test_no_launch_has_too_many_threads(program):
+    assert _look(program, "threads") > 1000
