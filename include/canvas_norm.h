@@ -17,7 +17,7 @@
  *   zh = z r2, q = D act scale w_post, t2 = mean_c(q zh):  dz = r2 (q - zh t2),  dgate = D act'(gate) scale w_post zh
  *   dw_post[c] = scale[c] K,  dscale[c] = w_post[c] K,  K = sum D act zh           (sums over n, h, w)
  *
- * Everything is computed in fp32 and rounded once where it is stored; u is computed from x' before its rounding, and backward
+ * Everything is computed in fp32 (the means of squares too: |z| and |x'| up to 1e19) and rounded once where it is stored; u is computed from x' before its rounding, and backward
  * computes that x' again from x, z and the gate (the rounded one would put 2^-9 of every term into the sums of dw_pre, and D
  * is a difference of nearly equal terms where the channels are few).
  * Deterministic: no atomics, sums in a fixed order.

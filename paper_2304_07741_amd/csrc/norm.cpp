@@ -63,6 +63,7 @@ int canvas_norm_compile(const int64_t shape[4], canvas_dtype dt, uint32_t parts,
         s.pre = (parts & CANVAS_NORM_PRE) != 0;
         s.gate = (int)gate;
         s.eps = eps;
+        while (s.down * s.down * s.C > 1.f) s.down *= 0.5f;
         h->inference = (flags & CANVAS_OPT_INFERENCE) != 0;
         h->plan = canvas::norm::plan_of(s);
         canvas_norm_info& I = h->info;

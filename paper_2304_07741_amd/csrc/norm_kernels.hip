@@ -36,7 +36,7 @@ __global__ __launch_bounds__(512) void k_maps_fwd(Shape s, Fwd a, int log_gx, in
     extern __shared__ float lds[];
     const int GX = 1 << log_gx, gx = threadIdx.x & (GX - 1), cy = threadIdx.x >> log_gx, CY = blockDim.x >> log_gx;
     const Where at = where_of<VEC>(s, pieces, total, (int64_t)tile::xcd_sequence() * GX + gx);
-    const float inv = 1.f / s.C;
+    const float inv = 1.f / s.C / (s.down * s.down);
     const bool gated = (PARTS & kPost) && s.gate, silu = s.gate == 2;
     constexpr int K = KC ? KC : 1;
     Vec<T, VEC> x[K], z[K], g[K];
@@ -57,7 +57,10 @@ __global__ __launch_bounds__(512) void k_maps_fwd(Shape s, Fwd a, int log_gx, in
         each([&](int k, int c) {
             if (!KC) load_z(k, c);
 #pragma unroll
-            for (int e = 0; e < VEC; e++) r2[e] += z[k].at(e) * z[k].at(e);
+            for (int e = 0; e < VEC; e++) {
+                const float v = z[k].at(e) * s.down;
+                r2[e] += v * v;
+            }
         });
         over_channels<VEC>(r2, gx, GX, lds);
 #pragma unroll
@@ -83,7 +86,8 @@ __global__ __launch_bounds__(512) void k_maps_fwd(Shape s, Fwd a, int log_gx, in
 #pragma unroll
         for (int e = 0; e < VEC; e++) {
             y[k][e] = joined(k, e, sw);
-            t[e] += y[k][e] * y[k][e];
+            const float v = y[k][e] * s.down;
+            t[e] += v * v;
         }
         if ((PARTS & kPost) && at.in) store<T, VEC>(a.x_out, at.base + c * s.P, y[k]);
     });
@@ -120,7 +124,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_fwd(Shape s, Fwd
     if (n >= s.N) return;  // (with several rows per workgroup a row is within a wave: no barriers)
     const int64_t row = n * s.C;
     const bool gated = (PARTS & kPost) && s.gate, silu = s.gate == 2;
-    const float inv = 1.f / s.C;
+    const float inv = 1.f / s.C / (s.down * s.down);
     Vec<T, V> x[KV], z[KV], g[KV];
 #pragma unroll
     for (int k = 0; k < KV; k++) {
@@ -134,7 +138,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_fwd(Shape s, Fwd
 #pragma unroll
         for (int k = 0; k < KV; k++)
 #pragma unroll
-            for (int e = 0; e < V; e++) r2 += z[k].at(e) * z[k].at(e);
+            for (int e = 0; e < V; e++) {
+                const float v = z[k].at(e) * s.down;
+                r2 += v * v;
+            }
         r2 = rsqrtf(over_row<TPR>(r2, buf) * inv + s.eps);
         if (a.r2 && t == 0) a.r2[n] = r2;
     }
@@ -160,7 +167,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_fwd(Shape s, Fwd
     for (int k = 0; k < KV; k++) {
         joined(k, y);
 #pragma unroll
-        for (int e = 0; e < V; e++) r1 += y[e] * y[e];
+        for (int e = 0; e < V; e++) {
+            const float v = y[e] * s.down;
+            r1 += v * v;
+        }
         if (PARTS & kPost) store_row<T, V>(a.x_out, row, (k * TPR + t) * V, s.C, y);
     }
     if (!(PARTS & kPre)) return;

@@ -13,6 +13,7 @@ struct Shape {
     bool bf16 = false, post = false, pre = false;
     int gate = 0;  // canvas_gate
     float eps = 0.f;
+    float down = 1.f;  // the power of two at C^-1/2 or below: squares are summed of values times it, so that the sum has the range of the mean
 };
 
 // How maps are cut: pieces side by side in a workgroup, its threads, channels that a thread holds.

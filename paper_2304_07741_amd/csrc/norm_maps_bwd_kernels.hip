@@ -102,7 +102,7 @@ __global__ __launch_bounds__(512, KC == 2 ? 3 : 1) void k_maps_bwd(Shape s, Bwd 
             });
             over_channels<VEC>(t1, gx, GX, lds);
 #pragma unroll
-            for (int e = 0; e < VEC; e++) t1[e] *= inv * r1[e] * r1[e] * r1[e];
+            for (int e = 0; e < VEC; e++) t1[e] = t1[e] * inv * r1[e] * r1[e] * r1[e];  // (the power alone may leave the range)
         }
         each([&](int k, int c) {
             again(k, c, true);
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(512, KC == 2 ? 3 : 1) void k_maps_bwd(Shape s, Bwd 
         if (kIsPost) {
             over_channels<VEC>(t2, gx, GX, lds);
 #pragma unroll
-            for (int e = 0; e < VEC; e++) t2[e] *= inv * r2[e] * r2[e];
+            for (int e = 0; e < VEC; e++) t2[e] = t2[e] * inv * r2[e] * r2[e];
             each([&](int k, int c) {
                 again(k, c, true);
                 if (!KC) branch(k);

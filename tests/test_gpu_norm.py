@@ -220,3 +220,25 @@ def test_more_and_more_channels_in_one_process(dtype):
         want = _reference(shape, maps, weights, B.CANVAS_GATE_SILU, True)
         for k, g in _run(shape, dtype, BOTH, B.CANVAS_GATE_SILU, maps, weights).items():
             assert_close(g.reshape(want[k].shape), want[k], TOL[dtype], f"{shape} {dtype} {k}")
+
+
+@pytest.mark.parametrize("scale,eps", [(1e15, 1e-3), (1e18, 1e-3), (1e-13, 1e-30), (0.0, 1e-30)])
+@pytest.mark.parametrize("shape", [(2, 64, 6, 6), (3, 200, 1, 1), (1, 2100, 3, 3), (2, 16, 1, 2), (2, 5000, 1, 1)], ids=lambda s: "x".join(map(str, s)))
+def test_gradients_of_maps_far_from_one(shape, scale, eps):
+    """The third power of 1 / |x'| leaves the range of fp32 long before the gradient does, which falls and rises as the first one."""
+    maps, weights = _case(shape, "f32", BOTH, B.CANVAS_GATE_SILU, 6)
+    maps["x"], maps["z"] = maps["x"] * scale, maps["z"] * scale
+    weights["scale"] = weights["scale"] * max(scale, 1e-20)          # (x' is of the size of x)
+    n, c, h, w = shape
+    m = {k: v.double().reshape(n, c, h * w) for k, v in maps.items()}
+    wt = {k: v.double() for k, v in weights.items()}
+    y, _ = ref.norm_forward(m["x"], m["z"], m["g"], wt["w_post"], wt["scale"], wt["w_pre"], B.CANVAS_GATE_SILU, eps)
+    want = ref.norm_backward(y, m["z"], m["g"], wt["w_post"], wt["scale"], wt["w_pre"], B.CANVAS_GATE_SILU, eps, None, m["du"])
+    r = harness.NormRunner(shape, "f32", BOTH, gate=B.CANVAS_GATE_SILU, eps=eps)
+    d = {k: v.cuda() for k, v in {**maps, **weights}.items()}
+    block = (d["z"], d["g"], d["w_post"], d["scale"], d["w_pre"])
+    out = r.forward(d["x"], *block)
+    got = r.backward(out["x_out"], *block, du=d["du"])
+    for k in ("dx", "dz", "dgate", "dw_pre"):
+        assert_close(got[k].double().cpu().numpy().reshape(want[k].shape), want[k].numpy(), TOL["f32"], f"{scale} {k}")
+    r.close()
