@@ -9,8 +9,8 @@
  *   update = X (transposed back),  master' = (1 - lr decay) master - lr update,  weights = master' in the plan's type
  *
  * The products run on the matrix units with fp32 sums.  Each operand is a pair of fp16 numbers that together hold 22 bits of
- * it, and a product adds the three pairings that matter, which is as exact as products in fp32 (|X| <= 1.3 throughout, so a
- * fixed scale keeps both numbers in range).  Where the longer side is several times the shorter one, two steps are joined, which
+ * it, and a product adds the three pairings that matter, which is as exact as products in fp32 (|X| <= 1.3 throughout; a
+ * power of two per matrix keeps both numbers in range where X is small).  Where the longer side is several times the shorter one, two steps are joined, which
  * changes the order of the products and not what they are: both polynomials of A are multiplied before X is.  The sum of squares is kept in 64 bits: gradients of any size that fp32 holds are
  * in range.  A matrix of zeros gives zeros; infinities and NaN make their own matrix NaN and no other.
  *

@@ -2,7 +2,9 @@
 //
 // A matrix of fp32 values v is held as two fp16 planes: hi = fp16(2^12 v), lo = fp16(2^12 v - hi).  |X| <= 1.3 and |b A + c A A + a I| <= 3.45
 // in every step and the product of two of the latter below 12 (spectral norms bound the elements), so hi stays in fp16's range, and lo
-// keeps 11 more bits of every element above 2^-15 of the largest possible one.  A product of two such matrices is hi hi + hi lo + lo hi on the matrix units with fp32
+// keeps 11 more bits of every element above 2^-15 of the largest possible one.  Where |v| is not far above the 1e-7 that is added to it, or
+// below, X is small: its planes hold 2^up X with |2^up X| in [1/2, 1) at the start, and each step, which makes X at most 3.4445 times as
+// large, takes as much from `up` until nothing is left.  A product of two such matrices is hi hi + hi lo + lo hi on the matrix units with fp32
 // sums; lo lo is below 2^-22 of a term.
 //
 // Per step, with both X [m][n] and its transpose at hand so that every operand is read along the index that is summed over:
@@ -47,6 +49,10 @@ struct Pair {
     int64_t plane, step;
     int ld;
 };
+
+// What the planes of X are scaled by beyond 2^12, where the start's exponent is `up`, after steps that can have made X 2^grown times as large.
+__device__ __forceinline__ int exponent_after(int up, int grown) { return up > grown ? up - grown : 0; }
+constexpr int grown_by(int steps) { return (steps * 1785 + 999) / 1000; }  // log2(3.4445) = 1.7843 per step
 
 __device__ __forceinline__ uint32_t pack_pair(float v) {  // v scaled: hi in the low half, lo in the high one
     const _Float16 h = (_Float16)v, l = (_Float16)(v - (float)h);
@@ -112,8 +118,12 @@ __global__ __launch_bounds__(kThreads) void k_mix(Shape s, Args a, double* sums)
     if (threadIdx.x == 0) sums[blockIdx.y * gridDim.x + blockIdx.x] = buf[0];
 }
 
-// 1 / (|v| + 1e-7) of this workgroup's matrix.
-__device__ double inverse_norm(const double* sums, int parts) {
+// 1 / (|v| + 1e-7) of this workgroup's matrix, and the power of two that brings |v| / (|v| + 1e-7) to [1/2, 1).
+struct Norm {
+    double inverse;
+    int up;
+};
+__device__ Norm norm_of(const double* sums, int parts) {
     __shared__ double buf[kThreads / 64];
     double t = 0;
     for (int k = threadIdx.x; k < parts; k += kThreads) t += sums[k];
@@ -124,11 +134,12 @@ __device__ double inverse_norm(const double* sums, int parts) {
     t = 0;
 #pragma unroll
     for (int w = 0; w < kThreads / 64; w++) t += buf[w];
-    return 1.0 / (sqrt(t) + kEps);
+    const double inverse = 1.0 / (sqrt(t) + kEps), part = sqrt(t) * inverse;
+    return Norm{inverse, part > 0 && part < 0.5 ? 1022 - (int)(__double_as_longlong(part) >> 52) : 0};
 }
 
 // X and X^T of the normalised direction, 64 x 64 elements per workgroup through LDS; zeros behind the columns.
-__global__ __launch_bounds__(kThreads) void k_start(Shape s, Args a, const double* sums, int parts, Pair x, Pair xt) {
+__global__ __launch_bounds__(kThreads) void k_start(Shape s, Args a, const double* sums, int parts, int* ups, Pair x, Pair xt) {
     __shared__ uint32_t img[64][65];
     const unsigned wide = (unsigned)((s.K + 63) / 64), by = blockIdx.x / wide;
     const int64_t len = s.R * s.K, r0 = (int64_t)by * 64, c0 = (int64_t)(blockIdx.x - by * wide) * 64;
@@ -151,7 +162,9 @@ __global__ __launch_bounds__(kThreads) void k_start(Shape s, Args a, const doubl
                 if (col + e < s.K) v[k][e] = direction(s, a, i + e, m ? m[i + e] : 0.f);
         }
     }
-    const double inv = inverse_norm(sums + (int64_t)blockIdx.y * parts, parts);
+    const Norm norm = norm_of(sums + (int64_t)blockIdx.y * parts, parts);
+    const double inv = ldexp(norm.inverse, norm.up);
+    if (blockIdx.x == 0 && threadIdx.x == 0) ups[blockIdx.y] = norm.up;
     // four pairs side by side
     auto put = [&](const Pair& to, int64_t row, int64_t col, const uint32_t (&p)[4]) {
         _Float16* at = to.hi + blockIdx.y * to.step + row * to.ld + col;
@@ -186,7 +199,7 @@ __global__ __launch_bounds__(kThreads) void k_start(Shape s, Args a, const doubl
 
 // Plans without products: the normalised direction itself.
 __global__ __launch_bounds__(kThreads) void k_normalised(Shape s, Args a, const double* sums, int parts) {
-    const double inv = inverse_norm(sums + (int64_t)blockIdx.y * parts, parts);
+    const double inv = norm_of(sums + (int64_t)blockIdx.y * parts, parts).inverse;
     const int64_t len = s.R * s.K, k = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (k >= len) return;
     const int64_t i = blockIdx.y * len + k;
@@ -207,7 +220,17 @@ struct Product {
     // per workgroup, which writes back its L2: 89 us against 10 for the Gram matrix of 512 x 2048.)
     int splits;
     f32x4* parts;
+    // Products with X: the exponents of the matrices, by how much the X that is read and the X that is written can have grown.
+    const int* ups = nullptr;
+    int grown_in = 0, grown_out = 0;
 };
+// The power of two that takes results from the scale of the operands' planes to that of the result's, apart from 2^12 (kLast: 2^24).
+template <Kind KIND>
+__device__ __forceinline__ int exponent_of(const Product& g, int grp) {
+    if (KIND == kSquare || !g.ups) return 0;
+    const int up = g.ups[grp], in = exponent_after(up, g.grown_in);
+    return KIND == kGram ? -2 * in : KIND == kUpdate ? exponent_after(up, g.grown_out) - in : -in;
+}
 
 struct Tile {
     int grp, i0, j0;
@@ -271,7 +294,7 @@ __device__ __forceinline__ void put_pairs(_Float16* to, int64_t plane, const uin
 // An image of BM x BN results, complete in LDS, to where it belongs: first as fp32, row by row; pairs are left in the same places,
 // which the transpose is written from.
 template <int BM, int BN, int THREADS, Kind KIND>
-__device__ __forceinline__ void emit(const Shape& s, const Args& args, const Product& g, int grp, int i0, int j0, bool diagonal, uint32_t* img) {
+__device__ __forceinline__ void emit(const Shape& s, const Args& args, const Product& g, int grp, int exponent, int i0, int j0, bool diagonal, uint32_t* img) {
     constexpr int kChunks = BN / 8;
 #pragma unroll 2
     for (int e = threadIdx.x; e < BM * kChunks; e += THREADS) {
@@ -284,7 +307,7 @@ __device__ __forceinline__ void emit(const Shape& s, const Args& args, const Pro
         if (KIND == kLast) {
             if (i >= g.rows || j >= g.cols) continue;
 #pragma unroll
-            for (int k = 0; k < 8; k++) v[k] *= 1.f / (kScale * kScale);
+            for (int k = 0; k < 8; k++) v[k] = ldexpf(v[k], exponent - 24);
             const int64_t first = (int64_t)grp * s.R * s.K + (int64_t)i * s.K + j;
             if ((s.K & 7) == 0)
                 finish_eight(s, args, first, v);
@@ -302,7 +325,7 @@ __device__ __forceinline__ void emit(const Shape& s, const Args& args, const Pro
         uint32_t p[8];
 #pragma unroll
         for (int k = 0; k < 8; k++) {
-            float w = v[k] * (1.f / kScale);
+            float w = KIND == kSquare ? v[k] * (1.f / kScale) : ldexpf(v[k], exponent - 12);
             if (KIND == kSquare) {
                 const uint32_t hw = ah[k >> 1] >> ((k & 1) * 16), lw = al[k >> 1] >> ((k & 1) * 16);
                 w = kC * w + (kB * (of_half(hw & 0xffffu) + of_half(lw & 0xffffu)) + (i == j + k ? kA * kScale : 0.f));
@@ -343,7 +366,7 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Shape s, Args args, Pro
     const unsigned seq = tile::xcd_sequence();
     const int task = seq / g.splits, split = seq - task * g.splits;
     const Tile at_tile = tile_of<BM, BN, KIND>(g, task);
-    const int grp = at_tile.grp, i0 = at_tile.i0, j0 = at_tile.j0;
+    const int grp = at_tile.grp, i0 = at_tile.i0, j0 = at_tile.j0, exponent = exponent_of<KIND>(g, grp);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = wave / F::WJ * (TM * 32), wj = wave % F::WJ * (TN * 32);
 
@@ -457,7 +480,7 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Shape s, Args args, Pro
                 for (int y = 0; y < TN; y++) to_image<BN>(img, acc[x][y], r, wj + y * 32);
             }
             __syncthreads();
-            emit<F::kRows, BN, kThreads, KIND>(s, args, g, grp, i0 + r0, j0, at_tile.diagonal, img);
+            emit<F::kRows, BN, kThreads, KIND>(s, args, g, grp, exponent, i0 + r0, j0, at_tile.diagonal, img);
         }
         return;
     }
@@ -495,7 +518,7 @@ __global__ __launch_bounds__(256) void k_add(Shape s, Args args, Product g) {
 #pragma unroll
     for (int e = 0; e < 4; e++) img[place<32>(wave * 8 + (lane >> 5) * 4 + e, lane & 31)] = __float_as_uint(v[e]);
     __syncthreads();
-    emit<32, 32, 256, KIND>(s, args, g, at.grp, at.i0 + bi * 32, at.j0 + bj * 32, at.diagonal, img);
+    emit<32, 32, 256, KIND>(s, args, g, at.grp, exponent_of<KIND>(g, at.grp), at.i0 + bi * 32, at.j0 + bj * 32, at.diagonal, img);
 }
 
 // Symmetric products of few rows: 32 x 32 results per workgroup, the sum over k shared out among its eight waves, which load their
@@ -550,7 +573,7 @@ __global__ __launch_bounds__(64 * kSlimWaves) void k_slim(Shape s, Args args, Pr
         for (int e = 0; e < 4; e++) img[place<32>(wave * 8 + (lane >> 5) * 4 + e, lane & 31)] = __float_as_uint(v[e]);
     }
     __syncthreads();
-    emit<32, 32, 64 * kSlimWaves, KIND>(s, args, g, at.grp, at.i0, at.j0, at.diagonal, img);
+    emit<32, 32, 64 * kSlimWaves, KIND>(s, args, g, at.grp, exponent_of<KIND>(g, at.grp), at.i0, at.j0, at.diagonal, img);
 }
 
 uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
@@ -661,7 +684,7 @@ Plan plan_of(const Shape& s) {
         if (c.splits > 1) p.part_bytes = std::max<uint64_t>(p.part_bytes, 4ull * c.side * c.side * c.tiles * c.splits * s.G);
     const int twos = by_twos(s) ? s.steps / 2 : 0, ones = s.steps - twos;
     p.launches += ones * (2 + (gram.splits > 1)) + (ones + 4 * twos) * (1 + (square.splits > 1));
-    p.workspace_bytes += 2 * up256(4ull * s.G * s.m * padded(s.n)) + 2 * up256(4ull * s.G * s.n * padded(s.m)) + 3 * up256(4ull * s.G * s.m * padded(s.m)) + up256(p.part_bytes);
+    p.workspace_bytes += up256(4ull * s.G) + 2 * up256(4ull * s.G * s.m * padded(s.n)) + 2 * up256(4ull * s.G * s.n * padded(s.m)) + 3 * up256(4ull * s.G * s.m * padded(s.m)) + up256(p.part_bytes);
     return p;
 }
 
@@ -683,6 +706,7 @@ void step(const Shape& s, const Plan& p, const Args& a, hipStream_t stream) {
     };
     double* sums = (double*)take(8ull * s.G * p.parts);
     f32x4* parts = (f32x4*)take(p.part_bytes);
+    int* ups = s.steps ? (int*)take(4ull * s.G) : nullptr;
     const unsigned G = (unsigned)s.G;
     CANVAS_LAUNCH(k_mix, dim3(p.parts, G), dim3(kThreads), 0, stream, s, a, sums);
     if (!s.steps) {
@@ -690,14 +714,15 @@ void step(const Shape& s, const Plan& p, const Args& a, hipStream_t stream) {
         return;
     }
     Pair x[2] = {pair(s.m, s.n), pair(s.m, s.n)}, xt[2] = {pair(s.n, s.m), pair(s.n, s.m)}, q = pair(s.m, s.m), b = pair(s.m, s.m), t = pair(s.m, s.m);
-    CANVAS_LAUNCH(k_start, dim3(blocks(s.K, 64) * blocks(s.R, 64), G), dim3(kThreads), 0, stream, s, a, sums, p.parts, x[0], xt[0]);
+    CANVAS_LAUNCH(k_start, dim3(blocks(s.K, 64) * blocks(s.R, 64), G), dim3(kThreads), 0, stream, s, a, sums, p.parts, ups, x[0], xt[0]);
     const int m = (int)s.m, n = (int)s.n;
     // C = P Q of symmetric matrices that commute
     auto both = [&](const Pair& p, const Pair& q, const Pair& c) { product<kGram>(s, a, Product{p, q, m, m, p.ld, c, c, 0, 0, 0, 0, parts}, stream); };
     auto polynomial = [&](const Pair& q, const Pair& b) { product<kSquare>(s, a, Product{q, q, m, m, q.ld, b, b, 0, 0, 0, 0, parts}, stream); };
     for (int k = 0, at = 0; k < s.steps; k++, at ^= 1) {
         const Pair &from = x[at], &from_t = xt[at], &to = x[at ^ 1], &to_t = xt[at ^ 1];
-        product<kGram>(s, a, Product{from, from, m, m, from.ld, q, q, 0, 0, 0, 0, parts}, stream);
+        const int grown = grown_by(k);
+        product<kGram>(s, a, Product{from, from, m, m, from.ld, q, q, 0, 0, 0, 0, parts, ups, grown}, stream);
         polynomial(q, b);
         Pair left = b;
         if (by_twos(s) && k + 1 < s.steps) {
@@ -709,11 +734,11 @@ void step(const Shape& s, const Plan& p, const Args& a, hipStream_t stream) {
             k++;
         }
         if (k + 1 < s.steps)
-            product<kUpdate>(s, a, Product{left, from_t, m, n, left.ld, to, to_t, 0, 0, 0, 0, parts}, stream);
+            product<kUpdate>(s, a, Product{left, from_t, m, n, left.ld, to, to_t, 0, 0, 0, 0, parts, ups, grown, grown_by(k + 1)}, stream);
         else if (s.tall)
-            product<kLast>(s, a, Product{from_t, left, n, m, left.ld, to, to_t, 0, 0, 0, 0, parts}, stream);
+            product<kLast>(s, a, Product{from_t, left, n, m, left.ld, to, to_t, 0, 0, 0, 0, parts, ups, grown}, stream);
         else
-            product<kLast>(s, a, Product{left, from_t, m, n, left.ld, to, to_t, 0, 0, 0, 0, parts}, stream);
+            product<kLast>(s, a, Product{left, from_t, m, n, left.ld, to, to_t, 0, 0, 0, 0, parts, ups, grown}, stream);
     }
 }
 

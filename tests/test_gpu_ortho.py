@@ -153,3 +153,29 @@ def test_larger_and_larger_small_matrices_in_one_process(dtype):
         grad, _, _ = _inputs(shape, 10)
         want = ref.ortho_step(grad.double(), None, 0, False, 5)
         assert _err(_step(shape, dtype, grad)["update"], want["update"]) <= (TOL_F32 if dtype == "f32" else TOL_BF16)
+
+
+@pytest.mark.parametrize("scale", [1e-38, 1e-30, 1e-20, 1e-14, 1e-12, 1e-11, 1e-10, 1e-9, 1.0, 1e30])
+@pytest.mark.parametrize("shape", [(2, 24, 40), (2, 200, 300), (2, 100, 450), (2, 300, 130), (1, 520, 776)], ids=lambda s: "x".join(map(str, s)))
+def test_gradients_of_any_size_to_the_same_relative_accuracy(shape, scale):
+    """|v| + 1e-7 leaves X small where |v| is, down to 1e-31; every matrix of a call has a size of its own."""
+    grad, _, _ = _inputs(shape, 12)
+    grad = grad * scale
+    if shape[0] > 1:
+        grad[1] *= 1e-3 if scale > 1e-30 else 1e3
+    for steps in (5, 2):
+        want = ref.ortho_step(grad.double(), None, 0, False, steps)["update"]
+        got = _step(shape, "f32", grad, steps=steps)["update"]
+        for g, w in zip(got, want):
+            assert float(w.norm()) > 0 and _err(g, w) <= TOL_F32
+
+
+@pytest.mark.parametrize("scale", [1e-25, 1e-12])
+@pytest.mark.parametrize("shape", [(1, 1700, 6200), (1, 2600, 1300), (14, 1250, 1300)], ids=lambda s: "x".join(map(str, s)))
+def test_small_gradients_in_large_tiles(shape, scale):
+    """The definition in 64 bits is computed on the GPU."""
+    grad, _, _ = _inputs(shape, 13)
+    grad = grad * scale
+    d = grad.double().cuda()
+    want = torch.stack([ref.newton_schulz(m, 5) for m in d]).cpu()
+    assert _err(_step(shape, "f32", grad)["update"], want) <= TOL_F32
