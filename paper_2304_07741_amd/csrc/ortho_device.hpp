@@ -12,6 +12,9 @@ namespace ortho {
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr double kEps = 1e-7;
 
+// 1 / (|v| + 1e-7) from the sum of squares.  (An infinity: NaN, so that the whole matrix is, and not the one element alone.)
+__device__ __forceinline__ double inverse_norm(double squares) { return 1.0 / (sqrt(squares) + kEps) + (squares - squares); }
+
 __device__ __forceinline__ float direction(const Shape& s, const Args& a, int64_t i, float m_new) {
     if (!a.momentum) return a.grad[i];
     return s.nesterov ? (float)(a.grad[i] + a.mu * m_new) : m_new;  // (mu in 64 bits: gradient and momentum may cancel)

@@ -134,7 +134,7 @@ __device__ Norm norm_of(const double* sums, int parts) {
     t = 0;
 #pragma unroll
     for (int w = 0; w < kThreads / 64; w++) t += buf[w];
-    const double inverse = 1.0 / (sqrt(t) + kEps), part = sqrt(t) * inverse;
+    const double inverse = inverse_norm(t), part = sqrt(t) * inverse;
     return Norm{inverse, part > 0 && part < 0.5 ? 1022 - (int)(__double_as_longlong(part) >> 52) : 0};
 }
 

@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kThreads) void k_small(Shape s, Args a) {
     t = 0;
 #pragma unroll
     for (int w = 0; w < kWaves; w++) t += s_sum[w];
-    const double inv = 1.0 / (sqrt(t) + kEps);
+    const double inv = inverse_norm(t);
     for (int i = tid; i < mp * ld; i += kThreads) x[i] = (float)(x[i] * inv);
     __syncthreads();
 

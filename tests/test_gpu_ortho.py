@@ -179,3 +179,15 @@ def test_small_gradients_in_large_tiles(shape, scale):
     d = grad.double().cuda()
     want = torch.stack([ref.newton_schulz(m, 5) for m in d]).cpu()
     assert _err(_step(shape, "f32", grad)["update"], want) <= TOL_F32
+
+
+@pytest.mark.parametrize("steps", [0, 1, 5])
+@pytest.mark.parametrize("shape", [(3, 24, 40), (3, 130, 200), (3, 100, 450)], ids=lambda s: "x".join(map(str, s)))
+def test_an_infinity_makes_its_whole_matrix_nan(shape, steps):
+    grad, _, _ = _inputs(shape, 14)
+    clean = _step(shape, "f32", grad, steps=steps)["update"]
+    for v in (math.inf, -math.inf, math.nan):
+        grad[1, 3, 5] = v
+        got = _step(shape, "f32", grad, steps=steps)["update"]
+        assert torch.isnan(got[1]).all()
+        assert torch.equal(got[0], clean[0]) and torch.equal(got[2], clean[2])
