@@ -10,7 +10,7 @@
 // thread's classes, few in general.  Theirs are read again, spread over the workgroup; what reaches the bound is collected in
 // LDS and ranked by counting.
 //
-// Backward: element by element from the row's (m, log S, entropy).
+// Backward: element by element from the row's (m, log S, entropy, 1 / S).
 //
 // Both are bound by memory on many rows: 4096 x 32768 in bf16 forward 44 us (6.0 TB/s, some of it from the last-level cache),
 // backward 108 us (5.0 TB/s).  With alternatives the search at a row's end is not hidden by other rows' loads: 1500 x 50021
@@ -21,6 +21,7 @@
 
 #include "../../include/canvas_logprob.h"
 #include "device_util.hpp"
+#include "exp_util.hpp"
 #include "launch.hpp"
 #include "tile_util.hpp"
 #include "wave_util.hpp"
@@ -31,7 +32,6 @@ namespace {
 
 using tile::u32x4;
 constexpr float kInf = __builtin_inff(), kLowest = -3.402823466e38f;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kMostClassesLog = 20;
 constexpr uint32_t kMostClasses = 1u << kMostClassesLog;
 static_assert(kMostClasses == CANVAS_LOGPROB_MAX_CLASSES && CANVAS_LOGPROB_MAX_TOP <= 64, "limits of the kernels");
@@ -312,7 +312,7 @@ struct Running {
 
 __device__ __forceinline__ Row row_of(const Running& r) {
     const bool empty = r.sum == 0.f;
-    return Row{r.m, empty ? -kInf : logf(r.sum), empty ? 0.f : logf(r.sum) - r.along / r.sum, 0.f};
+    return Row{r.m, empty ? -kInf : logf(r.sum), empty ? 0.f : logf(r.sum) - r.along / r.sum, empty ? 0.f : 1.f / r.sum};
 }
 template <class T>
 __device__ __forceinline__ void write_token(const Shape& s, const Fwd& a, int64_t row, const Row& r) {
@@ -539,9 +539,11 @@ __global__ __launch_bounds__(256) void k_bwd(Shape s, Bwd a, int pieces) {
             float d[V];
 #pragma unroll
             for (int e = 0; e < V; e++) {
-                const float lp = (Y::at(v[q], e) - r.most) * a.it - r.log_sum;
-                const float p = __builtin_amdgcn_exp2f(lp * kLog2e);
-                d[e] = -p * (g + h * (fmaxf(lp, -300.f) + r.entropy));
+                // (p from the exponent before log S rounds it; a NaN is in what the row left.  Gradients of 8 bits take the exponential as
+                // it is: its 3e-6 at worst is far below their 2e-3, and the other's three operations more cost 9 us at 4096 x 32768)
+                const float x = fmaxf((Y::at(v[q], e) - r.most) * a.it, -300.f);
+                const float p = (sizeof(T) == 4 ? exp_finite(x) : __builtin_amdgcn_exp2f(x * kLog2e)) * r.inverse;
+                d[e] = -p * (g + h * (x - r.log_sum + r.entropy));
                 if (begin + i + e == t) d[e] += g;
                 if (empty) d[e] = 0.f;
             }

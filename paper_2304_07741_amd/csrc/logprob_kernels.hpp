@@ -14,9 +14,9 @@ struct Shape {
 };
 
 // What backward needs of a row: its largest logit (the lowest finite value if there is none), log sum_i exp(z_i - z_max) (-inf for a row
-// with nothing left) and the entropy.
+// with nothing left), the entropy and 1 / sum_i exp(z_i - z_max).
 struct alignas(16) Row {
-    float most, log_sum, entropy, unused;
+    float most, log_sum, entropy, inverse;
 };
 
 // Rows are read in `segments` pieces of `length` classes by `threads` threads.
