@@ -24,8 +24,9 @@ namespace canvas {
 namespace norm {
 namespace {
 
+template <class T>
 __device__ __forceinline__ float act_of(bool silu, float g) {
-    const float s = sigmoid(g);
+    const float s = sigmoid<T>(g);
     return silu ? g * s : s;
 }
 
@@ -71,7 +72,7 @@ __global__ __launch_bounds__(512) void k_maps_fwd(Shape s, Fwd a, int log_gx, in
     }
     auto joined = [&](int k, int e, float sw) {
         float y = x[k].at(e);
-        if (PARTS & kPost) y += sw * (gated ? act_of(silu, g[k].at(e)) : 1.f) * (z[k].at(e) * r2[e]);
+        if (PARTS & kPost) y += sw * (gated ? act_of<T>(silu, g[k].at(e)) : 1.f) * (z[k].at(e) * r2[e]);
         return y;
     };
 #pragma unroll
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_fwd(Shape s, Fwd
 #pragma unroll
         for (int e = 0; e < V; e++) {
             y[e] = x[k].at(e);
-            if (PARTS & kPost) y[e] += sw[e] * w[e] * (gated ? act_of(silu, g[k].at(e)) : 1.f) * (z[k].at(e) * r2);
+            if (PARTS & kPost) y[e] += sw[e] * w[e] * (gated ? act_of<T>(silu, g[k].at(e)) : 1.f) * (z[k].at(e) * r2);
         }
     };
     float y[V], r1 = 0.f;

@@ -86,7 +86,7 @@ __global__ __launch_bounds__(512, KC == 2 ? 3 : 1) void k_maps_bwd(Shape s, Bwd 
         float m[KM][VEC], d[K][VEC];
         auto branch = [&](int k) {
 #pragma unroll
-            for (int e = 0; e < VEC; e++) m[k % KM][e] = kIsPost ? act<GATE>(GATE ? g[k].at(e) : 0.f) * (z[k].at(e) * r2[e]) : 0.f;
+            for (int e = 0; e < VEC; e++) m[k % KM][e] = kIsPost ? act<T, GATE>(GATE ? g[k].at(e) : 0.f) * (z[k].at(e) * r2[e]) : 0.f;
         };
         auto joined = [&](int k, int e) { return kIsPost ? x[k].at(e) + sw[k] * m[k % KM][e] : x[k].at(e); };  // x'
         auto whole = [&](int k, int e, float y) {                                                              // D
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(512, KC == 2 ? 3 : 1) void k_maps_bwd(Shape s, Bwd 
 #pragma unroll
                 for (int e = 0; e < VEC; e++) {
                     float av;
-                    const float slope = act_slope<GATE>(GATE ? g[k].at(e) : 0.f, av);
+                    const float slope = act_slope<T, GATE>(GATE ? g[k].at(e) : 0.f, av);
                     const float D = KC ? d[k][e] : whole(k, e, kIsPre ? joined(k, e) : 0.f), E = D * (sw[k] * r2[e]), zv = z[k].at(e);
                     dz[e] = E * av - zv * t2[e];
                     dg[e] = E * zv * slope;

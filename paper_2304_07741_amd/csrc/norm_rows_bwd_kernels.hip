@@ -78,7 +78,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_bwd(Shape s, Bwd
         float m[KX][V], d[KX][V];
         auto branch = [&](int k) {
 #pragma unroll
-            for (int e = 0; e < V; e++) m[k % KX][e] = kIsPost ? act<GATE>(GATE ? g[k % KX].at(e) : 0.f) * (z[k % KX].at(e) * r2) : 0.f;
+            for (int e = 0; e < V; e++) m[k % KX][e] = kIsPost ? act<T, GATE>(GATE ? g[k % KX].at(e) : 0.f) * (z[k % KX].at(e) * r2) : 0.f;
         };
         auto joined = [&](int k, int e) { return kIsPost ? x[k % KX].at(e) + sw[k % KS][e] * m[k % KX][e] : x[k % KX].at(e); };  // x'
         auto whole = [&](int k, int e, float y) {                                                                               // D
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rows_bwd(Shape s, Bwd
 #pragma unroll
                 for (int e = 0; e < V; e++) {
                     float av;
-                    const float slope = act_slope<GATE>(GATE ? g[k % KX].at(e) : 0.f, av);
+                    const float slope = act_slope<T, GATE>(GATE ? g[k % KX].at(e) : 0.f, av);
                     const float D = kLong ? whole(k, e, kIsPre ? joined(k, e) : 0.f) : d[k % KX][e], E = D * (sw[k % KS][e] * r2), zv = z[k % KX].at(e);
                     dz[e] = E * av - zv * t2;
                     dg[e] = E * zv * slope;

@@ -1,4 +1,6 @@
 """The norms between two blocks against their definition in 64 bits."""
+import math
+
 import pytest
 import torch
 
@@ -241,4 +243,43 @@ def test_gradients_of_maps_far_from_one(shape, scale, eps):
     got = r.backward(out["x_out"], *block, du=d["du"])
     for k in ("dx", "dz", "dgate", "dw_pre"):
         assert_close(got[k].double().cpu().numpy().reshape(want[k].shape), want[k].numpy(), TOL["f32"], f"{scale} {k}")
+    r.close()
+
+
+@pytest.mark.parametrize("gate", [B.CANVAS_GATE_SIGMOID, B.CANVAS_GATE_SILU])
+@pytest.mark.parametrize("shape", [(1, 64, 9, 10), (90, 64, 1, 1), (2, 30, 32, 3), (3, 2100, 1, 3)], ids=lambda s: "x".join(map(str, s)))
+def test_gates_to_a_few_units(shape, gate):
+    """x = 0, z = 1 and weights of one leave x' = act(gate), and a gradient of ones leaves dgate = act'(gate).  Exponential and reciprocal are good to a unit each
+    (2^-23), 1 + e^-g, the root and the products to half of one: 6e-7 in all, held to 8e-7 from gates of -80 on.  (The slope by its
+    terms' size: it is a difference.)"""
+    n = shape[0] * shape[1] * shape[2] * shape[3]
+    g = torch.linspace(-80, 20, n).reshape(shape)
+    one, w = torch.ones(shape), torch.ones(shape[1])
+    r = harness.NormRunner(shape, "f32", B.CANVAS_NORM_POST, gate=gate, eps=1e-12)
+    out = r.forward(torch.zeros(shape).cuda(), one.cuda(), g.cuda(), w.cuda(), w.cuda())
+    x_out = out["x_out"].double().cpu()
+    dgate = r.backward(out["x_out"], one.cuda(), g.cuda(), w.cuda(), w.cuda(), dx_out=one.cuda())["dgate"].double().cpu()
+    a, slope = ref.act(gate, g.double())
+    assert float(((x_out - a).abs() / a.abs().clamp(min=1e-38)).max()) <= 8e-7
+    s = torch.sigmoid(g.double())
+    size = s if gate == B.CANVAS_GATE_SIGMOID else s * (1 + g.double().abs())
+    assert float(((dgate - slope).abs() / size).max()) <= 8e-7
+    r.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 16, 4, 8), (2, 16, 1, 1)], ids=lambda s: "x".join(map(str, s)))
+def test_infinite_gates_and_nan(shape, dtype):
+    """A sigmoid gate of -inf shuts, of +inf opens and passes no gradient on; NaN stays NaN, where it is."""
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    g = torch.zeros(shape)
+    g[0, 0], g[0, 1], g[0, 2], g[0, 3], g[0, 4] = -math.inf, math.inf, math.nan, -1e38, 1e38
+    one, w = torch.ones(shape, dtype=dt, device="cuda"), torch.ones(shape[1], device="cuda")
+    r = harness.NormRunner(shape, dtype, B.CANVAS_NORM_POST, gate=B.CANVAS_GATE_SIGMOID, eps=1e-12)
+    out = r.forward(torch.zeros(shape, dtype=dt, device="cuda"), one, g.to(dt).cuda(), w, w)
+    x = out["x_out"].float().cpu()
+    d = r.backward(out["x_out"], one, g.to(dt).cuda(), w, w, dx_out=one)["dgate"].float().cpu()
+    assert (x[0, [0, 3]] == 0).all() and ((x[0, [1, 4]] - 1).abs() < 1e-6).all() and torch.isnan(x[0, 2]).all()
+    assert (d[0, [0, 1, 3, 4]] == 0).all() and torch.isnan(d[0, 2]).all()
+    assert ((x[0, 5:] - 0.5).abs() < 1e-6).all() and ((d[0, 5:] - 0.25).abs() < 1e-6).all()
     r.close()
