@@ -284,6 +284,9 @@ __device__ void select_keys(int k, uint64_t best, int pieces, uint64_t* lds, OWN
     for (int i = n + threadIdx.x; i < k; i += THREADS) put(i, (uint64_t)0);
 }
 
+// Of differences of logits, for powers of two.  (Finite: a difference of zero times an infinity has no value.)
+__device__ __forceinline__ float scale_of(float it) { return fminf(it * kLog2e, -kLowest); }
+
 // What a segment leaves for the join.
 struct alignas(16) Part {
     float m, sum, along, unused;
@@ -344,7 +347,7 @@ __global__ __launch_bounds__(THREADS * segments_of(THREADS, TOP)) void k_fwd(Sha
     __shared__ float2 sums[4];
     const int tid = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
     const int64_t tasks = s.rows * p.segments, per = segments_of(THREADS, TOP);
-    const float scale = a.it * kLog2e;
+    const float scale = scale_of(a.it);
     for (int64_t first = (int64_t)blockIdx.x * per; first < tasks; first += (int64_t)gridDim.x * per) {
         const int64_t task = first + (per > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0);
         if (per > 1 && task >= tasks) break;  // (a wave of its own: no barriers on this path)
@@ -470,7 +473,7 @@ __global__ __launch_bounds__(kJoin) void k_join(Shape s, Plan p, Fwd a) {
         const int lane = threadIdx.x & 63;
         const Part mine = lane < p.segments ? parts[lane] : Part{kLowest, 0.f, 0.f, 0.f};
         Running whole{mine.m, mine.sum, mine.along * kLog2e};
-        whole.raise(wave::over<1, wave::Max>(mine.m), a.it * kLog2e);
+        whole.raise(wave::over<1, wave::Max>(mine.m), scale_of(a.it));
         whole.sum = wave::over<1, wave::Sum>(whole.sum);
         whole.along = wave::over<1, wave::Sum>(whole.along) * kLn2;
         const Row r = row_of(whole);

@@ -297,3 +297,27 @@ def test_every_probability_in_the_gradient_to_a_few_units(rows, classes):
     # the token's own element is 1 - p
     own = got[torch.arange(rows), tokens] - (1 - p[torch.arange(rows), tokens])
     assert float(own.abs().max()) <= 2e-7
+
+
+@pytest.mark.parametrize("it", [3.4e38, 2.4e38, 1e30, 1e-30, 1.4e-45])
+@pytest.mark.parametrize("classes", [50, 5000, 140001])
+def test_extreme_temperatures(classes, it):
+    """Towards the largest class alone (ties share), and towards a uniform distribution: the largest finite fp32 numbers and the smallest one."""
+    gen = torch.Generator().manual_seed(4)
+    w = torch.randint(-3, 4, (5, classes), generator=gen).float()
+    w[1] = torch.randn(classes, generator=gen)
+    w[2, 1::2] = -math.inf
+    w[3] = 2.0
+    tokens = torch.tensor([0, int(w[1].argmax()), 0, 3, 1])
+    dlp, dent = torch.ones(5), torch.zeros(5)
+    it = float(torch.tensor(it))
+    want = ref.logprob_forward(w.double(), it, None, tokens, 5)
+    grad = ref.logprob_backward(w.double(), 1.0 if it > 1e38 else it, None, tokens, dlp.double(), dent.double())
+    got = _run(w, classes, "f32", tokens, None, it, dlp, dent, 5)
+    _same(got["logprob"], want["logprob"].float(), ABS, 1.0, "logprob")
+    _same(got["entropy"], want["entropy"], ABS, 1.0, "entropy")
+    assert torch.equal(got["top_index"].to(torch.int64), want["top_index"])
+    _same(got["top_logprob"], want["top_logprob"].float(), ABS, 1.0, "top_logprob")
+    assert not torch.isnan(got["dlogits"]).any()
+    if 1e-20 < it < 1e38:
+        _same(got["dlogits"], grad, ABS, float(grad.abs().max()), "dlogits")
