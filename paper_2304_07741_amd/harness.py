@@ -173,8 +173,8 @@ class _PlanRunner:
 class NormRunner(_PlanRunner):
     """The norms between two blocks (include/canvas_norm.h): x' = x + scale act(gate) norm(z) w_post, u = norm(x') w_pre.
 
-    forward() and backward() take the caller's tensors and return the runner's own buffers, which the next call overwrites.
-    Between the two the caller leaves x as it is.
+    forward() and backward() take the caller's tensors and return the runner's own buffers, which the next call overwrites:
+    backward() is of the last forward(), and knows it by the x_out that this returned.  Between the two the caller leaves x as it is.
     """
 
     _destroy = staticmethod(B.canvas_norm_destroy)
@@ -186,7 +186,7 @@ class NormRunner(_PlanRunner):
         self.info = B.canvas_norm_query(self.handle)
         self.post, self.pre, self.gate = bool(parts & B.CANVAS_NORM_POST), bool(parts & B.CANVAS_NORM_PRE), gate != B.CANVAS_GATE_NONE
         self.ws = self._workspace(self.info.workspace_bytes)
-        self.x = None
+        self.x = self.passed = None
         self.out = {}
         if self.post:
             self.out["x_out"] = self._empty(self.shape)
@@ -220,13 +220,17 @@ class NormRunner(_PlanRunner):
         self._of_the_block(z, gate, w_post, scale, w_pre)
         self._map("x", x)
         B.canvas_norm_forward(self.handle, x, z, gate, w_post, scale, w_pre, self.out.get("x_out"), self.out.get("u"), self.ws)
-        self.x = x
-        return self.out
+        self.x, self.passed = x, self.out["x_out"] if self.post else x
+        if not (self.post and self.grads):
+            return self.out
+        # every pass that may have a backward() hands out a tensor object of its own over the one buffer: those of earlier passes are told apart by it
+        self.passed = self.out["x_out"].detach()
+        return {**self.out, "x_out": self.passed}
 
     def backward(self, x_out, z=None, gate=None, w_post=None, scale=None, w_pre=None, dx_out=None, du=None):
-        """Of the runner's last forward(), whose x it has kept.  x_out: what that call returned under that name (x itself in a
-        plan without POST); it says which pass is meant, the kernel computes its values again in fp32."""
-        if self.x is None or x_out is not (self.out["x_out"] if self.post else self.x):
+        """Of the runner's last forward(), whose x it has kept.  x_out: what that very call returned under that name (x itself in a
+        plan without POST); what an earlier one returned is refused.  The kernel computes its values again in fp32."""
+        if self.x is None or x_out is not self.passed:
             raise ValueError("x_out: not the result of this runner's last forward()")
         self._of_the_block(z, gate, w_post, scale, w_pre)
         if self.pre:

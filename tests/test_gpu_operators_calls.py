@@ -229,3 +229,27 @@ def test_more_pixels_than_a_launch_has_workgroups(n, pixels):
         _periodic(got[k], v, n, k)
     small.close()
     r.close()
+
+
+def test_backward_of_an_earlier_pass_is_refused():
+    """Its inputs and statistics are gone: the runner has those of the last forward() only."""
+    shape = (2, 16, 4, 4)
+    r, (x, z, g, dy, du), _ = _norm_case(shape, "f32")
+    w = [torch.ones(16, device="cuda") for _ in range(3)]
+    first = r.forward(x, z, g, *w)
+    second = r.forward(z, x, g, *w)
+    with pytest.raises(ValueError):
+        r.backward(first["x_out"], z, g, *w, dx_out=dy, du=du)
+    with pytest.raises(ValueError):
+        r.backward(r.out["x_out"], x, g, *w, dx_out=dy, du=du)
+    got = {k: v.clone() for k, v in r.backward(second["x_out"], x, g, *w, dx_out=dy, du=du).items()}
+    for k, v in r.backward(second["x_out"], x, g, *w, dx_out=dy, du=du).items():
+        assert torch.equal(v, got[k]), k
+    r.close()
+    r = harness.NormRunner(shape, "f32", B.CANVAS_NORM_PRE)
+    r.forward(x, w_pre=w[0])
+    r.forward(z, w_pre=w[0])
+    with pytest.raises(ValueError):
+        r.backward(x, w_pre=w[0], dx_out=dy, du=du)
+    r.backward(z, w_pre=w[0], dx_out=dy, du=du)
+    r.close()
