@@ -149,6 +149,8 @@ class _PlanRunner:
         if not torch.cuda.is_available():
             raise RuntimeError("no GPU: the library has no CPU path")
         self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device(self.device.type, torch.cuda.current_device())
         self.tdtype = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
         self.cdtype = B.CANVAS_BF16 if dtype == "bf16" else B.CANVAS_F32
 

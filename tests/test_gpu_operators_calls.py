@@ -253,3 +253,16 @@ def test_backward_of_an_earlier_pass_is_refused():
         r.backward(x, w_pre=w[0], dx_out=dy, du=du)
     r.backward(z, w_pre=w[0], dx_out=dy, du=du)
     r.close()
+
+
+def test_a_device_without_its_number_is_the_current_one():
+    x = torch.randn(2, 16, 4, 4, device="cuda")
+    r = harness.NormRunner((2, 16, 4, 4), "f32", B.CANVAS_NORM_PRE, device="cuda")
+    r.forward(x, w_pre=torch.ones(16, device="cuda"))
+    r.close()
+    lp = harness.LogprobRunner(3, 10, "f32", device="cuda")
+    lp.forward(torch.zeros(3, 10, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda"))
+    lp.close()
+    o = harness.OrthoRunner((1, 8, 12), "f32", device="cuda")
+    o.step(torch.randn(1, 8, 12, device="cuda"))
+    o.close()
