@@ -266,13 +266,14 @@ class LogprobRunner(_PlanRunner):
 
     def _arguments(self, logits, tokens, mask):
         """(pitch, mask pitch) of tensors that were checked."""
-        if logits.shape != (self.rows, self.classes) or logits.dtype is not self.tdtype or logits.device != self.device or logits.stride(1) != 1:
+        if logits.shape != (self.rows, self.classes) or logits.dtype is not self.tdtype or logits.device != self.device \
+                or (logits.stride(1) != 1 and self.classes > 1):
             raise ValueError(f"logits: a {(self.rows, self.classes)} tensor of {self.tdtype} on {self.device} with dense rows is needed")
         _check_tensor("tokens", tokens, (self.rows,), torch.int64, self.device)
         pitch = logits.stride(0) if self.rows > 1 else self.classes
         if mask is None:
             return pitch, 0
-        if mask.dtype not in (torch.uint8, torch.bool) or mask.device != self.device or mask.stride(-1) != 1 \
+        if mask.dtype not in (torch.uint8, torch.bool) or mask.device != self.device or (mask.stride(-1) != 1 and self.classes > 1) \
                 or tuple(mask.shape) not in ((self.classes,), (self.rows, self.classes)):
             raise ValueError(f"mask: bytes or truth values of {(self.rows, self.classes)} or {(self.classes,)} on {self.device} are needed")
         return pitch, mask.stride(0) if mask.dim() == 2 and self.rows > 1 else 0

@@ -266,3 +266,22 @@ def test_a_device_without_its_number_is_the_current_one():
     o = harness.OrthoRunner((1, 8, 12), "f32", device="cuda")
     o.step(torch.randn(1, 8, 12, device="cuda"))
     o.close()
+
+
+def test_strides_of_a_single_class_or_row_do_not_matter():
+    tokens = torch.zeros(5, dtype=torch.int64, device="cuda")
+    lp = harness.LogprobRunner(5, 1, "f32", top_k=1)
+    column = torch.randn(1, 5, device="cuda").T            # [5, 1], strides 1 and 5
+    mask = torch.ones(1, 5, dtype=torch.bool, device="cuda").T
+    assert column.stride(1) == 5 and mask.stride(1) == 5
+    out = lp.forward(column, tokens, mask=mask)
+    assert (out["logprob"] == 0).all() and (out["top_index"] == 0).all()
+    mask[2] = False
+    assert float(lp.forward(column, tokens, mask=mask)["logprob"][2]) == float("-inf")
+    assert (lp.backward(column, tokens, torch.ones(5, device="cuda"), mask=mask)["dlogits"] == 0).all()
+    lp.close()
+    lp = harness.LogprobRunner(1, 5, "f32", top_k=1)
+    row = torch.as_strided(torch.arange(50.0, device="cuda"), (1, 5), (3, 1))   # (a pitch that is less than a row)
+    one = torch.as_strided(torch.ones(50, dtype=torch.uint8, device="cuda"), (1, 5), (3, 1))
+    assert int(lp.forward(row, tokens[:1], mask=one)["top_index"][0, 0]) == 4
+    lp.close()
