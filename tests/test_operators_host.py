@@ -165,3 +165,18 @@ def test_ortho_calls_refuse(lib):
     B.canvas_ortho_destroy(h)
     assert lib.canvas_ortho_query(None, None) == -4
     B.canvas_ortho_destroy(None)
+
+
+def test_stream_without_torchs_short_cut(monkeypatch):
+    """The current stream's address comes from torch's public interface where the functions without checks are missing."""
+    import torch
+
+    monkeypatch.setattr(B, "_current_stream", None, raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: type("Stream", (), {"cuda_stream": 12345}))
+    for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+        monkeypatch.delattr(torch._C, name, raising=False)
+    assert B._stream() == 12345
+    monkeypatch.setattr(B, "_current_stream", None, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 3, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 1000 + device, raising=False)
+    assert B._stream() == 1003
