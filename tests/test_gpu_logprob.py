@@ -321,3 +321,39 @@ def test_extreme_temperatures(classes, it):
     assert not torch.isnan(got["dlogits"]).any()
     if 1e-20 < it < 1e38:
         _same(got["dlogits"], grad, ABS, float(grad.abs().max()), "dlogits")
+
+
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_every_element_of_the_gradient_by_its_own_size(shape, dtype, masked):
+    """dlogit = it (g [token] - p (g + h (log p + H))), an element at a time.  Exponents of up to some 30 are rounded two or three times (2^-24 of
+    themselves each) and the sum by 1e-6, so p is good to 1e-5 of itself, and log p + H to 1e-5 of its terms; the token's g adds its own rounding of
+    2^-22, and bf16 the last one of 2^-8."""
+    rows, classes, pad = shape
+    it = 0.8 if masked else 1.0
+    wide, tokens, mask, it, dlp, dent = _case(rows, classes, pad, dtype, masked, sum(shape) + 1, it)
+    got = _run(wide, classes, dtype, tokens, mask, it, dlp, dent, 0)["dlogits"].double()
+    v = wide[:, :classes].double()
+    if masked:
+        v = v.masked_fill(~mask, -math.inf)
+    empty = (v == -math.inf).all(1)
+    z = torch.where(empty[:, None], torch.zeros(()).double(), v) * it
+    logp = torch.log_softmax(z, 1)
+    p = torch.exp(logp)
+    logp = torch.where(p > 0, logp, torch.zeros(()).double())
+    H = -(p * logp).sum(1, keepdim=True)
+    given = (tokens >= 0) & (tokens < classes)
+    g, h = torch.where(given, dlp, torch.zeros(())).double()[:, None], dent.double()[:, None]
+    want = -p * (g + h * (logp + H))
+    bound = 1e-5 * p * (g.abs() + h.abs() * (logp.abs() + H + 1))
+    at = torch.zeros(rows, classes, dtype=torch.bool)
+    at[given, tokens[given]] = True
+    want = want + at * g
+    bound = bound + at * g.abs() * 2.0 ** -22
+    dead = empty[:, None] | (~mask if masked else torch.zeros(rows, classes, dtype=torch.bool))
+    want, bound = torch.where(dead, torch.zeros(()).double(), want * it), torch.where(dead, torch.zeros(()).double(), bound * it)
+    if dtype == "bf16":
+        bound = bound + 2.0 ** -8 * want.abs()
+    over = (got - want).abs() - bound
+    assert float(over.max()) <= 1e-37, (float(over.max()), int(over.argmax()), float((over > 1e-37).double().mean()))

@@ -283,3 +283,16 @@ def test_infinite_gates_and_nan(shape, dtype):
     assert (d[0, [0, 1, 3, 4]] == 0).all() and torch.isnan(d[0, 2]).all()
     assert ((x[0, 5:] - 0.5).abs() < 1e-6).all() and ((d[0, 5:] - 0.25).abs() < 1e-6).all()
     r.close()
+
+
+@pytest.mark.parametrize("parts,gate", PLANS)
+@pytest.mark.parametrize("shape", [(5, 64, 1, 1), (37, 1000, 1, 1), (3, 4099, 1, 1), (2, 16384, 1, 1), (700, 48, 1, 1), (2, 33, 1, 2), (70, 24, 2, 2), (5, 64, 7, 7), (2, 257, 9, 13),
+                                   (3, 96, 16, 16), (2, 520, 14, 14), (1, 2100, 5, 8), (9, 40, 28, 28), (64, 64, 16, 16)], ids=lambda s: "x".join(map(str, s)))
+def test_weight_gradients_of_bf16_plans_are_fp32(shape, parts, gate):
+    """They are fp32 sums of what the bf16 maps hold, x' among it before its rounding: held to the bound of fp32 plans."""
+    maps, weights = _case(shape, "bf16", parts, gate, seed=sum(shape) + 1)
+    want = _reference(shape, maps, weights, gate, True)
+    got = _run(shape, "bf16", parts, gate, maps, weights)
+    for k in ("dw_post", "dscale", "dw_pre"):
+        if k in got:
+            assert_close(got[k].reshape(want[k].shape), want[k], TOL["f32"], f"{shape} {k}")

@@ -285,3 +285,35 @@ def test_strides_of_a_single_class_or_row_do_not_matter():
     one = torch.as_strided(torch.ones(50, dtype=torch.uint8, device="cuda"), (1, 5), (3, 1))
     assert int(lp.forward(row, tokens[:1], mask=one)["top_index"][0, 0]) == 4
     lp.close()
+
+
+def _seeded(make, seed):
+    """A case whose inputs are its own."""
+    r, inputs, run = make()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    for t in inputs:
+        t.copy_(torch.randn(t.shape, generator=gen, device="cuda"))
+    return r, run
+
+
+@pytest.mark.parametrize("make", [lambda: _norm_case((40, 96, 28, 28), "bf16"), lambda: _norm_case((600, 1000, 1, 1), "f32"), lambda: _norm_case((8, 2100, 5, 5), "bf16"),
+                                  lambda: _logprob_case(3, 150000, "bf16", 7), lambda: _logprob_case(2000, 5003, "f32", 5), lambda: _ortho_case((4, 24, 40), "f32"),
+                                  lambda: _ortho_case((1, 300, 900), "f32"), lambda: _ortho_case((2, 130, 700), "bf16")],
+                         ids=["norm_maps", "norm_rows", "norm_many_channels", "logprob_split", "logprob_rows", "ortho_small", "ortho_parts", "ortho_pairs"])
+def test_plans_with_inputs_of_their_own_on_two_streams(make):
+    """What one plan's call leaves in memory is never what the other one's should find there."""
+    cases = [_seeded(make, 50 + k) for k in range(2)]
+    alone = [{k: v.clone() for k, v in run().items()} for _, run in cases]
+    torch.cuda.synchronize()
+    assert any(not torch.equal(v, alone[1][k]) for k, v in alone[0].items())
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(5):
+        for (_, run), s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                run()
+    torch.cuda.synchronize()
+    for (r, _), want in zip(cases, alone):
+        for k, v in want.items():
+            assert torch.equal(v, {**r.out, **getattr(r, "grads", {})}[k]), k
+        r.close()
