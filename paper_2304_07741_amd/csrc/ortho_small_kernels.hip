@@ -97,15 +97,11 @@ __global__ __launch_bounds__(kThreads) void k_small(Shape s, Args a) {
             }
         }
         __syncthreads();
-        // X = a X + (b A + c A A) X by blocks of 16 columns, each read and written by one wave
+        // X = a X + (b A + c A A) X by blocks of 16 columns, each read and written by one wave.  (a X joins the sum at its end: as its first
+        // term it would have every later one rounded to its own size, which doubles the error where singular values spread.)
         for (int jt = wave; jt < chunks; jt += kWaves) {
             float* col = x + lg * 4 * ld + jt * 16 + lr;
-            f32x4 acc[4];
-#pragma unroll
-            for (int ti = 0; ti < 4; ti++)
-                if (ti < T)
-#pragma unroll
-                    for (int e = 0; e < 4; e++) acc[ti][e] = kA * col[(ti * 16 + e) * ld];
+            f32x4 acc[4] = {};
             for (int c = 0; c < T; c++) {
                 f32x4 v;
 #pragma unroll
@@ -122,7 +118,10 @@ __global__ __launch_bounds__(kThreads) void k_small(Shape s, Args a) {
             for (int ti = 0; ti < 4; ti++)
                 if (ti < T)
 #pragma unroll
-                    for (int e = 0; e < 4; e++) col[(ti * 16 + e) * ld] = acc[ti][e];
+                    for (int e = 0; e < 4; e++) {
+                        float& at = col[(ti * 16 + e) * ld];
+                        at = fmaf(kA, at, acc[ti][e]);
+                    }
         }
         __syncthreads();
     }

@@ -202,3 +202,24 @@ def test_operands_hold_all_their_bits(shape):
     grad, _, _ = _inputs(shape, 15)
     want = ref.ortho_step(grad.double(), None, 0, False, 5)["update"]
     assert _err(_step(shape, "f32", grad)["update"], want) <= 6e-6
+
+
+@pytest.mark.parametrize("span", [1.0, 1e-3, 1e-6])
+@pytest.mark.parametrize("shape", [(1, 24, 40), (1, 48, 80), (1, 64, 200), (1, 16, 300), (1, 200, 300), (1, 300, 200), (1, 128, 1024), (1, 520, 776)], ids=lambda s: "x".join(map(str, s)))
+def test_as_exact_as_products_in_fp32(shape, span):
+    """Singular values from one down to `span`, evenly on their logarithm: no more than half as much again as the formula's error with products in fp32."""
+    gen = torch.Generator().manual_seed(16)
+    side = min(shape[1:])
+    u, _ = torch.linalg.qr(torch.randn(shape[1], side, generator=gen, dtype=torch.float64))
+    v, _ = torch.linalg.qr(torch.randn(shape[2], side, generator=gen, dtype=torch.float64))
+    grad = ((u * torch.logspace(0, math.log10(span), side, dtype=torch.float64)) @ v.T).float()[None]
+    want = ref.newton_schulz(grad[0].double(), 5)
+    x = (grad[0] / (grad[0].norm() + 1e-7)).cuda()
+    x = x.T.contiguous() if shape[1] > shape[2] else x
+    a, b, c = ref.COEFFICIENTS
+    for _ in range(5):
+        q = x @ x.T.contiguous()
+        x = a * x + (b * q + c * (q @ q)) @ x
+    x = x.T if shape[1] > shape[2] else x
+    off = lambda t: float((t.double().cpu() - want).norm() / want.norm())  # noqa: E731
+    assert off(_step(shape, "f32", grad)["update"][0]) <= 1.5 * off(x) + 1e-7
