@@ -101,9 +101,11 @@ __global__ __launch_bounds__(kThreads) void k_small(Shape s, Args a) {
         // term it would have every later one rounded to its own size, which doubles the error where singular values spread.)
         for (int jt = wave; jt < chunks; jt += kWaves) {
             float* col = x + lg * 4 * ld + jt * 16 + lr;
-            f32x4 acc[4] = {};
-            for (int c = 0; c < T; c++) {
-                f32x4 v;
+            f32x4 acc[4] = {}, old[4];
+#pragma unroll
+            for (int c = 0; c < 4; c++) {
+                if (c >= T) break;
+                f32x4& v = old[c];
 #pragma unroll
                 for (int e = 0; e < 4; e++) v[e] = col[(c * 16 + e) * ld];
 #pragma unroll
@@ -118,10 +120,7 @@ __global__ __launch_bounds__(kThreads) void k_small(Shape s, Args a) {
             for (int ti = 0; ti < 4; ti++)
                 if (ti < T)
 #pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        float& at = col[(ti * 16 + e) * ld];
-                        at = fmaf(kA, at, acc[ti][e]);
-                    }
+                    for (int e = 0; e < 4; e++) col[(ti * 16 + e) * ld] = fmaf(kA, old[ti][e], acc[ti][e]);
         }
         __syncthreads();
     }
