@@ -12,9 +12,10 @@
 //
 // Backward: element by element from the row's (m, log S, entropy, 1 / S).
 //
-// Both are bound by memory on many rows: 4096 x 32768 in bf16 forward 44 us (6.0 TB/s, some of it from the last-level cache),
-// backward 108 us (5.0 TB/s).  With alternatives the search at a row's end is not hidden by other rows' loads: 1500 x 50021
-// with five of them takes 43 us, without 32.  Few rows are bound by latency: 256 x 1000 4 us per launch.
+// Both are bound by memory on many rows, here over three sets of logits in turn: 4096 x 32768 in bf16 forward 53 us (5.0 TB/s; 44 where the
+// last-level cache still holds some of them, 62 behind a backward whose gradients are still being written), backward 108 us (5.0
+// TB/s), in fp32 93 and 188 us (5.7 TB/s).  With alternatives the search at a row's end is not hidden by other rows' loads: 1500 x 50021
+// with five of them takes 43 us, without 39.  Few rows are bound by latency: 256 x 1000 4 us per launch.
 #include "logprob_kernels.hpp"
 
 #include <algorithm>

@@ -1,7 +1,7 @@
 // Residual norm, forward, and what forward and backward share on the host.  Both are bound by memory: five maps move forward, eight
-// backward, and everything in between stays in registers.  Forward: 64 x 64 x 56 x 56 in 27 us bf16 (4.8 TB/s) and 40-45 us fp32 (5.7-6.4
-// TB/s, some of it from the last-level cache), 128 x 256 x 14 x 14 in 17 us (3.7 TB/s), 128 x 512 x 7 x 7 in 13 us (2.4 TB/s, one round of
-// workgroups), rows 4096 x 2048 in fp32 28 us (6 TB/s), 8 x 1024 in bf16 4 us (the launch).
+// backward, and everything in between stays in registers.  Forward, over three sets of maps in turn: 64 x 64 x 56 x 56 in 30 us bf16 (4.3 TB/s) and 46 us fp32
+// (5.6 TB/s), 128 x 256 x 14 x 14 in 17 us (3.7 TB/s), 128 x 512 x 7 x 7 in 14 us (2.3 TB/s, one round of workgroups), rows 4096 x 2048 in
+// fp32 33 us (5.0 TB/s), without a gate 24 (5.7 TB/s), 8 x 1024 in bf16 4 us (the launch).
 //
 // Maps (planes of two pixels or more): a thread takes 16 bytes of pixels of `KC` channels, lanes side by side GX such pieces, the
 // other lanes and waves the channels in turn; sums over the channels go through lane exchanges and LDS.  The last piece of a

@@ -6,9 +6,9 @@
 //   E = D scale w_post r2:  dz = E act - z (r2^2 T2 / C),  dgate = E z act'
 // Bound by memory: eight maps move (five read, three written).  Some 50 operations per element are left beside them, which take
 // about as long where 8 pixels of bf16 lie in 16 bytes, so what only depends on the pixel is multiplied per pixel, and the gate's
-// kind is a constant of the kernel.  With the sums over the partials: 64 x 64 x 56 x 56 in 46 us bf16 (4.4 TB/s) and 87 us fp32
-// (4.7 TB/s), 64 x 256 x 28 x 28 in 56 us (3.7 TB/s), 128 x 256 x 14 x 14 in 39 us (2.6 TB/s), 128 x 512 x 7 x 7 in 24 us (2.1 TB/s): four
-// channels per thread leave two waves per SIMD, and the short planes' pieces overlap (56 pixels read for 49).
+// kind is a constant of the kernel.  With the sums over the partials, over three sets of maps in turn: 64 x 64 x 56 x 56 in 48 us bf16
+// (4.2 TB/s) and 86 us fp32 (4.8 TB/s), 64 x 256 x 28 x 28 in 63 us (3.3 TB/s), 128 x 256 x 14 x 14 in 38 us (2.7 TB/s; fp32 63 us, 3.3
+// TB/s), 128 x 512 x 7 x 7 in 24 us (2.1 TB/s): four channels per thread leave two waves per SIMD, and the short planes' pieces overlap (56 pixels read for 49).
 #include <atomic>
 
 #include "../../include/canvas_norm.h"

@@ -1,8 +1,8 @@
 // Residual norm, backward on rows of tokens (planes of one pixel): the passes of norm_maps_bwd_kernels.hip with one pixel per row,
 // TPR threads per row and KV times 16 bytes each.  Workgroups walk over rows and keep the sums of their channels.
-// Bound by memory.  With the sums over the partials: 4096 x 2048 in fp32 50 us (5.3 TB/s), 8192 x 512 in bf16 20 us (3.4 TB/s), 2048 x 4096
-// in bf16 36 us (3.7 TB/s; by 256 threads of 32 bytes 39), 4096 x 8192 in bf16 120 us (4.5 TB/s), 512 x 16384 in bf16 73 us (1.8
-// TB/s), whose values are read up to three times.
+// Bound by memory.  With the sums over the partials, over three sets of rows in turn: 4096 x 2048 in fp32 52 us (5.2 TB/s), 8192 x 512 in bf16
+// 20 us (3.3 TB/s), 2048 x 4096 in bf16 40 us (3.4 TB/s; over one set 36, by 256 threads of 32 bytes 39), 4096 x 8192 in bf16 119 us
+// (4.5 TB/s), 512 x 16384 in bf16 74 us (1.8 TB/s), whose values are read up to three times.
 #include <atomic>
 
 #include "launch.hpp"

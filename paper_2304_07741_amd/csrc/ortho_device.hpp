@@ -9,6 +9,7 @@
 namespace canvas {
 namespace ortho {
 
+// of the quintic Newton-Schulz step that K. Jordan et al. published in "Muon: an optimizer for hidden layers in neural networks" (2024)
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr double kEps = 1e-7;
 

@@ -17,8 +17,8 @@
 // weak); three steps at a time would leave two to three times that.
 //
 // Large matrices are bound by the matrix units, small ones by the launches that wait for each other.  2048 x 8192: the long products
-// take 190 us each (1080 TFLOP/s of fp16 products; a plain 8192 x 8192 x 8192 one of the library reaches 1145), Gram matrices 104 + 14 for the sums of their
-// parts, short products 37 + 10 (730 TFLOP/s), momentum and splitting 86; five steps 1437 us.  256 x 2304: 22 launches of 4-8 us, 119-122 us.
+// take 185-200 us each (1030-1110 TFLOP/s of fp16 products; a plain 8192 x 8192 x 8192 one of the library reaches 1145), Gram matrices 105 + 14 for the sums of
+// their parts, short products 36 + 10 (740 TFLOP/s), momentum and splitting 85; five steps 1.48 ms.  256 x 2304: 22 launches of 4-8 us, 119-122 us.
 #include "ortho_kernels.hpp"
 
 #include <algorithm>
