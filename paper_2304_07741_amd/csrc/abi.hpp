@@ -51,6 +51,13 @@ inline bool share_bytes(const Region& a, const Region& b) {
     const uint64_t a0 = (uint64_t)(uintptr_t)a.p, b0 = (uint64_t)(uintptr_t)b.p;
     if (a0 >= b0 + (b.rows - 1) * b.pitch + b.bytes || b0 >= a0 + (a.rows - 1) * a.pitch + a.bytes) return false;
     if (a.rows == 1) return true;
+    if (b.rows > 1 && a.pitch == b.pitch) {
+        // rows i of a and j of b lie as i - j says: the first difference with which a's row ends behind the beginning of b's
+        const int64_t pitch = (int64_t)a.pitch, d = (int64_t)(b0 - a0), n = d - (int64_t)a.bytes;
+        int64_t k = (n >= 0 ? n / pitch : -((-n + pitch - 1) / pitch)) + 1;
+        if (k < 1 - (int64_t)b.rows) k = 1 - (int64_t)b.rows;
+        return k < (int64_t)a.rows && k * pitch < d + (int64_t)b.bytes;
+    }
     // each row of b against the first of a's rows that ends behind its beginning
     for (uint64_t r = 0; r < b.rows; r++) {
         const uint64_t from = b0 + r * b.pitch, i = a0 + a.bytes > from ? 0 : (from - a0 - a.bytes) / a.pitch + 1;

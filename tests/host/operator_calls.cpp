@@ -7,6 +7,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <chrono>
 #include <cstdint>
 #include <cstdio>
 #include <cstring>
@@ -301,6 +302,26 @@ static void logprob_overlap() {
     }
 }
 
+// Gradients beside the logits in one wide buffer, a billion rows of them: told apart without looking at every row.
+static void many_rows_overlap() {
+    canvas_logprob* h = nullptr;
+    if (canvas_logprob_compile(1 << 30, 10, CANVAS_F32, 0, nullptr, &h)) return expect(false, "logprob compile");
+    canvas_logprob_info info;
+    canvas_logprob_query(h, &info);
+    const uint64_t at = 1ull << 44;
+    const auto begin = std::chrono::steady_clock::now();
+    for (int64_t off : {-20ll * ((1 << 30) - 1) - 10, -20ll * (1 << 29) - 5, -21ll, -20ll, -11ll, -10ll, -1ll, 0ll, 1ll, 9ll, 10ll, 11ll, 20ll, 20ll * (1 << 29) + 10, 20ll * ((1 << 30) - 1) + 9, 20ll << 30}) {
+        const int64_t left = ((off % 20) + 20) % 20;
+        const bool apart = left == 10 || off >= 20ll * ((1 << 30) - 1) + 10, same = off == 0;
+        g_launches.clear();
+        const int rc = canvas_logprob_backward(h, (void*)at, 20, 1.f, nullptr, 0, (int64_t*)place(3), (float*)place(4), (float*)place(5), (void*)(at + 4 * off), 20, kSpace, info.workspace_bytes, nullptr);
+        expect(rc == (apart || same ? CANVAS_OK : CANVAS_BAD_ARG) && g_launches.empty() == (rc != CANVAS_OK), "a billion rows, offset " + std::to_string(off));
+    }
+    const double s = std::chrono::duration<double>(std::chrono::steady_clock::now() - begin).count();
+    expect(s < 0.5, "a billion rows: " + std::to_string(s) + " s");
+    canvas_logprob_destroy(h);
+}
+
 static void ortho_overlap() {
     for (int64_t R : {8, 200}) {
         const int64_t shape[3] = {2, R, 80};
@@ -328,6 +349,7 @@ int main(int argc, char** argv) {
     if (what == "overlap") {
         norm_overlap();
         logprob_overlap();
+        many_rows_overlap();
         ortho_overlap();
     }
     if (what == "lds") lds();
