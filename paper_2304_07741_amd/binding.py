@@ -42,6 +42,17 @@ ORTHO_EXPORTS = ["canvas_ortho_compile", "canvas_ortho_query", "canvas_ortho_ste
 CANVAS_ORTHO_NESTEROV = 1
 CANVAS_ORTHO_MAX_SIDE = 16384
 CANVAS_ORTHO_MAX_STEPS = 16
+# include/canvas_gated.h
+GATED_EXPORTS = ["canvas_gated_compile", "canvas_gated_query", "canvas_gated_forward", "canvas_gated_backward", "canvas_gated_destroy"]
+CANVAS_GATED_SIGMOID, CANVAS_GATED_SILU, CANVAS_GATED_GELU = 0, 1, 2
+CANVAS_GATED_MAX_SIDE = 1 << 18
+# include/canvas_head.h
+HEAD_EXPORTS = ["canvas_head_compile", "canvas_head_query", "canvas_head_forward", "canvas_head_backward", "canvas_head_destroy"]
+CANVAS_HEAD_MAX_FEATURES = 1 << 18
+CANVAS_HEAD_MAX_CLASSES = 1 << 20
+# include/canvas_clip.h
+CLIP_EXPORTS = ["canvas_clip_compile", "canvas_clip_query", "canvas_clip_step", "canvas_clip_destroy"]
+CANVAS_CLIP_MAX_TENSORS = 65536
 
 
 class CanvasOptions(ctypes.Structure):
@@ -82,6 +93,21 @@ class CanvasLogprobInfo(ctypes.Structure):
 class CanvasOrthoInfo(ctypes.Structure):
     _fields_ = [("n_launches", ctypes.c_int32), ("reserved0", ctypes.c_int32), ("workspace_bytes", ctypes.c_uint64),
                 ("flops", ctypes.c_double), ("min_bytes", ctypes.c_double)]
+
+
+class CanvasGatedInfo(ctypes.Structure):
+    _fields_ = [("n_launches_fwd", ctypes.c_int32), ("n_launches_bwd", ctypes.c_int32), ("workspace_bytes", ctypes.c_uint64),
+                ("flops_fwd", ctypes.c_double), ("flops_bwd", ctypes.c_double), ("min_bytes_fwd", ctypes.c_double), ("min_bytes_bwd", ctypes.c_double)]
+
+
+class CanvasHeadInfo(ctypes.Structure):
+    _fields_ = [("n_launches_fwd", ctypes.c_int32), ("n_launches_bwd", ctypes.c_int32), ("pieces", ctypes.c_int32), ("reserved0", ctypes.c_int32),
+                ("workspace_bytes", ctypes.c_uint64), ("flops_fwd", ctypes.c_double), ("flops_bwd", ctypes.c_double),
+                ("min_bytes_fwd", ctypes.c_double), ("min_bytes_bwd", ctypes.c_double)]
+
+
+class CanvasClipInfo(ctypes.Structure):
+    _fields_ = [("n_launches", ctypes.c_int32), ("n_launches_norm", ctypes.c_int32), ("workspace_bytes", ctypes.c_uint64), ("min_bytes", ctypes.c_double)]
 
 
 class CanvasTarget(ctypes.Structure):
@@ -171,6 +197,23 @@ def load():
         lib.canvas_ortho_step.argtypes = [vp, vp, vp, vp, f64, vp, vp, f64, f64, vp, vp, vp, sz, vp]
         lib.canvas_ortho_destroy.argtypes = [vp]
         lib.canvas_ortho_destroy.restype = None
+        lib.canvas_gated_compile.argtypes = [i64, i64, i64, ctypes.c_int, ctypes.c_int, opt, ctypes.POINTER(vp)]
+        lib.canvas_gated_query.argtypes = [vp, ctypes.POINTER(CanvasGatedInfo)]
+        lib.canvas_gated_forward.argtypes = [vp] * 6 + [sz, vp]
+        lib.canvas_gated_backward.argtypes = [vp] * 9 + [sz, vp]
+        lib.canvas_gated_destroy.argtypes = [vp]
+        lib.canvas_gated_destroy.restype = None
+        lib.canvas_head_compile.argtypes = [i64, i64, i64, ctypes.c_int, opt, ctypes.POINTER(vp)]
+        lib.canvas_head_query.argtypes = [vp, ctypes.POINTER(CanvasHeadInfo)]
+        lib.canvas_head_forward.argtypes = [vp, vp, vp, f32, vp, vp, vp, vp, vp, sz, vp]
+        lib.canvas_head_backward.argtypes = [vp, vp, vp, f32] + [vp] * 7 + [sz, vp]
+        lib.canvas_head_destroy.argtypes = [vp]
+        lib.canvas_head_destroy.restype = None
+        lib.canvas_clip_compile.argtypes = [i32, ctypes.POINTER(i64), ctypes.POINTER(ctypes.c_int), ctypes.POINTER(ctypes.c_int), ctypes.POINTER(vp)]
+        lib.canvas_clip_query.argtypes = [vp, ctypes.POINTER(CanvasClipInfo)]
+        lib.canvas_clip_step.argtypes = [vp, vp, vp, f64, vp, vp, vp, sz, vp]
+        lib.canvas_clip_destroy.argtypes = [vp]
+        lib.canvas_clip_destroy.restype = None
         _lib = lib
     return _lib
 
@@ -393,6 +436,94 @@ def canvas_ortho_step(handle, grad, momentum, momentum_out, mu, master, master_o
 
 def canvas_ortho_destroy(handle):
     load().canvas_ortho_destroy(handle)
+
+
+# ---------------------------------------------------------------- gated pairs of FCs (include/canvas_gated.h)
+
+def canvas_gated_compile(rows, features, width, dtype, act=CANVAS_GATED_SILU, flags=0):
+    opt = CanvasOptions(flags=flags)
+    h = ctypes.c_void_p()
+    _check(load().canvas_gated_compile(int(rows), int(features), int(width), int(dtype), int(act), ctypes.byref(opt), ctypes.byref(h)))
+    return h
+
+
+def canvas_gated_query(handle):
+    info = CanvasGatedInfo()
+    _check(load().canvas_gated_query(handle, ctypes.byref(info)))
+    return info
+
+
+def canvas_gated_forward(handle, x, w_gate, w_up, y, workspace):
+    _check(load().canvas_gated_forward(handle, _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(y), _ptr(workspace), _bytes(workspace), _stream()))
+
+
+def canvas_gated_backward(handle, x, w_gate, w_up, dy, dx, dw_gate, dw_up, workspace):
+    _check(load().canvas_gated_backward(handle, _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(dy), _ptr(dx), _ptr(dw_gate), _ptr(dw_up), _ptr(workspace),
+                                        _bytes(workspace), _stream()))
+
+
+def canvas_gated_destroy(handle):
+    load().canvas_gated_destroy(handle)
+
+
+# ---------------------------------------------------------------- log probabilities without logits (include/canvas_head.h)
+
+def canvas_head_compile(rows, features, classes, dtype, flags=0):
+    opt = CanvasOptions(flags=flags)
+    h = ctypes.c_void_p()
+    _check(load().canvas_head_compile(int(rows), int(features), int(classes), int(dtype), ctypes.byref(opt), ctypes.byref(h)))
+    return h
+
+
+def canvas_head_query(handle):
+    info = CanvasHeadInfo()
+    _check(load().canvas_head_query(handle, ctypes.byref(info)))
+    return info
+
+
+def canvas_head_forward(handle, x, weight, inv_temperature, mask, tokens, logprob, entropy, workspace):
+    """mask, tokens and logprob, entropy may be None."""
+    _check(load().canvas_head_forward(handle, _ptr(x), _ptr(weight), float(inv_temperature), _ptr(mask), _ptr(tokens), _ptr(logprob), _ptr(entropy),
+                                      _ptr(workspace), _bytes(workspace), _stream()))
+
+
+def canvas_head_backward(handle, x, weight, inv_temperature, mask, tokens, dlogprob, dentropy, dx, dweight, workspace):
+    _check(load().canvas_head_backward(handle, _ptr(x), _ptr(weight), float(inv_temperature), _ptr(mask), _ptr(tokens), _ptr(dlogprob), _ptr(dentropy),
+                                       _ptr(dx), _ptr(dweight), _ptr(workspace), _bytes(workspace), _stream()))
+
+
+def canvas_head_destroy(handle):
+    load().canvas_head_destroy(handle)
+
+
+# ---------------------------------------------------------------- clipping of gradients (include/canvas_clip.h)
+
+def canvas_clip_compile(counts, types, out_types=None):
+    """counts: elements of each tensor; types and out_types: CANVAS_F32 or CANVAS_BF16 for each."""
+    n = len(counts)
+    kinds = lambda v: (ctypes.c_int * max(1, n))(*[int(t) for t in v])  # noqa: E731
+    if len(types) != n or (out_types is not None and len(out_types) != n):
+        raise ValueError("a type for each tensor is needed")
+    h = ctypes.c_void_p()
+    _check(load().canvas_clip_compile(n, (ctypes.c_int64 * max(1, n))(*[int(c) for c in counts]), kinds(types), None if out_types is None else kinds(out_types),
+                                      ctypes.byref(h)))
+    return h
+
+
+def canvas_clip_query(handle):
+    info = CanvasClipInfo()
+    _check(load().canvas_clip_query(handle, ctypes.byref(info)))
+    return info
+
+
+def canvas_clip_step(handle, grads, outs, max_norm, norm, scale, workspace):
+    """grads, outs: lists of tensors (outs None: the norm alone), as many as the plan has."""
+    _check(load().canvas_clip_step(handle, _ptrs(grads), None if outs is None else _ptrs(outs), float(max_norm), _ptr(norm), _ptr(scale), _ptr(workspace),
+                                   _bytes(workspace), _stream()))
+
+
+def canvas_clip_destroy(handle):
+    load().canvas_clip_destroy(handle)
 
 
 # ---------------------------------------------------------------- templates (include/canvas_template.h), host only

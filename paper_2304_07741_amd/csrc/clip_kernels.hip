@@ -1,0 +1,256 @@
+// The norm over many tensors and their scaling.
+//
+// Two passes over memory: squares, added up in 64 bits by each thread over its elements, then by each workgroup, then by every workgroup of the second
+// pass for itself, always in the same order; and the scaling.  The second pass goes through the tensors backwards: what the first one read last is still in the
+// last-level cache.
+#include "clip_kernels.hpp"
+
+#include <algorithm>
+
+#include "device_util.hpp"
+#include "launch.hpp"
+#include "tile_util.hpp"
+
+namespace canvas {
+namespace clip {
+namespace {
+
+using tile::u32x4;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+constexpr int kThreads = 256, kMostParts = 1024;
+
+struct Item {
+    const void* in;
+    void* out;
+    int64_t count;
+    uint32_t first;  // chunk
+    uint16_t bf16, out_bf16;
+};
+struct Items {
+    Item item[kBatch];
+    int n;
+    uint32_t chunks;
+};
+
+// The tensor that a chunk belongs to.
+__device__ __forceinline__ int item_of(const Items& a, uint32_t chunk) {
+    int lo = 0, hi = a.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.item[mid].first <= chunk)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+__device__ __forceinline__ bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = (e & 1) ? tile::hi_f32(w[e >> 1]) : tile::lo_f32(w[e >> 1]);
+}
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+#pragma unroll
+    for (int e = 0; e < 4; e++) v[e] = a[e], v[4 + e] = b[e];
+}
+__device__ __forceinline__ float load1(const uint16_t* p) { return bf16_to_f32(*p); }
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
+    *reinterpret_cast<u32x4*>(p) = u32x4{tile::pack_bf16(v[0], v[1]), tile::pack_bf16(v[2], v[3]), tile::pack_bf16(v[4], v[5]), tile::pack_bf16(v[6], v[7])};
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+    reinterpret_cast<f32x4*>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
+    reinterpret_cast<f32x4*>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
+}
+__device__ __forceinline__ void store1(uint16_t* p, float v) { *p = f32_to_bf16(v); }
+__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+
+constexpr int kTurns = kChunk / (8 * kThreads);
+template <class T>
+__device__ __forceinline__ double squares(const T* p, int n) {
+    double t = 0;
+    if (n == kChunk && aligned(p)) {
+        float v[kTurns][8];
+#pragma unroll
+        for (int k = 0; k < kTurns; k++) load8(p + (k * kThreads + threadIdx.x) * 8, v[k]);
+#pragma unroll
+        for (int k = 0; k < kTurns; k++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) t = fma((double)v[k][e], (double)v[k][e], t);
+        return t;
+    }
+    int done = 0;
+    if (aligned(p)) {
+        done = n & ~7;
+        for (int i = threadIdx.x * 8; i < done; i += 8 * kThreads) {
+            float v[8];
+            load8(p + i, v);
+#pragma unroll
+            for (int e = 0; e < 8; e++) t = fma((double)v[e], (double)v[e], t);
+        }
+    }
+    for (int i = done + threadIdx.x; i < n; i += kThreads) {
+        const double v = load1(p + i);
+        t = fma(v, v, t);
+    }
+    return t;
+}
+
+// Over the workgroup, in a fixed order; the sum is thread 0's.
+__device__ __forceinline__ double over_threads(double t) {
+    __shared__ double buf[kThreads];
+    buf[threadIdx.x] = t;
+    __syncthreads();
+    for (int o = kThreads / 2; o; o >>= 1) {
+        if ((int)threadIdx.x < o) buf[threadIdx.x] += buf[threadIdx.x + o];
+        __syncthreads();
+    }
+    return buf[0];
+}
+
+__global__ __launch_bounds__(kThreads) void k_squares(Items a, double* parts) {
+    double t = 0;
+    for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
+        const Item& item = a.item[item_of(a, c)];
+        const int64_t from = (int64_t)(c - item.first) * kChunk;
+        const int n = (int)(item.count - from < kChunk ? item.count - from : kChunk);
+        t += item.bf16 ? squares(static_cast<const uint16_t*>(item.in) + from, n) : squares(static_cast<const float*>(item.in) + from, n);
+    }
+    t = over_threads(t);
+    if (threadIdx.x == 0) parts[blockIdx.x] = t;
+}
+
+__device__ __forceinline__ double norm_of(const double* parts, int n) {
+    double t = 0;
+    for (int k = threadIdx.x; k < n; k += kThreads) t += parts[k];
+    return sqrt(over_threads(t));
+}
+// (NaN stays; a largest norm of infinity asks for no scaling)
+__device__ __forceinline__ double scale_of(double norm, double most) {
+    const double r = norm > 0 || norm != norm ? most / norm : 1.0;
+    return most > 1.7e308 || r >= 1.0 ? 1.0 : r;
+}
+__global__ __launch_bounds__(kThreads) void k_norm(const double* parts, int n, double most, double* kept, float* norm, float* scale) {
+    const double t = norm_of(parts, n);
+    if (threadIdx.x) return;
+    *kept = t;
+    *norm = (float)t;
+    if (scale) *scale = (float)scale_of(t, most);
+}
+
+template <class T, class O>
+__device__ __forceinline__ void scaled(const T* p, O* to, int n, double scale) {
+    const float s = (float)scale;
+    auto of = [&](float v) { return s >= 1.2e-38f || !(scale > 0) ? v * s : (float)(v * scale); };
+    if (n == kChunk && aligned(p) && aligned(to)) {
+        float v[kTurns][8];
+#pragma unroll
+        for (int k = 0; k < kTurns; k++) load8(p + (k * kThreads + threadIdx.x) * 8, v[k]);
+#pragma unroll
+        for (int k = 0; k < kTurns; k++) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[k][e] = of(v[k][e]);
+            store8(to + (k * kThreads + threadIdx.x) * 8, v[k]);
+        }
+        return;
+    }
+    int done = 0;
+    if (aligned(p) && aligned(to)) {
+        done = n & ~7;
+        for (int i = threadIdx.x * 8; i < done; i += 8 * kThreads) {
+            float v[8];
+            load8(p + i, v);
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[e] = of(v[e]);
+            store8(to + i, v);
+        }
+    }
+    for (int i = done + threadIdx.x; i < n; i += kThreads) store1(to + i, of(load1(p + i)));
+}
+
+// kept: the norm where a launch of its own has left it; else the parts are added here, and workgroup 0 of the first launch writes the results.
+__global__ __launch_bounds__(kThreads) void k_scale(Items a, const double* parts, int n, const double* kept, double most, float* norm, float* scale) {
+    const double t = kept ? *kept : norm_of(parts, n), s = scale_of(t, most);
+    if (!kept && norm && blockIdx.x == 0 && threadIdx.x == 0) {
+        *norm = (float)t;
+        if (scale) *scale = (float)s;
+    }
+    for (uint32_t k = blockIdx.x; k < a.chunks; k += gridDim.x) {
+        const uint32_t c = a.chunks - 1 - k;
+        const Item& item = a.item[item_of(a, c)];
+        if (s == 1.0 && item.in == item.out) continue;  // (nothing changes)
+        const int64_t from = (int64_t)(c - item.first) * kChunk;
+        const int n = (int)(item.count - from < kChunk ? item.count - from : kChunk);
+        if (item.bf16) {
+            const uint16_t* p = static_cast<const uint16_t*>(item.in) + from;
+            if (item.out_bf16)
+                scaled(p, static_cast<uint16_t*>(item.out) + from, n, s);
+            else
+                scaled(p, static_cast<float*>(item.out) + from, n, s);
+        } else {
+            const float* p = static_cast<const float*>(item.in) + from;
+            if (item.out_bf16)
+                scaled(p, static_cast<uint16_t*>(item.out) + from, n, s);
+            else
+                scaled(p, static_cast<float*>(item.out) + from, n, s);
+        }
+    }
+}
+
+}  // namespace
+
+void make_plan(Plan& p) {
+    Batch b;
+    auto close = [&] {
+        if (b.tensors.empty()) return;
+        p.batches.push_back(b);
+        b = Batch();
+    };
+    for (size_t i = 0; i < p.tensors.size(); i++) {
+        const int64_t chunks = (p.tensors[i].count + kChunk - 1) / kChunk;
+        if (!chunks) continue;
+        if ((int)b.tensors.size() == kBatch || b.chunks + chunks > INT32_MAX) close();
+        b.tensors.push_back((int)i);
+        b.chunks += chunks;
+    }
+    close();
+    const int most = std::max<int>(64, kMostParts / (int)std::max<size_t>(1, p.batches.size()));
+    for (Batch& c : p.batches) {
+        c.parts = (int)std::min<int64_t>(c.chunks, most);
+        c.first_part = p.parts;
+        p.parts += c.parts;
+    }
+    p.alone = p.parts > kMostParts || p.batches.empty();
+    const int n = (int)p.batches.size();
+    p.launches = 2 * n + p.alone;
+    p.launches_norm = n + 1;
+    p.workspace_bytes = 8ull * (p.parts + 1);
+    p.workspace_bytes = (p.workspace_bytes + 255) & ~(uint64_t)255;
+}
+
+void step(const Plan& p, const Args& a, hipStream_t stream) {
+    double *parts = reinterpret_cast<double*>(a.ws), *kept = parts + p.parts;
+    auto items = [&](const Batch& b) {
+        Items t{};
+        for (int i : b.tensors) {
+            t.item[t.n++] = Item{a.grads[i], a.outs ? a.outs[i] : nullptr, p.tensors[i].count, t.chunks, p.tensors[i].bf16, p.tensors[i].out_bf16};
+            t.chunks += (uint32_t)((p.tensors[i].count + kChunk - 1) / kChunk);
+        }
+        return t;
+    };
+    for (const Batch& b : p.batches) CANVAS_LAUNCH(k_squares, dim3(b.parts), dim3(kThreads), 0, stream, items(b), parts + b.first_part);
+    const bool alone = p.alone || !a.outs;
+    if (alone) CANVAS_LAUNCH(k_norm, dim3(1), dim3(kThreads), 0, stream, parts, p.parts, a.most, kept, a.norm, a.scale);
+    if (!a.outs) return;
+    for (size_t k = p.batches.size(); k--;) {
+        const Batch& b = p.batches[k];
+        const unsigned grid = (unsigned)std::min<int64_t>(b.chunks, 2048);
+        CANVAS_LAUNCH(k_scale, dim3(grid), dim3(kThreads), 0, stream, items(b), parts, p.parts, alone ? kept : nullptr, a.most, k ? nullptr : a.norm, k ? nullptr : a.scale);
+    }
+}
+
+}  // namespace clip
+}  // namespace canvas

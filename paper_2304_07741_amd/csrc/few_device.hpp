@@ -1,0 +1,125 @@
+// The inner part of a product of a weight [n][k] with few rows x [rows][k], up to 16 NT of them: bound by reading the weight, which goes straight from
+// memory to the registers of the wave that multiplies it.
+//
+// A workgroup takes R blocks of 16 rows of weights.  Its waves share out the summed index, kAhead times 64 bytes of a row each in turn, and
+// add up through LDS in the order of the waves.  bf16: the 16 x 16 x 32 product of the matrix units; fp32: their 16 x 16 x 4 one, whose products
+// and sums are those of fp32.  Rows may begin at any element.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "product_device.hpp"
+#include "tile_util.hpp"
+
+namespace canvas {
+namespace few {
+
+using product::f32x4;
+using tile::u32x4;
+
+constexpr int kWaves = 8, kThreads = 64 * kWaves, kAhead = 4;
+
+template <class T>
+struct Type;
+template <>
+struct Type<uint16_t> {
+    static constexpr int kEach = 8;  // elements of 16 bytes
+    static __device__ __forceinline__ void multiply(const u32x4& a, const u32x4& b, f32x4& c) { c = tile::mfma32(a, b, c); }
+};
+template <>
+struct Type<float> {
+    static constexpr int kEach = 4;
+    static __device__ __forceinline__ void multiply(const u32x4& a, const u32x4& b, f32x4& c) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
+    }
+};
+
+template <class T>
+__device__ __forceinline__ u32x4 load16(const T* p) {
+    u32x4 v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+// Elements k .. of a row of `end`, zeros behind it.
+template <class T>
+__device__ __forceinline__ u32x4 load_end(const T* row, int64_t k, int64_t end) {
+    T e[Type<T>::kEach];
+#pragma unroll
+    for (int i = 0; i < Type<T>::kEach; i++) e[i] = k + i < end ? row[k + i] : T(0);
+    u32x4 v;
+    __builtin_memcpy(&v, e, 16);
+    return v;
+}
+
+// sums[r][t]: of weight rows `w[r]` (this lane's row of the block) and rows `x[t]`; whole sums in waves 0 .. NT - 1, wave t those of rows 16 t ..:
+// register e of a lane is weight row (lane / 16) * 4 + e, row lane % 16 of x.
+template <class T, int R, int NT>
+__device__ __forceinline__ void accumulate(const T* const (&w)[R], const T* const (&x)[NT], int64_t depth, f32x4 (&sums)[R], f32x4* shared) {
+    using Y = Type<T>;
+    constexpr int kStep = 4 * Y::kEach, kTurn = kStep * kAhead;  // elements of a row that a wave takes per load, and per turn
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t mine = (lane >> 4) * Y::kEach;
+    f32x4 acc[R][NT] = {};
+    struct Turn {
+        u32x4 w[R][kAhead], x[NT][kAhead];
+    };
+    auto load = [&](int64_t k, Turn& t) {
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+#pragma unroll
+            for (int r = 0; r < R; r++) t.w[r][u] = load16(w[r] + k + u * kStep + mine);
+#pragma unroll
+            for (int n = 0; n < NT; n++) t.x[n][u] = load16(x[n] + k + u * kStep + mine);
+        }
+    };
+    auto multiply = [&](const Turn& t) {
+#pragma unroll
+        for (int u = 0; u < kAhead; u++)
+#pragma unroll
+            for (int r = 0; r < R; r++)
+#pragma unroll
+                for (int n = 0; n < NT; n++) Y::multiply(t.w[r][u], t.x[n][u], acc[r][n]);
+    };
+    const int64_t whole = depth / kTurn;
+    int64_t turn = wave;
+    if (turn < whole) {
+        Turn t[2];
+        load(turn * kTurn, t[0]);
+        for (; turn + kWaves < whole; turn += kWaves) {
+            load((turn + kWaves) * kTurn, t[1]);
+            multiply(t[0]);
+            t[0] = t[1];
+        }
+        multiply(t[0]);
+        turn += kWaves;
+    }
+    if (turn == whole) {  // what is left of the rows is one wave's
+#pragma unroll 1
+        for (int64_t k = whole * kTurn; k < depth; k += kStep) {
+            u32x4 a[R], b[NT];
+#pragma unroll
+            for (int r = 0; r < R; r++) a[r] = load_end(w[r], k + mine, depth);
+#pragma unroll
+            for (int n = 0; n < NT; n++) b[n] = load_end(x[n], k + mine, depth);
+#pragma unroll
+            for (int r = 0; r < R; r++)
+#pragma unroll
+                for (int n = 0; n < NT; n++) Y::multiply(a[r], b[n], acc[r][n]);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; r++)
+#pragma unroll
+        for (int n = 0; n < NT; n++) shared[((r * NT + n) * kWaves + wave) * 64 + lane] = acc[r][n];
+    __syncthreads();
+    if (wave >= NT) return;
+#pragma unroll
+    for (int r = 0; r < R; r++) {
+        sums[r] = f32x4{};
+#pragma unroll
+        for (int v = 0; v < kWaves; v++) sums[r] += shared[((r * NT + wave) * kWaves + v) * 64 + lane];
+    }
+}
+
+}  // namespace few
+}  // namespace canvas

@@ -1,0 +1,361 @@
+// The gated pair of FCs: y = act(x Wg^T) (x Wu^T).
+//
+// Forward: one product whose columns are those of both weights, 32 of the gate and 32 of the other in turn, so that a wave holds g and u of
+// the same results in the same places of its registers and y is theirs.  Training keeps g and u in fp32.
+// Backward: dg and du element by element from g, u and dy; then dx as one sum over the columns of both, and dWg and dWu as one launch.
+#include "gated_kernels.hpp"
+
+#include <algorithm>
+
+#include "../../include/canvas_gated.h"
+#include "device_util.hpp"
+#include "exp_util.hpp"
+#include "few_device.hpp"
+#include "launch.hpp"
+#include "product_device.hpp"
+#include "tile_util.hpp"
+
+namespace canvas {
+namespace gated {
+namespace {
+
+using product::f32x16;
+using product::f32x4;
+using product::Factor;
+using product::Form;
+using tile::u32x4;
+
+// act(g); with SLOPE its derivative too.  e^-|g| serves both signs; NaN stays (comparisons, not maxima).
+template <bool SLOPE>
+__device__ __forceinline__ float act_of(int act, float g, float& slope) {
+    if (act == CANVAS_GATED_GELU) {
+        const float cdf = 0.5f * erfcf(g * -0.70710678118654752f);
+        if (SLOPE) {
+            const float half = -0.5f * g * g;
+            slope = fmaf(g * 0.39894228040143268f, exp_finite(half < -300.f ? -300.f : half), cdf);
+        }
+        return g * cdf;
+    }
+    const float m = -fabsf(g), e = exp_finite(m < -300.f ? -300.f : m), r = __builtin_amdgcn_rcpf(1.f + e);
+    const float sig = g < 0.f ? e * r : r, other = g < 0.f ? r : e * r;  // other = 1 - sig without a difference
+    if (act == CANVAS_GATED_SIGMOID) {
+        if (SLOPE) slope = sig * other;
+        return sig;
+    }
+    if (SLOPE) slope = sig * fmaf(g, other, 1.f);
+    return g * sig;
+}
+
+struct FwdArgs {
+    Factor x, w;
+    int64_t rows, features, width, tiles_i, tiles_j, ld;
+    void* y;
+    float* pre;  // g, and u `plane` elements behind it
+    int64_t plane;
+    int act;
+};
+
+template <class F>
+__global__ __launch_bounds__(F::kThreads) void k_forward(FwdArgs a) {
+    constexpr int TM = F::TM, TN = F::TN, kCols = F::BN / 2;
+    constexpr bool kF32 = F::PLANES == 3;
+    static_assert(TN == 2, "a wave holds one block of each matrix");
+    __shared__ __align__(16) unsigned char first_buffer[F::kStage], second_buffer[F::kStage];
+    const product::Place at = product::place_of(a.tiles_i, a.tiles_j, 1, 1);
+    if (!at.inside) return;
+    const int64_t i0 = at.i * F::BM, j0 = at.j * kCols;
+    const int steps = (int)((a.features + F::BK - 1) / F::BK);
+    f32x16 acc[TM][TN] = {};
+    product::accumulate<F, product::kRows, product::kRows, true, false>(a.x, a.w, 0, i0, j0, a.features, 0, steps, steps, 1, first_buffer, second_buffer, acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / F::WJ * (TM * 32), wj = wave % F::WJ * 32;
+    const int64_t j = j0 + wj + (lane & 31);
+    uint16_t* img = reinterpret_cast<uint16_t*>(first_buffer);  // bf16: the tile of y
+    if (a.pre && j < a.width) {
+#pragma unroll
+        for (int x = 0; x < TM; x++)
+#pragma unroll
+            for (int k = 0; k < 16; k++) {
+                const int64_t i = i0 + wi + x * 32 + (k >> 2) * 8 + (lane >> 5) * 4 + (k & 3);
+                if (i >= a.rows) continue;
+                float* to = a.pre + i * a.ld + j;
+                to[0] = acc[x][0][k];
+                to[a.plane] = acc[x][1][k];
+            }
+    }
+#pragma unroll
+    for (int x = 0; x < TM; x++)
+#pragma unroll
+        for (int k = 0; k < 16; k++) {
+            const int r = wi + x * 32 + (k >> 2) * 8 + (lane >> 5) * 4 + (k & 3);
+            float unused;
+            const float y = act_of<false>(a.act, acc[x][0][k], unused) * acc[x][1][k];
+            if (kF32) {
+                if (i0 + r < a.rows && j < a.width) static_cast<float*>(a.y)[(i0 + r) * a.width + j] = y;
+            } else {
+                img[r * kCols + wj + (lane & 31)] = f32_to_bf16(y);
+            }
+        }
+    if (kF32) return;
+    static_assert(kF32 || F::BM * kCols * 2 <= F::kStage, "the tile of y in one buffer");
+    __syncthreads();
+    const bool whole = (a.width & 7) == 0;
+#pragma unroll 2
+    for (int e = threadIdx.x; e < F::BM * (kCols / 8); e += F::kThreads) {
+        const int r = e / (kCols / 8), c = (e - r * (kCols / 8)) * 8;
+        const int64_t i = i0 + r, col = j0 + c;
+        if (i >= a.rows || col >= a.width) continue;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(img + r * kCols + c);
+        uint16_t* to = static_cast<uint16_t*>(a.y) + i * a.width + col;
+        if (whole) {
+            *reinterpret_cast<u32x4*>(to) = v;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; k++)
+                if (col + k < a.width) to[k] = (uint16_t)(v[k >> 1] >> ((k & 1) * 16));
+        }
+    }
+}
+
+struct FewArgs {
+    const void *x, *w_gate, *w_up;
+    int64_t rows, features, width, ld;
+    void* y;
+    float* pre;
+    int64_t plane;
+    int act;
+};
+template <class T, int NT>
+__global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
+    __shared__ f32x4 shared[2 * NT * few::kWaves * 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t f0 = (int64_t)blockIdx.x * 16, row = f0 + (lane & 15) < a.width ? f0 + (lane & 15) : a.width - 1;
+    const T* const w[2] = {static_cast<const T*>(a.w_gate) + row * a.features, static_cast<const T*>(a.w_up) + row * a.features};
+    const T* x[NT];
+#pragma unroll
+    for (int n = 0; n < NT; n++) {
+        const int64_t t = n * 16 + (lane & 15);
+        x[n] = static_cast<const T*>(a.x) + (t < a.rows ? t : a.rows - 1) * a.features;
+    }
+    f32x4 sums[2];
+    few::accumulate<T, 2, NT>(w, x, a.features, sums, shared);
+    const int64_t t = wave * 16 + (lane & 15), f = f0 + (lane >> 4) * 4;
+    if (wave >= NT || t >= a.rows) return;
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        if (f + e >= a.width) break;
+        float unused;
+        const float y = act_of<false>(a.act, sums[0][e], unused) * sums[1][e];
+        const int64_t to = t * a.width + f + e;
+        if (sizeof(T) == 4)
+            static_cast<float*>(a.y)[to] = y;
+        else
+            static_cast<uint16_t*>(a.y)[to] = f32_to_bf16(y);
+        if (a.pre) {
+            float* keep = a.pre + t * a.ld + f + e;
+            keep[0] = sums[0][e];
+            keep[a.plane] = sums[1][e];
+        }
+    }
+}
+
+struct GradArgs {
+    const float* pre;
+    int64_t plane, rows, width, ld;
+    const void* dy;
+    uint16_t* to;  // dg, then du: planes of `plane` elements each
+    int act;
+};
+// dg and du, eight elements per thread and turn; zeros behind the columns.
+template <bool F32>
+__global__ __launch_bounds__(256) void k_grads(GradArgs a) {
+    constexpr int P = F32 ? 3 : 1;
+    const int64_t wide = a.ld / 8, n = a.rows * wide;
+    const bool whole = (a.width & 7) == 0;
+    for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < n; k += (int64_t)gridDim.x * 256) {
+        const int64_t row = k / wide, col = (k - row * wide) * 8, from = row * a.width + col;
+        const f32x4 g[2] = {*reinterpret_cast<const f32x4*>(a.pre + k * 8), *reinterpret_cast<const f32x4*>(a.pre + k * 8 + 4)};
+        const f32x4 u[2] = {*reinterpret_cast<const f32x4*>(a.pre + a.plane + k * 8), *reinterpret_cast<const f32x4*>(a.pre + a.plane + k * 8 + 4)};
+        float dy[8];
+        if (F32) {
+            const float* p = static_cast<const float*>(a.dy) + from;
+            if (whole) {
+                const f32x4 v[2] = {*reinterpret_cast<const f32x4*>(p), *reinterpret_cast<const f32x4*>(p + 4)};
+#pragma unroll
+                for (int e = 0; e < 8; e++) dy[e] = v[e >> 2][e & 3];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e++) dy[e] = col + e < a.width ? p[e] : 0.f;
+            }
+        } else {
+            const uint16_t* p = static_cast<const uint16_t*>(a.dy) + from;
+            if (whole) {
+                const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+                for (int e = 0; e < 8; e++) dy[e] = (e & 1) ? tile::hi_f32(v[e >> 1]) : tile::lo_f32(v[e >> 1]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e++) dy[e] = col + e < a.width ? bf16_to_f32(p[e]) : 0.f;
+            }
+        }
+        float dg[8], du[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            float slope;
+            const float act = act_of<true>(a.act, g[e >> 2][e & 3], slope);
+            const bool in = col + e < a.width;  // (behind the columns nothing was written)
+            du[e] = in ? dy[e] * act : 0.f;
+            dg[e] = in ? dy[e] * u[e >> 2][e & 3] * slope : 0.f;
+        }
+        uint16_t* to = a.to + k * 8;
+#pragma unroll
+        for (int which = 0; which < 2; which++) {
+            const float* v = which ? du : dg;
+            u32x4 w[P];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                if (F32) {
+                    uint16_t lo[3], hi[3];
+                    product::split(v[2 * e], lo);
+                    product::split(v[2 * e + 1], hi);
+#pragma unroll
+                    for (int h = 0; h < P; h++) w[h][e] = lo[h] | (uint32_t)hi[h] << 16;
+                } else {
+                    w[0][e] = tile::pack_bf16(v[2 * e], v[2 * e + 1]);
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < P; h++) *reinterpret_cast<u32x4*>(to + (which * P + h) * a.plane) = w[h];
+        }
+    }
+}
+
+constexpr int kFewRows = 32;
+uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
+
+template <class T>
+void launch_few(const FewArgs& a, hipStream_t stream) {
+    const dim3 grid((unsigned)((a.width + 15) / 16));
+    if (a.rows <= 16)
+        CANVAS_LAUNCH((k_few<T, 1>), grid, dim3(few::kThreads), 0, stream, a);
+    else
+        CANVAS_LAUNCH((k_few<T, 2>), grid, dim3(few::kThreads), 0, stream, a);
+}
+template <class F>
+void launch_forward(const FwdArgs& a, hipStream_t stream) {
+    CANVAS_LAUNCH(k_forward<F>, rows_of_workgroups(a.tiles_i * a.tiles_j, F::kThreads), dim3(F::kThreads), 0, stream, a);
+}
+
+// The three tensors that products read, as they read them.
+struct Operands {
+    Factor x, w;
+};
+Operands operands_of(const Shape& s, const Plan& p, const void* x, const void* w_gate, const void* w_up, char* ws) {
+    Operands o;
+    const void* given[3] = {x, w_gate, w_up};
+    const uint16_t* at[3];
+    for (int i = 0; i < 3; i++) at[i] = p.copies ? reinterpret_cast<const uint16_t*>(ws + p.copy_at[i]) : static_cast<const uint16_t*>(given[i]);
+    const int64_t ld = product::up8(s.features);
+    o.x = Factor{{at[0], at[0]}, ld, s.rows * ld, s.rows, nullptr};
+    o.w = Factor{{at[1], at[2]}, ld, s.width * ld, s.width, nullptr};
+    return o;
+}
+void make_copies(const Shape& s, const Plan& p, const void* x, const void* w_gate, const void* w_up, char* ws, hipStream_t stream) {
+    auto to = [&](int i) { return reinterpret_cast<uint16_t*>(ws + p.copy_at[i]); };
+    const product::Copy c[3] = {{x, to(0), s.rows, s.features}, {w_gate, to(1), s.width, s.features}, {w_up, to(2), s.width, s.features}};
+    product::copy(s.f32, c, 3, stream);
+}
+
+}  // namespace
+
+Plan plan_of(const Shape& s) {
+    Plan p;
+    const int64_t ld = product::up8(s.features), wide = product::up8(s.width), planes = s.f32 ? 3 : 1;
+    p.few = s.rows <= kFewRows;
+    p.copies = (s.f32 || ld != s.features) && !(p.few && s.inference);
+    p.forward = product::cut_of(s.f32, s.rows, 2 * s.width, s.features, 1, false);
+    p.forward.tiles_j = (s.width + p.forward.side / 2 - 1) / (p.forward.side / 2);
+    p.launches_fwd = 1 + (p.copies && !p.few);
+    p.most_tiles = p.few ? (s.width + 15) / 16 : p.forward.tiles();
+    uint64_t at = 0;
+    auto take = [&](uint64_t bytes) {
+        const uint64_t r = at;
+        at += up256(bytes);
+        return r;
+    };
+    if (p.copies) {
+        const int64_t rows[3] = {s.rows, s.width, s.width};
+        for (int i = 0; i < 3; i++) p.copy_at[i] = take(2ull * planes * rows[i] * ld);
+    }
+    if (!s.inference) {
+        p.dx = product::cut_of(s.f32, s.rows, s.features, 2 * s.width, 1, true);
+        p.dw = product::cut_of(s.f32, s.width, s.features, s.rows, 2, true);
+        p.launches_bwd = (p.copies && p.few) + 1 + product::launches_of(p.dx, false) + product::launches_of(p.dw, false);
+        p.most_tiles = std::max({p.most_tiles, p.dx.tiles() * p.dx.splits, 2 * p.dw.tiles() * p.dw.splits});
+        p.pre_at = take(8ull * s.rows * wide);
+        p.grad_at = take(4ull * planes * s.rows * wide);
+        p.parts_at = take(std::max(product::parts_bytes(p.dx, 1, false), product::parts_bytes(p.dw, 2, false)));
+    }
+    p.workspace_bytes = at;
+    return p;
+}
+
+void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
+    const int64_t ld = product::up8(s.width);
+    float* pre = s.inference ? nullptr : reinterpret_cast<float*>(a.ws + p.pre_at);
+    if (p.few) {
+        const FewArgs f{a.x, a.w_gate, a.w_up, s.rows, s.features, s.width, ld, a.y, pre, s.rows * ld, s.act};
+        return s.f32 ? launch_few<float>(f, stream) : launch_few<uint16_t>(f, stream);
+    }
+    if (p.copies) make_copies(s, p, a.x, a.w_gate, a.w_up, a.ws, stream);
+    const Operands o = operands_of(s, p, a.x, a.w_gate, a.w_up, a.ws);
+    const FwdArgs f{o.x, o.w, s.rows, s.features, s.width, p.forward.tiles_i, p.forward.tiles_j, ld, a.y, pre, s.rows * ld, s.act};
+    if (s.f32)
+        launch_forward<product::Triple>(f, stream);
+    else if (p.forward.side == 256)
+        launch_forward<product::Large>(f, stream);
+    else
+        launch_forward<product::Middle>(f, stream);
+}
+
+void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
+    const int64_t ld = product::up8(s.width), plane = s.rows * ld, planes = s.f32 ? 3 : 1;
+    if (p.copies && p.few) make_copies(s, p, a.x, a.w_gate, a.w_up, a.ws, stream);
+    uint16_t* grads = reinterpret_cast<uint16_t*>(a.ws + p.grad_at);
+    const GradArgs g{reinterpret_cast<const float*>(a.ws + p.pre_at), plane, s.rows, s.width, ld, a.dy, grads, s.act};
+    const dim3 grid((unsigned)std::min<int64_t>((plane / 8 + 255) / 256, 8192));
+    if (s.f32)
+        CANVAS_LAUNCH(k_grads<true>, grid, dim3(256), 0, stream, g);
+    else
+        CANVAS_LAUNCH(k_grads<false>, grid, dim3(256), 0, stream, g);
+    const Operands o = operands_of(s, p, a.x, a.w_gate, a.w_up, a.ws);
+    const uint16_t* of[2] = {grads, grads + planes * plane};
+    float* parts = reinterpret_cast<float*>(a.ws + p.parts_at);
+    product::Product d;
+    d.f32 = s.f32;
+    d.a = Factor{{of[0], of[1]}, ld, plane, s.rows, nullptr};
+    d.a_rows = true;
+    d.b = o.w;
+    d.b.count = s.features;
+    d.depth = s.width;
+    d.segments = 2;
+    d.out[0] = a.dx;
+    d.ld = s.features;
+    d.cut = p.dx;
+    d.parts = p.dx.splits > 1 ? parts : nullptr;
+    product::multiply(d, stream);
+    d.a.count = s.width;
+    d.a_rows = false;
+    d.b = o.x;
+    d.b.count = s.features;
+    d.depth = s.rows;
+    d.segments = 1;
+    d.results = 2;
+    d.out[0] = a.dw_gate;
+    d.out[1] = a.dw_up;
+    d.cut = p.dw;
+    d.parts = p.dw.splits > 1 ? parts : nullptr;
+    product::multiply(d, stream);
+}
+
+}  // namespace gated
+}  // namespace canvas

@@ -1,0 +1,540 @@
+// Log probabilities of given tokens from features and the head's weight.
+//
+// Forward: tiles of logits that never leave the registers.  Classes are the rows of a tile and the rows of x its columns, so that a lane
+// has the classes of its tile for one or two rows of x; it takes their largest logit m, S = sum exp(z - z_m) and sum exp(z - z_m) (z - z_m), joins them with the
+// other half of the wave, and leaves them to a second launch that joins the segments of all classes in a fixed order.
+// Backward: a piece of the classes at a time, a tile of logits is computed again and becomes their gradients in bf16 (three planes of them in fp32
+// plans), rows of x by classes; dx is the sum over all pieces' products with W, dW of the piece one product with x.
+#include "head_kernels.hpp"
+
+#include <algorithm>
+
+#include "../../include/canvas_head.h"
+#include "device_util.hpp"
+#include "exp_util.hpp"
+#include "few_device.hpp"
+#include "launch.hpp"
+#include "product_device.hpp"
+#include "tile_util.hpp"
+#include "wave_util.hpp"
+
+namespace canvas {
+namespace head {
+namespace {
+
+using product::f32x16;
+using product::f32x4;
+using product::Factor;
+using product::Form;
+using tile::u32x4;
+
+constexpr float kInf = __builtin_inff(), kLowest = -3.402823466e38f;
+
+// z - z_max of one logit, in powers of two: (logit - most) * scale.  The largest number in the place of a temperature that log2(e) takes past it.
+__device__ __forceinline__ float scale_of(float it) { return fminf(it * kLog2e, 3.402823466e38f); }
+
+// The sums of some logits of one row: e = exp(z - z_most) added up, and e (z - z_most) in powers of two.
+struct Sums {
+    float most, s, t;
+};
+__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float scale) {
+    Sums r;
+    r.most = fmaxf(a.most, b.most);
+    const float da = (a.most - r.most) * scale, db = (b.most - r.most) * scale, ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
+    r.s = fmaf(a.s, ea, b.s * eb);
+    // (a part so far below that its exponential is zero counts nothing, however far it is)
+    r.t = fmaf(ea, fmaf(a.s, fmaxf(da, -300.f), a.t), eb * fmaf(b.s, fmaxf(db, -300.f), b.t));
+    return r;
+}
+template <int O>
+__device__ __forceinline__ float from_lane(float v) { return __shfl_xor(v, O); }
+
+// Whether the mask allows each of four classes from c on (a multiple of four), and whether they are classes at all.
+__device__ __forceinline__ uint32_t allowed4(const uint8_t* mask, int64_t c, int64_t classes) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+        if (c + e < classes && (!mask || mask[c + e])) w |= 1u << e;
+    return w;
+}
+
+struct FwdArgs {
+    Factor w, x;
+    int64_t rows, features, classes, tiles_i, tiles_j;
+    float it;
+    const uint8_t* mask;
+    const int64_t* tokens;
+    Sums* sums;    // [segments][rows]
+    float* token;  // [rows]: the token's logit
+};
+
+// N logits of one row of x in a lane, the sums of those and of what the lanes LOW, 2 LOW, .. 32 apart hold.
+template <int N, int LOW>
+__device__ __forceinline__ Sums sums_of(const float (&z)[N], float scale) {
+    Sums r{kLowest, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < N; k++) r.most = fmaxf(r.most, z[k]);
+    if (LOW <= 16) r.most = fmaxf(r.most, from_lane<16>(r.most));
+    r.most = fmaxf(r.most, from_lane<32>(r.most));
+#pragma unroll
+    for (int k = 0; k < N; k++) {
+        const float d = (z[k] - r.most) * scale, e = __builtin_amdgcn_exp2f(d);  // (NaN and +inf make both sums NaN)
+        r.s += e;
+        r.t = fmaf(e, fmaxf(d, -300.f), r.t);
+    }
+    if (LOW <= 16) {
+        r.s += from_lane<16>(r.s);
+        r.t += from_lane<16>(r.t);
+    }
+    r.s += from_lane<32>(r.s);
+    r.t += from_lane<32>(r.t);
+    return r;
+}
+
+template <class F>
+__global__ __launch_bounds__(F::kThreads) void k_logits(FwdArgs a) {
+    constexpr int TM = F::TM, TN = F::TN;
+    __shared__ __align__(16) unsigned char first_buffer[F::kStage], second_buffer[F::kStage];
+    const product::Place at = product::place_of(a.tiles_i, a.tiles_j, 1, 1);
+    if (!at.inside) return;
+    const int64_t i0 = at.i * F::BM, j0 = at.j * F::BN;
+    const int steps = (int)((a.features + F::BK - 1) / F::BK);
+    f32x16 acc[TM][TN] = {};
+    product::accumulate<F, product::kRows, product::kRows, false, false>(a.w, a.x, 0, i0, j0, a.features, 0, steps, steps, 1, first_buffer, second_buffer, acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c0 = i0 + wave / F::WJ * (TM * 32) + (lane >> 5) * 4, t0 = j0 + wave % F::WJ * (TN * 32) + (lane & 31);
+    const float scale = scale_of(a.it);
+    if (a.mask || i0 + F::BM > a.classes) {
+#pragma unroll
+        for (int x = 0; x < TM; x++)
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                const uint32_t in = allowed4(a.mask, c0 + x * 32 + q * 8, a.classes);
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (!(in >> e & 1)) {
+#pragma unroll
+                        for (int y = 0; y < TN; y++) acc[x][y][q * 4 + e] = -kInf;
+                    }
+            }
+    }
+#pragma unroll
+    for (int y = 0; y < TN; y++) {
+        const int64_t t = t0 + y * 32;
+        if (a.token && t < a.rows) {
+            const int64_t c = a.tokens[t] - c0;
+            if (c >= 0 && c < TM * 32 && !(c & 4)) {
+#pragma unroll
+                for (int x = 0; x < TM; x++)
+#pragma unroll
+                    for (int k = 0; k < 16; k++)
+                        if (c == x * 32 + (k >> 2) * 8 + (k & 3)) a.token[t] = acc[x][y][k];
+            }
+        }
+        float z[TM * 16];
+#pragma unroll
+        for (int x = 0; x < TM; x++)
+#pragma unroll
+            for (int k = 0; k < 16; k++) z[x * 16 + k] = acc[x][y][k];
+        const Sums r = sums_of<TM * 16, 32>(z, scale);
+        if (lane < 32 && t < a.rows) a.sums[(at.i * F::WI + wave / F::WJ) * a.rows + t] = r;
+    }
+}
+
+struct FewArgs {
+    const void *x, *weight;
+    int64_t rows, features, classes;
+    float it;
+    const uint8_t* mask;
+    const int64_t* tokens;
+    Sums* sums;
+    float* token;
+};
+constexpr int kFewBlocks = 2, kFewClasses = 16 * kFewBlocks;  // of a workgroup
+template <class T, int NT>
+__global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
+    constexpr int R = kFewBlocks;
+    __shared__ f32x4 shared[R * NT * few::kWaves * 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t first = (int64_t)blockIdx.x * kFewClasses;
+    const T *w[R], *x[NT];
+#pragma unroll
+    for (int r = 0; r < R; r++) {
+        const int64_t c = first + r * 16 + (lane & 15);
+        w[r] = static_cast<const T*>(a.weight) + (c < a.classes ? c : a.classes - 1) * a.features;
+    }
+#pragma unroll
+    for (int n = 0; n < NT; n++) {
+        const int64_t t = n * 16 + (lane & 15);
+        x[n] = static_cast<const T*>(a.x) + (t < a.rows ? t : a.rows - 1) * a.features;
+    }
+    f32x4 sums[R];
+    few::accumulate<T, R, NT>(w, x, a.features, sums, shared);
+    if (wave >= NT) return;
+    const int64_t t = wave * 16 + (lane & 15), c0 = first + (lane >> 4) * 4;
+    float z[R * 4];
+#pragma unroll
+    for (int r = 0; r < R; r++) {
+        const uint32_t in = allowed4(a.mask, c0 + r * 16, a.classes);
+#pragma unroll
+        for (int e = 0; e < 4; e++) z[r * 4 + e] = in >> e & 1 ? sums[r][e] : -kInf;
+    }
+    if (a.token && t < a.rows) {
+        const int64_t c = a.tokens[t] - c0;
+#pragma unroll
+        for (int k = 0; k < R * 4; k++)
+            if (c == (k >> 2) * 16 + (k & 3)) a.token[t] = z[k];
+    }
+    const Sums r = sums_of<R * 4, 16>(z, scale_of(a.it));
+    if (lane < 16 && t < a.rows) a.sums[blockIdx.x * a.rows + t] = r;
+}
+
+struct RowArgs {
+    int64_t rows, classes;
+    int segments, across;  // rows of x by a workgroup: a power of two
+    float it;
+    const uint8_t* mask;
+    const int64_t* tokens;
+    const Sums* sums;
+    const float* token;
+    float *logprob, *entropy;
+    Row* row;
+};
+// Joins the segments of each row.
+__global__ __launch_bounds__(256) void k_rows(RowArgs a) {
+    __shared__ Sums part[256];
+    const int mine = threadIdx.x & (a.across - 1), turn = threadIdx.x / a.across, turns = 256 / a.across;
+    const int64_t t = (int64_t)blockIdx.x * a.across + mine;
+    const float scale = scale_of(a.it);
+    Sums r{kLowest, 0.f, 0.f};
+    if (t < a.rows) {
+        constexpr int kAhead = 4;
+        for (int k = turn; k < a.segments; k += turns * kAhead) {
+            Sums s[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; u++) s[u] = k + u * turns < a.segments ? a.sums[(int64_t)(k + u * turns) * a.rows + t] : Sums{kLowest, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < kAhead; u++) r = join(r, s[u], scale);
+        }
+    }
+    part[threadIdx.x] = r;
+    __syncthreads();
+    for (int o = turns / 2; o; o >>= 1) {
+        if (turn < o) part[threadIdx.x] = join(part[threadIdx.x], part[threadIdx.x + o * a.across], scale);
+        __syncthreads();
+    }
+    if (turn || t >= a.rows) return;
+    r = part[threadIdx.x];
+    const bool empty = r.s == 0.f;  // (the largest of what is left counts one)
+    const float log_sum = empty ? -kInf : logf(r.s), entropy = empty ? 0.f : log_sum - r.t / r.s * kLn2;
+    if (a.entropy) a.entropy[t] = entropy;
+    if (a.logprob) {
+        const int64_t c = a.tokens[t];
+        const bool given = c >= 0 && c < a.classes;
+        float v = 0.f;
+        if (given) {
+            // (a row with nothing left, and a masked token in a row of NaN, too)
+            const bool hidden = a.mask && !a.mask[c];
+            v = empty || hidden ? -kInf : (a.token[t] - r.most) * a.it - log_sum;
+        }
+        a.logprob[t] = v;
+    }
+    if (a.row) a.row[t] = Row{r.most, log_sum, entropy, empty ? 0.f : 1.f / r.s};
+}
+
+struct SlopeArgs {
+    int64_t rows, classes;
+    float it;
+    const int64_t* tokens;
+    const float *dlogprob, *dentropy;
+    const Row* row;
+    Slope* slope;
+    uint8_t* live;
+};
+__global__ __launch_bounds__(256) void k_slopes(SlopeArgs a) {
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (t >= a.rows) return;
+    const Row r = a.row[t];
+    const int64_t c = a.tokens ? a.tokens[t] : -1;
+    const bool given = c >= 0 && c < a.classes && a.dlogprob;
+    const float g = given ? a.dlogprob[t] * a.it : 0.f, h = a.dentropy ? a.dentropy[t] * a.it : 0.f;
+    // p (-g - h (log p + entropy)) with p = e / sum, log p = x ln 2 - log sum
+    const bool keep = r.log_sum != -kInf && (g != 0.f || h != 0.f);
+    a.slope[t] = Slope{r.most, -r.inverse * (g + h * (r.entropy - r.log_sum)), -r.inverse * h * kLn2, g, given ? (int32_t)c : -1, keep ? 0xffffffffu : 0u, {0, 0}};
+    a.live[t] = keep;
+}
+
+struct GradArgs {
+    Factor w, x;                   // of this piece
+    int64_t rows, features, classes, tiles_i, tiles_j;
+    int64_t first;                 // class of the piece
+    float it;
+    const uint8_t* mask;           // of this piece
+    const Slope* slope;
+    uint16_t* to;                  // [rows][ld], planes `plane` elements apart
+    int64_t ld, plane;
+};
+// The gradients of a tile of logits.
+template <class F>
+__global__ __launch_bounds__(F::kThreads) void k_grads(GradArgs a) {
+    constexpr int TM = F::TM, TN = F::TN, P = F::PLANES, kHalf = F::BN / 2;
+    __shared__ __align__(16) unsigned char first_buffer[F::kStage], second_buffer[F::kStage];
+    const product::Place at = product::place_of(a.tiles_i, a.tiles_j, 1, 1);
+    if (!at.inside) return;
+    const int64_t i0 = at.i * F::BM, j0 = at.j * F::BN;
+    const int steps = (int)((a.features + F::BK - 1) / F::BK);
+    f32x16 acc[TM][TN] = {};
+    product::accumulate<F, product::kRows, product::kRows, false, false>(a.w, a.x, 0, i0, j0, a.features, 0, steps, steps, 1, first_buffer, second_buffer, acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / F::WJ * (TM * 32) + (lane >> 5) * 4, wj = wave % F::WJ * (TN * 32) + (lane & 31);
+    const float scale = scale_of(a.it);
+#pragma unroll
+    for (int y = 0; y < TN; y++) {
+        const int64_t t = j0 + wj + y * 32;
+        Slope s{};
+        s.at = -1;
+        if (t < a.rows) s = a.slope[t];
+        const int64_t token = s.at - a.first - i0 - wi;
+        const bool here = s.at >= 0 && token >= 0 && token < TM * 32 && !(token & 4);
+#pragma unroll
+        for (int x = 0; x < TM; x++)
+#pragma unroll
+            for (int k = 0; k < 16; k++) {
+                const float d = (acc[x][y][k] - s.most) * scale, e = __builtin_amdgcn_exp2f(d);
+                acc[x][y][k] = e * fmaf(s.second, fmaxf(d, -300.f), s.first);
+            }
+        if (__any(here)) {
+#pragma unroll
+            for (int x = 0; x < TM; x++)
+#pragma unroll
+                for (int k = 0; k < 16; k++)
+                    if (here && token == x * 32 + (k >> 2) * 8 + (k & 3)) acc[x][y][k] += s.token;
+        }
+        if (!__all(s.keep)) {
+#pragma unroll
+            for (int x = 0; x < TM; x++)
+#pragma unroll
+                for (int k = 0; k < 16; k++)
+                    if (!s.keep) acc[x][y][k] = 0.f;
+        }
+    }
+    if (a.mask || i0 + F::BM > a.classes) {
+#pragma unroll
+        for (int x = 0; x < TM; x++)
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                const uint32_t in = allowed4(a.mask, i0 + wi + x * 32 + q * 8, a.classes);
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (!(in >> e & 1)) {
+#pragma unroll
+                        for (int y = 0; y < TN; y++) acc[x][y][q * 4 + e] = 0.f;
+                    }
+            }
+    }
+    // Plane by plane through LDS, rows of x by classes: the rows of the first half of the tile in one buffer, the others in the other.  16-byte pieces
+    // of row r are exchanged by the bits of r, so that the lanes of a wave, a row each, write to different banks.
+    static_assert(kHalf * F::BM * 2 <= F::kStage, "half a tile in a buffer");
+    constexpr int kPieces = F::BM / 8;
+#pragma unroll
+    for (int h = 0; h < P; h++) {
+        if (h) __syncthreads();
+        unsigned char* img = wave % F::WJ * (TN * 32) < kHalf ? first_buffer : second_buffer;
+#pragma unroll
+        for (int y = 0; y < TN; y++) {
+            const int r = (wj + y * 32) & (kHalf - 1);
+#pragma unroll
+            for (int x = 0; x < TM; x++)
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    uint32_t w[2];
+                    if (P == 1) {
+                        w[0] = tile::pack_bf16(acc[x][y][4 * q], acc[x][y][4 * q + 1]);
+                        w[1] = tile::pack_bf16(acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]);
+                    } else {
+                        uint16_t part[4][3];
+#pragma unroll
+                        for (int e = 0; e < 4; e++) product::split(acc[x][y][4 * q + e], part[e]);
+                        w[0] = part[0][h] | (uint32_t)part[1][h] << 16;
+                        w[1] = part[2][h] | (uint32_t)part[3][h] << 16;
+                    }
+                    const int c = wi + x * 32 + q * 8;  // of the tile, a multiple of 4
+                    __builtin_memcpy(img + r * (F::BM * 2) + ((((c >> 3) ^ r) & (kPieces - 1)) << 4) + (c & 4) * 2, w, 8);
+                }
+        }
+        __syncthreads();
+#pragma unroll 4
+        for (int e = threadIdx.x; e < F::BN * kPieces; e += F::kThreads) {
+            const int r = e / kPieces, c = e % kPieces;
+            const int64_t t = j0 + r, col = i0 + c * 8;
+            if (t >= a.rows || col >= a.ld) continue;
+            const unsigned char* from = r < kHalf ? first_buffer : second_buffer;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(from + (r & (kHalf - 1)) * (F::BM * 2) + (((c ^ r) & (kPieces - 1)) << 4));
+            *reinterpret_cast<u32x4*>(a.to + h * a.plane + t * a.ld + col) = v;
+        }
+    }
+}
+
+constexpr int kFewRows = 32;
+// Gradients of a piece's logits: as much as stays in the last-level cache between the launch that writes them and the two that read them.
+constexpr uint64_t kPieceBytes = 128u << 20;
+uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
+
+template <class T>
+void launch_few(const FewArgs& a, hipStream_t stream) {
+    const dim3 grid((unsigned)((a.classes + kFewClasses - 1) / kFewClasses));
+    if (a.rows <= 16)
+        CANVAS_LAUNCH((k_few<T, 1>), grid, dim3(few::kThreads), 0, stream, a);
+    else
+        CANVAS_LAUNCH((k_few<T, 2>), grid, dim3(few::kThreads), 0, stream, a);
+}
+template <class F>
+void launch_logits(const FwdArgs& a, hipStream_t stream) {
+    CANVAS_LAUNCH(k_logits<F>, rows_of_workgroups(a.tiles_i * a.tiles_j, F::kThreads), dim3(F::kThreads), 0, stream, a);
+}
+template <class F>
+void launch_grads(const GradArgs& a, hipStream_t stream) {
+    CANVAS_LAUNCH(k_grads<F>, rows_of_workgroups(a.tiles_i * a.tiles_j, F::kThreads), dim3(F::kThreads), 0, stream, a);
+}
+
+struct Operands {
+    Factor x, w;
+};
+Operands operands_of(const Shape& s, const Plan& p, const void* x, const void* w, char* ws) {
+    const int64_t ld = product::up8(s.features);
+    const uint16_t *ax = static_cast<const uint16_t*>(x), *aw = static_cast<const uint16_t*>(w);
+    if (p.copies) {
+        ax = reinterpret_cast<const uint16_t*>(ws + p.copy_at[0]);
+        aw = reinterpret_cast<const uint16_t*>(ws + p.copy_at[1]);
+    }
+    return Operands{Factor{{ax, ax}, ld, s.rows * ld, s.rows, nullptr}, Factor{{aw, aw}, ld, s.classes * ld, s.classes, nullptr}};
+}
+void make_copies(const Shape& s, const Plan& p, const void* x, const void* w, char* ws, hipStream_t stream) {
+    const product::Copy c[2] = {{x, reinterpret_cast<uint16_t*>(ws + p.copy_at[0]), s.rows, s.features}, {w, reinterpret_cast<uint16_t*>(ws + p.copy_at[1]), s.classes, s.features}};
+    product::copy(s.f32, c, 2, stream);
+}
+
+}  // namespace
+
+Plan plan_of(const Shape& s) {
+    Plan p;
+    const int64_t ld = product::up8(s.features), planes = s.f32 ? 3 : 1;
+    p.few = s.rows <= kFewRows;
+    p.copies = (s.f32 || ld != s.features) && !(p.few && s.inference);
+    p.logits = product::cut_of(s.f32, s.classes, s.rows, s.features, 1, false);
+    p.segments = (int)(p.few ? (s.classes + kFewClasses - 1) / kFewClasses : p.logits.tiles_i * 2);
+    p.launches_fwd = 2 + (p.copies && !p.few);
+    p.most_tiles = p.few ? p.segments : p.logits.tiles();
+    uint64_t at = 0;
+    auto take = [&](uint64_t bytes) {
+        const uint64_t r = at;
+        at += up256(bytes);
+        return r;
+    };
+    p.sums_at = take(sizeof(Sums) * (uint64_t)s.rows * p.segments);
+    p.token_at = take(4ull * s.rows);
+    if (p.copies) {
+        p.copy_at[0] = take(2ull * planes * s.rows * ld);
+        p.copy_at[1] = take(2ull * planes * s.classes * ld);
+    }
+    if (!s.inference) {
+        p.rows_at = take(sizeof(Row) * (uint64_t)s.rows);
+        p.slope_at = take(sizeof(Slope) * (uint64_t)s.rows);
+        p.live_at = take(s.rows);
+        const int64_t fit = std::max<int64_t>(1, (int64_t)(kPieceBytes / (2ull * planes * s.rows)) / 256) * 256;
+        p.pieces = (int)((s.classes + fit - 1) / fit);
+        p.length = std::min<int64_t>(((s.classes + p.pieces - 1) / p.pieces + 255) / 256 * 256, s.classes);
+        p.pieces = (int)((s.classes + p.length - 1) / p.length);
+        p.piece = product::cut_of(s.f32, p.length, s.rows, s.features, 1, false);
+        p.dx = product::cut_of(s.f32, s.rows, s.features, p.length, 1, true);
+        p.dw = product::cut_of(s.f32, p.length, s.features, s.rows, 1, true);
+        p.launches_bwd = (p.copies && p.few) + 1 + p.pieces * (2 + product::launches_of(p.dw, false)) + (product::launches_of(p.dx, p.pieces > 1) - 1);
+        p.most_tiles = std::max({p.most_tiles, p.piece.tiles(), p.dx.tiles() * p.dx.splits, p.dw.tiles() * p.dw.splits});
+        p.grad_at = take(2ull * planes * s.rows * product::up8(p.length));
+        p.parts_dx_at = take(product::parts_bytes(p.dx, 1, p.pieces > 1));
+        p.parts_dw_at = take(product::parts_bytes(p.dw, 1, false));
+    }
+    p.workspace_bytes = at;
+    return p;
+}
+
+void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
+    Sums* sums = reinterpret_cast<Sums*>(a.ws + p.sums_at);
+    float* token = a.logprob ? reinterpret_cast<float*>(a.ws + p.token_at) : nullptr;
+    if (p.few) {
+        const FewArgs f{a.x, a.weight, s.rows, s.features, s.classes, a.it, a.mask, a.tokens, sums, token};
+        if (s.f32)
+            launch_few<float>(f, stream);
+        else
+            launch_few<uint16_t>(f, stream);
+    } else {
+        if (p.copies) make_copies(s, p, a.x, a.weight, a.ws, stream);
+        const Operands o = operands_of(s, p, a.x, a.weight, a.ws);
+        const FwdArgs f{o.w, o.x, s.rows, s.features, s.classes, p.logits.tiles_i, p.logits.tiles_j, a.it, a.mask, a.tokens, sums, token};
+        if (s.f32)
+            launch_logits<product::Triple>(f, stream);
+        else if (p.logits.side == 256)
+            launch_logits<product::Large>(f, stream);
+        else
+            launch_logits<product::Middle>(f, stream);
+    }
+    int across = 1;
+    while (across < 16 && across * 2 <= s.rows) across *= 2;
+    const RowArgs r{s.rows, s.classes, p.segments, across, a.it, a.mask, a.tokens, sums, token, a.logprob, a.entropy, s.inference ? nullptr : reinterpret_cast<Row*>(a.ws + p.rows_at)};
+    CANVAS_LAUNCH(k_rows, rows_of_workgroups((s.rows + across - 1) / across, 256), dim3(256), 0, stream, r);
+}
+
+void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
+    if (p.copies && p.few) make_copies(s, p, a.x, a.weight, a.ws, stream);
+    const Operands o = operands_of(s, p, a.x, a.weight, a.ws);
+    Slope* slope = reinterpret_cast<Slope*>(a.ws + p.slope_at);
+    uint8_t* live = reinterpret_cast<uint8_t*>(a.ws + p.live_at);
+    uint16_t* grads = reinterpret_cast<uint16_t*>(a.ws + p.grad_at);
+    const SlopeArgs l{s.rows, s.classes, a.it, a.tokens, a.dlogprob, a.dentropy, reinterpret_cast<const Row*>(a.ws + p.rows_at), slope, live};
+    CANVAS_LAUNCH(k_slopes, dim3((unsigned)((s.rows + 255) / 256)), dim3(256), 0, stream, l);
+    const int64_t ld = product::up8(p.length), plane = s.rows * ld;
+    for (int n = 0; n < p.pieces; n++) {
+        const int64_t first = n * p.length, length = std::min(p.length, s.classes - first);
+        Factor w = o.w;
+        w.p[0] = w.p[1] = o.w.p[0] + first * o.w.ld;
+        w.count = length;
+        const uint8_t* mask = a.mask ? a.mask + first : nullptr;
+        const int64_t side = p.piece.side;
+        const GradArgs g{w, o.x, s.rows, s.features, length, (length + side - 1) / side, p.piece.tiles_j, first, a.it, mask, slope, grads, ld, plane};
+        if (s.f32)
+            launch_grads<product::Triple>(g, stream);
+        else if (side == 256)
+            launch_grads<product::Large>(g, stream);
+        else
+            launch_grads<product::Middle>(g, stream);
+        product::Product d;
+        d.f32 = s.f32;
+        d.a = Factor{{grads, grads}, ld, plane, s.rows, nullptr};
+        d.a_rows = true;
+        d.b = w;
+        d.b.count = s.features;
+        d.b.live = mask;
+        d.depth = length;
+        d.out[0] = a.dx;
+        d.ld = s.features;
+        d.cut = p.dx;
+        d.parts = p.dx.splits > 1 || p.pieces > 1 ? reinterpret_cast<float*>(a.ws + p.parts_dx_at) : nullptr;
+        d.first = n == 0;
+        d.last = n + 1 == p.pieces;
+        product::multiply(d, stream);
+        d.a.count = length;
+        d.a_rows = false;
+        d.b = o.x;
+        d.b.count = s.features;
+        d.b.live = live;
+        d.depth = s.rows;
+        d.out[0] = static_cast<char*>(a.dweight) + first * s.features * (s.f32 ? 4 : 2);
+        d.cut = p.dw;
+        d.cut.tiles_i = (length + p.dw.side - 1) / p.dw.side;
+        d.parts = p.dw.splits > 1 ? reinterpret_cast<float*>(a.ws + p.parts_dw_at) : nullptr;
+        d.first = d.last = true;
+        product::multiply(d, stream);
+    }
+}
+
+}  // namespace head
+}  // namespace canvas

@@ -1,0 +1,293 @@
+// The inner part of a product: a tile of results in the registers of a workgroup, both operands through LDS.
+//
+// Operands are loaded straight into LDS, a stage (BK summands of all rows of the tile) ahead of their use, into two arrays in turn.
+// Rows along k: 16-byte pieces of eight summands; piece c of row r lies at place c ^ (r / rows per line of all banks), so that the
+// pieces that 16 lanes read together fall on different banks.  Rows of k: the matrix units want eight summands of one index in a lane, so the
+// rows are read by the transposing load, a block of 4 summands x 16 indexes by 16 lanes; the 32-byte units of row k lie at unit ^
+// {0, 2, 5, 7}[k % 4], for the same reason.  What lies behind the end of the sum is not loaded: an offset outside the buffer gives zeros.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "launch.hpp"
+#include "product_kernels.hpp"
+#include "tile_util.hpp"
+
+namespace canvas {
+namespace product {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+using tile::bf16x8_t;
+using tile::u32x4;
+
+enum Side { kRows, kCols };
+
+// Tiles of BM x BN by WI x WJ waves, BK summands of PLANES planes at a time.
+template <int BM_, int BN_, int WI_, int WJ_, int PLANES_, int BK_>
+struct Form {
+    static constexpr int BM = BM_, BN = BN_, WI = WI_, WJ = WJ_, PLANES = PLANES_, BK = BK_;
+    static constexpr int kThreads = 64 * WI * WJ, TM = BM / WI / 32, TN = BN / WJ / 32, kUnits = BK / 16;
+    static constexpr int kBytesA = BM * BK * 2, kBytesB = BN * BK * 2;  // of a plane of a stage
+    static constexpr int kStage = PLANES * (kBytesA + kBytesB);
+};
+using Large = Form<256, 256, 2, 4, 1, 64>;
+using Middle = Form<128, 128, 2, 2, 1, 64>;
+using Triple = Form<128, 128, 2, 2, 3, 16>;
+
+constexpr uint32_t kOutside = 0x80000000u;  // an offset behind the end of every buffer
+__device__ __forceinline__ tile::rsrc_t buffer_from(const void* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffffff, 0x00020000); }
+// 16 bytes per lane to LDS, lane after lane behind `to` (the same for the whole wave).
+__device__ __forceinline__ void load_to_lds(tile::rsrc_t from, unsigned char* to, uint32_t offset) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, offset, 0, 0, 0);
+}
+// A barrier behind which everybody's loads to LDS have arrived.
+__device__ __forceinline__ void loads_arrived() {
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    __syncthreads();
+}
+
+template <int ROW>
+__device__ __forceinline__ int piece_of(int r, int c) { return c ^ ((r / (256 / ROW)) & (ROW / 16 - 1)); }
+__device__ __forceinline__ int unit_of(int k, int unit) { return unit ^ (((k & 1) << 1) | ((k >> 1) & 1) * 5); }
+
+// What a thread loads of one operand.  PAIRS: indexes are taken 32 by 32 from the two matrices in turn.  LIVE: rows of k may be left out.
+template <class F, int BX, Side SIDE, bool PAIRS, bool LIVE>
+struct Loader {
+    static constexpr int kRow = SIDE == kRows ? F::BK * 2 : BX * 2, kPieces = kRow / 16;
+    static constexpr int kPlane = BX * F::BK * 2, kTimes = kPlane / 16 / F::kThreads;
+    static_assert(kPlane % (16 * F::kThreads) == 0 && 256 % (SIDE == kRows ? kRow : 1) == 0, "whole pieces for every thread");
+    uint32_t offset[kTimes];
+    uint8_t alive[kTimes];
+    const uint16_t *at, *other;  // what the next load begins with; in the second matrix of a pair
+
+    static __device__ __forceinline__ int row_of(int tid, int q) { return (tid + q * F::kThreads) / kPieces; }
+    static __device__ __forceinline__ int place_of(int tid, int q) { return (tid + q * F::kThreads) % kPieces; }
+
+    // The tile from index `first` on, the sum from k on.
+    __device__ __forceinline__ void seek(const Factor& f, int which, int64_t first, int64_t k) {
+        const int64_t from = SIDE == kRows ? first * f.ld + k : first + k * f.ld;
+        at = (!PAIRS && which ? f.p[1] : f.p[0]) + from;
+        if (PAIRS) other = f.p[1] + from;
+    }
+    __device__ __forceinline__ void begin(const Factor& f, int64_t first) {
+        const int left = (int)(f.count - first < BX ? f.count - first : BX);  // indexes of the tile
+#pragma unroll
+        for (int q = 0; q < kTimes; q++) {
+            const int r = row_of(threadIdx.x, q), c = place_of(threadIdx.x, q);
+            if (SIDE == kRows) {
+                int row = PAIRS ? (r >> 6) * 32 + (r & 31) : r;
+                row = row < left ? row : left - 1;  // (behind the last one: that one again, for results that nobody keeps)
+                offset[q] = (uint32_t)row * (uint32_t)f.ld * 2u + piece_of<SIDE == kRows ? kRow : 256>(r, c) * 16;
+            } else {
+                const int piece = unit_of(r, c >> 1) * 2 + (c & 1);
+                offset[q] = piece * 8 < left ? (uint32_t)r * (uint32_t)f.ld * 2u + piece * 16 : kOutside;
+            }
+            alive[q] = 1;
+        }
+    }
+    // Asks which of the rows from k on are alive.
+    __device__ __forceinline__ void ask(const Factor& f, int64_t k, int64_t depth) {
+        if (!LIVE) return;
+#pragma unroll
+        for (int q = 0; q < kTimes; q++) {
+            const int64_t row = k + row_of(threadIdx.x, q);
+            alive[q] = f.live && row < depth ? f.live[row] : 1;
+        }
+    }
+    // The next BK summands, of which there are `left`.
+    __device__ __forceinline__ void load(const Factor& f, int64_t left, unsigned char* to) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        to += wave * 1024;
+        auto put = [&](int h, int q, uint32_t o) {
+            const bool second = PAIRS && ((((wave * 64 + q * F::kThreads) / kPieces) >> 5) & 1);
+            load_to_lds(buffer_from((second ? other : at) + h * f.plane), to + h * kPlane + q * (F::kThreads * 16), LIVE && !alive[q] ? kOutside : o);
+        };
+        if (left >= F::BK) {
+#pragma unroll
+            for (int h = 0; h < F::PLANES; h++)
+#pragma unroll
+                for (int q = 0; q < kTimes; q++) put(h, q, offset[q]);
+        } else {
+            int tid = threadIdx.x;
+            asm volatile("" : "+v"(tid));  // (what follows is computed here, not kept in registers through the loop)
+#pragma unroll
+            for (int q = 0; q < kTimes; q++) {
+                const int r = row_of(tid, q), behind = SIDE == kRows ? piece_of<SIDE == kRows ? kRow : 256>(r, place_of(tid, q)) * 8 : r;
+#pragma unroll
+                for (int h = 0; h < F::PLANES; h++) put(h, q, behind >= (int)left ? kOutside : offset[q]);
+            }
+        }
+        const int64_t step = SIDE == kRows ? F::BK : F::BK * f.ld;
+        at += step;
+        if (PAIRS) other += step;
+    }
+};
+
+// Where a lane reads its operands: of block x of 32 indexes, 16 summands from unit u on.  The exchange of places is an exclusive or of bits that
+// the unit (rows along k) or the block (rows of k) has to itself, so that the other one is a constant added to the address.
+template <class F, int BX, Side SIDE, int T>
+struct Reader {
+    static constexpr int kRow = SIDE == kRows ? F::BK * 2 : BX * 2, kPlane = BX * F::BK * 2, kKept = SIDE == kRows ? F::kUnits : T;
+    int at[kKept];
+    __device__ __forceinline__ void begin(int base) {  // base: the wave's first index, a multiple of 32 T
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int n = 0; n < kKept; n++) {
+            if (SIDE == kRows) {
+                const int r = base + (lane & 31);
+                at[n] = r * kRow + piece_of<SIDE == kRows ? kRow : 256>(r, n * 2 + (lane >> 5)) * 16;
+            } else {
+                const int j = lane & 15, g = lane >> 4;
+                at[n] = ((g >> 1) * 8 + (j >> 2)) * kRow + unit_of(j >> 2, (base + n * 32) / 16 + (g & 1)) * 32 + (j & 3) * 8;
+            }
+        }
+    }
+    __device__ __forceinline__ bf16x8_t read(const unsigned char* plane, int x, int unit) const {
+        bf16x8_t v;
+        if (SIDE == kRows) {
+            v = *reinterpret_cast<const bf16x8_t*>(plane + at[SIDE == kRows ? unit : 0] + x * (32 * kRow));
+        } else {
+            typedef __attribute__((address_space(3))) s16x4* Lds;
+            const unsigned char* p = plane + at[SIDE == kRows ? 0 : x] + unit * (16 * kRow);
+            const s16x4 two[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p), __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 4 * kRow))};
+            __builtin_memcpy(&v, two, 16);
+        }
+        return v;
+    }
+};
+
+// The sum over steps begin .. end (BK summands each, `per` of them in each of `segments` halves) of a tile from (i0, j0) on.  acc[x][y]: 32 x 32
+// results from (wave's row + 32 x, wave's column + 32 y) on; register k of a lane is row (k / 4) * 8 + (lane / 32) * 4 + k % 4, column lane % 32.
+template <class F, Side SA, Side SB, bool PAIRS, bool LIVE>
+__device__ __forceinline__ void accumulate(const Factor& a, const Factor& b, int which, int64_t i0, int64_t j0, int64_t depth, int begin, int end, int per,
+                                           int segments, unsigned char* first_buffer, unsigned char* second_buffer, f32x16 (&acc)[F::TM][F::TN]) {
+    constexpr int TM = F::TM, TN = F::TN, P = F::PLANES;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Loader<F, F::BM, SA, false, false> la;
+    Loader<F, F::BN, SB, PAIRS, LIVE> lb;
+    la.begin(a, i0);
+    lb.begin(b, j0);
+    Reader<F, F::BM, SA, TM> ra;
+    Reader<F, F::BN, SB, TN> rb;
+    ra.begin(wave / F::WJ * (TM * 32));
+    rb.begin(wave % F::WJ * (TN * 32));
+    const int half = segments == 2 && begin >= per, from = segments == 2 ? half : which;
+    int64_t done = (int64_t)(begin - half * per) * F::BK;  // summands of this half that were asked for
+    la.seek(a, from, i0, done);
+    lb.seek(b, from, j0, done);
+    auto ask = [&](int step) {
+        if (LIVE) lb.ask(b, (int64_t)step * F::BK, depth);  // (one segment)
+    };
+    auto load = [&](int step, unsigned char* to) {
+        if (step >= end) return;
+        la.load(a, depth - done, to);
+        lb.load(b, depth - done, to + P * F::kBytesA);
+        done += F::BK;
+        if (segments == 2 && step + 1 == per) {
+            done = 0;
+            la.seek(a, 1, i0, 0);
+            lb.seek(b, 1, j0, 0);
+        }
+    };
+    struct Operands {
+        bf16x8_t a[TM][P], b[TN][P];
+    };
+    auto read = [&](const unsigned char* buffer, int unit, Operands& o) {
+#pragma unroll
+        for (int h = 0; h < P; h++) {
+#pragma unroll
+            for (int x = 0; x < TM; x++) o.a[x][h] = ra.read(buffer + h * F::kBytesA, x, unit);
+#pragma unroll
+            for (int y = 0; y < TN; y++) o.b[y][h] = rb.read(buffer + P * F::kBytesA + h * F::kBytesB, y, unit);
+        }
+    };
+    auto multiply = [&](const Operands& o) {
+        // pairings of planes, the smallest products first; what is left out is below 2^-24 of a term
+        constexpr int kPairings = P == 1 ? 1 : 6, kOfA[6] = {2, 0, 1, 1, 0, 0}, kOfB[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+        for (int h = 0; h < kPairings; h++)
+#pragma unroll
+            for (int x = 0; x < TM; x++)
+#pragma unroll
+                for (int y = 0; y < TN; y++)
+                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(o.a[x][P == 1 ? 0 : kOfA[h]], o.b[y][P == 1 ? 0 : kOfB[h]], acc[x][y], 0, 0, 0);
+    };
+    Operands o[2];
+    // One stage, `now` its buffer: each unit's products run while the next one's operands are read; before the last unit
+    // everybody has read this buffer and the next stage has arrived, so the one behind that is asked for.
+    auto stage = [&](int step, int parity, unsigned char* now, unsigned char* next) {
+#pragma unroll
+        for (int unit = 0; unit < F::kUnits; unit++) {
+            Operands &mine = o[(unit + parity * F::kUnits) & 1], &then = o[(unit + 1 + parity * F::kUnits) & 1];
+            if (unit + 1 < F::kUnits) {
+                read(now, unit + 1, then);
+            } else {
+                loads_arrived();
+                load(step + 2, now);
+                ask(step + 3);
+                read(next, 0, then);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(mine);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    ask(begin);
+    load(begin, first_buffer);
+    ask(begin + 1);
+    load(begin + 1, second_buffer);
+    ask(begin + 2);
+    loads_arrived();
+    read(first_buffer, 0, o[0]);
+    int step = begin;
+    for (; step + 1 < end; step += 2) {
+        stage(step, 0, first_buffer, second_buffer);
+        stage(step + 1, 1, second_buffer, first_buffer);
+    }
+    if (step < end) stage(step, 0, first_buffer, second_buffer);
+    __syncthreads();
+}
+
+// The bits of a value by its first 8, the next 8 and the rest: a sum of three bf16 numbers that is exact (but for what lies below the smallest of
+// bf16's numbers).  Not finite: the first alone.
+__device__ __forceinline__ void split(float v, uint16_t (&part)[3]) {
+    const uint32_t u = __float_as_uint(v), top = u & 0xffff0000u;
+    part[0] = (uint16_t)(u >> 16);
+    if ((u & 0x7f800000u) == 0x7f800000u) {
+        part[0] = (u & 0x7fffffu) ? (uint16_t)(part[0] | 0x40u) : part[0];
+        part[1] = part[2] = 0;
+        return;
+    }
+    const float r = v - __uint_as_float(top);
+    const uint32_t mid = __float_as_uint(r) & 0xffff0000u;
+    part[1] = (uint16_t)(mid >> 16);
+    part[2] = (uint16_t)(__float_as_uint(r - __uint_as_float(mid)) >> 16);
+}
+
+// This workgroup's tile: bands of kBand tiles of rows, down each column of a band, in the order of the XCDs, so that the tiles that an XCD works on at a
+// time share their operands in its L2.
+constexpr int kBand = 8;
+struct Place {
+    int64_t i, j;
+    int which, split;
+    bool inside;
+};
+__device__ __forceinline__ Place place_of(int64_t tiles_i, int64_t tiles_j, int splits, int results) {
+    int64_t t = tile::xcd_sequence();
+    const int64_t tiles = tiles_i * tiles_j;
+    Place p;
+    p.inside = t < tiles * splits * results;
+    p.split = (int)(t / (tiles * results));
+    t -= p.split * (tiles * results);
+    p.which = (int)(t / tiles);
+    t -= p.which * tiles;
+    const int64_t band = t / (kBand * tiles_j), rows = tiles_i - band * kBand < kBand ? tiles_i - band * kBand : kBand;
+    t -= band * (kBand * tiles_j);
+    p.j = t / rows;
+    p.i = band * kBand + (t - p.j * rows);
+    return p;
+}
+
+}  // namespace product
+}  // namespace canvas

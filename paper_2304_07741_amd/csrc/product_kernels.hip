@@ -1,0 +1,259 @@
+// Products whose results are plain matrices, the ends of their sums, and copies of operands.
+#include "product_kernels.hpp"
+
+#include <algorithm>
+
+#include "device_util.hpp"
+#include "launch.hpp"
+#include "product_device.hpp"
+#include "tile_util.hpp"
+
+namespace canvas {
+namespace product {
+namespace {
+
+// What a kernel takes of a product.
+struct Task {
+    Factor a, b;
+    int64_t depth, tiles_i, tiles_j, ld;
+    int segments, results, splits;
+    void* out[2];
+    f32x4* parts;
+    bool first;
+};
+
+// Where element (r, c) of an image of rows of BN results is: columns are exchanged in pieces of 16 by bits of the row, so that
+// eight rows of a column, and the rows that the halves of a wave write at once, fall on different banks.
+template <int BN>
+__device__ __forceinline__ int place(int r, int c) {
+    return r * BN + (c ^ (((((r >> 3) & 3) << 4) ^ (((r >> 2) & 1) << 5)) & (BN - 1)));
+}
+template <int BN>
+__device__ __forceinline__ void to_image(float* img, const f32x16& acc, int r0, int c0) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int k = 0; k < 16; k++) img[place<BN>(r0 + (k >> 2) * 8 + (lane >> 5) * 4 + (k & 3), c0 + (lane & 31))] = acc[k];
+}
+
+// Results (i, j ..) from an image of ROWS x BN of them to memory, rounded where they are bf16.
+template <bool F32, int ROWS, int BN, int THREADS>
+__device__ __forceinline__ void emit(const Task& g, int which, int64_t i0, int64_t j0, const float* img) {
+    const bool whole = (g.ld & 7) == 0;
+#pragma unroll 2
+    for (int e = threadIdx.x; e < ROWS * (BN / 8); e += THREADS) {
+        const int r = e / (BN / 8), c = (e - r * (BN / 8)) * 8;
+        const int64_t i = i0 + r, j = j0 + c;
+        if (i >= g.a.count || j >= g.b.count) continue;
+        const f32x4* from = reinterpret_cast<const f32x4*>(img + place<BN>(r, c));  // (pieces of 16 columns stay together)
+        const f32x4 v[2] = {from[0], from[1]};
+        const int64_t at = i * g.ld + j;
+        if (F32) {
+            float* to = static_cast<float*>(g.out[which]) + at;
+            if (whole && j + 8 <= g.b.count) {
+                reinterpret_cast<f32x4*>(to)[0] = v[0];
+                reinterpret_cast<f32x4*>(to)[1] = v[1];
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; k++)
+                    if (j + k < g.b.count) to[k] = v[k >> 2][k & 3];
+            }
+        } else {
+            uint16_t* to = static_cast<uint16_t*>(g.out[which]) + at;
+            if (whole && j + 8 <= g.b.count) {
+                *reinterpret_cast<u32x4*>(to) = u32x4{tile::pack_bf16(v[0][0], v[0][1]), tile::pack_bf16(v[0][2], v[0][3]), tile::pack_bf16(v[1][0], v[1][1]), tile::pack_bf16(v[1][2], v[1][3])};
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; k++)
+                    if (j + k < g.b.count) to[k] = f32_to_bf16(v[k >> 2][k & 3]);
+            }
+        }
+    }
+}
+
+template <class F, Side SA, bool LIVE>
+__global__ __launch_bounds__(F::kThreads) void k_product(Task g) {
+    constexpr int TM = F::TM, TN = F::TN, BM = F::BM, BN = F::BN;
+    // (two arrays, not one: the compiler has to see that loads into the one do not concern reads of the other)
+    __shared__ __align__(16) unsigned char first_buffer[F::kStage], second_buffer[F::kStage];
+    const Place at = place_of(g.tiles_i, g.tiles_j, g.splits, g.results);
+    if (!at.inside) return;
+    const int64_t i0 = at.i * BM, j0 = at.j * BN;
+    const int per = (int)((g.depth + F::BK - 1) / F::BK), all = per * g.segments;
+    const int begin = (int)((int64_t)all * at.split / g.splits), end = (int)((int64_t)all * (at.split + 1) / g.splits);
+    f32x16 acc[TM][TN] = {};
+    accumulate<F, SA, kCols, false, LIVE>(g.a, g.b, at.which, i0, j0, g.depth, begin, end, per, g.segments, first_buffer, second_buffer, acc);
+    if (g.parts) {
+        f32x4* mine = g.parts + (((at.which * g.tiles_i + at.i) * g.tiles_j + at.j) * g.splits + at.split) * (BM * BN / 4) + threadIdx.x;
+#pragma unroll
+        for (int x = 0; x < TM; x++)
+#pragma unroll
+            for (int y = 0; y < TN; y++)
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    f32x4 v = {acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
+                    f32x4* to = mine + ((x * TN + y) * 4 + q) * F::kThreads;
+                    if (!g.first) v += *to;
+                    *to = v;
+                }
+        return;
+    }
+    constexpr int kRows = F::kStage / (BN * 4) / 32 * 32;  // of results that one buffer takes at once
+    float* img = reinterpret_cast<float*>(first_buffer);
+    const int wave = threadIdx.x >> 6, wi = wave / F::WJ * (TM * 32), wj = wave % F::WJ * (TN * 32);
+#pragma unroll 1
+    for (int r0 = 0; r0 < BM; r0 += kRows) {
+        if (r0) __syncthreads();
+#pragma unroll
+        for (int x = 0; x < TM; x++) {
+            const int r = wi + x * 32 - r0;
+            if (r < 0 || r >= kRows) continue;
+#pragma unroll
+            for (int y = 0; y < TN; y++) to_image<BN>(img, acc[x][y], r, wj + y * 32);
+        }
+        __syncthreads();
+        emit<F::PLANES == 3, kRows, BN, F::kThreads>(g, at.which, i0 + r0, j0, img);
+    }
+}
+
+// Adds the parts of 32 x 32 results, each of four waves every fourth part, and finishes them.
+template <class F>
+__global__ __launch_bounds__(256) void k_join(Task g) {
+    constexpr int kBlocks = F::BM / 32 * (F::BN / 32), kEach = F::BM * F::BN / 4;
+    __shared__ f32x4 sums[4][4][64];
+    __shared__ __align__(16) float img[32 * 32];
+    const int64_t number = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, tile = number / kBlocks, tiles = g.tiles_i * g.tiles_j;
+    if (tile >= tiles * g.results) return;
+    const int block = (int)(number - tile * kBlocks), bi = block / (F::BN / 32), bj = block - bi * (F::BN / 32);
+    const int which = (int)(tile / tiles);
+    const int64_t ti = (tile - which * tiles) / g.tiles_j, tj = tile - which * tiles - ti * g.tiles_j;
+    const int64_t i0 = ti * F::BM + bi * 32, j0 = tj * F::BN + bj * 32;
+    if (i0 >= g.a.count || j0 >= g.b.count) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // the block in the registers of the product's workgroup
+    const int owner = bi / F::TM * F::WJ + bj / F::TN, x = bi % F::TM, y = bj % F::TN;
+    const f32x4* from = g.parts + tile * g.splits * kEach + (x * F::TN + y) * 4 * F::kThreads + owner * 64 + lane;
+    f32x4 acc[4] = {};
+#pragma unroll 4
+    for (int part = wave; part < g.splits; part += 4)
+#pragma unroll
+        for (int q = 0; q < 4; q++) acc[q] += from[(int64_t)part * kEach + q * F::kThreads];
+#pragma unroll
+    for (int q = 0; q < 4; q++) sums[wave][q][lane] = acc[q];
+    __syncthreads();
+    const f32x4 v = (sums[0][wave][lane] + sums[1][wave][lane]) + (sums[2][wave][lane] + sums[3][wave][lane]);
+#pragma unroll
+    for (int e = 0; e < 4; e++) img[place<32>(wave * 8 + (lane >> 5) * 4 + e, lane & 31)] = v[e];
+    __syncthreads();
+    emit<F::PLANES == 3, 32, 32, 256>(g, which, i0, j0, img);
+}
+
+struct Copies {
+    Copy c[3];
+};
+// Eight elements of the copy per thread and turn; zeros behind the columns.
+template <bool F32>
+__global__ __launch_bounds__(256) void k_copy(Copies all) {
+    const Copy& c = all.c[blockIdx.y];
+    const int64_t wide = (c.cols + 7) / 8, n = c.rows * wide, plane = n * 8;
+    const bool whole = (c.cols & 7) == 0;
+    for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < n; k += (int64_t)gridDim.x * 256) {
+        const int64_t row = k / wide, col = (k - row * wide) * 8, from = row * c.cols + col;
+        if (F32) {
+            const float* x = static_cast<const float*>(c.from) + from;
+            float v[8];
+            if (whole) {
+                const f32x4 a = reinterpret_cast<const f32x4*>(x)[0], b = reinterpret_cast<const f32x4*>(x)[1];
+#pragma unroll
+                for (int e = 0; e < 4; e++) v[e] = a[e], v[4 + e] = b[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e++) v[e] = col + e < c.cols ? x[e] : 0.f;
+            }
+            u32x4 w[3];
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                uint16_t lo[3], hi[3];
+                split(v[2 * e], lo);
+                split(v[2 * e + 1], hi);
+#pragma unroll
+                for (int h = 0; h < 3; h++) w[h][e] = lo[h] | (uint32_t)hi[h] << 16;
+            }
+#pragma unroll
+            for (int h = 0; h < 3; h++) *reinterpret_cast<u32x4*>(c.to + h * plane + k * 8) = w[h];
+        } else {
+            const uint16_t* x = static_cast<const uint16_t*>(c.from) + from;
+            u32x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; e++) w[e] = (col + 2 * e < c.cols ? x[2 * e] : 0) | (uint32_t)(col + 2 * e + 1 < c.cols ? x[2 * e + 1] : 0) << 16;
+            *reinterpret_cast<u32x4*>(c.to + k * 8) = w;
+        }
+    }
+}
+
+template <class F, Side SA>
+void launch(const Product& p, const Task& t, hipStream_t stream) {
+    const dim3 grid = rows_of_workgroups(p.cut.tiles() * p.cut.splits * p.results, F::kThreads);
+    if (p.b.live)
+        CANVAS_LAUNCH((k_product<F, SA, true>), grid, dim3(F::kThreads), 0, stream, t);
+    else
+        CANVAS_LAUNCH((k_product<F, SA, false>), grid, dim3(F::kThreads), 0, stream, t);
+    if (p.parts && p.last) CANVAS_LAUNCH((k_join<F>), rows_of_workgroups(p.cut.tiles() * p.results * (F::BM / 32 * (F::BN / 32)), 256), dim3(256), 0, stream, t);
+}
+template <class F>
+void launch_form(const Product& p, const Task& t, hipStream_t stream) {
+    if (p.a_rows)
+        launch<F, kRows>(p, t, stream);
+    else
+        launch<F, kCols>(p, t, stream);
+}
+
+}  // namespace
+
+int64_t up8(int64_t n) { return (n + 7) & ~(int64_t)7; }
+
+Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, bool may_split) {
+    Cut c;
+    auto tiles = [&](int side) {
+        c.side = side;
+        c.tiles_i = (rows + side - 1) / side;
+        c.tiles_j = (cols + side - 1) / side;
+        return c.tiles() * results;
+    };
+    const int64_t steps = (depth + (f32 ? 15 : 63)) / (f32 ? 16 : 64);
+    if (!f32 && tiles(256) >= 180) return c;
+    const int64_t t = tiles(128);
+    if (may_split && t < 256) c.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / t, steps / (f32 ? 16 : 8)));
+    return c;
+}
+
+uint64_t parts_bytes(const Cut& c, int results, bool several) {
+    return c.splits > 1 || several ? 4ull * c.side * c.side * c.tiles() * c.splits * results : 0;
+}
+int launches_of(const Cut& c, bool several) { return 1 + (c.splits > 1 || several); }
+
+void multiply(const Product& p, hipStream_t stream) {
+    const Task t{p.a, p.b, p.depth, p.cut.tiles_i, p.cut.tiles_j, p.ld, p.segments, p.results, p.cut.splits, {p.out[0], p.out[1]}, reinterpret_cast<f32x4*>(p.parts), p.first};
+    if (p.f32)
+        launch_form<Triple>(p, t, stream);
+    else if (p.cut.side == 256)
+        launch_form<Large>(p, t, stream);
+    else
+        launch_form<Middle>(p, t, stream);
+}
+
+void copy(bool f32, const Copy* copies, int n, hipStream_t stream) {
+    Copies all{};
+    int64_t most = 0;
+    for (int i = 0; i < n; i++) {
+        all.c[i] = copies[i];
+        most = std::max(most, copies[i].rows * ((copies[i].cols + 7) / 8));
+    }
+    const dim3 grid((unsigned)std::min<int64_t>((most + 255) / 256, 4096), (unsigned)n);
+    if (f32)
+        CANVAS_LAUNCH(k_copy<true>, grid, dim3(256), 0, stream, all);
+    else
+        CANVAS_LAUNCH(k_copy<false>, grid, dim3(256), 0, stream, all);
+}
+
+}  // namespace product
+}  // namespace canvas

@@ -1,0 +1,59 @@
+// Products of bf16 matrices with fp32 sums, and of fp32 matrices as three bf16 planes each, for the operators whose hot part they are
+// (include/canvas_gated.h, canvas_head.h): plans, and the launches that those operators share.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace canvas {
+namespace product {
+
+// One operand.  In memory either rows of indexes with the summed index k along them, or rows of k with the indexes along them; leading
+// dimensions are multiples of 8, rows along k hold zeros from their end to the next multiple of 8.
+struct Factor {
+    const uint16_t* p[2] = {nullptr, nullptr};  // of the two halves of a sum over 2 * depth, or of the two results of a launch
+    int64_t ld = 0, plane = 0;                  // elements from row to row, and from one of three planes to the next
+    int64_t count = 0;                          // indexes
+    const uint8_t* live = nullptr;              // rows of k: 0 for those that count as zeros whatever they hold
+};
+
+// How results are cut: tiles of `side` x `side`, the sum over k in `splits` parts.
+struct Cut {
+    int side = 128, splits = 1;
+    int64_t tiles_i = 0, tiles_j = 0;
+    int64_t tiles() const { return tiles_i * tiles_j; }
+};
+
+// C[i][j] = sum_k A[i][k] B[j][k] for `results` pairs of matrices, or one sum over both of them.
+struct Product {
+    Factor a, b;
+    bool a_rows = false;   // A as rows of indexes (B, and A without it, as rows of k)
+    bool f32 = false;      // three planes, results in fp32; else one, results in bf16
+    int64_t depth = 0;     // of one of them
+    int segments = 1, results = 1;
+    void* out[2] = {nullptr, nullptr};
+    int64_t ld = 0;
+    Cut cut;
+    float* parts = nullptr;
+    // A sum that several launches add to, in order: each leaves its part in `parts`; the last one's is followed by the sum's end.
+    bool first = true, last = true;
+};
+
+int64_t up8(int64_t n);
+// `steps`: of the whole sum, each as deep as a tile takes at once.
+Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, bool may_split);
+uint64_t parts_bytes(const Cut& c, int results, bool several);
+// Launches of multiply(), the sum's end among them.
+int launches_of(const Cut& c, bool several);
+void multiply(const Product& p, hipStream_t stream);
+
+// A matrix of `rows` x `cols` elements as one bf16 plane (of bf16 elements) or three (of fp32 ones) with leading dimension up8(cols).
+struct Copy {
+    const void* from = nullptr;
+    uint16_t* to = nullptr;
+    int64_t rows = 0, cols = 0;
+};
+void copy(bool f32, const Copy* copies, int n, hipStream_t stream);
+
+}  // namespace product
+}  // namespace canvas

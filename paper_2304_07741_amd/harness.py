@@ -1,5 +1,7 @@
 """Device-memory plumbing around the C-ABI binding: allocates torch tensors, uploads a workload,
 calls forward/backward and downloads results.  No arithmetic of the method happens here."""
+import math
+
 import numpy as np
 import torch
 
@@ -329,6 +331,123 @@ class OrthoRunner(_PlanRunner):
             names += ["master", "weights"]
         B.canvas_ortho_step(self.handle, grad, momentum, m, mu, master, w, lr, decay, p, self.out["update"], self.ws)
         return {k: self.out[k] for k in names}
+
+
+class GatedRunner(_PlanRunner):
+    """A gated pair of FCs (include/canvas_gated.h): y = act(x w_gate^T) (x w_up^T); x [rows, features], weights [width, features].
+
+    forward() and backward() return the runner's own buffers, which the next call overwrites; backward() is of the last forward(), with the
+    same x and weights.
+    """
+
+    _destroy = staticmethod(B.canvas_gated_destroy)
+
+    def __init__(self, rows, features, width, dtype, act=B.CANVAS_GATED_SILU, flags=0, device="cuda:0"):
+        self._open(dtype, device)
+        self.shape, self.wshape = (int(rows), int(features)), (int(width), int(features))
+        self.handle = B.canvas_gated_compile(rows, features, width, self.cdtype, act, flags)
+        self.info = B.canvas_gated_query(self.handle)
+        self.ws = self._workspace(self.info.workspace_bytes)
+        self.out = {"y": self._empty((self.shape[0], self.wshape[0]))}
+        self.grads = {}
+        if not flags & B.CANVAS_OPT_INFERENCE:
+            self.grads = {"dx": self._empty(self.shape), "dw_gate": self._empty(self.wshape), "dw_up": self._empty(self.wshape)}
+
+    def _arguments(self, x, w_gate, w_up):
+        _check_tensor("x", x, self.shape, self.tdtype, self.device)
+        _check_tensor("w_gate", w_gate, self.wshape, self.tdtype, self.device)
+        _check_tensor("w_up", w_up, self.wshape, self.tdtype, self.device)
+
+    def forward(self, x, w_gate, w_up):
+        self._arguments(x, w_gate, w_up)
+        B.canvas_gated_forward(self.handle, x, w_gate, w_up, self.out["y"], self.ws)
+        return self.out
+
+    def backward(self, x, w_gate, w_up, dy):
+        self._arguments(x, w_gate, w_up)
+        _check_tensor("dy", dy, self.out["y"].shape, self.tdtype, self.device)
+        g = self.grads
+        B.canvas_gated_backward(self.handle, x, w_gate, w_up, dy, g.get("dx"), g.get("dw_gate"), g.get("dw_up"), self.ws)
+        return g
+
+
+class HeadRunner(_PlanRunner):
+    """Log probabilities of tokens with entropy from features and the head's weight (include/canvas_head.h), and the gradients of both.
+
+    x [rows, features], weight [classes, features]; mask: [classes] bytes or truth values, zero where a class is not allowed.
+    forward() and backward() return the runner's own buffers, which the next call overwrites; backward() is of the last forward(), with the
+    same x, weight, mask and temperature.
+    """
+
+    _destroy = staticmethod(B.canvas_head_destroy)
+
+    def __init__(self, rows, features, classes, dtype, flags=0, device="cuda:0"):
+        self._open(dtype, device)
+        self.rows, self.classes = int(rows), int(classes)
+        self.shape, self.wshape = (self.rows, int(features)), (self.classes, int(features))
+        self.handle = B.canvas_head_compile(rows, features, classes, self.cdtype, flags)
+        self.info = B.canvas_head_query(self.handle)
+        self.ws = self._workspace(self.info.workspace_bytes)
+        self.out = {"logprob": self._empty(self.rows, torch.float32), "entropy": self._empty(self.rows, torch.float32)}
+        self.grads = {} if flags & B.CANVAS_OPT_INFERENCE else {"dx": self._empty(self.shape), "dweight": self._empty(self.wshape)}
+
+    def _arguments(self, x, weight, tokens, mask):
+        _check_tensor("x", x, self.shape, self.tdtype, self.device)
+        _check_tensor("weight", weight, self.wshape, self.tdtype, self.device)
+        _check_tensor("tokens", tokens, (self.rows,), torch.int64, self.device)
+        if mask is not None:
+            _check_tensor("mask", mask, (self.classes,), torch.bool if mask.dtype is torch.bool else torch.uint8, self.device)
+
+    def forward(self, x, weight, tokens, mask=None, inv_temperature=1.0):
+        self._arguments(x, weight, tokens, mask)
+        B.canvas_head_forward(self.handle, x, weight, inv_temperature, mask, tokens, self.out["logprob"], self.out["entropy"], self.ws)
+        return self.out
+
+    def backward(self, x, weight, tokens, dlogprob=None, dentropy=None, mask=None, inv_temperature=1.0):
+        self._arguments(x, weight, tokens, mask)
+        for name, t in (("dlogprob", dlogprob), ("dentropy", dentropy)):
+            if t is not None:
+                _check_tensor(name, t, (self.rows,), torch.float32, self.device)
+        g = self.grads
+        B.canvas_head_backward(self.handle, x, weight, inv_temperature, mask, tokens, dlogprob, dentropy, g.get("dx"), g.get("dweight"), self.ws)
+        return g
+
+
+class ClipRunner(_PlanRunner):
+    """The norm over all gradients and their scaling to a largest norm (include/canvas_clip.h).
+
+    shapes, dtypes ("f32" or "bf16") and out_dtypes (the dtypes themselves if they are not given): one for each tensor.
+    """
+
+    _destroy = staticmethod(B.canvas_clip_destroy)
+
+    def __init__(self, shapes, dtypes, out_dtypes=None, device="cuda:0"):
+        kinds = {"f32": (torch.float32, B.CANVAS_F32), "bf16": (torch.bfloat16, B.CANVAS_BF16)}
+        out_dtypes = list(dtypes) if out_dtypes is None else list(out_dtypes)
+        self._open("f32", device)
+        self.shapes = [tuple(int(v) for v in s) for s in shapes]
+        self.dtypes, self.out_dtypes = [kinds[t][0] for t in dtypes], [kinds[t][0] for t in out_dtypes]
+        counts = [math.prod(s) for s in self.shapes]
+        self.handle = B.canvas_clip_compile(counts, [kinds[t][1] for t in dtypes], [kinds[t][1] for t in out_dtypes])
+        self.info = B.canvas_clip_query(self.handle)
+        self.ws = self._workspace(self.info.workspace_bytes)
+        self.norm, self.scale = self._empty((), torch.float32), self._empty((), torch.float32)
+        self.outs = None
+
+    def step(self, grads, max_norm, in_place=False):
+        """Returns norm, scale and grads, the scaled ones: buffers of the runner, or with in_place the arguments themselves."""
+        if len(grads) != len(self.shapes):
+            raise ValueError(f"grads: {len(self.shapes)} tensors are needed, got {len(grads)}")
+        for i, (t, s, d) in enumerate(zip(grads, self.shapes, self.dtypes)):
+            _check_tensor(f"grads[{i}]", t, s, d, self.device)
+        if in_place:
+            outs = list(grads)
+        else:
+            if self.outs is None:
+                self.outs = [self._empty(s, d) for s, d in zip(self.shapes, self.out_dtypes)]
+            outs = self.outs
+        B.canvas_clip_step(self.handle, grads, outs, max_norm, self.norm, self.scale, self.ws)
+        return {"norm": self.norm, "scale": self.scale, "grads": list(outs)}
 
 
 def run_case(case, flags=0, dy=None):
