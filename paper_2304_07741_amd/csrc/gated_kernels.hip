@@ -60,16 +60,19 @@ __global__ __launch_bounds__(F::kThreads) void k_forward(FwdArgs a) {
     constexpr int TM = F::TM, TN = F::TN, kCols = F::BN / 2;
     constexpr bool kF32 = F::PLANES == 3;
     static_assert(TN == 2, "a wave holds one block of each matrix");
-    __shared__ __align__(16) unsigned char first_buffer[F::kStage], second_buffer[F::kStage];
+    PRODUCT_BUFFERS(F, buffers);
     const product::Place at = product::place_of(a.tiles_i, a.tiles_j, 1, 1);
     if (!at.inside) return;
     const int64_t i0 = at.i * F::BM, j0 = at.j * kCols;
     const int steps = (int)((a.features + F::BK - 1) / F::BK);
     f32x16 acc[TM][TN] = {};
-    product::accumulate<F, product::kRows, product::kRows, true, false>(a.x, a.w, 0, i0, j0, a.features, 0, steps, steps, 1, first_buffer, second_buffer, acc);
+    product::accumulate<F, product::kRows, product::kRows, true>(a.x, a.w, 0, i0, j0, a.features, 0, steps, steps, 1, buffers, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / F::WJ * (TM * 32), wj = wave % F::WJ * 32;
     const int64_t j = j0 + wj + (lane & 31);
-    uint16_t* img = reinterpret_cast<uint16_t*>(first_buffer);  // bf16: the tile of y
+    // bf16: the tile of y, the rows of each row of waves in a buffer
+    constexpr int kEach = TM * 32;
+    static_assert(kF32 || (kEach * kCols * 2 <= F::kStage && F::WI <= F::BUFFERS), "the tile of y in the buffers");
+    uint16_t* img = reinterpret_cast<uint16_t*>(buffers.of(wave / F::WJ));
     if (a.pre && j < a.width) {
 #pragma unroll
         for (int x = 0; x < TM; x++)
@@ -92,11 +95,10 @@ __global__ __launch_bounds__(F::kThreads) void k_forward(FwdArgs a) {
             if (kF32) {
                 if (i0 + r < a.rows && j < a.width) static_cast<float*>(a.y)[(i0 + r) * a.width + j] = y;
             } else {
-                img[r * kCols + wj + (lane & 31)] = f32_to_bf16(y);
+                img[(r - wi) * kCols + wj + (lane & 31)] = f32_to_bf16(y);
             }
         }
     if (kF32) return;
-    static_assert(kF32 || F::BM * kCols * 2 <= F::kStage, "the tile of y in one buffer");
     __syncthreads();
     const bool whole = (a.width & 7) == 0;
 #pragma unroll 2
@@ -104,7 +106,7 @@ __global__ __launch_bounds__(F::kThreads) void k_forward(FwdArgs a) {
         const int r = e / (kCols / 8), c = (e - r * (kCols / 8)) * 8;
         const int64_t i = i0 + r, col = j0 + c;
         if (i >= a.rows || col >= a.width) continue;
-        const u32x4 v = *reinterpret_cast<const u32x4*>(img + r * kCols + c);
+        const u32x4 v = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(buffers.of(r / kEach)) + (r % kEach) * kCols + c);
         uint16_t* to = static_cast<uint16_t*>(a.y) + i * a.width + col;
         if (whole) {
             *reinterpret_cast<u32x4*>(to) = v;
@@ -255,8 +257,8 @@ Operands operands_of(const Shape& s, const Plan& p, const void* x, const void* w
     const uint16_t* at[3];
     for (int i = 0; i < 3; i++) at[i] = p.copies ? reinterpret_cast<const uint16_t*>(ws + p.copy_at[i]) : static_cast<const uint16_t*>(given[i]);
     const int64_t ld = product::up8(s.features);
-    o.x = Factor{{at[0], at[0]}, ld, s.rows * ld, s.rows, nullptr};
-    o.w = Factor{{at[1], at[2]}, ld, s.width * ld, s.width, nullptr};
+    o.x = Factor{{at[0], at[0]}, ld, s.rows * ld, s.rows};
+    o.w = Factor{{at[1], at[2]}, ld, s.width * ld, s.width};
     return o;
 }
 void make_copies(const Shape& s, const Plan& p, const void* x, const void* w_gate, const void* w_up, char* ws, hipStream_t stream) {
@@ -332,7 +334,7 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
     float* parts = reinterpret_cast<float*>(a.ws + p.parts_at);
     product::Product d;
     d.f32 = s.f32;
-    d.a = Factor{{of[0], of[1]}, ld, plane, s.rows, nullptr};
+    d.a = Factor{{of[0], of[1]}, ld, plane, s.rows};
     d.a_rows = true;
     d.b = o.w;
     d.b.count = s.features;

@@ -94,13 +94,13 @@ __device__ __forceinline__ Sums sums_of(const float (&z)[N], float scale) {
 template <class F>
 __global__ __launch_bounds__(F::kThreads) void k_logits(FwdArgs a) {
     constexpr int TM = F::TM, TN = F::TN;
-    __shared__ __align__(16) unsigned char first_buffer[F::kStage], second_buffer[F::kStage];
+    PRODUCT_BUFFERS(F, buffers);
     const product::Place at = product::place_of(a.tiles_i, a.tiles_j, 1, 1);
     if (!at.inside) return;
     const int64_t i0 = at.i * F::BM, j0 = at.j * F::BN;
     const int steps = (int)((a.features + F::BK - 1) / F::BK);
     f32x16 acc[TM][TN] = {};
-    product::accumulate<F, product::kRows, product::kRows, false, false>(a.w, a.x, 0, i0, j0, a.features, 0, steps, steps, 1, first_buffer, second_buffer, acc);
+    product::accumulate<F, product::kRows, product::kRows, false>(a.w, a.x, 0, i0, j0, a.features, 0, steps, steps, 1, buffers, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t c0 = i0 + wave / F::WJ * (TM * 32) + (lane >> 5) * 4, t0 = j0 + wave % F::WJ * (TN * 32) + (lane & 31);
     const float scale = scale_of(a.it);
@@ -249,7 +249,7 @@ struct SlopeArgs {
     const float *dlogprob, *dentropy;
     const Row* row;
     Slope* slope;
-    uint8_t* live;
+    uint8_t* live;  // whether the row's gradient is not all zeros
 };
 __global__ __launch_bounds__(256) void k_slopes(SlopeArgs a) {
     const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -278,13 +278,13 @@ struct GradArgs {
 template <class F>
 __global__ __launch_bounds__(F::kThreads) void k_grads(GradArgs a) {
     constexpr int TM = F::TM, TN = F::TN, P = F::PLANES, kHalf = F::BN / 2;
-    __shared__ __align__(16) unsigned char first_buffer[F::kStage], second_buffer[F::kStage];
+    PRODUCT_BUFFERS(F, buffers);
     const product::Place at = product::place_of(a.tiles_i, a.tiles_j, 1, 1);
     if (!at.inside) return;
     const int64_t i0 = at.i * F::BM, j0 = at.j * F::BN;
     const int steps = (int)((a.features + F::BK - 1) / F::BK);
     f32x16 acc[TM][TN] = {};
-    product::accumulate<F, product::kRows, product::kRows, false, false>(a.w, a.x, 0, i0, j0, a.features, 0, steps, steps, 1, first_buffer, second_buffer, acc);
+    product::accumulate<F, product::kRows, product::kRows, false>(a.w, a.x, 0, i0, j0, a.features, 0, steps, steps, 1, buffers, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / F::WJ * (TM * 32) + (lane >> 5) * 4, wj = wave % F::WJ * (TN * 32) + (lane & 31);
     const float scale = scale_of(a.it);
 #pragma unroll
@@ -331,14 +331,14 @@ __global__ __launch_bounds__(F::kThreads) void k_grads(GradArgs a) {
                     }
             }
     }
-    // Plane by plane through LDS, rows of x by classes: the rows of the first half of the tile in one buffer, the others in the other.  16-byte pieces
+    // Plane by plane through LDS, rows of x by classes: half of the rows in a buffer.  16-byte pieces
     // of row r are exchanged by the bits of r, so that the lanes of a wave, a row each, write to different banks.
     static_assert(kHalf * F::BM * 2 <= F::kStage, "half a tile in a buffer");
     constexpr int kPieces = F::BM / 8;
 #pragma unroll
     for (int h = 0; h < P; h++) {
         if (h) __syncthreads();
-        unsigned char* img = wave % F::WJ * (TN * 32) < kHalf ? first_buffer : second_buffer;
+        unsigned char* img = buffers.of(wave % F::WJ * (TN * 32) / kHalf);
 #pragma unroll
         for (int y = 0; y < TN; y++) {
             const int r = (wj + y * 32) & (kHalf - 1);
@@ -367,8 +367,7 @@ __global__ __launch_bounds__(F::kThreads) void k_grads(GradArgs a) {
             const int r = e / kPieces, c = e % kPieces;
             const int64_t t = j0 + r, col = i0 + c * 8;
             if (t >= a.rows || col >= a.ld) continue;
-            const unsigned char* from = r < kHalf ? first_buffer : second_buffer;
-            const u32x4 v = *reinterpret_cast<const u32x4*>(from + (r & (kHalf - 1)) * (F::BM * 2) + (((c ^ r) & (kPieces - 1)) << 4));
+            const u32x4 v = *reinterpret_cast<const u32x4*>(buffers.of(r / kHalf) + (r & (kHalf - 1)) * (F::BM * 2) + (((c ^ r) & (kPieces - 1)) << 4));
             *reinterpret_cast<u32x4*>(a.to + h * a.plane + t * a.ld + col) = v;
         }
     }
@@ -396,22 +395,7 @@ void launch_grads(const GradArgs& a, hipStream_t stream) {
     CANVAS_LAUNCH(k_grads<F>, rows_of_workgroups(a.tiles_i * a.tiles_j, F::kThreads), dim3(F::kThreads), 0, stream, a);
 }
 
-struct Operands {
-    Factor x, w;
-};
-Operands operands_of(const Shape& s, const Plan& p, const void* x, const void* w, char* ws) {
-    const int64_t ld = product::up8(s.features);
-    const uint16_t *ax = static_cast<const uint16_t*>(x), *aw = static_cast<const uint16_t*>(w);
-    if (p.copies) {
-        ax = reinterpret_cast<const uint16_t*>(ws + p.copy_at[0]);
-        aw = reinterpret_cast<const uint16_t*>(ws + p.copy_at[1]);
-    }
-    return Operands{Factor{{ax, ax}, ld, s.rows * ld, s.rows, nullptr}, Factor{{aw, aw}, ld, s.classes * ld, s.classes, nullptr}};
-}
-void make_copies(const Shape& s, const Plan& p, const void* x, const void* w, char* ws, hipStream_t stream) {
-    const product::Copy c[2] = {{x, reinterpret_cast<uint16_t*>(ws + p.copy_at[0]), s.rows, s.features}, {w, reinterpret_cast<uint16_t*>(ws + p.copy_at[1]), s.classes, s.features}};
-    product::copy(s.f32, c, 2, stream);
-}
+Factor factor_of(const uint16_t* at, int64_t rows, int64_t ld) { return Factor{{at, at}, ld, rows * ld, rows}; }
 
 }  // namespace
 
@@ -432,10 +416,8 @@ Plan plan_of(const Shape& s) {
     };
     p.sums_at = take(sizeof(Sums) * (uint64_t)s.rows * p.segments);
     p.token_at = take(4ull * s.rows);
-    if (p.copies) {
-        p.copy_at[0] = take(2ull * planes * s.rows * ld);
-        p.copy_at[1] = take(2ull * planes * s.classes * ld);
-    }
+    if (p.copies || !s.inference) p.copy_at[0] = take(2ull * planes * s.rows * ld);
+    if (p.copies) p.copy_at[1] = take(2ull * planes * s.classes * ld);
     if (!s.inference) {
         p.rows_at = take(sizeof(Row) * (uint64_t)s.rows);
         p.slope_at = take(sizeof(Slope) * (uint64_t)s.rows);
@@ -447,7 +429,8 @@ Plan plan_of(const Shape& s) {
         p.piece = product::cut_of(s.f32, p.length, s.rows, s.features, 1, false);
         p.dx = product::cut_of(s.f32, s.rows, s.features, p.length, 1, true);
         p.dw = product::cut_of(s.f32, p.length, s.features, s.rows, 1, true);
-        p.launches_bwd = (p.copies && p.few) + 1 + p.pieces * (2 + product::launches_of(p.dw, false)) + (product::launches_of(p.dx, p.pieces > 1) - 1);
+        if (!p.copies) p.copy_at[1] = take(2ull * p.length * ld);
+        p.launches_bwd = 2 + p.pieces * (2 + product::launches_of(p.dw, false)) + (product::launches_of(p.dx, p.pieces > 1) - 1);
         p.most_tiles = std::max({p.most_tiles, p.piece.tiles(), p.dx.tiles() * p.dx.splits, p.dw.tiles() * p.dw.splits});
         p.grad_at = take(2ull * planes * s.rows * product::up8(p.length));
         p.parts_dx_at = take(product::parts_bytes(p.dx, 1, p.pieces > 1));
@@ -467,9 +450,16 @@ void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
         else
             launch_few<uint16_t>(f, stream);
     } else {
-        if (p.copies) make_copies(s, p, a.x, a.weight, a.ws, stream);
-        const Operands o = operands_of(s, p, a.x, a.weight, a.ws);
-        const FwdArgs f{o.w, o.x, s.rows, s.features, s.classes, p.logits.tiles_i, p.logits.tiles_j, a.it, a.mask, a.tokens, sums, token};
+        const uint16_t *x = static_cast<const uint16_t*>(a.x), *w = static_cast<const uint16_t*>(a.weight);
+        if (p.copies) {
+            uint16_t *cx = reinterpret_cast<uint16_t*>(a.ws + p.copy_at[0]), *cw = reinterpret_cast<uint16_t*>(a.ws + p.copy_at[1]);
+            const product::Copy c[2] = {{x, cx, s.rows, s.features, nullptr}, {w, cw, s.classes, s.features, a.mask}};
+            product::copy(s.f32, c, 2, stream);
+            x = cx;
+            w = cw;
+        }
+        const int64_t ld = product::up8(s.features);
+        const FwdArgs f{factor_of(w, s.classes, ld), factor_of(x, s.rows, ld), s.rows, s.features, s.classes, p.logits.tiles_i, p.logits.tiles_j, a.it, a.mask, a.tokens, sums, token};
         if (s.f32)
             launch_logits<product::Triple>(f, stream);
         else if (p.logits.side == 256)
@@ -484,35 +474,45 @@ void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
 }
 
 void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
-    if (p.copies && p.few) make_copies(s, p, a.x, a.weight, a.ws, stream);
-    const Operands o = operands_of(s, p, a.x, a.weight, a.ws);
     Slope* slope = reinterpret_cast<Slope*>(a.ws + p.slope_at);
     uint8_t* live = reinterpret_cast<uint8_t*>(a.ws + p.live_at);
     uint16_t* grads = reinterpret_cast<uint16_t*>(a.ws + p.grad_at);
     const SlopeArgs l{s.rows, s.classes, a.it, a.tokens, a.dlogprob, a.dentropy, reinterpret_cast<const Row*>(a.ws + p.rows_at), slope, live};
     CANVAS_LAUNCH(k_slopes, dim3((unsigned)((s.rows + 255) / 256)), dim3(256), 0, stream, l);
+    // x with zeros for the rows without a gradient, and W (where it is not a copy that forward has left, piece by piece) with zeros for masked classes:
+    // products by the zeros of their gradients are zero then, whatever they hold
+    uint16_t *cx = reinterpret_cast<uint16_t*>(a.ws + p.copy_at[0]), *cw = reinterpret_cast<uint16_t*>(a.ws + p.copy_at[1]);
+    const bool whole = p.copies && p.few;
+    const product::Copy c[2] = {{a.x, cx, s.rows, s.features, live}, {a.weight, cw, s.classes, s.features, a.mask}};
+    product::copy(s.f32, c, whole ? 2 : 1, stream);
+    const int64_t lx = product::up8(s.features);
+    const Factor x = factor_of(cx, s.rows, lx), all = factor_of(p.copies ? cw : static_cast<const uint16_t*>(a.weight), s.classes, lx);
     const int64_t ld = product::up8(p.length), plane = s.rows * ld;
     for (int n = 0; n < p.pieces; n++) {
         const int64_t first = n * p.length, length = std::min(p.length, s.classes - first);
-        Factor w = o.w;
-        w.p[0] = w.p[1] = o.w.p[0] + first * o.w.ld;
+        Factor w = all;
+        w.p[0] = w.p[1] = all.p[0] + first * lx;
         w.count = length;
         const uint8_t* mask = a.mask ? a.mask + first : nullptr;
         const int64_t side = p.piece.side;
-        const GradArgs g{w, o.x, s.rows, s.features, length, (length + side - 1) / side, p.piece.tiles_j, first, a.it, mask, slope, grads, ld, plane};
+        const GradArgs g{w, x, s.rows, s.features, length, (length + side - 1) / side, p.piece.tiles_j, first, a.it, mask, slope, grads, ld, plane};
         if (s.f32)
             launch_grads<product::Triple>(g, stream);
         else if (side == 256)
             launch_grads<product::Large>(g, stream);
         else
             launch_grads<product::Middle>(g, stream);
+        if (mask && !p.copies) {
+            const product::Copy m{w.p[0], cw, length, s.features, mask};
+            product::copy(false, &m, 1, stream);
+            w.p[0] = w.p[1] = cw;
+        }
         product::Product d;
         d.f32 = s.f32;
-        d.a = Factor{{grads, grads}, ld, plane, s.rows, nullptr};
+        d.a = Factor{{grads, grads}, ld, plane, s.rows};
         d.a_rows = true;
         d.b = w;
         d.b.count = s.features;
-        d.b.live = mask;
         d.depth = length;
         d.out[0] = a.dx;
         d.ld = s.features;
@@ -523,9 +523,8 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
         product::multiply(d, stream);
         d.a.count = length;
         d.a_rows = false;
-        d.b = o.x;
+        d.b = x;
         d.b.count = s.features;
-        d.b.live = live;
         d.depth = s.rows;
         d.out[0] = static_cast<char*>(a.dweight) + first * s.features * (s.f32 ? 4 : 2);
         d.cut = p.dw;

@@ -1,12 +1,15 @@
 // The inner part of a product: a tile of results in the registers of a workgroup, both operands through LDS.
 //
-// Operands are loaded straight into LDS, a stage (BK summands of all rows of the tile) ahead of their use, into two arrays in turn.
+// Operands are loaded straight into LDS, BUFFERS - 1 stages (of BK summands of all rows of the tile) ahead of their use.
 // Rows along k: 16-byte pieces of eight summands; piece c of row r lies at place c ^ (r / rows per line of all banks), so that the
 // pieces that 16 lanes read together fall on different banks.  Rows of k: the matrix units want eight summands of one index in a lane, so the
 // rows are read by the transposing load, a block of 4 summands x 16 indexes by 16 lanes; the 32-byte units of row k lie at unit ^
-// {0, 2, 5, 7}[k % 4], for the same reason.  What lies behind the end of the sum is not loaded: an offset outside the buffer gives zeros.
+// {0, 2, 5, 7}[k % 4], for the same reason.  What lies behind the end of the sum is not loaded: an offset outside the buffer gives zeros, which
+// stages behind the last one load too, so that the number of loads in flight is always the same.
 #pragma once
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "launch.hpp"
 #include "product_kernels.hpp"
@@ -24,16 +27,27 @@ using tile::u32x4;
 enum Side { kRows, kCols };
 
 // Tiles of BM x BN by WI x WJ waves, BK summands of PLANES planes at a time.
-template <int BM_, int BN_, int WI_, int WJ_, int PLANES_, int BK_>
+template <int BM_, int BN_, int WI_, int WJ_, int PLANES_, int BK_, int BUFFERS_>
 struct Form {
-    static constexpr int BM = BM_, BN = BN_, WI = WI_, WJ = WJ_, PLANES = PLANES_, BK = BK_;
+    static constexpr int BM = BM_, BN = BN_, WI = WI_, WJ = WJ_, PLANES = PLANES_, BK = BK_, BUFFERS = BUFFERS_;
     static constexpr int kThreads = 64 * WI * WJ, TM = BM / WI / 32, TN = BN / WJ / 32, kUnits = BK / 16;
     static constexpr int kBytesA = BM * BK * 2, kBytesB = BN * BK * 2;  // of a plane of a stage
-    static constexpr int kStage = PLANES * (kBytesA + kBytesB);
+    static constexpr int kStage = PLANES * (kBytesA + kBytesB), kLoads = kStage / 16 / kThreads;
 };
-using Large = Form<256, 256, 2, 4, 1, 64>;
-using Middle = Form<128, 128, 2, 2, 1, 64>;
-using Triple = Form<128, 128, 2, 2, 3, 16>;
+using Large = Form<256, 256, 2, 4, 1, 64, 2>;
+using Middle = Form<128, 128, 2, 2, 1, 64, 2>;
+using Triple = Form<128, 128, 2, 2, 3, 16, 3>;
+
+// One array per stage in flight, not one for all: the compiler has to see that loads into the one do not concern reads of another.
+template <class F>
+struct Buffers {
+    unsigned char* at[3];
+    // (an array that is indexed by a variable would be kept in memory)
+    __device__ __forceinline__ unsigned char* of(int n) const { return n == 0 ? at[0] : n == 1 ? at[1] : at[2]; }
+};
+#define PRODUCT_BUFFERS(F, name)                                                                                                                  \
+    __shared__ __align__(16) unsigned char name##_0[F::kStage], name##_1[F::kStage], name##_2[F::BUFFERS > 2 ? F::kStage : 16]; \
+    const ::canvas::product::Buffers<F> name{{name##_0, name##_1, name##_2}}
 
 constexpr uint32_t kOutside = 0x80000000u;  // an offset behind the end of every buffer
 __device__ __forceinline__ tile::rsrc_t buffer_from(const void* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffffff, 0x00020000); }
@@ -41,24 +55,29 @@ __device__ __forceinline__ tile::rsrc_t buffer_from(const void* p) { return __bu
 __device__ __forceinline__ void load_to_lds(tile::rsrc_t from, unsigned char* to, uint32_t offset) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, offset, 0, 0, 0);
 }
-// A barrier behind which everybody's loads to LDS have arrived.
+// A barrier behind which everybody has read what it asked LDS for, and all but each thread's last N loads to LDS have arrived.
+template <int N>
 __device__ __forceinline__ void loads_arrived() {
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-    __syncthreads();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x70);  // vmcnt(N), lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 }
 
 template <int ROW>
 __device__ __forceinline__ int piece_of(int r, int c) { return c ^ ((r / (256 / ROW)) & (ROW / 16 - 1)); }
 __device__ __forceinline__ int unit_of(int k, int unit) { return unit ^ (((k & 1) << 1) | ((k >> 1) & 1) * 5); }
 
-// What a thread loads of one operand.  PAIRS: indexes are taken 32 by 32 from the two matrices in turn.  LIVE: rows of k may be left out.
-template <class F, int BX, Side SIDE, bool PAIRS, bool LIVE>
+// What a thread loads of one operand.  PAIRS: indexes are taken 32 by 32 from the two matrices in turn.
+template <class F, int BX, Side SIDE, bool PAIRS>
 struct Loader {
     static constexpr int kRow = SIDE == kRows ? F::BK * 2 : BX * 2, kPieces = kRow / 16;
     static constexpr int kPlane = BX * F::BK * 2, kTimes = kPlane / 16 / F::kThreads;
     static_assert(kPlane % (16 * F::kThreads) == 0 && 256 % (SIDE == kRows ? kRow : 1) == 0, "whole pieces for every thread");
     uint32_t offset[kTimes];
-    uint8_t alive[kTimes];
+    int behind;  // summands of a stage before this thread's, in its first piece; kApart more in each of the others
+    static constexpr int kApart = SIDE == kRows ? 0 : F::kThreads / kPieces;
+    static_assert(SIDE == kCols || kTimes == 1 || F::kThreads / kPieces % (256 / kRow * kPieces) == 0, "a thread's pieces are at the same place of their rows");
     const uint16_t *at, *other;  // what the next load begins with; in the second matrix of a pair
 
     static __device__ __forceinline__ int row_of(int tid, int q) { return (tid + q * F::kThreads) / kPieces; }
@@ -72,6 +91,7 @@ struct Loader {
     }
     __device__ __forceinline__ void begin(const Factor& f, int64_t first) {
         const int left = (int)(f.count - first < BX ? f.count - first : BX);  // indexes of the tile
+        behind = SIDE == kRows ? piece_of<SIDE == kRows ? kRow : 256>(row_of(threadIdx.x, 0), place_of(threadIdx.x, 0)) * 8 : row_of(threadIdx.x, 0);
 #pragma unroll
         for (int q = 0; q < kTimes; q++) {
             const int r = row_of(threadIdx.x, q), c = place_of(threadIdx.x, q);
@@ -83,41 +103,20 @@ struct Loader {
                 const int piece = unit_of(r, c >> 1) * 2 + (c & 1);
                 offset[q] = piece * 8 < left ? (uint32_t)r * (uint32_t)f.ld * 2u + piece * 16 : kOutside;
             }
-            alive[q] = 1;
-        }
-    }
-    // Asks which of the rows from k on are alive.
-    __device__ __forceinline__ void ask(const Factor& f, int64_t k, int64_t depth) {
-        if (!LIVE) return;
-#pragma unroll
-        for (int q = 0; q < kTimes; q++) {
-            const int64_t row = k + row_of(threadIdx.x, q);
-            alive[q] = f.live && row < depth ? f.live[row] : 1;
         }
     }
     // The next BK summands, of which there are `left`.
     __device__ __forceinline__ void load(const Factor& f, int64_t left, unsigned char* to) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         to += wave * 1024;
-        auto put = [&](int h, int q, uint32_t o) {
-            const bool second = PAIRS && ((((wave * 64 + q * F::kThreads) / kPieces) >> 5) & 1);
-            load_to_lds(buffer_from((second ? other : at) + h * f.plane), to + h * kPlane + q * (F::kThreads * 16), LIVE && !alive[q] ? kOutside : o);
-        };
-        if (left >= F::BK) {
+        const int some = left < F::BK ? (int)left : F::BK;
 #pragma unroll
-            for (int h = 0; h < F::PLANES; h++)
-#pragma unroll
-                for (int q = 0; q < kTimes; q++) put(h, q, offset[q]);
-        } else {
-            int tid = threadIdx.x;
-            asm volatile("" : "+v"(tid));  // (what follows is computed here, not kept in registers through the loop)
+        for (int h = 0; h < F::PLANES; h++)
 #pragma unroll
             for (int q = 0; q < kTimes; q++) {
-                const int r = row_of(tid, q), behind = SIDE == kRows ? piece_of<SIDE == kRows ? kRow : 256>(r, place_of(tid, q)) * 8 : r;
-#pragma unroll
-                for (int h = 0; h < F::PLANES; h++) put(h, q, behind >= (int)left ? kOutside : offset[q]);
+                const bool second = PAIRS && ((((wave * 64 + q * F::kThreads) / kPieces) >> 5) & 1);
+                load_to_lds(buffer_from((second ? other : at) + h * f.plane), to + h * kPlane + q * (F::kThreads * 16), behind < some - q * kApart ? offset[q] : kOutside);
             }
-        }
         const int64_t step = SIDE == kRows ? F::BK : F::BK * f.ld;
         at += step;
         if (PAIRS) other += step;
@@ -157,15 +156,31 @@ struct Reader {
     }
 };
 
+template <int N, int END, class F>
+__device__ __forceinline__ void turn(F&& f) {
+    if constexpr (N < END) {
+        f(std::integral_constant<int, N>());
+        turn<N + 1, END>(f);
+    }
+}
+template <int N, int END, class F>
+__device__ __forceinline__ void rest(int left, F&& f) {  // N .. left - 1
+    if constexpr (N + 1 < END) {
+        if (N >= left) return;
+        f(std::integral_constant<int, N>());
+        rest<N + 1, END>(left, f);
+    }
+}
+
 // The sum over steps begin .. end (BK summands each, `per` of them in each of `segments` halves) of a tile from (i0, j0) on.  acc[x][y]: 32 x 32
 // results from (wave's row + 32 x, wave's column + 32 y) on; register k of a lane is row (k / 4) * 8 + (lane / 32) * 4 + k % 4, column lane % 32.
-template <class F, Side SA, Side SB, bool PAIRS, bool LIVE>
+template <class F, Side SA, Side SB, bool PAIRS>
 __device__ __forceinline__ void accumulate(const Factor& a, const Factor& b, int which, int64_t i0, int64_t j0, int64_t depth, int begin, int end, int per,
-                                           int segments, unsigned char* first_buffer, unsigned char* second_buffer, f32x16 (&acc)[F::TM][F::TN]) {
-    constexpr int TM = F::TM, TN = F::TN, P = F::PLANES;
+                                           int segments, const Buffers<F>& buffers, f32x16 (&acc)[F::TM][F::TN]) {
+    constexpr int TM = F::TM, TN = F::TN, P = F::PLANES, N = F::BUFFERS;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    Loader<F, F::BM, SA, false, false> la;
-    Loader<F, F::BN, SB, PAIRS, LIVE> lb;
+    Loader<F, F::BM, SA, false> la;
+    Loader<F, F::BN, SB, PAIRS> lb;
     la.begin(a, i0);
     lb.begin(b, j0);
     Reader<F, F::BM, SA, TM> ra;
@@ -176,13 +191,10 @@ __device__ __forceinline__ void accumulate(const Factor& a, const Factor& b, int
     int64_t done = (int64_t)(begin - half * per) * F::BK;  // summands of this half that were asked for
     la.seek(a, from, i0, done);
     lb.seek(b, from, j0, done);
-    auto ask = [&](int step) {
-        if (LIVE) lb.ask(b, (int64_t)step * F::BK, depth);  // (one segment)
-    };
     auto load = [&](int step, unsigned char* to) {
-        if (step >= end) return;
-        la.load(a, depth - done, to);
-        lb.load(b, depth - done, to + P * F::kBytesA);
+        const int64_t left = step < end ? depth - done : 0;
+        la.load(a, left, to);
+        lb.load(b, left, to + P * F::kBytesA);
         done += F::BK;
         if (segments == 2 && step + 1 == per) {
             done = 0;
@@ -213,40 +225,47 @@ __device__ __forceinline__ void accumulate(const Factor& a, const Factor& b, int
                 for (int y = 0; y < TN; y++)
                     acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(o.a[x][P == 1 ? 0 : kOfA[h]], o.b[y][P == 1 ? 0 : kOfB[h]], acc[x][y], 0, 0, 0);
     };
+    constexpr int kPerProduct = 2;  // reads of LDS
     Operands o[2];
-    // One stage, `now` its buffer: each unit's products run while the next one's operands are read; before the last unit
-    // everybody has read this buffer and the next stage has arrived, so the one behind that is asked for.
-    auto stage = [&](int step, int parity, unsigned char* now, unsigned char* next) {
+    // Stage n of a turn: each unit's products run while the next one's operands are read; before the last unit everybody has
+    // read this buffer and the next stage has arrived, so this buffer takes the stage BUFFERS behind.  (The loads are
+    // spread over the products of that unit: asked for together they keep the wave, and the matrix units, waiting for their queue.)
+    auto stage = [&](int step, auto number) {
+        constexpr int n = decltype(number)::value, first = n * F::kUnits;
+        unsigned char *now = buffers.at[n % N], *next = buffers.at[(n + 1) % N];
 #pragma unroll
         for (int unit = 0; unit < F::kUnits; unit++) {
-            Operands &mine = o[(unit + parity * F::kUnits) & 1], &then = o[(unit + 1 + parity * F::kUnits) & 1];
-            if (unit + 1 < F::kUnits) {
-                read(now, unit + 1, then);
-            } else {
-                loads_arrived();
-                load(step + 2, now);
-                ask(step + 3);
-                read(next, 0, then);
-            }
+            Operands &mine = o[(first + unit) & 1], &then = o[(first + unit + 1) & 1];
+            constexpr int kProducts = TM * TN * (P == 1 ? 1 : 6), kReads = P * (TM * (SA == kRows ? 1 : 2) + TN * (SB == kRows ? 1 : 2));
+            const bool last = unit + 1 == F::kUnits;
+            if (last) loads_arrived<(N - 2) * F::kLoads>();
             __builtin_amdgcn_sched_barrier(0);
+            if (last) {
+                read(next, 0, then);
+                load(step + n + N, now);
+            } else {
+                read(now, unit + 1, then);
+            }
             multiply(mine);
+            // products all the time, what is asked for between them
+#pragma unroll
+            for (int k = 0; k < kProducts; k++) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                if (k * kPerProduct < kReads) __builtin_amdgcn_sched_group_barrier(0x100, kPerProduct, 0);
+                if (last && k < F::kLoads) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    ask(begin);
-    load(begin, first_buffer);
-    ask(begin + 1);
-    load(begin + 1, second_buffer);
-    ask(begin + 2);
-    loads_arrived();
-    read(first_buffer, 0, o[0]);
+#pragma unroll
+    for (int n = 0; n < N; n++) load(begin + n, buffers.at[n]);
+    loads_arrived<(N - 1) * F::kLoads>();
+    read(buffers.at[0], 0, o[0]);
+    constexpr int kTurn = (F::kUnits & 1) && (N & 1) ? 2 * N : N;  // stages until buffers and registers are the first ones again
     int step = begin;
-    for (; step + 1 < end; step += 2) {
-        stage(step, 0, first_buffer, second_buffer);
-        stage(step + 1, 1, second_buffer, first_buffer);
-    }
-    if (step < end) stage(step, 0, first_buffer, second_buffer);
-    __syncthreads();
+    for (; step + kTurn <= end; step += kTurn) turn<0, kTurn>([&](auto n) { stage(step, n); });
+    rest<0, kTurn>(end - step, [&](auto n) { stage(step, n); });
+    loads_arrived<0>();
 }
 
 // The bits of a value by its first 8, the next 8 and the rest: a sum of three bf16 numbers that is exact (but for what lies below the smallest of

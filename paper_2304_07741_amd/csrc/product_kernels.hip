@@ -70,18 +70,17 @@ __device__ __forceinline__ void emit(const Task& g, int which, int64_t i0, int64
     }
 }
 
-template <class F, Side SA, bool LIVE>
+template <class F, Side SA>
 __global__ __launch_bounds__(F::kThreads) void k_product(Task g) {
     constexpr int TM = F::TM, TN = F::TN, BM = F::BM, BN = F::BN;
-    // (two arrays, not one: the compiler has to see that loads into the one do not concern reads of the other)
-    __shared__ __align__(16) unsigned char first_buffer[F::kStage], second_buffer[F::kStage];
+    PRODUCT_BUFFERS(F, buffers);
     const Place at = place_of(g.tiles_i, g.tiles_j, g.splits, g.results);
     if (!at.inside) return;
     const int64_t i0 = at.i * BM, j0 = at.j * BN;
     const int per = (int)((g.depth + F::BK - 1) / F::BK), all = per * g.segments;
     const int begin = (int)((int64_t)all * at.split / g.splits), end = (int)((int64_t)all * (at.split + 1) / g.splits);
     f32x16 acc[TM][TN] = {};
-    accumulate<F, SA, kCols, false, LIVE>(g.a, g.b, at.which, i0, j0, g.depth, begin, end, per, g.segments, first_buffer, second_buffer, acc);
+    accumulate<F, SA, kCols, false>(g.a, g.b, at.which, i0, j0, g.depth, begin, end, per, g.segments, buffers, acc);
     if (g.parts) {
         f32x4* mine = g.parts + (((at.which * g.tiles_i + at.i) * g.tiles_j + at.j) * g.splits + at.split) * (BM * BN / 4) + threadIdx.x;
 #pragma unroll
@@ -97,21 +96,23 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Task g) {
                 }
         return;
     }
-    constexpr int kRows = F::kStage / (BN * 4) / 32 * 32;  // of results that one buffer takes at once
-    float* img = reinterpret_cast<float*>(first_buffer);
+    // through LDS, kRows rows of results to a buffer
+    constexpr int kRows = F::kStage / (BN * 4) / 32 * 32, kRound = 2 * kRows;
+    static_assert(BM % kRound == 0, "rows of results in the buffers");
     const int wave = threadIdx.x >> 6, wi = wave / F::WJ * (TM * 32), wj = wave % F::WJ * (TN * 32);
 #pragma unroll 1
-    for (int r0 = 0; r0 < BM; r0 += kRows) {
+    for (int r0 = 0; r0 < BM; r0 += kRound) {
         if (r0) __syncthreads();
 #pragma unroll
         for (int x = 0; x < TM; x++) {
             const int r = wi + x * 32 - r0;
-            if (r < 0 || r >= kRows) continue;
+            if (r < 0 || r >= kRound) continue;
 #pragma unroll
-            for (int y = 0; y < TN; y++) to_image<BN>(img, acc[x][y], r, wj + y * 32);
+            for (int y = 0; y < TN; y++) to_image<BN>(reinterpret_cast<float*>(buffers.of(r / kRows)), acc[x][y], r % kRows, wj + y * 32);
         }
         __syncthreads();
-        emit<F::PLANES == 3, kRows, BN, F::kThreads>(g, at.which, i0 + r0, j0, img);
+#pragma unroll
+        for (int n = 0; n < 2; n++) emit<F::PLANES == 3, kRows, BN, F::kThreads>(g, at.which, i0 + r0 + n * kRows, j0, reinterpret_cast<const float*>(buffers.at[n]));
     }
 }
 
@@ -158,6 +159,11 @@ __global__ __launch_bounds__(256) void k_copy(Copies all) {
     const bool whole = (c.cols & 7) == 0;
     for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < n; k += (int64_t)gridDim.x * 256) {
         const int64_t row = k / wide, col = (k - row * wide) * 8, from = row * c.cols + col;
+        if (c.live && !c.live[row]) {
+#pragma unroll
+            for (int h = 0; h < (F32 ? 3 : 1); h++) *reinterpret_cast<u32x4*>(c.to + h * plane + k * 8) = u32x4{};
+            continue;
+        }
         if (F32) {
             const float* x = static_cast<const float*>(c.from) + from;
             float v[8];
@@ -183,8 +189,12 @@ __global__ __launch_bounds__(256) void k_copy(Copies all) {
         } else {
             const uint16_t* x = static_cast<const uint16_t*>(c.from) + from;
             u32x4 w;
+            if (whole) {
+                w = *reinterpret_cast<const u32x4*>(x);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 4; e++) w[e] = (col + 2 * e < c.cols ? x[2 * e] : 0) | (uint32_t)(col + 2 * e + 1 < c.cols ? x[2 * e + 1] : 0) << 16;
+                for (int e = 0; e < 4; e++) w[e] = (col + 2 * e < c.cols ? x[2 * e] : 0) | (uint32_t)(col + 2 * e + 1 < c.cols ? x[2 * e + 1] : 0) << 16;
+            }
             *reinterpret_cast<u32x4*>(c.to + k * 8) = w;
         }
     }
@@ -193,10 +203,7 @@ __global__ __launch_bounds__(256) void k_copy(Copies all) {
 template <class F, Side SA>
 void launch(const Product& p, const Task& t, hipStream_t stream) {
     const dim3 grid = rows_of_workgroups(p.cut.tiles() * p.cut.splits * p.results, F::kThreads);
-    if (p.b.live)
-        CANVAS_LAUNCH((k_product<F, SA, true>), grid, dim3(F::kThreads), 0, stream, t);
-    else
-        CANVAS_LAUNCH((k_product<F, SA, false>), grid, dim3(F::kThreads), 0, stream, t);
+    CANVAS_LAUNCH((k_product<F, SA>), grid, dim3(F::kThreads), 0, stream, t);
     if (p.parts && p.last) CANVAS_LAUNCH((k_join<F>), rows_of_workgroups(p.cut.tiles() * p.results * (F::BM / 32 * (F::BN / 32)), 256), dim3(256), 0, stream, t);
 }
 template <class F>
@@ -220,9 +227,15 @@ Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, boo
         return c.tiles() * results;
     };
     const int64_t steps = (depth + (f32 ? 15 : 63)) / (f32 ? 16 : 64);
-    if (!f32 && tiles(256) >= 180) return c;
+    if (!f32) {
+        // a tile of 256 for more than half of the compute units, or parts of them
+        const int64_t t = tiles(256);
+        if (t >= 180) return c;
+        c.splits = may_split ? (int)std::max<int64_t>(1, std::min<int64_t>(256 / t, steps / 16)) : 1;
+        if (t * c.splits >= 180) return c;
+    }
     const int64_t t = tiles(128);
-    if (may_split && t < 256) c.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / t, steps / (f32 ? 16 : 8)));
+    c.splits = may_split && t < 256 ? (int)std::max<int64_t>(1, std::min<int64_t>(512 / t, steps / (f32 ? 16 : 8))) : 1;
     return c;
 }
 

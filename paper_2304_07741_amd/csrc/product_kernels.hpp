@@ -14,7 +14,6 @@ struct Factor {
     const uint16_t* p[2] = {nullptr, nullptr};  // of the two halves of a sum over 2 * depth, or of the two results of a launch
     int64_t ld = 0, plane = 0;                  // elements from row to row, and from one of three planes to the next
     int64_t count = 0;                          // indexes
-    const uint8_t* live = nullptr;              // rows of k: 0 for those that count as zeros whatever they hold
 };
 
 // How results are cut: tiles of `side` x `side`, the sum over k in `splits` parts.
@@ -48,10 +47,12 @@ int launches_of(const Cut& c, bool several);
 void multiply(const Product& p, hipStream_t stream);
 
 // A matrix of `rows` x `cols` elements as one bf16 plane (of bf16 elements) or three (of fp32 ones) with leading dimension up8(cols).
+// `live`: bytes by row, 0 for rows that are zeros in the copy whatever they hold.
 struct Copy {
     const void* from = nullptr;
     uint16_t* to = nullptr;
     int64_t rows = 0, cols = 0;
+    const uint8_t* live = nullptr;
 };
 void copy(bool f32, const Copy* copies, int n, hipStream_t stream);
 
