@@ -32,7 +32,8 @@ struct Form {
     static constexpr int BM = BM_, BN = BN_, WI = WI_, WJ = WJ_, PLANES = PLANES_, BK = BK_, BUFFERS = BUFFERS_;
     static constexpr int kThreads = 64 * WI * WJ, TM = BM / WI / 32, TN = BN / WJ / 32, kUnits = BK / 16;
     static constexpr int kBytesA = BM * BK * 2, kBytesB = BN * BK * 2;  // of a plane of a stage
-    static constexpr int kStage = PLANES * (kBytesA + kBytesB), kLoads = kStage / 16 / kThreads;
+    static constexpr int kStage = PLANES * (kBytesA + kBytesB), kLoadsA = PLANES * kBytesA / 16 / kThreads, kLoadsB = PLANES * kBytesB / 16 / kThreads, kLoads = kLoadsA + kLoadsB;  // of a thread
+    static constexpr bool kApart = kUnits > 1;  // the two operands' loads go to different units of products
 };
 using Large = Form<256, 256, 2, 4, 1, 64, 2>;
 using Middle = Form<128, 128, 2, 2, 1, 64, 2>;
@@ -41,13 +42,13 @@ using Triple = Form<128, 128, 2, 2, 3, 16, 3>;
 // One array per stage in flight, not one for all: the compiler has to see that loads into the one do not concern reads of another.
 template <class F>
 struct Buffers {
-    unsigned char* at[3];
+    unsigned char* at[4];
     // (an array that is indexed by a variable would be kept in memory)
-    __device__ __forceinline__ unsigned char* of(int n) const { return n == 0 ? at[0] : n == 1 ? at[1] : at[2]; }
+    __device__ __forceinline__ unsigned char* of(int n) const { return n == 0 ? at[0] : n == 1 ? at[1] : n == 2 ? at[2] : at[3]; }
 };
 #define PRODUCT_BUFFERS(F, name)                                                                                                                  \
-    __shared__ __align__(16) unsigned char name##_0[F::kStage], name##_1[F::kStage], name##_2[F::BUFFERS > 2 ? F::kStage : 16]; \
-    const ::canvas::product::Buffers<F> name{{name##_0, name##_1, name##_2}}
+    __shared__ __align__(16) unsigned char name##_0[F::kStage], name##_1[F::kStage], name##_2[F::BUFFERS > 2 ? F::kStage : 16], name##_3[F::BUFFERS > 3 ? F::kStage : 16]; \
+    const ::canvas::product::Buffers<F> name{{name##_0, name##_1, name##_2, name##_3}}
 
 constexpr uint32_t kOutside = 0x80000000u;  // an offset behind the end of every buffer
 __device__ __forceinline__ tile::rsrc_t buffer_from(const void* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffffff, 0x00020000); }
@@ -188,19 +189,17 @@ __device__ __forceinline__ void accumulate(const Factor& a, const Factor& b, int
     ra.begin(wave / F::WJ * (TM * 32));
     rb.begin(wave % F::WJ * (TN * 32));
     const int half = segments == 2 && begin >= per, from = segments == 2 ? half : which;
-    int64_t done = (int64_t)(begin - half * per) * F::BK;  // summands of this half that were asked for
-    la.seek(a, from, i0, done);
-    lb.seek(b, from, j0, done);
-    auto load = [&](int step, unsigned char* to) {
-        const int64_t left = step < end ? depth - done : 0;
-        la.load(a, left, to);
-        lb.load(b, left, to + P * F::kBytesA);
-        done += F::BK;
-        if (segments == 2 && step + 1 == per) {
-            done = 0;
-            la.seek(a, 1, i0, 0);
-            lb.seek(b, 1, j0, 0);
-        }
+    la.seek(a, from, i0, (int64_t)(begin - half * per) * F::BK);
+    lb.seek(b, from, j0, (int64_t)(begin - half * per) * F::BK);
+    // what is left of the sum, or of its half, from a step on
+    auto left = [&](int step) { return step < end ? depth - (int64_t)(segments == 2 && step >= per ? step - per : step) * F::BK : 0; };
+    auto load_a = [&](int step, unsigned char* to) {
+        la.load(a, left(step), to);
+        if (segments == 2 && step + 1 == per) la.seek(a, 1, i0, 0);
+    };
+    auto load_b = [&](int step, unsigned char* to) {
+        lb.load(b, left(step), to + P * F::kBytesA);
+        if (segments == 2 && step + 1 == per) lb.seek(b, 1, j0, 0);
     };
     struct Operands {
         bf16x8_t a[TM][P], b[TN][P];
@@ -228,11 +227,12 @@ __device__ __forceinline__ void accumulate(const Factor& a, const Factor& b, int
     constexpr int kPerProduct = 2;  // reads of LDS
     Operands o[2];
     // Stage n of a turn: each unit's products run while the next one's operands are read; before the last unit everybody has
-    // read this buffer and the next stage has arrived, so this buffer takes the stage BUFFERS behind.  (The loads are
-    // spread over the products of that unit: asked for together they keep the wave, and the matrix units, waiting for their queue.)
+    // read this buffer and the next stage has arrived, so this buffer takes the stage BUFFERS behind: its first
+    // operand in that unit, its second one in the next.  (Loads are spread over the products: asked for together they keep the wave, and the matrix
+    // units, waiting for their queue.)
     auto stage = [&](int step, auto number) {
         constexpr int n = decltype(number)::value, first = n * F::kUnits;
-        unsigned char *now = buffers.at[n % N], *next = buffers.at[(n + 1) % N];
+        unsigned char *now = buffers.at[n % N], *next = buffers.at[(n + 1) % N], *before = buffers.at[(n + N - 1) % N];
 #pragma unroll
         for (int unit = 0; unit < F::kUnits; unit++) {
             Operands &mine = o[(first + unit) & 1], &then = o[(first + unit + 1) & 1];
@@ -240,26 +240,27 @@ __device__ __forceinline__ void accumulate(const Factor& a, const Factor& b, int
             const bool last = unit + 1 == F::kUnits;
             if (last) loads_arrived<(N - 2) * F::kLoads>();
             __builtin_amdgcn_sched_barrier(0);
-            if (last) {
-                read(next, 0, then);
-                load(step + n + N, now);
-            } else {
-                read(now, unit + 1, then);
-            }
+            read(last ? next : now, last ? 0 : unit + 1, then);
+            if (unit == 0 && F::kApart) load_b(step + n + N - 1, before);
+            if (last) load_a(step + n + N, now);
+            if (last && !F::kApart) load_b(step + n + N, now);
             multiply(mine);
             // products all the time, what is asked for between them
 #pragma unroll
             for (int k = 0; k < kProducts; k++) {
                 __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
                 if (k * kPerProduct < kReads) __builtin_amdgcn_sched_group_barrier(0x100, kPerProduct, 0);
-                if (last && k < F::kLoads) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
+                if (k < (last ? F::kLoadsA + (F::kApart ? 0 : F::kLoadsB) : unit == 0 ? F::kLoadsB : 0)) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
 #pragma unroll
-    for (int n = 0; n < N; n++) load(begin + n, buffers.at[n]);
-    loads_arrived<(N - 1) * F::kLoads>();
+    for (int n = 0; n < N; n++) {
+        load_a(begin + n, buffers.at[n]);
+        if (n + 1 < N || !F::kApart) load_b(begin + n, buffers.at[n]);
+    }
+    loads_arrived<(N - 1) * F::kLoads - (F::kApart ? F::kLoadsB : 0)>();
     read(buffers.at[0], 0, o[0]);
     constexpr int kTurn = (F::kUnits & 1) && (N & 1) ? 2 * N : N;  // stages until buffers and registers are the first ones again
     int step = begin;
