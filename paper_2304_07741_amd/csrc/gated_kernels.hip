@@ -6,6 +6,7 @@
 #include "gated_kernels.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/canvas_gated.h"
 #include "device_util.hpp"
@@ -26,9 +27,9 @@ using product::Form;
 using tile::u32x4;
 
 // act(g); with SLOPE its derivative too.  e^-|g| serves both signs; NaN stays (comparisons, not maxima).
-template <bool SLOPE>
-__device__ __forceinline__ float act_of(int act, float g, float& slope) {
-    if (act == CANVAS_GATED_GELU) {
+template <int ACT, bool SLOPE>
+__device__ __forceinline__ float act_of(float g, float& slope) {
+    if (ACT == CANVAS_GATED_GELU) {
         const float cdf = 0.5f * erfcf(g * -0.70710678118654752f);
         if (SLOPE) {
             const float half = -0.5f * g * g;
@@ -38,7 +39,7 @@ __device__ __forceinline__ float act_of(int act, float g, float& slope) {
     }
     const float m = -fabsf(g), e = exp_finite(m < -300.f ? -300.f : m), r = __builtin_amdgcn_rcpf(1.f + e);
     const float sig = g < 0.f ? e * r : r, other = g < 0.f ? r : e * r;  // other = 1 - sig without a difference
-    if (act == CANVAS_GATED_SIGMOID) {
+    if (ACT == CANVAS_GATED_SIGMOID) {
         if (SLOPE) slope = sig * other;
         return sig;
     }
@@ -52,10 +53,9 @@ struct FwdArgs {
     void* y;
     float* pre;  // g, and u `plane` elements behind it
     int64_t plane;
-    int act;
 };
 
-template <class F>
+template <class F, int ACT>
 __global__ __launch_bounds__(F::kThreads) void k_forward(FwdArgs a) {
     constexpr int TM = F::TM, TN = F::TN, kCols = F::BN / 2;
     constexpr bool kF32 = F::PLANES == 3;
@@ -73,48 +73,53 @@ __global__ __launch_bounds__(F::kThreads) void k_forward(FwdArgs a) {
     constexpr int kEach = TM * 32;
     static_assert(kF32 || (kEach * kCols * 2 <= F::kStage && F::WI <= F::BUFFERS), "the tile of y in the buffers");
     uint16_t* img = reinterpret_cast<uint16_t*>(buffers.of(wave / F::WJ));
-    if (a.pre && j < a.width) {
-#pragma unroll
-        for (int x = 0; x < TM; x++)
-#pragma unroll
-            for (int k = 0; k < 16; k++) {
-                const int64_t i = i0 + wi + x * 32 + (k >> 2) * 8 + (lane >> 5) * 4 + (k & 3);
-                if (i >= a.rows) continue;
-                float* to = a.pre + i * a.ld + j;
-                to[0] = acc[x][0][k];
-                to[a.plane] = acc[x][1][k];
-            }
-    }
 #pragma unroll
     for (int x = 0; x < TM; x++)
 #pragma unroll
         for (int k = 0; k < 16; k++) {
             const int r = wi + x * 32 + (k >> 2) * 8 + (lane >> 5) * 4 + (k & 3);
             float unused;
-            const float y = act_of<false>(a.act, acc[x][0][k], unused) * acc[x][1][k];
+            const float y = act_of<ACT, false>(acc[x][0][k], unused) * acc[x][1][k];
             if (kF32) {
                 if (i0 + r < a.rows && j < a.width) static_cast<float*>(a.y)[(i0 + r) * a.width + j] = y;
             } else {
                 img[(r - wi) * kCols + wj + (lane & 31)] = f32_to_bf16(y);
             }
         }
-    if (kF32) return;
-    __syncthreads();
-    const bool whole = (a.width & 7) == 0;
+    // (g and u last: nothing waits for their way to memory)
+    if (!kF32) {
+        tile::lds_barrier();
+        const bool whole = (a.width & 7) == 0;
 #pragma unroll 2
-    for (int e = threadIdx.x; e < F::BM * (kCols / 8); e += F::kThreads) {
-        const int r = e / (kCols / 8), c = (e - r * (kCols / 8)) * 8;
-        const int64_t i = i0 + r, col = j0 + c;
-        if (i >= a.rows || col >= a.width) continue;
-        const u32x4 v = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(buffers.of(r / kEach)) + (r % kEach) * kCols + c);
-        uint16_t* to = static_cast<uint16_t*>(a.y) + i * a.width + col;
-        if (whole) {
-            *reinterpret_cast<u32x4*>(to) = v;
-        } else {
+        for (int e = threadIdx.x; e < F::BM * (kCols / 8); e += F::kThreads) {
+            const int r = e / (kCols / 8), c = (e - r * (kCols / 8)) * 8;
+            const int64_t i = i0 + r, col = j0 + c;
+            if (i >= a.rows || col >= a.width) continue;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(buffers.of(r / kEach)) + (r % kEach) * kCols + c);
+            uint16_t* to = static_cast<uint16_t*>(a.y) + i * a.width + col;
+            if (whole) {
+                *reinterpret_cast<u32x4*>(to) = v;
+            } else {
 #pragma unroll
-            for (int k = 0; k < 8; k++)
-                if (col + k < a.width) to[k] = (uint16_t)(v[k >> 1] >> ((k & 1) * 16));
+                for (int k = 0; k < 8; k++)
+                    if (col + k < a.width) to[k] = (uint16_t)(v[k >> 1] >> ((k & 1) * 16));
+            }
         }
+    }
+    if (a.pre) {
+        // (what lies behind the rows or the columns is outside the buffers, whose stores are dropped)
+        const int64_t bytes = (a.rows - i0) * a.ld * 4;
+        const int size = bytes < 0x7fffffff ? (int)bytes : 0x7fffffff;
+        const tile::rsrc_t to_g = tile::make_rsrc(a.pre + i0 * a.ld, size), to_u = tile::make_rsrc(a.pre + a.plane + i0 * a.ld, size);
+        const uint32_t first = j < a.width ? (uint32_t)j * 4u + (uint32_t)(wi + (lane >> 5) * 4) * (uint32_t)a.ld * 4u : product::kOutside, ld = (uint32_t)a.ld * 4u;
+#pragma unroll
+        for (int x = 0; x < TM; x++)
+#pragma unroll
+            for (int k = 0; k < 16; k++) {
+                const int o = (int)(first + (uint32_t)(x * 32 + (k >> 2) * 8 + (k & 3)) * ld);
+                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(acc[x][0][k]), to_g, o, 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(acc[x][1][k]), to_u, o, 0, 0);
+            }
     }
 }
 
@@ -124,9 +129,8 @@ struct FewArgs {
     void* y;
     float* pre;
     int64_t plane;
-    int act;
 };
-template <class T, int NT>
+template <class T, int NT, int ACT>
 __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
     __shared__ f32x4 shared[2 * NT * few::kWaves * 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -146,7 +150,7 @@ __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
     for (int e = 0; e < 4; e++) {
         if (f + e >= a.width) break;
         float unused;
-        const float y = act_of<false>(a.act, sums[0][e], unused) * sums[1][e];
+        const float y = act_of<ACT, false>(sums[0][e], unused) * sums[1][e];
         const int64_t to = t * a.width + f + e;
         if (sizeof(T) == 4)
             static_cast<float*>(a.y)[to] = y;
@@ -165,10 +169,9 @@ struct GradArgs {
     int64_t plane, rows, width, ld;
     const void* dy;
     uint16_t* to;  // dg, then du: planes of `plane` elements each
-    int act;
 };
 // dg and du, eight elements per thread and turn; zeros behind the columns.
-template <bool F32>
+template <bool F32, int ACT>
 __global__ __launch_bounds__(256) void k_grads(GradArgs a) {
     constexpr int P = F32 ? 3 : 1;
     const int64_t wide = a.ld / 8, n = a.rows * wide;
@@ -203,7 +206,7 @@ __global__ __launch_bounds__(256) void k_grads(GradArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; e++) {
             float slope;
-            const float act = act_of<true>(a.act, g[e >> 2][e & 3], slope);
+            const float act = act_of<ACT, true>(g[e >> 2][e & 3], slope);
             const bool in = col + e < a.width;  // (behind the columns nothing was written)
             du[e] = in ? dy[e] * act : 0.f;
             dg[e] = in ? dy[e] * u[e >> 2][e & 3] * slope : 0.f;
@@ -234,17 +237,31 @@ __global__ __launch_bounds__(256) void k_grads(GradArgs a) {
 constexpr int kFewRows = 32;
 uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
 
-template <class T>
-void launch_few(const FewArgs& a, hipStream_t stream) {
-    const dim3 grid((unsigned)((a.width + 15) / 16));
-    if (a.rows <= 16)
-        CANVAS_LAUNCH((k_few<T, 1>), grid, dim3(few::kThreads), 0, stream, a);
+// f with the activation as a constant
+template <class F>
+void with_act(int act, F f) {
+    if (act == CANVAS_GATED_SIGMOID)
+        f(std::integral_constant<int, CANVAS_GATED_SIGMOID>());
+    else if (act == CANVAS_GATED_SILU)
+        f(std::integral_constant<int, CANVAS_GATED_SILU>());
     else
-        CANVAS_LAUNCH((k_few<T, 2>), grid, dim3(few::kThreads), 0, stream, a);
+        f(std::integral_constant<int, CANVAS_GATED_GELU>());
+}
+template <class T>
+void launch_few(int act, const FewArgs& a, hipStream_t stream) {
+    const dim3 grid((unsigned)((a.width + 15) / 16));
+    with_act(act, [&](auto kind) {
+        if (a.rows <= 16)
+            CANVAS_LAUNCH((k_few<T, 1, decltype(kind)::value>), grid, dim3(few::kThreads), 0, stream, a);
+        else
+            CANVAS_LAUNCH((k_few<T, 2, decltype(kind)::value>), grid, dim3(few::kThreads), 0, stream, a);
+    });
 }
 template <class F>
-void launch_forward(const FwdArgs& a, hipStream_t stream) {
-    CANVAS_LAUNCH(k_forward<F>, rows_of_workgroups(a.tiles_i * a.tiles_j, F::kThreads), dim3(F::kThreads), 0, stream, a);
+void launch_forward(int act, const FwdArgs& a, hipStream_t stream) {
+    with_act(act, [&](auto kind) {
+        CANVAS_LAUNCH((k_forward<F, decltype(kind)::value>), rows_of_workgroups(a.tiles_i * a.tiles_j, F::kThreads), dim3(F::kThreads), 0, stream, a);
+    });
 }
 
 // The three tensors that products read, as they read them.
@@ -305,30 +322,32 @@ void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
     const int64_t ld = product::up8(s.width);
     float* pre = s.inference ? nullptr : reinterpret_cast<float*>(a.ws + p.pre_at);
     if (p.few) {
-        const FewArgs f{a.x, a.w_gate, a.w_up, s.rows, s.features, s.width, ld, a.y, pre, s.rows * ld, s.act};
-        return s.f32 ? launch_few<float>(f, stream) : launch_few<uint16_t>(f, stream);
+        const FewArgs f{a.x, a.w_gate, a.w_up, s.rows, s.features, s.width, ld, a.y, pre, s.rows * ld};
+        return s.f32 ? launch_few<float>(s.act, f, stream) : launch_few<uint16_t>(s.act, f, stream);
     }
     if (p.copies) make_copies(s, p, a.x, a.w_gate, a.w_up, a.ws, stream);
     const Operands o = operands_of(s, p, a.x, a.w_gate, a.w_up, a.ws);
-    const FwdArgs f{o.x, o.w, s.rows, s.features, s.width, p.forward.tiles_i, p.forward.tiles_j, ld, a.y, pre, s.rows * ld, s.act};
+    const FwdArgs f{o.x, o.w, s.rows, s.features, s.width, p.forward.tiles_i, p.forward.tiles_j, ld, a.y, pre, s.rows * ld};
     if (s.f32)
-        launch_forward<product::Triple>(f, stream);
+        launch_forward<product::Triple>(s.act, f, stream);
     else if (p.forward.side == 256)
-        launch_forward<product::Large>(f, stream);
+        launch_forward<product::Large>(s.act, f, stream);
     else
-        launch_forward<product::Middle>(f, stream);
+        launch_forward<product::Middle>(s.act, f, stream);
 }
 
 void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
     const int64_t ld = product::up8(s.width), plane = s.rows * ld, planes = s.f32 ? 3 : 1;
     if (p.copies && p.few) make_copies(s, p, a.x, a.w_gate, a.w_up, a.ws, stream);
     uint16_t* grads = reinterpret_cast<uint16_t*>(a.ws + p.grad_at);
-    const GradArgs g{reinterpret_cast<const float*>(a.ws + p.pre_at), plane, s.rows, s.width, ld, a.dy, grads, s.act};
+    const GradArgs g{reinterpret_cast<const float*>(a.ws + p.pre_at), plane, s.rows, s.width, ld, a.dy, grads};
     const dim3 grid((unsigned)std::min<int64_t>((plane / 8 + 255) / 256, 8192));
-    if (s.f32)
-        CANVAS_LAUNCH(k_grads<true>, grid, dim3(256), 0, stream, g);
-    else
-        CANVAS_LAUNCH(k_grads<false>, grid, dim3(256), 0, stream, g);
+    with_act(s.act, [&](auto kind) {
+        if (s.f32)
+            CANVAS_LAUNCH((k_grads<true, decltype(kind)::value>), grid, dim3(256), 0, stream, g);
+        else
+            CANVAS_LAUNCH((k_grads<false, decltype(kind)::value>), grid, dim3(256), 0, stream, g);
+    });
     const Operands o = operands_of(s, p, a.x, a.w_gate, a.w_up, a.ws);
     const uint16_t* of[2] = {grads, grads + planes * plane};
     float* parts = reinterpret_cast<float*>(a.ws + p.parts_at);

@@ -49,12 +49,12 @@ __device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float scale) 
 template <int O>
 __device__ __forceinline__ float from_lane(float v) { return __shfl_xor(v, O); }
 
-// Whether the mask allows each of four classes from c on (a multiple of four), and whether they are classes at all.
+// Bytes that are not zero for those of four classes from c on (a multiple of four) that are classes and that the mask allows.
 __device__ __forceinline__ uint32_t allowed4(const uint8_t* mask, int64_t c, int64_t classes) {
+    if (c + 4 <= classes) return mask ? *reinterpret_cast<const uint32_t*>(mask + c) : 0x01010101u;
     uint32_t w = 0;
-#pragma unroll
-    for (int e = 0; e < 4; e++)
-        if (c + e < classes && (!mask || mask[c + e])) w |= 1u << e;
+#pragma unroll 1
+    for (int e = 3; e >= 0; e--) w = w << 8 | (c + e < classes ? mask ? mask[c + e] : 1u : 0u);
     return w;
 }
 
@@ -99,11 +99,20 @@ __global__ __launch_bounds__(F::kThreads) void k_logits(FwdArgs a) {
     if (!at.inside) return;
     const int64_t i0 = at.i * F::BM, j0 = at.j * F::BN;
     const int steps = (int)((a.features + F::BK - 1) / F::BK);
-    f32x16 acc[TM][TN] = {};
-    product::accumulate<F, product::kRows, product::kRows, false>(a.w, a.x, 0, i0, j0, a.features, 0, steps, steps, 1, buffers, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t c0 = i0 + wave / F::WJ * (TM * 32) + (lane >> 5) * 4, t0 = j0 + wave % F::WJ * (TN * 32) + (lane & 31);
     const float scale = scale_of(a.it);
+    int token[TN];  // the row's token among this lane's classes, -1 if it is not
+#pragma unroll
+    for (int y = 0; y < TN; y++) {
+        token[y] = -1;
+        if (a.token && t0 + y * 32 < a.rows) {
+            const int64_t c = a.tokens[t0 + y * 32] - c0;
+            if (c >= 0 && c < TM * 32 && !(c & 4)) token[y] = (int)c;
+        }
+    }
+    f32x16 acc[TM][TN] = {};
+    product::accumulate<F, product::kRows, product::kRows, false>(a.w, a.x, 0, i0, j0, a.features, 0, steps, steps, 1, buffers, acc);
     if (a.mask || i0 + F::BM > a.classes) {
 #pragma unroll
         for (int x = 0; x < TM; x++)
@@ -112,7 +121,7 @@ __global__ __launch_bounds__(F::kThreads) void k_logits(FwdArgs a) {
                 const uint32_t in = allowed4(a.mask, c0 + x * 32 + q * 8, a.classes);
 #pragma unroll
                 for (int e = 0; e < 4; e++)
-                    if (!(in >> e & 1)) {
+                    if (!(in >> (8 * e) & 0xffu)) {
 #pragma unroll
                         for (int y = 0; y < TN; y++) acc[x][y][q * 4 + e] = -kInf;
                     }
@@ -121,15 +130,13 @@ __global__ __launch_bounds__(F::kThreads) void k_logits(FwdArgs a) {
 #pragma unroll
     for (int y = 0; y < TN; y++) {
         const int64_t t = t0 + y * 32;
-        if (a.token && t < a.rows) {
-            const int64_t c = a.tokens[t] - c0;
-            if (c >= 0 && c < TM * 32 && !(c & 4)) {
+        if (__any(token[y] >= 0)) {
+            float v = 0.f;
 #pragma unroll
-                for (int x = 0; x < TM; x++)
+            for (int x = 0; x < TM; x++)
 #pragma unroll
-                    for (int k = 0; k < 16; k++)
-                        if (c == x * 32 + (k >> 2) * 8 + (k & 3)) a.token[t] = acc[x][y][k];
-            }
+                for (int k = 0; k < 16; k++) v = token[y] == x * 32 + (k >> 2) * 8 + (k & 3) ? acc[x][y][k] : v;
+            if (token[y] >= 0) a.token[t] = v;
         }
         float z[TM * 16];
 #pragma unroll
@@ -177,7 +184,7 @@ __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
     for (int r = 0; r < R; r++) {
         const uint32_t in = allowed4(a.mask, c0 + r * 16, a.classes);
 #pragma unroll
-        for (int e = 0; e < 4; e++) z[r * 4 + e] = in >> e & 1 ? sums[r][e] : -kInf;
+        for (int e = 0; e < 4; e++) z[r * 4 + e] = in >> (8 * e) & 0xffu ? sums[r][e] : -kInf;
     }
     if (a.token && t < a.rows) {
         const int64_t c = a.tokens[t] - c0;
@@ -294,7 +301,7 @@ __global__ __launch_bounds__(F::kThreads) void k_grads(GradArgs a) {
         s.at = -1;
         if (t < a.rows) s = a.slope[t];
         const int64_t token = s.at - a.first - i0 - wi;
-        const bool here = s.at >= 0 && token >= 0 && token < TM * 32 && !(token & 4);
+        const int here = s.at >= 0 && token >= 0 && token < TM * 32 && !(token & 4) ? (int)token : -1;
 #pragma unroll
         for (int x = 0; x < TM; x++)
 #pragma unroll
@@ -302,19 +309,17 @@ __global__ __launch_bounds__(F::kThreads) void k_grads(GradArgs a) {
                 const float d = (acc[x][y][k] - s.most) * scale, e = __builtin_amdgcn_exp2f(d);
                 acc[x][y][k] = e * fmaf(s.second, fmaxf(d, -300.f), s.first);
             }
-        if (__any(here)) {
+        if (__any(here >= 0)) {
 #pragma unroll
             for (int x = 0; x < TM; x++)
 #pragma unroll
-                for (int k = 0; k < 16; k++)
-                    if (here && token == x * 32 + (k >> 2) * 8 + (k & 3)) acc[x][y][k] += s.token;
+                for (int k = 0; k < 16; k++) acc[x][y][k] += here == x * 32 + (k >> 2) * 8 + (k & 3) ? s.token : 0.f;
         }
-        if (!__all(s.keep)) {
+        if (__any(!s.keep)) {
 #pragma unroll
             for (int x = 0; x < TM; x++)
 #pragma unroll
-                for (int k = 0; k < 16; k++)
-                    if (!s.keep) acc[x][y][k] = 0.f;
+                for (int k = 0; k < 16; k++) acc[x][y][k] = s.keep ? acc[x][y][k] : 0.f;
         }
     }
     if (a.mask || i0 + F::BM > a.classes) {
@@ -325,7 +330,7 @@ __global__ __launch_bounds__(F::kThreads) void k_grads(GradArgs a) {
                 const uint32_t in = allowed4(a.mask, i0 + wi + x * 32 + q * 8, a.classes);
 #pragma unroll
                 for (int e = 0; e < 4; e++)
-                    if (!(in >> e & 1)) {
+                    if (!(in >> (8 * e) & 0xffu)) {
 #pragma unroll
                         for (int y = 0; y < TN; y++) acc[x][y][q * 4 + e] = 0.f;
                     }
@@ -337,7 +342,7 @@ __global__ __launch_bounds__(F::kThreads) void k_grads(GradArgs a) {
     constexpr int kPieces = F::BM / 8;
 #pragma unroll
     for (int h = 0; h < P; h++) {
-        if (h) __syncthreads();
+        if (h) tile::lds_barrier();
         unsigned char* img = buffers.of(wave % F::WJ * (TN * 32) / kHalf);
 #pragma unroll
         for (int y = 0; y < TN; y++) {
@@ -361,7 +366,7 @@ __global__ __launch_bounds__(F::kThreads) void k_grads(GradArgs a) {
                     __builtin_memcpy(img + r * (F::BM * 2) + ((((c >> 3) ^ r) & (kPieces - 1)) << 4) + (c & 4) * 2, w, 8);
                 }
         }
-        __syncthreads();
+        tile::lds_barrier();
 #pragma unroll 4
         for (int e = threadIdx.x; e < F::BN * kPieces; e += F::kThreads) {
             const int r = e / kPieces, c = e % kPieces;

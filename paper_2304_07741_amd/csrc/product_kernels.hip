@@ -102,7 +102,7 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Task g) {
     const int wave = threadIdx.x >> 6, wi = wave / F::WJ * (TM * 32), wj = wave % F::WJ * (TN * 32);
 #pragma unroll 1
     for (int r0 = 0; r0 < BM; r0 += kRound) {
-        if (r0) __syncthreads();
+        if (r0) tile::lds_barrier();
 #pragma unroll
         for (int x = 0; x < TM; x++) {
             const int r = wi + x * 32 - r0;
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Task g) {
 #pragma unroll
             for (int y = 0; y < TN; y++) to_image<BN>(reinterpret_cast<float*>(buffers.of(r / kRows)), acc[x][y], r % kRows, wj + y * 32);
         }
-        __syncthreads();
+        tile::lds_barrier();
 #pragma unroll
         for (int n = 0; n < 2; n++) emit<F::PLANES == 3, kRows, BN, F::kThreads>(g, at.which, i0 + r0 + n * kRows, j0, reinterpret_cast<const float*>(buffers.at[n]));
     }
