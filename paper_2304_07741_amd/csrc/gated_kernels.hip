@@ -55,6 +55,22 @@ struct FwdArgs {
     int64_t plane;
 };
 
+// Tiles whose columns are those of both matrices.
+using SmallPair = Form<64, 128, 2, 2, 1, 64, 3>;
+using SmallTriplePair = Form<64, 128, 2, 2, 3, 32, 2>;
+template <class F>
+struct Paired {
+    using Type = F;
+};
+template <>
+struct Paired<product::Small> {
+    using Type = SmallPair;
+};
+template <>
+struct Paired<product::SmallTriple> {
+    using Type = SmallTriplePair;
+};
+
 template <class F, int ACT>
 __global__ __launch_bounds__(F::kThreads) void k_forward(FwdArgs a) {
     constexpr int TM = F::TM, TN = F::TN, kCols = F::BN / 2;
@@ -67,59 +83,69 @@ __global__ __launch_bounds__(F::kThreads) void k_forward(FwdArgs a) {
     const int steps = (int)((a.features + F::BK - 1) / F::BK);
     f32x16 acc[TM][TN] = {};
     product::accumulate<F, product::kRows, product::kRows, true>(a.x, a.w, 0, i0, j0, a.features, 0, steps, steps, 1, buffers, acc);
+    // g and u through LDS, kRows rows of the tile at a time: a few lines of code for all elements (64 copies of the activation, one for each
+    // register, take longer to fetch than to run where there is little else to do), and whole vectors to memory.  Elements change places by bits of the row, so that what
+    // the halves of a wave write at once falls on different banks.
+    constexpr int kFit = F::kStage / (kCols * 4), kTwos = kFit >= 128 ? 128 : kFit >= 64 ? 64 : 32, kRows = kTwos < F::BM ? kTwos : F::BM;
+    static_assert(kRows <= kFit && F::BM % kRows == 0, "rows of the tile in a buffer");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / F::WJ * (TM * 32), wj = wave % F::WJ * 32;
-    const int64_t j = j0 + wj + (lane & 31);
-    // bf16: the tile of y, the rows of each row of waves in a buffer
-    constexpr int kEach = TM * 32;
-    static_assert(kF32 || (kEach * kCols * 2 <= F::kStage && F::WI <= F::BUFFERS), "the tile of y in the buffers");
-    uint16_t* img = reinterpret_cast<uint16_t*>(buffers.of(wave / F::WJ));
+    float *img_g = reinterpret_cast<float*>(buffers.at[0]), *img_u = reinterpret_cast<float*>(buffers.at[1]);
+    const bool whole = (a.width & 7) == 0;
+#pragma unroll 1
+    for (int r0 = 0; r0 < F::BM; r0 += kRows) {
+        if (r0) tile::lds_barrier();
 #pragma unroll
-    for (int x = 0; x < TM; x++)
-#pragma unroll
-        for (int k = 0; k < 16; k++) {
-            const int r = wi + x * 32 + (k >> 2) * 8 + (lane >> 5) * 4 + (k & 3);
-            float unused;
-            const float y = act_of<ACT, false>(acc[x][0][k], unused) * acc[x][1][k];
-            if (kF32) {
-                if (i0 + r < a.rows && j < a.width) static_cast<float*>(a.y)[(i0 + r) * a.width + j] = y;
-            } else {
-                img[(r - wi) * kCols + wj + (lane & 31)] = f32_to_bf16(y);
-            }
-        }
-    // (g and u last: nothing waits for their way to memory)
-    if (!kF32) {
-        tile::lds_barrier();
-        const bool whole = (a.width & 7) == 0;
-#pragma unroll 2
-        for (int e = threadIdx.x; e < F::BM * (kCols / 8); e += F::kThreads) {
-            const int r = e / (kCols / 8), c = (e - r * (kCols / 8)) * 8;
-            const int64_t i = i0 + r, col = j0 + c;
-            if (i >= a.rows || col >= a.width) continue;
-            const u32x4 v = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(buffers.of(r / kEach)) + (r % kEach) * kCols + c);
-            uint16_t* to = static_cast<uint16_t*>(a.y) + i * a.width + col;
-            if (whole) {
-                *reinterpret_cast<u32x4*>(to) = v;
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; k++)
-                    if (col + k < a.width) to[k] = (uint16_t)(v[k >> 1] >> ((k & 1) * 16));
-            }
-        }
-    }
-    if (a.pre) {
-        // (what lies behind the rows or the columns is outside the buffers, whose stores are dropped)
-        const int64_t bytes = (a.rows - i0) * a.ld * 4;
-        const int size = bytes < 0x7fffffff ? (int)bytes : 0x7fffffff;
-        const tile::rsrc_t to_g = tile::make_rsrc(a.pre + i0 * a.ld, size), to_u = tile::make_rsrc(a.pre + a.plane + i0 * a.ld, size);
-        const uint32_t first = j < a.width ? (uint32_t)j * 4u + (uint32_t)(wi + (lane >> 5) * 4) * (uint32_t)a.ld * 4u : product::kOutside, ld = (uint32_t)a.ld * 4u;
-#pragma unroll
-        for (int x = 0; x < TM; x++)
+        for (int x = 0; x < TM; x++) {
+            if (wi + x * 32 < r0 || wi + x * 32 >= r0 + kRows) continue;
 #pragma unroll
             for (int k = 0; k < 16; k++) {
-                const int o = (int)(first + (uint32_t)(x * 32 + (k >> 2) * 8 + (k & 3)) * ld);
-                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(acc[x][0][k]), to_g, o, 0, 0);
-                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(acc[x][1][k]), to_u, o, 0, 0);
+                const int r = wi + x * 32 - r0 + (k >> 2) * 8 + (lane >> 5) * 4 + (k & 3), c = (wj + (lane & 31)) ^ ((r >> 2 & 1) << 5);
+                img_g[r * kCols + c] = acc[x][0][k];
+                img_u[r * kCols + c] = acc[x][1][k];
             }
+        }
+        tile::lds_barrier();
+#pragma unroll 1
+        for (int e = threadIdx.x; e < kRows * (kCols / 8); e += F::kThreads) {
+            const int r = e / (kCols / 8), c = (e - r * (kCols / 8)) * 8, from = r * kCols + (c ^ ((r >> 2 & 1) << 5));
+            const int64_t i = i0 + r0 + r, j = j0 + c;
+            if (i >= a.rows || j >= a.width) continue;
+            const f32x4 g[2] = {*reinterpret_cast<const f32x4*>(img_g + from), *reinterpret_cast<const f32x4*>(img_g + from + 4)};
+            const f32x4 u[2] = {*reinterpret_cast<const f32x4*>(img_u + from), *reinterpret_cast<const f32x4*>(img_u + from + 4)};
+            float y[8];
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                float unused;
+                y[k] = act_of<ACT, false>(g[k >> 2][k & 3], unused) * u[k >> 2][k & 3];
+            }
+            if (a.pre) {  // (rows of a multiple of 8)
+                f32x4 *to = reinterpret_cast<f32x4*>(a.pre + i * a.ld + j), *to_u = reinterpret_cast<f32x4*>(a.pre + a.plane + i * a.ld + j);
+                to[0] = g[0];
+                to[1] = g[1];
+                to_u[0] = u[0];
+                to_u[1] = u[1];
+            }
+            if (kF32) {
+                float* to = static_cast<float*>(a.y) + i * a.width + j;
+                if (whole) {
+                    reinterpret_cast<f32x4*>(to)[0] = f32x4{y[0], y[1], y[2], y[3]};
+                    reinterpret_cast<f32x4*>(to)[1] = f32x4{y[4], y[5], y[6], y[7]};
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; k++)
+                        if (j + k < a.width) to[k] = y[k];
+                }
+            } else {
+                uint16_t* to = static_cast<uint16_t*>(a.y) + i * a.width + j;
+                if (whole) {
+                    *reinterpret_cast<u32x4*>(to) = u32x4{tile::pack_bf16(y[0], y[1]), tile::pack_bf16(y[2], y[3]), tile::pack_bf16(y[4], y[5]), tile::pack_bf16(y[6], y[7])};
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; k++)
+                        if (j + k < a.width) to[k] = f32_to_bf16(y[k]);
+                }
+            }
+        }
     }
 }
 
@@ -292,7 +318,8 @@ Plan plan_of(const Shape& s) {
     p.few = s.rows <= kFewRows;
     p.copies = (s.f32 || ld != s.features) && !(p.few && s.inference);
     p.forward = product::cut_of(s.f32, s.rows, 2 * s.width, s.features, 1, false);
-    p.forward.tiles_j = (s.width + p.forward.side / 2 - 1) / (p.forward.side / 2);
+    const int64_t pairs = p.forward.side == 64 ? 64 : p.forward.side / 2;  // results of a tile's row (Paired)
+    p.forward.tiles_j = (s.width + pairs - 1) / pairs;
     p.launches_fwd = 1 + (p.copies && !p.few);
     p.most_tiles = p.few ? (s.width + 15) / 16 : p.forward.tiles();
     uint64_t at = 0;
@@ -328,12 +355,7 @@ void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
     if (p.copies) make_copies(s, p, a.x, a.w_gate, a.w_up, a.ws, stream);
     const Operands o = operands_of(s, p, a.x, a.w_gate, a.w_up, a.ws);
     const FwdArgs f{o.x, o.w, s.rows, s.features, s.width, p.forward.tiles_i, p.forward.tiles_j, ld, a.y, pre, s.rows * ld};
-    if (s.f32)
-        launch_forward<product::Triple>(s.act, f, stream);
-    else if (p.forward.side == 256)
-        launch_forward<product::Large>(s.act, f, stream);
-    else
-        launch_forward<product::Middle>(s.act, f, stream);
+    product::with_form(s.f32, p.forward.side, [&](auto form) { launch_forward<typename Paired<decltype(form)>::Type>(s.act, f, stream); });
 }
 
 void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {

@@ -465,12 +465,7 @@ void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
         }
         const int64_t ld = product::up8(s.features);
         const FwdArgs f{factor_of(w, s.classes, ld), factor_of(x, s.rows, ld), s.rows, s.features, s.classes, p.logits.tiles_i, p.logits.tiles_j, a.it, a.mask, a.tokens, sums, token};
-        if (s.f32)
-            launch_logits<product::Triple>(f, stream);
-        else if (p.logits.side == 256)
-            launch_logits<product::Large>(f, stream);
-        else
-            launch_logits<product::Middle>(f, stream);
+        product::with_form(s.f32, p.logits.side, [&](auto form) { launch_logits<decltype(form)>(f, stream); });
     }
     int across = 1;
     while (across < 16 && across * 2 <= s.rows) across *= 2;
@@ -501,12 +496,7 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
         const uint8_t* mask = a.mask ? a.mask + first : nullptr;
         const int64_t side = p.piece.side;
         const GradArgs g{w, x, s.rows, s.features, length, (length + side - 1) / side, p.piece.tiles_j, first, a.it, mask, slope, grads, ld, plane};
-        if (s.f32)
-            launch_grads<product::Triple>(g, stream);
-        else if (side == 256)
-            launch_grads<product::Large>(g, stream);
-        else
-            launch_grads<product::Middle>(g, stream);
+        product::with_form(s.f32, side, [&](auto form) { launch_grads<decltype(form)>(g, stream); });
         if (mask && !p.copies) {
             const product::Copy m{w.p[0], cw, length, s.features, mask};
             product::copy(false, &m, 1, stream);

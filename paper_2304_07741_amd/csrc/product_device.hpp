@@ -4,7 +4,7 @@
 // Rows along k: 16-byte pieces of eight summands; piece c of row r lies at place c ^ (r / rows per line of all banks), so that the
 // pieces that 16 lanes read together fall on different banks.  Rows of k: the matrix units want eight summands of one index in a lane, so the
 // rows are read by the transposing load, a block of 4 summands x 16 indexes by 16 lanes; the 32-byte units of row k lie at unit ^
-// {0, 2, 5, 7}[k % 4], for the same reason.  What lies behind the end of the sum is not loaded: an offset outside the buffer gives zeros, which
+// {0, 2, 5, 7}[k % 4] ({0, 0, 2, 2} where a line of all banks holds two rows), for the same reason.  What lies behind the end of the sum is not loaded: an offset outside the buffer gives zeros, which
 // stages behind the last one load too, so that the number of loads in flight is always the same.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -37,7 +37,24 @@ struct Form {
 };
 using Large = Form<256, 256, 2, 4, 1, 64, 2>;
 using Middle = Form<128, 128, 2, 2, 1, 64, 2>;
+using Small = Form<64, 64, 2, 2, 1, 64, 3>;
 using Triple = Form<128, 128, 2, 2, 3, 16, 3>;
+using SmallTriple = Form<64, 64, 2, 2, 3, 32, 3>;
+
+// f with the form that a cut asks for
+template <class F>
+void with_form(bool f32, int side, F f) {
+    if (f32 && side == 128)
+        f(Triple());
+    else if (f32)
+        f(SmallTriple());
+    else if (side == 256)
+        f(Large());
+    else if (side == 128)
+        f(Middle());
+    else
+        f(Small());
+}
 
 // One array per stage in flight, not one for all: the compiler has to see that loads into the one do not concern reads of another.
 template <class F>
@@ -67,7 +84,11 @@ __device__ __forceinline__ void loads_arrived() {
 
 template <int ROW>
 __device__ __forceinline__ int piece_of(int r, int c) { return c ^ ((r / (256 / ROW)) & (ROW / 16 - 1)); }
-__device__ __forceinline__ int unit_of(int k, int unit) { return unit ^ (((k & 1) << 1) | ((k >> 1) & 1) * 5); }
+template <int ROW>
+__device__ __forceinline__ int unit_of(int k, int unit) {
+    static_assert(ROW >= 128, "four units in a row at least");
+    return unit ^ (ROW == 128 ? k & 2 : ((k & 1) << 1) | ((k >> 1) & 1) * 5);
+}
 
 // What a thread loads of one operand.  PAIRS: indexes are taken 32 by 32 from the two matrices in turn.
 template <class F, int BX, Side SIDE, bool PAIRS>
@@ -101,7 +122,7 @@ struct Loader {
                 row = row < left ? row : left - 1;  // (behind the last one: that one again, for results that nobody keeps)
                 offset[q] = (uint32_t)row * (uint32_t)f.ld * 2u + piece_of<SIDE == kRows ? kRow : 256>(r, c) * 16;
             } else {
-                const int piece = unit_of(r, c >> 1) * 2 + (c & 1);
+                const int piece = unit_of<SIDE == kRows ? 256 : kRow>(r, c >> 1) * 2 + (c & 1);
                 offset[q] = piece * 8 < left ? (uint32_t)r * (uint32_t)f.ld * 2u + piece * 16 : kOutside;
             }
         }
@@ -139,7 +160,7 @@ struct Reader {
                 at[n] = r * kRow + piece_of<SIDE == kRows ? kRow : 256>(r, n * 2 + (lane >> 5)) * 16;
             } else {
                 const int j = lane & 15, g = lane >> 4;
-                at[n] = ((g >> 1) * 8 + (j >> 2)) * kRow + unit_of(j >> 2, (base + n * 32) / 16 + (g & 1)) * 32 + (j & 3) * 8;
+                at[n] = ((g >> 1) * 8 + (j >> 2)) * kRow + unit_of<SIDE == kRows ? 256 : kRow>(j >> 2, (base + n * 32) / 16 + (g & 1)) * 32 + (j & 3) * 8;
             }
         }
     }

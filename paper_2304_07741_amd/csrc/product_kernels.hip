@@ -97,7 +97,7 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Task g) {
         return;
     }
     // through LDS, kRows rows of results to a buffer
-    constexpr int kRows = F::kStage / (BN * 4) / 32 * 32, kRound = 2 * kRows;
+    constexpr int kFit = F::kStage / (BN * 4) / 32 * 32, kRows = kFit < BM / 2 ? kFit : BM / 2, kRound = 2 * kRows;
     static_assert(BM % kRound == 0, "rows of results in the buffers");
     const int wave = threadIdx.x >> 6, wi = wave / F::WJ * (TM * 32), wj = wave % F::WJ * (TN * 32);
 #pragma unroll 1
@@ -227,15 +227,17 @@ Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, boo
         return c.tiles() * results;
     };
     const int64_t steps = (depth + (f32 ? 15 : 63)) / (f32 ? 16 : 64);
+    // the largest tile that gives more than half of the compute units one, or a part of one
     if (!f32) {
-        // a tile of 256 for more than half of the compute units, or parts of them
         const int64_t t = tiles(256);
-        if (t >= 180) return c;
-        c.splits = may_split ? (int)std::max<int64_t>(1, std::min<int64_t>(256 / t, steps / 16)) : 1;
+        c.splits = may_split && t < 180 ? (int)std::max<int64_t>(1, std::min<int64_t>(256 / t, steps / 16)) : 1;
         if (t * c.splits >= 180) return c;
     }
-    const int64_t t = tiles(128);
-    c.splits = may_split && t < 256 ? (int)std::max<int64_t>(1, std::min<int64_t>(512 / t, steps / (f32 ? 16 : 8))) : 1;
+    int64_t t = tiles(128);
+    c.splits = may_split && t < 256 ? (int)std::max<int64_t>(1, std::min<int64_t>(512 / t, steps / (f32 ? 32 : 8))) : 1;
+    if (t * c.splits >= 160) return c;
+    t = tiles(64);
+    c.splits = may_split && t < 256 ? (int)std::max<int64_t>(1, std::min<int64_t>(512 / t, steps / (f32 ? 16 : 4))) : 1;
     return c;
 }
 
@@ -246,12 +248,7 @@ int launches_of(const Cut& c, bool several) { return 1 + (c.splits > 1 || severa
 
 void multiply(const Product& p, hipStream_t stream) {
     const Task t{p.a, p.b, p.depth, p.cut.tiles_i, p.cut.tiles_j, p.ld, p.segments, p.results, p.cut.splits, {p.out[0], p.out[1]}, reinterpret_cast<f32x4*>(p.parts), p.first};
-    if (p.f32)
-        launch_form<Triple>(p, t, stream);
-    else if (p.cut.side == 256)
-        launch_form<Large>(p, t, stream);
-    else
-        launch_form<Middle>(p, t, stream);
+    with_form(p.f32, p.cut.side, [&](auto form) { launch_form<decltype(form)>(p, t, stream); });
 }
 
 void copy(bool f32, const Copy* copies, int n, hipStream_t stream) {
