@@ -194,7 +194,8 @@ struct GradArgs {
     const float* pre;
     int64_t plane, rows, width, ld;
     const void* dy;
-    uint16_t* to;  // dg, then du: planes of `plane` elements each
+    uint16_t *dg, *du;
+    int64_t pitch;
 };
 // dg and du, eight elements per thread and turn; zeros behind the columns.
 template <bool F32, int ACT>
@@ -237,10 +238,10 @@ __global__ __launch_bounds__(256) void k_grads(GradArgs a) {
             du[e] = in ? dy[e] * act : 0.f;
             dg[e] = in ? dy[e] * u[e >> 2][e & 3] * slope : 0.f;
         }
-        uint16_t* to = a.to + k * 8;
 #pragma unroll
         for (int which = 0; which < 2; which++) {
             const float* v = which ? du : dg;
+            uint16_t* to = (which ? a.du : a.dg) + row * a.pitch;
             u32x4 w[P];
 #pragma unroll
             for (int e = 0; e < 4; e++) {
@@ -255,7 +256,7 @@ __global__ __launch_bounds__(256) void k_grads(GradArgs a) {
                 }
             }
 #pragma unroll
-            for (int h = 0; h < P; h++) *reinterpret_cast<u32x4*>(to + (which * P + h) * a.plane) = w[h];
+            for (int h = 0; h < P; h++) *reinterpret_cast<u32x4*>(to + product::column<P>(col, h)) = w[h];
         }
     }
 }
@@ -299,9 +300,9 @@ Operands operands_of(const Shape& s, const Plan& p, const void* x, const void* w
     const void* given[3] = {x, w_gate, w_up};
     const uint16_t* at[3];
     for (int i = 0; i < 3; i++) at[i] = p.copies ? reinterpret_cast<const uint16_t*>(ws + p.copy_at[i]) : static_cast<const uint16_t*>(given[i]);
-    const int64_t ld = product::up8(s.features);
-    o.x = Factor{{at[0], at[0]}, ld, s.rows * ld, s.rows};
-    o.w = Factor{{at[1], at[2]}, ld, s.width * ld, s.width};
+    const int64_t ld = product::pitch(s.f32, s.features);
+    o.x = Factor{{at[0], at[0]}, ld, s.rows};
+    o.w = Factor{{at[1], at[2]}, ld, s.width};
     return o;
 }
 void make_copies(const Shape& s, const Plan& p, const void* x, const void* w_gate, const void* w_up, char* ws, hipStream_t stream) {
@@ -314,9 +315,9 @@ void make_copies(const Shape& s, const Plan& p, const void* x, const void* w_gat
 
 Plan plan_of(const Shape& s) {
     Plan p;
-    const int64_t ld = product::up8(s.features), wide = product::up8(s.width), planes = s.f32 ? 3 : 1;
+    const int64_t ld = product::pitch(s.f32, s.features), wide = product::padded(s.f32, s.width);
     p.few = s.rows <= kFewRows;
-    p.copies = (s.f32 || ld != s.features) && !(p.few && s.inference);
+    p.copies = (s.f32 || s.features % 8) && !(p.few && s.inference);
     p.forward = product::cut_of(s.f32, s.rows, 2 * s.width, s.features, 1, false);
     const int64_t pairs = p.forward.side == 64 ? 64 : p.forward.side / 2;  // results of a tile's row (Paired)
     p.forward.tiles_j = (s.width + pairs - 1) / pairs;
@@ -330,7 +331,7 @@ Plan plan_of(const Shape& s) {
     };
     if (p.copies) {
         const int64_t rows[3] = {s.rows, s.width, s.width};
-        for (int i = 0; i < 3; i++) p.copy_at[i] = take(2ull * planes * rows[i] * ld);
+        for (int i = 0; i < 3; i++) p.copy_at[i] = take(2ull * rows[i] * ld);
     }
     if (!s.inference) {
         p.dx = product::cut_of(s.f32, s.rows, s.features, 2 * s.width, 1, true);
@@ -338,7 +339,7 @@ Plan plan_of(const Shape& s) {
         p.launches_bwd = (p.copies && p.few) + 1 + product::launches_of(p.dx, false) + product::launches_of(p.dw, false);
         p.most_tiles = std::max({p.most_tiles, p.dx.tiles() * p.dx.splits, 2 * p.dw.tiles() * p.dw.splits});
         p.pre_at = take(8ull * s.rows * wide);
-        p.grad_at = take(4ull * planes * s.rows * wide);
+        p.grad_at = take(4ull * s.rows * product::pitch(s.f32, s.width));
         p.parts_at = take(std::max(product::parts_bytes(p.dx, 1, false), product::parts_bytes(p.dw, 2, false)));
     }
     p.workspace_bytes = at;
@@ -346,7 +347,7 @@ Plan plan_of(const Shape& s) {
 }
 
 void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
-    const int64_t ld = product::up8(s.width);
+    const int64_t ld = product::padded(s.f32, s.width);
     float* pre = s.inference ? nullptr : reinterpret_cast<float*>(a.ws + p.pre_at);
     if (p.few) {
         const FewArgs f{a.x, a.w_gate, a.w_up, s.rows, s.features, s.width, ld, a.y, pre, s.rows * ld};
@@ -359,10 +360,10 @@ void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
 }
 
 void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
-    const int64_t ld = product::up8(s.width), plane = s.rows * ld, planes = s.f32 ? 3 : 1;
+    const int64_t ld = product::padded(s.f32, s.width), plane = s.rows * ld, wide = product::pitch(s.f32, s.width);
     if (p.copies && p.few) make_copies(s, p, a.x, a.w_gate, a.w_up, a.ws, stream);
-    uint16_t* grads = reinterpret_cast<uint16_t*>(a.ws + p.grad_at);
-    const GradArgs g{reinterpret_cast<const float*>(a.ws + p.pre_at), plane, s.rows, s.width, ld, a.dy, grads};
+    uint16_t *dg = reinterpret_cast<uint16_t*>(a.ws + p.grad_at), *du = dg + s.rows * wide;
+    const GradArgs g{reinterpret_cast<const float*>(a.ws + p.pre_at), plane, s.rows, s.width, ld, a.dy, dg, du, wide};
     const dim3 grid((unsigned)std::min<int64_t>((plane / 8 + 255) / 256, 8192));
     with_act(s.act, [&](auto kind) {
         if (s.f32)
@@ -371,11 +372,10 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
             CANVAS_LAUNCH((k_grads<false, decltype(kind)::value>), grid, dim3(256), 0, stream, g);
     });
     const Operands o = operands_of(s, p, a.x, a.w_gate, a.w_up, a.ws);
-    const uint16_t* of[2] = {grads, grads + planes * plane};
     float* parts = reinterpret_cast<float*>(a.ws + p.parts_at);
     product::Product d;
     d.f32 = s.f32;
-    d.a = Factor{{of[0], of[1]}, ld, plane, s.rows};
+    d.a = Factor{{dg, du}, wide, s.rows};
     d.a_rows = true;
     d.b = o.w;
     d.b.count = s.features;

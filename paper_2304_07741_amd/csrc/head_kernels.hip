@@ -278,8 +278,8 @@ struct GradArgs {
     float it;
     const uint8_t* mask;           // of this piece
     const Slope* slope;
-    uint16_t* to;                  // [rows][ld], planes `plane` elements apart
-    int64_t ld, plane;
+    uint16_t* to;                  // [rows][ld], `wide` columns
+    int64_t ld, wide;
 };
 // The gradients of a tile of logits.
 template <class F>
@@ -371,9 +371,9 @@ __global__ __launch_bounds__(F::kThreads) void k_grads(GradArgs a) {
         for (int e = threadIdx.x; e < F::BN * kPieces; e += F::kThreads) {
             const int r = e / kPieces, c = e % kPieces;
             const int64_t t = j0 + r, col = i0 + c * 8;
-            if (t >= a.rows || col >= a.ld) continue;
+            if (t >= a.rows || col >= a.wide) continue;
             const u32x4 v = *reinterpret_cast<const u32x4*>(buffers.of(r / kHalf) + (r & (kHalf - 1)) * (F::BM * 2) + (((c ^ r) & (kPieces - 1)) << 4));
-            *reinterpret_cast<u32x4*>(a.to + h * a.plane + t * a.ld + col) = v;
+            *reinterpret_cast<u32x4*>(a.to + t * a.ld + product::column<P>(col, h)) = v;
         }
     }
 }
@@ -400,15 +400,15 @@ void launch_grads(const GradArgs& a, hipStream_t stream) {
     CANVAS_LAUNCH(k_grads<F>, rows_of_workgroups(a.tiles_i * a.tiles_j, F::kThreads), dim3(F::kThreads), 0, stream, a);
 }
 
-Factor factor_of(const uint16_t* at, int64_t rows, int64_t ld) { return Factor{{at, at}, ld, rows * ld, rows}; }
+Factor factor_of(const uint16_t* at, int64_t rows, int64_t ld) { return Factor{{at, at}, ld, rows}; }
 
 }  // namespace
 
 Plan plan_of(const Shape& s) {
     Plan p;
-    const int64_t ld = product::up8(s.features), planes = s.f32 ? 3 : 1;
+    const int64_t ld = product::pitch(s.f32, s.features), planes = s.f32 ? 3 : 1;
     p.few = s.rows <= kFewRows;
-    p.copies = (s.f32 || ld != s.features) && !(p.few && s.inference);
+    p.copies = (s.f32 || s.features % 8) && !(p.few && s.inference);
     p.logits = product::cut_of(s.f32, s.classes, s.rows, s.features, 1, false);
     p.segments = (int)(p.few ? (s.classes + kFewClasses - 1) / kFewClasses : p.logits.tiles_i * 2);
     p.launches_fwd = 2 + (p.copies && !p.few);
@@ -421,8 +421,8 @@ Plan plan_of(const Shape& s) {
     };
     p.sums_at = take(sizeof(Sums) * (uint64_t)s.rows * p.segments);
     p.token_at = take(4ull * s.rows);
-    if (p.copies || !s.inference) p.copy_at[0] = take(2ull * planes * s.rows * ld);
-    if (p.copies) p.copy_at[1] = take(2ull * planes * s.classes * ld);
+    if (p.copies || !s.inference) p.copy_at[0] = take(2ull * s.rows * ld);
+    if (p.copies) p.copy_at[1] = take(2ull * s.classes * ld);
     if (!s.inference) {
         p.rows_at = take(sizeof(Row) * (uint64_t)s.rows);
         p.slope_at = take(sizeof(Slope) * (uint64_t)s.rows);
@@ -437,7 +437,7 @@ Plan plan_of(const Shape& s) {
         if (!p.copies) p.copy_at[1] = take(2ull * p.length * ld);
         p.launches_bwd = 2 + p.pieces * (2 + product::launches_of(p.dw, false)) + (product::launches_of(p.dx, p.pieces > 1) - 1);
         p.most_tiles = std::max({p.most_tiles, p.piece.tiles(), p.dx.tiles() * p.dx.splits, p.dw.tiles() * p.dw.splits});
-        p.grad_at = take(2ull * planes * s.rows * product::up8(p.length));
+        p.grad_at = take(2ull * s.rows * product::pitch(s.f32, p.length));
         p.parts_dx_at = take(product::parts_bytes(p.dx, 1, p.pieces > 1));
         p.parts_dw_at = take(product::parts_bytes(p.dw, 1, false));
     }
@@ -463,7 +463,7 @@ void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
             x = cx;
             w = cw;
         }
-        const int64_t ld = product::up8(s.features);
+        const int64_t ld = product::pitch(s.f32, s.features);
         const FwdArgs f{factor_of(w, s.classes, ld), factor_of(x, s.rows, ld), s.rows, s.features, s.classes, p.logits.tiles_i, p.logits.tiles_j, a.it, a.mask, a.tokens, sums, token};
         product::with_form(s.f32, p.logits.side, [&](auto form) { launch_logits<decltype(form)>(f, stream); });
     }
@@ -485,9 +485,9 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
     const bool whole = p.copies && p.few;
     const product::Copy c[2] = {{a.x, cx, s.rows, s.features, live}, {a.weight, cw, s.classes, s.features, a.mask}};
     product::copy(s.f32, c, whole ? 2 : 1, stream);
-    const int64_t lx = product::up8(s.features);
+    const int64_t lx = product::pitch(s.f32, s.features);
     const Factor x = factor_of(cx, s.rows, lx), all = factor_of(p.copies ? cw : static_cast<const uint16_t*>(a.weight), s.classes, lx);
-    const int64_t ld = product::up8(p.length), plane = s.rows * ld;
+    const int64_t ld = product::pitch(s.f32, p.length), wide = product::padded(s.f32, p.length);
     for (int n = 0; n < p.pieces; n++) {
         const int64_t first = n * p.length, length = std::min(p.length, s.classes - first);
         Factor w = all;
@@ -495,7 +495,7 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
         w.count = length;
         const uint8_t* mask = a.mask ? a.mask + first : nullptr;
         const int64_t side = p.piece.side;
-        const GradArgs g{w, x, s.rows, s.features, length, (length + side - 1) / side, p.piece.tiles_j, first, a.it, mask, slope, grads, ld, plane};
+        const GradArgs g{w, x, s.rows, s.features, length, (length + side - 1) / side, p.piece.tiles_j, first, a.it, mask, slope, grads, ld, wide};
         product::with_form(s.f32, side, [&](auto form) { launch_grads<decltype(form)>(g, stream); });
         if (mask && !p.copies) {
             const product::Copy m{w.p[0], cw, length, s.features, mask};
@@ -504,7 +504,7 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
         }
         product::Product d;
         d.f32 = s.f32;
-        d.a = Factor{{grads, grads}, ld, plane, s.rows};
+        d.a = Factor{{grads, grads}, ld, s.rows};
         d.a_rows = true;
         d.b = w;
         d.b.count = s.features;

@@ -105,9 +105,10 @@ struct Loader {
     static __device__ __forceinline__ int row_of(int tid, int q) { return (tid + q * F::kThreads) / kPieces; }
     static __device__ __forceinline__ int place_of(int tid, int q) { return (tid + q * F::kThreads) % kPieces; }
 
+    static __device__ __forceinline__ uint32_t bytes_of(int piece) { return (uint32_t)column<F::PLANES>(piece * 8, 0) * 2u; }
     // The tile from index `first` on, the sum from k on.
     __device__ __forceinline__ void seek(const Factor& f, int which, int64_t first, int64_t k) {
-        const int64_t from = SIDE == kRows ? first * f.ld + k : first + k * f.ld;
+        const int64_t from = SIDE == kRows ? first * f.ld + k * F::PLANES : first * F::PLANES + k * f.ld;  // (whole pieces of 16)
         at = (!PAIRS && which ? f.p[1] : f.p[0]) + from;
         if (PAIRS) other = f.p[1] + from;
     }
@@ -120,10 +121,10 @@ struct Loader {
             if (SIDE == kRows) {
                 int row = PAIRS ? (r >> 6) * 32 + (r & 31) : r;
                 row = row < left ? row : left - 1;  // (behind the last one: that one again, for results that nobody keeps)
-                offset[q] = (uint32_t)row * (uint32_t)f.ld * 2u + piece_of<SIDE == kRows ? kRow : 256>(r, c) * 16;
+                offset[q] = (uint32_t)row * (uint32_t)f.ld * 2u + bytes_of(piece_of<SIDE == kRows ? kRow : 256>(r, c));
             } else {
                 const int piece = unit_of<SIDE == kRows ? 256 : kRow>(r, c >> 1) * 2 + (c & 1);
-                offset[q] = piece * 8 < left ? (uint32_t)r * (uint32_t)f.ld * 2u + piece * 16 : kOutside;
+                offset[q] = piece * 8 < left ? (uint32_t)r * (uint32_t)f.ld * 2u + bytes_of(piece) : kOutside;
             }
         }
     }
@@ -137,9 +138,9 @@ struct Loader {
 #pragma unroll
             for (int q = 0; q < kTimes; q++) {
                 const bool second = PAIRS && ((((wave * 64 + q * F::kThreads) / kPieces) >> 5) & 1);
-                load_to_lds(buffer_from((second ? other : at) + h * f.plane), to + h * kPlane + q * (F::kThreads * 16), behind < some - q * kApart ? offset[q] : kOutside);
+                load_to_lds(buffer_from((second ? other : at) + h * 16), to + h * kPlane + q * (F::kThreads * 16), behind < some - q * kApart ? offset[q] : kOutside);
             }
-        const int64_t step = SIDE == kRows ? F::BK : F::BK * f.ld;
+        const int64_t step = SIDE == kRows ? F::BK * F::PLANES : F::BK * f.ld;
         at += step;
         if (PAIRS) other += step;
     }

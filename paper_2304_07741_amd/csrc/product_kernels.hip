@@ -151,17 +151,19 @@ __global__ __launch_bounds__(256) void k_join(Task g) {
 struct Copies {
     Copy c[3];
 };
-// Eight elements of the copy per thread and turn; zeros behind the columns.
+// Eight columns per thread and turn; zeros behind the last one.
 template <bool F32>
 __global__ __launch_bounds__(256) void k_copy(Copies all) {
     const Copy& c = all.c[blockIdx.y];
-    const int64_t wide = (c.cols + 7) / 8, n = c.rows * wide, plane = n * 8;
+    constexpr int P = F32 ? 3 : 1;
+    const int64_t wide = padded(F32, c.cols) / 8, n = c.rows * wide, ld = pitch(F32, c.cols);
     const bool whole = (c.cols & 7) == 0;
     for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < n; k += (int64_t)gridDim.x * 256) {
         const int64_t row = k / wide, col = (k - row * wide) * 8, from = row * c.cols + col;
-        if (c.live && !c.live[row]) {
+        uint16_t* to = c.to + row * ld;
+        if (col >= c.cols || (c.live && !c.live[row])) {
 #pragma unroll
-            for (int h = 0; h < (F32 ? 3 : 1); h++) *reinterpret_cast<u32x4*>(c.to + h * plane + k * 8) = u32x4{};
+            for (int h = 0; h < P; h++) *reinterpret_cast<u32x4*>(to + column<P>(col, h)) = u32x4{};
             continue;
         }
         if (F32) {
@@ -185,7 +187,7 @@ __global__ __launch_bounds__(256) void k_copy(Copies all) {
                 for (int h = 0; h < 3; h++) w[h][e] = lo[h] | (uint32_t)hi[h] << 16;
             }
 #pragma unroll
-            for (int h = 0; h < 3; h++) *reinterpret_cast<u32x4*>(c.to + h * plane + k * 8) = w[h];
+            for (int h = 0; h < 3; h++) *reinterpret_cast<u32x4*>(to + column<P>(col, h)) = w[h];
         } else {
             const uint16_t* x = static_cast<const uint16_t*>(c.from) + from;
             u32x4 w;
@@ -195,7 +197,7 @@ __global__ __launch_bounds__(256) void k_copy(Copies all) {
 #pragma unroll
                 for (int e = 0; e < 4; e++) w[e] = (col + 2 * e < c.cols ? x[2 * e] : 0) | (uint32_t)(col + 2 * e + 1 < c.cols ? x[2 * e + 1] : 0) << 16;
             }
-            *reinterpret_cast<u32x4*>(c.to + k * 8) = w;
+            *reinterpret_cast<u32x4*>(to + col) = w;
         }
     }
 }
@@ -215,8 +217,6 @@ void launch_form(const Product& p, const Task& t, hipStream_t stream) {
 }
 
 }  // namespace
-
-int64_t up8(int64_t n) { return (n + 7) & ~(int64_t)7; }
 
 Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, bool may_split) {
     Cut c;
@@ -256,7 +256,7 @@ void copy(bool f32, const Copy* copies, int n, hipStream_t stream) {
     int64_t most = 0;
     for (int i = 0; i < n; i++) {
         all.c[i] = copies[i];
-        most = std::max(most, copies[i].rows * ((copies[i].cols + 7) / 8));
+        most = std::max(most, copies[i].rows * padded(f32, copies[i].cols) / 8);
     }
     const dim3 grid((unsigned)std::min<int64_t>((most + 255) / 256, 4096), (unsigned)n);
     if (f32)

@@ -8,13 +8,19 @@
 namespace canvas {
 namespace product {
 
-// One operand.  In memory either rows of indexes with the summed index k along them, or rows of k with the indexes along them; leading
-// dimensions are multiples of 8, rows along k hold zeros from their end to the next multiple of 8.
+// One operand.  In memory either rows of indexes with the summed index k along them, or rows of k with the indexes along them.  bf16: rows of a multiple of 8
+// elements.  fp32 matrices: rows of pieces of 16 columns, each its first, second and third plane in turn, so that what a stage of a product takes of a
+// row lies together.  From their end to the next multiple of 8 or 16 rows hold zeros.
 struct Factor {
     const uint16_t* p[2] = {nullptr, nullptr};  // of the two halves of a sum over 2 * depth, or of the two results of a launch
-    int64_t ld = 0, plane = 0;                  // elements from row to row, and from one of three planes to the next
+    int64_t ld = 0;                             // elements of all planes from row to row
     int64_t count = 0;                          // indexes
 };
+__host__ __device__ inline int64_t padded(bool f32, int64_t cols) { return f32 ? (cols + 15) / 16 * 16 : (cols + 7) / 8 * 8; }
+__host__ __device__ inline int64_t pitch(bool f32, int64_t cols) { return padded(f32, cols) * (f32 ? 3 : 1); }
+// Where eight columns from `col` (a multiple of 8) on begin in their row, plane h.
+template <int PLANES>
+__host__ __device__ constexpr int64_t column(int64_t col, int h) { return PLANES == 1 ? col : col / 16 * 48 + h * 16 + col % 16; }
 
 // How results are cut: tiles of `side` x `side`, the sum over k in `splits` parts.
 struct Cut {
@@ -38,7 +44,6 @@ struct Product {
     bool first = true, last = true;
 };
 
-int64_t up8(int64_t n);
 // `steps`: of the whole sum, each as deep as a tile takes at once.
 Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, bool may_split);
 uint64_t parts_bytes(const Cut& c, int results, bool several);
@@ -46,7 +51,7 @@ uint64_t parts_bytes(const Cut& c, int results, bool several);
 int launches_of(const Cut& c, bool several);
 void multiply(const Product& p, hipStream_t stream);
 
-// A matrix of `rows` x `cols` elements as one bf16 plane (of bf16 elements) or three (of fp32 ones) with leading dimension up8(cols).
+// A matrix of `rows` x `cols` elements laid out as a Factor.
 // `live`: bytes by row, 0 for rows that are zeros in the copy whatever they hold.
 struct Copy {
     const void* from = nullptr;
