@@ -218,27 +218,50 @@ void launch_form(const Product& p, const Task& t, hipStream_t stream) {
 
 }  // namespace
 
+// What a form costs, in us: a stage of a workgroup where a few compute units have one, where each has one, and where each has two or three (`slots`), and
+// the beginning and the end of a tile.  Measured, us of rows x columns x summands without parts, for tiles of 256, 128, 64, and in fp32 of 128, 64:
+//   256 x 256 x 4096      77   33   23    130   51      1024 x 1024 x 4096    80   48   26    136   63      2048 x 2048 x 4096    80   56   60    158  217
+//   2048 x 4096 x 4096    86   66  109    290  483      4096 x 4096 x 4096   106  136  222    551  701      4096 x 4096 x 256     18   20   29     48   61
+// in four parts: 1024 x 1024 x 4096    33   27   26     52   60
+struct Speed {
+    int side, depth, slots;
+    double few, one, two, three, ends;
+};
+constexpr Speed kSpeeds[2][3] = {{{256, 64, 1, 1.15, 1.6, 0, 0, 8.0}, {128, 64, 2, 0.55, 0.80, 0.95, 0, 4.8}, {64, 64, 3, 0.34, 0.36, 0.43, 0.51, 2.6}},
+                                 {{128, 16, 2, 0.51, 0.60, 1.10, 0, 4.8}, {64, 32, 2, 0.39, 0.46, 0.82, 0, 1.0}, {0, 0, 0, 0, 0, 0, 0, 0}}};
+
 Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, bool may_split) {
-    Cut c;
-    auto tiles = [&](int side) {
-        c.side = side;
-        c.tiles_i = (rows + side - 1) / side;
-        c.tiles_j = (cols + side - 1) / side;
-        return c.tiles() * results;
-    };
-    const int64_t steps = (depth + (f32 ? 15 : 63)) / (f32 ? 16 : 64);
-    // the largest tile that gives more than half of the compute units one, or a part of one
-    if (!f32) {
-        const int64_t t = tiles(256);
-        c.splits = may_split && t < 180 ? (int)std::max<int64_t>(1, std::min<int64_t>(256 / t, steps / 16)) : 1;
-        if (t * c.splits >= 180) return c;
+    Cut best;
+    double least = 0;
+    for (const Speed& v : kSpeeds[f32]) {
+        if (!v.side) continue;
+        Cut c;
+        c.side = v.side;
+        c.tiles_i = (rows + v.side - 1) / v.side;
+        c.tiles_j = (cols + v.side - 1) / v.side;
+        const int64_t tiles = c.tiles() * results, steps = (depth + v.depth - 1) / v.depth;
+        // `n` workgroups at a time
+        auto turn = [&](int64_t n, double stages) {
+            const double at[4] = {v.few, v.one, v.two, v.three};
+            const int k = (int)((n - 1) / 256);
+            const double share = (double)(n - k * 256) / 256;
+            return stages * (at[k] + (at[k + 1] - at[k]) * share) + v.ends * (0.4 + 0.6 * n / (256.0 * v.slots));
+        };
+        for (int splits = 1; splits <= 32; splits += splits < 4 ? 1 : splits < 8 ? 2 : splits / 4) {
+            if (splits > 1 && (!may_split || tiles * splits > 1024 || steps / splits < 2)) break;
+            const double each = (double)((steps + splits - 1) / splits);
+            const int64_t all = tiles * splits, slots = 256 * v.slots, rest = all % slots;
+            double t = (double)(all / slots) * turn(slots, each) + (rest ? turn(rest, each) : 0);
+            // parts of a sum: a launch, and their way to memory and back
+            if (splits > 1) t += 4 + 0.15e-6 * 4 * v.side * v.side * (double)all;
+            if (!least || t < least) {
+                least = t;
+                best = c;
+                best.splits = splits;
+            }
+        }
     }
-    int64_t t = tiles(128);
-    c.splits = may_split && t < 256 ? (int)std::max<int64_t>(1, std::min<int64_t>(512 / t, steps / (f32 ? 32 : 8))) : 1;
-    if (t * c.splits >= 160) return c;
-    t = tiles(64);
-    c.splits = may_split && t < 256 ? (int)std::max<int64_t>(1, std::min<int64_t>(512 / t, steps / (f32 ? 16 : 4))) : 1;
-    return c;
+    return best;
 }
 
 uint64_t parts_bytes(const Cut& c, int results, bool several) {
