@@ -77,7 +77,7 @@ __global__ __launch_bounds__(F::kThreads) void k_forward(FwdArgs a) {
     constexpr bool kF32 = F::PLANES == 3;
     static_assert(TN == 2, "a wave holds one block of each matrix");
     PRODUCT_BUFFERS(F, buffers);
-    const product::Place at = product::place_of(a.tiles_i, a.tiles_j, 1, 1);
+    const product::Place at = product::place_of(tile::xcd_sequence(), a.tiles_i, a.tiles_j, 1, 1);
     if (!at.inside) return;
     const int64_t i0 = at.i * F::BM, j0 = at.j * kCols;
     const int steps = (int)((a.features + F::BK - 1) / F::BK);
@@ -336,11 +336,12 @@ Plan plan_of(const Shape& s) {
     if (!s.inference) {
         p.dx = product::cut_of(s.f32, s.rows, s.features, 2 * s.width, 1, true);
         p.dw = product::cut_of(s.f32, s.width, s.features, s.rows, 2, true);
-        p.launches_bwd = (p.copies && p.few) + 1 + product::launches_of(p.dx, false) + product::launches_of(p.dw, false);
-        p.most_tiles = std::max({p.most_tiles, p.dx.tiles() * p.dx.splits, 2 * p.dw.tiles() * p.dw.splits});
+        p.launches_bwd = (p.copies && p.few) + 1 + product::launches_of(p.dx, p.dw, false);
+        p.most_tiles = std::max(p.most_tiles, p.dx.tiles() * p.dx.splits + 2 * p.dw.tiles() * p.dw.splits);
         p.pre_at = take(8ull * s.rows * wide);
         p.grad_at = take(4ull * s.rows * product::pitch(s.f32, s.width));
-        p.parts_at = take(std::max(product::parts_bytes(p.dx, 1, false), product::parts_bytes(p.dw, 2, false)));
+        p.parts_at = take(product::parts_bytes(p.dx, 1, false));
+        p.parts_dw_at = take(product::parts_bytes(p.dw, 2, false));
     }
     p.workspace_bytes = at;
     return p;
@@ -372,7 +373,6 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
             CANVAS_LAUNCH((k_grads<false, decltype(kind)::value>), grid, dim3(256), 0, stream, g);
     });
     const Operands o = operands_of(s, p, a.x, a.w_gate, a.w_up, a.ws);
-    float* parts = reinterpret_cast<float*>(a.ws + p.parts_at);
     product::Product d;
     d.f32 = s.f32;
     d.a = Factor{{dg, du}, wide, s.rows};
@@ -384,20 +384,20 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
     d.out[0] = a.dx;
     d.ld = s.features;
     d.cut = p.dx;
-    d.parts = p.dx.splits > 1 ? parts : nullptr;
-    product::multiply(d, stream);
-    d.a.count = s.width;
-    d.a_rows = false;
-    d.b = o.x;
-    d.b.count = s.features;
-    d.depth = s.rows;
-    d.segments = 1;
-    d.results = 2;
-    d.out[0] = a.dw_gate;
-    d.out[1] = a.dw_up;
-    d.cut = p.dw;
-    d.parts = p.dw.splits > 1 ? parts : nullptr;
-    product::multiply(d, stream);
+    d.parts = p.dx.splits > 1 ? reinterpret_cast<float*>(a.ws + p.parts_at) : nullptr;
+    product::Product w = d;
+    w.a.count = s.width;
+    w.a_rows = false;
+    w.b = o.x;
+    w.b.count = s.features;
+    w.depth = s.rows;
+    w.segments = 1;
+    w.results = 2;
+    w.out[0] = a.dw_gate;
+    w.out[1] = a.dw_up;
+    w.cut = p.dw;
+    w.parts = p.dw.splits > 1 ? reinterpret_cast<float*>(a.ws + p.parts_dw_at) : nullptr;
+    product::multiply(d, w, stream);
 }
 
 }  // namespace gated

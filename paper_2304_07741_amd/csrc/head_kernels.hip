@@ -95,7 +95,7 @@ template <class F>
 __global__ __launch_bounds__(F::kThreads) void k_logits(FwdArgs a) {
     constexpr int TM = F::TM, TN = F::TN;
     PRODUCT_BUFFERS(F, buffers);
-    const product::Place at = product::place_of(a.tiles_i, a.tiles_j, 1, 1);
+    const product::Place at = product::place_of(tile::xcd_sequence(), a.tiles_i, a.tiles_j, 1, 1);
     if (!at.inside) return;
     const int64_t i0 = at.i * F::BM, j0 = at.j * F::BN;
     const int steps = (int)((a.features + F::BK - 1) / F::BK);
@@ -250,25 +250,32 @@ __global__ __launch_bounds__(256) void k_rows(RowArgs a) {
 }
 
 struct SlopeArgs {
-    int64_t rows, classes;
+    int64_t rows, classes, features;
     float it;
     const int64_t* tokens;
     const float *dlogprob, *dentropy;
     const Row* row;
     Slope* slope;
-    uint8_t* live;  // whether the row's gradient is not all zeros
+    const void* x;
+    uint16_t* copy;
 };
+// Slopes of the rows, and x as products read it: with zeros for the rows without a gradient, whose products by the zeros of their logits' gradients are
+// zero then, whatever they hold.
+template <bool F32>
 __global__ __launch_bounds__(256) void k_slopes(SlopeArgs a) {
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (t >= a.rows) return;
-    const Row r = a.row[t];
-    const int64_t c = a.tokens ? a.tokens[t] : -1;
-    const bool given = c >= 0 && c < a.classes && a.dlogprob;
-    const float g = given ? a.dlogprob[t] * a.it : 0.f, h = a.dentropy ? a.dentropy[t] * a.it : 0.f;
-    // p (-g - h (log p + entropy)) with p = e / sum, log p = x ln 2 - log sum
-    const bool keep = r.log_sum != -kInf && (g != 0.f || h != 0.f);
-    a.slope[t] = Slope{r.most, -r.inverse * (g + h * (r.entropy - r.log_sum)), -r.inverse * h * kLn2, g, given ? (int32_t)c : -1, keep ? 0xffffffffu : 0u, {0, 0}};
-    a.live[t] = keep;
+    const int64_t wide = product::padded(F32, a.features) / 8, n = a.rows * wide, ld = product::pitch(F32, a.features);
+    for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < n; k += (int64_t)gridDim.x * 256) {
+        const int64_t t = k / wide, col = (k - t * wide) * 8;
+        const Row r = a.row[t];
+        const int64_t c = a.tokens ? a.tokens[t] : -1;
+        const bool given = c >= 0 && c < a.classes && a.dlogprob;
+        const float g = given ? a.dlogprob[t] * a.it : 0.f, h = a.dentropy ? a.dentropy[t] * a.it : 0.f;
+        // p (-g - h (log p + entropy)) with p = e / sum, log p = x ln 2 - log sum
+        const bool keep = r.log_sum != -kInf && (g != 0.f || h != 0.f);
+        if (col == 0)
+            a.slope[t] = Slope{r.most, -r.inverse * (g + h * (r.entropy - r.log_sum)), -r.inverse * h * kLn2, g, given ? (int32_t)c : -1, keep ? 0xffffffffu : 0u, {0, 0}};
+        product::copy8<F32>(a.x, a.features, t, col, keep, a.copy + t * ld);
+    }
 }
 
 struct GradArgs {
@@ -286,7 +293,7 @@ template <class F>
 __global__ __launch_bounds__(F::kThreads) void k_grads(GradArgs a) {
     constexpr int TM = F::TM, TN = F::TN, P = F::PLANES, kHalf = F::BN / 2;
     PRODUCT_BUFFERS(F, buffers);
-    const product::Place at = product::place_of(a.tiles_i, a.tiles_j, 1, 1);
+    const product::Place at = product::place_of(tile::xcd_sequence(), a.tiles_i, a.tiles_j, 1, 1);
     if (!at.inside) return;
     const int64_t i0 = at.i * F::BM, j0 = at.j * F::BN;
     const int steps = (int)((a.features + F::BK - 1) / F::BK);
@@ -426,7 +433,6 @@ Plan plan_of(const Shape& s) {
     if (!s.inference) {
         p.rows_at = take(sizeof(Row) * (uint64_t)s.rows);
         p.slope_at = take(sizeof(Slope) * (uint64_t)s.rows);
-        p.live_at = take(s.rows);
         const int64_t fit = std::max<int64_t>(1, (int64_t)(kPieceBytes / (2ull * planes * s.rows)) / 256) * 256;
         p.pieces = (int)((s.classes + fit - 1) / fit);
         p.length = std::min<int64_t>(((s.classes + p.pieces - 1) / p.pieces + 255) / 256 * 256, s.classes);
@@ -435,8 +441,8 @@ Plan plan_of(const Shape& s) {
         p.dx = product::cut_of(s.f32, s.rows, s.features, p.length, 1, true);
         p.dw = product::cut_of(s.f32, p.length, s.features, s.rows, 1, true);
         if (!p.copies) p.copy_at[1] = take(2ull * p.length * ld);
-        p.launches_bwd = 2 + p.pieces * (2 + product::launches_of(p.dw, false)) + (product::launches_of(p.dx, p.pieces > 1) - 1);
-        p.most_tiles = std::max({p.most_tiles, p.piece.tiles(), p.dx.tiles() * p.dx.splits, p.dw.tiles() * p.dw.splits});
+        p.launches_bwd = 1 + (p.copies && p.few) + p.pieces + (p.pieces - 1) * product::launches_of(product::Cut{p.dx.side}, p.dw, false) + product::launches_of(p.dx, p.dw, p.pieces > 1);
+        p.most_tiles = std::max({p.most_tiles, p.piece.tiles(), p.dx.tiles() * p.dx.splits + p.dw.tiles() * p.dw.splits});
         p.grad_at = take(2ull * s.rows * product::pitch(s.f32, p.length));
         p.parts_dx_at = take(product::parts_bytes(p.dx, 1, p.pieces > 1));
         p.parts_dw_at = take(product::parts_bytes(p.dw, 1, false));
@@ -475,16 +481,19 @@ void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
 
 void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
     Slope* slope = reinterpret_cast<Slope*>(a.ws + p.slope_at);
-    uint8_t* live = reinterpret_cast<uint8_t*>(a.ws + p.live_at);
     uint16_t* grads = reinterpret_cast<uint16_t*>(a.ws + p.grad_at);
-    const SlopeArgs l{s.rows, s.classes, a.it, a.tokens, a.dlogprob, a.dentropy, reinterpret_cast<const Row*>(a.ws + p.rows_at), slope, live};
-    CANVAS_LAUNCH(k_slopes, dim3((unsigned)((s.rows + 255) / 256)), dim3(256), 0, stream, l);
-    // x with zeros for the rows without a gradient, and W (where it is not a copy that forward has left, piece by piece) with zeros for masked classes:
-    // products by the zeros of their gradients are zero then, whatever they hold
+    // W, where it is not a copy that forward has left, has zeros for masked classes too, whole or piece by piece
     uint16_t *cx = reinterpret_cast<uint16_t*>(a.ws + p.copy_at[0]), *cw = reinterpret_cast<uint16_t*>(a.ws + p.copy_at[1]);
-    const bool whole = p.copies && p.few;
-    const product::Copy c[2] = {{a.x, cx, s.rows, s.features, live}, {a.weight, cw, s.classes, s.features, a.mask}};
-    product::copy(s.f32, c, whole ? 2 : 1, stream);
+    const SlopeArgs l{s.rows, s.classes, s.features, a.it, a.tokens, a.dlogprob, a.dentropy, reinterpret_cast<const Row*>(a.ws + p.rows_at), slope, a.x, cx};
+    const dim3 grid((unsigned)std::min<int64_t>((s.rows * product::padded(s.f32, s.features) / 8 + 255) / 256, 4096));
+    if (s.f32)
+        CANVAS_LAUNCH(k_slopes<true>, grid, dim3(256), 0, stream, l);
+    else
+        CANVAS_LAUNCH(k_slopes<false>, grid, dim3(256), 0, stream, l);
+    if (p.copies && p.few) {
+        const product::Copy c{a.weight, cw, s.classes, s.features, a.mask};
+        product::copy(s.f32, &c, 1, stream);
+    }
     const int64_t lx = product::pitch(s.f32, s.features);
     const Factor x = factor_of(cx, s.rows, lx), all = factor_of(p.copies ? cw : static_cast<const uint16_t*>(a.weight), s.classes, lx);
     const int64_t ld = product::pitch(s.f32, p.length), wide = product::padded(s.f32, p.length);
@@ -515,18 +524,18 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
         d.parts = p.dx.splits > 1 || p.pieces > 1 ? reinterpret_cast<float*>(a.ws + p.parts_dx_at) : nullptr;
         d.first = n == 0;
         d.last = n + 1 == p.pieces;
-        product::multiply(d, stream);
-        d.a.count = length;
-        d.a_rows = false;
-        d.b = x;
-        d.b.count = s.features;
-        d.depth = s.rows;
-        d.out[0] = static_cast<char*>(a.dweight) + first * s.features * (s.f32 ? 4 : 2);
-        d.cut = p.dw;
-        d.cut.tiles_i = (length + p.dw.side - 1) / p.dw.side;
-        d.parts = p.dw.splits > 1 ? reinterpret_cast<float*>(a.ws + p.parts_dw_at) : nullptr;
-        d.first = d.last = true;
-        product::multiply(d, stream);
+        product::Product e = d;
+        e.a.count = length;
+        e.a_rows = false;
+        e.b = x;
+        e.b.count = s.features;
+        e.depth = s.rows;
+        e.out[0] = static_cast<char*>(a.dweight) + first * s.features * (s.f32 ? 4 : 2);
+        e.cut = p.dw;
+        e.cut.tiles_i = (length + p.dw.side - 1) / p.dw.side;
+        e.parts = p.dw.splits > 1 ? reinterpret_cast<float*>(a.ws + p.parts_dw_at) : nullptr;
+        e.first = e.last = true;
+        product::multiply(d, e, stream);
     }
 }
 

@@ -307,7 +307,47 @@ __device__ __forceinline__ void split(float v, uint16_t (&part)[3]) {
     part[2] = (uint16_t)(__float_as_uint(r - __uint_as_float(mid)) >> 16);
 }
 
-// This workgroup's tile: bands of kBand tiles of rows, down each column of a band, in the order of the XCDs, so that the tiles that an XCD works on at a
+// Columns col .. col + 7 of a row of a matrix, to the row of its copy (`to`): zeros behind the last column, and where the row is not kept.
+template <bool F32>
+__device__ __forceinline__ void copy8(const void* matrix, int64_t cols, int64_t row, int64_t col, bool keep, uint16_t* to) {
+    constexpr int P = F32 ? 3 : 1;
+    u32x4 w[P] = {};
+    if (keep && col < cols) {
+        const bool whole = (cols & 7) == 0;
+        if (F32) {
+            const float* x = static_cast<const float*>(matrix) + row * cols + col;
+            float v[8];
+            if (whole) {
+                const f32x4 a = reinterpret_cast<const f32x4*>(x)[0], b = reinterpret_cast<const f32x4*>(x)[1];
+#pragma unroll
+                for (int e = 0; e < 4; e++) v[e] = a[e], v[4 + e] = b[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e++) v[e] = col + e < cols ? x[e] : 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                uint16_t lo[3], hi[3];
+                split(v[2 * e], lo);
+                split(v[2 * e + 1], hi);
+#pragma unroll
+                for (int h = 0; h < P; h++) w[h][e] = lo[h] | (uint32_t)hi[h] << 16;
+            }
+        } else {
+            const uint16_t* x = static_cast<const uint16_t*>(matrix) + row * cols + col;
+            if (whole) {
+                w[0] = *reinterpret_cast<const u32x4*>(x);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; e++) w[0][e] = (col + 2 * e < cols ? x[2 * e] : 0) | (uint32_t)(col + 2 * e + 1 < cols ? x[2 * e + 1] : 0) << 16;
+            }
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < P; h++) *reinterpret_cast<u32x4*>(to + column<P>(col, h)) = w[h];
+}
+
+// Tile t of a launch's order: bands of kBand tiles of rows, down each column of a band, in the order of the XCDs, so that the tiles that an XCD works on at a
 // time share their operands in its L2.
 constexpr int kBand = 8;
 struct Place {
@@ -315,8 +355,7 @@ struct Place {
     int which, split;
     bool inside;
 };
-__device__ __forceinline__ Place place_of(int64_t tiles_i, int64_t tiles_j, int splits, int results) {
-    int64_t t = tile::xcd_sequence();
+__device__ __forceinline__ Place place_of(int64_t t, int64_t tiles_i, int64_t tiles_j, int splits, int results) {
     const int64_t tiles = tiles_i * tiles_j;
     Place p;
     p.inside = t < tiles * splits * results;

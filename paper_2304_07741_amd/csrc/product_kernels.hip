@@ -71,10 +71,9 @@ __device__ __forceinline__ void emit(const Task& g, int which, int64_t i0, int64
 }
 
 template <class F, Side SA>
-__global__ __launch_bounds__(F::kThreads) void k_product(Task g) {
+__device__ __forceinline__ void run(const Task& g, int64_t number, const Buffers<F>& buffers) {
     constexpr int TM = F::TM, TN = F::TN, BM = F::BM, BN = F::BN;
-    PRODUCT_BUFFERS(F, buffers);
-    const Place at = place_of(g.tiles_i, g.tiles_j, g.splits, g.results);
+    const Place at = place_of(number, g.tiles_i, g.tiles_j, g.splits, g.results);
     if (!at.inside) return;
     const int64_t i0 = at.i * BM, j0 = at.j * BN;
     const int per = (int)((g.depth + F::BK - 1) / F::BK), all = per * g.segments;
@@ -116,13 +115,30 @@ __global__ __launch_bounds__(F::kThreads) void k_product(Task g) {
     }
 }
 
+// Two products in one launch, the first with rows of the summed index along it.  (Neither waits for the other, and small ones do not fill the chip.)
+template <class F>
+__global__ __launch_bounds__(F::kThreads) void k_products(Task first, Task second, int64_t firsts) {
+    PRODUCT_BUFFERS(F, buffers);
+    // each XCD takes its eighth of the first product's tiles, then its share of the second's (they may take twice as long as the others)
+    const unsigned total = gridDim.x * gridDim.y, lin = blockIdx.y * gridDim.x + blockIdx.x, xcd = lin & 7u, n = (unsigned)firsts;
+    auto before = [&](unsigned all) { return xcd * (all >> 3) + (xcd < (all & 7u) ? xcd : (all & 7u)); };
+    const unsigned mine = (n >> 3) + (xcd < (n & 7u)), at = lin >> 3;
+    if (at < mine)
+        run<F, kRows>(first, before(n) + at, buffers);
+    else
+        run<F, kCols>(second, before(total) - before(n) + at - mine, buffers);
+}
+template <class F, Side SA>
+__global__ __launch_bounds__(F::kThreads) void k_product(Task g) {
+    PRODUCT_BUFFERS(F, buffers);
+    run<F, SA>(g, tile::xcd_sequence(), buffers);
+}
+
 // Adds the parts of 32 x 32 results, each of four waves every fourth part, and finishes them.
 template <class F>
-__global__ __launch_bounds__(256) void k_join(Task g) {
+__device__ __forceinline__ void join(const Task& g, int64_t number, f32x4 (&sums)[4][4][64], float* img) {
     constexpr int kBlocks = F::BM / 32 * (F::BN / 32), kEach = F::BM * F::BN / 4;
-    __shared__ f32x4 sums[4][4][64];
-    __shared__ __align__(16) float img[32 * 32];
-    const int64_t number = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, tile = number / kBlocks, tiles = g.tiles_i * g.tiles_j;
+    const int64_t tile = number / kBlocks, tiles = g.tiles_i * g.tiles_j;
     if (tile >= tiles * g.results) return;
     const int block = (int)(number - tile * kBlocks), bi = block / (F::BN / 32), bj = block - bi * (F::BN / 32);
     const int which = (int)(tile / tiles);
@@ -147,74 +163,38 @@ __global__ __launch_bounds__(256) void k_join(Task g) {
     __syncthreads();
     emit<F::PLANES == 3, 32, 32, 256>(g, which, i0, j0, img);
 }
+template <class F>
+__global__ __launch_bounds__(256) void k_join(Task first, Task second, int64_t firsts) {
+    __shared__ f32x4 sums[4][4][64];
+    __shared__ __align__(16) float img[32 * 32];
+    const int64_t number = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (number < firsts)
+        join<F>(first, number, sums, img);
+    else
+        join<F>(second, number - firsts, sums, img);
+}
 
 struct Copies {
     Copy c[3];
 };
-// Eight columns per thread and turn; zeros behind the last one.
+// Eight columns per thread and turn.
 template <bool F32>
 __global__ __launch_bounds__(256) void k_copy(Copies all) {
     const Copy& c = all.c[blockIdx.y];
-    constexpr int P = F32 ? 3 : 1;
     const int64_t wide = padded(F32, c.cols) / 8, n = c.rows * wide, ld = pitch(F32, c.cols);
-    const bool whole = (c.cols & 7) == 0;
     for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < n; k += (int64_t)gridDim.x * 256) {
-        const int64_t row = k / wide, col = (k - row * wide) * 8, from = row * c.cols + col;
-        uint16_t* to = c.to + row * ld;
-        if (col >= c.cols || (c.live && !c.live[row])) {
-#pragma unroll
-            for (int h = 0; h < P; h++) *reinterpret_cast<u32x4*>(to + column<P>(col, h)) = u32x4{};
-            continue;
-        }
-        if (F32) {
-            const float* x = static_cast<const float*>(c.from) + from;
-            float v[8];
-            if (whole) {
-                const f32x4 a = reinterpret_cast<const f32x4*>(x)[0], b = reinterpret_cast<const f32x4*>(x)[1];
-#pragma unroll
-                for (int e = 0; e < 4; e++) v[e] = a[e], v[4 + e] = b[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; e++) v[e] = col + e < c.cols ? x[e] : 0.f;
-            }
-            u32x4 w[3];
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                uint16_t lo[3], hi[3];
-                split(v[2 * e], lo);
-                split(v[2 * e + 1], hi);
-#pragma unroll
-                for (int h = 0; h < 3; h++) w[h][e] = lo[h] | (uint32_t)hi[h] << 16;
-            }
-#pragma unroll
-            for (int h = 0; h < 3; h++) *reinterpret_cast<u32x4*>(to + column<P>(col, h)) = w[h];
-        } else {
-            const uint16_t* x = static_cast<const uint16_t*>(c.from) + from;
-            u32x4 w;
-            if (whole) {
-                w = *reinterpret_cast<const u32x4*>(x);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; e++) w[e] = (col + 2 * e < c.cols ? x[2 * e] : 0) | (uint32_t)(col + 2 * e + 1 < c.cols ? x[2 * e + 1] : 0) << 16;
-            }
-            *reinterpret_cast<u32x4*>(to + col) = w;
-        }
+        const int64_t row = k / wide, col = (k - row * wide) * 8;
+        copy8<F32>(c.from, c.cols, row, col, !c.live || c.live[row], c.to + row * ld);
     }
 }
 
-template <class F, Side SA>
-void launch(const Product& p, const Task& t, hipStream_t stream) {
-    const dim3 grid = rows_of_workgroups(p.cut.tiles() * p.cut.splits * p.results, F::kThreads);
-    CANVAS_LAUNCH((k_product<F, SA>), grid, dim3(F::kThreads), 0, stream, t);
-    if (p.parts && p.last) CANVAS_LAUNCH((k_join<F>), rows_of_workgroups(p.cut.tiles() * p.results * (F::BM / 32 * (F::BN / 32)), 256), dim3(256), 0, stream, t);
+Task task_of(const Product& p) {
+    return Task{p.a, p.b, p.depth, p.cut.tiles_i, p.cut.tiles_j, p.ld, p.segments, p.results, p.cut.splits, {p.out[0], p.out[1]}, reinterpret_cast<f32x4*>(p.parts), p.first};
 }
+int64_t workgroups(const Product& p) { return p.cut.tiles() * p.cut.splits * p.results; }
+// Of the launch that adds the parts of a product; none if it leaves none, or others add to them.
 template <class F>
-void launch_form(const Product& p, const Task& t, hipStream_t stream) {
-    if (p.a_rows)
-        launch<F, kRows>(p, t, stream);
-    else
-        launch<F, kCols>(p, t, stream);
-}
+int64_t joins(const Product& p) { return p.parts && p.last ? p.cut.tiles() * p.results * (F::BM / 32 * (F::BN / 32)) : 0; }
 
 }  // namespace
 
@@ -267,11 +247,37 @@ Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, boo
 uint64_t parts_bytes(const Cut& c, int results, bool several) {
     return c.splits > 1 || several ? 4ull * c.side * c.side * c.tiles() * c.splits * results : 0;
 }
-int launches_of(const Cut& c, bool several) { return 1 + (c.splits > 1 || several); }
+bool together(const Product& x, const Product& y) { return x.cut.side == y.cut.side && x.a_rows && !y.a_rows; }
+int launches_of(const Cut& x, const Cut& y, bool several) {
+    const bool jx = x.splits > 1 || several, jy = y.splits > 1;
+    return x.side == y.side ? 1 + (jx || jy) : 2 + jx + jy;
+}
 
 void multiply(const Product& p, hipStream_t stream) {
-    const Task t{p.a, p.b, p.depth, p.cut.tiles_i, p.cut.tiles_j, p.ld, p.segments, p.results, p.cut.splits, {p.out[0], p.out[1]}, reinterpret_cast<f32x4*>(p.parts), p.first};
-    with_form(p.f32, p.cut.side, [&](auto form) { launch_form<decltype(form)>(p, t, stream); });
+    with_form(p.f32, p.cut.side, [&](auto form) {
+        using F = decltype(form);
+        const Task t = task_of(p);
+        const dim3 grid = rows_of_workgroups(workgroups(p), F::kThreads);
+        if (p.a_rows)
+            CANVAS_LAUNCH((k_product<F, kRows>), grid, dim3(F::kThreads), 0, stream, t);
+        else
+            CANVAS_LAUNCH((k_product<F, kCols>), grid, dim3(F::kThreads), 0, stream, t);
+        if (const int64_t n = joins<F>(p)) CANVAS_LAUNCH((k_join<F>), rows_of_workgroups(n, 256), dim3(256), 0, stream, t, t, n);
+    });
+}
+void multiply(const Product& x, const Product& y, hipStream_t stream) {
+    if (!together(x, y)) {
+        multiply(x, stream);
+        multiply(y, stream);
+        return;
+    }
+    with_form(x.f32, x.cut.side, [&](auto form) {
+        using F = decltype(form);
+        const Task t = task_of(x), u = task_of(y);
+        CANVAS_LAUNCH((k_products<F>), rows_of_workgroups(workgroups(x) + workgroups(y), F::kThreads), dim3(F::kThreads), 0, stream, t, u, workgroups(x));
+        const int64_t nx = joins<F>(x), ny = joins<F>(y);
+        if (nx + ny) CANVAS_LAUNCH((k_join<F>), rows_of_workgroups(nx + ny, 256), dim3(256), 0, stream, t, u, nx);
+    });
 }
 
 void copy(bool f32, const Copy* copies, int n, hipStream_t stream) {

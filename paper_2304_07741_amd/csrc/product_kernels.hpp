@@ -44,12 +44,13 @@ struct Product {
     bool first = true, last = true;
 };
 
-// `steps`: of the whole sum, each as deep as a tile takes at once.
 Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, bool may_split);
 uint64_t parts_bytes(const Cut& c, int results, bool several);
-// Launches of multiply(), the sum's end among them.
-int launches_of(const Cut& c, bool several);
+// One product, or two that do not wait for each other, the first with a_rows.
 void multiply(const Product& p, hipStream_t stream);
+void multiply(const Product& x, const Product& y, hipStream_t stream);
+// Launches of the latter; `several`: more than one adds to x.
+int launches_of(const Cut& x, const Cut& y, bool several);
 
 // A matrix of `rows` x `cols` elements laid out as a Factor.
 // `live`: bytes by row, 0 for rows that are zeros in the copy whatever they hold.
