@@ -518,7 +518,8 @@ def canvas_clip_query(handle):
 
 def canvas_clip_step(handle, grads, outs, max_norm, norm, scale, workspace):
     """grads, outs: lists of tensors (outs None: the norm alone), as many as the plan has."""
-    _check(load().canvas_clip_step(handle, _ptrs(grads), None if outs is None else _ptrs(outs), float(max_norm), _ptr(norm), _ptr(scale), _ptr(workspace),
+    addresses = lambda tensors: (ctypes.c_void_p * max(1, len(tensors)))(*[t.data_ptr() for t in tensors])  # noqa: E731
+    _check(load().canvas_clip_step(handle, addresses(grads), None if outs is None else addresses(outs), float(max_norm), _ptr(norm), _ptr(scale), _ptr(workspace),
                                    _bytes(workspace), _stream()))
 
 

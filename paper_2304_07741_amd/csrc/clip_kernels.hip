@@ -17,7 +17,8 @@ namespace {
 
 using tile::u32x4;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-constexpr int kThreads = 256, kMostParts = 1024;
+constexpr int kThreads = 256, kMostParts = 2048;
+constexpr int64_t kAloneElements = 1 << 14;  // up to which one workgroup does all of it
 
 struct Item {
     const void* in;
@@ -141,10 +142,16 @@ __global__ __launch_bounds__(kThreads) void k_norm(const double* parts, int n, d
     if (scale) *scale = (float)scale_of(t, most);
 }
 
+// (a scale below fp32's smallest normal number: products in 64 bits)
+struct Scaling {
+    double scale;
+    float s;
+    __device__ __forceinline__ explicit Scaling(double v) : scale(v), s((float)v) {}
+    __device__ __forceinline__ float of(float v) const { return s >= 1.2e-38f || !(scale > 0) ? v * s : (float)(v * scale); }
+};
 template <class T, class O>
 __device__ __forceinline__ void scaled(const T* p, O* to, int n, double scale) {
-    const float s = (float)scale;
-    auto of = [&](float v) { return s >= 1.2e-38f || !(scale > 0) ? v * s : (float)(v * scale); };
+    const Scaling by(scale);
     if (n == kChunk && aligned(p) && aligned(to)) {
         float v[kTurns][8];
 #pragma unroll
@@ -152,7 +159,7 @@ __device__ __forceinline__ void scaled(const T* p, O* to, int n, double scale) {
 #pragma unroll
         for (int k = 0; k < kTurns; k++) {
 #pragma unroll
-            for (int e = 0; e < 8; e++) v[k][e] = of(v[k][e]);
+            for (int e = 0; e < 8; e++) v[k][e] = by.of(v[k][e]);
             store8(to + (k * kThreads + threadIdx.x) * 8, v[k]);
         }
         return;
@@ -164,11 +171,11 @@ __device__ __forceinline__ void scaled(const T* p, O* to, int n, double scale) {
             float v[8];
             load8(p + i, v);
 #pragma unroll
-            for (int e = 0; e < 8; e++) v[e] = of(v[e]);
+            for (int e = 0; e < 8; e++) v[e] = by.of(v[e]);
             store8(to + i, v);
         }
     }
-    for (int i = done + threadIdx.x; i < n; i += kThreads) store1(to + i, of(load1(p + i)));
+    for (int i = done + threadIdx.x; i < n; i += kThreads) store1(to + i, by.of(load1(p + i)));
 }
 
 // kept: the norm where a launch of its own has left it; else the parts are added here, and workgroup 0 of the first launch writes the results.
@@ -200,6 +207,44 @@ __global__ __launch_bounds__(kThreads) void k_scale(Items a, const double* parts
     }
 }
 
+// Few elements: one workgroup does all of it, a chunk at a time.
+constexpr int kAlone = 1024;
+__global__ __launch_bounds__(kAlone) void k_alone(Items a, double most, float* norm, float* scale) {
+    __shared__ double buf[kAlone / 64];
+    double t = 0;
+    for (int k = 0; k < a.n; k++) {
+        const Item& item = a.item[k];
+        for (int64_t i = threadIdx.x; i < item.count; i += kAlone) {
+            const double v = item.bf16 ? load1(static_cast<const uint16_t*>(item.in) + i) : load1(static_cast<const float*>(item.in) + i);
+            t = fma(v, v, t);
+        }
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) t += __shfl_xor(t, o);
+    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = t;
+    __syncthreads();
+    t = 0;
+#pragma unroll
+    for (int w = 0; w < kAlone / 64; w++) t += buf[w];
+    const double all = sqrt(t), s = scale_of(all, most);
+    if (threadIdx.x == 0) {
+        *norm = (float)all;
+        if (scale) *scale = (float)s;
+    }
+    const Scaling by(s);
+    for (int k = 0; k < a.n; k++) {
+        const Item& item = a.item[k];
+        if (s == 1.0 && item.in == item.out) continue;
+        for (int64_t i = threadIdx.x; i < item.count; i += kAlone) {
+            const float v = by.of(item.bf16 ? load1(static_cast<const uint16_t*>(item.in) + i) : load1(static_cast<const float*>(item.in) + i));
+            if (item.out_bf16)
+                store1(static_cast<uint16_t*>(item.out) + i, v);
+            else
+                store1(static_cast<float*>(item.out) + i, v);
+        }
+    }
+}
+
 }  // namespace
 
 void make_plan(Plan& p) {
@@ -217,6 +262,9 @@ void make_plan(Plan& p) {
         b.chunks += chunks;
     }
     close();
+    int64_t all = 0;
+    for (const Tensor& t : p.tensors) all += t.count;
+    p.one = p.batches.size() == 1 && all <= kAloneElements;
     const int most = std::max<int>(64, kMostParts / (int)std::max<size_t>(1, p.batches.size()));
     for (Batch& c : p.batches) {
         c.parts = (int)std::min<int64_t>(c.chunks, most);
@@ -225,7 +273,7 @@ void make_plan(Plan& p) {
     }
     p.alone = p.parts > kMostParts || p.batches.empty();
     const int n = (int)p.batches.size();
-    p.launches = 2 * n + p.alone;
+    p.launches = p.one ? 1 : 2 * n + p.alone;
     p.launches_norm = n + 1;
     p.workspace_bytes = 8ull * (p.parts + 1);
     p.workspace_bytes = (p.workspace_bytes + 255) & ~(uint64_t)255;
@@ -241,6 +289,10 @@ void step(const Plan& p, const Args& a, hipStream_t stream) {
         }
         return t;
     };
+    if (p.one && a.outs) {
+        CANVAS_LAUNCH(k_alone, dim3(1), dim3(kAlone), 0, stream, items(p.batches[0]), a.most, a.norm, a.scale);
+        return;
+    }
     for (const Batch& b : p.batches) CANVAS_LAUNCH(k_squares, dim3(b.parts), dim3(kThreads), 0, stream, items(b), parts + b.first_part);
     const bool alone = p.alone || !a.outs;
     if (alone) CANVAS_LAUNCH(k_norm, dim3(1), dim3(kThreads), 0, stream, parts, p.parts, a.most, kept, a.norm, a.scale);

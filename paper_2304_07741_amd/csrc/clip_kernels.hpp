@@ -15,7 +15,7 @@ struct Tensor {
 
 // Tensors are handed to a launch as its arguments, up to kBatch of those that have elements at a time.
 constexpr int kBatch = 96;
-constexpr int kChunk = 8192;  // elements that a workgroup takes at a time
+constexpr int kChunk = 16384;  // elements that a workgroup takes at a time
 struct Batch {
     std::vector<int> tensors;
     int64_t chunks = 0;
@@ -26,6 +26,7 @@ struct Plan {
     std::vector<Tensor> tensors;
     std::vector<Batch> batches;
     int parts = 0;
+    bool one = false;        // few elements: one workgroup, one launch
     bool alone = false;      // the parts are added by a launch of their own, not by every workgroup that scales
     uint64_t workspace_bytes = 0;
     int launches = 0, launches_norm = 0;

@@ -439,9 +439,10 @@ class ClipRunner(_PlanRunner):
         if len(grads) != len(self.shapes):
             raise ValueError(f"grads: {len(self.shapes)} tensors are needed, got {len(grads)}")
         for i, (t, s, d) in enumerate(zip(grads, self.shapes, self.dtypes)):
-            _check_tensor(f"grads[{i}]", t, s, d, self.device)
+            if t is None or t.shape != s or t.dtype is not d or t.device != self.device or not t.is_contiguous():
+                _check_tensor(f"grads[{i}]", t, s, d, self.device)
         if in_place:
-            outs = list(grads)
+            outs = grads
         else:
             if self.outs is None:
                 self.outs = [self._empty(s, d) for s, d in zip(self.shapes, self.out_dtypes)]
