@@ -28,6 +28,7 @@ struct Plan {
     int parts = 0;
     bool one = false;        // few elements: one workgroup, one launch
     bool alone = false;      // the parts are added by a launch of their own, not by every workgroup that scales
+    bool past = false;       // what is written goes past the last-level cache
     uint64_t workspace_bytes = 0;
     int launches = 0, launches_norm = 0;
 };
