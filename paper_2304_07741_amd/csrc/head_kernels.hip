@@ -30,20 +30,33 @@ using tile::u32x4;
 
 constexpr float kInf = __builtin_inff(), kLowest = -3.402823466e38f;
 
-// z - z_max of one logit, in powers of two: (logit - most) * scale.  The largest number in the place of a temperature that log2(e) takes past it.
-__device__ __forceinline__ float scale_of(float it) { return fminf(it * kLog2e, 3.402823466e38f); }
+// e^x of one logit's x = (logit - most) * it, at most 0, and x itself in the unit that the exponential is taken in, not below -300 of it (NaN stays in the
+// former).  bf16 plans: powers of two by one multiplication, whose argument is rounded by up to 2^-24 of itself; fp32 plans to about a unit of the last place.
+template <bool F32>
+struct Exp {
+    float scale;
+    // (the largest number in the place of a temperature that log2(e) takes past it)
+    __device__ __forceinline__ explicit Exp(float it) : scale(F32 ? it : fminf(it * kLog2e, 3.402823466e38f)) {}
+    __device__ __forceinline__ float of(float logit, float most, float& x) const {
+        const float d = (logit - most) * scale;
+        x = fmaxf(d, -300.f);
+        return F32 ? exp_finite(d < -300.f ? -300.f : d) : __builtin_amdgcn_exp2f(d);
+    }
+    static constexpr float kUnit = F32 ? 1.f : kLn2;
+};
 
-// The sums of some logits of one row: e = exp(z - z_most) added up, and e (z - z_most) in powers of two.
+// The sums of some logits of one row, x = (logit - most) * it: e^x added up, and e^x x.
 struct Sums {
     float most, s, t;
 };
-__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float scale) {
+__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float it) {
+    const Exp<true> power(it);
     Sums r;
     r.most = fmaxf(a.most, b.most);
-    const float da = (a.most - r.most) * scale, db = (b.most - r.most) * scale, ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
+    float xa, xb;
+    const float ea = power.of(a.most, r.most, xa), eb = power.of(b.most, r.most, xb);
     r.s = fmaf(a.s, ea, b.s * eb);
-    // (a part so far below that its exponential is zero counts nothing, however far it is)
-    r.t = fmaf(ea, fmaf(a.s, fmaxf(da, -300.f), a.t), eb * fmaf(b.s, fmaxf(db, -300.f), b.t));
+    r.t = fmaf(ea, fmaf(a.s, xa, a.t), eb * fmaf(b.s, xb, b.t));
     return r;
 }
 template <int O>
@@ -69,8 +82,9 @@ struct FwdArgs {
 };
 
 // N logits of one row of x in a lane, the sums of those and of what the lanes LOW, 2 LOW, .. 32 apart hold.
-template <int N, int LOW>
-__device__ __forceinline__ Sums sums_of(const float (&z)[N], float scale) {
+template <int N, int LOW, bool F32>
+__device__ __forceinline__ Sums sums_of(const float (&z)[N], float it) {
+    const Exp<F32> power(it);
     Sums r{kLowest, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < N; k++) r.most = fmaxf(r.most, z[k]);
@@ -78,10 +92,12 @@ __device__ __forceinline__ Sums sums_of(const float (&z)[N], float scale) {
     r.most = fmaxf(r.most, from_lane<32>(r.most));
 #pragma unroll
     for (int k = 0; k < N; k++) {
-        const float d = (z[k] - r.most) * scale, e = __builtin_amdgcn_exp2f(d);  // (NaN and +inf make both sums NaN)
+        float x;
+        const float e = power.of(z[k], r.most, x);  // (NaN and +inf make both sums NaN)
         r.s += e;
-        r.t = fmaf(e, fmaxf(d, -300.f), r.t);
+        r.t = fmaf(e, x, r.t);
     }
+    r.t *= power.kUnit;
     if (LOW <= 16) {
         r.s += from_lane<16>(r.s);
         r.t += from_lane<16>(r.t);
@@ -101,7 +117,6 @@ __global__ __launch_bounds__(F::kThreads) void k_logits(FwdArgs a) {
     const int steps = (int)((a.features + F::BK - 1) / F::BK);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t c0 = i0 + wave / F::WJ * (TM * 32) + (lane >> 5) * 4, t0 = j0 + wave % F::WJ * (TN * 32) + (lane & 31);
-    const float scale = scale_of(a.it);
     int token[TN];  // the row's token among this lane's classes, -1 if it is not
 #pragma unroll
     for (int y = 0; y < TN; y++) {
@@ -143,7 +158,7 @@ __global__ __launch_bounds__(F::kThreads) void k_logits(FwdArgs a) {
         for (int x = 0; x < TM; x++)
 #pragma unroll
             for (int k = 0; k < 16; k++) z[x * 16 + k] = acc[x][y][k];
-        const Sums r = sums_of<TM * 16, 32>(z, scale);
+        const Sums r = sums_of<TM * 16, 32, F::PLANES == 3>(z, a.it);
         if (lane < 32 && t < a.rows) a.sums[(at.i * F::WI + wave / F::WJ) * a.rows + t] = r;
     }
 }
@@ -192,7 +207,7 @@ __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
         for (int k = 0; k < R * 4; k++)
             if (c == (k >> 2) * 16 + (k & 3)) a.token[t] = z[k];
     }
-    const Sums r = sums_of<R * 4, 16>(z, scale_of(a.it));
+    const Sums r = sums_of<R * 4, 16, sizeof(T) == 4>(z, a.it);
     if (lane < 16 && t < a.rows) a.sums[blockIdx.x * a.rows + t] = r;
 }
 
@@ -212,7 +227,6 @@ __global__ __launch_bounds__(256) void k_rows(RowArgs a) {
     __shared__ Sums part[256];
     const int mine = threadIdx.x & (a.across - 1), turn = threadIdx.x / a.across, turns = 256 / a.across;
     const int64_t t = (int64_t)blockIdx.x * a.across + mine;
-    const float scale = scale_of(a.it);
     Sums r{kLowest, 0.f, 0.f};
     if (t < a.rows) {
         constexpr int kAhead = 4;
@@ -221,19 +235,19 @@ __global__ __launch_bounds__(256) void k_rows(RowArgs a) {
 #pragma unroll
             for (int u = 0; u < kAhead; u++) s[u] = k + u * turns < a.segments ? a.sums[(int64_t)(k + u * turns) * a.rows + t] : Sums{kLowest, 0.f, 0.f};
 #pragma unroll
-            for (int u = 0; u < kAhead; u++) r = join(r, s[u], scale);
+            for (int u = 0; u < kAhead; u++) r = join(r, s[u], a.it);
         }
     }
     part[threadIdx.x] = r;
     __syncthreads();
     for (int o = turns / 2; o; o >>= 1) {
-        if (turn < o) part[threadIdx.x] = join(part[threadIdx.x], part[threadIdx.x + o * a.across], scale);
+        if (turn < o) part[threadIdx.x] = join(part[threadIdx.x], part[threadIdx.x + o * a.across], a.it);
         __syncthreads();
     }
     if (turn || t >= a.rows) return;
     r = part[threadIdx.x];
     const bool empty = r.s == 0.f;  // (the largest of what is left counts one)
-    const float log_sum = empty ? -kInf : logf(r.s), entropy = empty ? 0.f : log_sum - r.t / r.s * kLn2;
+    const float log_sum = empty ? -kInf : logf(r.s), entropy = empty ? 0.f : log_sum - r.t / r.s;
     if (a.entropy) a.entropy[t] = entropy;
     if (a.logprob) {
         const int64_t c = a.tokens[t];
@@ -270,10 +284,10 @@ __global__ __launch_bounds__(256) void k_slopes(SlopeArgs a) {
         const int64_t c = a.tokens ? a.tokens[t] : -1;
         const bool given = c >= 0 && c < a.classes && a.dlogprob;
         const float g = given ? a.dlogprob[t] * a.it : 0.f, h = a.dentropy ? a.dentropy[t] * a.it : 0.f;
-        // p (-g - h (log p + entropy)) with p = e / sum, log p = x ln 2 - log sum
+        // p (-g - h (log p + entropy)) with p = e^x / sum, log p = x - log sum
         const bool keep = r.log_sum != -kInf && (g != 0.f || h != 0.f);
         if (col == 0)
-            a.slope[t] = Slope{r.most, -r.inverse * (g + h * (r.entropy - r.log_sum)), -r.inverse * h * kLn2, g, given ? (int32_t)c : -1, keep ? 0xffffffffu : 0u, {0, 0}};
+            a.slope[t] = Slope{r.most, -r.inverse * (g + h * (r.entropy - r.log_sum)), -r.inverse * h * Exp<F32>::kUnit, g, given ? (int32_t)c : -1, keep ? 0xffffffffu : 0u, {0, 0}};
         product::copy8<F32>(a.x, a.features, t, col, keep, a.copy + t * ld);
     }
 }
@@ -300,7 +314,7 @@ __global__ __launch_bounds__(F::kThreads) void k_grads(GradArgs a) {
     f32x16 acc[TM][TN] = {};
     product::accumulate<F, product::kRows, product::kRows, false>(a.w, a.x, 0, i0, j0, a.features, 0, steps, steps, 1, buffers, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / F::WJ * (TM * 32) + (lane >> 5) * 4, wj = wave % F::WJ * (TN * 32) + (lane & 31);
-    const float scale = scale_of(a.it);
+    const Exp<P == 3> power(a.it);
 #pragma unroll
     for (int y = 0; y < TN; y++) {
         const int64_t t = j0 + wj + y * 32;
@@ -313,8 +327,9 @@ __global__ __launch_bounds__(F::kThreads) void k_grads(GradArgs a) {
         for (int x = 0; x < TM; x++)
 #pragma unroll
             for (int k = 0; k < 16; k++) {
-                const float d = (acc[x][y][k] - s.most) * scale, e = __builtin_amdgcn_exp2f(d);
-                acc[x][y][k] = e * fmaf(s.second, fmaxf(d, -300.f), s.first);
+                float d;
+                const float e = power.of(acc[x][y][k], s.most, d);
+                acc[x][y][k] = e * fmaf(s.second, d, s.first);
             }
         if (__any(here >= 0)) {
 #pragma unroll

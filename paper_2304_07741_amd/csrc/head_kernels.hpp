@@ -19,7 +19,7 @@ struct Shape {
 struct alignas(16) Row {
     float most, log_sum, entropy, inverse;
 };
-// The gradient of a row's logits: exp(z_i - z_max) (first + second (z_i - z_max) / ln 2), and `token` more at the token.
+// The gradient of a row's logits: e^x (first + second x) with x = z_i - z_max (in fp32 plans; in powers of two in bf16 ones), and `token` more at the token.
 struct alignas(16) Slope {
     float most, first, second, token;
     int32_t at;        // the token, -1 if there is none
