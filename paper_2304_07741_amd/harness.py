@@ -142,6 +142,13 @@ def _check_tensor(name, t, shape, dtype, device):
         raise ValueError(f"{name}: a contiguous {shape} tensor of {dtype} on {device} is needed, got {got}")
 
 
+def _check_last(passed, given):
+    """backward() reads what the last forward() has left in the workspace: it takes the same arguments (tensors: the same memory, which the runner keeps alive)."""
+    same = lambda a, b: a.data_ptr() == b.data_ptr() if torch.is_tensor(a) and torch.is_tensor(b) else a is b or (not torch.is_tensor(a) and a == b)  # noqa: E731
+    if passed is None or not all(same(a, b) for a, b in zip(passed, given)):
+        raise ValueError("not the arguments of this runner's last forward()")
+
+
 class _PlanRunner:
     """One compiled plan, its workspace and the buffers it writes; close() releases the plan."""
 
@@ -336,11 +343,12 @@ class OrthoRunner(_PlanRunner):
 class GatedRunner(_PlanRunner):
     """A gated pair of FCs (include/canvas_gated.h): y = act(x w_gate^T) (x w_up^T); x [rows, features], weights [width, features].
 
-    forward() and backward() return the runner's own buffers, which the next call overwrites; backward() is of the last forward(), with the
-    same x and weights.
+    forward() and backward() return the runner's own buffers, which the next call overwrites; backward() is of the last forward(), whose
+    tensors it is given again.
     """
 
     _destroy = staticmethod(B.canvas_gated_destroy)
+    passed = None
 
     def __init__(self, rows, features, width, dtype, act=B.CANVAS_GATED_SILU, flags=0, device="cuda:0"):
         self._open(dtype, device)
@@ -361,10 +369,12 @@ class GatedRunner(_PlanRunner):
     def forward(self, x, w_gate, w_up):
         self._arguments(x, w_gate, w_up)
         B.canvas_gated_forward(self.handle, x, w_gate, w_up, self.out["y"], self.ws)
+        self.passed = (x, w_gate, w_up)
         return self.out
 
     def backward(self, x, w_gate, w_up, dy):
         self._arguments(x, w_gate, w_up)
+        _check_last(self.passed, (x, w_gate, w_up))
         _check_tensor("dy", dy, self.out["y"].shape, self.tdtype, self.device)
         g = self.grads
         B.canvas_gated_backward(self.handle, x, w_gate, w_up, dy, g.get("dx"), g.get("dw_gate"), g.get("dw_up"), self.ws)
@@ -375,11 +385,12 @@ class HeadRunner(_PlanRunner):
     """Log probabilities of tokens with entropy from features and the head's weight (include/canvas_head.h), and the gradients of both.
 
     x [rows, features], weight [classes, features]; mask: [classes] bytes or truth values, zero where a class is not allowed.
-    forward() and backward() return the runner's own buffers, which the next call overwrites; backward() is of the last forward(), with the
-    same x, weight, mask and temperature.
+    forward() and backward() return the runner's own buffers, which the next call overwrites; backward() is of the last forward(), whose
+    x, weight, mask and temperature it is given again.
     """
 
     _destroy = staticmethod(B.canvas_head_destroy)
+    passed = None
 
     def __init__(self, rows, features, classes, dtype, flags=0, device="cuda:0"):
         self._open(dtype, device)
@@ -401,10 +412,12 @@ class HeadRunner(_PlanRunner):
     def forward(self, x, weight, tokens, mask=None, inv_temperature=1.0):
         self._arguments(x, weight, tokens, mask)
         B.canvas_head_forward(self.handle, x, weight, inv_temperature, mask, tokens, self.out["logprob"], self.out["entropy"], self.ws)
+        self.passed = (x, weight, mask, inv_temperature)
         return self.out
 
     def backward(self, x, weight, tokens, dlogprob=None, dentropy=None, mask=None, inv_temperature=1.0):
         self._arguments(x, weight, tokens, mask)
+        _check_last(self.passed, (x, weight, mask, inv_temperature))
         for name, t in (("dlogprob", dlogprob), ("dentropy", dentropy)):
             if t is not None:
                 _check_tensor(name, t, (self.rows,), torch.float32, self.device)
