@@ -45,7 +45,7 @@ def test_every_declared_symbol_is_exported(lib, header, names):
 def test_gated_compile_and_query(lib):
     h = B.canvas_gated_compile(100, 64, 256, B.CANVAS_BF16, B.CANVAS_GATED_GELU)
     info = B.canvas_gated_query(h)
-    assert info.n_launches_fwd >= 1 and info.n_launches_bwd >= 3 and info.workspace_bytes >= 8 * 100 * 256
+    assert info.n_launches_fwd >= 1 and info.n_launches_bwd >= 2 and info.workspace_bytes >= 4 * 100 * 256
     assert info.flops_fwd == 4.0 * 100 * 64 * 256 and info.flops_bwd == 2 * info.flops_fwd
     assert info.min_bytes_fwd == 2.0 * (100 * 64 + 2 * 64 * 256 + 100 * 256)
     B.canvas_gated_destroy(h)
@@ -94,7 +94,7 @@ def test_gated_calls_refuse(lib):
 def test_head_compile_and_query(lib):
     h = B.canvas_head_compile(1000, 64, 5000, B.CANVAS_BF16)
     info = B.canvas_head_query(h)
-    assert info.n_launches_fwd >= 2 and info.n_launches_bwd >= 4 and info.pieces >= 1
+    assert info.n_launches_fwd >= 2 and info.n_launches_bwd >= 3 and info.pieces >= 1
     assert info.flops_fwd == 2.0 * 1000 * 64 * 5000 and info.flops_bwd == 3 * info.flops_fwd
     B.canvas_head_destroy(h)
     # the logits of 2^16 rows x 2^18 classes would take 32 GB: the workspace holds a piece of them
