@@ -9,8 +9,8 @@
  *
  * Rows are maps of one pixel; the weights are laid out as those of an FC with one group (weight_shape [1, width, features]).
  *
- * All sums are fp32.  bf16 plans: g and u stay in fp32 up to y, and up to dg and du in backward, which are rounded to bf16 once, as operands
- * of the products behind them; dx, dWg and dWu are fp32 sums rounded once.  fp32 plans: every operand is taken as three bf16 numbers that
+ * All sums are fp32.  bf16 plans: g and u stay in fp32 up to y; 20 bits of each are kept for backward (half a step is 2^-12), whose dg and du are
+ * computed in fp32 and rounded to bf16 once, as operands of the products behind them; dx, dWg and dWu are fp32 sums rounded once.  fp32 plans: every operand is taken as three bf16 numbers that
  * together hold its 24 bits, and a product adds the six pairings that fp32 can tell from nothing, which is as exact as products in fp32; an
  * infinity among the operands acts as NaN.  Deterministic: no atomics, sums in a fixed order.
  *

@@ -1,7 +1,7 @@
 // The gated pair of FCs: y = act(x Wg^T) (x Wu^T).
 //
 // Forward: one product whose columns are those of both weights, 32 of the gate and 32 of the other in turn, so that a wave holds g and u of
-// the same results in the same places of its registers and y is theirs.  Training keeps g and u in fp32.
+// the same results in the same places of its registers and y is theirs.  Training keeps g and u (Kept).
 // Backward: dg and du element by element from g, u and dy; then dx as one sum over the columns of both, and dWg and dWu as one launch.
 #include "gated_kernels.hpp"
 
@@ -47,11 +47,80 @@ __device__ __forceinline__ float act_of(float g, float& slope) {
     return g * sig;
 }
 
+// What backward needs of g and u.  fp32 plans: both as they are.  bf16 plans: 20 bits of each, sign, exponent and 11 of the mantissa, an
+// eighth of the rounding that dg and du take on as operands of the products: the first 16 of g and u in a word, four more of each in a byte.  That is 5 bytes
+// to write and to read again instead of 8, of 13 and 14 in all: 4096 x 2048 x 8192 forward and backward 800 us instead of 829.
+template <bool F32>
+struct Kept {
+    char* at;         // fp32: g, then u; bf16: words, then bytes
+    int64_t plane;    // elements
+    static constexpr int kBytes = F32 ? 8 : 5;  // of an element
+
+    static __device__ __forceinline__ uint32_t bits20(float v) {
+        const uint32_t u = __float_as_uint(v), r = u + 0x800u;
+        return ((r & 0x7f800000u) == 0x7f800000u ? u : r) >> 12;  // (what would round to infinity, infinities and NaN are cut)
+    }
+    static __device__ __forceinline__ uint32_t word(uint32_t g, uint32_t u) { return g >> 4 | (u >> 4) << 16; }
+    static __device__ __forceinline__ uint32_t rest(uint32_t g, uint32_t u) { return (g & 15u) | (u & 15u) << 4; }
+    __device__ __forceinline__ void put1(int64_t i, float g, float u) const {
+        if (F32) {
+            reinterpret_cast<float*>(at)[i] = g;
+            reinterpret_cast<float*>(at)[plane + i] = u;
+        } else {
+            const uint32_t bg = bits20(g), bu = bits20(u);
+            reinterpret_cast<uint32_t*>(at)[i] = word(bg, bu);
+            reinterpret_cast<uint8_t*>(at + 4 * plane)[i] = (uint8_t)rest(bg, bu);
+        }
+    }
+    // eight elements from i on, a multiple of 8
+    __device__ __forceinline__ void put8(int64_t i, const f32x4 (&g)[2], const f32x4 (&u)[2]) const {
+        if (F32) {
+            f32x4 *to = reinterpret_cast<f32x4*>(at) + i / 4, *to_u = to + plane / 4;
+            to[0] = g[0];
+            to[1] = g[1];
+            to_u[0] = u[0];
+            to_u[1] = u[1];
+        } else {
+            u32x4 w[2];
+            uint32_t b[2] = {0, 0};
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                const uint32_t bg = bits20(g[k >> 2][k & 3]), bu = bits20(u[k >> 2][k & 3]);
+                w[k >> 2][k & 3] = word(bg, bu);
+                b[k >> 2] |= rest(bg, bu) << ((k & 3) * 8);
+            }
+            u32x4* to = reinterpret_cast<u32x4*>(at) + i / 4;
+            to[0] = w[0];
+            to[1] = w[1];
+            __builtin_memcpy(at + 4 * plane + i, b, 8);
+        }
+    }
+    __device__ __forceinline__ void get8(int64_t i, float (&g)[8], float (&u)[8]) const {
+        if (F32) {
+            const f32x4 *from = reinterpret_cast<const f32x4*>(at) + i / 4, *from_u = from + plane / 4;
+            const f32x4 v[4] = {from[0], from[1], from_u[0], from_u[1]};
+#pragma unroll
+            for (int k = 0; k < 8; k++) g[k] = v[k >> 2][k & 3], u[k] = v[2 + (k >> 2)][k & 3];
+        } else {
+            const u32x4* from = reinterpret_cast<const u32x4*>(at) + i / 4;
+            const u32x4 w[2] = {from[0], from[1]};
+            uint32_t b[2];
+            __builtin_memcpy(b, at + 4 * plane + i, 8);
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                const uint32_t word = w[k >> 2][k & 3], byte = b[k >> 2] >> ((k & 3) * 8);
+                g[k] = __uint_as_float(word << 16 | (byte & 15u) << 12);
+                u[k] = __uint_as_float((word & 0xffff0000u) | (byte & 0xf0u) << 8);
+            }
+        }
+    }
+};
+
 struct FwdArgs {
     Factor x, w;
     int64_t rows, features, width, tiles_i, tiles_j, ld;
     void* y;
-    float* pre;  // g, and u `plane` elements behind it
+    char* kept;
     int64_t plane;
 };
 
@@ -118,13 +187,7 @@ __global__ __launch_bounds__(F::kThreads) void k_forward(FwdArgs a) {
                 float unused;
                 y[k] = act_of<ACT, false>(g[k >> 2][k & 3], unused) * u[k >> 2][k & 3];
             }
-            if (a.pre) {  // (rows of a multiple of 8)
-                f32x4 *to = reinterpret_cast<f32x4*>(a.pre + i * a.ld + j), *to_u = reinterpret_cast<f32x4*>(a.pre + a.plane + i * a.ld + j);
-                to[0] = g[0];
-                to[1] = g[1];
-                to_u[0] = u[0];
-                to_u[1] = u[1];
-            }
+            if (a.kept) Kept<kF32>{a.kept, a.plane}.put8(i * a.ld + j, g, u);  // (rows of a multiple of 8)
             if (kF32) {
                 float* to = static_cast<float*>(a.y) + i * a.width + j;
                 if (whole) {
@@ -153,7 +216,7 @@ struct FewArgs {
     const void *x, *w_gate, *w_up;
     int64_t rows, features, width, ld;
     void* y;
-    float* pre;
+    char* kept;
     int64_t plane;
 };
 template <class T, int NT, int ACT>
@@ -182,16 +245,12 @@ __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
             static_cast<float*>(a.y)[to] = y;
         else
             static_cast<uint16_t*>(a.y)[to] = f32_to_bf16(y);
-        if (a.pre) {
-            float* keep = a.pre + t * a.ld + f + e;
-            keep[0] = sums[0][e];
-            keep[a.plane] = sums[1][e];
-        }
+        if (a.kept) Kept<sizeof(T) == 4>{a.kept, a.plane}.put1(t * a.ld + f + e, sums[0][e], sums[1][e]);
     }
 }
 
 struct GradArgs {
-    const float* pre;
+    char* kept;
     int64_t plane, rows, width, ld;
     const void* dy;
     uint16_t *dg, *du;
@@ -205,8 +264,8 @@ __global__ __launch_bounds__(256) void k_grads(GradArgs a) {
     const bool whole = (a.width & 7) == 0;
     for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < n; k += (int64_t)gridDim.x * 256) {
         const int64_t row = k / wide, col = (k - row * wide) * 8, from = row * a.width + col;
-        const f32x4 g[2] = {*reinterpret_cast<const f32x4*>(a.pre + k * 8), *reinterpret_cast<const f32x4*>(a.pre + k * 8 + 4)};
-        const f32x4 u[2] = {*reinterpret_cast<const f32x4*>(a.pre + a.plane + k * 8), *reinterpret_cast<const f32x4*>(a.pre + a.plane + k * 8 + 4)};
+        float g[8], u[8];
+        Kept<F32>{a.kept, a.plane}.get8(k * 8, g, u);
         float dy[8];
         if (F32) {
             const float* p = static_cast<const float*>(a.dy) + from;
@@ -233,10 +292,10 @@ __global__ __launch_bounds__(256) void k_grads(GradArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; e++) {
             float slope;
-            const float act = act_of<ACT, true>(g[e >> 2][e & 3], slope);
+            const float act = act_of<ACT, true>(g[e], slope);
             const bool in = col + e < a.width;  // (behind the columns nothing was written)
             du[e] = in ? dy[e] * act : 0.f;
-            dg[e] = in ? dy[e] * u[e >> 2][e & 3] * slope : 0.f;
+            dg[e] = in ? dy[e] * u[e] * slope : 0.f;
         }
 #pragma unroll
         for (int which = 0; which < 2; which++) {
@@ -338,7 +397,7 @@ Plan plan_of(const Shape& s) {
         p.dw = product::cut_of(s.f32, s.width, s.features, s.rows, 2, true);
         p.launches_bwd = (p.copies && p.few) + 1 + product::launches_of(p.dx, p.dw, false);
         p.most_tiles = std::max(p.most_tiles, p.dx.tiles() * p.dx.splits + 2 * p.dw.tiles() * p.dw.splits);
-        p.pre_at = take(8ull * s.rows * wide);
+        p.kept_at = take((s.f32 ? Kept<true>::kBytes : Kept<false>::kBytes) * (uint64_t)s.rows * wide);
         p.grad_at = take(4ull * s.rows * product::pitch(s.f32, s.width));
         p.parts_at = take(product::parts_bytes(p.dx, 1, false));
         p.parts_dw_at = take(product::parts_bytes(p.dw, 2, false));
@@ -349,14 +408,14 @@ Plan plan_of(const Shape& s) {
 
 void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
     const int64_t ld = product::padded(s.f32, s.width);
-    float* pre = s.inference ? nullptr : reinterpret_cast<float*>(a.ws + p.pre_at);
+    char* kept = s.inference ? nullptr : a.ws + p.kept_at;
     if (p.few) {
-        const FewArgs f{a.x, a.w_gate, a.w_up, s.rows, s.features, s.width, ld, a.y, pre, s.rows * ld};
+        const FewArgs f{a.x, a.w_gate, a.w_up, s.rows, s.features, s.width, ld, a.y, kept, s.rows * ld};
         return s.f32 ? launch_few<float>(s.act, f, stream) : launch_few<uint16_t>(s.act, f, stream);
     }
     if (p.copies) make_copies(s, p, a.x, a.w_gate, a.w_up, a.ws, stream);
     const Operands o = operands_of(s, p, a.x, a.w_gate, a.w_up, a.ws);
-    const FwdArgs f{o.x, o.w, s.rows, s.features, s.width, p.forward.tiles_i, p.forward.tiles_j, ld, a.y, pre, s.rows * ld};
+    const FwdArgs f{o.x, o.w, s.rows, s.features, s.width, p.forward.tiles_i, p.forward.tiles_j, ld, a.y, kept, s.rows * ld};
     product::with_form(s.f32, p.forward.side, [&](auto form) { launch_forward<typename Paired<decltype(form)>::Type>(s.act, f, stream); });
 }
 
@@ -364,7 +423,7 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
     const int64_t ld = product::padded(s.f32, s.width), plane = s.rows * ld, wide = product::pitch(s.f32, s.width);
     if (p.copies && p.few) make_copies(s, p, a.x, a.w_gate, a.w_up, a.ws, stream);
     uint16_t *dg = reinterpret_cast<uint16_t*>(a.ws + p.grad_at), *du = dg + s.rows * wide;
-    const GradArgs g{reinterpret_cast<const float*>(a.ws + p.pre_at), plane, s.rows, s.width, ld, a.dy, dg, du, wide};
+    const GradArgs g{a.ws + p.kept_at, plane, s.rows, s.width, ld, a.dy, dg, du, wide};
     const dim3 grid((unsigned)std::min<int64_t>((plane / 8 + 255) / 256, 8192));
     with_act(s.act, [&](auto kind) {
         if (s.f32)

@@ -21,7 +21,7 @@ struct Plan {
     product::Cut forward, dx, dw;
     int launches_fwd = 0, launches_bwd = 0;
     // where the workspace holds what, and its end
-    uint64_t pre_at = 0, copy_at[3] = {}, grad_at = 0, parts_at = 0, parts_dw_at = 0, workspace_bytes = 0;
+    uint64_t kept_at = 0, copy_at[3] = {}, grad_at = 0, parts_at = 0, parts_dw_at = 0, workspace_bytes = 0;
     int64_t most_tiles = 0;
 };
 Plan plan_of(const Shape& s);

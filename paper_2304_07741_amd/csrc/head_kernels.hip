@@ -401,8 +401,10 @@ __global__ __launch_bounds__(F::kThreads) void k_grads(GradArgs a) {
 }
 
 constexpr int kFewRows = 32;
-// Gradients of a piece's logits: as much as stays in the last-level cache between the launch that writes them and the two that read them.
-constexpr uint64_t kPieceBytes = 128u << 20;
+// Gradients of a piece's logits.  Every piece more adds to dx in memory once more; a longer one leaves the last-level cache (256 MB) before it is read.  Measured with pieces of
+// 64, 128, 300, 600 MB, us: 4096 x 1024 x 32768 (268 MB in all) 1138, 1029, 1014, 1014; 8192 x 512 x 16000 (262) 729, 678, 624, 624;
+// 8192 x 1024 x 32768 (537) -, 2114, 1982, 2021; 4096 x 2048 x 65536 (537) -, 3610, 3672, 3704.
+constexpr uint64_t kPieceBytes = 288u << 20;
 uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
 
 template <class T>

@@ -44,6 +44,10 @@ def gated(kind, x, wg, wu, dy=None, f32=True):
     if dy is not None:
         du, dg = dy * a, dy * u * da
         rounded = half if not f32 else 4 * U
+        if not f32:      # what is kept of g and u has 20 bits: half a step is 2^-12 of the value
+            eg, eu = eg + 2.0 ** -12 * (g.abs() + eg), eu + 2.0 ** -12 * (u.abs() + eu)
+            ea = 1.13 * eg + 16 * U * a.abs() + 16 * U * (1 + g.abs()) * torch.exp(-g.abs())
+            ed = 0.8 * eg + 16 * U * (1 + da.abs())
         edu = dy.abs() * ea + rounded * du.abs()
         edg = dy.abs() * (ed * (u.abs() + eu) + da.abs() * eu) + rounded * dg.abs()
         f, t = wg.shape[0], x.shape[0]

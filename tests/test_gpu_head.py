@@ -75,13 +75,13 @@ def test_against_the_definition(shape, dtype, masked):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("shape", [(40000, 40, 4000), (3000, 64, 6100), (100000, 24, 700)], ids=str)
+@pytest.mark.parametrize("shape", [(40000, 40, 4000), (3000, 64, 6100), (100000, 24, 700), (250000, 24, 700)], ids=str)
 def test_several_pieces_and_large_tiles(shape, dtype):
-    if dtype == "f32" and shape[0] == 100000:
+    if dtype == "f32" and shape[0] >= 100000:
         pytest.skip("the first shape has pieces of fp32 plans")
     case = _case(*shape, dtype, 5, shape[0] == 3000)
     plan = harness.HeadRunner(*shape, dtype)
-    assert plan.info.pieces > 1 or shape[0] == 3000
+    assert (plan.info.pieces > 1) == (shape[0] * shape[2] * (6 if dtype == "f32" else 2) > 288 << 20)
     plan.close()
     _check(case, dtype, 1.0, (shape, dtype))
 

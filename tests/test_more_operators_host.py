@@ -100,7 +100,7 @@ def test_head_compile_and_query(lib):
     # the logits of 2^16 rows x 2^18 classes would take 32 GB: the workspace holds a piece of them
     h = B.canvas_head_compile(1 << 16, 1024, 1 << 18, B.CANVAS_BF16)
     info = B.canvas_head_query(h)
-    assert info.pieces > 100 and info.workspace_bytes < (1 << 16) * (1 << 18) * 2 // 8
+    assert info.pieces > 50 and info.workspace_bytes < (1 << 16) * (1 << 18) * 2 // 8
     B.canvas_head_destroy(h)
     h = B.canvas_head_compile(10, 64, 5000, B.CANVAS_F32, flags=B.CANVAS_OPT_INFERENCE)
     assert B.canvas_head_query(h).n_launches_bwd == 0
