@@ -393,8 +393,7 @@ Plan plan_of(const Shape& s) {
         for (int i = 0; i < 3; i++) p.copy_at[i] = take(2ull * rows[i] * ld);
     }
     if (!s.inference) {
-        p.dx = product::cut_of(s.f32, s.rows, s.features, 2 * s.width, 1, true);
-        p.dw = product::cut_of(s.f32, s.width, s.features, s.rows, 2, true);
+        product::cuts_of(s.f32, {s.rows, s.features, 2 * s.width, 1}, {s.width, s.features, s.rows, 2}, p.dx, p.dw);
         p.launches_bwd = (p.copies && p.few) + 1 + product::launches_of(p.dx, p.dw, false);
         p.most_tiles = std::max(p.most_tiles, p.dx.tiles() * p.dx.splits + 2 * p.dw.tiles() * p.dw.splits);
         p.kept_at = take((s.f32 ? Kept<true>::kBytes : Kept<false>::kBytes) * (uint64_t)s.rows * wide);

@@ -190,19 +190,23 @@ __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
         const int64_t t = n * 16 + (lane & 15);
         x[n] = static_cast<const T*>(a.x) + (t < a.rows ? t : a.rows - 1) * a.features;
     }
+    // (asked for ahead of the weights: a workgroup's end is short then)
+    const int64_t t = wave * 16 + (lane & 15), c0 = first + (lane >> 4) * 4;
+    const bool known = a.token && wave < NT && t < a.rows;
+    const int64_t c = known ? a.tokens[t] - c0 : -1;
+    uint32_t in[R];
+#pragma unroll
+    for (int r = 0; r < R; r++) in[r] = wave < NT ? allowed4(a.mask, c0 + r * 16, a.classes) : 0u;
     f32x4 sums[R];
     few::accumulate<T, R, NT>(w, x, a.features, sums, shared);
     if (wave >= NT) return;
-    const int64_t t = wave * 16 + (lane & 15), c0 = first + (lane >> 4) * 4;
     float z[R * 4];
 #pragma unroll
     for (int r = 0; r < R; r++) {
-        const uint32_t in = allowed4(a.mask, c0 + r * 16, a.classes);
 #pragma unroll
-        for (int e = 0; e < 4; e++) z[r * 4 + e] = in >> (8 * e) & 0xffu ? sums[r][e] : -kInf;
+        for (int e = 0; e < 4; e++) z[r * 4 + e] = in[r] >> (8 * e) & 0xffu ? sums[r][e] : -kInf;
     }
-    if (a.token && t < a.rows) {
-        const int64_t c = a.tokens[t] - c0;
+    if (known) {
 #pragma unroll
         for (int k = 0; k < R * 4; k++)
             if (c == (k >> 2) * 16 + (k & 3)) a.token[t] = z[k];
@@ -455,8 +459,7 @@ Plan plan_of(const Shape& s) {
         p.length = std::min<int64_t>(((s.classes + p.pieces - 1) / p.pieces + 255) / 256 * 256, s.classes);
         p.pieces = (int)((s.classes + p.length - 1) / p.length);
         p.piece = product::cut_of(s.f32, p.length, s.rows, s.features, 1, false);
-        p.dx = product::cut_of(s.f32, s.rows, s.features, p.length, 1, true);
-        p.dw = product::cut_of(s.f32, p.length, s.features, s.rows, 1, true);
+        product::cuts_of(s.f32, {s.rows, s.features, p.length, 1}, {p.length, s.features, s.rows, 1}, p.dx, p.dw);
         if (!p.copies) p.copy_at[1] = take(2ull * p.length * ld);
         p.launches_bwd = 1 + (p.copies && p.few) + p.pieces + (p.pieces - 1) * product::launches_of(product::Cut{p.dx.side}, p.dw, false) + product::launches_of(p.dx, p.dw, p.pieces > 1);
         p.most_tiles = std::max({p.most_tiles, p.piece.tiles(), p.dx.tiles() * p.dx.splits + p.dw.tiles() * p.dw.splits});
@@ -490,8 +493,10 @@ void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
         const FwdArgs f{factor_of(w, s.classes, ld), factor_of(x, s.rows, ld), s.rows, s.features, s.classes, p.logits.tiles_i, p.logits.tiles_j, a.it, a.mask, a.tokens, sums, token};
         product::with_form(s.f32, p.logits.side, [&](auto form) { launch_logits<decltype(form)>(f, stream); });
     }
-    int across = 1;
-    while (across < 16 && across * 2 <= s.rows) across *= 2;
+    // as many threads to a row as give each a few segments (16 rows of 1563: 8 us with 256 threads each, 20 with 16)
+    int turns = 16;
+    while (turns < 256 && turns * 6 < p.segments) turns *= 2;
+    const int across = 256 / turns;
     const RowArgs r{s.rows, s.classes, p.segments, across, a.it, a.mask, a.tokens, sums, token, a.logprob, a.entropy, s.inference ? nullptr : reinterpret_cast<Row*>(a.ws + p.rows_at)};
     CANVAS_LAUNCH(k_rows, rows_of_workgroups((s.rows + across - 1) / across, 256), dim3(256), 0, stream, r);
 }

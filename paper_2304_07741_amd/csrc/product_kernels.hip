@@ -210,38 +210,65 @@ struct Speed {
 constexpr Speed kSpeeds[2][3] = {{{256, 64, 1, 1.15, 1.6, 0, 0, 8.0}, {128, 64, 2, 0.55, 0.80, 0.95, 0, 4.8}, {64, 64, 3, 0.34, 0.36, 0.43, 0.51, 2.6}},
                                  {{128, 16, 2, 0.51, 0.60, 1.10, 0, 4.8}, {64, 32, 2, 0.39, 0.46, 0.82, 0, 1.0}, {0, 0, 0, 0, 0, 0, 0, 0}}};
 
-Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, bool may_split) {
-    Cut best;
-    double least = 0;
-    for (const Speed& v : kSpeeds[f32]) {
-        if (!v.side) continue;
-        Cut c;
-        c.side = v.side;
-        c.tiles_i = (rows + v.side - 1) / v.side;
-        c.tiles_j = (cols + v.side - 1) / v.side;
-        const int64_t tiles = c.tiles() * results, steps = (depth + v.depth - 1) / v.depth;
-        // `n` workgroups at a time
-        auto turn = [&](int64_t n, double stages) {
-            const double at[4] = {v.few, v.one, v.two, v.three};
-            const int k = (int)((n - 1) / 256);
-            const double share = (double)(n - k * 256) / 256;
-            return stages * (at[k] + (at[k + 1] - at[k]) * share) + v.ends * (0.4 + 0.6 * n / (256.0 * v.slots));
-        };
-        for (int splits = 1; splits <= 32; splits += splits < 4 ? 1 : splits < 8 ? 2 : splits / 4) {
-            if (splits > 1 && (!may_split || tiles * splits > 1024 || steps / splits < 2)) break;
-            const double each = (double)((steps + splits - 1) / splits);
-            const int64_t all = tiles * splits, slots = 256 * v.slots, rest = all % slots;
-            double t = (double)(all / slots) * turn(slots, each) + (rest ? turn(rest, each) : 0);
-            // parts of a sum: a launch, and their way to memory and back
-            if (splits > 1) t += 4 + 0.15e-6 * 4 * v.side * v.side * (double)all;
-            if (!least || t < least) {
-                least = t;
-                best = c;
-                best.splits = splits;
-            }
+// The best way of a form, and what it takes.
+Cut cut_with(const Speed& v, int64_t rows, int64_t cols, int64_t depth, int results, bool may_split, double& least) {
+    Cut c;
+    c.side = v.side;
+    c.tiles_i = (rows + v.side - 1) / v.side;
+    c.tiles_j = (cols + v.side - 1) / v.side;
+    const int64_t tiles = c.tiles() * results, steps = (depth + v.depth - 1) / v.depth;
+    // `n` workgroups at a time
+    auto turn = [&](int64_t n, double stages) {
+        const double at[4] = {v.few, v.one, v.two, v.three};
+        const int k = (int)((n - 1) / 256);
+        const double share = (double)(n - k * 256) / 256;
+        return stages * (at[k] + (at[k + 1] - at[k]) * share) + v.ends * (0.4 + 0.6 * n / (256.0 * v.slots));
+    };
+    least = 0;
+    Cut best = c;
+    for (int splits = 1; splits <= 32; splits += splits < 4 ? 1 : splits < 8 ? 2 : splits / 4) {
+        if (splits > 1 && (!may_split || tiles * splits > 1024 || steps / splits < 2)) break;
+        const double each = (double)((steps + splits - 1) / splits);
+        const int64_t all = tiles * splits, slots = 256 * v.slots, rest = all % slots;
+        double t = (double)(all / slots) * turn(slots, each) + (rest ? turn(rest, each) : 0);
+        // parts of a sum: a launch, and their way to memory and back
+        if (splits > 1) t += 4 + 0.15e-6 * 4 * v.side * v.side * (double)all;
+        if (!least || t < least) {
+            least = t;
+            best.splits = splits;
         }
     }
     return best;
+}
+
+Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, bool may_split) {
+    Cut best;
+    double least = 0, t;
+    for (const Speed& v : kSpeeds[f32]) {
+        if (!v.side) continue;
+        const Cut c = cut_with(v, rows, cols, depth, results, may_split, t);
+        if (!least || t < least) {
+            least = t;
+            best = c;
+        }
+    }
+    return best;
+}
+
+void cuts_of(bool f32, const Size& x, const Size& y, Cut& cx, Cut& cy) {
+    double least = 0;
+    for (const Speed& v : kSpeeds[f32])
+        for (const Speed& w : kSpeeds[f32]) {
+            if (!v.side || !w.side) continue;
+            double tx, ty;
+            const Cut a = cut_with(v, x.rows, x.cols, x.depth, x.results, true, tx), b = cut_with(w, y.rows, y.cols, y.depth, y.results, true, ty);
+            const double t = tx + ty + (v.side == w.side ? 0 : 4);  // (a launch more)
+            if (!least || t < least) {
+                least = t;
+                cx = a;
+                cy = b;
+            }
+        }
 }
 
 uint64_t parts_bytes(const Cut& c, int results, bool several) {

@@ -45,6 +45,12 @@ struct Product {
 };
 
 Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, bool may_split);
+// Of two products that one launch may take if their tiles are alike.
+struct Size {
+    int64_t rows, cols, depth;
+    int results;
+};
+void cuts_of(bool f32, const Size& x, const Size& y, Cut& cx, Cut& cy);
 uint64_t parts_bytes(const Cut& c, int results, bool several);
 // One product, or two that do not wait for each other, the first with a_rows.
 void multiply(const Product& p, hipStream_t stream);
