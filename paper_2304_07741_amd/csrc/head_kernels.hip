@@ -525,9 +525,8 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
         w.p[0] = w.p[1] = all.p[0] + first * lx;
         w.count = length;
         const uint8_t* mask = a.mask ? a.mask + first : nullptr;
-        const int64_t side = p.piece.side;
-        const GradArgs g{w, x, s.rows, s.features, length, (length + side - 1) / side, p.piece.tiles_j, first, a.it, mask, slope, grads, ld, wide};
-        product::with_form(s.f32, side, [&](auto form) { launch_grads<decltype(form)>(g, stream); });
+        const GradArgs g{w, x, s.rows, s.features, length, (length + p.piece.high - 1) / p.piece.high, p.piece.tiles_j, first, a.it, mask, slope, grads, ld, wide};
+        product::with_form(s.f32, p.piece.side, [&](auto form) { launch_grads<decltype(form)>(g, stream); });
         if (mask && !p.copies) {
             const product::Copy m{w.p[0], cw, length, s.features, mask};
             product::copy(false, &m, 1, stream);
@@ -554,7 +553,7 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
         e.depth = s.rows;
         e.out[0] = static_cast<char*>(a.dweight) + first * s.features * (s.f32 ? 4 : 2);
         e.cut = p.dw;
-        e.cut.tiles_i = (length + p.dw.side - 1) / p.dw.side;
+        e.cut.tiles_i = (length + p.dw.high - 1) / p.dw.high;
         e.parts = p.dw.splits > 1 ? reinterpret_cast<float*>(a.ws + p.parts_dw_at) : nullptr;
         e.first = e.last = true;
         product::multiply(d, e, stream);

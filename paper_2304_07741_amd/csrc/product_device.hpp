@@ -38,13 +38,16 @@ struct Form {
 using Large = Form<256, 256, 2, 4, 1, 64, 2>;
 using Middle = Form<128, 128, 2, 2, 1, 64, 2>;
 using Small = Form<64, 64, 2, 2, 1, 64, 3>;
+using Wide = Form<128, 256, 2, 4, 3, 32, 2>;
 using Triple = Form<128, 128, 2, 2, 3, 16, 3>;
 using SmallTriple = Form<64, 64, 2, 2, 3, 32, 3>;
 
 // f with the form that a cut asks for
 template <class F>
 void with_form(bool f32, int side, F f) {
-    if (f32 && side == 128)
+    if (f32 && side == 256)
+        f(Wide());
+    else if (f32 && side == 128)
         f(Triple());
     else if (f32)
         f(SmallTriple());

@@ -203,18 +203,21 @@ int64_t joins(const Product& p) { return p.parts && p.last ? p.cut.tiles() * p.r
 //   256 x 256 x 4096      77   33   23    130   51      1024 x 1024 x 4096    80   48   26    136   63      2048 x 2048 x 4096    80   56   60    158  217
 //   2048 x 4096 x 4096    86   66  109    290  483      4096 x 4096 x 4096   106  136  222    551  701      4096 x 4096 x 256     18   20   29     48   61
 // in four parts: 1024 x 1024 x 4096    33   27   26     52   60
+// fp32's 128 x 256 are for long sums over many tiles (4096^3: 247 TFLOP/s, 128 x 128 reach 191; 512 summands: 212 and 188).  Where they are taken by this rule, us
+// with and without them: 4096 x 1024 x 2 * 4096 forward 353 and 380, 3000 x 1500 x 2 * 3900 both ways 1207 and 1237, a head of 256 x 1024 x 32000 475 and 490.
 struct Speed {
-    int side, depth, slots;
+    int side, high, depth, slots;
     double few, one, two, three, ends;
 };
-constexpr Speed kSpeeds[2][3] = {{{256, 64, 1, 1.15, 1.6, 0, 0, 8.0}, {128, 64, 2, 0.55, 0.80, 0.95, 0, 4.8}, {64, 64, 3, 0.34, 0.36, 0.43, 0.51, 2.6}},
-                                 {{128, 16, 2, 0.51, 0.60, 1.10, 0, 4.8}, {64, 32, 2, 0.39, 0.46, 0.82, 0, 1.0}, {0, 0, 0, 0, 0, 0, 0, 0}}};
+constexpr Speed kSpeeds[2][3] = {{{256, 256, 64, 1, 1.15, 1.6, 0, 0, 8.0}, {128, 128, 64, 2, 0.55, 0.80, 0.95, 0, 4.8}, {64, 64, 64, 3, 0.34, 0.36, 0.43, 0.51, 2.6}},
+                                 {{256, 128, 32, 1, 1.5, 2.05, 0, 0, 8.0}, {128, 128, 16, 2, 0.51, 0.60, 1.10, 0, 4.8}, {64, 64, 32, 2, 0.39, 0.46, 0.82, 0, 1.0}}};
 
 // The best way of a form, and what it takes.
 Cut cut_with(const Speed& v, int64_t rows, int64_t cols, int64_t depth, int results, bool may_split, double& least) {
     Cut c;
     c.side = v.side;
-    c.tiles_i = (rows + v.side - 1) / v.side;
+    c.high = v.high;
+    c.tiles_i = (rows + v.high - 1) / v.high;
     c.tiles_j = (cols + v.side - 1) / v.side;
     const int64_t tiles = c.tiles() * results, steps = (depth + v.depth - 1) / v.depth;
     // `n` workgroups at a time
@@ -232,7 +235,7 @@ Cut cut_with(const Speed& v, int64_t rows, int64_t cols, int64_t depth, int resu
         const int64_t all = tiles * splits, slots = 256 * v.slots, rest = all % slots;
         double t = (double)(all / slots) * turn(slots, each) + (rest ? turn(rest, each) : 0);
         // parts of a sum: a launch, and their way to memory and back
-        if (splits > 1) t += 4 + 0.15e-6 * 4 * v.side * v.side * (double)all;
+        if (splits > 1) t += 4 + 0.15e-6 * 4 * v.high * v.side * (double)all;
         if (!least || t < least) {
             least = t;
             best.splits = splits;
@@ -245,7 +248,6 @@ Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, boo
     Cut best;
     double least = 0, t;
     for (const Speed& v : kSpeeds[f32]) {
-        if (!v.side) continue;
         const Cut c = cut_with(v, rows, cols, depth, results, may_split, t);
         if (!least || t < least) {
             least = t;
@@ -259,7 +261,6 @@ void cuts_of(bool f32, const Size& x, const Size& y, Cut& cx, Cut& cy) {
     double least = 0;
     for (const Speed& v : kSpeeds[f32])
         for (const Speed& w : kSpeeds[f32]) {
-            if (!v.side || !w.side) continue;
             double tx, ty;
             const Cut a = cut_with(v, x.rows, x.cols, x.depth, x.results, true, tx), b = cut_with(w, y.rows, y.cols, y.depth, y.results, true, ty);
             const double t = tx + ty + (v.side == w.side ? 0 : 4);  // (a launch more)
@@ -272,7 +273,7 @@ void cuts_of(bool f32, const Size& x, const Size& y, Cut& cx, Cut& cy) {
 }
 
 uint64_t parts_bytes(const Cut& c, int results, bool several) {
-    return c.splits > 1 || several ? 4ull * c.side * c.side * c.tiles() * c.splits * results : 0;
+    return c.splits > 1 || several ? 4ull * c.high * c.side * c.tiles() * c.splits * results : 0;
 }
 bool together(const Product& x, const Product& y) { return x.cut.side == y.cut.side && x.a_rows && !y.a_rows; }
 int launches_of(const Cut& x, const Cut& y, bool several) {

@@ -22,9 +22,9 @@ __host__ __device__ inline int64_t pitch(bool f32, int64_t cols) { return padded
 template <int PLANES>
 __host__ __device__ constexpr int64_t column(int64_t col, int h) { return PLANES == 1 ? col : col / 16 * 48 + h * 16 + col % 16; }
 
-// How results are cut: tiles of `side` x `side`, the sum over k in `splits` parts.
+// How results are cut: tiles of `high` x `side`, the sum over k in `splits` parts.
 struct Cut {
-    int side = 128, splits = 1;
+    int side = 128, high = 128, splits = 1;
     int64_t tiles_i = 0, tiles_j = 0;
     int64_t tiles() const { return tiles_i * tiles_j; }
 };
