@@ -141,7 +141,7 @@ struct Paired<product::SmallTriple> {
 };
 
 template <class F, int ACT>
-__global__ __launch_bounds__(F::kThreads) void k_forward(FwdArgs a) {
+__global__ __launch_bounds__(F::kThreads, 2) void k_forward(FwdArgs a) {
     constexpr int TM = F::TM, TN = F::TN, kCols = F::BN / 2;
     constexpr bool kF32 = F::PLANES == 3;
     static_assert(TN == 2, "a wave holds one block of each matrix");

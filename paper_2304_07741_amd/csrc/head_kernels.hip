@@ -108,7 +108,7 @@ __device__ __forceinline__ Sums sums_of(const float (&z)[N], float it) {
 }
 
 template <class F>
-__global__ __launch_bounds__(F::kThreads) void k_logits(FwdArgs a) {
+__global__ __launch_bounds__(F::kThreads, 2) void k_logits(FwdArgs a) {
     constexpr int TM = F::TM, TN = F::TN;
     PRODUCT_BUFFERS(F, buffers);
     const product::Place at = product::place_of(tile::xcd_sequence(), a.tiles_i, a.tiles_j, 1, 1);
@@ -308,7 +308,7 @@ struct GradArgs {
 };
 // The gradients of a tile of logits.
 template <class F>
-__global__ __launch_bounds__(F::kThreads) void k_grads(GradArgs a) {
+__global__ __launch_bounds__(F::kThreads, 2) void k_grads(GradArgs a) {
     constexpr int TM = F::TM, TN = F::TN, P = F::PLANES, kHalf = F::BN / 2;
     PRODUCT_BUFFERS(F, buffers);
     const product::Place at = product::place_of(tile::xcd_sequence(), a.tiles_i, a.tiles_j, 1, 1);

@@ -117,7 +117,7 @@ __device__ __forceinline__ void run(const Task& g, int64_t number, const Buffers
 
 // Two products in one launch, the first with rows of the summed index along it.  (Neither waits for the other, and small ones do not fill the chip.)
 template <class F>
-__global__ __launch_bounds__(F::kThreads) void k_products(Task first, Task second, int64_t firsts) {
+__global__ __launch_bounds__(F::kThreads, 2) void k_products(Task first, Task second, int64_t firsts) {
     PRODUCT_BUFFERS(F, buffers);
     // each XCD takes its eighth of the first product's tiles, then its share of the second's (they may take twice as long as the others)
     const unsigned total = gridDim.x * gridDim.y, lin = blockIdx.y * gridDim.x + blockIdx.x, xcd = lin & 7u, n = (unsigned)firsts;
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(F::kThreads) void k_products(Task first, Task secon
         run<F, kCols>(second, before(total) - before(n) + at - mine, buffers);
 }
 template <class F, Side SA>
-__global__ __launch_bounds__(F::kThreads) void k_product(Task g) {
+__global__ __launch_bounds__(F::kThreads, 2) void k_product(Task g) {
     PRODUCT_BUFFERS(F, buffers);
     run<F, SA>(g, tile::xcd_sequence(), buffers);
 }
