@@ -3,7 +3,7 @@
 // Forward: tiles of logits that never leave the registers.  Classes are the rows of a tile and the rows of x its columns, so that a lane
 // has the classes of its tile for one or two rows of x; it takes their largest logit m, S = sum exp(z - z_m) and sum exp(z - z_m) (z - z_m), joins them with the
 // other half of the wave, and leaves them to a second launch that joins the segments of all classes in a fixed order.
-// Backward: a piece of the classes at a time, a tile of logits is computed again and becomes their gradients in bf16 (three planes of them in fp32
+// Backward: a piece of the classes at a time, a tile of logits is computed again, by the same sums in the same order as in forward, and becomes their gradients in bf16 (three planes of them in fp32
 // plans), rows of x by classes; dx is the sum over all pieces' products with W, dW of the piece one product with x.
 #include "head_kernels.hpp"
 
@@ -171,6 +171,7 @@ struct FewArgs {
     const int64_t* tokens;
     Sums* sums;
     float* token;
+    float* logits;  // for backward, [rows][classes to the next multiple of 8]
 };
 constexpr int kFewBlocks = 2, kFewClasses = 16 * kFewBlocks;  // of a workgroup
 template <class T, int NT>
@@ -205,6 +206,12 @@ __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
     for (int r = 0; r < R; r++) {
 #pragma unroll
         for (int e = 0; e < 4; e++) z[r * 4 + e] = in[r] >> (8 * e) & 0xffu ? sums[r][e] : -kInf;
+    }
+    if (a.logits && t < a.rows) {
+        float* to = a.logits + t * ((a.classes + 7) & ~(int64_t)7) + c0;
+#pragma unroll
+        for (int r = 0; r < R; r++)
+            if (c0 + r * 16 < a.classes) *reinterpret_cast<f32x4*>(to + r * 16) = f32x4{z[r * 4], z[r * 4 + 1], z[r * 4 + 2], z[r * 4 + 3]};
     }
     if (known) {
 #pragma unroll
@@ -404,6 +411,56 @@ __global__ __launch_bounds__(F::kThreads, 2) void k_grads(GradArgs a) {
     }
 }
 
+// The gradients of the logits that forward has kept of few rows, eight per thread.  A tile would compute them by sums in another order than forward's, and a cold distribution
+// multiplies what they differ by.  16 x 1024 x 50000 both ways: 112 us (127 with a tile's sums, which read W once more), 32 x 2048 x 131072 488 (568); fp32 16 x 1024 x 50000 320 (386).
+struct FewGradArgs {
+    const float* logits;
+    int64_t rows, classes, all;  // of the piece; of all pieces
+    int64_t first;
+    float it;
+    const uint8_t* mask;         // of this piece
+    const Slope* slope;
+    uint16_t* to;
+    int64_t ld, wide;
+};
+template <bool F32>
+__global__ __launch_bounds__(256) void k_few_grads(FewGradArgs a) {
+    constexpr int P = F32 ? 3 : 1;
+    const int64_t t = blockIdx.y, col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (col >= a.wide) return;
+    const Slope s = a.slope[t];
+    u32x4 w[P] = {};
+    if (s.keep && col < a.classes) {
+        const f32x4* from = reinterpret_cast<const f32x4*>(a.logits + t * ((a.all + 7) & ~(int64_t)7) + a.first + col);
+        const f32x4 z[2] = {from[0], from[1]};
+        const uint32_t in[2] = {allowed4(a.mask, col, a.classes), allowed4(a.mask, col + 4, a.classes)};
+        const int64_t token = s.at >= 0 ? s.at - a.first - col : -1;
+        const Exp<F32> power(a.it);
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+            float d;
+            const float e = power.of(z[k >> 2][k & 3], s.most, d);
+            const float slope = fmaf(e, fmaf(s.second, d, s.first), token == k ? s.token : 0.f);
+            v[k] = in[k >> 2] >> (8 * (k & 3)) & 0xffu ? slope : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            if (F32) {
+                uint16_t lo[3], hi[3];
+                product::split(v[2 * k], lo);
+                product::split(v[2 * k + 1], hi);
+#pragma unroll
+                for (int h = 0; h < P; h++) w[h][k] = lo[h] | (uint32_t)hi[h] << 16;
+            } else {
+                w[0][k] = tile::pack_bf16(v[2 * k], v[2 * k + 1]);
+            }
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < P; h++) *reinterpret_cast<u32x4*>(a.to + t * a.ld + product::column<P>(col, h)) = w[h];
+}
+
 constexpr int kFewRows = 32;
 // Gradients of a piece's logits.  Every piece more adds to dx in memory once more; a longer one leaves the last-level cache (256 MB) before it is read.  Measured with pieces of
 // 64, 128, 300, 600 MB, us: 4096 x 1024 x 32768 (268 MB in all) 1138, 1029, 1014, 1014; 8192 x 512 x 16000 (262) 729, 678, 624, 624;
@@ -466,6 +523,7 @@ Plan plan_of(const Shape& s) {
         p.grad_at = take(2ull * s.rows * product::pitch(s.f32, p.length));
         p.parts_dx_at = take(product::parts_bytes(p.dx, 1, p.pieces > 1));
         p.parts_dw_at = take(product::parts_bytes(p.dw, 1, false));
+        if (p.few) p.logits_at = take(4ull * s.rows * ((s.classes + 7) / 8 * 8));
     }
     p.workspace_bytes = at;
     return p;
@@ -475,7 +533,7 @@ void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
     Sums* sums = reinterpret_cast<Sums*>(a.ws + p.sums_at);
     float* token = a.logprob ? reinterpret_cast<float*>(a.ws + p.token_at) : nullptr;
     if (p.few) {
-        const FewArgs f{a.x, a.weight, s.rows, s.features, s.classes, a.it, a.mask, a.tokens, sums, token};
+        const FewArgs f{a.x, a.weight, s.rows, s.features, s.classes, a.it, a.mask, a.tokens, sums, token, s.inference ? nullptr : reinterpret_cast<float*>(a.ws + p.logits_at)};
         if (s.f32)
             launch_few<float>(f, stream);
         else
@@ -525,8 +583,17 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
         w.p[0] = w.p[1] = all.p[0] + first * lx;
         w.count = length;
         const uint8_t* mask = a.mask ? a.mask + first : nullptr;
-        const GradArgs g{w, x, s.rows, s.features, length, (length + p.piece.high - 1) / p.piece.high, p.piece.tiles_j, first, a.it, mask, slope, grads, ld, wide};
-        product::with_form(s.f32, p.piece.side, [&](auto form) { launch_grads<decltype(form)>(g, stream); });
+        if (p.few) {
+            const FewGradArgs g{reinterpret_cast<const float*>(a.ws + p.logits_at), s.rows, length, s.classes, first, a.it, mask, slope, grads, ld, wide};
+            const dim3 grid((unsigned)((wide / 8 + 255) / 256), (unsigned)s.rows);
+            if (s.f32)
+                CANVAS_LAUNCH(k_few_grads<true>, grid, dim3(256), 0, stream, g);
+            else
+                CANVAS_LAUNCH(k_few_grads<false>, grid, dim3(256), 0, stream, g);
+        } else {
+            const GradArgs g{w, x, s.rows, s.features, length, (length + p.piece.high - 1) / p.piece.high, p.piece.tiles_j, first, a.it, mask, slope, grads, ld, wide};
+            product::with_form(s.f32, p.piece.side, [&](auto form) { launch_grads<decltype(form)>(g, stream); });
+        }
         if (mask && !p.copies) {
             const product::Copy m{w.p[0], cw, length, s.features, mask};
             product::copy(false, &m, 1, stream);

@@ -201,3 +201,23 @@ def test_gradients_against_differences():
         want, got = (loss[0] - loss[1]) / 2.0 ** -8, float((g[name].double() * v.double()).sum())
         assert abs(want - got) <= 2e-3 * float(g[name].double().norm() * v.double().norm()), (name, want, got)
     r.close()
+
+
+@pytest.mark.parametrize("rows", [3, 20, 40])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_of_cold_distributions_add_up_to_nothing(dtype, rows):
+    # The gradients of a row's logits add up to zero, which a column of ones in W shows in dx, however much the temperature multiplies the rounding of the logits:
+    # forward and backward have to mean the same logits.  Per unit of |g| it: 500 terms and their sum of e^x, fp32, each off by at most (500 + 90 * 3 + 8) 2^-24
+    # (the sum, three roundings of an argument that is 90 at most, or 126 in powers of two, the rest), once for p and once for the sum that dx is: 2^-12.
+    # bf16: dlogit's rounding, half a step of numbers that add up to 2 |g| it in all, 2^-7, and dx's own.
+    it, classes, features = 1e6, 500, 136
+    gen = torch.Generator().manual_seed(rows)
+    dt = TYPES[dtype]
+    x = torch.randn(rows, features, generator=gen).to(dt).cuda()
+    w = torch.randn(classes, features, generator=gen).to(dt)
+    x[:, 0], w[:, 0] = 0, 1
+    tokens = torch.randint(0, classes, (rows,), generator=gen).cuda()
+    g = torch.randn(rows, generator=gen).cuda()
+    out = _run(x, w.cuda(), tokens, None, g, None, dtype, it=it)
+    left = out["dx"][:, 0].double().abs() / (g.double().abs() * it)
+    assert float(left.max()) <= (2.0 ** -12 if dtype == "f32" else 2.0 ** -7 * (1 + 2.0 ** -8) + 2.0 ** -12), left.max()
