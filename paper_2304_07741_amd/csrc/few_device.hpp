@@ -1,7 +1,7 @@
 // The inner part of a product of a weight [n][k] with few rows x [rows][k], up to 16 NT of them: bound by reading the weight, which goes straight from
 // memory to the registers of the wave that multiplies it.
 //
-// A workgroup takes R blocks of 16 rows of weights.  Its waves share out the summed index, kAhead times 64 bytes of a row each in turn, and
+// A workgroup takes R blocks of 16 rows of weights.  Its waves share out the summed index, AHEAD times 64 bytes of a row each in turn, and
 // add up through LDS in the order of the waves.  bf16: the 16 x 16 x 32 product of the matrix units; fp32: their 16 x 16 x 4 one, whose products
 // and sums are those of fp32.  Rows may begin at any element.
 #pragma once
@@ -16,7 +16,7 @@ namespace few {
 using product::f32x4;
 using tile::u32x4;
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves, kAhead = 4;
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
 
 template <class T>
 struct Type;
@@ -53,19 +53,19 @@ __device__ __forceinline__ u32x4 load_end(const T* row, int64_t k, int64_t end) 
 
 // sums[r][t]: of weight rows `w[r]` (this lane's row of the block) and rows `x[t]`; whole sums in waves 0 .. NT - 1, wave t those of rows 16 t ..:
 // register e of a lane is weight row (lane / 16) * 4 + e, row lane % 16 of x.
-template <class T, int R, int NT>
+template <class T, int R, int NT, int AHEAD>
 __device__ __forceinline__ void accumulate(const T* const (&w)[R], const T* const (&x)[NT], int64_t depth, f32x4 (&sums)[R], f32x4* shared) {
     using Y = Type<T>;
-    constexpr int kStep = 4 * Y::kEach, kTurn = kStep * kAhead;  // elements of a row that a wave takes per load, and per turn
+    constexpr int kStep = 4 * Y::kEach, kTurn = kStep * AHEAD;  // elements of a row that a wave takes per load, and per turn
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t mine = (lane >> 4) * Y::kEach;
     f32x4 acc[R][NT] = {};
     struct Turn {
-        u32x4 w[R][kAhead], x[NT][kAhead];
+        u32x4 w[R][AHEAD], x[NT][AHEAD];
     };
     auto load = [&](int64_t k, Turn& t) {
 #pragma unroll
-        for (int u = 0; u < kAhead; u++) {
+        for (int u = 0; u < AHEAD; u++) {
 #pragma unroll
             for (int r = 0; r < R; r++) t.w[r][u] = load16(w[r] + k + u * kStep + mine);
 #pragma unroll
@@ -74,7 +74,7 @@ __device__ __forceinline__ void accumulate(const T* const (&w)[R], const T* cons
     };
     auto multiply = [&](const Turn& t) {
 #pragma unroll
-        for (int u = 0; u < kAhead; u++)
+        for (int u = 0; u < AHEAD; u++)
 #pragma unroll
             for (int r = 0; r < R; r++)
 #pragma unroll

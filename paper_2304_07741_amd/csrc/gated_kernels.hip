@@ -232,7 +232,7 @@ __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
         x[n] = static_cast<const T*>(a.x) + (t < a.rows ? t : a.rows - 1) * a.features;
     }
     f32x4 sums[2];
-    few::accumulate<T, 2, NT>(w, x, a.features, sums, shared);
+    few::accumulate<T, 2, NT, 4>(w, x, a.features, sums, shared);
     const int64_t t = wave * 16 + (lane & 15), f = f0 + (lane >> 4) * 4;
     if (wave >= NT || t >= a.rows) return;
 #pragma unroll

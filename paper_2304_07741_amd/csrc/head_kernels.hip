@@ -173,13 +173,15 @@ struct FewArgs {
     float* token;
     float* logits;  // for backward, [rows][classes to the next multiple of 8]
 };
-constexpr int kFewBlocks = 2, kFewClasses = 16 * kFewBlocks;  // of a workgroup
-template <class T, int NT>
+// Blocks of 16 classes of a workgroup.  With 17 rows or more x is as much to read from the L2 as two blocks' weights from memory: four where there are enough of them (32 x 2048 x 131072:
+// 122 us instead of 135; 20 x 1000 x 50021 38 and 44; fp32 32 x 1024 x 50000 66 and 70; but 17 x 333 x 3000 12 instead of 10; 24 x 256 x 10000 the same).
+constexpr int64_t kManyClasses = 16384;
+int few_blocks(int64_t rows, int64_t classes) { return rows > 16 && classes > kManyClasses ? 4 : 2; }
+template <class T, int NT, int R>
 __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
-    constexpr int R = kFewBlocks;
     __shared__ f32x4 shared[R * NT * few::kWaves * 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t first = (int64_t)blockIdx.x * kFewClasses;
+    const int64_t first = (int64_t)blockIdx.x * (16 * R);
     const T *w[R], *x[NT];
 #pragma unroll
     for (int r = 0; r < R; r++) {
@@ -199,7 +201,7 @@ __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
 #pragma unroll
     for (int r = 0; r < R; r++) in[r] = wave < NT ? allowed4(a.mask, c0 + r * 16, a.classes) : 0u;
     f32x4 sums[R];
-    few::accumulate<T, R, NT>(w, x, a.features, sums, shared);
+    few::accumulate<T, R, NT, R == 2 ? 4 : 2>(w, x, a.features, sums, shared);
     if (wave >= NT) return;
     float z[R * 4];
 #pragma unroll
@@ -470,11 +472,14 @@ uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
 
 template <class T>
 void launch_few(const FewArgs& a, hipStream_t stream) {
-    const dim3 grid((unsigned)((a.classes + kFewClasses - 1) / kFewClasses));
+    const int blocks = few_blocks(a.rows, a.classes);
+    const dim3 grid((unsigned)((a.classes + 16 * blocks - 1) / (16 * blocks)));
     if (a.rows <= 16)
-        CANVAS_LAUNCH((k_few<T, 1>), grid, dim3(few::kThreads), 0, stream, a);
+        CANVAS_LAUNCH((k_few<T, 1, 2>), grid, dim3(few::kThreads), 0, stream, a);
+    else if (blocks == 2)
+        CANVAS_LAUNCH((k_few<T, 2, 2>), grid, dim3(few::kThreads), 0, stream, a);
     else
-        CANVAS_LAUNCH((k_few<T, 2>), grid, dim3(few::kThreads), 0, stream, a);
+        CANVAS_LAUNCH((k_few<T, 2, 4>), grid, dim3(few::kThreads), 0, stream, a);
 }
 template <class F>
 void launch_logits(const FwdArgs& a, hipStream_t stream) {
@@ -495,7 +500,8 @@ Plan plan_of(const Shape& s) {
     p.few = s.rows <= kFewRows;
     p.copies = (s.f32 || s.features % 8) && !(p.few && s.inference);
     p.logits = product::cut_of(s.f32, s.classes, s.rows, s.features, 1, false);
-    p.segments = (int)(p.few ? (s.classes + kFewClasses - 1) / kFewClasses : p.logits.tiles_i * 2);
+    const int few = 16 * few_blocks(s.rows, s.classes);
+    p.segments = (int)(p.few ? (s.classes + few - 1) / few : p.logits.tiles_i * 2);
     p.launches_fwd = 2 + (p.copies && !p.few);
     p.most_tiles = p.few ? p.segments : p.logits.tiles();
     uint64_t at = 0;

@@ -86,6 +86,12 @@ def test_several_pieces_and_large_tiles(shape, dtype):
     _check(case, dtype, 1.0, (shape, dtype))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(17, 33, 16385), (32, 72, 17001)], ids=str)
+def test_few_rows_of_many_classes(shape, dtype):
+    _check(_case(*shape, dtype, 6, True), dtype, 1.0, (shape, dtype))
+
+
 @pytest.mark.parametrize("dlp,dent", [(True, False), (False, True), (False, False)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_gradients_that_are_not_given(dtype, dlp, dent):
