@@ -13,7 +13,7 @@ TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 # one more than it, sums of one step and of one more, sums cut into parts (many rows and few weights), tiles of 256
 SHAPES = [(1, 1, 1), (1, 17, 3), (3, 5, 7), (4, 2048, 40), (16, 64, 33), (17, 136, 64), (32, 1001, 50), (33, 40, 24), (64, 64, 256), (128, 64, 64), (129, 72, 65),
           (130, 1000, 300), (257, 65, 129), (300, 128, 1), (1500, 8, 16), (9001, 64, 64), (5000, 100, 24)]
-LARGE = [(3100, 72, 2000), (2900, 328, 1900), (700, 700, 6000)]
+LARGE = [(3100, 72, 2000), (2900, 328, 1900), (700, 700, 6000), (1001, 1993, 8101)]
 
 
 def _case(rows, features, width, dtype, seed, std=1.0):

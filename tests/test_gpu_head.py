@@ -92,6 +92,11 @@ def test_few_rows_of_many_classes(shape, dtype):
     _check(_case(*shape, dtype, 6, True), dtype, 1.0, (shape, dtype))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_sums(dtype):
+    _check(_case(1001, 1993, 8101, dtype, 8, True), dtype, 1.0, dtype)
+
+
 @pytest.mark.parametrize("dlp,dent", [(True, False), (False, True), (False, False)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_gradients_that_are_not_given(dtype, dlp, dent):
