@@ -8,8 +8,8 @@
  *   dx = sum_i dlogit_i W_i,  dW_i = sum over the rows of dlogit_i x
  *
  * as canvas_logprob.h has them for logits that are at hand.  Forward keeps the largest logit and the sums of each row; backward takes the
- * classes a piece at a time, computes a piece's logits again, the same ones, and leaves its gradients in the workspace only.  (Of up to 32 rows forward
- * leaves the logits in the workspace too, which is less to read than W.)
+ * classes a piece at a time, computes a piece's logits again, the same ones, and leaves its gradients in the workspace only.  (Where that is faster, forward
+ * leaves logits in the workspace, in fp32: those of up to 32 rows, and up to a GiB of others.)
  *
  * A masked class is not looked at (its row of W may be NaN) and has a gradient of zeros.  A row of x that has nothing left (all classes masked
  * or -inf) has the log probability -inf, the entropy 0 and a gradient of zeros.  A token that is no class (negative, say, for positions
@@ -44,7 +44,7 @@ typedef struct canvas_head canvas_head;
 typedef struct canvas_head_info {
     int32_t n_launches_fwd, n_launches_bwd; /* kernels enqueued per call */
     int32_t pieces, reserved0;              /* how many pieces backward takes the classes in */
-    uint64_t workspace_bytes;               /* the rows' sums, a piece's dlogit, copies of operands, parts of sums, few rows' logits */
+    uint64_t workspace_bytes;               /* the rows' sums, a piece's dlogit, copies of operands, parts of sums, some logits */
     double flops_fwd, flops_bwd;            /* of the products above; backward computes the logits again */
     double min_bytes_fwd, min_bytes_bwd;    /* every tensor of a call read or written once; without a mask */
 } canvas_head_info;

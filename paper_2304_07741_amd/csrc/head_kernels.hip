@@ -3,7 +3,7 @@
 // Forward: tiles of logits that never leave the registers.  Classes are the rows of a tile and the rows of x its columns, so that a lane
 // has the classes of its tile for one or two rows of x; it takes their largest logit m, S = sum exp(z - z_m) and sum exp(z - z_m) (z - z_m), joins them with the
 // other half of the wave, and leaves them to a second launch that joins the segments of all classes in a fixed order.
-// Backward: a piece of the classes at a time, a tile of logits is computed again, by the same sums in the same order as in forward, and becomes their gradients in bf16 (three planes of them in fp32
+// Backward: a piece of the classes at a time, a tile of logits is read, or computed again by the same sums in the same order as in forward, and becomes their gradients in bf16 (three planes of them in fp32
 // plans), rows of x by classes; dx is the sum over all pieces' products with W, dW of the piece one product with x.
 #include "head_kernels.hpp"
 
@@ -79,7 +79,12 @@ struct FwdArgs {
     const int64_t* tokens;
     Sums* sums;    // [segments][rows]
     float* token;  // [rows]: the token's logit
+    f32x4* kept;   // for backward, those of the first classes, as the tiles' workgroups hold them
+    int64_t kept_classes;
 };
+// A tile's logits, or where they are.
+template <class F>
+__device__ __forceinline__ f32x4* kept_of(f32x4* kept, int64_t tile) { return kept + tile * (F::BM * F::BN / 4) + threadIdx.x; }
 
 // N logits of one row of x in a lane, the sums of those and of what the lanes LOW, 2 LOW, .. 32 apart hold.
 template <int N, int LOW, bool F32>
@@ -128,6 +133,15 @@ __global__ __launch_bounds__(F::kThreads, 2) void k_logits(FwdArgs a) {
     }
     f32x16 acc[TM][TN] = {};
     product::accumulate<F, product::kRows, product::kRows, false>(a.w, a.x, 0, i0, j0, a.features, 0, steps, steps, 1, buffers, acc);
+    if (i0 < a.kept_classes) {
+        f32x4* to = kept_of<F>(a.kept, at.i * a.tiles_j + at.j);
+#pragma unroll
+        for (int x = 0; x < TM; x++)
+#pragma unroll
+            for (int y = 0; y < TN; y++)
+#pragma unroll
+                for (int q = 0; q < 4; q++) to[((x * TN + y) * 4 + q) * F::kThreads] = f32x4{acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
+    }
     if (a.mask || i0 + F::BM > a.classes) {
 #pragma unroll
         for (int x = 0; x < TM; x++)
@@ -314,9 +328,10 @@ struct GradArgs {
     const Slope* slope;
     uint16_t* to;                  // [rows][ld], `wide` columns
     int64_t ld, wide;
+    f32x4* kept;                   // the piece's logits, where forward has left them
 };
 // The gradients of a tile of logits.
-template <class F>
+template <class F, bool KEPT>
 __global__ __launch_bounds__(F::kThreads, 2) void k_grads(GradArgs a) {
     constexpr int TM = F::TM, TN = F::TN, P = F::PLANES, kHalf = F::BN / 2;
     PRODUCT_BUFFERS(F, buffers);
@@ -325,7 +340,21 @@ __global__ __launch_bounds__(F::kThreads, 2) void k_grads(GradArgs a) {
     const int64_t i0 = at.i * F::BM, j0 = at.j * F::BN;
     const int steps = (int)((a.features + F::BK - 1) / F::BK);
     f32x16 acc[TM][TN] = {};
-    product::accumulate<F, product::kRows, product::kRows, false>(a.w, a.x, 0, i0, j0, a.features, 0, steps, steps, 1, buffers, acc);
+    if (KEPT) {
+        const f32x4* from = kept_of<F>(a.kept, at.i * a.tiles_j + at.j);
+#pragma unroll
+        for (int x = 0; x < TM; x++)
+#pragma unroll
+            for (int y = 0; y < TN; y++)
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    const f32x4 v = from[((x * TN + y) * 4 + q) * F::kThreads];
+#pragma unroll
+                    for (int e = 0; e < 4; e++) acc[x][y][4 * q + e] = v[e];
+                }
+    } else {
+        product::accumulate<F, product::kRows, product::kRows, false>(a.w, a.x, 0, i0, j0, a.features, 0, steps, steps, 1, buffers, acc);
+    }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / F::WJ * (TM * 32) + (lane >> 5) * 4, wj = wave % F::WJ * (TN * 32) + (lane & 31);
     const Exp<P == 3> power(a.it);
 #pragma unroll
@@ -468,6 +497,12 @@ constexpr int kFewRows = 32;
 // 64, 128, 300, 600 MB, us: 4096 x 1024 x 32768 (268 MB in all) 1138, 1029, 1014, 1014; 8192 x 512 x 16000 (262) 729, 678, 624, 624;
 // 8192 x 1024 x 32768 (537) -, 2114, 1982, 2021; 4096 x 2048 x 65536 (537) -, 3610, 3672, 3704.
 constexpr uint64_t kPieceBytes = 288u << 20;
+// Logits that forward leaves for backward, a tile as its workgroup holds it: those of the first pieces, up to a GiB.  To write and read them is memory's work, to compute them again the matrix
+// units', which is more with many features, and in fp32.  Both ways with the logits and with their computing again, us: 4096 x 4096 x 32768 2872 and 3513; 4096 x 2048 x 65536 3236 and 3712;
+// 4096 x 1024 x 32768 995 and 1018; 4000 x 512 x 16000 385 and 355; fp32 4000 x 1000 x 30000 4300 and 5360; 8000 x 200 x 16000 1586 and 1684; 2000 x 128 x 20000 434 and 430;
+// 4000 x 64 x 10000 375 and 349.  In the L2s: 256 x 512 x 1000 26 and 28; 250 x 256 x 2000 28 and 29; fp32 256 x 512 x 1000 42 and 48; 1000 x 100 x 2000 48 and 50.
+constexpr uint64_t kKeptBytes = 1u << 30, kNearBytes = 16u << 20;
+int64_t kept_from(bool f32, uint64_t bytes) { return bytes <= kNearBytes ? (f32 ? 1 : 256) : f32 ? 192 : 1024; }
 uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
 
 template <class T>
@@ -487,7 +522,11 @@ void launch_logits(const FwdArgs& a, hipStream_t stream) {
 }
 template <class F>
 void launch_grads(const GradArgs& a, hipStream_t stream) {
-    CANVAS_LAUNCH(k_grads<F>, rows_of_workgroups(a.tiles_i * a.tiles_j, F::kThreads), dim3(F::kThreads), 0, stream, a);
+    const dim3 grid = rows_of_workgroups(a.tiles_i * a.tiles_j, F::kThreads);
+    if (a.kept)
+        CANVAS_LAUNCH((k_grads<F, true>), grid, dim3(F::kThreads), 0, stream, a);
+    else
+        CANVAS_LAUNCH((k_grads<F, false>), grid, dim3(F::kThreads), 0, stream, a);
 }
 
 Factor factor_of(const uint16_t* at, int64_t rows, int64_t ld) { return Factor{{at, at}, ld, rows}; }
@@ -521,7 +560,15 @@ Plan plan_of(const Shape& s) {
         p.pieces = (int)((s.classes + fit - 1) / fit);
         p.length = std::min<int64_t>(((s.classes + p.pieces - 1) / p.pieces + 255) / 256 * 256, s.classes);
         p.pieces = (int)((s.classes + p.length - 1) / p.length);
-        p.piece = product::cut_of(s.f32, p.length, s.rows, s.features, 1, false);
+        p.piece = p.logits;
+        p.piece.tiles_i = (p.length + p.piece.high - 1) / p.piece.high;
+        if (p.few) {
+            p.logits_at = take(4ull * s.rows * ((s.classes + 7) / 8 * 8));
+        } else {
+            const uint64_t each = 4ull * p.piece.tiles() * p.piece.high * p.piece.side;
+            if (s.features >= kept_from(s.f32, each * p.pieces)) p.kept = (int)std::min<uint64_t>(p.pieces, kKeptBytes / each);
+            p.logits_at = take(each * p.kept);
+        }
         product::cuts_of(s.f32, {s.rows, s.features, p.length, 1}, {p.length, s.features, s.rows, 1}, p.dx, p.dw);
         if (!p.copies) p.copy_at[1] = take(2ull * p.length * ld);
         p.launches_bwd = 1 + (p.copies && p.few) + p.pieces + (p.pieces - 1) * product::launches_of(product::Cut{p.dx.side}, p.dw, false) + product::launches_of(p.dx, p.dw, p.pieces > 1);
@@ -529,7 +576,6 @@ Plan plan_of(const Shape& s) {
         p.grad_at = take(2ull * s.rows * product::pitch(s.f32, p.length));
         p.parts_dx_at = take(product::parts_bytes(p.dx, 1, p.pieces > 1));
         p.parts_dw_at = take(product::parts_bytes(p.dw, 1, false));
-        if (p.few) p.logits_at = take(4ull * s.rows * ((s.classes + 7) / 8 * 8));
     }
     p.workspace_bytes = at;
     return p;
@@ -554,7 +600,7 @@ void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
             w = cw;
         }
         const int64_t ld = product::pitch(s.f32, s.features);
-        const FwdArgs f{factor_of(w, s.classes, ld), factor_of(x, s.rows, ld), s.rows, s.features, s.classes, p.logits.tiles_i, p.logits.tiles_j, a.it, a.mask, a.tokens, sums, token};
+        const FwdArgs f{factor_of(w, s.classes, ld), factor_of(x, s.rows, ld), s.rows, s.features, s.classes, p.logits.tiles_i, p.logits.tiles_j, a.it, a.mask, a.tokens, sums, token, reinterpret_cast<f32x4*>(a.ws + p.logits_at), p.kept * p.length};
         product::with_form(s.f32, p.logits.side, [&](auto form) { launch_logits<decltype(form)>(f, stream); });
     }
     // as many threads to a row as give each a few segments (16 rows of 1563: 8 us with 256 threads each, 20 with 16)
@@ -597,7 +643,8 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
             else
                 CANVAS_LAUNCH(k_few_grads<false>, grid, dim3(256), 0, stream, g);
         } else {
-            const GradArgs g{w, x, s.rows, s.features, length, (length + p.piece.high - 1) / p.piece.high, p.piece.tiles_j, first, a.it, mask, slope, grads, ld, wide};
+            const GradArgs g{w, x, s.rows, s.features, length, (length + p.piece.high - 1) / p.piece.high, p.piece.tiles_j, first, a.it, mask, slope, grads, ld, wide,
+                             n < p.kept ? reinterpret_cast<f32x4*>(a.ws + p.logits_at) + first * p.piece.tiles_j * p.piece.side / 4 : nullptr};
             product::with_form(s.f32, p.piece.side, [&](auto form) { launch_grads<decltype(form)>(g, stream); });
         }
         if (mask && !p.copies) {

@@ -29,6 +29,7 @@ struct alignas(16) Slope {
 
 struct Plan {
     bool few = false, copies = false;
+    int kept = 0;                        // pieces whose logits forward leaves for backward
     product::Cut logits, piece, dx, dw;  // `piece`: of the logits of one piece
     int segments = 0;                    // of the classes: what forward leaves sums of
     int pieces = 1;

@@ -92,6 +92,16 @@ def test_few_rows_of_many_classes(shape, dtype):
     _check(_case(*shape, dtype, 6, True), dtype, 1.0, (shape, dtype))
 
 
+def test_logits_of_some_pieces_are_left_for_backward():
+    """More than a GiB of logits: those of the first pieces are read again, the others computed again."""
+    shape = (70000, 200, 4100)
+    case = _case(*shape, "f32", 9, True)
+    plan = harness.HeadRunner(*shape, "f32")
+    assert plan.info.pieces > 8 and 1 << 30 < 4 * shape[0] * shape[2]
+    plan.close()
+    _check(case, "f32", 0.8, shape)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_long_sums(dtype):
     _check(_case(1001, 1993, 8101, dtype, 8, True), dtype, 1.0, dtype)
