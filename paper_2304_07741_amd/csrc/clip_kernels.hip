@@ -2,7 +2,8 @@
 //
 // Two passes over memory: squares, added up in 64 bits by each thread over its elements, then by each workgroup, then by every workgroup of the second
 // pass for itself, always in the same order; and the scaling.  The second pass goes through the tensors backwards: what the first one read last is still in the
-// last-level cache.
+// last-level cache.  Bound by memory: 2^28 elements of bf16, squares 91 us (5.9 TB/s), scaling 189 (5.7); 25.5 M elements of both types to fp32 19 and 33.  Chunks of 16384 elements, 64 a
+// thread: all of a chunk's loads are in flight at once.
 #include "clip_kernels.hpp"
 
 #include <algorithm>
@@ -218,7 +219,7 @@ __global__ __launch_bounds__(kThreads) void k_scale(Items a, const double* parts
     }
 }
 
-// Few elements: one workgroup does all of it, a chunk at a time.
+// Few elements: one workgroup does all of it, in one launch (two tensors of 3000 elements 7 us; in two launches 12 of 60000 in all take 13.6).
 constexpr int kAlone = 1024;
 __global__ __launch_bounds__(kAlone) void k_alone(Items a, double most, float* norm, float* scale) {
     __shared__ double buf[kAlone / 64];

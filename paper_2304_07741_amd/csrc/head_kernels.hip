@@ -112,6 +112,9 @@ __device__ __forceinline__ Sums sums_of(const float (&z)[N], float it) {
     return r;
 }
 
+// Bound by the matrix units; a tile's exponentials, and the logits that are kept, are not hidden by another tile where one fills its compute unit.
+// 4096 x 1024 x 32768 bf16: 264 us (1.04 PFLOP/s), 315 with 537 MB of logits kept; 1500 x 1000 x 50021 170 us, 4.6 rounds of tiles of 256.  (With a branch
+// per register for the token's logit instead of selections 345.)
 template <class F>
 __global__ __launch_bounds__(F::kThreads, 2) void k_logits(FwdArgs a) {
     constexpr int TM = F::TM, TN = F::TN;
@@ -191,6 +194,7 @@ struct FewArgs {
 // 122 us instead of 135; 20 x 1000 x 50021 38 and 44; fp32 32 x 1024 x 50000 66 and 70; but 17 x 333 x 3000 12 instead of 10; 24 x 256 x 10000 the same).
 constexpr int64_t kManyClasses = 16384;
 int few_blocks(int64_t rows, int64_t classes) { return rows > 16 && classes > kManyClasses ? 4 : 2; }
+// Bound by the weight's bytes: 4 x 2048 x 131072 bf16, 537 MB in 95 us, 5.7 TB/s.
 template <class T, int NT, int R>
 __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
     __shared__ f32x4 shared[R * NT * few::kWaves * 64];
@@ -249,7 +253,7 @@ struct RowArgs {
     float *logprob, *entropy;
     Row* row;
 };
-// Joins the segments of each row.
+// Joins the segments of each row: latency of a few dependent loads and lane exchanges; 4 rows of 4096 segments 7.6 us, 4096 of 256 12 us.
 __global__ __launch_bounds__(256) void k_rows(RowArgs a) {
     __shared__ Sums part[256];
     const int mine = threadIdx.x & (a.across - 1), turn = threadIdx.x / a.across, turns = 256 / a.across;
@@ -301,7 +305,7 @@ struct SlopeArgs {
     uint16_t* copy;
 };
 // Slopes of the rows, and x as products read it: with zeros for the rows without a gradient, whose products by the zeros of their logits' gradients are
-// zero then, whatever they hold.
+// zero then, whatever they hold.  A few us: 4096 x 1024 bf16 6.2.
 template <bool F32>
 __global__ __launch_bounds__(256) void k_slopes(SlopeArgs a) {
     const int64_t wide = product::padded(F32, a.features) / 8, n = a.rows * wide, ld = product::pitch(F32, a.features);
@@ -330,7 +334,8 @@ struct GradArgs {
     int64_t ld, wide;
     f32x4* kept;                   // the piece's logits, where forward has left them
 };
-// The gradients of a tile of logits.
+// The gradients of a tile of logits.  4096 x 1024 x 32768 bf16: 187 us from kept logits (805 MB, 4.3 TB/s: one workgroup to a compute unit reads, computes and writes in turn), 279 with their
+// product, of which the matrix units are the bound.
 template <class F, bool KEPT>
 __global__ __launch_bounds__(F::kThreads, 2) void k_grads(GradArgs a) {
     constexpr int TM = F::TM, TN = F::TN, P = F::PLANES, kHalf = F::BN / 2;

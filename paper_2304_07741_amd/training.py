@@ -8,7 +8,7 @@
     loss = mean of -log p(label) - entropy_weight * entropy      canvas_logprob
     W = W - lr * orthogonalised momentum                canvas_ortho, on the fp32 gradients of every FC
 
-With `widen` the head is a gated pair of FCs in front of the classes, and the logits are never kept; with `max_norm` all gradients are scaled down together
+With `widen` the head is a gated pair of FCs in front of the classes, and the logits are no tensor of the step; with `max_norm` all gradients are scaled down together
 before the updates take them:
 
     v = act(p Wg^T) (p Wu^T),  p = mean over the pixels of u_L      canvas_dag, canvas_gated
