@@ -13,7 +13,7 @@ namespace product {
 namespace {
 
 // What a kernel takes of a product.
-struct Task {
+struct Job {
     Factor a, b;
     int64_t depth, tiles_i, tiles_j, ld;
     int segments, results, splits;
@@ -37,7 +37,7 @@ __device__ __forceinline__ void to_image(float* img, const f32x16& acc, int r0, 
 
 // Results (i, j ..) from an image of ROWS x BN of them to memory, rounded where they are bf16.
 template <bool F32, int ROWS, int BN, int THREADS>
-__device__ __forceinline__ void emit(const Task& g, int which, int64_t i0, int64_t j0, const float* img) {
+__device__ __forceinline__ void emit(const Job& g, int which, int64_t i0, int64_t j0, const float* img) {
     const bool whole = (g.ld & 7) == 0;
 #pragma unroll 2
     for (int e = threadIdx.x; e < ROWS * (BN / 8); e += THREADS) {
@@ -71,7 +71,7 @@ __device__ __forceinline__ void emit(const Task& g, int which, int64_t i0, int64
 }
 
 template <class F, Side SA>
-__device__ __forceinline__ void run(const Task& g, int64_t number, const Buffers<F>& buffers) {
+__device__ __forceinline__ void run(const Job& g, int64_t number, const Buffers<F>& buffers) {
     constexpr int TM = F::TM, TN = F::TN, BM = F::BM, BN = F::BN;
     const Place at = place_of(number, g.tiles_i, g.tiles_j, g.splits, g.results);
     if (!at.inside) return;
@@ -118,7 +118,7 @@ __device__ __forceinline__ void run(const Task& g, int64_t number, const Buffers
 // Two products in one launch, the first with rows of the summed index along it.  (Neither waits for the other, and small ones do not fill the chip.)
 // Bound by the matrix units: the gradients of 4096 x 2048 x 2 * 8192 bf16 in 500 us (1.1 PFLOP/s), of 1500 x 1000 x 2 * 2731 fp32 in 192 (171 TFLOP/s of fp32 results).
 template <class F>
-__global__ __launch_bounds__(F::kThreads, 2) void k_products(Task first, Task second, int64_t firsts) {
+__global__ __launch_bounds__(F::kThreads, 2) void k_products(Job first, Job second, int64_t firsts) {
     PRODUCT_BUFFERS(F, buffers);
     // each XCD takes its eighth of the first product's tiles, then its share of the second's (they may take twice as long as the others)
     const unsigned total = gridDim.x * gridDim.y, lin = blockIdx.y * gridDim.x + blockIdx.x, xcd = lin & 7u, n = (unsigned)firsts;
@@ -130,14 +130,14 @@ __global__ __launch_bounds__(F::kThreads, 2) void k_products(Task first, Task se
         run<F, kCols>(second, before(total) - before(n) + at - mine, buffers);
 }
 template <class F, Side SA>
-__global__ __launch_bounds__(F::kThreads, 2) void k_product(Task g) {
+__global__ __launch_bounds__(F::kThreads, 2) void k_product(Job g) {
     PRODUCT_BUFFERS(F, buffers);
     run<F, SA>(g, tile::xcd_sequence(), buffers);
 }
 
 // Adds the parts of 32 x 32 results, each of four waves every fourth part, and finishes them.  Bound by memory, mostly the last-level cache: four parts of 4096 x 2048, 151 MB in 20 us.
 template <class F>
-__device__ __forceinline__ void join(const Task& g, int64_t number, f32x4 (&sums)[4][4][64], float* img) {
+__device__ __forceinline__ void join(const Job& g, int64_t number, f32x4 (&sums)[4][4][64], float* img) {
     constexpr int kBlocks = F::BM / 32 * (F::BN / 32), kEach = F::BM * F::BN / 4;
     const int64_t tile = number / kBlocks, tiles = g.tiles_i * g.tiles_j;
     if (tile >= tiles * g.results) return;
@@ -165,7 +165,7 @@ __device__ __forceinline__ void join(const Task& g, int64_t number, f32x4 (&sums
     emit<F::PLANES == 3, 32, 32, 256>(g, which, i0, j0, img);
 }
 template <class F>
-__global__ __launch_bounds__(256) void k_join(Task first, Task second, int64_t firsts) {
+__global__ __launch_bounds__(256) void k_join(Job first, Job second, int64_t firsts) {
     __shared__ f32x4 sums[4][4][64];
     __shared__ __align__(16) float img[32 * 32];
     const int64_t number = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
@@ -189,8 +189,8 @@ __global__ __launch_bounds__(256) void k_copy(Copies all) {
     }
 }
 
-Task task_of(const Product& p) {
-    return Task{p.a, p.b, p.depth, p.cut.tiles_i, p.cut.tiles_j, p.ld, p.segments, p.results, p.cut.splits, {p.out[0], p.out[1]}, reinterpret_cast<f32x4*>(p.parts), p.first};
+Job job_of(const Product& p) {
+    return Job{p.a, p.b, p.depth, p.cut.tiles_i, p.cut.tiles_j, p.ld, p.segments, p.results, p.cut.splits, {p.out[0], p.out[1]}, reinterpret_cast<f32x4*>(p.parts), p.first};
 }
 int64_t workgroups(const Product& p) { return p.cut.tiles() * p.cut.splits * p.results; }
 // Of the launch that adds the parts of a product; none if it leaves none, or others add to them.
@@ -285,7 +285,7 @@ int launches_of(const Cut& x, const Cut& y, bool several) {
 void multiply(const Product& p, hipStream_t stream) {
     with_form(p.f32, p.cut.side, [&](auto form) {
         using F = decltype(form);
-        const Task t = task_of(p);
+        const Job t = job_of(p);
         const dim3 grid = rows_of_workgroups(workgroups(p), F::kThreads);
         if (p.a_rows)
             CANVAS_LAUNCH((k_product<F, kRows>), grid, dim3(F::kThreads), 0, stream, t);
@@ -302,7 +302,7 @@ void multiply(const Product& x, const Product& y, hipStream_t stream) {
     }
     with_form(x.f32, x.cut.side, [&](auto form) {
         using F = decltype(form);
-        const Task t = task_of(x), u = task_of(y);
+        const Job t = job_of(x), u = job_of(y);
         CANVAS_LAUNCH((k_products<F>), rows_of_workgroups(workgroups(x) + workgroups(y), F::kThreads), dim3(F::kThreads), 0, stream, t, u, workgroups(x));
         const int64_t nx = joins<F>(x), ny = joins<F>(y);
         if (nx + ny) CANVAS_LAUNCH((k_join<F>), rows_of_workgroups(nx + ny, 256), dim3(256), 0, stream, t, u, nx);
