@@ -9,7 +9,7 @@
  *
  * as canvas_logprob.h has them for logits that are at hand.  Forward keeps the largest logit and the sums of each row; backward takes the
  * classes a piece at a time, computes a piece's logits again, the same ones, and leaves its gradients in the workspace only.  (Where that is faster, forward
- * leaves logits in the workspace, in fp32: those of up to 32 rows, and up to a GiB of others.)
+ * leaves logits in the workspace, in fp32: those of few rows, and up to a GiB of others.)
  *
  * A masked class is not looked at (its row of W may be NaN) and has a gradient of zeros.  A row of x that has nothing left (all classes masked
  * or -inf) has the log probability -inf, the entropy 0 and a gradient of zeros.  A token that is no class (negative, say, for positions

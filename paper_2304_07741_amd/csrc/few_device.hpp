@@ -1,5 +1,5 @@
-// The inner part of a product of a weight [n][k] with few rows x [rows][k], up to 16 NT of them: bound by reading the weight, which goes straight from
-// memory to the registers of the wave that multiplies it.
+// The inner part of a product of a weight [n][k] with few rows x [rows][k], 16 NT of them at a time: up to 32 rows bound by reading the weight, which goes straight from
+// memory to the registers of the wave that multiplies it; more rows by the matrix units (82 TFLOP/s in fp32, workgroups of 32 x 64 results).
 //
 // A workgroup takes R blocks of 16 rows of weights.  Its waves share out the summed index, AHEAD times 64 bytes of a row each in turn, and
 // add up through LDS in the order of the waves.  bf16: the 16 x 16 x 32 product of the matrix units; fp32: their 16 x 16 x 4 one, whose products
@@ -17,6 +17,19 @@ using product::f32x4;
 using tile::u32x4;
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
+// Loads of 64 bytes a row that are in flight, by what the registers of two or three waves a SIMD unit hold.
+constexpr int ahead(int blocks, int nt) { return blocks * nt > 4 ? 2 : 4; }
+// Whether this is the way for `rows` rows, by blocks of 64 of them, against `results` rows of weights.  Always up to 32.  More in fp32, where tiles need copies of both operands in planes first (10
+// bytes an element, and a launch) and do not share out the summed index, if that takes 1.25 times as long (`tiles`: us of the products in tiles).  Both in us, without copies and
+// with: pairs 64 x 1000 x 2 * 2731 16 and 55; 512 x 512 x 2 * 512 10 and 23; 250 x 4000 x 2 * 1000 57 and 146; 128 x 2000 x 2 * 8000 117 and 182; 256 x 2000 x 2 * 8000 225 and 174;
+// heads 64 x 1000 x 50000 112 and 228; 256 x 512 x 1000 14 and 18; 2000 x 300 x 1000 30 and 22.  bf16: 64 x 2048 x 2 * 8192 24 and 14, 512 x 512 x 2 * 512 5.6 and 5.9.
+constexpr int64_t kRows = 32, kMostRows = 4096;
+inline bool fits(bool f32, int64_t rows, int64_t results, int64_t features, double tiles) {
+    if (rows <= kRows || !f32 || rows > kMostRows) return rows <= kRows;
+    const int64_t turns = ((results + 31) / 32 * ((rows + 63) / 64) + 255) / 256;
+    const double here = 2 + (double)turns * (1.8 + 0.0128 * (double)features);
+    return 1.25 * here < 1.15 * tiles + 6 + 10.0 * (double)(rows + results) * (double)features / 4e6;
+}
 
 template <class T>
 struct Type;

@@ -232,12 +232,12 @@ __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
     const T* x[NT];
 #pragma unroll
     for (int n = 0; n < NT; n++) {
-        const int64_t t = n * 16 + (lane & 15);
+        const int64_t t = blockIdx.y * (16 * NT) + n * 16 + (lane & 15);
         x[n] = static_cast<const T*>(a.x) + (t < a.rows ? t : a.rows - 1) * a.features;
     }
     f32x4 sums[2];
-    few::accumulate<T, 2, NT, 4>(w, x, a.features, sums, shared);
-    const int64_t t = wave * 16 + (lane & 15), f = f0 + (lane >> 4) * 4;
+    few::accumulate<T, 2, NT, few::ahead(2, NT)>(w, x, a.features, sums, shared);
+    const int64_t t = blockIdx.y * (16 * NT) + wave * 16 + (lane & 15), f = f0 + (lane >> 4) * 4;
     if (wave >= NT || t >= a.rows) return;
 #pragma unroll
     for (int e = 0; e < 4; e++) {
@@ -325,7 +325,6 @@ __global__ __launch_bounds__(256) void k_grads(GradArgs a) {
     }
 }
 
-constexpr int kFewRows = 32;
 uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
 
 // f with the activation as a constant
@@ -340,12 +339,14 @@ void with_act(int act, F f) {
 }
 template <class T>
 void launch_few(int act, const FewArgs& a, hipStream_t stream) {
-    const dim3 grid((unsigned)((a.width + 15) / 16));
+    const dim3 grid((unsigned)((a.width + 15) / 16), (unsigned)((a.rows + 63) / 64));
     with_act(act, [&](auto kind) {
         if (a.rows <= 16)
             CANVAS_LAUNCH((k_few<T, 1, decltype(kind)::value>), grid, dim3(few::kThreads), 0, stream, a);
-        else
+        else if (a.rows <= few::kRows)
             CANVAS_LAUNCH((k_few<T, 2, decltype(kind)::value>), grid, dim3(few::kThreads), 0, stream, a);
+        else if constexpr (sizeof(T) == 4)
+            CANVAS_LAUNCH((k_few<T, 4, decltype(kind)::value>), grid, dim3(few::kThreads), 0, stream, a);
     });
 }
 template <class F>
@@ -380,9 +381,10 @@ void make_copies(const Shape& s, const Plan& p, const void* x, const void* w_gat
 Plan plan_of(const Shape& s) {
     Plan p;
     const int64_t ld = product::pitch(s.f32, s.features), wide = product::padded(s.f32, s.width);
-    p.few = s.rows <= kFewRows;
+    double tiles;
+    p.forward = product::cut_of(s.f32, s.rows, 2 * s.width, s.features, 1, false, &tiles);
+    p.few = few::fits(s.f32, s.rows, 2 * s.width, s.features, tiles);
     p.copies = (s.f32 || s.features % 8) && !(p.few && s.inference);
-    p.forward = product::cut_of(s.f32, s.rows, 2 * s.width, s.features, 1, false);
     const int64_t pairs = p.forward.side == 64 ? 64 : p.forward.side / 2;  // results of a tile's row (Paired)
     p.forward.tiles_j = (s.width + pairs - 1) / pairs;
     p.launches_fwd = 1 + (p.copies && !p.few);

@@ -16,7 +16,7 @@ struct Shape {
 };
 
 struct Plan {
-    bool few = false;      // few rows: the weights are read once, as they are
+    bool few = false;      // few rows (few::fits): operands are read as they are
     bool copies = false;   // products read copies of x and the weights: three planes of fp32 ones, rows of a multiple of 8 of bf16 ones
     product::Cut forward, dx, dw;
     int launches_fwd = 0, launches_bwd = 0;

@@ -193,7 +193,7 @@ struct FewArgs {
 // Blocks of 16 classes of a workgroup.  With 17 rows or more x is as much to read from the L2 as two blocks' weights from memory: four where there are enough of them (32 x 2048 x 131072:
 // 122 us instead of 135; 20 x 1000 x 50021 38 and 44; fp32 32 x 1024 x 50000 66 and 70; but 17 x 333 x 3000 12 instead of 10; 24 x 256 x 10000 the same).
 constexpr int64_t kManyClasses = 16384;
-int few_blocks(int64_t rows, int64_t classes) { return rows > 16 && classes > kManyClasses ? 4 : 2; }
+int few_blocks(int64_t rows, int64_t classes) { return rows > 16 && rows <= few::kRows && classes > kManyClasses ? 4 : 2; }
 // Bound by the weight's bytes: 4 x 2048 x 131072 bf16, 537 MB in 95 us, 5.7 TB/s.
 template <class T, int NT, int R>
 __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
@@ -208,18 +208,18 @@ __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
     }
 #pragma unroll
     for (int n = 0; n < NT; n++) {
-        const int64_t t = n * 16 + (lane & 15);
+        const int64_t t = blockIdx.y * (16 * NT) + n * 16 + (lane & 15);
         x[n] = static_cast<const T*>(a.x) + (t < a.rows ? t : a.rows - 1) * a.features;
     }
     // (asked for ahead of the weights: a workgroup's end is short then)
-    const int64_t t = wave * 16 + (lane & 15), c0 = first + (lane >> 4) * 4;
+    const int64_t t = blockIdx.y * (16 * NT) + wave * 16 + (lane & 15), c0 = first + (lane >> 4) * 4;
     const bool known = a.token && wave < NT && t < a.rows;
     const int64_t c = known ? a.tokens[t] - c0 : -1;
     uint32_t in[R];
 #pragma unroll
     for (int r = 0; r < R; r++) in[r] = wave < NT ? allowed4(a.mask, c0 + r * 16, a.classes) : 0u;
     f32x4 sums[R];
-    few::accumulate<T, R, NT, R == 2 ? 4 : 2>(w, x, a.features, sums, shared);
+    few::accumulate<T, R, NT, few::ahead(R, NT)>(w, x, a.features, sums, shared);
     if (wave >= NT) return;
     float z[R * 4];
 #pragma unroll
@@ -497,7 +497,6 @@ __global__ __launch_bounds__(256) void k_few_grads(FewGradArgs a) {
     for (int h = 0; h < P; h++) *reinterpret_cast<u32x4*>(a.to + t * a.ld + product::column<P>(col, h)) = w[h];
 }
 
-constexpr int kFewRows = 32;
 // Gradients of a piece's logits.  Every piece more adds to dx in memory once more; a longer one leaves the last-level cache (256 MB) before it is read.  Measured with pieces of
 // 64, 128, 300, 600 MB, us: 4096 x 1024 x 32768 (268 MB in all) 1138, 1029, 1014, 1014; 8192 x 512 x 16000 (262) 729, 678, 624, 624;
 // 8192 x 1024 x 32768 (537) -, 2114, 1982, 2021; 4096 x 2048 x 65536 (537) -, 3610, 3672, 3704.
@@ -513,13 +512,15 @@ uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
 template <class T>
 void launch_few(const FewArgs& a, hipStream_t stream) {
     const int blocks = few_blocks(a.rows, a.classes);
-    const dim3 grid((unsigned)((a.classes + 16 * blocks - 1) / (16 * blocks)));
+    const dim3 grid((unsigned)((a.classes + 16 * blocks - 1) / (16 * blocks)), (unsigned)((a.rows + 63) / 64));
     if (a.rows <= 16)
         CANVAS_LAUNCH((k_few<T, 1, 2>), grid, dim3(few::kThreads), 0, stream, a);
-    else if (blocks == 2)
+    else if (a.rows <= few::kRows && blocks == 2)
         CANVAS_LAUNCH((k_few<T, 2, 2>), grid, dim3(few::kThreads), 0, stream, a);
-    else
+    else if (a.rows <= few::kRows)
         CANVAS_LAUNCH((k_few<T, 2, 4>), grid, dim3(few::kThreads), 0, stream, a);
+    else if constexpr (sizeof(T) == 4)
+        CANVAS_LAUNCH((k_few<T, 4, 2>), grid, dim3(few::kThreads), 0, stream, a);
 }
 template <class F>
 void launch_logits(const FwdArgs& a, hipStream_t stream) {
@@ -541,11 +542,12 @@ Factor factor_of(const uint16_t* at, int64_t rows, int64_t ld) { return Factor{{
 Plan plan_of(const Shape& s) {
     Plan p;
     const int64_t ld = product::pitch(s.f32, s.features), planes = s.f32 ? 3 : 1;
-    p.few = s.rows <= kFewRows;
+    double tiles;
+    p.logits = product::cut_of(s.f32, s.classes, s.rows, s.features, 1, false, &tiles);
+    p.few = few::fits(s.f32, s.rows, s.classes, s.features, tiles);
     p.copies = (s.f32 || s.features % 8) && !(p.few && s.inference);
-    p.logits = product::cut_of(s.f32, s.classes, s.rows, s.features, 1, false);
-    const int few = 16 * few_blocks(s.rows, s.classes);
-    p.segments = (int)(p.few ? (s.classes + few - 1) / few : p.logits.tiles_i * 2);
+    const int segment = 16 * few_blocks(s.rows, s.classes);
+    p.segments = (int)(p.few ? (s.classes + segment - 1) / segment : p.logits.tiles_i * 2);
     p.launches_fwd = 2 + (p.copies && !p.few);
     p.most_tiles = p.few ? p.segments : p.logits.tiles();
     uint64_t at = 0;

@@ -245,7 +245,7 @@ Cut cut_with(const Speed& v, int64_t rows, int64_t cols, int64_t depth, int resu
     return best;
 }
 
-Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, bool may_split) {
+Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, bool may_split, double* us) {
     Cut best;
     double least = 0, t;
     for (const Speed& v : kSpeeds[f32]) {
@@ -255,6 +255,7 @@ Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, boo
             best = c;
         }
     }
+    if (us) *us = least;
     return best;
 }
 

@@ -44,7 +44,8 @@ struct Product {
     bool first = true, last = true;
 };
 
-Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, bool may_split);
+// `us`: about what it takes.
+Cut cut_of(bool f32, int64_t rows, int64_t cols, int64_t depth, int results, bool may_split, double* us = nullptr);
 // Of two products that one launch may take if their tiles are alike.
 struct Size {
     int64_t rows, cols, depth;
