@@ -18,8 +18,8 @@
  * of its row NaN, and dW with them.
  *
  * All sums are fp32.  bf16 plans: dlogit is rounded to bf16 once, as the operand of the products behind it; dx and dW are fp32 sums rounded
- * once.  fp32 plans: every operand is taken as three bf16 numbers that together hold its 24 bits, and a product adds the six pairings
- * that fp32 can tell from nothing, which is as exact as products in fp32; an infinity among the operands acts as NaN.  Deterministic: no
+ * once.  fp32 plans: products are those of fp32, or, of larger operands, each is taken as three bf16 numbers that together hold its 24 bits and a product adds the
+ * six pairings that fp32 can tell from nothing, which is as exact; an infinity among the operands may act as NaN.  Deterministic: no
  * atomics, sums in a fixed order.
  *
  * Pointers: device pointers, owned by the caller, 16-byte aligned, contiguous; x, W and their gradients in the plan's element type.  What a

@@ -507,6 +507,7 @@ def canvas_clip_compile(counts, types, out_types=None):
     h = ctypes.c_void_p()
     _check(load().canvas_clip_compile(n, (ctypes.c_int64 * max(1, n))(*[int(c) for c in counts]), kinds(types), None if out_types is None else kinds(out_types),
                                       ctypes.byref(h)))
+    h.tensors = n
     return h
 
 
@@ -518,6 +519,8 @@ def canvas_clip_query(handle):
 
 def canvas_clip_step(handle, grads, outs, max_norm, norm, scale, workspace):
     """grads, outs: lists of tensors (outs None: the norm alone), as many as the plan has."""
+    if any(len(tensors) != handle.tensors for tensors in (grads, grads if outs is None else outs)):
+        raise ValueError(f"{handle.tensors} tensors are needed")
     addresses = lambda tensors: (ctypes.c_void_p * max(1, len(tensors)))(*[t.data_ptr() for t in tensors])  # noqa: E731
     _check(load().canvas_clip_step(handle, addresses(grads), None if outs is None else addresses(outs), float(max_norm), _ptr(norm), _ptr(scale), _ptr(workspace),
                                    _bytes(workspace), _stream()))

@@ -5,6 +5,7 @@ import os
 import re
 
 import pytest
+import torch
 
 from paper_2304_07741_amd import binding as B
 
@@ -202,3 +203,12 @@ def test_clip_calls_refuse(lib):
     assert lib.canvas_clip_step(h, array((P(0), P(0))), array((P(0), P(0))), 1.0, P(4), None, P(6), 1 << 20, None) == -4
     B.canvas_clip_destroy(h)
     assert lib.canvas_clip_query(None, ctypes.byref(B.CanvasClipInfo())) == -4
+
+
+def test_clip_step_wants_as_many_tensors_as_its_plan_has(lib):
+    h = B.canvas_clip_compile([8, 8], [B.CANVAS_F32] * 2)
+    t = torch.zeros(8)
+    for grads, outs in (([t], None), ([t] * 3, [t] * 3), ([t] * 2, [t])):
+        with pytest.raises(ValueError, match="2 tensors are needed"):
+            B.canvas_clip_step(h, grads, outs, 1.0, t[:1], None, t)
+    B.canvas_clip_destroy(h)
