@@ -1,5 +1,5 @@
 // The inner part of a product of a weight [n][k] with few rows x [rows][k], 16 NT of them at a time: up to 32 rows bound by reading the weight, which goes straight from
-// memory to the registers of the wave that multiplies it; more rows by the matrix units (82 TFLOP/s in fp32, workgroups of 32 x 64 results).
+// memory to the registers of the wave that multiplies it; more rows by the matrix units (92 TFLOP/s in fp32, workgroups of 32 x 64 results; 82 with the four products of a pair of loads one after the other on one sum).
 //
 // A workgroup takes R blocks of 16 rows of weights.  Its waves share out the summed index, AHEAD times 64 bytes of a row each in turn, and
 // add up through LDS in the order of the waves.  bf16: the 16 x 16 x 32 product of the matrix units; fp32: their 16 x 16 x 4 one, whose products
@@ -21,13 +21,13 @@ constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int ahead(int blocks, int nt) { return blocks * nt > 4 ? 2 : 4; }
 // Whether this is the way for `rows` rows, by blocks of 64 of them, against `results` rows of weights.  Always up to 32.  More in fp32, where tiles need copies of both operands in planes first (10
 // bytes an element, and a launch) and do not share out the summed index, if that takes 1.25 times as long (`tiles`: us of the products in tiles).  Both in us, without copies and
-// with: pairs 64 x 1000 x 2 * 2731 16 and 55; 512 x 512 x 2 * 512 10 and 23; 250 x 4000 x 2 * 1000 57 and 146; 128 x 2000 x 2 * 8000 117 and 182; 256 x 2000 x 2 * 8000 225 and 174;
-// heads 64 x 1000 x 50000 112 and 228; 256 x 512 x 1000 14 and 18; 2000 x 300 x 1000 30 and 22.  bf16: 64 x 2048 x 2 * 8192 24 and 14, 512 x 512 x 2 * 512 5.6 and 5.9.
+// with: pairs 64 x 1000 x 2 * 2731 16 and 55; 512 x 512 x 2 * 512 10 and 23; 250 x 4000 x 2 * 1000 50 and 146; 128 x 2000 x 2 * 8000 103 and 182; 256 x 2000 x 2 * 8000 194 and 173;
+// heads 64 x 1000 x 50000 109 and 228; 256 x 512 x 1000 14 and 18; 2000 x 300 x 1000 30 and 22.  bf16: 64 x 2048 x 2 * 8192 24 and 14, 512 x 512 x 2 * 512 5.6 and 5.9.
 constexpr int64_t kRows = 32, kMostRows = 4096;
 inline bool fits(bool f32, int64_t rows, int64_t results, int64_t features, double tiles) {
     if (rows <= kRows || !f32 || rows > kMostRows) return rows <= kRows;
     const int64_t turns = ((results + 31) / 32 * ((rows + 63) / 64) + 255) / 256;
-    const double here = 2 + (double)turns * (1.8 + 0.0128 * (double)features);
+    const double here = 2 + (double)turns * (1.8 + 0.0114 * (double)features);
     return 1.25 * here < 1.15 * tiles + 6 + 10.0 * (double)(rows + results) * (double)features / 4e6;
 }
 
@@ -36,14 +36,15 @@ struct Type;
 template <>
 struct Type<uint16_t> {
     static constexpr int kEach = 8;  // elements of 16 bytes
-    static __device__ __forceinline__ void multiply(const u32x4& a, const u32x4& b, f32x4& c) { c = tile::mfma32(a, b, c); }
+    static constexpr int kProducts = 1;  // of 16 bytes of each operand
+    static __device__ __forceinline__ void multiply(const u32x4& a, const u32x4& b, int, f32x4& c) { c = tile::mfma32(a, b, c); }
 };
 template <>
 struct Type<float> {
     static constexpr int kEach = 4;
-    static __device__ __forceinline__ void multiply(const u32x4& a, const u32x4& b, f32x4& c) {
-#pragma unroll
-        for (int e = 0; e < 4; e++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
+    static constexpr int kProducts = 4;
+    static __device__ __forceinline__ void multiply(const u32x4& a, const u32x4& b, int e, f32x4& c) {
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
     }
 };
 
@@ -89,9 +90,11 @@ __device__ __forceinline__ void accumulate(const T* const (&w)[R], const T* cons
 #pragma unroll
         for (int u = 0; u < AHEAD; u++)
 #pragma unroll
-            for (int r = 0; r < R; r++)
+            for (int e = 0; e < Y::kProducts; e++)
 #pragma unroll
-                for (int n = 0; n < NT; n++) Y::multiply(t.w[r][u], t.x[n][u], acc[r][n]);
+                for (int r = 0; r < R; r++)
+#pragma unroll
+                    for (int n = 0; n < NT; n++) Y::multiply(t.w[r][u], t.x[n][u], e, acc[r][n]);
     };
     const int64_t whole = depth / kTurn;
     int64_t turn = wave;
@@ -115,9 +118,11 @@ __device__ __forceinline__ void accumulate(const T* const (&w)[R], const T* cons
 #pragma unroll
             for (int n = 0; n < NT; n++) b[n] = load_end(x[n], k + mine, depth);
 #pragma unroll
-            for (int r = 0; r < R; r++)
+            for (int e = 0; e < Y::kProducts; e++)
 #pragma unroll
-                for (int n = 0; n < NT; n++) Y::multiply(a[r], b[n], acc[r][n]);
+                for (int r = 0; r < R; r++)
+#pragma unroll
+                    for (int n = 0; n < NT; n++) Y::multiply(a[r], b[n], e, acc[r][n]);
         }
     }
 #pragma unroll
