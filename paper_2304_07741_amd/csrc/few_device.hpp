@@ -48,6 +48,11 @@ struct Type<float> {
     }
 };
 
+// Nothing that a lane leaves in LDS for another of its wave changes places with what that one reads.
+__device__ __forceinline__ void in_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 template <class T>
 __device__ __forceinline__ u32x4 load16(const T* p) {
     u32x4 v;
@@ -65,14 +70,32 @@ __device__ __forceinline__ u32x4 load_end(const T* row, int64_t k, int64_t end) 
     return v;
 }
 
-// sums[r][t]: of weight rows `w[r]` (this lane's row of the block) and rows `x[t]`; whole sums in waves 0 .. NT - 1, wave t those of rows 16 t ..:
+// Which row of a block of 16 a lane loads, and which 16 of 64 bytes.  As the matrix units want them, lane % 16: no two lanes beside each other share a line, which the L1 serves one after the other.
+// STAGED: four lanes beside each other take 64 bytes of a row, and the wave's own piece of LDS gives each lane its operands.  That is for bf16, most where rows begin anywhere: pairs, us,
+// 7 x 3869 x 2 * 530 10 instead of 25, 27 x 3869 x 2 * 530 13 and 36, 32 x 2048 x 2 * 8192 15.3 and 17, 4 x 2048 x 2 * 8192 12 and 12; heads of 7 x 1001 x 50000 45 and 50, 32 x 2048 x 131072
+// 117 and 121, but of 4 x 2048 x 131072 107 instead of 102.  fp32, whose matrix instructions take longer: 128 x 2000 x 2 * 8000 107 instead of 103, 512 x 512 x 2 * 512 8.8 and 10.3.
+template <bool STAGED>
+struct Lanes {
+    static constexpr bool kStaged = STAGED;
+    static __device__ __forceinline__ int row() { return kStaged ? (threadIdx.x & 63) >> 2 : threadIdx.x & 15; }
+    static __device__ __forceinline__ int piece() { return kStaged ? threadIdx.x & 3 : (threadIdx.x & 63) >> 4; }
+};
+// Pieces of row r lie at place piece ^ (r / 4), so that 16 lanes read 16 pieces on different banks.
+__device__ __forceinline__ int place_of(int row, int piece) { return row * 4 + (piece ^ (row >> 2)); }
+// f32x4 elements of LDS that accumulate() takes.
+template <bool STAGED, int R, int NT>
+constexpr int kShared = kWaves * 64 * (R * NT > R + NT || !STAGED ? R * NT : R + NT);
+
+// sums[r][t]: of weight rows `w[r]` (the row that this lane loads of the block) and rows `x[t]`; whole sums in waves 0 .. NT - 1, wave t those of rows 16 t ..:
 // register e of a lane is weight row (lane / 16) * 4 + e, row lane % 16 of x.
-template <class T, int R, int NT, int AHEAD>
+template <bool STAGED, class T, int R, int NT, int AHEAD>
 __device__ __forceinline__ void accumulate(const T* const (&w)[R], const T* const (&x)[NT], int64_t depth, f32x4 (&sums)[R], f32x4* shared) {
     using Y = Type<T>;
     constexpr int kStep = 4 * Y::kEach, kTurn = kStep * AHEAD;  // elements of a row that a wave takes per load, and per turn
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t mine = (lane >> 4) * Y::kEach;
+    const int64_t mine = Lanes<STAGED>::piece() * Y::kEach;
+    u32x4* const stage = reinterpret_cast<u32x4*>(shared) + wave * ((R + NT) * 64);
+    const int put = place_of(Lanes<STAGED>::row(), Lanes<STAGED>::piece()), get = place_of(lane & 15, lane >> 4);
     f32x4 acc[R][NT] = {};
     struct Turn {
         u32x4 w[R][AHEAD], x[NT][AHEAD];
@@ -86,15 +109,40 @@ __device__ __forceinline__ void accumulate(const T* const (&w)[R], const T* cons
             for (int n = 0; n < NT; n++) t.x[n][u] = load16(x[n] + k + u * kStep + mine);
         }
     };
+    // of 64 bytes of each row
+    auto products = [&](const u32x4 (&a)[R], const u32x4 (&b)[NT]) {
+#pragma unroll
+        for (int e = 0; e < Y::kProducts; e++)
+#pragma unroll
+            for (int r = 0; r < R; r++)
+#pragma unroll
+                for (int n = 0; n < NT; n++) Y::multiply(a[r], b[n], e, acc[r][n]);
+    };
+    auto step = [&](const u32x4 (&a)[R], const u32x4 (&b)[NT]) {
+        if (!STAGED) return products(a, b);
+        u32x4 p[R], q[NT];
+        in_order();  // (a wave's accesses to LDS are)
+#pragma unroll
+        for (int r = 0; r < R; r++) stage[r * 64 + put] = a[r];
+#pragma unroll
+        for (int n = 0; n < NT; n++) stage[(R + n) * 64 + put] = b[n];
+        in_order();
+#pragma unroll
+        for (int r = 0; r < R; r++) p[r] = stage[r * 64 + get];
+#pragma unroll
+        for (int n = 0; n < NT; n++) q[n] = stage[(R + n) * 64 + get];
+        products(p, q);
+    };
     auto multiply = [&](const Turn& t) {
 #pragma unroll
-        for (int u = 0; u < AHEAD; u++)
+        for (int u = 0; u < AHEAD; u++) {
+            u32x4 a[R], b[NT];
 #pragma unroll
-            for (int e = 0; e < Y::kProducts; e++)
+            for (int r = 0; r < R; r++) a[r] = t.w[r][u];
 #pragma unroll
-                for (int r = 0; r < R; r++)
-#pragma unroll
-                    for (int n = 0; n < NT; n++) Y::multiply(t.w[r][u], t.x[n][u], e, acc[r][n]);
+            for (int n = 0; n < NT; n++) b[n] = t.x[n][u];
+            step(a, b);
+        }
     };
     const int64_t whole = depth / kTurn;
     int64_t turn = wave;
@@ -117,14 +165,10 @@ __device__ __forceinline__ void accumulate(const T* const (&w)[R], const T* cons
             for (int r = 0; r < R; r++) a[r] = load_end(w[r], k + mine, depth);
 #pragma unroll
             for (int n = 0; n < NT; n++) b[n] = load_end(x[n], k + mine, depth);
-#pragma unroll
-            for (int e = 0; e < Y::kProducts; e++)
-#pragma unroll
-                for (int r = 0; r < R; r++)
-#pragma unroll
-                    for (int n = 0; n < NT; n++) Y::multiply(a[r], b[n], e, acc[r][n]);
+            step(a, b);
         }
     }
+    if (STAGED) __syncthreads();
 #pragma unroll
     for (int r = 0; r < R; r++)
 #pragma unroll

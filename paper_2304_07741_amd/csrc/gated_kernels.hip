@@ -225,18 +225,19 @@ struct FewArgs {
 // 16 results of y for all rows of x by a workgroup; bound by the weights' bytes: 4 x 2048 x 2 * 8192 bf16, 67 MB in 12.4 us, 5.4 TB/s.
 template <class T, int NT, int ACT>
 __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
-    __shared__ f32x4 shared[2 * NT * few::kWaves * 64];
+    constexpr bool kStaged = sizeof(T) == 2;
+    __shared__ f32x4 shared[few::kShared<kStaged, 2, NT>];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t f0 = (int64_t)blockIdx.x * 16, row = f0 + (lane & 15) < a.width ? f0 + (lane & 15) : a.width - 1;
+    const int64_t f0 = (int64_t)blockIdx.x * 16, mine = few::Lanes<kStaged>::row(), row = f0 + mine < a.width ? f0 + mine : a.width - 1;
     const T* const w[2] = {static_cast<const T*>(a.w_gate) + row * a.features, static_cast<const T*>(a.w_up) + row * a.features};
     const T* x[NT];
 #pragma unroll
     for (int n = 0; n < NT; n++) {
-        const int64_t t = blockIdx.y * (16 * NT) + n * 16 + (lane & 15);
+        const int64_t t = blockIdx.y * (16 * NT) + n * 16 + mine;
         x[n] = static_cast<const T*>(a.x) + (t < a.rows ? t : a.rows - 1) * a.features;
     }
     f32x4 sums[2];
-    few::accumulate<T, 2, NT, few::ahead(2, NT)>(w, x, a.features, sums, shared);
+    few::accumulate<kStaged, T, 2, NT, few::ahead(2, NT)>(w, x, a.features, sums, shared);
     const int64_t t = blockIdx.y * (16 * NT) + wave * 16 + (lane & 15), f = f0 + (lane >> 4) * 4;
     if (wave >= NT || t >= a.rows) return;
 #pragma unroll

@@ -190,25 +190,25 @@ struct FewArgs {
     float* token;
     float* logits;  // for backward, [rows][classes to the next multiple of 8]
 };
-// Blocks of 16 classes of a workgroup.  With 17 rows or more x is as much to read from the L2 as two blocks' weights from memory: four where there are enough of them (32 x 2048 x 131072:
-// 122 us instead of 135; 20 x 1000 x 50021 38 and 44; fp32 32 x 1024 x 50000 66 and 70; but 17 x 333 x 3000 12 instead of 10; 24 x 256 x 10000 the same).
+// Blocks of 16 classes of a workgroup.  With 17 rows or more x is as much to read from the L2 as two blocks' weights from memory: four where there are enough of them (32 x 2048 x 131072,
+// without LDS between: 122 us instead of 135; 20 x 1000 x 50021 38 and 44; fp32 32 x 1024 x 50000 66 and 70; but 17 x 333 x 3000 12 instead of 10; 24 x 256 x 10000 the same).
 constexpr int64_t kManyClasses = 16384;
 int few_blocks(int64_t rows, int64_t classes) { return rows > 16 && rows <= few::kRows && classes > kManyClasses ? 4 : 2; }
 // Bound by the weight's bytes: 4 x 2048 x 131072 bf16, 537 MB in 95 us, 5.7 TB/s.
-template <class T, int NT, int R>
+template <class T, int NT, int R, bool STAGED>
 __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
-    __shared__ f32x4 shared[R * NT * few::kWaves * 64];
+    __shared__ f32x4 shared[few::kShared<STAGED, R, NT>];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t first = (int64_t)blockIdx.x * (16 * R);
+    const int64_t first = (int64_t)blockIdx.x * (16 * R), mine = few::Lanes<STAGED>::row();
     const T *w[R], *x[NT];
 #pragma unroll
     for (int r = 0; r < R; r++) {
-        const int64_t c = first + r * 16 + (lane & 15);
+        const int64_t c = first + r * 16 + mine;
         w[r] = static_cast<const T*>(a.weight) + (c < a.classes ? c : a.classes - 1) * a.features;
     }
 #pragma unroll
     for (int n = 0; n < NT; n++) {
-        const int64_t t = blockIdx.y * (16 * NT) + n * 16 + (lane & 15);
+        const int64_t t = blockIdx.y * (16 * NT) + n * 16 + mine;
         x[n] = static_cast<const T*>(a.x) + (t < a.rows ? t : a.rows - 1) * a.features;
     }
     // (asked for ahead of the weights: a workgroup's end is short then)
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
 #pragma unroll
     for (int r = 0; r < R; r++) in[r] = wave < NT ? allowed4(a.mask, c0 + r * 16, a.classes) : 0u;
     f32x4 sums[R];
-    few::accumulate<T, R, NT, few::ahead(R, NT)>(w, x, a.features, sums, shared);
+    few::accumulate<STAGED, T, R, NT, few::ahead(R, NT)>(w, x, a.features, sums, shared);
     if (wave >= NT) return;
     float z[R * 4];
 #pragma unroll
@@ -513,14 +513,17 @@ template <class T>
 void launch_few(const FewArgs& a, hipStream_t stream) {
     const int blocks = few_blocks(a.rows, a.classes);
     const dim3 grid((unsigned)((a.classes + 16 * blocks - 1) / (16 * blocks)), (unsigned)((a.rows + 63) / 64));
-    if (a.rows <= 16)
-        CANVAS_LAUNCH((k_few<T, 1, 2>), grid, dim3(few::kThreads), 0, stream, a);
+    constexpr bool kStaged = sizeof(T) == 2;
+    if (a.rows <= 16 && kStaged && a.features % 8)
+        CANVAS_LAUNCH((k_few<T, 1, 2, kStaged>), grid, dim3(few::kThreads), 0, stream, a);
+    else if (a.rows <= 16)
+        CANVAS_LAUNCH((k_few<T, 1, 2, false>), grid, dim3(few::kThreads), 0, stream, a);
     else if (a.rows <= few::kRows && blocks == 2)
-        CANVAS_LAUNCH((k_few<T, 2, 2>), grid, dim3(few::kThreads), 0, stream, a);
+        CANVAS_LAUNCH((k_few<T, 2, 2, kStaged>), grid, dim3(few::kThreads), 0, stream, a);
     else if (a.rows <= few::kRows)
-        CANVAS_LAUNCH((k_few<T, 2, 4>), grid, dim3(few::kThreads), 0, stream, a);
+        CANVAS_LAUNCH((k_few<T, 2, 4, kStaged>), grid, dim3(few::kThreads), 0, stream, a);
     else if constexpr (sizeof(T) == 4)
-        CANVAS_LAUNCH((k_few<T, 4, 2>), grid, dim3(few::kThreads), 0, stream, a);
+        CANVAS_LAUNCH((k_few<T, 4, 2, kStaged>), grid, dim3(few::kThreads), 0, stream, a);
 }
 template <class F>
 void launch_logits(const FwdArgs& a, hipStream_t stream) {
