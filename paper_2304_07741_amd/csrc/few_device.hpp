@@ -1,5 +1,5 @@
-// The inner part of a product of a weight [n][k] with few rows x [rows][k], 16 NT of them at a time: up to 32 rows bound by reading the weight, which goes straight from
-// memory to the registers of the wave that multiplies it; more rows by the matrix units (92 TFLOP/s in fp32, workgroups of 32 x 64 results; 82 with the four products of a pair of loads one after the other on one sum).
+// The inner part of a product of a weight [n][k] with few rows x [rows][k], 16 NT of them at a time: up to 32 rows bound by reading the weight, which goes from
+// memory to the registers of the wave that multiplies it, in most bf16 products through that wave's piece of LDS (Lanes); more rows by the matrix units (92 TFLOP/s in fp32, workgroups of 32 x 64 results; 82 with the four products of a pair of loads one after the other on one sum).
 //
 // A workgroup takes R blocks of 16 rows of weights.  Its waves share out the summed index, AHEAD times 64 bytes of a row each in turn, and
 // add up through LDS in the order of the waves.  bf16: the 16 x 16 x 32 product of the matrix units; fp32: their 16 x 16 x 4 one, whose products
