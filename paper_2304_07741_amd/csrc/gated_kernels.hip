@@ -14,6 +14,7 @@
 #include "few_device.hpp"
 #include "launch.hpp"
 #include "product_device.hpp"
+#include "row_util.hpp"
 #include "tile_util.hpp"
 
 namespace canvas {
@@ -267,32 +268,20 @@ template <bool F32, int ACT>
 __global__ __launch_bounds__(256) void k_grads(GradArgs a) {
     constexpr int P = F32 ? 3 : 1;
     const int64_t wide = a.ld / 8, n = a.rows * wide;
-    const bool whole = (a.width & 7) == 0;
     for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < n; k += (int64_t)gridDim.x * 256) {
-        const int64_t row = k / wide, col = (k - row * wide) * 8, from = row * a.width + col;
+        const int64_t row = k / wide, col = (k - row * wide) * 8;
         float g[8], u[8];
         Kept<F32>{a.kept, a.plane}.get8(k * 8, g, u);
+        using T = std::conditional_t<F32, float, uint16_t>;
+        T given[8];
+        rows::load8(static_cast<const T*>(a.dy) + row * a.width, col, a.width, given);
         float dy[8];
-        if (F32) {
-            const float* p = static_cast<const float*>(a.dy) + from;
-            if (whole) {
-                const f32x4 v[2] = {*reinterpret_cast<const f32x4*>(p), *reinterpret_cast<const f32x4*>(p + 4)};
 #pragma unroll
-                for (int e = 0; e < 8; e++) dy[e] = v[e >> 2][e & 3];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; e++) dy[e] = col + e < a.width ? p[e] : 0.f;
-            }
-        } else {
-            const uint16_t* p = static_cast<const uint16_t*>(a.dy) + from;
-            if (whole) {
-                const u32x4 v = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-                for (int e = 0; e < 8; e++) dy[e] = (e & 1) ? tile::hi_f32(v[e >> 1]) : tile::lo_f32(v[e >> 1]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; e++) dy[e] = col + e < a.width ? bf16_to_f32(p[e]) : 0.f;
-            }
+        for (int e = 0; e < 8; e++) {
+            if constexpr (F32)
+                dy[e] = given[e];
+            else
+                dy[e] = bf16_to_f32(given[e]);
         }
         float dg[8], du[8];
 #pragma unroll
