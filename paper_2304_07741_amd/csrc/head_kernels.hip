@@ -257,7 +257,7 @@ struct RowArgs {
 __global__ __launch_bounds__(256) void k_rows(RowArgs a) {
     __shared__ Sums part[256];
     const int mine = threadIdx.x & (a.across - 1), turn = threadIdx.x / a.across, turns = 256 / a.across;
-    const int64_t t = (int64_t)blockIdx.x * a.across + mine;
+    const int64_t t = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * a.across + mine;
     Sums r{kLowest, 0.f, 0.f};
     if (t < a.rows) {
         constexpr int kAhead = 4;
