@@ -245,7 +245,7 @@ __device__ __forceinline__ void accumulate(const Factor& a, const Factor& b, int
     // pair of 3320 summands: 5e-7 instead of 1.4e-6; gradients of a head of 16 x 1624 x 1023: 7e-7 instead of 1.7e-6; for half a percent of the time.
     f32x16 low[TM][TN] = {};
     auto multiply = [&](const Operands& o) {
-        // pairings of planes, the smallest products first; what is left out is below 2^-24 of a term
+        // pairings of planes, the smallest products first; what is left out is 2^-24 of a term at most (split)
         constexpr int kPairings = P == 1 ? 1 : 6, kOfA[6] = {2, 0, 1, 1, 0, 0}, kOfB[6] = {0, 2, 1, 0, 1, 0};
 #pragma unroll
         for (int h = 0; h < kPairings; h++)
@@ -308,18 +308,21 @@ __device__ __forceinline__ void accumulate(const Factor& a, const Factor& b, int
     }
 }
 
-// The bits of a value by its first 8, the next 8 and the rest: a sum of three bf16 numbers that is exact (but for what lies below the smallest of
-// bf16's numbers).  Not finite: the first alone.
+// A value as the sum of three bf16 numbers: what is left of it rounded to nearest, twice, and the rest, which eight bits hold (but for what lies below the smallest
+// of bf16's numbers).  The second is 2^-8 of the value at most and the third 2^-17, of either sign, so that what a product leaves out of the nine, 2^-24 of it at most, adds up to
+// nothing.  Cut where rounding would make an infinity.  Not finite: the first alone.
 __device__ __forceinline__ void split(float v, uint16_t (&part)[3]) {
-    const uint32_t u = __float_as_uint(v), top = u & 0xffff0000u;
-    part[0] = (uint16_t)(u >> 16);
+    const uint32_t u = __float_as_uint(v);
     if ((u & 0x7f800000u) == 0x7f800000u) {
+        part[0] = (uint16_t)(u >> 16);
         part[0] = (u & 0x7fffffu) ? (uint16_t)(part[0] | 0x40u) : part[0];
         part[1] = part[2] = 0;
         return;
     }
+    const uint32_t near = (u + 0x8000u) & 0xffff0000u, top = (near & 0x7f800000u) == 0x7f800000u ? u & 0xffff0000u : near;
     const float r = v - __uint_as_float(top);
-    const uint32_t mid = __float_as_uint(r) & 0xffff0000u;
+    const uint32_t mid = (__float_as_uint(r) + 0x8000u) & 0xffff0000u;
+    part[0] = (uint16_t)(top >> 16);
     part[1] = (uint16_t)(mid >> 16);
     part[2] = (uint16_t)(__float_as_uint(r - __uint_as_float(mid)) >> 16);
 }
