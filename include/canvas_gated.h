@@ -9,8 +9,8 @@
  *
  * Rows are maps of one pixel; the weights are laid out as those of an FC with one group (weight_shape [1, width, features]).
  *
- * All sums are fp32.  bf16 plans: g and u stay in fp32 up to y; 20 bits of each are kept for backward (half a step is 2^-12), whose dg and du are
- * computed in fp32 and rounded to bf16 once, as operands of the products behind them; dx, dWg and dWu are fp32 sums rounded once.  fp32 plans: products are those of fp32, or, of larger
+ * All sums are fp32.  bf16 plans: g and u stay in fp32 up to y, and up to backward, whose dg and du are computed in fp32 and rounded to bf16 once,
+ * as operands of the products behind them; dx, dWg and dWu are fp32 sums rounded once.  fp32 plans: products are those of fp32, or, of larger
  * operands, each is taken as three bf16 numbers that together hold its 24 bits (smaller ones than 2^-100 lose their last) and a product adds the six largest of their nine; what
  * is left out is half a step of fp32 at most, of either sign.  An infinity among the operands may act as NaN.  Deterministic: no atomics, sums in a fixed order.
  *

@@ -48,72 +48,30 @@ __device__ __forceinline__ float act_of(float g, float& slope) {
     return g * sig;
 }
 
-// What backward needs of g and u.  fp32 plans: both as they are.  bf16 plans: 20 bits of each, sign, exponent and 11 of the mantissa, an
-// eighth of the rounding that dg and du take on as operands of the products: the first 16 of g and u in a word, four more of each in a byte.  That is 5 bytes
-// to write and to read again instead of 8, of 7 and 11 in all: 4096 x 2048 x 8192 forward and backward 807 us instead of 854.
-template <bool F32>
+// What backward needs of g and u: both as they are, in fp32.  (20 bits of each in bf16 plans would be 5 bytes an element to write and to read again instead of 8:
+// 4096 x 2048 x 8192 forward and backward 801 us instead of 832, with gradients that are no longer those of g and u.)
 struct Kept {
-    char* at;         // fp32: g, then u; bf16: words, then bytes
-    int64_t plane;    // elements
-    static constexpr int kBytes = F32 ? 8 : 5;  // of an element
+    float* at;      // g, then u
+    int64_t plane;  // elements
+    static constexpr int kBytes = 8;  // of an element
 
-    static __device__ __forceinline__ uint32_t bits20(float v) {
-        const uint32_t u = __float_as_uint(v), r = u + 0x800u;
-        return ((r & 0x7f800000u) == 0x7f800000u ? u : r) >> 12;  // (what would round to infinity, infinities and NaN are cut)
-    }
-    static __device__ __forceinline__ uint32_t word(uint32_t g, uint32_t u) { return g >> 4 | (u >> 4) << 16; }
-    static __device__ __forceinline__ uint32_t rest(uint32_t g, uint32_t u) { return (g & 15u) | (u & 15u) << 4; }
     __device__ __forceinline__ void put1(int64_t i, float g, float u) const {
-        if (F32) {
-            reinterpret_cast<float*>(at)[i] = g;
-            reinterpret_cast<float*>(at)[plane + i] = u;
-        } else {
-            const uint32_t bg = bits20(g), bu = bits20(u);
-            reinterpret_cast<uint32_t*>(at)[i] = word(bg, bu);
-            reinterpret_cast<uint8_t*>(at + 4 * plane)[i] = (uint8_t)rest(bg, bu);
-        }
+        at[i] = g;
+        at[plane + i] = u;
     }
     // eight elements from i on, a multiple of 8
     __device__ __forceinline__ void put8(int64_t i, const f32x4 (&g)[2], const f32x4 (&u)[2]) const {
-        if (F32) {
-            f32x4 *to = reinterpret_cast<f32x4*>(at) + i / 4, *to_u = to + plane / 4;
-            to[0] = g[0];
-            to[1] = g[1];
-            to_u[0] = u[0];
-            to_u[1] = u[1];
-        } else {
-            u32x4 w[2];
-            uint32_t b[2] = {0, 0};
-#pragma unroll
-            for (int k = 0; k < 8; k++) {
-                const uint32_t bg = bits20(g[k >> 2][k & 3]), bu = bits20(u[k >> 2][k & 3]);
-                w[k >> 2][k & 3] = word(bg, bu);
-                b[k >> 2] |= rest(bg, bu) << ((k & 3) * 8);
-            }
-            u32x4* to = reinterpret_cast<u32x4*>(at) + i / 4;
-            to[0] = w[0];
-            to[1] = w[1];
-            __builtin_memcpy(at + 4 * plane + i, b, 8);
-        }
+        f32x4 *to = reinterpret_cast<f32x4*>(at) + i / 4, *to_u = to + plane / 4;
+        to[0] = g[0];
+        to[1] = g[1];
+        to_u[0] = u[0];
+        to_u[1] = u[1];
     }
     __device__ __forceinline__ void get8(int64_t i, float (&g)[8], float (&u)[8]) const {
-        if (F32) {
-            const f32x4 *from = reinterpret_cast<const f32x4*>(at) + i / 4, *from_u = from + plane / 4;
-            const f32x4 v[4] = {from[0], from[1], from_u[0], from_u[1]};
+        const f32x4 *from = reinterpret_cast<const f32x4*>(at) + i / 4, *from_u = from + plane / 4;
+        const f32x4 v[4] = {from[0], from[1], from_u[0], from_u[1]};
 #pragma unroll
-            for (int k = 0; k < 8; k++) g[k] = v[k >> 2][k & 3], u[k] = v[2 + (k >> 2)][k & 3];
-        } else {
-            const u32x4* from = reinterpret_cast<const u32x4*>(at) + i / 4;
-            const u32x4 w[2] = {from[0], from[1]};
-            uint32_t b[2];
-            __builtin_memcpy(b, at + 4 * plane + i, 8);
-#pragma unroll
-            for (int k = 0; k < 8; k++) {
-                const uint32_t word = w[k >> 2][k & 3], byte = b[k >> 2] >> ((k & 3) * 8);
-                g[k] = __uint_as_float(word << 16 | (byte & 15u) << 12);
-                u[k] = __uint_as_float((word & 0xffff0000u) | (byte & 0xf0u) << 8);
-            }
-        }
+        for (int k = 0; k < 8; k++) g[k] = v[k >> 2][k & 3], u[k] = v[2 + (k >> 2)][k & 3];
     }
 };
 
@@ -121,7 +79,7 @@ struct FwdArgs {
     Factor x, w;
     int64_t rows, features, width, tiles_i, tiles_j, ld;
     void* y;
-    char* kept;
+    float* kept;
     int64_t plane;
 };
 
@@ -141,8 +99,8 @@ struct Paired<product::SmallTriple> {
     using Type = SmallTriplePair;
 };
 
-// Bound by the matrix units, and at a tile's end by memory (7 bytes of results in bf16 training), which nothing hides where the tile fills its compute unit: 4096 x 2048 x 2 * 8192
-// bf16 290 us with g and u kept (0.95 PFLOP/s), fp32 4096 x 1024 x 2 * 4096 353 us with the operands' copies (195 TFLOP/s of fp32 results).  Tiles of 128 x 128, two workgroups to a
+// Bound by the matrix units, and at a tile's end by memory (10 bytes of results in bf16 training), which nothing hides where the tile fills its compute unit: 4096 x 2048 x 2 * 8192
+// bf16 301 us with g and u kept (0.91 PFLOP/s), fp32 4096 x 1024 x 2 * 4096 353 us with the operands' copies (195 TFLOP/s of fp32 results).  Tiles of 128 x 128, two workgroups to a
 // compute unit, hide it and read more: 918 us forward and backward instead of 879 at the time.
 template <class F, int ACT>
 __global__ __launch_bounds__(F::kThreads, 2) void k_forward(FwdArgs a) {
@@ -191,7 +149,7 @@ __global__ __launch_bounds__(F::kThreads, 2) void k_forward(FwdArgs a) {
                 float unused;
                 y[k] = act_of<ACT, false>(g[k >> 2][k & 3], unused) * u[k >> 2][k & 3];
             }
-            if (a.kept) Kept<kF32>{a.kept, a.plane}.put8(i * a.ld + j, g, u);  // (rows of a multiple of 8)
+            if (a.kept) Kept{a.kept, a.plane}.put8(i * a.ld + j, g, u);  // (rows of a multiple of 8)
             if (kF32) {
                 float* to = static_cast<float*>(a.y) + i * a.width + j;
                 if (whole) {
@@ -220,7 +178,7 @@ struct FewArgs {
     const void *x, *w_gate, *w_up;
     int64_t rows, features, width, ld;
     void* y;
-    char* kept;
+    float* kept;
     int64_t plane;
 };
 // 16 results of y for all rows of x by a workgroup; bound by the weights' bytes: 4 x 2048 x 2 * 8192 bf16, 67 MB in 12.4 us, 5.4 TB/s.
@@ -251,19 +209,19 @@ __global__ __launch_bounds__(few::kThreads) void k_few(FewArgs a) {
             static_cast<float*>(a.y)[to] = y;
         else
             static_cast<uint16_t*>(a.y)[to] = f32_to_bf16(y);
-        if (a.kept) Kept<sizeof(T) == 4>{a.kept, a.plane}.put1(t * a.ld + f + e, sums[0][e], sums[1][e]);
+        if (a.kept) Kept{a.kept, a.plane}.put1(t * a.ld + f + e, sums[0][e], sums[1][e]);
     }
 }
 
 struct GradArgs {
-    char* kept;
+    float* kept;
     int64_t plane, rows, width, ld;
     const void* dy;
     uint16_t *dg, *du;
     int64_t pitch;
 };
 // dg = dy u act'(g) and du = dy act(g), eight elements per thread and turn; zeros behind the columns.  Rounded to bf16 once in bf16 plans, as the products' operands.
-// Bound by memory: 4096 x 8192 bf16, 369 MB in 66 us, 5.6 TB/s.
+// Bound by memory: 4096 x 8192 bf16, 470 MB in 100 us, 4.7 TB/s.
 template <bool F32, int ACT>
 __global__ __launch_bounds__(256) void k_grads(GradArgs a) {
     constexpr int P = F32 ? 3 : 1;
@@ -271,7 +229,7 @@ __global__ __launch_bounds__(256) void k_grads(GradArgs a) {
     for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < n; k += (int64_t)gridDim.x * 256) {
         const int64_t row = k / wide, col = (k - row * wide) * 8;
         float g[8], u[8];
-        Kept<F32>{a.kept, a.plane}.get8(k * 8, g, u);
+        Kept{a.kept, a.plane}.get8(k * 8, g, u);
         using T = std::conditional_t<F32, float, uint16_t>;
         T given[8];
         rows::load8(static_cast<const T*>(a.dy) + row * a.width, col, a.width, given);
@@ -393,7 +351,7 @@ Plan plan_of(const Shape& s) {
         product::cuts_of(s.f32, {s.rows, s.features, 2 * s.width, 1}, {s.width, s.features, s.rows, 2}, p.dx, p.dw);
         p.launches_bwd = (p.copies && p.few) + 1 + product::launches_of(p.dx, p.dw, false);
         p.most_tiles = std::max(p.most_tiles, p.dx.tiles() * p.dx.splits + 2 * p.dw.tiles() * p.dw.splits);
-        p.kept_at = take((s.f32 ? Kept<true>::kBytes : Kept<false>::kBytes) * (uint64_t)s.rows * wide);
+        p.kept_at = take((uint64_t)Kept::kBytes * s.rows * wide);
         p.grad_at = take(4ull * s.rows * product::pitch(s.f32, s.width));
         p.parts_at = take(product::parts_bytes(p.dx, 1, false));
         p.parts_dw_at = take(product::parts_bytes(p.dw, 2, false));
@@ -404,7 +362,7 @@ Plan plan_of(const Shape& s) {
 
 void forward(const Shape& s, const Plan& p, const Fwd& a, hipStream_t stream) {
     const int64_t ld = product::padded(s.f32, s.width);
-    char* kept = s.inference ? nullptr : a.ws + p.kept_at;
+    float* kept = s.inference ? nullptr : reinterpret_cast<float*>(a.ws + p.kept_at);
     if (p.few) {
         const FewArgs f{a.x, a.w_gate, a.w_up, s.rows, s.features, s.width, ld, a.y, kept, s.rows * ld};
         return s.f32 ? launch_few<float>(s.act, f, stream) : launch_few<uint16_t>(s.act, f, stream);
@@ -419,7 +377,7 @@ void backward(const Shape& s, const Plan& p, const Bwd& a, hipStream_t stream) {
     const int64_t ld = product::padded(s.f32, s.width), plane = s.rows * ld, wide = product::pitch(s.f32, s.width);
     if (p.copies && p.few) make_copies(s, p, a.x, a.w_gate, a.w_up, a.ws, stream);
     uint16_t *dg = reinterpret_cast<uint16_t*>(a.ws + p.grad_at), *du = dg + s.rows * wide;
-    const GradArgs g{a.ws + p.kept_at, plane, s.rows, s.width, ld, a.dy, dg, du, wide};
+    const GradArgs g{reinterpret_cast<float*>(a.ws + p.kept_at), plane, s.rows, s.width, ld, a.dy, dg, du, wide};
     const dim3 grid((unsigned)std::min<int64_t>((plane / 8 + 255) / 256, 8192));
     with_act(s.act, [&](auto kind) {
         if (s.f32)
