@@ -1,5 +1,5 @@
 /* C ABI: log probabilities of given tokens with the entropy of their distributions, straight from features and the head's weight, and the
- * gradients of both: the loss of a head with many classes whose logits (rows x classes) are not kept.
+ * gradients of both: the loss of a head with many classes whose logits (rows x classes) are no tensor of the step.
  *
  * x [rows, features], W [classes, features].  With z_i = inv_temperature * (x . W_i) over the classes that the mask allows:
  *
@@ -8,8 +8,9 @@
  *   dx = sum_i dlogit_i W_i,  dW_i = sum over the rows of dlogit_i x
  *
  * as canvas_logprob.h has them for logits that are at hand.  Forward keeps the largest logit and the sums of each row; backward takes the
- * classes a piece at a time, computes a piece's logits again, the same ones, and leaves its gradients in the workspace only.  (Where that is faster, forward
- * leaves logits in the workspace, in fp32: those of few rows, and up to a GiB of others.)
+ * classes a piece at a time, computes a piece's logits again, the same ones, and leaves its gradients (up to 288 MB of pieces of 256 classes and more) in the
+ * workspace only.  Some logits are not computed again but left there by forward, in fp32: those of few rows (up to 32; in fp32 plans of any number that takes the same
+ * way, 512 MB at most), all where they are 16 MB or less, and of plans with 2048 features or more (fp32: 512) those of the first pieces, up to a GiB.
  *
  * A masked class is not looked at (its row of W may be NaN) and has a gradient of zeros.  A row of x that has nothing left (all classes masked
  * or -inf) has the log probability -inf, the entropy 0 and a gradient of zeros.  A token that is no class (negative, say, for positions

@@ -501,12 +501,13 @@ __global__ __launch_bounds__(256) void k_few_grads(FewGradArgs a) {
 // 64, 128, 300, 600 MB, us: 4096 x 1024 x 32768 (268 MB in all) 1138, 1029, 1014, 1014; 8192 x 512 x 16000 (262) 729, 678, 624, 624;
 // 8192 x 1024 x 32768 (537) -, 2114, 1982, 2021; 4096 x 2048 x 65536 (537) -, 3610, 3672, 3704.
 constexpr uint64_t kPieceBytes = 288u << 20;
-// Logits that forward leaves for backward, a tile as its workgroup holds it: those of the first pieces, up to a GiB.  To write and read them is memory's work, to compute them again the matrix
-// units', which is more with many features, and in fp32.  Both ways with the logits and with their computing again, us: 4096 x 4096 x 32768 2872 and 3513; 4096 x 2048 x 65536 3236 and 3712;
-// 4096 x 1024 x 32768 995 and 1018; 4000 x 512 x 16000 385 and 355; fp32 4000 x 1000 x 30000 4300 and 5360; 8000 x 200 x 16000 1586 and 1684; 2000 x 128 x 20000 434 and 430;
-// 4000 x 64 x 10000 375 and 349.  In the L2s: 256 x 512 x 1000 26 and 28; 250 x 256 x 2000 28 and 29; fp32 256 x 512 x 1000 42 and 48; 1000 x 100 x 2000 48 and 50.
+// Logits that forward leaves for backward, a tile as its workgroup holds it: those of the first pieces, up to a GiB, where to compute them again takes about an eighth longer and more.  To write and
+// read them is memory's work, to compute them again the matrix units', which is more with many features, and in fp32.  Both ways with the logits and with their computing again, us:
+// 4096 x 4096 x 32768 2885 and 3640; 4096 x 2048 x 65536 3249 and 3711; 1000 x 2048 x 10000 197 and 225; fp32 4000 x 1000 x 30000 4350 and 5295; 2000 x 512 x 20000 862 and 1015.  Less is not worth their
+// memory: 4096 x 1536 x 32768 1432 and 1559; 4096 x 1024 x 32768 997 and 1025, with 961 MB of workspace and 424; fp32 8000 x 300 x 16000 2050 and 2274; 4000 x 256 x 16000 860 and 919.
+// In the L2s: 256 x 512 x 1000 26 and 28; 250 x 256 x 2000 28 and 29; fp32 256 x 512 x 1000 42 and 48; 1000 x 100 x 2000 48 and 50.
 constexpr uint64_t kKeptBytes = 1u << 30, kNearBytes = 16u << 20;
-int64_t kept_from(bool f32, uint64_t bytes) { return bytes <= kNearBytes ? (f32 ? 1 : 256) : f32 ? 192 : 1024; }
+int64_t kept_from(bool f32, uint64_t bytes) { return bytes <= kNearBytes ? (f32 ? 1 : 256) : f32 ? 512 : 2048; }
 uint64_t up256(uint64_t v) { return (v + 255) & ~(uint64_t)255; }
 
 template <class T>
