@@ -3,12 +3,13 @@
  *
  *   norm = (sum of the squares of all elements of all tensors)^(1/2)
  *   scale = min(1, max_norm / norm)                 (1 for a norm of zero)
- *   out_i = scale * grad_i                          element by element, rounded once to out_i's type
+ *   out_i = scale * grad_i                          element by element
  *
  * Squares are added in 64 bits: gradients of any size that their types hold are in range (a norm that fp32 does not hold is written as
- * infinity, the scale is right all the same).  NaN among the elements makes norm, scale and all
- * of out NaN.  An infinity makes the norm infinite and the scale 0: finite elements become 0, infinite ones NaN.  max_norm = infinity asks
- * for the norm and, where a tensor's types differ, for its conversion.  Deterministic: no atomics, sums in a fixed order.
+ * infinity, the scale is right all the same).  The scale is rounded to fp32 and so is its product with an element, which is rounded again where out_i is bf16; scales
+ * below fp32's normal numbers are taken in 64 bits.  NaN among the elements makes norm, scale and all of out NaN.  An infinity makes the norm infinite and the scale 0: finite
+ * elements become 0, infinite ones NaN.  max_norm = infinity asks for the norm and, where a tensor's types differ, for its conversion: the scale is 1 whatever the norm, and
+ * every element stays what it is, NaN and infinities too; the norm tells of them.  Deterministic: no atomics, sums in a fixed order.
  *
  * Pointers: device pointers, owned by the caller, aligned to their element (16-byte aligned ones are read in whole vectors).  out_i may be
  * grad_i itself where both have one type; apart from that, what a call writes must not share bytes with anything else that it reads or writes

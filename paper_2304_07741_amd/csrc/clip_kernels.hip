@@ -140,10 +140,10 @@ __device__ __forceinline__ double norm_of(const double* parts, int n) {
     for (int k = threadIdx.x; k < n; k += kThreads) t += parts[k];
     return sqrt(over_threads(t));
 }
-// (NaN stays; a largest norm of infinity asks for no scaling)
+// (NaN stays; a largest norm of infinity asks for no scaling, whatever the norm)
 __device__ __forceinline__ double scale_of(double norm, double most) {
     const double r = norm > 0 || norm != norm ? most / norm : 1.0;
-    return most > 1.7e308 || r >= 1.0 ? 1.0 : r;
+    return most == __builtin_inf() || r >= 1.0 ? 1.0 : r;
 }
 __global__ __launch_bounds__(kThreads) void k_norm(const double* parts, int n, double most, double* kept, float* norm, float* scale) {
     const double t = norm_of(parts, n);
