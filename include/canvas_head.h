@@ -43,10 +43,11 @@ extern "C" {
 typedef struct canvas_head canvas_head;
 
 typedef struct canvas_head_info {
-    int32_t n_launches_fwd, n_launches_bwd; /* kernels enqueued per call */
-    int32_t pieces, reserved0;              /* how many pieces backward takes the classes in */
+    int32_t n_launches_fwd, n_launches_bwd; /* kernels enqueued per call, without a mask */
+    int32_t pieces;                         /* how many pieces backward takes the classes in */
+    int32_t n_launches_bwd_mask;            /* as many more with one: copies of a weight that is otherwise read as it is */
     uint64_t workspace_bytes;               /* the rows' sums, a piece's dlogit, copies of operands, parts of sums, some logits */
-    double flops_fwd, flops_bwd;            /* of the products above; backward computes the logits again */
+    double flops_fwd, flops_bwd;            /* of the products above; backward's with those of the logits that it computes again */
     double min_bytes_fwd, min_bytes_bwd;    /* every tensor of a call read or written once; without a mask */
 } canvas_head_info;
 

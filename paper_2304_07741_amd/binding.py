@@ -101,8 +101,8 @@ class CanvasGatedInfo(ctypes.Structure):
 
 
 class CanvasHeadInfo(ctypes.Structure):
-    _fields_ = [("n_launches_fwd", ctypes.c_int32), ("n_launches_bwd", ctypes.c_int32), ("pieces", ctypes.c_int32), ("reserved0", ctypes.c_int32),
-                ("workspace_bytes", ctypes.c_uint64), ("flops_fwd", ctypes.c_double), ("flops_bwd", ctypes.c_double),
+    _fields_ = [("n_launches_fwd", ctypes.c_int32), ("n_launches_bwd", ctypes.c_int32), ("pieces", ctypes.c_int32),
+                ("n_launches_bwd_mask", ctypes.c_int32), ("workspace_bytes", ctypes.c_uint64), ("flops_fwd", ctypes.c_double), ("flops_bwd", ctypes.c_double),
                 ("min_bytes_fwd", ctypes.c_double), ("min_bytes_bwd", ctypes.c_double)]
 
 

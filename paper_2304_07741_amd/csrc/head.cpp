@@ -49,13 +49,14 @@ int canvas_head_compile(int64_t rows, int64_t features, int64_t classes, canvas_
         canvas_head_info& I = h->info;
         I.n_launches_fwd = h->plan.launches_fwd;
         I.n_launches_bwd = h->plan.launches_bwd;
+        I.n_launches_bwd_mask = h->plan.launches_mask;
         I.pieces = s.inference ? 0 : h->plan.pieces;
         I.workspace_bytes = h->plan.workspace_bytes;
         const double t = (double)rows, c = (double)features, v = (double)classes, e = s.f32 ? 4 : 2;
         I.flops_fwd = 2 * t * c * v;
         I.min_bytes_fwd = e * (t * c + v * c) + 16 * t;
         if (!s.inference) {
-            I.flops_bwd = 6 * t * c * v;
+            I.flops_bwd = 4 * t * c * v + 2 * t * c * (double)h->plan.again;
             I.min_bytes_bwd = 2 * e * (t * c + v * c) + 16 * t;
         }
         *out = h.release();

@@ -583,6 +583,8 @@ Plan plan_of(const Shape& s) {
         product::cuts_of(s.f32, {s.rows, s.features, p.length, 1}, {p.length, s.features, s.rows, 1}, p.dx, p.dw);
         if (!p.copies) p.copy_at[1] = take(2ull * p.length * ld);
         p.launches_bwd = 1 + (p.copies && p.few) + p.pieces + (p.pieces - 1) * product::launches_of(product::Cut{p.dx.side}, p.dw, false) + product::launches_of(p.dx, p.dw, p.pieces > 1);
+        p.launches_mask = p.copies ? 0 : p.pieces;
+        p.again = p.few ? 0 : s.classes - std::min(s.classes, p.kept * p.length);
         p.most_tiles = std::max({p.most_tiles, p.piece.tiles(), p.dx.tiles() * p.dx.splits + p.dw.tiles() * p.dw.splits});
         p.grad_at = take(2ull * s.rows * product::pitch(s.f32, p.length));
         p.parts_dx_at = take(product::parts_bytes(p.dx, 1, p.pieces > 1));

@@ -35,6 +35,8 @@ struct Plan {
     int pieces = 1;
     int64_t length = 0;                  // of a piece
     int launches_fwd = 0, launches_bwd = 0;
+    int launches_mask = 0;               // more of backward with a mask
+    int64_t again = 0;                   // classes whose logits backward computes
     uint64_t rows_at = 0, sums_at = 0, token_at = 0, copy_at[2] = {}, slope_at = 0, grad_at = 0, logits_at = 0, parts_dx_at = 0, parts_dw_at = 0, workspace_bytes = 0;
     int64_t most_tiles = 0;
 };
