@@ -149,6 +149,10 @@ def _check_last(passed, given):
         raise ValueError("not the arguments of this runner's last forward()")
 
 
+# (no part of torch's interface, so it may be missing; current_device() takes 0.3 us longer)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 class _PlanRunner:
     """One compiled plan, its workspace and the buffers it writes; close() releases the plan."""
 
@@ -162,6 +166,13 @@ class _PlanRunner:
             self.device = torch.device(self.device.type, torch.cuda.current_device())
         self.tdtype = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
         self.cdtype = B.CANVAS_BF16 if dtype == "bf16" else B.CANVAS_F32
+
+    def _call(self, f, *args):
+        """On the runner's device, on torch's current stream of it, whichever device is the current one."""
+        if _current_device() == self.device.index:
+            return f(*args)
+        with torch.cuda.device(self.device):
+            return f(*args)
 
     def _workspace(self, n):
         return torch.empty(max(16, int(n)), dtype=torch.uint8, device=self.device)
@@ -230,7 +241,7 @@ class NormRunner(_PlanRunner):
     def forward(self, x, z=None, gate=None, w_post=None, scale=None, w_pre=None):
         self._of_the_block(z, gate, w_post, scale, w_pre)
         self._map("x", x)
-        B.canvas_norm_forward(self.handle, x, z, gate, w_post, scale, w_pre, self.out.get("x_out"), self.out.get("u"), self.ws)
+        self._call(B.canvas_norm_forward, self.handle, x, z, gate, w_post, scale, w_pre, self.out.get("x_out"), self.out.get("u"), self.ws)
         self.x, self.passed = x, self.out["x_out"] if self.post else x
         if not (self.post and self.grads):
             return self.out
@@ -249,8 +260,8 @@ class NormRunner(_PlanRunner):
         if dx_out is not None or not self.pre:
             self._map("dx_out", dx_out)
         g = self.grads
-        B.canvas_norm_backward(self.handle, self.x, z, gate, w_post, scale, w_pre, dx_out, du, g.get("dx"), g.get("dz"), g.get("dgate"),
-                               g.get("dw_post"), g.get("dscale"), g.get("dw_pre"), self.ws)
+        self._call(B.canvas_norm_backward, self.handle, self.x, z, gate, w_post, scale, w_pre, dx_out, du, g.get("dx"), g.get("dz"), g.get("dgate"),
+                   g.get("dw_post"), g.get("dscale"), g.get("dw_pre"), self.ws)
         return g
 
 
@@ -290,8 +301,8 @@ class LogprobRunner(_PlanRunner):
     def forward(self, logits, tokens, mask=None, inv_temperature=1.0):
         pitch, mask_pitch = self._arguments(logits, tokens, mask)
         o = self.out
-        B.canvas_logprob_forward(self.handle, logits, pitch, inv_temperature, mask, mask_pitch, tokens, o["logprob"], o["entropy"],
-                                 o.get("top_logprob"), o.get("top_index"), self.ws)
+        self._call(B.canvas_logprob_forward, self.handle, logits, pitch, inv_temperature, mask, mask_pitch, tokens, o["logprob"], o["entropy"],
+                   o.get("top_logprob"), o.get("top_index"), self.ws)
         return o
 
     def backward(self, logits, tokens, dlogprob=None, dentropy=None, mask=None, inv_temperature=1.0):
@@ -299,8 +310,8 @@ class LogprobRunner(_PlanRunner):
         for name, t in (("dlogprob", dlogprob), ("dentropy", dentropy)):
             if t is not None:
                 _check_tensor(name, t, (self.rows,), torch.float32, self.device)
-        B.canvas_logprob_backward(self.handle, logits, pitch, inv_temperature, mask, mask_pitch, tokens, dlogprob, dentropy,
-                                  self.grads["dlogits"], self.classes, self.ws)
+        self._call(B.canvas_logprob_backward, self.handle, logits, pitch, inv_temperature, mask, mask_pitch, tokens, dlogprob, dentropy,
+                   self.grads["dlogits"], self.classes, self.ws)
         return self.grads
 
 
@@ -336,7 +347,7 @@ class OrthoRunner(_PlanRunner):
         if master is not None:
             w, p = self._buffer("master", torch.float32), self._buffer("weights")
             names += ["master", "weights"]
-        B.canvas_ortho_step(self.handle, grad, momentum, m, mu, master, w, lr, decay, p, self.out["update"], self.ws)
+        self._call(B.canvas_ortho_step, self.handle, grad, momentum, m, mu, master, w, lr, decay, p, self.out["update"], self.ws)
         return {k: self.out[k] for k in names}
 
 
@@ -368,7 +379,7 @@ class GatedRunner(_PlanRunner):
 
     def forward(self, x, w_gate, w_up):
         self._arguments(x, w_gate, w_up)
-        B.canvas_gated_forward(self.handle, x, w_gate, w_up, self.out["y"], self.ws)
+        self._call(B.canvas_gated_forward, self.handle, x, w_gate, w_up, self.out["y"], self.ws)
         self.passed = (x, w_gate, w_up)
         return self.out
 
@@ -377,7 +388,7 @@ class GatedRunner(_PlanRunner):
         _check_last(self.passed, (x, w_gate, w_up))
         _check_tensor("dy", dy, self.out["y"].shape, self.tdtype, self.device)
         g = self.grads
-        B.canvas_gated_backward(self.handle, x, w_gate, w_up, dy, g.get("dx"), g.get("dw_gate"), g.get("dw_up"), self.ws)
+        self._call(B.canvas_gated_backward, self.handle, x, w_gate, w_up, dy, g.get("dx"), g.get("dw_gate"), g.get("dw_up"), self.ws)
         return g
 
 
@@ -411,7 +422,7 @@ class HeadRunner(_PlanRunner):
 
     def forward(self, x, weight, tokens, mask=None, inv_temperature=1.0):
         self._arguments(x, weight, tokens, mask)
-        B.canvas_head_forward(self.handle, x, weight, inv_temperature, mask, tokens, self.out["logprob"], self.out["entropy"], self.ws)
+        self._call(B.canvas_head_forward, self.handle, x, weight, inv_temperature, mask, tokens, self.out["logprob"], self.out["entropy"], self.ws)
         self.passed = (x, weight, mask, inv_temperature)
         return self.out
 
@@ -422,7 +433,7 @@ class HeadRunner(_PlanRunner):
             if t is not None:
                 _check_tensor(name, t, (self.rows,), torch.float32, self.device)
         g = self.grads
-        B.canvas_head_backward(self.handle, x, weight, inv_temperature, mask, tokens, dlogprob, dentropy, g.get("dx"), g.get("dweight"), self.ws)
+        self._call(B.canvas_head_backward, self.handle, x, weight, inv_temperature, mask, tokens, dlogprob, dentropy, g.get("dx"), g.get("dweight"), self.ws)
         return g
 
 
@@ -460,7 +471,7 @@ class ClipRunner(_PlanRunner):
             if self.outs is None:
                 self.outs = [self._empty(s, d) for s, d in zip(self.shapes, self.out_dtypes)]
             outs = self.outs
-        B.canvas_clip_step(self.handle, grads, outs, max_norm, self.norm, self.scale, self.ws)
+        self._call(B.canvas_clip_step, self.handle, grads, outs, max_norm, self.norm, self.scale, self.ws)
         return {"norm": self.norm, "scale": self.scale, "grads": list(outs)}
 
 
