@@ -15,8 +15,9 @@
  * A masked class is not looked at (its row of W may be NaN) and has a gradient of zeros.  A row of x that has nothing left (all classes masked
  * or -inf) has the log probability -inf, the entropy 0 and a gradient of zeros.  A token that is no class (negative, say, for positions
  * without a target) has the log probability 0 and adds nothing to the gradient: without dentropy such a row of x may be NaN, and its gradient
- * is zero.  A masked token has the log probability -inf.  NaN or +inf among the allowed logits makes log probability, entropy and gradients
- * of its row NaN, and dW with them.
+ * is zero.  So it is of any row whose dlogprob and dentropy are zero or not given.  A masked token has the log probability -inf.  NaN or +inf among the allowed logits makes
+ * log probability, entropy and gradients of its row NaN, and dW with them.  dx is a sum over all allowed classes: NaN or an infinity in one's row of W makes the same element
+ * of dx NaN in every row, those without a gradient among them (zero times it is NaN).
  *
  * All sums are fp32.  bf16 plans: dlogit is rounded to bf16 once, as the operand of the products behind it; dx and dW are fp32 sums rounded
  * once.  fp32 plans: products are those of fp32, or, of larger operands, each is taken as three bf16 numbers that together hold its 24 bits (smaller ones than 2^-100

@@ -53,3 +53,31 @@ def test_backward_after_one_of_other_rows(shape, dtype):
         again = r.backward(x, w, some, a, None, mask=mask)
         assert torch.equal(again["dx"], first["dx"]) and torch.equal(again["dweight"], first["dweight"])
     r.close()
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("-inf")])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [9, 150])
+def test_an_allowed_class_that_is_not_finite(rows, dtype, value):
+    """One element of a weight: zero times it is NaN in that element of dx, of rows without a gradient too, and of no other element where the logits stay numbers."""
+    x, w, tokens, _, a, _ = _case(rows, 40, 300, dtype, 4, False)
+    x, tokens[0] = x.abs() + 0.5, 7                        # (logits of -inf, not of +inf)
+    tokens[tokens == 5] = 6
+    w[5, 3] = value
+    got = _run(x, w, tokens, None, a, None, dtype)
+    assert bool(torch.isnan(got["dx"][:, 3]).all())
+    if value == value and dtype == "bf16":
+        keep = torch.arange(40, device="cuda") != 3
+        assert bool(torch.isfinite(got["logprob"]).all()) and bool(torch.isfinite(got["dx"][:, keep]).all()) and bool(torch.isfinite(got["dweight"]).all())
+        assert not got["dweight"][5].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [9, 150])
+def test_rows_whose_gradients_are_zero_may_be_nan(rows, dtype):
+    x, w, tokens, mask, a, b = _case(rows, 40, 300, dtype, 4, True)
+    a[::3], b[::3] = 0, 0
+    want = _run(x, w, tokens, mask, a, b, dtype)
+    x[::3] = float("nan")
+    got = _run(x, w, tokens, mask, a, b, dtype)
+    assert not want["dx"][::3].any() and torch.equal(got["dx"], want["dx"]) and torch.equal(got["dweight"], want["dweight"])
