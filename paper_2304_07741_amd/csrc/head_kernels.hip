@@ -113,7 +113,7 @@ __device__ __forceinline__ Sums sums_of(const float (&z)[N], float it) {
 }
 
 // Bound by the matrix units; a tile's exponentials, and the logits that are kept, are not hidden by another tile where one fills its compute unit.
-// 4096 x 1024 x 32768 bf16: 264 us (1.04 PFLOP/s), 315 with 537 MB of logits kept; 1500 x 1000 x 50021 170 us, 4.6 rounds of tiles of 256.  (With a branch
+// 4096 x 1024 x 32768 bf16: 272 us (1.01 PFLOP/s), 315 with 537 MB of logits kept; 4096 x 4096 x 32768, which keeps them, 914 (1.2); 1500 x 1000 x 50021 170 us, 4.6 rounds of tiles of 256.  (With a branch
 // per register for the token's logit instead of selections 345.)
 template <class F>
 __global__ __launch_bounds__(F::kThreads, 2) void k_logits(FwdArgs a) {
@@ -334,8 +334,8 @@ struct GradArgs {
     int64_t ld, wide;
     f32x4* kept;                   // the piece's logits, where forward has left them
 };
-// The gradients of a tile of logits.  4096 x 1024 x 32768 bf16: 187 us from kept logits (805 MB, 4.3 TB/s: one workgroup to a compute unit reads, computes and writes in turn), 279 with their
-// product, of which the matrix units are the bound.
+// The gradients of a tile of logits.  4096 x 32768 of them in bf16 plans: 172 us from kept logits (805 MB, 4.7 TB/s: one workgroup to a compute unit reads, computes and writes in turn), 289 with their
+// product over 1024 features, of which the matrix units are the bound.
 template <class F, bool KEPT>
 __global__ __launch_bounds__(F::kThreads, 2) void k_grads(GradArgs a) {
     constexpr int TM = F::TM, TN = F::TN, P = F::PLANES, kHalf = F::BN / 2;
